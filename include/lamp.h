@@ -192,6 +192,128 @@ lamp_status_t lamp_instnorm_relu_bwd(const lamp_tensor_t *dz_a, const lamp_tenso
                                      double *sums, lamp_tensor_t *dy, void *cuda_stream);
 
 /* ------------------------------------------------------------------------
+ * Channel-mixing (pointwise) layers in 8 bits.  No passage of the paper: they stand beside the dense bf16 convolutions
+ * for the 1x1x1 layers of a network (bottleneck, head, the linear layers of a token block over the voxels).
+ * An operand of the matrix product is a matrix [rows][k], k being the axis the product sums over:
+ *   element (r, j) = e4m3 code q[r * q_pitch + j]  times  scale[(j / 128) * scale_pitch + r]           (tile_scale = 0)
+ *                                                   or  scale[(j / 128) * scale_pitch + r / 128]     (tile_scale = 1)
+ * The scales are block-major, so that the 128 scales a tile of rows needs are one contiguous line.
+ * q 16-byte aligned, q_pitch (bytes) a multiple of 16 and >= k; bytes behind k are neither read nor written.
+ * scale 4-byte aligned, scale_pitch >= rows (tile_scale = 0) or >= ceil(rows / 128).  rows, k < 2^31.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+    void   *q;
+    int64_t q_pitch;
+    float  *scale;
+    int64_t scale_pitch;
+    int64_t rows, k;
+    int32_t tile_scale;
+} lamp_fp8_operand_t;
+
+/* Quantises x (bf16 or fp32, any channel slice) into `out`.
+ * transpose = 0: rows = voxels of x (n*d*h*w), k = channels - the operand of y = x W^T and its data gradient.
+ * transpose = 1: rows = channels, k = voxels - the operands of a weight gradient, and (tile_scale) the transposed weights
+ *                of a data gradient (codes and scales are then those of transpose = 0, transposed).
+ * Per block of 128 along k (and of 128 rows when tile_scale): amax = the largest finite |x|, at least 2^-100;
+ * scale = amax * (1/448) and code = round-to-nearest-even(x * (448 / amax)), each operation in fp32.  Elements that are
+ * not finite become the NaN code.  c, c_pitch and c_offset are multiples of 8. */
+lamp_status_t lamp_fp8_quantize(const lamp_tensor_t *x, int32_t transpose, const lamp_fp8_operand_t *out, void *cuda_stream);
+
+/* y[m][n] = bias[n] + sum_k a(m, k) * b(n, k), m = 0 .. a->rows - 1 (the voxels of y, n*d*h*w of them), n = 0 .. b->rows - 1
+ * (the channels of y).  The products of one block of 128 are summed on the tensor cores, the blocks in fp32 with
+ * their scales: y = bias + sum_blocks (sum_block qa qb) * sa * sb.  sa * sb must be finite in fp32.
+ * y: bf16 or fp32, any c, c_pitch and c_offset.  bias: fp32 [n] or NULL.  The sum runs in a fixed order (results repeat
+ * bit for bit).  No workspace: where few tiles would leave SMs idle, the CTAs of a cluster share the k axis of a tile and
+ * add their parts through distributed shared memory. */
+lamp_status_t lamp_gemm_fp8(const lamp_fp8_operand_t *a, const lamp_fp8_operand_t *b, const float *bias, lamp_tensor_t *y,
+                            void *cuda_stream);
+
+/* ------------------------------------------------------------------------
+ * Norms around a residual block over the channels of each voxel, fused with the block's gate, residual scale and sum.
+ * No passage of the paper (its blocks use InstanceNorm, above); the gate per sample and channel has the form of the
+ * squeeze-and-excitation step's e[n][c].  With y = the output of a block's last layer, x = the block's input:
+ *     t = x + r[c] * g * N_post(y),     h = N_pre(t),
+ *     N(v) = (v - mean) / sqrt(var + eps) * w[c] + b[c]   over the c channels of a voxel (biased variance), or with
+ *     rms = 1:  v / sqrt(mean(v^2) + eps) * w[c] + b[c].
+ * h is the input of the NEXT block, so one pass serves the end of one block and the start of the next; h is the norm of
+ * t as stored (rounded to the type of out), which is what the backward pass reads.
+ * Arithmetic in fp32, mean and variance in two passes over the row.
+ * w, b, res_scale: fp32 [c] or NULL (1, 0, 1).  g = gate[n][c] (fp32), or sigmoid(gate_logits) per element, or 1 (both NULL).
+ * Types: x, out and the gradients of them share one type, y, h, gate_logits and their gradients another; (bf16, bf16),
+ * (fp32, bf16) or (fp32, fp32).  All tensors have the same n, d, h, w, c; c, c_pitch and c_offset are multiples of 8 and
+ * c <= 8192.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+    int32_t rms;
+    float   eps;                          /* >= 0 */
+    const float *post_w, *post_b;
+    const float *pre_w, *pre_b;
+    const float *gate;
+    const lamp_tensor_t *gate_logits;
+    const float *res_scale;
+} lamp_block_norm_t;
+
+/* y == NULL: t = x (the norm in front of the first block; out must be NULL).  h and h_fp8 may each be NULL; out may be x
+ * (the same view), and is required when y is given.  h_fp8 (tile_scale = 0, rows = n*d*h*w, k = c) receives h in 8 bits,
+ * quantised from fp32 as lamp_fp8_quantize does, ready to be an operand of lamp_gemm_fp8. */
+lamp_status_t lamp_block_norm_fwd(const lamp_block_norm_t *p, const lamp_tensor_t *y, const lamp_tensor_t *x, lamp_tensor_t *out,
+                                  lamp_tensor_t *h, const lamp_fp8_operand_t *h_fp8, void *cuda_stream);
+
+/* Gradients of the parameters, fp32 [c] (gate: [n][c]); each may be NULL. */
+typedef struct {
+    float *post_w, *post_b, *pre_w, *pre_b, *gate, *res_scale;
+} lamp_block_norm_grads_t;
+
+/* t: the stored sum (x when y is NULL).  dout: the gradient that reaches t past the next block, or NULL for none; dh: the
+ * gradient of h, or NULL for none (one of the two is required).
+ *     dt = dout + dN_pre(dh),  dx = dt,  dy = dN_post(dt * r * g),  dgate_logits = dt * r * N_post(y) * g (1 - g).
+ * dx may be dout (the same view).  y, dy and dgate_logits are NULL together when there is no post-norm (dgate_logits also
+ * when there are no logits).  Sums over voxels run in a fixed order.  The workspace needs
+ * lamp_block_norm_bwd_workspace_bytes, which is 0 when no member of grads is asked for (grads itself may be NULL). */
+size_t        lamp_block_norm_bwd_workspace_bytes(const lamp_tensor_t *t, const lamp_block_norm_t *p);
+lamp_status_t lamp_block_norm_bwd(const lamp_block_norm_t *p, const lamp_tensor_t *y, const lamp_tensor_t *t,
+                                  const lamp_tensor_t *dout, const lamp_tensor_t *dh, lamp_tensor_t *dx, lamp_tensor_t *dy,
+                                  lamp_tensor_t *dgate_logits, const lamp_block_norm_grads_t *grads,
+                                  void *ws, size_t ws_bytes, void *cuda_stream);
+
+/* ------------------------------------------------------------------------
+ * Distillation from a teacher's top logits: the loss that trains a narrow network on what a wide one answered, beside the
+ * softmax-Dice loss on labels.  (No passage of the paper; it trains networks of 32, 64 and 128 filters on one task.)
+ * z: the student's logits, one row of c classes per voxel (bf16 or fp32; any c, c_pitch, c_offset).  Of the teacher, k listed
+ * classes per row: index idx[row][k] and logit logits[row][k] (fp32).  With T = temperature,
+ *     p_j = exp(logits_j / T - lse),  lse = log sum_j exp(logits_j / T) over the listed classes, or the teacher's own log-sum
+ *           over all its classes, lse[row] (of logits / T), where the list leaves out mass that should not be spread;
+ *     q_i = exp(z_i / T) / sum_i exp(z_i / T) over all c classes;
+ *     loss_row = T^2 sum_j p_j (log p_j - log q_{idx_j}),      dloss_row / dz_i = T (q_i sum_j p_j - sum_{j: idx_j = i} p_j).
+ * Entries with idx outside [0, c) are absent; p_j = 0 contributes 0; the same class listed twice counts twice.  A row
+ * with no entry left (none listed, or all logits -inf) has loss 0 and gradient 0.  The class with z = -inf has q = 0.
+ * row_weight: fp32 [rows], or NULL for 1 / rows each.  Rows of weight 0 are not read: their loss, log-sum and gradient are 0.
+ * Sums are held in fp32 (log-sums, losses of a row) and fp64 (over rows), in a fixed order.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+    const int32_t *idx;                   /* [rows][k] */
+    const float   *logits;                /* [rows][k] */
+    const float   *lse;                   /* [rows] or NULL */
+    int32_t        k;                     /* 1 .. 1024 */
+    float          temperature;           /* > 0 */
+} lamp_teacher_topk_t;
+
+/* Scratch for `loss`; not needed where loss is NULL.  Depends on the shape of z only. */
+size_t        lamp_distill_topk_workspace_bytes(const lamp_tensor_t *z);
+/* loss_rows: fp32 [rows]; lse: fp32 [rows], log sum_i exp(z_i / T), needed by the backward call; loss: fp32 scalar
+ * sum_r row_weight[r] * loss_rows[r].  Each of the three may be NULL. */
+lamp_status_t lamp_distill_topk_fwd(const lamp_tensor_t *z, const lamp_teacher_topk_t *teacher, const float *row_weight,
+                                    float *loss_rows, float *lse, float *loss, void *ws, size_t ws_bytes, void *cuda_stream);
+/* dz = row_grad[row] * dloss_row / dz in the type of z (row_grad: fp32 [rows] or NULL for 1 / rows; rows of gradient 0 are not
+ * read).  dz may be z (the same view). */
+lamp_status_t lamp_distill_topk_bwd(const lamp_tensor_t *z, const lamp_teacher_topk_t *teacher, const float *row_grad,
+                                    const float *lse, lamp_tensor_t *dz, void *cuda_stream);
+/* Loss and gradient of sum_r row_weight[r] * loss_rows[r] in one pass over the logits.  dz may be z. */
+lamp_status_t lamp_distill_topk_fwd_bwd(const lamp_tensor_t *z, const lamp_teacher_topk_t *teacher, const float *row_weight,
+                                        float *loss_rows, float *loss, lamp_tensor_t *dz, void *ws, size_t ws_bytes,
+                                        void *cuda_stream);
+
+/* ------------------------------------------------------------------------
  * U-Net (Sec. 2.2, Eq. 2; widths per Sec. 3).
  *   encoder level l: convs_per_level x [conv 3x3x3 s1 p1 -> InstanceNorm -> ReLU]; between
  *   levels a conv 3x3x3 s2 p1 -> InstanceNorm -> ReLU; decoder level l: transposed conv 2x2x2 s2

@@ -41,6 +41,25 @@ class UNetSpec(C.Structure):
                 ("in_channels", C.c_int32), ("num_classes", C.c_int32), ("in_eps", C.c_float), ("se_ratio", C.c_int32)]
 
 
+class Fp8Operand(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("q_pitch", C.c_int64), ("scale", C.c_void_p), ("scale_pitch", C.c_int64),
+                ("rows", C.c_int64), ("k", C.c_int64), ("tile_scale", C.c_int32)]
+
+
+class BlockNorm(C.Structure):
+    _fields_ = [("rms", C.c_int32), ("eps", C.c_float), ("post_w", C.c_void_p), ("post_b", C.c_void_p), ("pre_w", C.c_void_p),
+                ("pre_b", C.c_void_p), ("gate", C.c_void_p), ("gate_logits", C.POINTER(Tensor)), ("res_scale", C.c_void_p)]
+
+
+class BlockNormGrads(C.Structure):
+    _fields_ = [("post_w", C.c_void_p), ("post_b", C.c_void_p), ("pre_w", C.c_void_p), ("pre_b", C.c_void_p),
+                ("gate", C.c_void_p), ("res_scale", C.c_void_p)]
+
+
+class TeacherTopk(C.Structure):
+    _fields_ = [("idx", C.c_void_p), ("logits", C.c_void_p), ("lse", C.c_void_p), ("k", C.c_int32), ("temperature", C.c_float)]
+
+
 _lib = None
 
 
@@ -54,6 +73,7 @@ def lib():
         vp, sz, i32, f32 = C.c_void_p, C.c_size_t, C.c_int32, C.c_float
         TP, DP, SP = C.POINTER(Tensor), C.POINTER(ConvDesc), C.POINTER(UNetSpec)
         I3 = C.POINTER(C.c_int32)
+        FP, NP, GP, KP = C.POINTER(Fp8Operand), C.POINTER(BlockNorm), C.POINTER(BlockNormGrads), C.POINTER(TeacherTopk)
         sig = {
             "lamp_conv3d_workspace_bytes": (sz, [DP, TP, C.c_int]),
             "lamp_conv3d_workspace_min_bytes": (sz, [DP, TP, C.c_int]),
@@ -69,6 +89,15 @@ def lib():
             "lamp_se_bwd_reduce": (C.c_int, [TP, TP, vp, vp, vp]),
             "lamp_se_excite_bwd": (C.c_int, [vp, C.c_int64, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]),
             "lamp_se_apply_bwd": (C.c_int, [TP, vp, vp, TP, vp]),
+            "lamp_fp8_quantize": (C.c_int, [TP, i32, FP, vp]),
+            "lamp_gemm_fp8": (C.c_int, [FP, FP, vp, TP, vp]),
+            "lamp_block_norm_fwd": (C.c_int, [NP, TP, TP, TP, TP, FP, vp]),
+            "lamp_block_norm_bwd_workspace_bytes": (sz, [TP, NP]),
+            "lamp_block_norm_bwd": (C.c_int, [NP, TP, TP, TP, TP, TP, TP, TP, GP, vp, sz, vp]),
+            "lamp_distill_topk_workspace_bytes": (sz, [TP]),
+            "lamp_distill_topk_fwd": (C.c_int, [TP, KP, vp, vp, vp, vp, vp, sz, vp]),
+            "lamp_distill_topk_bwd": (C.c_int, [TP, KP, vp, vp, TP, vp]),
+            "lamp_distill_topk_fwd_bwd": (C.c_int, [TP, KP, vp, vp, vp, TP, vp, sz, vp]),
             "lamp_unet_create": (C.c_int, [SP, C.POINTER(vp)]),
             "lamp_unet_se_layout": (C.c_int, [vp, i32, C.POINTER(sz), C.POINTER(i32)]),
             "lamp_unet_destroy": (None, [vp]),
@@ -107,6 +136,8 @@ EXPORTS = ["lamp_conv3d_workspace_bytes", "lamp_conv3d_workspace_min_bytes", "la
            "lamp_conv3d_wgrad",
            "lamp_instnorm_relu_fwd", "lamp_instnorm_relu_bwd",
            "lamp_se_squeeze", "lamp_se_excite", "lamp_se_apply_fwd", "lamp_se_bwd_reduce", "lamp_se_excite_bwd", "lamp_se_apply_bwd",
+           "lamp_fp8_quantize", "lamp_gemm_fp8", "lamp_block_norm_fwd", "lamp_block_norm_bwd_workspace_bytes", "lamp_block_norm_bwd",
+           "lamp_distill_topk_workspace_bytes", "lamp_distill_topk_fwd", "lamp_distill_topk_bwd", "lamp_distill_topk_fwd_bwd",
            "lamp_unet_create", "lamp_unet_se_layout", "lamp_unet_destroy",
            "lamp_unet_num_layers", "lamp_unet_weight_count", "lamp_unet_bias_count", "lamp_unet_param_layout",
            "lamp_unet_workspace_bytes", "lamp_unet_tensor_layout", "lamp_unet_forward", "lamp_unet_forward_layers", "lamp_unet_train_step",
@@ -351,6 +382,182 @@ def lamp_se_excite_bwd(de_sums, voxels_per_sample, n, c, cr, e, hidden, mean, w1
 
 def lamp_se_apply_bwd(dout, e, ds_over_v, dz):
     _check(lib().lamp_se_apply_bwd(C.byref(_td(dout)), _ptr(e), _ptr(ds_over_v), C.byref(_td(dz)), _stream()), "lamp_se_apply_bwd")
+
+
+# --- 8-bit layers, block norms, distillation -----------------------------------------------------------------------
+# The descriptors below hold the tensors they point at, and the calls refuse (ValueError) tensors of another type, size or
+# device than the entry point reads: a pointer alone would not show it.
+_FP8_TYPES = (torch.uint8, torch.float8_e4m3fn)
+
+
+def _vec(t, n, what, dev, dtype=torch.float32):
+    """Device pointer of a contiguous vector of n elements (None stays None)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous() or t.get_device() != dev:
+        raise ValueError(f"{what}: want a contiguous {dtype} tensor of {n} elements on cuda:{dev}, got {tuple(t.shape)} {t.dtype} on {t.device}")
+    return t.data_ptr()
+
+
+def _view(x, dev, what):
+    """Descriptor of a tensor argument (torch tensor on the current device, or a Tensor); None stays None."""
+    if x is None or isinstance(x, Tensor):
+        return x
+    if x.get_device() != dev:
+        raise ValueError(f"{what}: on {x.device}, the current device is cuda:{dev}")
+    if x.dim() != 5 or not x.is_contiguous() or x.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"{what}: want a contiguous bf16 or fp32 tensor [n, d, h, w, c], got {tuple(x.shape)} {x.dtype}")
+    n, d, h, w, c = x.shape
+    return Tensor(x.data_ptr(), LAMP_BF16 if x.dtype is torch.bfloat16 else LAMP_F32, n, d, h, w, c, c, 0)
+
+
+def _byref(s):
+    return None if s is None else C.byref(s)
+
+
+def fp8_operand(q, scale, rows=None, k=None, tile_scale=False) -> Fp8Operand:
+    """Operand [rows][k] of lamp_gemm_fp8: q uint8 or float8_e4m3fn [rows, pitch], scale fp32 [ceil(k/128), pitch]."""
+    if q.dtype not in _FP8_TYPES or q.dim() != 2 or scale.dtype is not torch.float32 or scale.dim() != 2 or not q.is_cuda:
+        raise ValueError("fp8_operand: q is a CUDA uint8 or float8_e4m3fn matrix, scale an fp32 matrix")
+    if scale.get_device() != q.get_device():
+        raise ValueError("fp8_operand: q and scale are on different devices")
+    rows = q.shape[0] if rows is None else rows
+    k = q.shape[1] if k is None else k
+    blocks = -(-k // 128)
+    if rows > q.shape[0] or k > q.shape[1] or q.stride(1) != 1 or scale.stride(1) != 1 or scale.shape[0] < blocks or \
+            scale.shape[1] < (-(-rows // 128) if tile_scale else rows):
+        raise ValueError(f"fp8_operand: [{rows}, {k}] does not fit q {tuple(q.shape)} and scale {tuple(scale.shape)}")
+    # the stride of an axis of one element says nothing: the pitch only has to cover the row
+    qp = q.stride(0) if q.shape[0] > 1 else -(-max(q.stride(0), q.shape[1]) // 16) * 16
+    sp = scale.stride(0) if scale.shape[0] > 1 else max(scale.stride(0), scale.shape[1])
+    o = Fp8Operand(q.data_ptr(), qp, scale.data_ptr(), sp, rows, k, 1 if tile_scale else 0)
+    o.keep = (q, scale)
+    return o
+
+
+def _operand(o, dev, what):
+    keep = getattr(o, "keep", None)
+    if keep is not None and keep[0].get_device() != dev:
+        raise ValueError(f"{what}: on {keep[0].device}, the current device is cuda:{dev}")
+    return C.byref(o)
+
+
+def lamp_fp8_quantize(x, out: Fp8Operand, transpose=False):
+    dev = torch.cuda.current_device()
+    _check(lib().lamp_fp8_quantize(_byref(_view(x, dev, "x")), 1 if transpose else 0, _operand(out, dev, "out"), _stream()), "lamp_fp8_quantize")
+
+
+def lamp_gemm_fp8(a: Fp8Operand, b: Fp8Operand, y, bias=None):
+    dev = torch.cuda.current_device()
+    _check(lib().lamp_gemm_fp8(_operand(a, dev, "a"), _operand(b, dev, "b"), _vec(bias, b.rows, "bias", dev), _byref(_view(y, dev, "y")),
+                               _stream()), "lamp_gemm_fp8")
+
+
+def block_norm(rms=False, eps=1e-5, post_w=None, post_b=None, pre_w=None, pre_b=None, gate=None, gate_logits=None,
+               res_scale=None) -> BlockNorm:
+    """Parameters of lamp_block_norm_fwd / _bwd: fp32 vectors [c] (gate: [n, c]), gate_logits a tensor like y."""
+    p = BlockNorm()
+    p.rms, p.eps = 1 if rms else 0, eps
+    p.keep = (("post_w", post_w), ("post_b", post_b), ("pre_w", pre_w), ("pre_b", pre_b), ("res_scale", res_scale))
+    p.keep_gate, p.keep_logits = gate, gate_logits
+    return p
+
+
+def _norm_params(p, shape, dev):
+    """Fills in the pointers, checked against the shape of the call's tensors."""
+    for name, v in p.keep:
+        setattr(p, name, _vec(v, shape.c, name, dev))
+    p.gate = _vec(p.keep_gate, shape.n * shape.c, "gate", dev)
+    if p.keep_logits is not None:
+        p.keep_view = _view(p.keep_logits, dev, "gate_logits")
+        p.gate_logits = C.pointer(p.keep_view)
+    return C.byref(p)
+
+
+def lamp_block_norm_fwd(p: BlockNorm, y, x, out, h=None, h_fp8=None):
+    dev = torch.cuda.current_device()
+    vx = _view(x, dev, "x")
+    _check(lib().lamp_block_norm_fwd(_norm_params(p, vx, dev), _byref(_view(y, dev, "y")), C.byref(vx), _byref(_view(out, dev, "out")),
+                                     _byref(_view(h, dev, "h")), None if h_fp8 is None else _operand(h_fp8, dev, "h_fp8"), _stream()),
+           "lamp_block_norm_fwd")
+
+
+def lamp_block_norm_bwd_workspace_bytes(t, p: BlockNorm):
+    dev = torch.cuda.current_device()
+    vt = _view(t, dev, "t")
+    return lib().lamp_block_norm_bwd_workspace_bytes(C.byref(vt), _norm_params(p, vt, dev))
+
+
+def lamp_block_norm_bwd(p: BlockNorm, y, t, dout, dh, dx, dy, ws=None, dgate_logits=None, dpost_w=None, dpost_b=None, dpre_w=None,
+                        dpre_b=None, dgate=None, dres_scale=None):
+    dev = torch.cuda.current_device()
+    vt = _view(t, dev, "t")
+    c = vt.c
+    g = BlockNormGrads(_vec(dpost_w, c, "dpost_w", dev), _vec(dpost_b, c, "dpost_b", dev), _vec(dpre_w, c, "dpre_w", dev),
+                       _vec(dpre_b, c, "dpre_b", dev), _vec(dgate, vt.n * c, "dgate", dev), _vec(dres_scale, c, "dres_scale", dev))
+    if ws is not None and ws.get_device() != dev:
+        raise ValueError(f"ws: on {ws.device}, the current device is cuda:{dev}")
+    w, nbytes = _ws(ws)
+    _check(lib().lamp_block_norm_bwd(_norm_params(p, vt, dev), _byref(_view(y, dev, "y")), C.byref(vt), _byref(_view(dout, dev, "dout")),
+                                     _byref(_view(dh, dev, "dh")), _byref(_view(dx, dev, "dx")), _byref(_view(dy, dev, "dy")),
+                                     _byref(_view(dgate_logits, dev, "dgate_logits")), C.byref(g), w, nbytes, _stream()),
+           "lamp_block_norm_bwd")
+
+
+def teacher_topk(idx, logits, temperature=1.0, lse=None) -> TeacherTopk:
+    """The teacher's k listed classes per row: idx int32 [rows, k], logits fp32 [rows, k], lse fp32 [rows] or None."""
+    t = TeacherTopk()
+    if idx.dim() != 2:
+        raise ValueError("teacher_topk: idx is a matrix [rows, k]")
+    t.k, t.temperature = idx.shape[1], temperature
+    t.keep = (idx, logits, lse)
+    return t
+
+
+def _teacher(t, z, dev):
+    rows = z.n * z.d * z.h * z.w
+    idx, logits, lse = t.keep
+    t.idx = _vec(idx, rows * t.k, "idx", dev, torch.int32)
+    t.logits = _vec(logits, rows * t.k, "logits", dev)
+    t.lse = _vec(lse, rows, "lse", dev)
+    return C.byref(t), rows
+
+
+def lamp_distill_topk_workspace_bytes(z):
+    return lib().lamp_distill_topk_workspace_bytes(C.byref(_td(z)))
+
+
+def _scratch(ws, dev):
+    if ws is not None and ws.get_device() != dev:
+        raise ValueError(f"ws: on {ws.device}, the current device is cuda:{dev}")
+    return _ws(ws)
+
+
+def lamp_distill_topk_fwd(z, teacher: TeacherTopk, row_weight=None, loss_rows=None, lse=None, loss=None, ws=None):
+    dev = torch.cuda.current_device()
+    vz = _view(z, dev, "z")
+    t, rows = _teacher(teacher, vz, dev)
+    w, nbytes = _scratch(ws, dev)
+    _check(lib().lamp_distill_topk_fwd(C.byref(vz), t, _vec(row_weight, rows, "row_weight", dev), _vec(loss_rows, rows, "loss_rows", dev),
+                                       _vec(lse, rows, "lse", dev), _vec(loss, 1, "loss", dev), w, nbytes, _stream()), "lamp_distill_topk_fwd")
+
+
+def lamp_distill_topk_bwd(z, teacher: TeacherTopk, row_grad, lse, dz):
+    dev = torch.cuda.current_device()
+    vz = _view(z, dev, "z")
+    t, rows = _teacher(teacher, vz, dev)
+    _check(lib().lamp_distill_topk_bwd(C.byref(vz), t, _vec(row_grad, rows, "row_grad", dev), _vec(lse, rows, "lse", dev),
+                                       _byref(_view(dz, dev, "dz")), _stream()), "lamp_distill_topk_bwd")
+
+
+def lamp_distill_topk_fwd_bwd(z, teacher: TeacherTopk, row_weight, loss_rows, loss, dz, ws=None):
+    dev = torch.cuda.current_device()
+    vz = _view(z, dev, "z")
+    t, rows = _teacher(teacher, vz, dev)
+    w, nbytes = _scratch(ws, dev)
+    _check(lib().lamp_distill_topk_fwd_bwd(C.byref(vz), t, _vec(row_weight, rows, "row_weight", dev), _vec(loss_rows, rows, "loss_rows", dev),
+                                           _vec(loss, 1, "loss", dev), _byref(_view(dz, dev, "dz")), w, nbytes, _stream()),
+           "lamp_distill_topk_fwd_bwd")
 
 
 def lamp_rmsprop_step(grad, master, v, param_bf16=None, lr=1e-3, alpha=0.99, eps=1e-8):

@@ -89,7 +89,7 @@ int sm_count()
 
 static bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
 
-static lamp_status_t check_tensor(const lamp_tensor_t *t, bool allow_f32, bool any_channels)
+lamp_status_t check_tensor(const lamp_tensor_t *t, bool allow_f32, bool any_channels)
 {
     if (!t || !t->ptr) return LAMP_ERR_INVALID_ARG;
     if (t->n < 0 || t->d < 0 || t->h < 0 || t->w < 0 || t->c <= 0 || t->c_offset < 0) return LAMP_ERR_INVALID_ARG;

@@ -1,0 +1,393 @@
+// Backward pass of the norms around a residual block (block_norm.cuh has the layout).  Per row, with th, yh the normalised
+// t and y, and all means over the channels (mean(a), mean(b) only for LayerNorm):
+//     a  = dh w_pre,        dt = dout + rstd_t (a - mean(a) - th mean(a th)),          dx = dt
+//     b  = dt r g w_post,   dy = rstd_y (b - mean(b) - yh mean(b yh)),                 dlogit = dt r (yh w_post + b_post) g (1 - g)
+// Means and deviations are computed again from the rows, which are read anyway.  Bound by memory: t, y, dout, dh read once, dx
+// and dy written once.
+// Parameter gradients are sums over voxels of four products per channel, P = dt g' yh, Q = dt g' (g' = the gate where it has
+// a value per element, else 1), dh th and dh: each thread adds them up for its own channels over the rows it works on, a CTA
+// joins its threads in a fixed order and leaves one row of 4 c partial sums in the workspace; block_norm_finish_kernel adds
+// those in a fixed order (fp64) and forms  dw_post = r g P, db_post = r g Q, dr = g (w P + b Q), dg = r (w P + b Q).
+#include "block_norm.cuh"
+
+namespace lamp {
+
+namespace {
+
+using namespace bn;
+
+struct BwdParams {
+    const void *y, *t, *dout, *dh, *logits;
+    void *dx, *dy, *dl;
+    int64_t py, pt, pdo, pdh, pl, pdx, pdy, pdl;
+    int64_t rows;
+    int32_t parts, c, rms;
+    float eps;
+    const float *post_w, *post_b, *pre_w, *gate, *res;
+    float *part;                     // [samples * parts][4][c] or NULL
+};
+
+template <bool SF, bool BF, int TPR, int U, int MAXT>
+__global__ void __launch_bounds__(MAXT)
+block_norm_bwd_kernel(const BwdParams P)
+{
+    extern __shared__ __align__(16) float par[];
+    __shared__ float red[2][32];
+    const int threads = TPR ? TPR : blockDim.x;
+    const int groups = TPR ? blockDim.x / TPR : 1, group = TPR ? threadIdx.x / TPR : 0, tt = TPR ? threadIdx.x % TPR : threadIdx.x;
+    const int units = P.c / 8;
+    const bool post = P.y != nullptr, pre = P.dh != nullptr;
+    const int64_t sample = blockIdx.x / P.parts, part = blockIdx.x - sample * P.parts;
+    const int64_t base = sample * P.rows;
+    pdl_launch_dependents();
+    pdl_wait();
+    for (int ch = threadIdx.x; ch < P.c; ch += blockDim.x) {
+        const float rg = (P.res ? P.res[ch] : 1.f) * (P.gate ? P.gate[sample * P.c + ch] : 1.f);
+        store_par(par, 0, units, ch, rg * (P.post_w ? P.post_w[ch] : 1.f));
+        store_par(par, 1, units, ch, P.post_b ? rg * P.post_b[ch] : 0.f);
+        store_par(par, 2, units, ch, P.pre_w ? P.pre_w[ch] : 1.f);
+    }
+    __syncthreads();
+    const float4 *par4 = reinterpret_cast<const float4 *>(par);
+    const float inv_c = 1.f / (float)P.c;
+    int turn = 0;
+
+    float acc[U][4][8];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[u][k][j] = 0.f;
+
+    const int64_t step = (int64_t)P.parts * groups;
+    for (int64_t r0 = part * groups; r0 < P.rows; r0 += step) {
+        const int64_t row = r0 + group;
+        const bool active = row < P.rows;
+        Raw<SF> rt[U], rdo[U];
+        Raw<BF> ry[U], rdh[U], rl[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int ch = (u * threads + tt) * 8;
+            const bool in = active && ch < P.c;
+            const int64_t r = base + row;
+            rt[u] = in && pre ? load_raw<SF>(P.t, r * P.pt + ch) : zero_raw<SF>();
+            rdh[u] = in && pre ? load_raw<BF>(P.dh, r * P.pdh + ch) : zero_raw<BF>();
+            ry[u] = in && post ? load_raw<BF>(P.y, r * P.py + ch) : zero_raw<BF>();
+            rdo[u] = in && P.dout ? load_raw<SF>(P.dout, r * P.pdo + ch) : zero_raw<SF>();
+            rl[u] = in && P.logits ? load_raw<BF>(P.logits, r * P.pl + ch) : zero_raw<BF>();
+        }
+        float th[U][8], yh[U][8], dt[U][8];
+        float st = 0.f, sy = 0.f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            to_float<SF>(rt[u], th[u]);
+            to_float<BF>(ry[u], yh[u]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) { st += th[u][j]; sy += yh[u][j]; }
+        }
+        if (!P.rms) row_sum2<TPR>(st, sy, red, turn); else st = sy = 0.f;
+        const float mt = st * inv_c, my = sy * inv_c;
+        float qt = 0.f, qy = 0.f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const bool in = (u * threads + tt) * 8 < P.c;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                th[u][j] = in ? th[u][j] - mt : 0.f;
+                yh[u][j] = in ? yh[u][j] - my : 0.f;
+                qt = fmaf(th[u][j], th[u][j], qt);
+                qy = fmaf(yh[u][j], yh[u][j], qy);
+            }
+        }
+        row_sum2<TPR>(qt, qy, red, turn);
+        // a row past the end takes part in the sums with zeros only, whatever eps is
+        const float rst = active ? 1.f / sqrtf(qt * inv_c + P.eps) : 0.f, rsy = active ? 1.f / sqrtf(qy * inv_c + P.eps) : 0.f;
+        if (pre) {
+            float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int unit = u * threads + tt;
+                float w[8], d[8];
+                to_float<BF>(rdh[u], d);
+                if (unit < units) load_par(par4, 2, units, unit, w);
+                else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) w[j] = 0.f;
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    th[u][j] *= rst;
+                    acc[u][2][j] = fmaf(d[j], th[u][j], acc[u][2][j]);
+                    acc[u][3][j] += d[j];
+                    dt[u][j] = d[j] * w[j];
+                    s1 += dt[u][j];
+                    s2 = fmaf(dt[u][j], th[u][j], s2);
+                }
+            }
+            row_sum2<TPR>(s1, s2, red, turn);
+            const float m1 = P.rms ? 0.f : s1 * inv_c, m2 = s2 * inv_c;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float d[8];
+                to_float<SF>(rdo[u], d);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) dt[u][j] = fmaf(rst, dt[u][j] - m1 - th[u][j] * m2, d[j]);
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) to_float<SF>(rdo[u], dt[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int unit = u * threads + tt;
+            if (active && unit < units) store8<SF>(P.dx, (base + row) * P.pdx + unit * 8, dt[u]);
+        }
+        if (post) {
+            float s1 = 0.f, s2 = 0.f;
+            float b[U][8];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int unit = u * threads + tt;
+                const bool in = active && unit < units;
+                float w[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) w[j] = 0.f;
+                if (in) load_par(par4, 0, units, unit, w);
+                float g[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) { g[j] = 1.f; yh[u][j] *= rsy; }
+                if (P.logits) {
+                    float lg[8], wb[8];
+                    to_float<BF>(rl[u], lg);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) g[j] = 1.f / (1.f + __expf(-lg[j]));
+                    if (in) {
+                        load_par(par4, 1, units, unit, wb);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) lg[j] = dt[u][j] * fmaf(yh[u][j], w[j], wb[j]) * (g[j] * (1.f - g[j]));
+                        store8<BF>(P.dl, (base + row) * P.pdl + unit * 8, lg);
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float d = in ? dt[u][j] * g[j] : 0.f;
+                    acc[u][0][j] = fmaf(d, yh[u][j], acc[u][0][j]);
+                    acc[u][1][j] += d;
+                    b[u][j] = d * w[j];
+                    s1 += b[u][j];
+                    s2 = fmaf(b[u][j], yh[u][j], s2);
+                }
+            }
+            row_sum2<TPR>(s1, s2, red, turn);
+            const float m1 = P.rms ? 0.f : s1 * inv_c, m2 = s2 * inv_c;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int unit = u * threads + tt;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) b[u][j] = rsy * (b[u][j] - m1 - yh[u][j] * m2);
+                if (active && unit < units) store8<BF>(P.dy, (base + row) * P.pdy + unit * 8, b[u]);
+            }
+        }
+    }
+    if (!P.part) return;
+    float *dst = P.part + (int64_t)blockIdx.x * 4 * P.c;
+    if (TPR == 0) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int unit = u * threads + tt;
+            if (unit < units)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) dst[k * P.c + unit * 8 + j] = acc[u][k][j];
+        }
+    } else {
+        // rows of the CTA's groups, one product at a time: [group][channel] in shared memory, added in group order
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            __syncthreads();
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int unit = u * threads + tt;
+                if (unit < units)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) par[group * P.c + unit * 8 + j] = acc[u][k][j];
+            }
+            __syncthreads();
+            for (int ch = threadIdx.x; ch < P.c; ch += blockDim.x) {
+                float s = 0.f;
+                for (int g = 0; g < groups; ++g) s += par[g * P.c + ch];
+                dst[k * P.c + ch] = s;
+            }
+        }
+    }
+}
+
+// 32 channels per CTA (one per lane); the 8 warps share the partial rows of a sample, or, with 8 samples or more, take
+// whole samples.
+struct FinishParams {
+    const float *part;
+    int32_t parts, c;
+    int64_t samples;
+    const float *post_w, *post_b, *gate, *res;
+    float *dpost_w, *dpost_b, *dpre_w, *dpre_b, *dgate, *dres;
+};
+
+__global__ void __launch_bounds__(256)
+block_norm_finish_kernel(const FinishParams P)
+{
+    __shared__ double sm[8][4][32];
+    pdl_launch_dependents();
+    pdl_wait();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int ch = blockIdx.x * 32 + lane;
+    const bool in = ch < P.c;
+    const double w = in && P.post_w ? P.post_w[ch] : 1.0, b = in && P.post_b ? P.post_b[ch] : 0.0, r = in && P.res ? P.res[ch] : 1.0;
+    const bool whole = P.samples >= 8;                              // a warp takes whole samples
+    double tot[5] = {0, 0, 0, 0, 0};                                // dw_post, db_post, dw_pre, db_pre, dr
+    for (int64_t s = whole ? warp : 0; s < P.samples; s += whole ? 8 : 1) {
+        double v[4] = {0, 0, 0, 0};
+        if (in) {
+#pragma unroll 4
+            for (int p = whole ? 0 : warp; p < P.parts; p += whole ? 1 : 8) {
+                const float *src = P.part + (s * P.parts + p) * 4 * P.c + ch;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[k] += (double)src[(int64_t)k * P.c];
+            }
+        }
+        const double g = in && P.gate ? P.gate[s * P.c + ch] : 1.0;
+        if (!whole && P.gate) {                                     // the sample's sums over all warps, in warp order
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sm[warp][k][lane] = v[k];
+            __syncthreads();
+            if (warp == 0) {
+                for (int i = 1; i < 8; ++i)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[k] += sm[i][k][lane];
+            } else {
+                v[0] = v[1] = v[2] = v[3] = 0;
+            }
+        }
+        if (P.dgate && in && (whole || warp == 0)) P.dgate[s * P.c + ch] = (float)(r * (w * v[0] + b * v[1]));
+        tot[0] += r * g * v[0]; tot[1] += r * g * v[1]; tot[2] += v[2]; tot[3] += v[3]; tot[4] += g * (w * v[0] + b * v[1]);
+    }
+    float *outs[5] = {P.dpost_w, P.dpost_b, P.dpre_w, P.dpre_b, P.dres};
+#pragma unroll
+    for (int k = 0; k < 5; ++k) {
+        __syncthreads();
+        sm[warp][0][lane] = tot[k];
+        __syncthreads();
+        if (warp == 0 && in && outs[k]) {
+            double v = 0;
+            for (int i = 0; i < 8; ++i) v += sm[i][0][lane];
+            outs[k][ch] = (float)v;
+        }
+    }
+}
+
+int64_t parts_of(const lamp_tensor_t *t, const lamp_block_norm_t *p, int64_t *samples)
+{
+    const Shape sh = shape_of(t->c);
+    *samples = p->gate ? t->n : 1;
+    const int64_t rows = voxels(t) / (*samples > 0 ? *samples : 1), need = (rows + sh.rows_per_cta - 1) / sh.rows_per_cta;
+    int64_t room = (int64_t)sm_count() * (sh.threads <= 256 ? 512 / sh.threads : 1) / (*samples > 0 ? *samples : 1);
+    if (room < 1) room = 1;
+    return need < room ? need : room;
+}
+
+template <bool SF, bool BF, int TPR, int U, int MAXT>
+lamp_status_t launch(const BwdParams &P, int64_t samples, const Shape &sh, cudaStream_t st)
+{
+    const int groups = TPR ? sh.threads / TPR : 1;
+    int smem = P.c * 12;
+    if (TPR && groups * P.c * 4 > smem) smem = groups * P.c * 4;
+    if (smem > 32 * 1024) {                                  // static shared memory counts too: well below the 48 KB default
+        static SmemAttrOnce attr;
+        const lamp_status_t s = attr.ensure(block_norm_bwd_kernel<SF, BF, TPR, U, MAXT>, MAX_C * 12);
+        if (s != LAMP_OK) return s;
+    }
+    return launch_pdl(samples * P.parts <= 8 * (int64_t)sm_count(), block_norm_bwd_kernel<SF, BF, TPR, U, MAXT>, dim3((unsigned)(samples * P.parts)),
+                      dim3(sh.threads), (size_t)smem, st, P);
+}
+
+template <bool SF, bool BF>
+lamp_status_t dispatch(const BwdParams &P, int64_t samples, const Shape &sh, cudaStream_t st)
+{
+    if (sh.tpr == 4) return launch<SF, BF, 4, 1, 256>(P, samples, sh, st);
+    if (sh.tpr == 8) return launch<SF, BF, 8, 1, 256>(P, samples, sh, st);
+    if (sh.tpr == 16) return launch<SF, BF, 16, 1, 256>(P, samples, sh, st);
+    if (sh.tpr == 32 && sh.u == 1) return launch<SF, BF, 32, 1, 256>(P, samples, sh, st);
+    if (sh.tpr == 32) return launch<SF, BF, 32, 2, 256>(P, samples, sh, st);
+    return sh.threads <= 256 ? launch<SF, BF, 0, 2, 256>(P, samples, sh, st) : launch<SF, BF, 0, 2, 512>(P, samples, sh, st);
+}
+
+}  // namespace
+
+}  // namespace lamp
+
+using namespace lamp;
+
+extern "C" size_t lamp_block_norm_bwd_workspace_bytes(const lamp_tensor_t *t, const lamp_block_norm_t *p)
+{
+    if (!t || check_norm_tensor(t, t) != LAMP_OK || check_norm_params(p, t) != LAMP_OK) return 0;
+    int64_t samples;
+    const int64_t parts = parts_of(t, p, &samples);
+    return (size_t)(samples * parts) * 4 * t->c * sizeof(float);
+}
+
+extern "C" lamp_status_t lamp_block_norm_bwd(const lamp_block_norm_t *p, const lamp_tensor_t *y, const lamp_tensor_t *t, const lamp_tensor_t *dout,
+                                             const lamp_tensor_t *dh, lamp_tensor_t *dx, lamp_tensor_t *dy, lamp_tensor_t *dgate_logits,
+                                             const lamp_block_norm_grads_t *grads, void *ws, size_t ws_bytes, void *cuda_stream)
+{
+    lamp_status_t s;
+    if (!t || (s = check_norm_tensor(t, t)) != LAMP_OK) return t ? s : LAMP_ERR_INVALID_ARG;
+    if ((s = check_norm_params(p, t)) != LAMP_OK) return s;
+    if ((!dout && !dh) || !dx || (y == nullptr) != (dy == nullptr)) return LAMP_ERR_INVALID_ARG;
+    if ((p->gate_logits == nullptr) != (dgate_logits == nullptr) || (!y && (p->gate_logits || p->gate || p->res_scale))) return LAMP_ERR_INVALID_ARG;
+    const lamp_tensor_t *stream[2] = {dout, dx}, *branch[5] = {y, dh, dy, p->gate_logits, dgate_logits};
+    for (const lamp_tensor_t *v : stream) {
+        if (!v) continue;
+        if ((s = check_norm_tensor(v, t)) != LAMP_OK) return s;
+        if (v->dtype != t->dtype) return LAMP_ERR_UNSUPPORTED;
+    }
+    int bf = -1;
+    for (const lamp_tensor_t *v : branch) {
+        if (!v) continue;
+        if ((s = check_norm_tensor(v, t)) != LAMP_OK) return s;
+        if (bf >= 0 && v->dtype != bf) return LAMP_ERR_UNSUPPORTED;
+        bf = v->dtype;
+    }
+    if (bf < 0) return LAMP_ERR_INVALID_ARG;                           // neither a post-norm nor a pre-norm
+    if (t->dtype == LAMP_BF16 && bf == LAMP_F32) return LAMP_ERR_UNSUPPORTED;
+    const lamp_block_norm_grads_t none = {}, *g = grads ? grads : &none;
+    const bool want = g->post_w || g->post_b || g->pre_w || g->pre_b || g->gate || g->res_scale;
+    if (((uintptr_t)g->post_w | (uintptr_t)g->post_b | (uintptr_t)g->pre_w | (uintptr_t)g->pre_b | (uintptr_t)g->gate | (uintptr_t)g->res_scale) & 3)
+        return LAMP_ERR_INVALID_ARG;
+    if (g->gate && !p->gate) return LAMP_ERR_INVALID_ARG;
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    int64_t samples;
+    const int64_t parts = parts_of(t, p, &samples);
+    if (voxels(t) == 0) {                                              // empty sums
+        float *z[5] = {g->post_w, g->post_b, g->pre_w, g->pre_b, g->res_scale};
+        for (float *q : z) if (q) LAMP_CUDA_OK(cudaMemsetAsync(q, 0, (size_t)t->c * 4, st));
+        if (g->gate && t->n) LAMP_CUDA_OK(cudaMemsetAsync(g->gate, 0, (size_t)t->n * t->c * 4, st));
+        return LAMP_OK;
+    }
+    if (samples * parts > 2147483647ll) return LAMP_ERR_UNSUPPORTED;
+    if (want && (!ws || ((uintptr_t)ws & 15) || ws_bytes < (size_t)(samples * parts) * 4 * t->c * sizeof(float))) return LAMP_ERR_WORKSPACE;
+    BwdParams P = {};
+    auto put = [](const lamp_tensor_t *v, auto &ptr, int64_t &pitch) { if (v) { const TView w = make_view(v); ptr = w.p; pitch = w.pitch; } };
+    put(y, P.y, P.py); put(t, P.t, P.pt); put(dout, P.dout, P.pdo); put(dh, P.dh, P.pdh); put(p->gate_logits, P.logits, P.pl);
+    put(dx, P.dx, P.pdx); put(dy, P.dy, P.pdy); put(dgate_logits, P.dl, P.pdl);
+    P.rows = voxels(t) / samples; P.parts = (int32_t)parts; P.c = t->c; P.rms = p->rms; P.eps = p->eps;
+    P.post_w = p->post_w; P.post_b = p->post_b; P.pre_w = p->pre_w; P.gate = p->gate; P.res = p->res_scale;
+    P.part = want ? (float *)ws : nullptr;
+    const Shape sh = shape_of(P.c);
+    if (t->dtype == LAMP_BF16) s = dispatch<false, false>(P, samples, sh, st);
+    else s = bf == LAMP_F32 ? dispatch<true, true>(P, samples, sh, st) : dispatch<true, false>(P, samples, sh, st);
+    if (s != LAMP_OK || !want) return s;
+    FinishParams F = {(const float *)ws, (int32_t)parts, P.c, samples, P.post_w, P.post_b, P.gate, P.res, g->post_w, g->post_b, g->pre_w, g->pre_b, g->gate, g->res_scale};
+    return launch_pdl(true, block_norm_finish_kernel, dim3((unsigned)((P.c + 31) / 32)), dim3(256), 0, st, F);
+}

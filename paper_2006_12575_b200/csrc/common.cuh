@@ -80,6 +80,21 @@ static inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; 
 void *tensor_map_encoder();
 // api.cu.  Number of SMs of the current device.
 int sm_count();
+// api.cu.  Argument check of a tensor view; any_channels: c, c_pitch, c_offset of a bf16 view need not be multiples of 8.
+lamp_status_t check_tensor(const lamp_tensor_t *t, bool allow_f32, bool any_channels);
+// The same for tensors that may be empty: one without voxels needs no buffer.
+static inline lamp_status_t check_view(const lamp_tensor_t *t, bool any_channels)
+{
+    if (!t) return LAMP_ERR_INVALID_ARG;
+    lamp_tensor_t v = *t;
+    if (!v.ptr && v.n >= 0 && v.d >= 0 && v.h >= 0 && v.w >= 0 && voxels(&v) == 0) v.ptr = (void *)16;
+    return check_tensor(&v, true, any_channels);
+}
+// fp8_gemm.cu.  Argument check of an 8-bit operand.
+lamp_status_t check_fp8_operand(const lamp_fp8_operand_t *o);
+// block_norm_fwd.cu.  Argument checks of the block norm: a tensor of the shape of `like`, and the parameters.
+lamp_status_t check_norm_tensor(const lamp_tensor_t *t, const lamp_tensor_t *like);
+lamp_status_t check_norm_params(const lamp_block_norm_t *p, const lamp_tensor_t *like);
 
 // cudaFuncAttributeMaxDynamicSharedMemorySize is a per-device attribute of a kernel: a launcher keeps one of these
 // per kernel instantiation and asks it before every launch; the attribute is set on the first launch on each device

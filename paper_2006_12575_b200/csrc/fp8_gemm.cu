@@ -1,0 +1,527 @@
+// Matrix product of two e4m3 operands with fp32 scales per block of 128 along k:
+//   y[m][n] = bias[n] + sum_b ( sum_{k in block b} qa[m][k] qb[n][k] ) * sa[b][m] * sb[b][n or n/128]
+//
+// The scales are arbitrary fp32 numbers, so the tensor cores can only sum within a block of 128; the blocks are
+// added in fp32 registers ("promotion").  One operand lies on the 128 lanes of the tensor memory, the other on BN columns.
+// Per CTA, warp-specialised:
+//   warp 0     TMA producer: per block of k a [128 x 128 B] lane tile and a [BN x 128 B] column tile, 128-byte swizzle.
+//              Rows and bytes beyond the operand are zero-filled (code 0 = 0.0): no size has to be a multiple of the tile.
+//   warp 1     tcgen05.mma kind::f8f6f4, four instructions (K = 32 each) per block, always into a fresh accumulator; the
+//              accumulators rotate through tensor memory (NACC of them), so block b + 1 is multiplied while block b is promoted.
+//   warps 2..  promotion: tcgen05.ld of an accumulator, acc += part * scale with packed fp32 FMAs, then the epilogue.
+// A scale per column needs one more multiplication per element than a scalar one: COLVEC.
+// Few rows of a (m <= 64) put b on the lanes (swap): 128 weight rows per tile, the tokens on 16..64 columns.
+// Few tiles: the CTAs of a cluster share the k axis of a tile, leave their fp32 parts in their shared memory, and each adds
+// a slice of the columns over all of them in rank order - no workspace, no second launch, the same order every time.
+// Every mbarrier wait is bounded; on expiry the CTA records LAMP_ERR_TIMEOUT and winds down.
+#include <cuda.h>
+#include <cudaTypedefs.h>
+#include "common.cuh"
+#include "umma_ptx.cuh"
+
+namespace lamp {
+
+namespace {
+
+using namespace ptx;
+
+constexpr int KB = 128;                       // codes per scale block = bytes per shared-memory row
+constexpr int MAX_STAGES = 10, MAX_ACC = 4;
+
+struct GemmParams {
+    int32_t rows_l, rows_c;                   // rows of the lane operand and of the column operand
+    int32_t kblocks;
+    int32_t nl, nc;                           // tiles per axis
+    int64_t tiles;
+    int32_t splits;                           // CTAs (of one cluster) that share the blocks of a tile
+    const float *sl, *sc;
+    int64_t pl, pc;                           // scale pitches
+    int32_t tile_l, tile_c;                   // scale per 128 rows
+    const float *bias;
+    void *y;
+    int64_t y_pitch;
+    int32_t y_f32, swap;
+    int32_t vec;                              // alignment of every row's tile start: 2 = 32 bytes, 1 = 16 bytes, 0 = neither
+    int *status;
+};
+
+template <int BN> struct GemmLayout {
+    static constexpr int A_BYTES = 128 * KB, C_BYTES = BN * KB, STAGE_BYTES = A_BYTES + C_BYTES;
+    static constexpr int STAGES = BN == 256 ? 4 : BN == 128 ? 6 : BN == 64 ? 8 : 9;
+    static constexpr int NACC = BN == 256 ? 2 : 4;
+    static constexpr int NEPI = BN >= 64 ? 8 : 4;                 // promotion warps
+    static constexpr int CW = BN >= 64 ? BN / 2 : BN;             // columns per promotion warp
+    static constexpr int THREADS = 64 + 32 * NEPI;
+    static constexpr int TMEM_COLS = NACC * BN;                   // 64 .. 512, a power of two
+    static constexpr int SCALE_BYTES = NEPI * 2 * CW * 4;
+    static constexpr int BAR_BYTES = (2 * MAX_STAGES + 2 * MAX_ACC) * 8 + 16;
+    static constexpr int TOTAL = 1024 + STAGES * STAGE_BYTES + SCALE_BYTES + BAR_BYTES;
+    static_assert(BN * 128 * 4 <= STAGES * STAGE_BYTES, "the split-k parts reuse the stages");
+    static_assert(TOTAL <= 227 * 1024 && STAGES <= MAX_STAGES && NACC <= MAX_ACC, "");
+};
+
+// Instruction descriptor: D fp32, A and B e4m3, both K-major, M = 128, N = n.
+__host__ __device__ constexpr uint32_t idesc_e4m3(uint32_t n) { return (1u << 4) | ((n >> 3) << 17) | ((128u >> 4) << 24); }
+
+__device__ __forceinline__ void umma_fp8(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}"
+                 ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int c0, int c1)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1) : "memory");
+}
+// 32 lanes x 16 columns into 16 registers
+__device__ __forceinline__ void tmem_ld_x16(uint32_t taddr, uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+                 "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(taddr) : "memory");
+}
+
+// two fp32 values in one 64-bit register
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pack2(uint32_t lo, uint32_t hi)
+{
+    f32x2 v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "r"(lo), "r"(hi));
+    return v;
+}
+__device__ __forceinline__ void unpack2(f32x2 v, float &lo, float &hi)
+{
+    uint32_t a, b;
+    asm("mov.b64 {%0, %1}, %2;" : "=r"(a), "=r"(b) : "l"(v));
+    lo = __uint_as_float(a); hi = __uint_as_float(b);
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c)
+{
+    f32x2 d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b)
+{
+    f32x2 d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+
+__device__ __forceinline__ uint32_t cluster_rank()
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync_all()
+{
+    asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
+}
+__device__ __forceinline__ float ld_peer_f32(uint32_t addr, uint32_t rank)
+{
+    uint32_t a;
+    float v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+    return v;
+}
+
+// NV consecutive outputs of one row (columns col .. col + NV - 1, of which `left` exist)
+template <int NV>
+__device__ __forceinline__ void store_row(const GemmParams &P, int64_t row, int col, const float (&v)[NV])
+{
+    const int left = P.rows_c - col;
+    if (left <= 0) return;
+    if (P.y_f32) {
+        float *o = (float *)P.y + row * P.y_pitch + col;
+        if (NV % 4 == 0 && left >= NV && P.vec >= 1) {
+            if (NV % 8 == 0 && P.vec == 2) {
+#pragma unroll
+                for (int j = 0; j + 8 <= NV; j += 8) {
+                    uint32_t u[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) u[i] = __float_as_uint(v[j + i]);
+                    st_global_32B(o + j, u);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j + 4 <= NV; j += 4) *reinterpret_cast<float4 *>(o + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) if (j < left) o[j] = v[j];
+        }
+    } else {
+        bf16 *o = (bf16 *)P.y + row * P.y_pitch + col;
+        if (NV % 8 == 0 && left >= NV && P.vec >= 1) {
+            uint32_t u[(NV + 1) / 2];
+#pragma unroll
+            for (int j = 0; j + 2 <= NV; j += 2) {
+                __nv_bfloat162 h = __floats2bfloat162_rn(v[j], v[j + 1]);
+                u[j / 2] = *reinterpret_cast<uint32_t *>(&h);
+            }
+            if (NV % 16 == 0 && P.vec == 2) {
+#pragma unroll
+                for (int j = 0; j + 16 <= NV; j += 16) {
+                    uint32_t w[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) w[i] = u[(j / 2 + i) % ((NV + 1) / 2)];
+                    st_global_32B(o + j, w);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j + 8 <= NV; j += 8)
+                    *reinterpret_cast<uint4 *>(o + j) = make_uint4(u[j / 2], u[(j / 2 + 1) % ((NV + 1) / 2)], u[(j / 2 + 2) % ((NV + 1) / 2)],
+                                                                   u[(j / 2 + 3) % ((NV + 1) / 2)]);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) if (j < left) o[j] = f2bf(v[j]);
+        }
+    }
+}
+
+// the finished sums of NV columns of lane row `row`: bias, rounding, store
+template <int NV>
+__device__ __forceinline__ void finish(const GemmParams &P, int64_t row, int col, float (&v)[NV])
+{
+    if (row >= P.rows_l) return;
+    if (P.swap) {                              // lanes = channels of y, columns = its voxels
+        const float b = P.bias ? __ldg(P.bias + row) : 0.f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            if (col + j >= P.rows_c) break;
+            const int64_t at = (int64_t)(col + j) * P.y_pitch + row;
+            if (P.y_f32) ((float *)P.y)[at] = v[j] + b; else ((bf16 *)P.y)[at] = f2bf(v[j] + b);
+        }
+    } else {
+        if (P.bias) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) if (col + j < P.rows_c) v[j] += __ldg(P.bias + col + j);
+        }
+        store_row<NV>(P, row, col, v);
+    }
+}
+
+// Sum over the cluster's parts of CW / S columns of this thread's lane row, and their store.
+template <int CW, int S>
+__device__ __forceinline__ void reduce_parts(const GemmParams &P, uint32_t part_base, int lane_row, int64_t row, int col_local, int col0, uint32_t rank)
+{
+    constexpr int CWS = CW / S, CH = CWS < 16 ? CWS : 16;
+#pragma unroll 1
+    for (int j0 = 0; j0 < CWS; j0 += CH) {
+        const int cl = col_local + (int)rank * CWS + j0;
+        float v[CH];
+#pragma unroll
+        for (int j = 0; j < CH; ++j) v[j] = 0.f;
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+#pragma unroll
+            for (int j = 0; j < CH; ++j) v[j] += ld_peer_f32(part_base + ((cl + j) * 128 + lane_row) * 4, s);
+        finish<CH>(P, row, col0 + cl, v);
+    }
+}
+
+template <int BN, bool COLVEC>
+__global__ void __launch_bounds__(GemmLayout<BN>::THREADS, 1)
+fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constant__ CUtensorMap map_c, const GemmParams P)
+{
+    using L = GemmLayout<BN>;
+    constexpr int STAGES = L::STAGES, NACC = L::NACC, CW = L::CW;
+    constexpr uint32_t IDESC = idesc_e4m3(BN);
+
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    float *scale_buf = (float *)(smem + STAGES * L::STAGE_BYTES);
+    uint64_t *bars = (uint64_t *)(smem + STAGES * L::STAGE_BYTES + L::SCALE_BYTES);
+    uint32_t *tmem_slot = (uint32_t *)(bars + 2 * MAX_STAGES + 2 * MAX_ACC);
+    volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t full0 = smem_u32(bars), empty0 = smem_u32(bars + MAX_STAGES);
+    const uint32_t tfull0 = smem_u32(bars + 2 * MAX_STAGES), tempty0 = smem_u32(bars + 2 * MAX_STAGES + MAX_ACC);
+
+    pdl_launch_dependents();
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
+        for (int a = 0; a < NACC; ++a) { mbar_init(tfull0 + 8 * a, 1); mbar_init(tempty0 + 8 * a, L::NEPI); }
+        *abort_flag = 0;
+        mbar_init_fence();
+    }
+    if (warp == 1) tmem_alloc(smem_u32(tmem_slot), L::TMEM_COLS);
+    pdl_wait();                 // everything above touched shared and tensor memory only
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_slot;
+
+    // with splits > 1 the grid is tiles * splits CTAs and each has one (tile, split); otherwise it walks over tiles
+    const int S = P.splits;
+    const uint32_t rank = S > 1 ? cluster_rank() : 0u;
+    const int64_t tile0 = S > 1 ? blockIdx.x / S : blockIdx.x;
+    const int64_t tile_step = S > 1 ? P.tiles : gridDim.x;
+    const int kb0 = (int)((int64_t)P.kblocks * rank / S), kb1 = (int)((int64_t)P.kblocks * (rank + 1) / S);
+
+    if (warp == 0) {
+        // ------------------------------------------------------------------ TMA producer
+        if (lane == 0) {
+            int stage = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            for (int64_t tile = tile0; tile < P.tiles && ok; tile += tile_step) {
+                const int l0 = (int)(tile / P.nc) * 128, c0 = (int)(tile % P.nc) * BN;
+                for (int kb = kb0; kb < kb1; ++kb) {
+                    if (!mbar_wait(empty0 + 8 * stage, phase ^ 1, abort_flag)) { ok = false; break; }
+                    const uint32_t fb = full0 + 8 * stage;
+                    mbar_expect_tx(fb, L::STAGE_BYTES);
+                    const uint32_t sa = smem_u32(smem + stage * L::STAGE_BYTES);
+                    tma_load_2d(sa, &map_l, fb, kb * KB, l0);
+                    tma_load_2d(sa + L::A_BYTES, &map_c, fb, kb * KB, c0);
+                    if (++stage == STAGES) { stage = 0; phase ^= 1; }
+                }
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        // ------------------------------------------------------------------ MMA issuer
+        if (lane == 0) {
+            int stage = 0;
+            uint32_t phase = 0, acc = 0, acc_phase = 0;
+            bool ok = true;
+            for (int64_t tile = tile0; tile < P.tiles && ok; tile += tile_step) {
+                for (int kb = kb0; kb < kb1; ++kb) {
+                    if (!mbar_wait(tempty0 + 8 * acc, acc_phase ^ 1, abort_flag)) { ok = false; break; }
+                    if (!mbar_wait(full0 + 8 * stage, phase, abort_flag)) { ok = false; break; }
+                    tc_fence_after();
+                    const uint32_t sa = smem_u32(smem + stage * L::STAGE_BYTES);
+                    const uint64_t da = make_desc(sa, 0, 8 * KB, 2), dc = make_desc(sa + L::A_BYTES, 0, 8 * KB, 2);
+#pragma unroll
+                    for (int k = 0; k < KB / 32; ++k)        // 32 codes = 32 bytes = 2 descriptor address units
+                        umma_fp8(tmem_base + acc * BN, da + 2 * k, dc + 2 * k, IDESC, k ? 1u : 0u);
+                    umma_commit(empty0 + 8 * stage);         // frees the stage once these MMAs have read it
+                    umma_commit(tfull0 + 8 * acc);           // the block's sums are complete
+                    if (++stage == STAGES) { stage = 0; phase ^= 1; }
+                    if (++acc == NACC) { acc = 0; acc_phase ^= 1; }
+                }
+            }
+        }
+        __syncwarp();
+    } else {
+        // ------------------------------------------------------------------ promotion
+        const int q = warp & 3, half = (warp - 2) >> 2;                    // lane quarter and column part of this warp
+        const int lane_row = q * 32 + lane;
+        float *sbuf = scale_buf + (warp - 2) * 2 * CW;
+        uint32_t acc = 0, acc_phase = 0;
+        bool ok = true;
+        for (int64_t tile = tile0; tile < P.tiles; tile += tile_step) {
+            const int64_t row = (tile / P.nc) * 128 + lane_row;
+            const int col0 = (int)(tile % P.nc) * BN, cbase = col0 + half * CW;
+            const bool row_in = row < P.rows_l;
+            const float *slp = P.sl + (P.tile_l ? row / 128 : row);
+            const float *scp = P.sc + (P.tile_c ? cbase / 128 : cbase);
+            const bool c_in = cbase < P.rows_c;
+            constexpr int NS = COLVEC ? (CW + 31) / 32 : 1;
+            float sl_next = 0.f, sc_next[NS];
+            auto load_scales = [&](int kb) {
+                sl_next = row_in ? __ldg(slp + (int64_t)kb * P.pl) : 0.f;
+                if constexpr (COLVEC) {
+#pragma unroll
+                    for (int i = 0; i < NS; ++i) {
+                        const int j = i * 32 + lane;
+                        sc_next[i] = (j < CW && cbase + j < P.rows_c) ? __ldg(scp + (int64_t)kb * P.pc + j) : 0.f;
+                    }
+                } else {
+                    sc_next[0] = c_in ? __ldg(scp + (int64_t)kb * P.pc) : 0.f;
+                }
+            };
+            f32x2 sum[CW / 2];
+#pragma unroll
+            for (int i = 0; i < CW / 2; ++i) sum[i] = 0ull;
+            load_scales(kb0);
+            for (int kb = kb0; kb < kb1; ++kb) {
+                float s = sl_next;
+                float *sb = sbuf + (kb & 1) * CW;
+                if constexpr (COLVEC) {
+#pragma unroll
+                    for (int i = 0; i < NS; ++i) if (i * 32 + lane < CW) sb[i * 32 + lane] = sc_next[i];
+                    __syncwarp();                               // the buffer of block kb - 2 has been read by every lane
+                } else {
+                    s *= sc_next[0];
+                }
+                if (kb + 1 < kb1) load_scales(kb + 1);
+                const f32x2 s2 = pack2(__float_as_uint(s), __float_as_uint(s));
+                ok = ok && __all_sync(0xffffffffu, mbar_wait(tfull0 + 8 * acc, acc_phase, abort_flag));
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t trow = tmem_base + ((uint32_t)(q * 32) << 16) + acc * BN + half * CW;
+                uint32_t r[2][16];
+                tmem_ld_x16(trow, r[0]);
+#pragma unroll
+                for (int c = 0; c < CW / 16; ++c) {
+                    tmem_ld_wait();
+                    if (c + 1 < CW / 16) tmem_ld_x16(trow + (c + 1) * 16, r[(c + 1) & 1]);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        f32x2 v = pack2(r[c & 1][2 * j], r[c & 1][2 * j + 1]);
+                        if constexpr (COLVEC) v = mul2(v, *reinterpret_cast<const f32x2 *>(sb + c * 16 + 2 * j));
+                        sum[c * 8 + j] = fma2(v, s2, sum[c * 8 + j]);
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(tempty0 + 8 * acc);
+                if (++acc == NACC) { acc = 0; acc_phase ^= 1; }
+            }
+            if (S == 1) {
+                if (!ok) break;
+#pragma unroll
+                for (int c = 0; c < CW / 16; ++c) {
+                    float v[16];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) unpack2(sum[c * 8 + j], v[2 * j], v[2 * j + 1]);
+                    finish<16>(P, row, cbase + c * 16, v);
+                }
+            } else {
+                // every stage of this CTA has been read: its memory takes the parts, [column][lane row]
+                float *part = (float *)smem;
+#pragma unroll
+                for (int j = 0; j < CW / 2; ++j) {
+                    float a, b;
+                    unpack2(sum[j], a, b);
+                    part[(half * CW + 2 * j) * 128 + lane_row] = a;
+                    part[(half * CW + 2 * j + 1) * 128 + lane_row] = b;
+                }
+            }
+        }
+        if (lane == 0 && !ok && P.status) atomicExch(P.status, (int)LAMP_ERR_TIMEOUT);
+    }
+    __syncwarp();
+    if (S > 1) {
+        cluster_sync_all();
+        if (warp >= 2) {
+            const int q = warp & 3, half = (warp - 2) >> 2, lane_row = q * 32 + lane;
+            const int64_t row = (tile0 / P.nc) * 128 + lane_row;
+            const int col0 = (int)(tile0 % P.nc) * BN;
+            const uint32_t base = smem_u32(smem);
+            if (S == 2) reduce_parts<CW, 2>(P, base, lane_row, row, half * CW, col0, rank);
+            else if (S == 4) reduce_parts<CW, 4>(P, base, lane_row, row, half * CW, col0, rank);
+            else reduce_parts<CW, 8>(P, base, lane_row, row, half * CW, col0, rank);
+        }
+        cluster_sync_all();      // no CTA leaves while a peer still reads its parts
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 1) tmem_dealloc(tmem_base, L::TMEM_COLS);
+}
+
+bool encode_operand(const lamp_fp8_operand_t *o, int box_rows, CUtensorMap *map)
+{
+    PFN_cuTensorMapEncodeTiled_v12000 enc = (PFN_cuTensorMapEncodeTiled_v12000)tensor_map_encoder();
+    if (!enc) return false;
+    const cuuint64_t gdim[2] = {(cuuint64_t)o->k, (cuuint64_t)o->rows};
+    const cuuint64_t gstride[1] = {(cuuint64_t)o->q_pitch};
+    const cuuint32_t box[2] = {(cuuint32_t)KB, (cuuint32_t)box_rows};
+    const cuuint32_t es[2] = {1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, o->q, gdim, gstride, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int BN, bool COLVEC>
+lamp_status_t launch(const lamp_fp8_operand_t *l, const lamp_fp8_operand_t *c, const GemmParams &P, cudaStream_t st)
+{
+    using L = GemmLayout<BN>;
+    CUtensorMap ml, mc;
+    if (!encode_operand(l, 128, &ml) || !encode_operand(c, BN, &mc)) return LAMP_ERR_CUDA;
+    static SmemAttrOnce attr;
+    { const lamp_status_t as = attr.ensure(fp8_gemm_kernel<BN, COLVEC>, (int)L::TOTAL); if (as != LAMP_OK) return as; }
+    const int sms = sm_count();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(P.splits > 1 ? (unsigned)(P.tiles * P.splits) : (unsigned)(P.tiles < sms ? P.tiles : sms));
+    cfg.blockDim = dim3(L::THREADS);
+    cfg.dynamicSmemBytes = L::TOTAL;
+    cfg.stream = st;
+    cudaLaunchAttribute at[2];
+    int na = 0;
+    if (P.tiles <= 4 * (int64_t)sms) {
+        at[na].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at[na++].val.programmaticStreamSerializationAllowed = 1;
+    }
+    if (P.splits > 1) {
+        at[na].id = cudaLaunchAttributeClusterDimension;
+        at[na].val.clusterDim.x = P.splits;
+        at[na].val.clusterDim.y = 1;
+        at[na++].val.clusterDim.z = 1;
+    }
+    cfg.attrs = at;
+    cfg.numAttrs = na;
+    return cudaLaunchKernelEx(&cfg, fp8_gemm_kernel<BN, COLVEC>, ml, mc, P) == cudaSuccess ? LAMP_OK : LAMP_ERR_CUDA;
+}
+
+template <int BN>
+lamp_status_t launch_cv(const lamp_fp8_operand_t *l, const lamp_fp8_operand_t *c, const GemmParams &P, cudaStream_t st)
+{
+    return c->tile_scale ? launch<BN, false>(l, c, P, st) : launch<BN, true>(l, c, P, st);
+}
+
+}  // namespace
+
+lamp_status_t check_fp8_operand(const lamp_fp8_operand_t *o)
+{
+    if (!o || o->rows < 0 || o->k < 0) return LAMP_ERR_INVALID_ARG;
+    if (o->tile_scale != 0 && o->tile_scale != 1) return LAMP_ERR_INVALID_ARG;
+    if (o->rows > 2147483647ll - 256 || o->k > 2147483647ll - 256) return LAMP_ERR_UNSUPPORTED;
+    if (o->q_pitch < o->k || (o->q_pitch & 15) || o->scale_pitch < (o->tile_scale ? (o->rows + 127) / 128 : o->rows)) return LAMP_ERR_INVALID_ARG;
+    if ((double)o->rows * (double)o->q_pitch > 1099511627776.0) return LAMP_ERR_UNSUPPORTED;       // 2^40 B
+    if ((double)o->scale_pitch * (double)((o->k + 127) / 128) > 1099511627776.0 / 4) return LAMP_ERR_UNSUPPORTED;
+    if (o->rows == 0 || o->k == 0) return LAMP_OK;
+    if (!o->q || !o->scale || ((uintptr_t)o->q & 15) || ((uintptr_t)o->scale & 3)) return LAMP_ERR_INVALID_ARG;
+    return LAMP_OK;
+}
+
+}  // namespace lamp
+
+using namespace lamp;
+
+extern "C" lamp_status_t lamp_gemm_fp8(const lamp_fp8_operand_t *a, const lamp_fp8_operand_t *b, const float *bias, lamp_tensor_t *y,
+                                       void *cuda_stream)
+{
+    lamp_status_t s;
+    if ((s = check_fp8_operand(a)) != LAMP_OK || (s = check_fp8_operand(b)) != LAMP_OK) return s;
+    if ((s = check_view(y, true)) != LAMP_OK) return s;
+    if (a->k != b->k || a->k == 0 || voxels(y) != a->rows || (int64_t)y->c != b->rows || ((uintptr_t)bias & 3)) return LAMP_ERR_INVALID_ARG;
+    if (a->rows == 0) return LAMP_OK;
+    const TView v = make_view(y);
+
+    GemmParams P = {};
+    const bool swap = a->rows <= 64 && b->rows > a->rows;
+    const lamp_fp8_operand_t *l = swap ? b : a, *c = swap ? a : b;
+    P.rows_l = (int32_t)l->rows; P.rows_c = (int32_t)c->rows;
+    P.kblocks = (int32_t)((a->k + KB - 1) / KB);
+    P.sl = l->scale; P.sc = c->scale; P.pl = l->scale_pitch; P.pc = c->scale_pitch;
+    P.tile_l = l->tile_scale; P.tile_c = c->tile_scale;
+    P.bias = bias; P.y = v.p; P.y_pitch = v.pitch; P.y_f32 = v.f32; P.swap = swap;
+    const size_t es = v.f32 ? 4 : 2;
+    const uintptr_t mis = (uintptr_t)v.p | (uintptr_t)(v.pitch * es);
+    P.vec = (mis & 31) == 0 ? 2 : (mis & 15) == 0 ? 1 : 0;
+    P.status = status_word_ptr();
+    const int sms = sm_count();
+    P.nl = (P.rows_l + 127) / 128;
+    int bn = P.rows_c <= 16 ? 16 : P.rows_c <= 32 ? 32 : P.rows_c <= 64 ? 64 : 128;
+    if (P.rows_c > 128 && (int64_t)P.nl * ((P.rows_c + 255) / 256) >= sms) bn = 256;
+    P.nc = (P.rows_c + bn - 1) / bn;
+    P.tiles = (int64_t)P.nl * P.nc;
+    P.splits = 1;
+    while (P.splits < 8 && P.tiles * P.splits * 2 <= sms && P.kblocks >= 4 * P.splits) P.splits *= 2;
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    switch (bn) {
+    case 16: return launch_cv<16>(l, c, P, st);
+    case 32: return launch_cv<32>(l, c, P, st);
+    case 64: return launch_cv<64>(l, c, P, st);
+    case 128: return launch_cv<128>(l, c, P, st);
+    default: return launch_cv<256>(l, c, P, st);
+    }
+}
