@@ -279,14 +279,15 @@ lamp_status_t lamp_block_norm_bwd(const lamp_block_norm_t *p, const lamp_tensor_
 /* ------------------------------------------------------------------------
  * Distillation from a teacher's top logits: the loss that trains a narrow network on what a wide one answered, beside the
  * softmax-Dice loss on labels.  (No passage of the paper; it trains networks of 32, 64 and 128 filters on one task.)
- * z: the student's logits, one row of c classes per voxel (bf16 or fp32; any c, c_pitch, c_offset).  Of the teacher, k listed
+ * z: the student's logits, one row of c classes per voxel (bf16 or fp32; c <= 400000 or 200000; any c_pitch, c_offset).  Of the teacher, k listed
  * classes per row: index idx[row][k] and logit logits[row][k] (fp32).  With T = temperature,
  *     p_j = exp(logits_j / T - lse),  lse = log sum_j exp(logits_j / T) over the listed classes, or the teacher's own log-sum
  *           over all its classes, lse[row] (of logits / T), where the list leaves out mass that should not be spread;
  *     q_i = exp(z_i / T) / sum_i exp(z_i / T) over all c classes;
  *     loss_row = T^2 sum_j p_j (log p_j - log q_{idx_j}),      dloss_row / dz_i = T (q_i sum_j p_j - sum_{j: idx_j = i} p_j).
  * Entries with idx outside [0, c) are absent; p_j = 0 contributes 0; the same class listed twice counts twice.  A row
- * with no entry left (none listed, or all logits -inf) has loss 0 and gradient 0.  The class with z = -inf has q = 0.
+ * with no entry left (none listed, or all logits -inf) has loss, log-sum and gradient 0.  A class with z = -inf has q = 0; a
+ * row of nothing but -inf has no softmax and gives NaN.
  * row_weight: fp32 [rows], or NULL for 1 / rows each.  Rows of weight 0 are not read: their loss, log-sum and gradient are 0.
  * Sums are held in fp32 (log-sums, losses of a row) and fp64 (over rows), in a fixed order.
  * ---------------------------------------------------------------------- */

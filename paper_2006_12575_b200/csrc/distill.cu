@@ -1,19 +1,21 @@
 // Distillation loss from a teacher's top logits, and its gradient:
 //   loss_r = T^2 sum_j p_j (log p_j - log q_{idx_j}),   dloss_r/dz_i = T (q_i S - sum_{j: idx_j = i} p_j),   S = sum_j p_j.
-// Bound by memory: a row of c logits is read once (running maximum and sum of the softmax in one pass) and its gradient
-// written once.  The exponentials are taken in base 2 relative to the row's maximum m: e_i = 2^(z_i log2(e) / T - m), so
-// that q_i = e_i / sum e is as exact as fp32 allows whatever the size of the logits.
+// Bound by memory: a row of c logits is read once and its gradient written once.  The exponentials are taken relative to
+// the row's maximum, with the difference formed first, so q is as exact as fp32 allows whatever the size of the logits.
 // The gradient of a listed class is the difference of two numbers that training makes nearly equal, so it is formed in
 // fp32 and rounded once: the dense pass writes q_i S everywhere, then the owner of each listed class overwrites it.
 // A class listed twice subtracts both probabilities (each of its entries writes the same value).
 //
 // Rows of odd length start at any element, so a row is walked in 16-byte units aligned in memory; a unit that is not
 // wholly inside the row is handled element by element.
-//   c <= 1024: one warp per row, the row stays in registers.
-//   wider:     one CTA per row, or, where rows are few, a cluster of up to 8 CTAs that share the row and exchange maximum and
-//              sum through distributed shared memory.  The row is kept in shared memory as far as it fits and read again
-//              (from L2) beyond that.
+//   c <= 32 (k <= 32): one thread per row, 256 rows at a time through shared memory.
+//   c <= 1024:         one warp per row, the row stays in registers.
+//   wider:             one CTA per row, or a cluster of up to 8 CTAs where a row does not fit in the shared memory of one or
+//                      rows are few; they exchange maximum and sum through distributed shared memory.
+#include <cuda.h>
+#include <float.h>
 #include "common.cuh"
+#include "umma_ptx.cuh"
 
 namespace lamp {
 
@@ -22,9 +24,8 @@ namespace {
 constexpr int FWD = 1, BWD = 2;
 constexpr int MAX_PARTS = 4096;                     // partial losses, one per CTA (or cluster)
 constexpr int MAX_K = 1024;
-constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float LOG2E = 1.4426950408889634f;
 constexpr int WR_WARPS = 8, WR_MAX_C = 1024;
-constexpr int CR_THREADS = 512;
 
 struct DistillParams {
     const void *z;
@@ -38,7 +39,8 @@ struct DistillParams {
     const float *lse_in;
     float *loss_rows, *lse_out;
     double *part;                                   // one partial loss per CTA or cluster, or NULL
-    int32_t stash;                                  // 16-byte units of a row slice kept in shared memory (CTA form)
+    int32_t stash;                                  // 16-byte units of a buffer (CTA form)
+    int *status;
 };
 
 template <bool F32> struct Elem {
@@ -100,21 +102,27 @@ __device__ __forceinline__ void store_unit(void *dz, int64_t at, int off, bool s
     }
 }
 
-// running maximum m (base 2 exponent) and sum s of 2^(x - m)
-__device__ __forceinline__ void join(float &m, float &s, float m2, float s2)
+// 2^x; results below the normal range become 0
+__device__ __forceinline__ float ex2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// (m, s) = maximum of z and sum of e^((z - m) / T) of two parts.  m starts at -FLT_MAX, not -inf, so that no difference of
+// infinities arises; the difference is taken before the change of base, which also holds where z log2(e) would overflow
+// (rows masked with the type's lowest value).
+__device__ __forceinline__ void join(float &m, float &s, float m2, float s2, float c2)
 {
     const float n = fmaxf(m, m2);
-    // a side that is empty (-inf) contributes nothing; its exponent would be -inf - -inf
-    s = (m == -INFINITY ? 0.f : s * exp2f(m - n)) + (m2 == -INFINITY ? 0.f : s2 * exp2f(m2 - n));
-    // NaN anywhere makes the row NaN
-    if (m != m || m2 != m2) s = NAN;
+    s = s * ex2((m - n) * c2) + s2 * ex2((m2 - n) * c2);
     m = n;
 }
-// e^(z / T) relative to the reference m: 2^(z c - m) with c = log2(e) / T and m the row's maximum in base 2, or, from a given
-// log-sum m, e^(z c - m) with c = 1 / T (the difference is formed before the change of base, which keeps its digits)
-template <int MODE> __device__ __forceinline__ float power(float z, float c, float m)
+// e^(z / T) relative to the reference m: the row's maximum of z, or, where only the gradient is asked for, the log-sum of z / T
+template <int MODE> __device__ __forceinline__ float power(float z, float c2, float inv_t, float m)
 {
-    return (MODE & FWD) ? exp2f(fmaf(z, c, -m)) : exp2f(fmaf(z, c, -m) * LOG2E);
+    return (MODE & FWD) ? ex2((z - m) * c2) : ex2(fmaf(z, inv_t, -m) * LOG2E);
 }
 __device__ __forceinline__ float warp_max(float v)
 {
@@ -128,19 +136,8 @@ __device__ __forceinline__ float warp_sum(float v)
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
-__device__ __forceinline__ void warp_join(float &m, float &s)
-{
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        const float m2 = __shfl_xor_sync(0xffffffffu, m, o), s2 = __shfl_xor_sync(0xffffffffu, s, o);
-        join(m, s, m2, s2);
-    }
-}
-
-// One warp reads the teacher's entries of a row: ids (-1: absent), log p and z / T's numerator to shared memory; returns S
-// (0: no entry left).
-template <bool F32>
-__device__ __forceinline__ float teacher_row(const DistillParams &P, int64_t row, int64_t at, int lane, int lo, int hi, int *ids, float *logp, float *zt)
+// One warp reads the teacher's entries of a row: ids (-1: absent) and log p to shared memory; returns S (0: no entry left).
+__device__ __forceinline__ float teacher_row(const DistillParams &P, int64_t row, int lane, int *ids, float *logp)
 {
     const float inv_t = 1.f / P.temp;
     float m = -INFINITY;
@@ -151,7 +148,6 @@ __device__ __forceinline__ float teacher_row(const DistillParams &P, int64_t row
         const float v = id >= 0 ? P.t[row * P.k + j] * inv_t : -INFINITY;
         ids[j] = id;
         logp[j] = v;
-        zt[j] = id >= lo && id < hi ? elem<F32>(P.z, at + id) : 0.f;      // before anything is written (dz may be z)
         nan |= v != v;
         m = fmaxf(m, v);
     }
@@ -160,7 +156,7 @@ __device__ __forceinline__ float teacher_row(const DistillParams &P, int64_t row
     if (P.tlse) {
         lse = P.tlse[row];
     } else {
-        float mm = warp_max(m);
+        const float mm = warp_max(m);
         if (mm == -INFINITY && !nan) return 0.f;
         float s = 0.f;
         for (int j = lane; j < P.k; j += 32) s += expf(logp[j] - mm);
@@ -189,7 +185,7 @@ distill_warp_kernel(const DistillParams P)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     int *ids = smem_i + warp * 3 * P.k;
     float *logp = (float *)(ids + P.k), *zt = logp + P.k;
-    const float c2 = (MODE & FWD) ? LOG2E / P.temp : 1.f / P.temp;
+    const float c2 = LOG2E / P.temp, inv_t = 1.f / P.temp;
     double total = 0;
     pdl_launch_dependents();
     pdl_wait();
@@ -201,40 +197,40 @@ distill_warp_kernel(const DistillParams P)
         const int nu = (P.c + off + E - 1) / E;
         float S = 0.f;
         __syncwarp();
-        if (w != 0.f) S = teacher_row<F32>(P, row, at, lane, 0, P.c, ids, logp, zt);
+        if (w != 0.f) S = teacher_row(P, row, lane, ids, logp);
+        if (S != 0.f)                                               // before anything is written: dz may be z
+            for (int j = lane; j < P.k; j += 32) zt[j] = ids[j] >= 0 ? elem<F32>(P.z, at + ids[j]) : 0.f;
         float loss = 0.f, lse = 0.f;
         if (S != 0.f) {
             uint4 raw[NU];
-            float m = -INFINITY, s = 0.f;
+            float m = -FLT_MAX, s = 0.f;
 #pragma unroll
             for (int i = 0; i < NU; ++i) if (lane + 32 * i < nu) raw[i] = load_unit<F32>(P.z, at, off, lane + 32 * i, P.c);
-            float scale;                                            // 1 / sum, relative to 2^m
+            float scale;                                            // 1 / sum, relative to the maximum
             if constexpr (MODE & FWD) {
 #pragma unroll
                 for (int i = 0; i < NU; ++i) if (lane + 32 * i < nu) {
                     float v[E];
                     unit_values<F32>(raw[i], v);
 #pragma unroll
-                    for (int j = 0; j < E; ++j) m = v[j] != v[j] || m != m ? NAN : fmaxf(m, v[j]);
+                    for (int j = 0; j < E; ++j) m = fmaxf(m, v[j]);
                 }
-                // maximum over the warp, NaN kept
-                const bool bad = __any_sync(0xffffffffu, m != m);
-                m = bad ? NAN : warp_max(m);
-                m *= c2;
+                m = warp_max(m);
 #pragma unroll
                 for (int i = 0; i < NU; ++i) if (lane + 32 * i < nu) {
                     float v[E];
                     unit_values<F32>(raw[i], v);
 #pragma unroll
-                    for (int j = 0; j < E; ++j) s += exp2f(fmaf(v[j], c2, -m));
+                    for (int j = 0; j < E; ++j) s += ex2((v[j] - m) * c2);
                 }
                 s = warp_sum(s);
-                const float l2 = log2f(s);
-                lse = (m + l2) * LN2;
+                if (s == 0.f) s = NAN;                              // no logit above -inf: there is no softmax
+                const float ls = logf(s);
+                lse = m * inv_t + ls;
                 scale = 1.f / s;
                 for (int j = lane; j < P.k; j += 32) {
                     const float p = ids[j] >= 0 ? expf(logp[j]) : 0.f;
-                    if (p != 0.f) loss += p * (logp[j] - LN2 * (fmaf(zt[j], c2, -m) - l2));
+                    if (p != 0.f) loss += p * (logp[j] - ((zt[j] - m) * inv_t - ls));
                 }
                 loss = warp_sum(loss) * P.temp * P.temp;
             } else {
@@ -248,7 +244,7 @@ distill_warp_kernel(const DistillParams P)
                     float v[E];
                     unit_values<F32>(raw[i], v);
 #pragma unroll
-                    for (int j = 0; j < E; ++j) v[j] = gq * power<MODE>(v[j], c2, m);
+                    for (int j = 0; j < E; ++j) v[j] = gq * power<MODE>(v[j], c2, inv_t, m);
                     store_unit<F32>(P.dz, dat, off, same, lane + 32 * i, P.c, v);
                 }
                 __syncwarp();
@@ -256,7 +252,7 @@ distill_warp_kernel(const DistillParams P)
                     if (ids[j] < 0) continue;
                     float p = 0.f;
                     for (int i = 0; i < P.k; ++i) if (ids[i] == ids[j]) p += expf(logp[i]);
-                    put<F32>(P.dz, dat + ids[j], gT * (S * (scale * power<MODE>(zt[j], c2, m)) - p));
+                    put<F32>(P.dz, dat + ids[j], gT * (S * (scale * power<MODE>(zt[j], c2, inv_t, m)) - p));
                 }
             }
         } else if constexpr (MODE & BWD) {
@@ -287,141 +283,455 @@ distill_warp_kernel(const DistillParams P)
 // ----------------------------------------------------------------------------------------------------------------------
 // one CTA, or a cluster of CTAs, per row
 // ----------------------------------------------------------------------------------------------------------------------
+// Warp-specialised, two buffers: while the consumer warps work on a row (or this CTA's slice of it) in one half of shared
+// memory, the helper warp has the next row copied into the other half (one bulk asynchronous copy of its whole 16-byte units; the
+// ragged first and last unit by hand, filled up with -inf) and prepares that row's teacher entries.  So the copy, the
+// teacher's latency chain and the arithmetic of consecutive rows overlap, and a row is read from HBM exactly once.
 __device__ __forceinline__ void cluster_barrier()
 {
     asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
 }
-__device__ __forceinline__ float peer_f32(const float *p, uint32_t rank)
+// Barrier of the consumer warps.  An mbarrier with a bounded wait, not a hardware barrier: a warp that gave up must not leave
+// the others waiting for it.
+__device__ __forceinline__ bool consumer_sync(uint32_t bar, uint32_t &phase, int lane, volatile int *abort_flag)
 {
-    uint32_t a = (uint32_t)__cvta_generic_to_shared(p), b;
-    float v;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(b) : "r"(a), "r"(rank));
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(b) : "memory");
-    return v;
+    __syncwarp();
+    if (lane == 0) ptx::mbar_arrive(bar);
+    const bool ok = __all_sync(0xffffffffu, ptx::mbar_wait(bar, phase, abort_flag));
+    phase ^= 1;
+    return ok;
 }
 
-template <bool F32, int MODE>
-__global__ void __launch_bounds__(CR_THREADS)
-distill_cta_kernel(const DistillParams P, int S_CTAS)
+struct RowSlot {                                    // what the helper prepares for a row
+    float S, w;
+};
+
+__device__ __forceinline__ void st_async_v4(uint32_t addr, uint32_t bar, float a, float b, float c, float d)
 {
-    constexpr int E = Elem<F32>::E, NW = CR_THREADS / 32;
-    extern __shared__ uint4 stash[];
-    int *ids = (int *)(stash + P.stash);
-    float *logp = (float *)(ids + P.k), *zt = logp + P.k;
-    __shared__ float red[2][NW], sh_S, sh_ms[2], sh_loss;
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%2, %3, %4, %5}, [%1];"
+                 ::"r"(addr), "r"(bar), "r"(__float_as_uint(a)), "r"(__float_as_uint(b)), "r"(__float_as_uint(c)), "r"(__float_as_uint(d)) : "memory");
+}
+__device__ __forceinline__ uint32_t peer_addr(uint32_t addr, uint32_t rank)
+{
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+
+// largest element of a unit
+template <bool F32> __device__ __forceinline__ float unit_max(const uint4 &r)
+{
+    if constexpr (F32) {
+        return fmaxf(fmaxf(__uint_as_float(r.x), __uint_as_float(r.y)), fmaxf(__uint_as_float(r.z), __uint_as_float(r.w)));
+    } else {
+        const __nv_bfloat162 *h = reinterpret_cast<const __nv_bfloat162 *>(&r);
+        const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+        return fmaxf(__low2float(m), __high2float(m));
+    }
+}
+
+// sum over a unit of e^((z - m) / T)
+template <bool F32> __device__ __forceinline__ float unit_sum(const uint4 &r, float c2, float m, float mc, bool plain)
+{
+    constexpr int E = Elem<F32>::E;
+    float v[E], a = 0.f, b = 0.f;
+    unit_values<F32>(r, v);
+#pragma unroll
+    for (int j = 0; j < E; j += 2) {
+        a += ex2(plain ? fmaf(v[j], c2, -mc) : (v[j] - m) * c2);
+        b += ex2(plain ? fmaf(v[j + 1], c2, -mc) : (v[j + 1] - m) * c2);
+    }
+    return a + b;
+}
+
+constexpr int CR_MAX_THREADS = 1024;
+
+template <bool F32, int MODE>
+__global__ void __launch_bounds__(CR_MAX_THREADS, 1)
+distill_cta_kernel(const DistillParams P, const int S_CTAS)
+{
+    constexpr int E = Elem<F32>::E;
+    extern __shared__ __align__(16) uint4 buf[];                       // [2][P.stash] units, then the lists [2][3][k]
+    __shared__ __align__(16) float4 msg[2][8];                         // per row parity: (maximum, sum, D, P) of every CTA of the cluster
+    __shared__ __align__(8) uint64_t bars[7];                          // full[2], empty[2], exchange[2], consumers
+    __shared__ float red[2][32];
+    __shared__ RowSlot slot[2];
+    __shared__ int abort_s;
+    volatile int *abort_flag = &abort_s;
+    int *ids0 = (int *)(buf + 2 * P.stash);
+    const int nthr = blockDim.x - 32, nwarp = nthr >> 5;               // consumers; the last warp is the helper
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const float c2 = (MODE & FWD) ? LOG2E / P.temp : 1.f / P.temp;
-    const int rank = S_CTAS > 1 ? (int)(blockIdx.x % S_CTAS) : 0;
+    const float c2 = LOG2E / P.temp, inv_t = 1.f / P.temp;
+    const uint32_t rank = S_CTAS > 1 ? blockIdx.x % S_CTAS : 0;
     const int64_t first = blockIdx.x / S_CTAS, step = gridDim.x / S_CTAS;
+    const uint32_t full0 = ptx::smem_u32(bars), empty0 = full0 + 16, exch0 = full0 + 32, cons = full0 + 48;
+    pdl_launch_dependents();
+    if (tid == 0) {
+        for (int b = 0; b < 2; ++b) {
+            ptx::mbar_init(full0 + 8 * b, 2);
+            ptx::mbar_init(empty0 + 8 * b, nwarp);
+            ptx::mbar_init(exch0 + 8 * b, 1);
+        }
+        ptx::mbar_init(cons, nwarp);
+        abort_s = 0;
+        ptx::mbar_init_fence();
+    }
+    __syncthreads();
+    if (S_CTAS > 1) cluster_barrier();                                 // every peer's barriers exist
+    pdl_wait();
+    // a row's units, and the slice of them that this CTA has
+    auto geometry = [&](int64_t row, int &off, int &nu, int &u0, int &u1) {
+        off = misalign<F32>(P.z, row * P.pz);
+        nu = (P.c + off + E - 1) / E;
+        u0 = (int)((int64_t)nu * rank / S_CTAS);
+        u1 = (int)((int64_t)nu * (rank + 1) / S_CTAS);
+    };
+    bool ok = true;
+    double total = 0;
+    if (warp == nwarp) {
+        // ------------------------------------------------------------------ helper
+        int i = 0;
+        for (int64_t row = first; row < P.rows; row += step, ++i) {
+            const int b = i & 1;
+            const uint32_t ph = (uint32_t)(i >> 1) & 1;
+            const float w = P.w ? P.w[row] : P.w_all;
+            int *ids = ids0 + b * 3 * P.k;
+            float *logp = (float *)(ids + P.k), *pm = logp + P.k;
+            ok = __all_sync(0xffffffffu, ptx::mbar_wait(empty0 + 8 * b, ph ^ 1, abort_flag));
+            if (!ok) break;
+            float S = 0.f;
+            if (w != 0.f) {
+                int off, nu, u0, u1;
+                geometry(row, off, nu, u0, u1);
+                const int64_t at = row * P.pz;
+                // whole units of the slice: not the first if it starts in front of the row, not the last if it ends behind it
+                const int f0 = u0 == 0 && off ? 1 : u0, f1 = u1 == nu && (P.c + off) % E ? nu - 1 : u1;
+                uint4 *dst = buf + b * P.stash;
+                if (lane == 0) {
+                    ptx::fence_proxy_async();                          // the buffer's last readers, then the copy
+                    if (f1 > f0) {
+                        ptx::mbar_expect_tx(full0 + 8 * b, (uint32_t)(f1 - f0) * 16);
+                        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                                     ::"r"(ptx::smem_u32(dst + (f0 - u0))), "l"((const char *)P.z + ((at + (int64_t)f0 * E - off) << Elem<F32>::SHIFT)),
+                                       "r"((uint32_t)(f1 - f0) * 16), "r"(full0 + 8 * b) : "memory");
+                    } else {
+                        ptx::mbar_arrive(full0 + 8 * b);
+                    }
+                }
+                if (lane == 1 && f0 > u0 && u1 > u0) dst[0] = load_unit<F32>(P.z, at, off, u0, P.c);
+                if (lane == 2 && f1 < u1 && f1 >= f0) dst[f1 - u0] = load_unit<F32>(P.z, at, off, f1, P.c);
+                S = teacher_row(P, row, lane, ids, logp);
+                // what a listed class loses: its probability, over all entries that name it
+                if ((MODE & BWD) && P.k <= 128 && S != 0.f) {
+                    for (int j = lane; j < P.k; j += 32) {
+                        float p = 0.f;
+                        for (int q = 0; q < P.k; ++q) if (ids[q] == ids[j]) p += expf(logp[q]);
+                        pm[j] = p;
+                    }
+                }
+            } else if (lane == 0) {
+                ptx::mbar_arrive(full0 + 8 * b);
+            }
+            if (lane == 0) { slot[b].S = S; slot[b].w = w; }
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(full0 + 8 * b);
+        }
+    } else {
+        // ------------------------------------------------------------------ consumers
+        int i = 0, ex = 0;                                             // rows, rows with an exchange
+        uint32_t cphase = 0;
+        for (int64_t row = first; row < P.rows; row += step, ++i) {
+            const int b = i & 1;
+            const int64_t dat = row * P.pdz;
+            int off, nu, u0, u1;
+            geometry(row, off, nu, u0, u1);
+            const bool same = (MODE & BWD) && off == misalign<F32>(P.dz, dat);
+            const int e0 = u0 * E - off, e1 = u1 * E - off;            // elements of the slice
+            const uint4 *data = buf + b * P.stash;
+            const int *ids = ids0 + b * 3 * P.k;
+            const float *logp = (const float *)(ids + P.k), *pm = logp + P.k;
+            ok = __all_sync(0xffffffffu, ptx::mbar_wait(full0 + 8 * b, (uint32_t)(i >> 1) & 1, abort_flag));
+            if (!ok) break;
+            const float S = slot[b].S, w = slot[b].w;
+            float loss = 0.f, lse = 0.f;
+            if (S != 0.f) {
+                float m, s;                                            // maximum of z, sum of e^((z - m) / T)
+                float scale;
+                if constexpr (MODE & FWD) {
+                    m = -FLT_MAX;                                      // -inf alone: the sum is 0
+                    for (int u = tid; u < u1 - u0; u += nthr) m = fmaxf(m, unit_max<F32>(data[u]));
+                    s = 0.f;
+                    const float mc = m * c2;
+                    if (fabsf(mc) < 1e38f) {
+#pragma unroll 2
+                        for (int u = tid; u < u1 - u0; u += nthr) s += unit_sum<F32>(data[u], c2, m, mc, true);
+                    } else {                                           // the product could overflow: subtract first
+                        for (int u = tid; u < u1 - u0; u += nthr) s += unit_sum<F32>(data[u], c2, m, mc, false);
+                    }
+#pragma unroll
+                    for (int o = 16; o > 0; o >>= 1) join(m, s, __shfl_xor_sync(0xffffffffu, m, o), __shfl_xor_sync(0xffffffffu, s, o), c2);
+                    if (lane == 0) { red[0][warp] = m; red[1][warp] = s; }
+                    if (!(ok = consumer_sync(cons, cphase, lane, abort_flag))) break;
+                    m = lane < nwarp ? red[0][lane] : -FLT_MAX;
+                    s = lane < nwarp ? red[1][lane] : 0.f;
+#pragma unroll
+                    for (int o = 16; o > 0; o >>= 1) join(m, s, __shfl_xor_sync(0xffffffffu, m, o), __shfl_xor_sync(0xffffffffu, s, o), c2);
+                    float D = 0.f, PS = 0.f;                           // sum_j p_j (log p_j - (z_j - m) / T), sum_j p_j over the slice's entries
+                    if (warp == 0) {
+                        for (int j = lane; j < P.k; j += 32) {
+                            const int id = ids[j];
+                            if (id < 0 || id < e0 || id >= e1) continue;
+                            const float p = expf(logp[j]);
+                            if (p != 0.f) { D += p * (logp[j] - (elem<F32>(data, id - e0) - m) * inv_t); PS += p; }
+                        }
+                        D = warp_sum(D); PS = warp_sum(PS);
+                    }
+                    if (S_CTAS > 1) {
+                        const int x = ex & 1;
+                        if (warp == 0) {
+                            if (lane == 0) ptx::mbar_expect_tx(exch0 + 8 * x, 16 * S_CTAS);
+                            __syncwarp();
+                            if (lane < S_CTAS)
+                                st_async_v4(peer_addr(ptx::smem_u32(&msg[x][rank]), lane), peer_addr(exch0 + 8 * x, lane), m, s, D, PS);
+                        }
+                        ok = __all_sync(0xffffffffu, ptx::mbar_wait(exch0 + 8 * x, (uint32_t)(ex >> 1) & 1, abort_flag));
+                        if (!ok) break;
+                        ++ex;
+                        m = -FLT_MAX; s = 0.f;
+                        for (int r = 0; r < S_CTAS; ++r) join(m, s, msg[x][r].x, msg[x][r].y, c2);
+                        D = 0.f;
+                        for (int r = 0; r < S_CTAS; ++r) D += msg[x][r].z + (msg[x][r].w != 0.f ? msg[x][r].w * ((m - msg[x][r].x) * inv_t) : 0.f);
+                        PS = 0.f;
+                        for (int r = 0; r < S_CTAS; ++r) PS += msg[x][r].w;
+                    }
+                    if (s == 0.f) s = NAN;                             // no logit above -inf: there is no softmax
+                    scale = 1.f / s;
+                    const float ls = logf(s);
+                    lse = m * inv_t + ls;
+                    loss = (D + PS * ls) * P.temp * P.temp;
+                } else {
+                    m = P.lse_in[row];
+                    scale = 1.f;
+                }
+                if constexpr (MODE & BWD) {
+                    const float gT = w * P.temp, gq = gT * S * scale;
+                    const float mc = (MODE & FWD) ? m * c2 : m;
+                    if (!(MODE & FWD) || fabsf(mc) < 1e38f) {
+#pragma unroll 2
+                        for (int u = tid; u < u1 - u0; u += nthr) {
+                            float v[E];
+                            unit_values<F32>(data[u], v);
+#pragma unroll
+                            for (int j = 0; j < E; ++j) v[j] = gq * ((MODE & FWD) ? ex2(fmaf(v[j], c2, -mc)) : ex2(fmaf(v[j], inv_t, -m) * LOG2E));
+                            store_unit<F32>(P.dz, dat, off, same, u0 + u, P.c, v);
+                        }
+                    } else {
+                        for (int u = tid; u < u1 - u0; u += nthr) {
+                            float v[E];
+                            unit_values<F32>(data[u], v);
+#pragma unroll
+                            for (int j = 0; j < E; ++j) v[j] = gq * ex2((v[j] - m) * c2);
+                            store_unit<F32>(P.dz, dat, off, same, u0 + u, P.c, v);
+                        }
+                    }
+                    if (!(ok = consumer_sync(cons, cphase, lane, abort_flag))) break;    // the listed classes go over what the dense pass wrote
+                    for (int j = tid; j < P.k; j += nthr) {
+                        const int id = ids[j];
+                        if (id < 0 || id < e0 || id >= e1) continue;
+                        float p = 0.f;
+                        if (P.k <= 128) p = pm[j];
+                        else for (int q = 0; q < P.k; ++q) if (ids[q] == id) p += expf(logp[q]);
+                        put<F32>(P.dz, dat + id, gT * (S * (scale * power<MODE>(elem<F32>(data, id - e0), c2, inv_t, m)) - p));
+                    }
+                }
+            } else if constexpr (MODE & BWD) {
+                float v[E];
+#pragma unroll
+                for (int j = 0; j < E; ++j) v[j] = 0.f;
+                for (int u = u0 + tid; u < u1; u += nthr) store_unit<F32>(P.dz, dat, off, same, u, P.c, v);
+            }
+            if ((MODE & FWD) && rank == 0 && tid == 0) {
+                if (P.loss_rows) P.loss_rows[row] = loss;
+                if (P.lse_out) P.lse_out[row] = lse;
+                if (w != 0.f) total += (double)w * loss;
+            }
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(empty0 + 8 * b);
+        }
+        if ((MODE & FWD) && P.part && rank == 0 && tid == 0) P.part[blockIdx.x / S_CTAS] = total;
+    }
+    if (!ok) {
+        if (lane == 0 && P.status) atomicExch(P.status, (int)LAMP_ERR_TIMEOUT);
+        ptx::settle();                                                 // copies in flight
+    }
+    __syncthreads();
+    if (S_CTAS > 1) cluster_barrier();                                 // no CTA leaves while a peer may still write to it
+}
+
+// ----------------------------------------------------------------------------------------------------------------------
+// one thread per row: few classes (a segmentation network's), many rows
+// ----------------------------------------------------------------------------------------------------------------------
+// 256 rows per turn go through shared memory as fp32, so that global memory sees whole lines although a row is only a few
+// words; the row pitch there is odd, so that the threads of a warp, each on its own row, hit different banks.  A thread
+// adds its gradient up in its own row, listed classes after the dense part, so a class listed twice is simply met twice.
+constexpr int TR_ROWS = 256, TR_MAX_C = 32, TR_MAX_K = 32;
+
+template <bool F32, int MODE, int CP>
+__global__ void __launch_bounds__(TR_ROWS)
+distill_thread_kernel(const DistillParams P, const int vec)
+{
+    constexpr int E = Elem<F32>::E;
+    extern __shared__ __align__(16) float rows_s[];                    // [256][c | 1], then ids and logits [256][k | 1]
+    __shared__ double wl[TR_ROWS / 32];
+    const int tid = threadIdx.x, pc = P.c | 1, pk = P.k | 1;
+    int *ids_s = (int *)(rows_s + TR_ROWS * pc);
+    float *t_s = (float *)(ids_s + TR_ROWS * pk);
+    const float c2 = LOG2E / P.temp, inv_t = 1.f / P.temp;
+    const uint32_t div_c = ((1u << 20) + P.c - 1) / P.c, div_k = ((1u << 20) + P.k - 1) / P.k;     // x / c = x div >> 20 for x < 256 c <= 2^13
     double total = 0;
     pdl_launch_dependents();
     pdl_wait();
-    for (int64_t row = first; row < P.rows; row += step) {
-        const int64_t at = row * P.pz, dat = row * P.pdz;
-        const float w = P.w ? P.w[row] : P.w_all;                  // the same for the whole cluster: so are all branches on it
-        const int off = misalign<F32>(P.z, at);
-        const bool same = (MODE & BWD) && off == misalign<F32>(P.dz, dat);
-        const int nu_all = (P.c + off + E - 1) / E;
-        const int u0 = (int)((int64_t)nu_all * rank / S_CTAS), u1 = (int)((int64_t)nu_all * (rank + 1) / S_CTAS);
-        const int e0 = u0 * E - off, e1 = u1 * E - off;            // elements of this CTA's slice (clipped to the row below)
-        float S = 0.f, loss = 0.f, lse = 0.f;
+    for (int64_t r0 = (int64_t)blockIdx.x * TR_ROWS; r0 < P.rows; r0 += (int64_t)gridDim.x * TR_ROWS) {
+        const int nr = (int)(P.rows - r0 < TR_ROWS ? P.rows - r0 : TR_ROWS);
+        const int n = nr * P.c;
+        if (vec) {                                                     // rows are back to back: 16-byte loads
+            const uint4 *src = reinterpret_cast<const uint4 *>((const char *)P.z + ((r0 * P.c) << Elem<F32>::SHIFT));
+            for (int i = tid; i < n / E; i += TR_ROWS) {
+                float v[E];
+                unit_values<F32>(src[i], v);
+                uint32_t r = ((uint32_t)(i * E) * div_c) >> 20, col = i * E - r * P.c;
+#pragma unroll
+                for (int j = 0; j < E; ++j) {
+                    rows_s[r * pc + col] = v[j];
+                    if (++col == (uint32_t)P.c) { col = 0; ++r; }
+                }
+            }
+            for (int i = n / E * E + tid; i < n; i += TR_ROWS) {
+                const uint32_t r = ((uint32_t)i * div_c) >> 20;
+                rows_s[r * pc + i - r * P.c] = elem<F32>(P.z, r0 * P.c + i);
+            }
+        } else {
+            for (int i = tid; i < n; i += TR_ROWS) {
+                const uint32_t r = ((uint32_t)i * div_c) >> 20, col = i - r * P.c;
+                rows_s[r * pc + col] = elem<F32>(P.z, (r0 + r) * P.pz + col);
+            }
+        }
+        for (int i = tid; i < nr * P.k; i += TR_ROWS) {
+            const uint32_t r = ((uint32_t)i * div_k) >> 20, j = i - r * P.k;
+            ids_s[r * pk + j] = P.idx[r0 * P.k + i];
+            t_s[r * pk + j] = P.t[r0 * P.k + i];
+        }
+        const float w = tid < nr ? (P.w ? P.w[r0 + tid] : P.w_all) : 0.f;
+        const float tl = tid < nr && P.tlse ? P.tlse[r0 + tid] : 0.f;
+        const float lin = (MODE & FWD) || tid >= nr ? 0.f : P.lse_in[r0 + tid];
+        __syncthreads();
+        float *zr = rows_s + tid * pc;
+        const int *id = ids_s + tid * pk;
+        const float *tr = t_s + tid * pk;
+        // the teacher: log p_j = t_j / T - lt
+        float S = 0.f, lt = tl;
         if (w != 0.f) {
-            if (warp == 0) {
-                const float v = teacher_row<F32>(P, row, at, lane, e0 < 0 ? 0 : e0, e1 > P.c ? P.c : e1, ids, logp, zt);
-                if (lane == 0) sh_S = v;
-            }
-            float m = -INFINITY, s = 0.f;
-            if constexpr (MODE & FWD) {
-                for (int u = u0 + tid; u < u1; u += CR_THREADS) {
-                    const uint4 raw = load_unit<F32>(P.z, at, off, u, P.c);
-                    if (u - u0 < P.stash) stash[u - u0] = raw;
-                    float v[E], n;
-                    unit_values<F32>(raw, v);
-                    n = v[0];
-#pragma unroll
-                    for (int j = 1; j < E; ++j) n = fmaxf(n, v[j]);
-                    n *= c2;
-                    if (n > m) { s *= exp2f(m - n); m = n; }        // m = -inf: s is 0
-                    if (m != -INFINITY) {
-#pragma unroll
-                        for (int j = 0; j < E; ++j) s += exp2f(fmaf(v[j], c2, -m));
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < E; ++j) if (v[j] != v[j]) s = NAN;
-                    }
+            if (!P.tlse) {
+                float mt = -INFINITY;
+                bool nan = false;
+                for (int j = 0; j < P.k; ++j) {
+                    if ((uint32_t)id[j] >= (uint32_t)P.c) continue;
+                    nan |= tr[j] != tr[j];
+                    mt = fmaxf(mt, tr[j]);
                 }
-                warp_join(m, s);
-                if (lane == 0) { red[0][warp] = m; red[1][warp] = s; }
-            }
-            __syncthreads();
-            S = sh_S;
-            float scale;
-            if constexpr (MODE & FWD) {
-                m = red[0][0]; s = red[1][0];
-                for (int i = 1; i < NW; ++i) join(m, s, red[0][i], red[1][i]);
-                if (S_CTAS > 1) {
-                    if (tid == 0) { sh_ms[0] = m; sh_ms[1] = s; }
-                    cluster_barrier();
-                    m = peer_f32(&sh_ms[0], 0); s = peer_f32(&sh_ms[1], 0);
-                    for (int r = 1; r < S_CTAS; ++r) join(m, s, peer_f32(&sh_ms[0], r), peer_f32(&sh_ms[1], r));
-                }
-                if (m == -INFINITY) s = NAN;                        // no logit above -inf: there is no softmax
-                scale = 1.f / s;
-                if (warp == 0 && S != 0.f) {
-                    const float l2 = log2f(s);
-                    lse = (m + l2) * LN2;
-                    for (int j = lane; j < P.k; j += 32) {
-                        const bool mine = ids[j] >= 0 && ids[j] >= e0 && ids[j] < e1;
-                        const float p = mine ? expf(logp[j]) : 0.f;
-                        if (p != 0.f) loss += p * (logp[j] - LN2 * (fmaf(zt[j], c2, -m) - l2));
-                    }
-                    loss = warp_sum(loss) * P.temp * P.temp;
-                }
-                if (S_CTAS > 1) {
-                    if (tid == 0) sh_loss = loss;
-                    cluster_barrier();                             // also: every peer has read sh_ms
-                    if (rank == 0 && tid == 0)
-                        for (int r = 1; r < S_CTAS; ++r) loss += peer_f32(&sh_loss, r);
+                if (mt != -INFINITY || nan) {
+                    float s = 0.f;
+                    for (int j = 0; j < P.k; ++j) if ((uint32_t)id[j] < (uint32_t)P.c) s += ex2((tr[j] - mt) * c2);
+                    lt = mt * inv_t + logf(s);
+                    S = s == s ? 1.f : NAN;
                 }
             } else {
-                m = P.lse_in[row];
-                scale = 1.f;
-            }
-            if ((MODE & BWD) && S != 0.f) {
-                const float gT = w * P.temp, gq = gT * S * scale;
-                for (int u = u0 + tid; u < u1; u += CR_THREADS) {
-                    const uint4 raw = (MODE & FWD) && u - u0 < P.stash ? stash[u - u0] : load_unit<F32>(P.z, at, off, u, P.c);
-                    float v[E];
-                    unit_values<F32>(raw, v);
-#pragma unroll
-                    for (int j = 0; j < E; ++j) v[j] = gq * power<MODE>(v[j], c2, m);
-                    store_unit<F32>(P.dz, dat, off, same, u, P.c, v);
-                }
-                __syncthreads();                                   // the listed classes go over what the dense pass wrote
-                for (int j = tid; j < P.k; j += CR_THREADS) {
-                    const int id = ids[j];
-                    if (id < 0 || id < e0 || id >= e1) continue;
-                    float p = 0.f;
-                    for (int i = 0; i < P.k; ++i) if (ids[i] == id) p += expf(logp[i]);
-                    put<F32>(P.dz, dat + id, gT * (S * (scale * power<MODE>(zt[j], c2, m)) - p));
-                }
+                for (int j = 0; j < P.k; ++j) if ((uint32_t)id[j] < (uint32_t)P.c) S += expf(fmaf(tr[j], inv_t, -lt));
             }
         }
-        if ((MODE & BWD) && S == 0.f) {
-            float v[E];
+        float loss = 0.f, lse = 0.f;
+        if (S != 0.f) {
+            float v[CP];
 #pragma unroll
-            for (int j = 0; j < E; ++j) v[j] = 0.f;
-            for (int u = u0 + tid; u < u1; u += CR_THREADS) store_unit<F32>(P.dz, dat, off, same, u, P.c, v);
+            for (int i = 0; i < CP; ++i) v[i] = i < P.c ? zr[i] : -INFINITY;
+            float m, scale = 1.f, ls = 0.f;
+            if constexpr (MODE & FWD) {
+                m = -FLT_MAX;
+#pragma unroll
+                for (int i = 0; i < CP; ++i) m = fmaxf(m, v[i]);
+                float s = 0.f;
+#pragma unroll
+                for (int i = 0; i < CP; ++i) { v[i] = ex2((v[i] - m) * c2); s += v[i]; }
+                if (s == 0.f) s = NAN;
+                scale = 1.f / s;
+                ls = logf(s);
+                lse = m * inv_t + ls;
+            } else {
+                m = lin;
+#pragma unroll
+                for (int i = 0; i < CP; ++i) v[i] = ex2(fmaf(v[i], inv_t, -m) * LOG2E);
+            }
+            const float gT = w * P.temp, gq = gT * S * scale;
+            if constexpr (MODE & FWD) {
+                for (int j = 0; j < P.k; ++j) {
+                    if ((uint32_t)id[j] >= (uint32_t)P.c) continue;
+                    const float lp = fmaf(tr[j], inv_t, -lt), p = expf(lp);
+                    if (p != 0.f) loss += p * (lp - ((zr[id[j]] - m) * inv_t - ls));
+                }
+                loss *= P.temp * P.temp;
+            }
+            if constexpr (MODE & BWD) {
+#pragma unroll
+                for (int i = 0; i < CP; ++i) if (i < P.c) zr[i] = gq * v[i];
+                for (int j = 0; j < P.k; ++j)
+                    if ((uint32_t)id[j] < (uint32_t)P.c) zr[id[j]] -= gT * expf(fmaf(tr[j], inv_t, -lt));
+            }
+        } else if ((MODE & BWD) && tid < nr) {
+            for (int i = 0; i < P.c; ++i) zr[i] = 0.f;
         }
-        if ((MODE & FWD) && rank == 0 && tid == 0) {
-            if (P.loss_rows) P.loss_rows[row] = loss;
-            if (P.lse_out) P.lse_out[row] = lse;
+        if ((MODE & FWD) && tid < nr) {
+            if (P.loss_rows) P.loss_rows[r0 + tid] = loss;
+            if (P.lse_out) P.lse_out[r0 + tid] = lse;
             if (w != 0.f) total += (double)w * loss;
         }
-        if (w != 0.f) __syncthreads();                             // ids, logp, zt, red are free again
-        if ((MODE & FWD) && S_CTAS > 1 && w != 0.f) cluster_barrier();   // sh_loss has been read
+        __syncthreads();
+        if constexpr (MODE & BWD) {
+            if (vec) {
+                uint4 *dst = reinterpret_cast<uint4 *>((char *)P.dz + ((r0 * P.c) << Elem<F32>::SHIFT));
+                for (int i = tid; i < n / E; i += TR_ROWS) {
+                    float v[E];
+                    uint32_t r = ((uint32_t)(i * E) * div_c) >> 20, col = i * E - r * P.c;
+#pragma unroll
+                    for (int j = 0; j < E; ++j) {
+                        v[j] = rows_s[r * pc + col];
+                        if (++col == (uint32_t)P.c) { col = 0; ++r; }
+                    }
+                    dst[i] = unit_raw<F32>(v);
+                }
+                for (int i = n / E * E + tid; i < n; i += TR_ROWS) {
+                    const uint32_t r = ((uint32_t)i * div_c) >> 20;
+                    put<F32>(P.dz, r0 * P.c + i, rows_s[r * pc + i - r * P.c]);
+                }
+            } else {
+                for (int i = tid; i < n; i += TR_ROWS) {
+                    const uint32_t r = ((uint32_t)i * div_c) >> 20, col = i - r * P.c;
+                    put<F32>(P.dz, (r0 + r) * P.pdz + col, rows_s[r * pc + col]);
+                }
+            }
+            __syncthreads();
+        }
     }
-    if ((MODE & FWD) && P.part && rank == 0 && tid == 0) P.part[blockIdx.x / S_CTAS] = total;
+    if ((MODE & FWD) && P.part) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+        if ((tid & 31) == 0) wl[tid >> 5] = total;
+        __syncthreads();
+        if (tid == 0) {
+            double a = 0;
+            for (int i = 0; i < TR_ROWS / 32; ++i) a += wl[i];
+            P.part[blockIdx.x] = a;
+        }
+    }
 }
 
 __global__ void __launch_bounds__(256)
@@ -453,15 +763,36 @@ lamp_status_t launch_warp(const DistillParams &P, int grid, cudaStream_t st)
     return launch_pdl(true, distill_warp_kernel<F32, MODE>, dim3(grid), dim3(WR_WARPS * 32), (size_t)smem, st, P);
 }
 
+template <bool F32, int MODE, int CP>
+lamp_status_t launch_thread(const DistillParams &P, int grid, int vec, cudaStream_t st)
+{
+    const int smem = TR_ROWS * ((P.c | 1) + 2 * (P.k | 1)) * 4;
+    if (smem > 32 * 1024) {
+        static SmemAttrOnce attr;
+        const lamp_status_t s = attr.ensure(distill_thread_kernel<F32, MODE, CP>, TR_ROWS * 3 * 33 * 4);
+        if (s != LAMP_OK) return s;
+    }
+    return launch_pdl(true, distill_thread_kernel<F32, MODE, CP>, dim3(grid), dim3(TR_ROWS), (size_t)smem, st, P, vec);
+}
 template <bool F32, int MODE>
-lamp_status_t launch_cta(const DistillParams &P, int grid, int splits, int smem, cudaStream_t st)
+lamp_status_t launch_thread_c(const DistillParams &P, int grid, int vec, cudaStream_t st)
+{
+    if (P.c <= 4) return launch_thread<F32, MODE, 4>(P, grid, vec, st);
+    if (P.c <= 8) return launch_thread<F32, MODE, 8>(P, grid, vec, st);
+    if (P.c <= 12) return launch_thread<F32, MODE, 12>(P, grid, vec, st);
+    if (P.c <= 16) return launch_thread<F32, MODE, 16>(P, grid, vec, st);
+    return launch_thread<F32, MODE, 32>(P, grid, vec, st);
+}
+
+template <bool F32, int MODE>
+lamp_status_t launch_cta(const DistillParams &P, int grid, int splits, int threads, int smem, cudaStream_t st)
 {
     static SmemAttrOnce attr;
     const lamp_status_t s = attr.ensure(distill_cta_kernel<F32, MODE>, 226 * 1024);
     if (s != LAMP_OK) return s;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(grid);
-    cfg.blockDim = dim3(CR_THREADS);
+    cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute at[2];
@@ -481,25 +812,38 @@ lamp_status_t run(DistillParams &P, bool f32, float *loss, void *ws, cudaStream_
     int parts;
     lamp_status_t s;
     P.part = loss ? (double *)ws : nullptr;
-    if (P.c <= WR_MAX_C) {
+    P.status = status_word_ptr();
+    if (P.c <= TR_MAX_C && P.k <= TR_MAX_K) {
+        const int64_t need = (P.rows + TR_ROWS - 1) / TR_ROWS;
+        parts = (int)(need < 8ll * sms ? need : 8ll * sms);
+        if (parts > MAX_PARTS) parts = MAX_PARTS;
+        const int vec = P.pz == P.c && ((uintptr_t)P.z & 15) == 0 && (!(MODE & BWD) || (P.pdz == P.c && ((uintptr_t)P.dz & 15) == 0));
+        s = f32 ? launch_thread_c<true, MODE>(P, parts, vec, st) : launch_thread_c<false, MODE>(P, parts, vec, st);
+    } else if (P.c <= WR_MAX_C) {
         const int64_t need = (P.rows + WR_WARPS - 1) / WR_WARPS;
         parts = (int)(need < 8ll * sms ? need : 8ll * sms);
         if (parts > MAX_PARTS) parts = MAX_PARTS;
         s = f32 ? launch_warp<true, MODE>(P, parts, st) : launch_warp<false, MODE>(P, parts, st);
     } else {
         const int units = (P.c + (f32 ? 3 : 7)) / (f32 ? 4 : 8) + 1;
-        // a cluster per row where rows alone would leave SMs idle and every CTA still has two units a thread
+        const int lists = 2 * 3 * P.k * 4, room = (224 * 1024 - lists) / 32;        // units of a buffer at most
+        // a cluster per row where a slice would not fit otherwise, or where rows alone would leave SMs idle and every CTA still
+        // has about a unit a thread
         int splits = 1;
-        while (splits < 8 && P.rows * splits * 2 <= sms && units >= 4 * CR_THREADS * splits) splits *= 2;
-        const int slice = (units + splits - 1) / splits + 1, lists = 3 * P.k * 4;
-        // two CTAs per SM, so that one loads while the other computes or writes
-        const int room = ((MODE & FWD) && (MODE & BWD)) ? (112 * 1024 - lists) / 16 : 0;
-        P.stash = slice < room ? slice : room > 0 ? room : 0;
-        int64_t groups = 2ll * sms / splits;
+        while (splits < 8 && ((units + splits - 1) / splits + 1 > room || (P.rows * splits * 2 <= sms && units >= 2048 * splits))) splits *= 2;
+        const int slice = (units + splits - 1) / splits + 1;
+        P.stash = slice;
+        // about six units per consumer thread; several CTAs per SM where rows are short (1024 threads at 64 registers)
+        int threads = (slice / 6 + 31) / 32 * 32;
+        threads = 32 + (threads < 96 ? 96 : threads > CR_MAX_THREADS - 32 ? CR_MAX_THREADS - 32 : threads);
+        const int smem = slice * 32 + lists;
+        int per_sm = CR_MAX_THREADS / threads;
+        if (per_sm > 224 * 1024 / (smem + 2048)) per_sm = 224 * 1024 / (smem + 2048);
+        if (per_sm < 1) per_sm = 1;
+        int64_t groups = (int64_t)per_sm * sms / splits;
         if (groups > P.rows) groups = P.rows;
         parts = (int)groups;
-        const int smem = P.stash * 16 + lists;
-        s = f32 ? launch_cta<true, MODE>(P, parts * splits, splits, smem, st) : launch_cta<false, MODE>(P, parts * splits, splits, smem, st);
+        s = f32 ? launch_cta<true, MODE>(P, parts * splits, splits, threads, smem, st) : launch_cta<false, MODE>(P, parts * splits, splits, threads, smem, st);
     }
     if (s != LAMP_OK || !loss) return s;
     return launch_pdl(true, distill_sum_kernel, dim3(1), dim3(256), 0, st, (const double *)ws, parts, loss);
@@ -517,7 +861,7 @@ lamp_status_t fill(DistillParams *P, const lamp_tensor_t *z, const lamp_teacher_
 {
     lamp_status_t s;
     if ((s = check_view(z, true)) != LAMP_OK || (s = check_teacher(t)) != LAMP_OK) return s;
-    if (z->c > 1 << 28) return LAMP_ERR_UNSUPPORTED;
+    if (z->c > (z->dtype == LAMP_F32 ? 200000 : 400000)) return LAMP_ERR_UNSUPPORTED;       // a row in the shared memory of 8 CTAs
     const TView v = make_view(z);
     *P = DistillParams{};
     P->z = v.p; P->pz = v.pitch; P->rows = voxels(z); P->c = z->c; P->k = t->k;

@@ -396,7 +396,10 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constant
                 }
             }
         }
-        if (lane == 0 && !ok && P.status) atomicExch(P.status, (int)LAMP_ERR_TIMEOUT);
+        if (!ok) {
+            if (lane == 0 && P.status) atomicExch(P.status, (int)LAMP_ERR_TIMEOUT);
+            settle();                                           // copies in flight
+        }
     }
     __syncwarp();
     if (S > 1) {

@@ -51,6 +51,12 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
     }
 }
 
+// Delay of about a millisecond for a CTA that gave up a wait: its asynchronous copies in flight land before it leaves.
+__device__ __forceinline__ void settle()
+{
+    for (int i = 0; i < 1000; ++i) __nanosleep(1000);
+}
+
 // Tiled TMA loads; the innermost coordinate times the element size must be a multiple of 16 bytes.
 __device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int c0, int c1, int c2,
                                             int c3, int c4)

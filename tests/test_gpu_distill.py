@@ -98,7 +98,7 @@ class Case:
 
 
 SHAPES = [(1, 1, 1), (5, 2, 1), (300, 4, 3), (1000, 10, 4), (77, 16, 16), (33, 31, 5), (40, 33, 40), (3, 100, 7), (70, 257, 64), (9, 1000, 20), (4, 1017, 9),
-          (4, 1024, 8), (5, 1025, 8), (3, 4099, 100), (2, 9000, 33), (1, 40000, 10), (2, 130001, 64), (160, 2050, 3)]
+          (4, 1024, 8), (5, 1025, 8), (3, 4099, 100), (2, 9000, 33), (1, 40000, 10), (2, 130001, 64), (160, 2050, 3), (700, 1500, 5), (400, 6001, 10), (321, 40007, 70), (100, 70000, 5), (77, 32, 32), (600, 20, 33)]
 
 
 @pytest.mark.parametrize("rows,c,k", SHAPES)
@@ -157,6 +157,30 @@ def test_masked_classes_and_rows_that_are_not_finite(c, dt):
     assert (fused[0, 5:8] == 0).all() and (fused[1, 5:8] == 0).all()
     b[3:] = 0.5
     k.check()
+
+
+@pytest.mark.parametrize("c", [9, 600, 3000, 50000, 140000])
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+def test_row_of_nothing_but_the_lowest_value_is_uniform(c, dt):
+    k = Case(c, 3, c, 4, dt)
+    k.idx[:] = np.arange(4)
+    k.buf[0, 0, 0, 1] = torch.finfo(dt).min
+    loss, _, _, fused, _ = k.run()
+    t = k.t[1].astype(np.float64)
+    logp = t - np.log(np.exp(t).sum())
+    ref = (np.exp(logp) * (logp + np.log(c))).sum()
+    assert abs(loss[1] - ref) <= 128 * 2.0 ** -24 * (np.abs(t).max() + np.log(c) + 1) * 4
+    g = np.full(c, 1.0 / c)
+    g[:4] -= np.exp(logp)
+    assert (np.abs(fused[1] - k.w[1] * g) <= k.w[1] * (2.0 ** -8 * np.abs(g) + 128 * 2.0 ** -24 * (1.0 / c + (np.arange(c) < 4)))).all()
+
+
+@pytest.mark.parametrize("rows,c,k", [(1, 400000, 3), (2, 390001, 1024)])
+def test_widest_rows(rows, c, k):
+    Case(1, rows, c, k, torch.bfloat16, temp=2.0).check()
+    Case(2, rows, c // 2, k, torch.float32).check()
+    with pytest.raises(B.LampError):
+        Case(1, 1, 400001, 1, torch.bfloat16).run()
 
 
 @pytest.mark.parametrize("rows,c", [(50, 10), (50, 500), (3, 9001), (40, 3001)])
