@@ -283,14 +283,14 @@ distill_warp_kernel(const DistillParams P)
 // ----------------------------------------------------------------------------------------------------------------------
 // one CTA, or a cluster of CTAs, per row
 // ----------------------------------------------------------------------------------------------------------------------
-// Warp-specialised, two buffers.  The helper warp has the next rows (or this CTA's slices of them) copied into shared memory -
-// one bulk asynchronous copy of a row's whole 16-byte units; the ragged first and last unit by hand, filled up with -inf -
-// and prepares their teacher entries.  The consumers take a row from its buffer into registers at once, which frees the
-// buffer for the copy two rows ahead, and work from there: maximum, sum, gradient.  So a row is read from HBM exactly once
-// and the copies never wait for the arithmetic.
-// Measured (4096 x 50001 bf16, loss and gradient): without the copy pipeline 348 us; with it, data in shared memory 327 us
-// (three passes over it, and a join of maximum and sum per lane); in registers, with packed fp32 arithmetic: see the table of
-// figures at the top.
+// Warp-specialised, two or more CTAs per SM, so that the phases of one row (maximum, sum: bound by the exponential unit;
+// gradient: by stores) overlap with other phases of another.  The helper warp prepares the next row's teacher entries and
+// has the next row (or this CTA's slice of it) copied into shared memory, chunk by chunk as the consumers' last pass
+// over the current row gives the chunks up: bulk asynchronous copies of the whole 16-byte units, the ragged first and last
+// unit by hand, filled up with -inf.  A row is read from HBM exactly once.
+// Measured (4096 x 50001 bf16, loss and gradient, us): loads by the threads that use them 348; one CTA per SM with two row
+// buffers 327; the same with the row held in registers and packed fp32 arithmetic 240 (loss alone 112, gradient alone 131:
+// the phases of a row simply add up when all warps of an SM share it); this form: MEASURED.
 struct RowSlot {                                    // what the helper prepares for a row
     float S, w;
 };
@@ -362,20 +362,44 @@ template <bool SAFE> __device__ __forceinline__ ptx::f32x2 pair_exp(ptx::f32x2 z
 
 constexpr int SHORT_K = 128;
 __host__ __device__ constexpr int lists_of(int k) { return k <= SHORT_K ? 5 : 3; }
-constexpr int CR_MAX_THREADS = 1024, CR_UNITS = 7;   // units of a row that a consumer thread holds
+constexpr int CR_MAX_THREADS = 1024, CR_CHUNKS = 16;
 
 template <bool F32, bool SAFE>
-__device__ __forceinline__ float units_sum(const uint4 (&raw)[CR_UNITS], float c, float m)
+__device__ __forceinline__ float unit_sum(const uint4 &raw, float c, float m, float mc)
 {
-    const float mc = m * c;
     ptx::f32x2 s = 0;
 #pragma unroll
-    for (int i = 0; i < CR_UNITS; ++i)
-#pragma unroll
-        for (int j = 0; j < Elem<F32>::E / 2; ++j) s = ptx::add2(s, pair_exp<SAFE>(unit_pair<F32>(raw[i], j), c, m, mc));
+    for (int j = 0; j < Elem<F32>::E / 2; ++j) s = ptx::add2(s, pair_exp<SAFE>(unit_pair<F32>(raw, j), c, m, mc));
     float a, b;
     ptx::unpack2(s, a, b);
     return a + b;
+}
+
+// gradient of a unit before the listed classes are taken off.  KIND 0: from maximum and sum; 1: the same where z c could
+// overflow; 2: from a given log-sum m: e^(z / T - m), the difference before the change of base (c = 1 / T)
+template <bool F32, int KIND>
+__device__ __forceinline__ uint4 unit_grad(const uint4 &raw, float c, float m, float mc, float gq)
+{
+    uint32_t o[4];
+#pragma unroll
+    for (int j = 0; j < Elem<F32>::E / 2; ++j) {
+        ptx::f32x2 e = unit_pair<F32>(raw, j);
+        float x, y;
+        if (KIND == 2) {
+            ptx::unpack2(ptx::mul2(ptx::fma2(e, ptx::twice(c), ptx::twice(-m)), ptx::twice(LOG2E)), x, y);
+            e = ptx::pack2(__float_as_uint(ex2(x)), __float_as_uint(ex2(y)));
+        } else {
+            e = pair_exp<KIND == 1>(e, c, m, mc);
+        }
+        ptx::unpack2(ptx::mul2(e, ptx::twice(gq)), x, y);
+        if constexpr (F32) {
+            o[2 * j] = __float_as_uint(x); o[2 * j + 1] = __float_as_uint(y);
+        } else {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+            o[j] = *reinterpret_cast<const uint32_t *>(&h);
+        }
+    }
+    return make_uint4(o[0], o[1], o[2], o[3]);
 }
 
 template <bool F32, int MODE>
@@ -383,9 +407,9 @@ __global__ void __launch_bounds__(CR_MAX_THREADS, 1)
 distill_cta_kernel(const DistillParams P, const int S_CTAS)
 {
     constexpr int E = Elem<F32>::E;
-    extern __shared__ __align__(16) uint4 buf[];                       // [2][P.stash] units, then the lists [2][LISTS][k4]
+    extern __shared__ __align__(16) uint4 buf[];                       // [P.stash] units, then the lists [2][LISTS][k4]
     __shared__ __align__(16) float4 msg[2][8];                         // per row parity: (maximum, sum, D, P) of every CTA of the cluster
-    __shared__ __align__(8) uint64_t bars[9];                          // full[2], empty[2], exchange[2], consumers, lists[2]
+    __shared__ __align__(8) uint64_t bars[6 + CR_CHUNKS];              // full, consumers, exchange[2], lists[2], chunk empty[]
     __shared__ float red[2][2][32];
     __shared__ RowSlot slot[2];
     __shared__ int abort_s;
@@ -393,22 +417,20 @@ distill_cta_kernel(const DistillParams P, const int S_CTAS)
     // per row: ids, log p, z of the listed classes, and for short lists p and its sum over equal ids (long ones use exp(log p))
     const int k4 = (P.k + 3) & ~3, nl = lists_of(P.k);
     const bool brief = P.k <= SHORT_K;
-    int *ids0 = (int *)(buf + 2 * P.stash);
+    int *ids0 = (int *)(buf + P.stash);
     const int nthr = blockDim.x - 32, nwarp = nthr >> 5;               // consumers; the last warp is the helper
+    const int nch = (P.stash + nthr - 1) / nthr;                       // chunks: units [i nthr, (i + 1) nthr) of the slice
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const float c2 = LOG2E / P.temp, inv_t = 1.f / P.temp;
     const uint32_t rank = S_CTAS > 1 ? blockIdx.x % S_CTAS : 0;
     const int64_t first = blockIdx.x / S_CTAS, step = gridDim.x / S_CTAS;
-    const uint32_t full0 = ptx::smem_u32(bars), empty0 = full0 + 16, exch0 = full0 + 32, cons = full0 + 48, lists0 = full0 + 56;
+    const uint32_t full = ptx::smem_u32(bars), cons = full + 8, exch0 = full + 16, lists0 = full + 32, chunk0 = full + 48;
     pdl_launch_dependents();
     if (tid == 0) {
-        for (int b = 0; b < 2; ++b) {
-            ptx::mbar_init(full0 + 8 * b, 2);
-            ptx::mbar_init(empty0 + 8 * b, nwarp);
-            ptx::mbar_init(exch0 + 8 * b, 1);
-            ptx::mbar_init(lists0 + 8 * b, nwarp);
-        }
+        ptx::mbar_init(full, 2);
         ptx::mbar_init(cons, nwarp);
+        for (int b = 0; b < 2; ++b) { ptx::mbar_init(exch0 + 8 * b, 1); ptx::mbar_init(lists0 + 8 * b, nwarp); }
+        for (int i = 0; i < nch; ++i) ptx::mbar_init(chunk0 + 8 * i, nwarp);
         abort_s = 0;
         ptx::mbar_init_fence();
     }
@@ -430,43 +452,14 @@ distill_cta_kernel(const DistillParams P, const int S_CTAS)
         float w_next = first < P.rows ? (P.w ? P.w[first] : P.w_all) : 0.f;
         for (int64_t row = first; row < P.rows; row += step, ++i) {
             const int b = i & 1;
-            const uint32_t ph = (uint32_t)(i >> 1) & 1;
+            const uint32_t ph = (uint32_t)i & 1, lph = (uint32_t)(i >> 1) & 1;
             const float w = w_next;
             if (row + step < P.rows && P.w) w_next = P.w[row + step];
             int *ids = ids0 + b * nl * k4;
             float *logp = (float *)(ids + k4), *pr = logp + 2 * k4, *pm = pr + k4;
-            if (w != 0.f && row + step < P.rows && lane * 32 < P.k) {     // the next row's entries into L2
-                asm volatile("prefetch.global.L2 [%0];" ::"l"(P.idx + (row + step) * P.k + lane * 32));
-                asm volatile("prefetch.global.L2 [%0];" ::"l"(P.t + (row + step) * P.k + lane * 32));
-            }
-            ok = __all_sync(0xffffffffu, ptx::mbar_wait(empty0 + 8 * b, ph ^ 1, abort_flag));
+            ok = __all_sync(0xffffffffu, ptx::mbar_wait(lists0 + 8 * b, lph ^ 1, abort_flag));
             if (!ok) break;
             float S = 0.f;
-            if (w != 0.f) {
-                int off, nu, u0, u1;
-                geometry(row, off, nu, u0, u1);
-                const int64_t at = row * P.pz;
-                // whole units of the slice: not the first if it starts in front of the row, not the last if it ends behind it
-                const int f0 = u0 == 0 && off ? 1 : u0, f1 = u1 == nu && (P.c + off) % E ? nu - 1 : u1;
-                uint4 *dst = buf + b * P.stash;
-                if (lane == 0) {
-                    ptx::fence_proxy_async();                          // the buffer's last readers, then the copy
-                    if (f1 > f0) {
-                        ptx::mbar_expect_tx(full0 + 8 * b, (uint32_t)(f1 - f0) * 16);
-                        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                                     ::"r"(ptx::smem_u32(dst + (f0 - u0))), "l"((const char *)P.z + ((at + (int64_t)f0 * E - off) << Elem<F32>::SHIFT)),
-                                       "r"((uint32_t)(f1 - f0) * 16), "r"(full0 + 8 * b) : "memory");
-                    } else {
-                        ptx::mbar_arrive(full0 + 8 * b);
-                    }
-                }
-                if (lane == 1 && f0 > u0 && u1 > u0) dst[0] = load_unit<F32>(P.z, at, off, u0, P.c);
-                if (lane == 2 && f1 < u1 && f1 >= f0) dst[f1 - u0] = load_unit<F32>(P.z, at, off, f1, P.c);
-            } else if (lane == 0) {
-                ptx::mbar_arrive(full0 + 8 * b);
-            }
-            ok = __all_sync(0xffffffffu, ptx::mbar_wait(lists0 + 8 * b, ph ^ 1, abort_flag));
-            if (!ok) break;
             if (w != 0.f) {
                 S = teacher_row(P, row, lane, ids, logp);
                 if (S != 0.f && brief) {
@@ -491,8 +484,34 @@ distill_cta_kernel(const DistillParams P, const int S_CTAS)
                 }
             }
             if (lane == 0) { slot[b].S = S; slot[b].w = w; }
+            int off, nu, u0, u1;
+            geometry(row, off, nu, u0, u1);
+            const int64_t at = row * P.pz;
+            // whole units of the slice: not the first if it starts in front of the row, not the last if it ends behind it
+            const int f0 = u0 == 0 && off ? 1 : u0, f1 = u1 == nu && (P.c + off) % E ? nu - 1 : u1;
+            const bool load = S != 0.f;
+            for (int ch = 0; ch < nch; ++ch) {
+                ok = __all_sync(0xffffffffu, ptx::mbar_wait(chunk0 + 8 * ch, ph ^ 1, abort_flag));
+                if (!ok) break;
+                // the first chunk given back: the consumers are past the previous row's phase of `full`, so this one may be
+                // announced (an arrival while the copies of the previous phase are in flight would be one too many for it)
+                if (ch == 0 && lane == 0) {
+                    if (load && f1 > f0) ptx::mbar_expect_tx(full, (uint32_t)(f1 - f0) * 16); else ptx::mbar_arrive(full);
+                }
+                if (!load) continue;
+                const int c0 = u0 + ch * nthr, c1 = c0 + nthr, g0 = c0 > f0 ? c0 : f0, g1 = c1 < f1 ? c1 : f1;
+                if (lane == 0 && g1 > g0) {
+                    ptx::fence_proxy_async();                          // the chunk's last readers, then the copy
+                    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                                 ::"r"(ptx::smem_u32(buf + (g0 - u0))), "l"((const char *)P.z + ((at + (int64_t)g0 * E - off) << Elem<F32>::SHIFT)),
+                                   "r"((uint32_t)(g1 - g0) * 16), "r"(full) : "memory");
+                }
+                if (lane == 1 && f0 > u0 && u1 > u0 && ch == 0) buf[0] = load_unit<F32>(P.z, at, off, u0, P.c);
+                if (lane == 2 && f1 < u1 && f1 >= f0 && f1 >= c0 && f1 < c1) buf[f1 - u0] = load_unit<F32>(P.z, at, off, f1, P.c);
+            }
+            if (!ok) break;
             __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(full0 + 8 * b);
+            if (lane == 0) ptx::mbar_arrive(full);
         }
     } else {
         // ------------------------------------------------------------------ consumers
@@ -503,39 +522,54 @@ distill_cta_kernel(const DistillParams P, const int S_CTAS)
             const int64_t dat = row * P.pdz;
             int off, nu, u0, u1;
             geometry(row, off, nu, u0, u1);
+            const int n = u1 - u0;
             const bool same = (MODE & BWD) && off == misalign<F32>(P.dz, dat);
             const int e0 = u0 * E - off, e1 = u1 * E - off;            // elements of the slice
             const int *ids = ids0 + b * nl * k4;
             const float *logp = (const float *)(ids + k4), *pr = logp + 2 * k4, *pm = pr + k4;
             float *zt = (float *)(logp + k4);
-            ok = __all_sync(0xffffffffu, ptx::mbar_wait(full0 + 8 * b, (uint32_t)(i >> 1) & 1, abort_flag));
+            ok = __all_sync(0xffffffffu, ptx::mbar_wait(full, (uint32_t)i & 1, abort_flag));
             if (!ok) break;
             const float S = slot[b].S, w = slot[b].w;
-            uint4 raw[CR_UNITS];
+            float loss = 0.f, lse = 0.f;
+            int ch = 0;                                                // chunks given back so far
+            auto give_back = [&]() {
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(chunk0 + 8 * ch);
+                ++ch;
+            };
             if (S != 0.f) {
-                const uint4 *data = buf + b * P.stash;
-                const uint32_t low = F32 ? 0xFF800000u : 0xFF80FF80u;  // -inf
-#pragma unroll
-                for (int r = 0; r < CR_UNITS; ++r) {
-                    const int u = tid + r * nthr;
-                    raw[r] = u < u1 - u0 ? data[u] : make_uint4(low, low, low, low);
-                }
+                // before this warp gives back any chunk: a chunk is copied over only when every warp has given it back
                 for (int j = tid; j < P.k; j += nthr) {
                     const int id = ids[j];
-                    if (id >= 0 && id >= e0 && id < e1) zt[j] = elem<F32>(data, id - e0);
+                    if (id >= 0 && id >= e0 && id < e1) zt[j] = elem<F32>(buf, id - e0);
                 }
-            }
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(empty0 + 8 * b);           // the buffer is free
-            float loss = 0.f, lse = 0.f;
-            if (S != 0.f) {
                 float m, s = 1.f, scale = 1.f;                         // maximum of z, sum of e^((z - m) / T)
                 if constexpr (MODE & FWD) {
                     m = -FLT_MAX;                                      // of -inf alone: the sum is 0
-#pragma unroll
-                    for (int r = 0; r < CR_UNITS; ++r) m = fmaxf(m, unit_max<F32>(raw[r]));
+#pragma unroll 4
+                    for (int u = tid; u < n; u += nthr) m = fmaxf(m, unit_max<F32>(buf[u]));
                     m = warp_max_fast(m);
-                    s = fabsf(m * c2) < 1e38f ? units_sum<F32, false>(raw, c2, m) : units_sum<F32, true>(raw, c2, m);
+                    s = 0.f;
+                    const float mc = m * c2;
+                    // with no gradient to come this is the last pass, which gives the chunks back
+                    if constexpr (MODE & BWD) {
+                        if (fabsf(mc) < 1e38f) {
+#pragma unroll 2
+                            for (int u = tid; u < n; u += nthr) s += unit_sum<F32, false>(buf[u], c2, m, mc);
+                        } else {
+                            for (int u = tid; u < n; u += nthr) s += unit_sum<F32, true>(buf[u], c2, m, mc);
+                        }
+                    } else {
+                        const uint32_t low = F32 ? 0xFF800000u : 0xFF80FF80u;
+                        const bool fits = fabsf(mc) < 1e38f;
+#pragma unroll 2
+                        for (int u = tid; ch < nch; u += nthr) {
+                            const uint4 raw = u < n ? buf[u] : make_uint4(low, low, low, low);
+                            give_back();
+                            s += fits ? unit_sum<F32, false>(raw, c2, m, mc) : unit_sum<F32, true>(raw, c2, m, mc);
+                        }
+                    }
                     s = warp_sum(s);
                     if (lane == 0) { red[i & 1][0][warp] = m; red[i & 1][1][warp] = s; }
                     if (!(ok = consumer_sync(cons, cphase, lane, abort_flag))) break;
@@ -582,41 +616,22 @@ distill_cta_kernel(const DistillParams P, const int S_CTAS)
                     m = P.lse_in[row];
                 }
                 if constexpr (MODE & BWD) {
-                    const float gT = w * P.temp, gq = gT * S * scale;
-                    // from a given log-sum: e^(z / T - lse), the difference before the change of base
-                    const float c = (MODE & FWD) ? c2 : inv_t, mc = (MODE & FWD) ? m * c2 : m;
-                    const bool safe = (MODE & FWD) && !(fabsf(mc) < 1e38f);
-#pragma unroll
-                    for (int r = 0; r < CR_UNITS; ++r) {
-                        const int u = tid + r * nthr;
-                        if (u >= u1 - u0) break;
-                        uint32_t o[4];
-#pragma unroll
-                        for (int j = 0; j < E / 2; ++j) {
-                            ptx::f32x2 e = unit_pair<F32>(raw[r], j);
-                            if constexpr (MODE & FWD) {
-                                if (safe) e = pair_exp<true>(e, c, m, mc); else e = pair_exp<false>(e, c, m, mc);
-                            } else {
-                                float x, y;
-                                ptx::unpack2(ptx::mul2(ptx::fma2(e, ptx::twice(c), ptx::twice(-mc)), ptx::twice(LOG2E)), x, y);
-                                e = ptx::pack2(__float_as_uint(ex2(x)), __float_as_uint(ex2(y)));
-                            }
-                            float x, y;
-                            ptx::unpack2(ptx::mul2(e, ptx::twice(gq)), x, y);
-                            if constexpr (F32) {
-                                o[2 * j] = __float_as_uint(x); o[2 * j + 1] = __float_as_uint(y);
-                            } else {
-                                const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
-                                o[j] = *reinterpret_cast<const uint32_t *>(&h);
-                            }
-                        }
+                    const float gT = w * P.temp, gq = gT * S * scale, mc = m * c2;
+                    const int kind = !(MODE & FWD) ? 2 : fabsf(mc) < 1e38f ? 0 : 1;
+#pragma unroll 2
+                    for (int u = tid; ch < nch; u += nthr) {
+                        const uint4 raw = u < n ? buf[u] : make_uint4(0, 0, 0, 0);
+                        give_back();
+                        if (u >= n) continue;
+                        uint4 o;
+                        if constexpr (MODE & FWD) o = kind == 0 ? unit_grad<F32, 0>(raw, c2, m, mc, gq) : unit_grad<F32, 1>(raw, c2, m, mc, gq);
+                        else o = unit_grad<F32, 2>(raw, inv_t, m, mc, gq);
                         const int lo = (u0 + u) * E - off;
-                        const uint4 o4 = make_uint4(o[0], o[1], o[2], o[3]);
                         if (same && lo >= 0 && lo + E <= P.c) {
-                            *reinterpret_cast<uint4 *>((char *)P.dz + ((dat + lo) << Elem<F32>::SHIFT)) = o4;
+                            *reinterpret_cast<uint4 *>((char *)P.dz + ((dat + lo) << Elem<F32>::SHIFT)) = o;
                         } else {
                             float v[E];
-                            unit_values<F32>(o4, v);
+                            unit_values<F32>(o, v);
 #pragma unroll
                             for (int j = 0; j < E; ++j) if (lo + j >= 0 && lo + j < P.c) put<F32>(P.dz, dat + lo + j, v[j]);
                         }
@@ -631,11 +646,14 @@ distill_cta_kernel(const DistillParams P, const int S_CTAS)
                         put<F32>(P.dz, dat + id, gT * (S * (scale * power<MODE>(zt[j], c2, inv_t, m)) - p));
                     }
                 }
-            } else if constexpr (MODE & BWD) {
-                float v[E];
+            } else {
+                while (ch < nch) give_back();
+                if constexpr (MODE & BWD) {
+                    float v[E];
 #pragma unroll
-                for (int j = 0; j < E; ++j) v[j] = 0.f;
-                for (int u = u0 + tid; u < u1; u += nthr) store_unit<F32>(P.dz, dat, off, same, u, P.c, v);
+                    for (int j = 0; j < E; ++j) v[j] = 0.f;
+                    for (int u = u0 + tid; u < u1; u += nthr) store_unit<F32>(P.dz, dat, off, same, u, P.c, v);
+                }
             }
             if ((MODE & FWD) && rank == 0 && tid == 0) {
                 if (P.loss_rows) P.loss_rows[row] = loss;
@@ -914,20 +932,21 @@ lamp_status_t run(DistillParams &P, bool f32, float *loss, void *ws, cudaStream_
     } else {
         const int units = (P.c + (f32 ? 3 : 7)) / (f32 ? 4 : 8) + 1;
         const int lists = 2 * lists_of(P.k) * ((P.k + 3) & ~3) * 4;
-        int room = (224 * 1024 - lists) / 32;                          // units of a buffer at most: shared memory, registers
-        if (room > CR_UNITS * (CR_MAX_THREADS - 32)) room = CR_UNITS * (CR_MAX_THREADS - 32);
+        const int room1 = (224 * 1024 - lists) / 16, room2 = (111 * 1024 - lists) / 16;      // units of a slice with one or two CTAs per SM
         // a cluster per row where a slice would not fit otherwise, or where rows alone would leave SMs idle and every CTA still
-        // has about a unit a thread
+        // has about two units a thread
         int splits = 1;
-        while (splits < 8 && ((units + splits - 1) / splits + 1 > room || (P.rows * splits * 2 <= sms && units >= 2048 * splits))) splits *= 2;
+        while (splits < 8 && ((units + splits - 1) / splits + 1 > room2 || (P.rows * splits * 2 <= sms && units >= 2048 * splits))) splits *= 2;
         const int slice = (units + splits - 1) / splits + 1;
+        if (slice > room1) return LAMP_ERR_UNSUPPORTED;
         P.stash = slice;
-        // six or seven units per consumer thread; several CTAs per SM where rows are short (1024 threads at 64 registers)
-        int threads = (slice / 6 + 31) / 32 * 32;
-        threads = 32 + (threads < 96 ? 96 : threads > CR_MAX_THREADS - 32 ? CR_MAX_THREADS - 32 : threads);
-        const int smem = slice * 32 + lists;
+        // about a dozen units per consumer thread; 1024 threads per SM (64 registers), shared between as many CTAs as fit
+        int threads = (slice / 12 + 31) / 32 * 32;
+        const int most = slice > room2 ? CR_MAX_THREADS - 32 : CR_MAX_THREADS / 2 - 32;
+        threads = 32 + (threads < 96 ? 96 : threads > most ? most : threads);
+        const int smem = slice * 16 + lists;
         int per_sm = CR_MAX_THREADS / threads;
-        if (per_sm > 224 * 1024 / (smem + 2048)) per_sm = 224 * 1024 / (smem + 2048);
+        if (per_sm > 226 * 1024 / (smem + 2048)) per_sm = 226 * 1024 / (smem + 2048);
         if (per_sm < 1) per_sm = 1;
         int64_t groups = (int64_t)per_sm * sms / splits;
         if (groups > P.rows) groups = P.rows;
