@@ -364,6 +364,87 @@ constexpr int SHORT_K = 128;
 __host__ __device__ constexpr int lists_of(int k) { return k <= SHORT_K ? 5 : 3; }
 constexpr int CR_MAX_THREADS = 1024, CR_CHUNKS = 16;
 
+// Short lists (k <= SHORT_K): a row's entries in the helper's registers, lane + 32 i, loaded a row ahead.
+struct Entries {
+    int id[SHORT_K / 32];
+    float t[SHORT_K / 32];
+    __device__ __forceinline__ void load(const DistillParams &P, int64_t row, int lane)
+    {
+#pragma unroll
+        for (int i = 0; i < SHORT_K / 32; ++i) {
+            const int j = lane + 32 * i;
+            id[i] = j < P.k ? P.idx[row * P.k + j] : -1;
+            t[i] = j < P.k ? P.t[row * P.k + j] : 0.f;
+        }
+    }
+    // To the lists: ids (-1: absent), log p, p, and pm = p summed over the entries that name the same class.  Returns S.
+    template <bool GRAD>
+    __device__ __forceinline__ float to_lists(const DistillParams &P, float tlse, int lane, int k4, int *ids, float *logp, float *pr, float *pm)
+    {
+        const float inv_t = 1.f / P.temp, c2 = LOG2E / P.temp;
+        float m = -FLT_MAX, p[SHORT_K / 32];
+        bool some = false;
+#pragma unroll
+        for (int i = 0; i < SHORT_K / 32; ++i) {
+            if ((uint32_t)id[i] >= (uint32_t)P.c) id[i] = -1;
+            if (id[i] < 0) continue;
+            some |= t[i] != -INFINITY;                              // NaN counts
+            m = fmaxf(m, t[i]);
+        }
+        if (!__any_sync(0xffffffffu, some)) return 0.f;
+        float S = 0.f, ls = 0.f, inv = 1.f;
+        if (!P.tlse) {
+            m = warp_max_fast(m);
+#pragma unroll
+            for (int i = 0; i < SHORT_K / 32; ++i) { p[i] = id[i] >= 0 ? ex2((t[i] - m) * c2) : 0.f; S += p[i]; }
+            S = warp_sum(S);
+            ls = logf(S);
+            inv = 1.f / S;
+            S = S == S ? 1.f : NAN;
+        } else {
+#pragma unroll
+            for (int i = 0; i < SHORT_K / 32; ++i) { p[i] = id[i] >= 0 ? expf(fmaf(t[i], inv_t, -tlse)) : 0.f; S += p[i]; }
+            S = warp_sum(S);
+        }
+#pragma unroll
+        for (int i = 0; i < SHORT_K / 32; ++i) {
+            const int j = lane + 32 * i;
+            p[i] *= inv;
+            if (j < k4) {
+                ids[j] = id[i];
+                logp[j] = P.tlse ? fmaf(t[i], inv_t, -tlse) : (t[i] - m) * inv_t - ls;
+                pr[j] = p[i];
+                pm[j] = p[i];
+            }
+        }
+        __syncwarp();
+        if (GRAD) {
+            bool twice = false;
+            if (P.k <= 32) {
+                const uint32_t same = __match_any_sync(0xffffffffu, id[0]);      // by every lane, also those without an entry
+                twice = id[0] >= 0 && same != 1u << lane;
+            } else {
+                int n = 0;                                           // entries equal to one of this lane's: itself, and any other
+                for (int q = 0; q < k4; q += 4) {
+                    const int4 v = *reinterpret_cast<const int4 *>(ids + q);
+#pragma unroll
+                    for (int i = 0; i < SHORT_K / 32; ++i)
+                        if (id[i] >= 0) n += (v.x == id[i]) + (v.y == id[i]) + (v.z == id[i]) + (v.w == id[i]) - (q == ((lane + 32 * i) & ~3));
+                }
+                twice = n != 0;
+            }
+            if (__any_sync(0xffffffffu, twice)) {
+                for (int j = lane; j < P.k; j += 32) {
+                    float s = 0.f;
+                    for (int q = 0; q < P.k; ++q) s += ids[q] == ids[j] ? pr[q] : 0.f;
+                    pm[j] = s;
+                }
+            }
+        }
+        return S;
+    }
+};
+
 template <bool F32, bool SAFE>
 __device__ __forceinline__ float unit_sum(const uint4 &raw, float c, float m, float mc)
 {
@@ -450,6 +531,9 @@ distill_cta_kernel(const DistillParams P, const int S_CTAS)
         // ------------------------------------------------------------------ helper
         int i = 0;
         float w_next = first < P.rows ? (P.w ? P.w[first] : P.w_all) : 0.f;
+        float tl = P.tlse && first < P.rows ? P.tlse[first] : 0.f;
+        Entries ahead;
+        if (brief && first < P.rows) ahead.load(P, first, lane);
         for (int64_t row = first; row < P.rows; row += step, ++i) {
             const int b = i & 1;
             const uint32_t ph = (uint32_t)i & 1, lph = (uint32_t)(i >> 1) & 1;
@@ -461,28 +545,14 @@ distill_cta_kernel(const DistillParams P, const int S_CTAS)
             if (!ok) break;
             float S = 0.f;
             if (w != 0.f) {
-                S = teacher_row(P, row, lane, ids, logp);
-                if (S != 0.f && brief) {
-                    for (int j = lane; j < k4; j += 32) {
-                        pr[j] = j < P.k && ids[j] >= 0 ? expf(logp[j]) : 0.f;
-                        if (j >= P.k) ids[j] = -1;
-                    }
-                    __syncwarp();
-                    // what a listed class loses: its probability, over all entries that name it
-                    if (MODE & BWD) {
-                        for (int j = lane; j < P.k; j += 32) {
-                            const int id = ids[j];
-                            float p = 0.f;
-                            for (int q = 0; q < k4; q += 4) {
-                                const int4 i4 = *reinterpret_cast<const int4 *>(ids + q);
-                                const float4 p4 = *reinterpret_cast<const float4 *>(pr + q);
-                                p += (i4.x == id ? p4.x : 0.f) + (i4.y == id ? p4.y : 0.f) + (i4.z == id ? p4.z : 0.f) + (i4.w == id ? p4.w : 0.f);
-                            }
-                            pm[j] = p;
-                        }
-                    }
+                if (brief) {
+                    S = ahead.template to_lists<(MODE & BWD) != 0>(P, tl, lane, k4, ids, logp, pr, pm);
+                } else {
+                    S = teacher_row(P, row, lane, ids, logp);
                 }
             }
+            if (brief && row + step < P.rows) ahead.load(P, row + step, lane);
+            if (P.tlse && row + step < P.rows) tl = P.tlse[row + step];
             if (lane == 0) { slot[b].S = S; slot[b].w = w; }
             int off, nu, u0, u1;
             geometry(row, off, nu, u0, u1);
