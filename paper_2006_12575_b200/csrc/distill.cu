@@ -8,10 +8,12 @@
 //
 // Rows of odd length start at any element, so a row is walked in 16-byte units aligned in memory; a unit that is not
 // wholly inside the row is handled element by element.
-//   c <= 32 (k <= 32): one thread per row, 256 rows at a time through shared memory.
-//   c <= 1024:         one warp per row, the row stays in registers.
-//   wider:             one CTA per row, or a cluster of up to 8 CTAs where a row does not fit in the shared memory of one or
-//                      rows are few; they exchange maximum and sum through distributed shared memory.
+//   c <= 128, k <= 32:  one thread per row, many rows at a time through shared memory.
+//   c <= 1272 bf16 or 636 fp32, k <= 128:  one warp per row, the row in registers, the next row on its way (held so, rows of
+//           3000 classes took 389 us where the CTA form takes 251: too few warps fit).
+//   c <= 1024, longer lists:  one warp per row.
+//   wider:  one CTA per row, or a cluster of up to 8 CTAs where a row does not fit in the shared memory of one or rows are
+//           few; they exchange maximum and sum through distributed shared memory.
 #include <cuda.h>
 #include <float.h>
 #include "common.cuh"
@@ -26,6 +28,7 @@ constexpr int MAX_PARTS = 4096;                     // partial losses, one per C
 constexpr int MAX_K = 1024;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr int WR_WARPS = 8, WR_MAX_C = 1024;
+constexpr int RW_MAX_UNITS = 5;                     // 16-byte units per lane of a row held by one warp
 
 struct DistillParams {
     const void *z;
@@ -136,6 +139,14 @@ __device__ __forceinline__ float warp_sum(float v)
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
+// largest value of the warp, none of them NaN: floats ordered as integers, one instruction for the warp
+__device__ __forceinline__ float warp_max_fast(float v)
+{
+    int i = __float_as_int(v);
+    i ^= (i >> 31) & 0x7fffffff;
+    i = __reduce_max_sync(0xffffffffu, i);
+    return __int_as_float(i ^ ((i >> 31) & 0x7fffffff));
+}
 // One warp reads the teacher's entries of a row: ids (-1: absent) and log p to shared memory; returns S (0: no entry left).
 __device__ __forceinline__ float teacher_row(const DistillParams &P, int64_t row, int lane, int *ids, float *logp)
 {
@@ -172,8 +183,92 @@ __device__ __forceinline__ float teacher_row(const DistillParams &P, int64_t row
     return P.tlse || S != S ? S : 1.f;
 }
 
+// A row's teacher entries in the registers of a warp (k <= 32 KE), lane + 32 i, so that they can be loaded a row ahead.
+constexpr int SHORT_K = 128;
+template <int KE> struct Entries {
+    int id[KE];
+    float t[KE];
+    __device__ __forceinline__ void load(const DistillParams &P, int64_t row, int lane)
+    {
+#pragma unroll
+        for (int i = 0; i < KE; ++i) {
+            const int j = lane + 32 * i;
+            id[i] = j < P.k ? P.idx[row * P.k + j] : -1;
+            t[i] = j < P.k ? P.t[row * P.k + j] : 0.f;
+        }
+    }
+    // ids of absent entries become -1; p and log p of the others.  Returns S (0: no entry left).
+    __device__ __forceinline__ float prepare(const DistillParams &P, float tlse, float (&p)[KE], float (&logp)[KE])
+    {
+        const float inv_t = 1.f / P.temp, c2 = LOG2E / P.temp;
+        float m = -FLT_MAX;
+        bool some = false;
+#pragma unroll
+        for (int i = 0; i < KE; ++i) {
+            if ((uint32_t)id[i] >= (uint32_t)P.c) id[i] = -1;
+            p[i] = logp[i] = 0.f;
+            if (id[i] < 0) continue;
+            some |= t[i] != -INFINITY;                              // NaN counts
+            m = fmaxf(m, t[i]);
+        }
+        if (!__any_sync(0xffffffffu, some)) return 0.f;
+        float S = 0.f;
+        if (P.tlse) {
+#pragma unroll
+            for (int i = 0; i < KE; ++i) {
+                logp[i] = fmaf(t[i], inv_t, -tlse);
+                p[i] = id[i] >= 0 ? expf(logp[i]) : 0.f;
+                S += p[i];
+            }
+            return warp_sum(S);
+        }
+        m = warp_max_fast(m);
+#pragma unroll
+        for (int i = 0; i < KE; ++i) { p[i] = id[i] >= 0 ? ex2((t[i] - m) * c2) : 0.f; S += p[i]; }
+        S = warp_sum(S);
+        const float ls = logf(S), inv = 1.f / S;
+#pragma unroll
+        for (int i = 0; i < KE; ++i) { p[i] *= inv; logp[i] = (t[i] - m) * inv_t - ls; }
+        return S == S ? 1.f : NAN;
+    }
+    // pm = p summed over the entries that name the same class.  ids, pr: 32 KE words of shared memory of this warp, which
+    // then hold ids and p (k4: k up to a multiple of 4).
+    __device__ __forceinline__ void merge(int k, int k4, int lane, const float (&p)[KE], float (&pm)[KE], int *ids, float *pr) const
+    {
+        bool twice = false;
+#pragma unroll
+        for (int i = 0; i < KE; ++i) {
+            const int j = lane + 32 * i;
+            if (j < k4) { ids[j] = id[i]; pr[j] = p[i]; }
+            pm[i] = p[i];
+        }
+        __syncwarp();
+        if (k <= 32) {
+            const uint32_t same = __match_any_sync(0xffffffffu, id[0]);      // by every lane, also those without an entry
+            twice = id[0] >= 0 && same != 1u << lane;
+        } else {
+            int n = 0;                                              // entries equal to one of this lane's, but for itself
+            for (int q = 0; q < k4; q += 4) {
+                const int4 v = *reinterpret_cast<const int4 *>(ids + q);
+#pragma unroll
+                for (int i = 0; i < KE; ++i)
+                    if (id[i] >= 0) n += (v.x == id[i]) + (v.y == id[i]) + (v.z == id[i]) + (v.w == id[i]) - (q == ((lane + 32 * i) & ~3));
+            }
+            twice = n != 0;
+        }
+        if (__any_sync(0xffffffffu, twice)) {
+#pragma unroll
+            for (int i = 0; i < KE; ++i) {
+                float s = 0.f;
+                for (int q = 0; q < k; ++q) s += ids[q] == id[i] ? pr[q] : 0.f;
+                pm[i] = s;
+            }
+        }
+    }
+};
+
 // ----------------------------------------------------------------------------------------------------------------------
-// one warp per row
+// one warp per row, lists of any length
 // ----------------------------------------------------------------------------------------------------------------------
 template <bool F32, int MODE>
 __global__ void __launch_bounds__(WR_WARPS * 32)
@@ -280,6 +375,224 @@ distill_warp_kernel(const DistillParams P)
     }
 }
 
+// largest element of a unit
+template <bool F32> __device__ __forceinline__ float unit_max(const uint4 &r)
+{
+    if constexpr (F32) {
+        return fmaxf(fmaxf(__uint_as_float(r.x), __uint_as_float(r.y)), fmaxf(__uint_as_float(r.z), __uint_as_float(r.w)));
+    } else {
+        const __nv_bfloat162 *h = reinterpret_cast<const __nv_bfloat162 *>(&r);
+        const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+        return fmaxf(__low2float(m), __high2float(m));
+    }
+}
+// pair i of a unit as two packed fp32 values
+template <bool F32> __device__ __forceinline__ ptx::f32x2 unit_pair(const uint4 &r, int i)
+{
+    if constexpr (F32) return i == 0 ? ptx::pack2(r.x, r.y) : ptx::pack2(r.z, r.w);
+    const uint32_t w = i == 0 ? r.x : i == 1 ? r.y : i == 2 ? r.z : r.w;
+    return ptx::pack2(w << 16, w & 0xFFFF0000u);
+}
+// e^((z - m) / T) of a packed pair: 2^(z c - m c) in one packed FMA, or, where the products could overflow, the difference first
+template <bool SAFE> __device__ __forceinline__ ptx::f32x2 pair_exp(ptx::f32x2 z, float c, float m, float mc)
+{
+    float a, b;
+    if (SAFE) {
+        ptx::unpack2(z, a, b);
+        a = (a - m) * c; b = (b - m) * c;
+    } else {
+        ptx::unpack2(ptx::fma2(z, ptx::twice(c), ptx::twice(-mc)), a, b);
+    }
+    return ptx::pack2(__float_as_uint(ex2(a)), __float_as_uint(ex2(b)));
+}
+
+template <bool F32, bool SAFE>
+__device__ __forceinline__ float unit_sum(const uint4 &raw, float c, float m, float mc)
+{
+    ptx::f32x2 s = 0;
+#pragma unroll
+    for (int j = 0; j < Elem<F32>::E / 2; ++j) s = ptx::add2(s, pair_exp<SAFE>(unit_pair<F32>(raw, j), c, m, mc));
+    float a, b;
+    ptx::unpack2(s, a, b);
+    return a + b;
+}
+
+// gradient of a unit before the listed classes are taken off.  KIND 0: from maximum and sum; 1: the same where z c could
+// overflow; 2: from a given log-sum m: e^(z / T - m), the difference before the change of base (c = 1 / T)
+template <bool F32, int KIND>
+__device__ __forceinline__ uint4 unit_grad(const uint4 &raw, float c, float m, float mc, float gq)
+{
+    uint32_t o[4];
+#pragma unroll
+    for (int j = 0; j < Elem<F32>::E / 2; ++j) {
+        ptx::f32x2 e = unit_pair<F32>(raw, j);
+        float x, y;
+        if (KIND == 2) {
+            ptx::unpack2(ptx::mul2(ptx::fma2(e, ptx::twice(c), ptx::twice(-m)), ptx::twice(LOG2E)), x, y);
+            e = ptx::pack2(__float_as_uint(ex2(x)), __float_as_uint(ex2(y)));
+        } else {
+            e = pair_exp<KIND == 1>(e, c, m, mc);
+        }
+        ptx::unpack2(ptx::mul2(e, ptx::twice(gq)), x, y);
+        if constexpr (F32) {
+            o[2 * j] = __float_as_uint(x); o[2 * j + 1] = __float_as_uint(y);
+        } else {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+            o[j] = *reinterpret_cast<const uint32_t *>(&h);
+        }
+    }
+    return make_uint4(o[0], o[1], o[2], o[3]);
+}
+
+// a unit of the gradient, already in its type
+template <bool F32>
+__device__ __forceinline__ void put_unit(void *dz, int64_t at, int off, bool same, int u, int c, const uint4 &o)
+{
+    constexpr int E = Elem<F32>::E;
+    const int lo = u * E - off;
+    if (same && lo >= 0 && lo + E <= c) {
+        *reinterpret_cast<uint4 *>((char *)dz + ((at + lo) << Elem<F32>::SHIFT)) = o;
+    } else {
+        float v[E];
+        unit_values<F32>(o, v);
+#pragma unroll
+        for (int j = 0; j < E; ++j) if (lo + j >= 0 && lo + j < c) put<F32>(dz, at + lo + j, v[j]);
+    }
+}
+
+// ----------------------------------------------------------------------------------------------------------------------
+// one warp per row, short lists
+// ----------------------------------------------------------------------------------------------------------------------
+// A warp has few instructions per row and long latencies in front of them (weight -> entries -> listed logits), so they are
+// taken out of the chain: entries and weight are loaded two rows ahead, the row and its listed logits one row ahead, all in
+// registers.  NU units of 16 bytes per lane.
+template <bool F32, int MODE, int NU, int KE>
+__global__ void __launch_bounds__(WR_WARPS * 32)
+distill_row_kernel(const DistillParams P)
+{
+    constexpr int E = Elem<F32>::E;
+    __shared__ __align__(16) int sh_ids[WR_WARPS][32 * KE];
+    __shared__ __align__(16) float sh_p[WR_WARPS][32 * KE];
+    __shared__ double wl[WR_WARPS];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, k4 = (P.k + 3) & ~3;
+    const float c2 = LOG2E / P.temp, inv_t = 1.f / P.temp;
+    const uint32_t low = F32 ? 0xFF800000u : 0xFF80FF80u;                   // -inf
+    double total = 0;
+    pdl_launch_dependents();
+    pdl_wait();
+    const int64_t first = (int64_t)blockIdx.x * WR_WARPS + warp, step = (int64_t)gridDim.x * WR_WARPS;
+    // one row ahead (b_) and two rows ahead (a_)
+    Entries<KE> a_e, b_e;
+    float a_w = 0.f, b_w = 0.f, a_tl = 0.f, b_tl = 0.f, b_lse = 0.f, b_z[KE];
+    uint4 b_raw[NU];
+    auto far = [&](int64_t row) {
+        a_w = 0.f;
+        if (row >= P.rows) return;
+        a_e.load(P, row, lane);
+        a_w = P.w ? P.w[row] : P.w_all;
+        if (P.tlse) a_tl = P.tlse[row];
+    };
+    auto near = [&](int64_t row) {                                          // what far() loaded, and the row itself
+        b_e = a_e; b_w = a_w; b_tl = a_tl;
+        if (b_w == 0.f) return;
+        const int64_t at = row * P.pz;
+        const int off = misalign<F32>(P.z, at), nu = (P.c + off + E - 1) / E;
+#pragma unroll
+        for (int i = 0; i < NU; ++i) b_raw[i] = lane + 32 * i < nu ? load_unit<F32>(P.z, at, off, lane + 32 * i, P.c) : make_uint4(low, low, low, low);
+#pragma unroll
+        for (int i = 0; i < KE; ++i) b_z[i] = (uint32_t)b_e.id[i] < (uint32_t)P.c ? elem<F32>(P.z, at + b_e.id[i]) : 0.f;
+        if (!(MODE & FWD)) b_lse = P.lse_in[row];
+    };
+    far(first);
+    near(first);
+    far(first + step);
+    for (int64_t row = first; row < P.rows; row += step) {
+        const float w = b_w, tl = b_tl, lse_in = b_lse;
+        Entries<KE> e = b_e;
+        float zt[KE];
+        uint4 raw[NU];
+#pragma unroll
+        for (int i = 0; i < KE; ++i) zt[i] = b_z[i];
+#pragma unroll
+        for (int i = 0; i < NU; ++i) raw[i] = b_raw[i];
+        if (row + step < P.rows) {
+            near(row + step);
+            far(row + 2 * step);
+        }
+        const int64_t dat = row * P.pdz;
+        const int off = misalign<F32>(P.z, row * P.pz), nu = (P.c + off + E - 1) / E;
+        const bool same = (MODE & BWD) && off == misalign<F32>(P.dz, dat);
+        float p[KE], logp[KE], S = 0.f, loss = 0.f, lse = 0.f;
+        if (w != 0.f) S = e.prepare(P, tl, p, logp);
+        if (S != 0.f) {
+            float m, scale = 1.f;
+            if constexpr (MODE & FWD) {
+                m = -FLT_MAX;
+#pragma unroll
+                for (int i = 0; i < NU; ++i) m = fmaxf(m, unit_max<F32>(raw[i]));
+                m = warp_max_fast(m);
+                const float mc = m * c2;
+                float s = 0.f;
+                if (fabsf(mc) < 1e38f) {
+#pragma unroll
+                    for (int i = 0; i < NU; ++i) s += unit_sum<F32, false>(raw[i], c2, m, mc);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < NU; ++i) s += unit_sum<F32, true>(raw[i], c2, m, mc);
+                }
+                s = warp_sum(s);
+                if (s == 0.f) s = NAN;                                      // no logit above -inf: there is no softmax
+                const float ls = logf(s);
+                lse = m * inv_t + ls;
+                scale = 1.f / s;
+#pragma unroll
+                for (int i = 0; i < KE; ++i) if (p[i] != 0.f) loss += p[i] * (logp[i] - ((zt[i] - m) * inv_t - ls));
+                loss = warp_sum(loss) * P.temp * P.temp;
+            } else {
+                m = lse_in;
+            }
+            if constexpr (MODE & BWD) {
+                const float gT = w * P.temp, gq = gT * S * scale, mc = m * c2;
+                const bool fits = fabsf(mc) < 1e38f;
+#pragma unroll
+                for (int i = 0; i < NU; ++i) {
+                    const int u = lane + 32 * i;
+                    if (u >= nu) break;
+                    uint4 o;
+                    if constexpr (MODE & FWD) o = fits ? unit_grad<F32, 0>(raw[i], c2, m, mc, gq) : unit_grad<F32, 1>(raw[i], c2, m, mc, gq);
+                    else o = unit_grad<F32, 2>(raw[i], inv_t, m, mc, gq);
+                    put_unit<F32>(P.dz, dat, off, same, u, P.c, o);
+                }
+                float pm[KE];
+                e.merge(P.k, k4, lane, p, pm, sh_ids[warp], sh_p[warp]);
+                __syncwarp();                                               // the listed classes go over what the dense pass wrote
+#pragma unroll
+                for (int i = 0; i < KE; ++i)
+                    if (e.id[i] >= 0) put<F32>(P.dz, dat + e.id[i], gT * (S * (scale * power<MODE>(zt[i], c2, inv_t, m)) - pm[i]));
+            }
+        } else if constexpr (MODE & BWD) {
+            for (int u = lane; u < nu; u += 32) put_unit<F32>(P.dz, dat, off, same, u, P.c, make_uint4(0, 0, 0, 0));
+        }
+        if constexpr (MODE & FWD) {
+            if (lane == 0) {
+                if (P.loss_rows) P.loss_rows[row] = loss;
+                if (P.lse_out) P.lse_out[row] = lse;
+                if (w != 0.f) total += (double)w * loss;
+            }
+        }
+        __syncwarp();                                                       // sh_ids, sh_p are free again
+    }
+    if ((MODE & FWD) && P.part) {
+        if (lane == 0) wl[warp] = total;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            double a = 0;
+            for (int i = 0; i < WR_WARPS; ++i) a += wl[i];
+            P.part[blockIdx.x] = a;
+        }
+    }
+}
+
 // ----------------------------------------------------------------------------------------------------------------------
 // one CTA, or a cluster of CTAs, per row
 // ----------------------------------------------------------------------------------------------------------------------
@@ -321,167 +634,8 @@ __device__ __forceinline__ uint32_t peer_addr(uint32_t addr, uint32_t rank)
     return r;
 }
 
-// largest element of a unit
-template <bool F32> __device__ __forceinline__ float unit_max(const uint4 &r)
-{
-    if constexpr (F32) {
-        return fmaxf(fmaxf(__uint_as_float(r.x), __uint_as_float(r.y)), fmaxf(__uint_as_float(r.z), __uint_as_float(r.w)));
-    } else {
-        const __nv_bfloat162 *h = reinterpret_cast<const __nv_bfloat162 *>(&r);
-        const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
-        return fmaxf(__low2float(m), __high2float(m));
-    }
-}
-// largest value of the warp, none of them NaN: floats ordered as integers, one instruction for the warp
-__device__ __forceinline__ float warp_max_fast(float v)
-{
-    int i = __float_as_int(v);
-    i ^= (i >> 31) & 0x7fffffff;
-    i = __reduce_max_sync(0xffffffffu, i);
-    return __int_as_float(i ^ ((i >> 31) & 0x7fffffff));
-}
-// pair i of a unit as two packed fp32 values
-template <bool F32> __device__ __forceinline__ ptx::f32x2 unit_pair(const uint4 &r, int i)
-{
-    if constexpr (F32) return i == 0 ? ptx::pack2(r.x, r.y) : ptx::pack2(r.z, r.w);
-    const uint32_t w = i == 0 ? r.x : i == 1 ? r.y : i == 2 ? r.z : r.w;
-    return ptx::pack2(w << 16, w & 0xFFFF0000u);
-}
-// e^((z - m) / T) of a packed pair: 2^(z c - m c) in one packed FMA, or, where the products could overflow, the difference first
-template <bool SAFE> __device__ __forceinline__ ptx::f32x2 pair_exp(ptx::f32x2 z, float c, float m, float mc)
-{
-    float a, b;
-    if (SAFE) {
-        ptx::unpack2(z, a, b);
-        a = (a - m) * c; b = (b - m) * c;
-    } else {
-        ptx::unpack2(ptx::fma2(z, ptx::twice(c), ptx::twice(-mc)), a, b);
-    }
-    return ptx::pack2(__float_as_uint(ex2(a)), __float_as_uint(ex2(b)));
-}
-
-constexpr int SHORT_K = 128;
 __host__ __device__ constexpr int lists_of(int k) { return k <= SHORT_K ? 5 : 3; }
 constexpr int CR_MAX_THREADS = 1024, CR_CHUNKS = 16;
-
-// Short lists (k <= SHORT_K): a row's entries in the helper's registers, lane + 32 i, loaded a row ahead.
-struct Entries {
-    int id[SHORT_K / 32];
-    float t[SHORT_K / 32];
-    __device__ __forceinline__ void load(const DistillParams &P, int64_t row, int lane)
-    {
-#pragma unroll
-        for (int i = 0; i < SHORT_K / 32; ++i) {
-            const int j = lane + 32 * i;
-            id[i] = j < P.k ? P.idx[row * P.k + j] : -1;
-            t[i] = j < P.k ? P.t[row * P.k + j] : 0.f;
-        }
-    }
-    // To the lists: ids (-1: absent), log p, p, and pm = p summed over the entries that name the same class.  Returns S.
-    template <bool GRAD>
-    __device__ __forceinline__ float to_lists(const DistillParams &P, float tlse, int lane, int k4, int *ids, float *logp, float *pr, float *pm)
-    {
-        const float inv_t = 1.f / P.temp, c2 = LOG2E / P.temp;
-        float m = -FLT_MAX, p[SHORT_K / 32];
-        bool some = false;
-#pragma unroll
-        for (int i = 0; i < SHORT_K / 32; ++i) {
-            if ((uint32_t)id[i] >= (uint32_t)P.c) id[i] = -1;
-            if (id[i] < 0) continue;
-            some |= t[i] != -INFINITY;                              // NaN counts
-            m = fmaxf(m, t[i]);
-        }
-        if (!__any_sync(0xffffffffu, some)) return 0.f;
-        float S = 0.f, ls = 0.f, inv = 1.f;
-        if (!P.tlse) {
-            m = warp_max_fast(m);
-#pragma unroll
-            for (int i = 0; i < SHORT_K / 32; ++i) { p[i] = id[i] >= 0 ? ex2((t[i] - m) * c2) : 0.f; S += p[i]; }
-            S = warp_sum(S);
-            ls = logf(S);
-            inv = 1.f / S;
-            S = S == S ? 1.f : NAN;
-        } else {
-#pragma unroll
-            for (int i = 0; i < SHORT_K / 32; ++i) { p[i] = id[i] >= 0 ? expf(fmaf(t[i], inv_t, -tlse)) : 0.f; S += p[i]; }
-            S = warp_sum(S);
-        }
-#pragma unroll
-        for (int i = 0; i < SHORT_K / 32; ++i) {
-            const int j = lane + 32 * i;
-            p[i] *= inv;
-            if (j < k4) {
-                ids[j] = id[i];
-                logp[j] = P.tlse ? fmaf(t[i], inv_t, -tlse) : (t[i] - m) * inv_t - ls;
-                pr[j] = p[i];
-                pm[j] = p[i];
-            }
-        }
-        __syncwarp();
-        if (GRAD) {
-            bool twice = false;
-            if (P.k <= 32) {
-                const uint32_t same = __match_any_sync(0xffffffffu, id[0]);      // by every lane, also those without an entry
-                twice = id[0] >= 0 && same != 1u << lane;
-            } else {
-                int n = 0;                                           // entries equal to one of this lane's: itself, and any other
-                for (int q = 0; q < k4; q += 4) {
-                    const int4 v = *reinterpret_cast<const int4 *>(ids + q);
-#pragma unroll
-                    for (int i = 0; i < SHORT_K / 32; ++i)
-                        if (id[i] >= 0) n += (v.x == id[i]) + (v.y == id[i]) + (v.z == id[i]) + (v.w == id[i]) - (q == ((lane + 32 * i) & ~3));
-                }
-                twice = n != 0;
-            }
-            if (__any_sync(0xffffffffu, twice)) {
-                for (int j = lane; j < P.k; j += 32) {
-                    float s = 0.f;
-                    for (int q = 0; q < P.k; ++q) s += ids[q] == ids[j] ? pr[q] : 0.f;
-                    pm[j] = s;
-                }
-            }
-        }
-        return S;
-    }
-};
-
-template <bool F32, bool SAFE>
-__device__ __forceinline__ float unit_sum(const uint4 &raw, float c, float m, float mc)
-{
-    ptx::f32x2 s = 0;
-#pragma unroll
-    for (int j = 0; j < Elem<F32>::E / 2; ++j) s = ptx::add2(s, pair_exp<SAFE>(unit_pair<F32>(raw, j), c, m, mc));
-    float a, b;
-    ptx::unpack2(s, a, b);
-    return a + b;
-}
-
-// gradient of a unit before the listed classes are taken off.  KIND 0: from maximum and sum; 1: the same where z c could
-// overflow; 2: from a given log-sum m: e^(z / T - m), the difference before the change of base (c = 1 / T)
-template <bool F32, int KIND>
-__device__ __forceinline__ uint4 unit_grad(const uint4 &raw, float c, float m, float mc, float gq)
-{
-    uint32_t o[4];
-#pragma unroll
-    for (int j = 0; j < Elem<F32>::E / 2; ++j) {
-        ptx::f32x2 e = unit_pair<F32>(raw, j);
-        float x, y;
-        if (KIND == 2) {
-            ptx::unpack2(ptx::mul2(ptx::fma2(e, ptx::twice(c), ptx::twice(-m)), ptx::twice(LOG2E)), x, y);
-            e = ptx::pack2(__float_as_uint(ex2(x)), __float_as_uint(ex2(y)));
-        } else {
-            e = pair_exp<KIND == 1>(e, c, m, mc);
-        }
-        ptx::unpack2(ptx::mul2(e, ptx::twice(gq)), x, y);
-        if constexpr (F32) {
-            o[2 * j] = __float_as_uint(x); o[2 * j + 1] = __float_as_uint(y);
-        } else {
-            const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
-            o[j] = *reinterpret_cast<const uint32_t *>(&h);
-        }
-    }
-    return make_uint4(o[0], o[1], o[2], o[3]);
-}
 
 template <bool F32, int MODE>
 __global__ void __launch_bounds__(CR_MAX_THREADS, 1)
@@ -532,7 +686,7 @@ distill_cta_kernel(const DistillParams P, const int S_CTAS)
         int i = 0;
         float w_next = first < P.rows ? (P.w ? P.w[first] : P.w_all) : 0.f;
         float tl = P.tlse && first < P.rows ? P.tlse[first] : 0.f;
-        Entries ahead;
+        Entries<SHORT_K / 32> ahead;
         if (brief && first < P.rows) ahead.load(P, first, lane);
         for (int64_t row = first; row < P.rows; row += step, ++i) {
             const int b = i & 1;
@@ -546,7 +700,14 @@ distill_cta_kernel(const DistillParams P, const int S_CTAS)
             float S = 0.f;
             if (w != 0.f) {
                 if (brief) {
-                    S = ahead.template to_lists<(MODE & BWD) != 0>(P, tl, lane, k4, ids, logp, pr, pm);
+                    float p[SHORT_K / 32], lp[SHORT_K / 32], q[SHORT_K / 32];
+                    S = ahead.prepare(P, tl, p, lp);
+                    if (S != 0.f) {
+                        ahead.merge(P.k, k4, lane, p, q, ids, pr);
+#pragma unroll
+                        for (int e = 0; e < SHORT_K / 32; ++e)
+                            if (lane + 32 * e < k4) { logp[lane + 32 * e] = lp[e]; pm[lane + 32 * e] = q[e]; }
+                    }
                 } else {
                     S = teacher_row(P, row, lane, ids, logp);
                 }
@@ -696,15 +857,7 @@ distill_cta_kernel(const DistillParams P, const int S_CTAS)
                         uint4 o;
                         if constexpr (MODE & FWD) o = kind == 0 ? unit_grad<F32, 0>(raw, c2, m, mc, gq) : unit_grad<F32, 1>(raw, c2, m, mc, gq);
                         else o = unit_grad<F32, 2>(raw, inv_t, m, mc, gq);
-                        const int lo = (u0 + u) * E - off;
-                        if (same && lo >= 0 && lo + E <= P.c) {
-                            *reinterpret_cast<uint4 *>((char *)P.dz + ((dat + lo) << Elem<F32>::SHIFT)) = o;
-                        } else {
-                            float v[E];
-                            unit_values<F32>(o, v);
-#pragma unroll
-                            for (int j = 0; j < E; ++j) if (lo + j >= 0 && lo + j < P.c) put<F32>(P.dz, dat + lo + j, v[j]);
-                        }
+                        put_unit<F32>(P.dz, dat, off, same, u0 + u, P.c, o);
                     }
                     if (!(ok = consumer_sync(cons, cphase, lane, abort_flag))) break;    // the listed classes go over what the dense pass wrote
                     for (int j = tid; j < P.k; j += nthr) {
@@ -746,23 +899,27 @@ distill_cta_kernel(const DistillParams P, const int S_CTAS)
 // ----------------------------------------------------------------------------------------------------------------------
 // one thread per row: few classes (a segmentation network's), many rows
 // ----------------------------------------------------------------------------------------------------------------------
-// 256 rows per turn go through shared memory as fp32, so that global memory sees whole lines although a row is only a few
+// 256 rows (128 of more than 32 classes) per turn go through shared memory as fp32, so that global memory sees whole lines although a row is only a few
 // words; the row pitch there is odd, so that the threads of a warp, each on its own row, hit different banks.  A thread
 // adds its gradient up in its own row, listed classes after the dense part, so a class listed twice is simply met twice.
-constexpr int TR_ROWS = 256, TR_MAX_C = 32, TR_MAX_K = 32;
+constexpr int TR_MAX_C = 128, TR_REG_C = 32, TR_MAX_K = 32;
+__host__ __device__ constexpr int tr_rows(int cp) { return cp ? 256 : 128; }      // CP = 0: more than TR_REG_C classes
 
 template <bool F32, int MODE, int CP>
-__global__ void __launch_bounds__(TR_ROWS)
+__global__ void __launch_bounds__(tr_rows(CP))
 distill_thread_kernel(const DistillParams P, const int vec)
 {
-    constexpr int E = Elem<F32>::E;
-    extern __shared__ __align__(16) float rows_s[];                    // [256][c | 1], then ids and logits [256][k | 1]
+    constexpr int E = Elem<F32>::E, TR_ROWS = tr_rows(CP);
+    extern __shared__ __align__(16) float rows_s[];                    // [rows][c | 1], then ids and logits [rows][k | 1]
     __shared__ double wl[TR_ROWS / 32];
     const int tid = threadIdx.x, pc = P.c | 1, pk = P.k | 1;
     int *ids_s = (int *)(rows_s + TR_ROWS * pc);
     float *t_s = (float *)(ids_s + TR_ROWS * pk);
     const float c2 = LOG2E / P.temp, inv_t = 1.f / P.temp;
-    const uint32_t div_c = ((1u << 20) + P.c - 1) / P.c, div_k = ((1u << 20) + P.k - 1) / P.k;     // x / c = x div >> 20 for x < 256 c <= 2^13
+    // x / c = umulhi(x, ceil(2^32 / c)) for x < 2^14, c in 2 .. 128 (the error x (div c - 2^32) stays below 2^32)
+    const uint32_t div_c = (uint32_t)((0x100000000ull + P.c - 1) / P.c), div_k = (uint32_t)((0x100000000ull + P.k - 1) / P.k);
+    auto over_c = [&](int x) { return P.c == 1 ? (uint32_t)x : __umulhi((uint32_t)x, div_c); };
+    auto over_k = [&](int x) { return P.k == 1 ? (uint32_t)x : __umulhi((uint32_t)x, div_k); };
     double total = 0;
     pdl_launch_dependents();
     pdl_wait();
@@ -774,7 +931,7 @@ distill_thread_kernel(const DistillParams P, const int vec)
             for (int i = tid; i < n / E; i += TR_ROWS) {
                 float v[E];
                 unit_values<F32>(src[i], v);
-                uint32_t r = ((uint32_t)(i * E) * div_c) >> 20, col = i * E - r * P.c;
+                uint32_t r = over_c(i * E), col = i * E - r * P.c;
 #pragma unroll
                 for (int j = 0; j < E; ++j) {
                     rows_s[r * pc + col] = v[j];
@@ -782,17 +939,17 @@ distill_thread_kernel(const DistillParams P, const int vec)
                 }
             }
             for (int i = n / E * E + tid; i < n; i += TR_ROWS) {
-                const uint32_t r = ((uint32_t)i * div_c) >> 20;
+                const uint32_t r = over_c(i);
                 rows_s[r * pc + i - r * P.c] = elem<F32>(P.z, r0 * P.c + i);
             }
         } else {
             for (int i = tid; i < n; i += TR_ROWS) {
-                const uint32_t r = ((uint32_t)i * div_c) >> 20, col = i - r * P.c;
+                const uint32_t r = over_c(i), col = i - r * P.c;
                 rows_s[r * pc + col] = elem<F32>(P.z, (r0 + r) * P.pz + col);
             }
         }
         for (int i = tid; i < nr * P.k; i += TR_ROWS) {
-            const uint32_t r = ((uint32_t)i * div_k) >> 20, j = i - r * P.k;
+            const uint32_t r = over_k(i), j = i - r * P.k;
             ids_s[r * pk + j] = P.idx[r0 * P.k + i];
             t_s[r * pk + j] = P.t[r0 * P.k + i];
         }
@@ -826,38 +983,57 @@ distill_thread_kernel(const DistillParams P, const int vec)
         }
         float loss = 0.f, lse = 0.f;
         if (S != 0.f) {
-            float v[CP];
+            // CP > 0: the row in registers; otherwise it is walked in shared memory, where the exponentials replace the logits
+            float v[CP ? CP : 1];
+            if constexpr (CP > 0) {
 #pragma unroll
-            for (int i = 0; i < CP; ++i) v[i] = i < P.c ? zr[i] : -INFINITY;
+                for (int i = 0; i < CP; ++i) v[i] = i < P.c ? zr[i] : -INFINITY;
+            }
             float m, scale = 1.f, ls = 0.f;
             if constexpr (MODE & FWD) {
                 m = -FLT_MAX;
-#pragma unroll
-                for (int i = 0; i < CP; ++i) m = fmaxf(m, v[i]);
                 float s = 0.f;
+                if constexpr (CP > 0) {
 #pragma unroll
-                for (int i = 0; i < CP; ++i) { v[i] = ex2((v[i] - m) * c2); s += v[i]; }
+                    for (int i = 0; i < CP; ++i) m = fmaxf(m, v[i]);
+#pragma unroll
+                    for (int i = 0; i < CP; ++i) { v[i] = ex2((v[i] - m) * c2); s += v[i]; }
+                } else {
+#pragma unroll 4
+                    for (int i = 0; i < P.c; ++i) m = fmaxf(m, zr[i]);
+                }
+                // the listed logits, before their exponentials take their place
+                float zl = 0.f;
+                for (int j = 0; j < P.k; ++j) {
+                    if ((uint32_t)id[j] >= (uint32_t)P.c) continue;
+                    const float lp = fmaf(tr[j], inv_t, -lt), p = expf(lp);
+                    if (p != 0.f) { loss += p * (lp - (zr[id[j]] - m) * inv_t); zl += p; }
+                }
+                if constexpr (CP == 0) {
+#pragma unroll 4
+                    for (int i = 0; i < P.c; ++i) { const float e = ex2((zr[i] - m) * c2); s += e; if (MODE & BWD) zr[i] = e; }
+                }
                 if (s == 0.f) s = NAN;
                 scale = 1.f / s;
                 ls = logf(s);
                 lse = m * inv_t + ls;
+                loss = (loss + zl * ls) * P.temp * P.temp;
             } else {
                 m = lin;
+                if constexpr (CP > 0) {
 #pragma unroll
-                for (int i = 0; i < CP; ++i) v[i] = ex2(fmaf(v[i], inv_t, -m) * LOG2E);
+                    for (int i = 0; i < CP; ++i) v[i] = ex2(fmaf(v[i], inv_t, -m) * LOG2E);
+                }
             }
             const float gT = w * P.temp, gq = gT * S * scale;
-            if constexpr (MODE & FWD) {
-                for (int j = 0; j < P.k; ++j) {
-                    if ((uint32_t)id[j] >= (uint32_t)P.c) continue;
-                    const float lp = fmaf(tr[j], inv_t, -lt), p = expf(lp);
-                    if (p != 0.f) loss += p * (lp - ((zr[id[j]] - m) * inv_t - ls));
-                }
-                loss *= P.temp * P.temp;
-            }
             if constexpr (MODE & BWD) {
+                if constexpr (CP > 0) {
 #pragma unroll
-                for (int i = 0; i < CP; ++i) if (i < P.c) zr[i] = gq * v[i];
+                    for (int i = 0; i < CP; ++i) if (i < P.c) zr[i] = gq * v[i];
+                } else {
+#pragma unroll 4
+                    for (int i = 0; i < P.c; ++i) zr[i] = gq * ((MODE & FWD) ? zr[i] : ex2(fmaf(zr[i], inv_t, -m) * LOG2E));
+                }
                 for (int j = 0; j < P.k; ++j)
                     if ((uint32_t)id[j] < (uint32_t)P.c) zr[id[j]] -= gT * expf(fmaf(tr[j], inv_t, -lt));
             }
@@ -875,7 +1051,7 @@ distill_thread_kernel(const DistillParams P, const int vec)
                 uint4 *dst = reinterpret_cast<uint4 *>((char *)P.dz + ((r0 * P.c) << Elem<F32>::SHIFT));
                 for (int i = tid; i < n / E; i += TR_ROWS) {
                     float v[E];
-                    uint32_t r = ((uint32_t)(i * E) * div_c) >> 20, col = i * E - r * P.c;
+                    uint32_t r = over_c(i * E), col = i * E - r * P.c;
 #pragma unroll
                     for (int j = 0; j < E; ++j) {
                         v[j] = rows_s[r * pc + col];
@@ -884,12 +1060,12 @@ distill_thread_kernel(const DistillParams P, const int vec)
                     dst[i] = unit_raw<F32>(v);
                 }
                 for (int i = n / E * E + tid; i < n; i += TR_ROWS) {
-                    const uint32_t r = ((uint32_t)i * div_c) >> 20;
+                    const uint32_t r = over_c(i);
                     put<F32>(P.dz, r0 * P.c + i, rows_s[r * pc + i - r * P.c]);
                 }
             } else {
                 for (int i = tid; i < n; i += TR_ROWS) {
-                    const uint32_t r = ((uint32_t)i * div_c) >> 20, col = i - r * P.c;
+                    const uint32_t r = over_c(i), col = i - r * P.c;
                     put<F32>(P.dz, (r0 + r) * P.pdz + col, rows_s[r * pc + col]);
                 }
             }
@@ -938,13 +1114,27 @@ lamp_status_t launch_warp(const DistillParams &P, int grid, cudaStream_t st)
     return launch_pdl(true, distill_warp_kernel<F32, MODE>, dim3(grid), dim3(WR_WARPS * 32), (size_t)smem, st, P);
 }
 
+template <bool F32, int MODE, int NU>
+lamp_status_t launch_row(const DistillParams &P, int grid, cudaStream_t st)
+{
+    if (P.k <= 32) return launch_pdl(true, distill_row_kernel<F32, MODE, NU, 1>, dim3(grid), dim3(WR_WARPS * 32), (size_t)0, st, P);
+    return launch_pdl(true, distill_row_kernel<F32, MODE, NU, SHORT_K / 32>, dim3(grid), dim3(WR_WARPS * 32), (size_t)0, st, P);
+}
+template <bool F32, int MODE>
+lamp_status_t launch_row_u(const DistillParams &P, int nu, int grid, cudaStream_t st)
+{
+    if (nu == 2) return launch_row<F32, MODE, 2>(P, grid, st);
+    return launch_row<F32, MODE, RW_MAX_UNITS>(P, grid, st);
+}
+
 template <bool F32, int MODE, int CP>
 lamp_status_t launch_thread(const DistillParams &P, int grid, int vec, cudaStream_t st)
 {
+    constexpr int TR_ROWS = tr_rows(CP);
     const int smem = TR_ROWS * ((P.c | 1) + 2 * (P.k | 1)) * 4;
     if (smem > 32 * 1024) {
         static SmemAttrOnce attr;
-        const lamp_status_t s = attr.ensure(distill_thread_kernel<F32, MODE, CP>, TR_ROWS * 3 * 33 * 4);
+        const lamp_status_t s = attr.ensure(distill_thread_kernel<F32, MODE, CP>, TR_ROWS * ((CP ? 33 : TR_MAX_C + 1) + 2 * 33) * 4);
         if (s != LAMP_OK) return s;
     }
     return launch_pdl(true, distill_thread_kernel<F32, MODE, CP>, dim3(grid), dim3(TR_ROWS), (size_t)smem, st, P, vec);
@@ -956,7 +1146,8 @@ lamp_status_t launch_thread_c(const DistillParams &P, int grid, int vec, cudaStr
     if (P.c <= 8) return launch_thread<F32, MODE, 8>(P, grid, vec, st);
     if (P.c <= 12) return launch_thread<F32, MODE, 12>(P, grid, vec, st);
     if (P.c <= 16) return launch_thread<F32, MODE, 16>(P, grid, vec, st);
-    return launch_thread<F32, MODE, 32>(P, grid, vec, st);
+    if (P.c <= TR_REG_C) return launch_thread<F32, MODE, 32>(P, grid, vec, st);
+    return launch_thread<F32, MODE, 0>(P, grid, vec, st);
 }
 
 template <bool F32, int MODE>
@@ -989,11 +1180,17 @@ lamp_status_t run(DistillParams &P, bool f32, float *loss, void *ws, cudaStream_
     P.part = loss ? (double *)ws : nullptr;
     P.status = status_word_ptr();
     if (P.c <= TR_MAX_C && P.k <= TR_MAX_K) {
-        const int64_t need = (P.rows + TR_ROWS - 1) / TR_ROWS;
-        parts = (int)(need < 8ll * sms ? need : 8ll * sms);
+        const int turn = tr_rows(P.c <= TR_REG_C), room = P.c <= TR_REG_C ? 8 : 3;
+        const int64_t need = (P.rows + turn - 1) / turn;
+        parts = (int)(need < (int64_t)room * sms ? need : (int64_t)room * sms);
         if (parts > MAX_PARTS) parts = MAX_PARTS;
         const int vec = P.pz == P.c && ((uintptr_t)P.z & 15) == 0 && (!(MODE & BWD) || (P.pdz == P.c && ((uintptr_t)P.dz & 15) == 0));
         s = f32 ? launch_thread_c<true, MODE>(P, parts, vec, st) : launch_thread_c<false, MODE>(P, parts, vec, st);
+    } else if (P.k <= SHORT_K && P.c <= (f32 ? 4 : 8) * (32 * RW_MAX_UNITS - 1)) {
+        const int units = (P.c + (f32 ? 3 : 7)) / (f32 ? 4 : 8) + 1, nu = units <= 64 ? 2 : RW_MAX_UNITS;
+        const int64_t need = (P.rows + WR_WARPS - 1) / WR_WARPS, room = (int64_t)sms * (nu == 2 && P.k <= 32 ? 3 : 2);
+        parts = (int)(need < room ? need : room);
+        s = f32 ? launch_row_u<true, MODE>(P, nu, parts, st) : launch_row_u<false, MODE>(P, nu, parts, st);
     } else if (P.c <= WR_MAX_C) {
         const int64_t need = (P.rows + WR_WARPS - 1) / WR_WARPS;
         parts = (int)(need < 8ll * sms ? need : 8ll * sms);

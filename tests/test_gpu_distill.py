@@ -98,7 +98,8 @@ class Case:
 
 
 SHAPES = [(1, 1, 1), (5, 2, 1), (300, 4, 3), (1000, 10, 4), (77, 16, 16), (33, 31, 5), (40, 33, 40), (3, 100, 7), (70, 257, 64), (9, 1000, 20), (4, 1017, 9),
-          (4, 1024, 8), (5, 1025, 8), (3, 4099, 100), (2, 9000, 33), (1, 40000, 10), (2, 130001, 64), (160, 2050, 3), (700, 1500, 5), (400, 6001, 10), (321, 40007, 70), (100, 70000, 5), (77, 32, 32), (600, 20, 33)]
+          (4, 1024, 8), (5, 1025, 8), (3, 4099, 100), (2, 9000, 33), (1, 40000, 10), (2, 130001, 64), (160, 2050, 3), (700, 1500, 5), (400, 6001, 10), (321, 40007, 70), (100, 70000, 5), (77, 32, 32), (600, 20, 33), (700, 128, 32),
+          (300, 65, 8), (50, 4344, 100), (30, 2172, 33), (33, 4345, 128), (9, 2173, 129), (3000, 140, 4), (900, 600, 40)]
 
 
 @pytest.mark.parametrize("rows,c,k", SHAPES)
@@ -108,12 +109,12 @@ def test_loss_and_gradient_match_oracle(rows, c, k, dt):
 
 
 @pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("c,pitch,off", [(10, 16, 0), (10, 13, 3), (7, 24, 8), (301, 320, 5), (1001, 1003, 1), (2051, 2063, 2), (20000, 20011, 7)])
+@pytest.mark.parametrize("c,pitch,off", [(10, 16, 0), (10, 13, 3), (7, 24, 8), (77, 79, 1), (301, 320, 5), (1001, 1003, 1), (2051, 2063, 2), (20000, 20011, 7)])
 def test_slices_of_any_alignment(c, pitch, off, dt):
     Case(c, 6, c, min(c, 9), dt, temp=1.3, pitch=pitch, off=off).check()
 
 
-@pytest.mark.parametrize("c", [12, 200, 5000, 70001])
+@pytest.mark.parametrize("c", [12, 70, 200, 2100, 5000, 70001])
 @pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
 def test_rows_without_weight_or_entries(c, dt):
     k = Case(c, 9, c, 6, dt, temp=1.5)
@@ -132,7 +133,7 @@ def test_rows_without_weight_or_entries(c, dt):
     k.check()
 
 
-@pytest.mark.parametrize("c", [9, 600, 3000, 50000])
+@pytest.mark.parametrize("c", [9, 90, 600, 3000, 50000])
 @pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
 def test_masked_classes_and_rows_that_are_not_finite(c, dt):
     """Logits of -inf and of the type's lowest value (masks), listed and unlisted; +inf and NaN stay in their rows."""
@@ -159,7 +160,7 @@ def test_masked_classes_and_rows_that_are_not_finite(c, dt):
     k.check()
 
 
-@pytest.mark.parametrize("c", [9, 600, 3000, 50000, 140000])
+@pytest.mark.parametrize("c", [9, 90, 600, 3000, 50000, 140000])
 @pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
 def test_row_of_nothing_but_the_lowest_value_is_uniform(c, dt):
     k = Case(c, 3, c, 4, dt)
