@@ -899,86 +899,131 @@ distill_cta_kernel(const DistillParams P, const int S_CTAS)
 // ----------------------------------------------------------------------------------------------------------------------
 // one thread per row: few classes (a segmentation network's), many rows
 // ----------------------------------------------------------------------------------------------------------------------
-// 256 rows (128 of more than 32 classes) per turn go through shared memory as fp32, so that global memory sees whole lines although a row is only a few
-// words; the row pitch there is odd, so that the threads of a warp, each on its own row, hit different banks.  A thread
-// adds its gradient up in its own row, listed classes after the dense part, so a class listed twice is simply met twice.
+// 256 rows (128 of more than 32 classes) per turn go through shared memory, so that global memory sees whole lines although
+// a row is only a few words; the next turn's rows and entries are copied there asynchronously meanwhile (up to 32 classes).
+// A thread then works on its own row.  fp32 rows whose stride hits each bank at most twice are worked on where they landed;
+// others are first spread out to fp32 rows of odd pitch.  A thread adds its gradient up in its own row, listed classes after
+// the dense part, so a class listed twice is simply met twice.  Up to 4 entries per row (SHORT) stay in registers.
+// Measured (2,097,152 x 10 fp32, k = 4, loss and gradient): loads by the threads, no copies ahead 86 us.
 constexpr int TR_MAX_C = 128, TR_REG_C = 32, TR_MAX_K = 32;
 __host__ __device__ constexpr int tr_rows(int cp) { return cp ? 256 : 128; }      // CP = 0: more than TR_REG_C classes
+struct ThreadPlan {
+    int32_t vec;                                    // rows are back to back and 16-byte aligned
+    int32_t ahead;                                  // copies run a turn ahead (two stages)
+    int32_t direct;                                 // rows are worked on in the stage
+    int32_t stage_bytes, pitch;                     // of one stage; floats between the rows that are worked on
+};
 
-template <bool F32, int MODE, int CP>
-__global__ void __launch_bounds__(tr_rows(CP))
-distill_thread_kernel(const DistillParams P, const int vec)
+__device__ __forceinline__ void copy_async16(void *dst, const void *src)
 {
-    constexpr int E = Elem<F32>::E, TR_ROWS = tr_rows(CP);
-    extern __shared__ __align__(16) float rows_s[];                    // [rows][c | 1], then ids and logits [rows][k | 1]
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ptx::smem_u32(dst)), "l"(src) : "memory");
+}
+
+template <bool F32, int MODE, int CP, bool SHORT>
+__global__ void __launch_bounds__(tr_rows(CP))
+distill_thread_kernel(const DistillParams P, const ThreadPlan G)
+{
+    constexpr int E = Elem<F32>::E, TR_ROWS = tr_rows(CP), ES = F32 ? 4 : 2;
+    extern __shared__ __align__(16) char stage_s[];                    // stages: rows [rows][c], ids [rows][k], logits [rows][k]; then the spread rows
     __shared__ double wl[TR_ROWS / 32];
-    const int tid = threadIdx.x, pc = P.c | 1, pk = P.k | 1;
-    int *ids_s = (int *)(rows_s + TR_ROWS * pc);
-    float *t_s = (float *)(ids_s + TR_ROWS * pk);
+    const int tid = threadIdx.x, c = P.c, k = P.k;
+    float *spread = (float *)(stage_s + (G.ahead ? 2 : 1) * G.stage_bytes);
+    const int zb = (TR_ROWS * c * ES + 15) & ~15, kbytes = (TR_ROWS * k * 4 + 15) & ~15;
     const float c2 = LOG2E / P.temp, inv_t = 1.f / P.temp;
     // x / c = umulhi(x, ceil(2^32 / c)) for x < 2^14, c in 2 .. 128 (the error x (div c - 2^32) stays below 2^32)
-    const uint32_t div_c = (uint32_t)((0x100000000ull + P.c - 1) / P.c), div_k = (uint32_t)((0x100000000ull + P.k - 1) / P.k);
-    auto over_c = [&](int x) { return P.c == 1 ? (uint32_t)x : __umulhi((uint32_t)x, div_c); };
-    auto over_k = [&](int x) { return P.k == 1 ? (uint32_t)x : __umulhi((uint32_t)x, div_k); };
+    const uint32_t div_c = (uint32_t)((0x100000000ull + c - 1) / c);
+    auto over_c = [&](int x) { return c == 1 ? (uint32_t)x : __umulhi((uint32_t)x, div_c); };
     double total = 0;
     pdl_launch_dependents();
     pdl_wait();
-    for (int64_t r0 = (int64_t)blockIdx.x * TR_ROWS; r0 < P.rows; r0 += (int64_t)gridDim.x * TR_ROWS) {
+    // a turn's rows and entries into a stage: asynchronously where all of them are there in whole 16-byte units
+    auto fill = [&](int64_t r0, char *st) {
         const int nr = (int)(P.rows - r0 < TR_ROWS ? P.rows - r0 : TR_ROWS);
-        const int n = nr * P.c;
-        if (vec) {                                                     // rows are back to back: 16-byte loads
-            const uint4 *src = reinterpret_cast<const uint4 *>((const char *)P.z + ((r0 * P.c) << Elem<F32>::SHIFT));
-            for (int i = tid; i < n / E; i += TR_ROWS) {
-                float v[E];
-                unit_values<F32>(src[i], v);
-                uint32_t r = over_c(i * E), col = i * E - r * P.c;
-#pragma unroll
-                for (int j = 0; j < E; ++j) {
-                    rows_s[r * pc + col] = v[j];
-                    if (++col == (uint32_t)P.c) { col = 0; ++r; }
-                }
-            }
-            for (int i = n / E * E + tid; i < n; i += TR_ROWS) {
-                const uint32_t r = over_c(i);
-                rows_s[r * pc + i - r * P.c] = elem<F32>(P.z, r0 * P.c + i);
+        if (G.ahead && nr == TR_ROWS) {
+            const char *z = (const char *)P.z + r0 * c * ES, *id = (const char *)(P.idx + r0 * k), *tt = (const char *)(P.t + r0 * k);
+            for (int i = tid; i < TR_ROWS * c * ES / 16; i += TR_ROWS) copy_async16(st + i * 16, z + i * 16);
+            for (int i = tid; i < TR_ROWS * k * 4 / 16; i += TR_ROWS) {
+                copy_async16(st + zb + i * 16, id + i * 16);
+                copy_async16(st + zb + kbytes + i * 16, tt + i * 16);
             }
         } else {
-            for (int i = tid; i < n; i += TR_ROWS) {
-                const uint32_t r = over_c(i), col = i - r * P.c;
-                rows_s[r * pc + col] = elem<F32>(P.z, (r0 + r) * P.pz + col);
+            for (int i = tid; i < nr * c; i += TR_ROWS) {
+                const uint32_t r = over_c(i), col = i - r * c;
+                if constexpr (F32) ((float *)st)[i] = ((const float *)P.z)[(r0 + r) * P.pz + col];
+                else ((bf16 *)st)[i] = ((const bf16 *)P.z)[(r0 + r) * P.pz + col];
+            }
+            for (int i = tid; i < nr * k; i += TR_ROWS) {
+                ((int *)(st + zb))[i] = P.idx[r0 * k + i];
+                ((float *)(st + zb + kbytes))[i] = P.t[r0 * k + i];
             }
         }
-        for (int i = tid; i < nr * P.k; i += TR_ROWS) {
-            const uint32_t r = over_k(i), j = i - r * P.k;
-            ids_s[r * pk + j] = P.idx[r0 * P.k + i];
-            t_s[r * pk + j] = P.t[r0 * P.k + i];
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    const int64_t first = (int64_t)blockIdx.x * TR_ROWS, step = (int64_t)gridDim.x * TR_ROWS;
+    float w_n = 0.f, tl_n = 0.f, lin_n = 0.f;
+    auto scalars = [&](int64_t r) {
+        w_n = r < P.rows ? (P.w ? P.w[r] : P.w_all) : 0.f;
+        if (P.tlse) tl_n = r < P.rows ? P.tlse[r] : 0.f;
+        if (!(MODE & FWD)) lin_n = r < P.rows ? P.lse_in[r] : 0.f;
+    };
+    if (first < P.rows && G.ahead) fill(first, stage_s);
+    scalars(first + tid);
+    int s_at = 0;
+    for (int64_t r0 = first; r0 < P.rows; r0 += step) {
+        const int nr = (int)(P.rows - r0 < TR_ROWS ? P.rows - r0 : TR_ROWS);
+        char *st = stage_s + s_at * G.stage_bytes;
+        if (!G.ahead) fill(r0, st);
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncthreads();                                               // the stage is filled; the other one has been read
+        const float w = w_n, tl = tl_n, lin = lin_n;
+        if (G.ahead && r0 + step < P.rows) { s_at ^= 1; fill(r0 + step, stage_s + s_at * G.stage_bytes); }
+        scalars(r0 + step + tid);
+        float *zr = (G.direct ? (float *)st : spread) + tid * G.pitch;
+        if (!G.direct) {
+            const int n = nr * c;
+            for (int i = tid; i < (n + E - 1) / E; i += TR_ROWS) {
+                float v[E];
+                unit_values<F32>(reinterpret_cast<const uint4 *>(st)[i], v);
+                uint32_t r = over_c(i * E), col = i * E - r * c;
+#pragma unroll
+                for (int j = 0; j < E; ++j) {
+                    if (i * E + j < n) spread[r * G.pitch + col] = v[j];
+                    if (++col == (uint32_t)c) { col = 0; ++r; }
+                }
+            }
+            __syncthreads();
         }
-        const float w = tid < nr ? (P.w ? P.w[r0 + tid] : P.w_all) : 0.f;
-        const float tl = tid < nr && P.tlse ? P.tlse[r0 + tid] : 0.f;
-        const float lin = (MODE & FWD) || tid >= nr ? 0.f : P.lse_in[r0 + tid];
-        __syncthreads();
-        float *zr = rows_s + tid * pc;
-        const int *id = ids_s + tid * pk;
-        const float *tr = t_s + tid * pk;
-        // the teacher: log p_j = t_j / T - lt
+        const int *id_s = (const int *)(st + zb) + tid * k;
+        const float *t_s = (const float *)(st + zb + kbytes) + tid * k;
+        int id4[SHORT ? 4 : 1];
+        float t4[SHORT ? 4 : 1];
+        if constexpr (SHORT) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { id4[j] = j < k && tid < nr ? id_s[j] : -1; t4[j] = j < k && tid < nr ? t_s[j] : 0.f; }
+        }
+        // every entry of a listed class: f(class, t)
+        auto entries = [&](auto f) {
+            if constexpr (SHORT) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) if ((uint32_t)id4[j] < (uint32_t)c) f(id4[j], t4[j]);
+            } else {
+                for (int j = 0; j < k; ++j) { const int id = id_s[j]; if ((uint32_t)id < (uint32_t)c) f(id, t_s[j]); }
+            }
+        };
+        // the teacher: log p = t / T - lt
         float S = 0.f, lt = tl;
         if (w != 0.f) {
             if (!P.tlse) {
-                float mt = -INFINITY;
+                float mt = -INFINITY, s = 0.f;
                 bool nan = false;
-                for (int j = 0; j < P.k; ++j) {
-                    if ((uint32_t)id[j] >= (uint32_t)P.c) continue;
-                    nan |= tr[j] != tr[j];
-                    mt = fmaxf(mt, tr[j]);
-                }
+                entries([&](int, float t) { nan |= t != t; mt = fmaxf(mt, t); });
                 if (mt != -INFINITY || nan) {
-                    float s = 0.f;
-                    for (int j = 0; j < P.k; ++j) if ((uint32_t)id[j] < (uint32_t)P.c) s += ex2((tr[j] - mt) * c2);
+                    entries([&](int, float t) { s += ex2((t - mt) * c2); });
                     lt = mt * inv_t + logf(s);
                     S = s == s ? 1.f : NAN;
                 }
             } else {
-                for (int j = 0; j < P.k; ++j) if ((uint32_t)id[j] < (uint32_t)P.c) S += expf(fmaf(tr[j], inv_t, -lt));
+                entries([&](int, float t) { S += expf(fmaf(t, inv_t, -lt)); });
             }
         }
         float loss = 0.f, lse = 0.f;
@@ -987,7 +1032,7 @@ distill_thread_kernel(const DistillParams P, const int vec)
             float v[CP ? CP : 1];
             if constexpr (CP > 0) {
 #pragma unroll
-                for (int i = 0; i < CP; ++i) v[i] = i < P.c ? zr[i] : -INFINITY;
+                for (int i = 0; i < CP; ++i) v[i] = i < c ? zr[i] : -INFINITY;
             }
             float m, scale = 1.f, ls = 0.f;
             if constexpr (MODE & FWD) {
@@ -1000,24 +1045,23 @@ distill_thread_kernel(const DistillParams P, const int vec)
                     for (int i = 0; i < CP; ++i) { v[i] = ex2((v[i] - m) * c2); s += v[i]; }
                 } else {
 #pragma unroll 4
-                    for (int i = 0; i < P.c; ++i) m = fmaxf(m, zr[i]);
+                    for (int i = 0; i < c; ++i) m = fmaxf(m, zr[i]);
                 }
                 // the listed logits, before their exponentials take their place
-                float zl = 0.f;
-                for (int j = 0; j < P.k; ++j) {
-                    if ((uint32_t)id[j] >= (uint32_t)P.c) continue;
-                    const float lp = fmaf(tr[j], inv_t, -lt), p = expf(lp);
-                    if (p != 0.f) { loss += p * (lp - (zr[id[j]] - m) * inv_t); zl += p; }
-                }
+                float ps = 0.f;
+                entries([&](int id, float t) {
+                    const float lp = fmaf(t, inv_t, -lt), p = expf(lp);
+                    if (p != 0.f) { loss += p * (lp - (zr[id] - m) * inv_t); ps += p; }
+                });
                 if constexpr (CP == 0) {
 #pragma unroll 4
-                    for (int i = 0; i < P.c; ++i) { const float e = ex2((zr[i] - m) * c2); s += e; if (MODE & BWD) zr[i] = e; }
+                    for (int i = 0; i < c; ++i) { const float e = ex2((zr[i] - m) * c2); s += e; if (MODE & BWD) zr[i] = e; }
                 }
                 if (s == 0.f) s = NAN;
                 scale = 1.f / s;
                 ls = logf(s);
                 lse = m * inv_t + ls;
-                loss = (loss + zl * ls) * P.temp * P.temp;
+                loss = (loss + ps * ls) * P.temp * P.temp;
             } else {
                 m = lin;
                 if constexpr (CP > 0) {
@@ -1029,48 +1073,49 @@ distill_thread_kernel(const DistillParams P, const int vec)
             if constexpr (MODE & BWD) {
                 if constexpr (CP > 0) {
 #pragma unroll
-                    for (int i = 0; i < CP; ++i) if (i < P.c) zr[i] = gq * v[i];
+                    for (int i = 0; i < CP; ++i) if (i < c) zr[i] = gq * v[i];
                 } else {
 #pragma unroll 4
-                    for (int i = 0; i < P.c; ++i) zr[i] = gq * ((MODE & FWD) ? zr[i] : ex2(fmaf(zr[i], inv_t, -m) * LOG2E));
+                    for (int i = 0; i < c; ++i) zr[i] = gq * ((MODE & FWD) ? zr[i] : ex2(fmaf(zr[i], inv_t, -m) * LOG2E));
                 }
-                for (int j = 0; j < P.k; ++j)
-                    if ((uint32_t)id[j] < (uint32_t)P.c) zr[id[j]] -= gT * expf(fmaf(tr[j], inv_t, -lt));
+                entries([&](int id, float t) { zr[id] -= gT * expf(fmaf(t, inv_t, -lt)); });
             }
         } else if ((MODE & BWD) && tid < nr) {
-            for (int i = 0; i < P.c; ++i) zr[i] = 0.f;
+            for (int i = 0; i < c; ++i) zr[i] = 0.f;
         }
         if ((MODE & FWD) && tid < nr) {
             if (P.loss_rows) P.loss_rows[r0 + tid] = loss;
             if (P.lse_out) P.lse_out[r0 + tid] = lse;
             if (w != 0.f) total += (double)w * loss;
         }
-        __syncthreads();
         if constexpr (MODE & BWD) {
-            if (vec) {
-                uint4 *dst = reinterpret_cast<uint4 *>((char *)P.dz + ((r0 * P.c) << Elem<F32>::SHIFT));
+            __syncthreads();
+            const int n = nr * c;
+            if (G.vec) {
+                uint4 *dst = reinterpret_cast<uint4 *>((char *)P.dz + r0 * c * ES);
                 for (int i = tid; i < n / E; i += TR_ROWS) {
+                    if (G.direct) { dst[i] = reinterpret_cast<const uint4 *>(st)[i]; continue; }
                     float v[E];
-                    uint32_t r = over_c(i * E), col = i * E - r * P.c;
+                    uint32_t r = over_c(i * E), col = i * E - r * c;
 #pragma unroll
                     for (int j = 0; j < E; ++j) {
-                        v[j] = rows_s[r * pc + col];
-                        if (++col == (uint32_t)P.c) { col = 0; ++r; }
+                        v[j] = spread[r * G.pitch + col];
+                        if (++col == (uint32_t)c) { col = 0; ++r; }
                     }
                     dst[i] = unit_raw<F32>(v);
                 }
                 for (int i = n / E * E + tid; i < n; i += TR_ROWS) {
                     const uint32_t r = over_c(i);
-                    put<F32>(P.dz, r0 * P.c + i, rows_s[r * pc + i - r * P.c]);
+                    put<F32>(P.dz, r0 * c + i, (G.direct ? (float *)st : spread)[r * G.pitch + i - r * c]);
                 }
             } else {
                 for (int i = tid; i < n; i += TR_ROWS) {
-                    const uint32_t r = over_c(i), col = i - r * P.c;
-                    put<F32>(P.dz, (r0 + r) * P.pdz + col, rows_s[r * pc + col]);
+                    const uint32_t r = over_c(i), col = i - r * c;
+                    put<F32>(P.dz, (r0 + r) * P.pdz + col, (G.direct ? (float *)st : spread)[r * G.pitch + col]);
                 }
             }
-            __syncthreads();
         }
+        if (!G.ahead) __syncthreads();                                 // the stage and the spread rows are free again
     }
     if ((MODE & FWD) && P.part) {
 #pragma unroll
@@ -1128,24 +1173,30 @@ lamp_status_t launch_row_u(const DistillParams &P, int nu, int grid, cudaStream_
 }
 
 template <bool F32, int MODE, int CP>
-lamp_status_t launch_thread(const DistillParams &P, int grid, int vec, cudaStream_t st)
+lamp_status_t launch_thread(const DistillParams &P, int grid, bool vec, cudaStream_t st)
 {
-    constexpr int TR_ROWS = tr_rows(CP);
-    const int smem = TR_ROWS * ((P.c | 1) + 2 * (P.k | 1)) * 4;
+    constexpr int R = tr_rows(CP), ES = F32 ? 4 : 2;
+    ThreadPlan G = {};
+    G.vec = vec;
+    G.ahead = CP > 0 && vec && (((uintptr_t)P.idx | (uintptr_t)P.t) & 15) == 0;
+    G.direct = F32 && (P.c % 4 != 0);                                  // stride c: each bank is hit by c's power of two, at most 2
+    G.pitch = G.direct ? P.c : P.c | 1;
+    G.stage_bytes = ((R * P.c * ES + 15) & ~15) + 2 * ((R * P.k * 4 + 15) & ~15);
+    const int smem = (G.ahead ? 2 : 1) * G.stage_bytes + (G.direct ? 0 : R * G.pitch * 4);
+    const bool brief = P.k <= 4;
+    auto kernel = brief ? distill_thread_kernel<F32, MODE, CP, true> : distill_thread_kernel<F32, MODE, CP, false>;
     if (smem > 32 * 1024) {
-        static SmemAttrOnce attr;
-        const lamp_status_t s = attr.ensure(distill_thread_kernel<F32, MODE, CP>, TR_ROWS * ((CP ? 33 : TR_MAX_C + 1) + 2 * 33) * 4);
+        static SmemAttrOnce attr[2];
+        const lamp_status_t s = attr[brief].ensure(kernel, 226 * 1024);
         if (s != LAMP_OK) return s;
     }
-    return launch_pdl(true, distill_thread_kernel<F32, MODE, CP>, dim3(grid), dim3(TR_ROWS), (size_t)smem, st, P, vec);
+    return launch_pdl(true, kernel, dim3(grid), dim3(R), (size_t)smem, st, P, G);
 }
 template <bool F32, int MODE>
-lamp_status_t launch_thread_c(const DistillParams &P, int grid, int vec, cudaStream_t st)
+lamp_status_t launch_thread_c(const DistillParams &P, int grid, bool vec, cudaStream_t st)
 {
     if (P.c <= 4) return launch_thread<F32, MODE, 4>(P, grid, vec, st);
-    if (P.c <= 8) return launch_thread<F32, MODE, 8>(P, grid, vec, st);
     if (P.c <= 12) return launch_thread<F32, MODE, 12>(P, grid, vec, st);
-    if (P.c <= 16) return launch_thread<F32, MODE, 16>(P, grid, vec, st);
     if (P.c <= TR_REG_C) return launch_thread<F32, MODE, 32>(P, grid, vec, st);
     return launch_thread<F32, MODE, 0>(P, grid, vec, st);
 }
@@ -1180,11 +1231,11 @@ lamp_status_t run(DistillParams &P, bool f32, float *loss, void *ws, cudaStream_
     P.part = loss ? (double *)ws : nullptr;
     P.status = status_word_ptr();
     if (P.c <= TR_MAX_C && P.k <= TR_MAX_K) {
-        const int turn = tr_rows(P.c <= TR_REG_C), room = P.c <= TR_REG_C ? 8 : 3;
+        const int turn = tr_rows(P.c <= TR_REG_C), room = 27;
         const int64_t need = (P.rows + turn - 1) / turn;
         parts = (int)(need < (int64_t)room * sms ? need : (int64_t)room * sms);
         if (parts > MAX_PARTS) parts = MAX_PARTS;
-        const int vec = P.pz == P.c && ((uintptr_t)P.z & 15) == 0 && (!(MODE & BWD) || (P.pdz == P.c && ((uintptr_t)P.dz & 15) == 0));
+        const bool vec = P.pz == P.c && ((uintptr_t)P.z & 15) == 0 && (!(MODE & BWD) || (P.pdz == P.c && ((uintptr_t)P.dz & 15) == 0));
         s = f32 ? launch_thread_c<true, MODE>(P, parts, vec, st) : launch_thread_c<false, MODE>(P, parts, vec, st);
     } else if (P.k <= SHORT_K && P.c <= (f32 ? 4 : 8) * (32 * RW_MAX_UNITS - 1)) {
         const int units = (P.c + (f32 ? 3 : 7)) / (f32 ? 4 : 8) + 1, nu = units <= 64 ? 2 : RW_MAX_UNITS;
