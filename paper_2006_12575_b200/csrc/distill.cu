@@ -928,7 +928,7 @@ distill_thread_kernel(const DistillParams P, const ThreadPlan G)
     __shared__ double wl[TR_ROWS / 32];
     const int tid = threadIdx.x, c = P.c, k = P.k;
     float *spread = (float *)(stage_s + (G.ahead ? 2 : 1) * G.stage_bytes);
-    const int zb = (TR_ROWS * c * ES + 15) & ~15, kbytes = (TR_ROWS * k * 4 + 15) & ~15;
+    const int zb = G.ahead ? (TR_ROWS * c * ES + 15) & ~15 : 0, kbytes = (TR_ROWS * k * 4 + 15) & ~15;
     const float c2 = LOG2E / P.temp, inv_t = 1.f / P.temp;
     // x / c = umulhi(x, ceil(2^32 / c)) for x < 2^14, c in 2 .. 128 (the error x (div c - 2^32) stays below 2^32)
     const uint32_t div_c = (uint32_t)((0x100000000ull + c - 1) / c);
@@ -936,6 +936,16 @@ distill_thread_kernel(const DistillParams P, const ThreadPlan G)
     double total = 0;
     pdl_launch_dependents();
     pdl_wait();
+    auto spread_unit = [&](const uint4 &raw, int i0, int n) {          // elements i0 .. of the turn to the rows of odd pitch
+        float v[E];
+        unit_values<F32>(raw, v);
+        uint32_t r = over_c(i0), col = i0 - r * c;
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            if (i0 + j < n) spread[r * G.pitch + col] = v[j];
+            if (++col == (uint32_t)c) { col = 0; ++r; }
+        }
+    };
     // a turn's rows and entries into a stage: asynchronously where all of them are there in whole 16-byte units
     auto fill = [&](int64_t r0, char *st) {
         const int nr = (int)(P.rows - r0 < TR_ROWS ? P.rows - r0 : TR_ROWS);
@@ -947,10 +957,18 @@ distill_thread_kernel(const DistillParams P, const ThreadPlan G)
                 copy_async16(st + zb + kbytes + i * 16, tt + i * 16);
             }
         } else {
-            for (int i = tid; i < nr * c; i += TR_ROWS) {
-                const uint32_t r = over_c(i), col = i - r * c;
-                if constexpr (F32) ((float *)st)[i] = ((const float *)P.z)[(r0 + r) * P.pz + col];
-                else ((bf16 *)st)[i] = ((const bf16 *)P.z)[(r0 + r) * P.pz + col];
+            const int n = nr * c;
+            if (!G.ahead && G.vec) {                                   // straight to where the rows are worked on
+                const uint4 *src = reinterpret_cast<const uint4 *>((const char *)P.z + r0 * c * ES);
+                for (int i = tid; i < n / E; i += TR_ROWS) spread_unit(src[i], i * E, n);
+                for (int i = n / E * E + tid; i < n; i += TR_ROWS) spread[over_c(i) * G.pitch + i - over_c(i) * c] = elem<F32>(P.z, r0 * c + i);
+            } else {
+                for (int i = tid; i < n; i += TR_ROWS) {
+                    const uint32_t r = over_c(i), col = i - r * c;
+                    if (!G.ahead) spread[r * G.pitch + col] = elem<F32>(P.z, (r0 + r) * P.pz + col);
+                    else if constexpr (F32) ((float *)st)[i] = elem<F32>(P.z, (r0 + r) * P.pz + col);
+                    else ((bf16 *)st)[i] = ((const bf16 *)P.z)[(r0 + r) * P.pz + col];
+                }
             }
             for (int i = tid; i < nr * k; i += TR_ROWS) {
                 ((int *)(st + zb))[i] = P.idx[r0 * k + i];
@@ -979,53 +997,69 @@ distill_thread_kernel(const DistillParams P, const ThreadPlan G)
         if (G.ahead && r0 + step < P.rows) { s_at ^= 1; fill(r0 + step, stage_s + s_at * G.stage_bytes); }
         scalars(r0 + step + tid);
         float *zr = (G.direct ? (float *)st : spread) + tid * G.pitch;
-        if (!G.direct) {
-            const int n = nr * c;
-            for (int i = tid; i < (n + E - 1) / E; i += TR_ROWS) {
-                float v[E];
-                unit_values<F32>(reinterpret_cast<const uint4 *>(st)[i], v);
-                uint32_t r = over_c(i * E), col = i * E - r * c;
-#pragma unroll
-                for (int j = 0; j < E; ++j) {
-                    if (i * E + j < n) spread[r * G.pitch + col] = v[j];
-                    if (++col == (uint32_t)c) { col = 0; ++r; }
-                }
-            }
+        if (G.ahead && !G.direct) {
+            for (int i = tid; i < (nr * c + E - 1) / E; i += TR_ROWS) spread_unit(reinterpret_cast<const uint4 *>(st)[i], i * E, nr * c);
             __syncthreads();
         }
         const int *id_s = (const int *)(st + zb) + tid * k;
         const float *t_s = (const float *)(st + zb + kbytes) + tid * k;
+        // the teacher: S and, for every entry of a listed class, log p and p.  Short lists keep them in registers.
         int id4[SHORT ? 4 : 1];
-        float t4[SHORT ? 4 : 1];
+        float lp4[SHORT ? 4 : 1], p4[SHORT ? 4 : 1];
+        float S = 0.f, lt = tl;                                        // log p = t / T - lt
         if constexpr (SHORT) {
+            float mt = -INFINITY;
+            bool nan = false;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) { id4[j] = j < k && tid < nr ? id_s[j] : -1; t4[j] = j < k && tid < nr ? t_s[j] : 0.f; }
-        }
-        // every entry of a listed class: f(class, t)
-        auto entries = [&](auto f) {
-            if constexpr (SHORT) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) if ((uint32_t)id4[j] < (uint32_t)c) f(id4[j], t4[j]);
-            } else {
-                for (int j = 0; j < k; ++j) { const int id = id_s[j]; if ((uint32_t)id < (uint32_t)c) f(id, t_s[j]); }
+            for (int j = 0; j < 4; ++j) {
+                id4[j] = -1; lp4[j] = -INFINITY;
+                if (j < k && w != 0.f) {
+                    id4[j] = id_s[j];
+                    if ((uint32_t)id4[j] < (uint32_t)c) lp4[j] = t_s[j]; else id4[j] = -1;
+                    nan |= lp4[j] != lp4[j];
+                    mt = fmaxf(mt, lp4[j]);
+                }
             }
-        };
-        // the teacher: log p = t / T - lt
-        float S = 0.f, lt = tl;
-        if (w != 0.f) {
             if (!P.tlse) {
-                float mt = -INFINITY, s = 0.f;
-                bool nan = false;
-                entries([&](int, float t) { nan |= t != t; mt = fmaxf(mt, t); });
                 if (mt != -INFINITY || nan) {
-                    entries([&](int, float t) { s += ex2((t - mt) * c2); });
-                    lt = mt * inv_t + logf(s);
-                    S = s == s ? 1.f : NAN;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) { lp4[j] -= mt; p4[j] = ex2(lp4[j] * c2); S += p4[j]; }
+                    const float inv = 1.f / S, l = logf(S);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) { p4[j] *= inv; lp4[j] = fmaf(lp4[j], inv_t, -l); }
+                    S = S == S ? 1.f : NAN;
                 }
             } else {
-                entries([&](int, float t) { S += expf(fmaf(t, inv_t, -lt)); });
+#pragma unroll
+                for (int j = 0; j < 4; ++j) { lp4[j] = fmaf(lp4[j], inv_t, -lt); p4[j] = id4[j] >= 0 ? expf(lp4[j]) : 0.f; S += p4[j]; }
             }
+        } else if (w != 0.f) {
+            float mt = -INFINITY;
+            bool nan = false;
+            for (int j = 0; j < k; ++j) {
+                if ((uint32_t)id_s[j] >= (uint32_t)c) continue;
+                nan |= t_s[j] != t_s[j];
+                mt = fmaxf(mt, t_s[j]);
+            }
+            if (!P.tlse && (mt != -INFINITY || nan)) {
+                float s = 0.f;
+                for (int j = 0; j < k; ++j) if ((uint32_t)id_s[j] < (uint32_t)c) s += ex2((t_s[j] - mt) * c2);
+                lt = mt * inv_t + logf(s);
+                S = s == s ? 1.f : NAN;
+            }
+            if (P.tlse) for (int j = 0; j < k; ++j) if ((uint32_t)id_s[j] < (uint32_t)c) S += expf(fmaf(t_s[j], inv_t, -lt));
         }
+        auto entries = [&](auto f) {                                   // f(class, log p, p)
+            if constexpr (SHORT) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) if (id4[j] >= 0) f(id4[j], lp4[j], p4[j]);
+            } else {
+                for (int j = 0; j < k; ++j) {
+                    const int id = id_s[j];
+                    if ((uint32_t)id < (uint32_t)c) { const float lp = fmaf(t_s[j], inv_t, -lt); f(id, lp, expf(lp)); }
+                }
+            }
+        };
         float loss = 0.f, lse = 0.f;
         if (S != 0.f) {
             // CP > 0: the row in registers; otherwise it is walked in shared memory, where the exponentials replace the logits
@@ -1049,8 +1083,7 @@ distill_thread_kernel(const DistillParams P, const ThreadPlan G)
                 }
                 // the listed logits, before their exponentials take their place
                 float ps = 0.f;
-                entries([&](int id, float t) {
-                    const float lp = fmaf(t, inv_t, -lt), p = expf(lp);
+                entries([&](int id, float lp, float p) {
                     if (p != 0.f) { loss += p * (lp - (zr[id] - m) * inv_t); ps += p; }
                 });
                 if constexpr (CP == 0) {
@@ -1078,7 +1111,7 @@ distill_thread_kernel(const DistillParams P, const ThreadPlan G)
 #pragma unroll 4
                     for (int i = 0; i < c; ++i) zr[i] = gq * ((MODE & FWD) ? zr[i] : ex2(fmaf(zr[i], inv_t, -m) * LOG2E));
                 }
-                entries([&](int id, float t) { zr[id] -= gT * expf(fmaf(t, inv_t, -lt)); });
+                entries([&](int id, float, float p) { zr[id] -= gT * p; });
             }
         } else if ((MODE & BWD) && tid < nr) {
             for (int i = 0; i < c; ++i) zr[i] = 0.f;
@@ -1179,9 +1212,9 @@ lamp_status_t launch_thread(const DistillParams &P, int grid, bool vec, cudaStre
     ThreadPlan G = {};
     G.vec = vec;
     G.ahead = CP > 0 && vec && (((uintptr_t)P.idx | (uintptr_t)P.t) & 15) == 0;
-    G.direct = F32 && (P.c % 4 != 0);                                  // stride c: each bank is hit by c's power of two, at most 2
+    G.direct = G.ahead && F32 && P.c % 4 != 0;                               // stride c: each bank is hit by c's power of two, at most 2
     G.pitch = G.direct ? P.c : P.c | 1;
-    G.stage_bytes = ((R * P.c * ES + 15) & ~15) + 2 * ((R * P.k * 4 + 15) & ~15);
+    G.stage_bytes = (G.ahead ? (R * P.c * ES + 15) & ~15 : 0) + 2 * ((R * P.k * 4 + 15) & ~15);
     const int smem = (G.ahead ? 2 : 1) * G.stage_bytes + (G.direct ? 0 : R * G.pitch * 4);
     const bool brief = P.k <= 4;
     auto kernel = brief ? distill_thread_kernel<F32, MODE, CP, true> : distill_thread_kernel<F32, MODE, CP, false>;
@@ -1197,6 +1230,7 @@ lamp_status_t launch_thread_c(const DistillParams &P, int grid, bool vec, cudaSt
 {
     if (P.c <= 4) return launch_thread<F32, MODE, 4>(P, grid, vec, st);
     if (P.c <= 12) return launch_thread<F32, MODE, 12>(P, grid, vec, st);
+    if (P.c <= 20) return launch_thread<F32, MODE, 20>(P, grid, vec, st);
     if (P.c <= TR_REG_C) return launch_thread<F32, MODE, 32>(P, grid, vec, st);
     return launch_thread<F32, MODE, 0>(P, grid, vec, st);
 }
