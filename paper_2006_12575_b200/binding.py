@@ -152,8 +152,12 @@ def _check(st, what):
         raise LampError(st, what)
 
 
+# handle of the current stream of a device, without the Stream object around it (3 us a call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+
+
 def _stream():
-    return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    return _raw_stream(torch.cuda.current_device())
 
 
 def _ptr(t):
@@ -417,60 +421,74 @@ def _byref(s):
 
 def fp8_operand(q, scale, rows=None, k=None, tile_scale=False) -> Fp8Operand:
     """Operand [rows][k] of lamp_gemm_fp8: q uint8 or float8_e4m3fn [rows, pitch], scale fp32 [ceil(k/128), pitch]."""
-    if q.dtype not in _FP8_TYPES or q.dim() != 2 or scale.dtype is not torch.float32 or scale.dim() != 2 or not q.is_cuda:
-        raise ValueError("fp8_operand: q is a CUDA uint8 or float8_e4m3fn matrix, scale an fp32 matrix")
-    if scale.get_device() != q.get_device():
-        raise ValueError("fp8_operand: q and scale are on different devices")
-    rows = q.shape[0] if rows is None else rows
-    k = q.shape[1] if k is None else k
-    blocks = -(-k // 128)
-    if rows > q.shape[0] or k > q.shape[1] or q.stride(1) != 1 or scale.stride(1) != 1 or scale.shape[0] < blocks or \
-            scale.shape[1] < (-(-rows // 128) if tile_scale else rows):
+    dev = q.get_device()
+    if q.dtype not in _FP8_TYPES or scale.dtype is not torch.float32 or dev < 0 or scale.get_device() != dev:
+        raise ValueError("fp8_operand: q is a CUDA uint8 or float8_e4m3fn matrix, scale an fp32 matrix on the same device")
+    (qr, qc), (sr, sc), (qp, q1), (sp, s1) = q.shape, scale.shape, q.stride(), scale.stride()
+    if rows is None:
+        rows = qr
+    if k is None:
+        k = qc
+    if rows > qr or k > qc or q1 != 1 or s1 != 1 or sr * 128 < k or sc < ((rows + 127) // 128 if tile_scale else rows):
         raise ValueError(f"fp8_operand: [{rows}, {k}] does not fit q {tuple(q.shape)} and scale {tuple(scale.shape)}")
     # the stride of an axis of one element says nothing: the pitch only has to cover the row
-    qp = q.stride(0) if q.shape[0] > 1 else -(-max(q.stride(0), q.shape[1]) // 16) * 16
-    sp = scale.stride(0) if scale.shape[0] > 1 else max(scale.stride(0), scale.shape[1])
+    if qr <= 1:
+        qp = (max(qp, qc) + 15) // 16 * 16
+    if sr <= 1:
+        sp = max(sp, sc)
     o = Fp8Operand(q.data_ptr(), qp, scale.data_ptr(), sp, rows, k, 1 if tile_scale else 0)
-    o.keep = (q, scale)
+    o.keep, o.dev = (q, scale), dev
     return o
 
 
 def _operand(o, dev, what):
-    keep = getattr(o, "keep", None)
-    if keep is not None and keep[0].get_device() != dev:
-        raise ValueError(f"{what}: on {keep[0].device}, the current device is cuda:{dev}")
+    if getattr(o, "dev", dev) != dev:
+        raise ValueError(f"{what}: on cuda:{o.dev}, the current device is cuda:{dev}")
     return C.byref(o)
 
 
 def lamp_fp8_quantize(x, out: Fp8Operand, transpose=False):
     dev = torch.cuda.current_device()
-    _check(lib().lamp_fp8_quantize(_byref(_view(x, dev, "x")), 1 if transpose else 0, _operand(out, dev, "out"), _stream()), "lamp_fp8_quantize")
+    _check(lib().lamp_fp8_quantize(_byref(_view(x, dev, "x")), 1 if transpose else 0, _operand(out, dev, "out"), _raw_stream(dev)), "lamp_fp8_quantize")
 
 
 def lamp_gemm_fp8(a: Fp8Operand, b: Fp8Operand, y, bias=None):
     dev = torch.cuda.current_device()
     _check(lib().lamp_gemm_fp8(_operand(a, dev, "a"), _operand(b, dev, "b"), _vec(bias, b.rows, "bias", dev), _byref(_view(y, dev, "y")),
-                               _stream()), "lamp_gemm_fp8")
+                               _raw_stream(dev)), "lamp_gemm_fp8")
 
 
 def block_norm(rms=False, eps=1e-5, post_w=None, post_b=None, pre_w=None, pre_b=None, gate=None, gate_logits=None,
                res_scale=None) -> BlockNorm:
     """Parameters of lamp_block_norm_fwd / _bwd: fp32 vectors [c] (gate: [n, c]), gate_logits a tensor like y."""
+    keep = (post_w, post_b, pre_w, pre_b, res_scale)
+    first = next((v for v in keep if v is not None), None)
     p = BlockNorm()
     p.rms, p.eps = 1 if rms else 0, eps
-    p.keep = (("post_w", post_w), ("post_b", post_b), ("pre_w", pre_w), ("pre_b", pre_b), ("res_scale", res_scale))
-    p.keep_gate, p.keep_logits = gate, gate_logits
+    p.c = p.dev = None                                              # of the vectors, for the calls to check
+    if first is not None:
+        p.c, p.dev = first.numel(), first.get_device()
+        ptr = [_vec(v, p.c, name, p.dev) for v, name in zip(keep, ("post_w", "post_b", "pre_w", "pre_b", "res_scale"))]
+        p.post_w, p.post_b, p.pre_w, p.pre_b, p.res_scale = ptr
+    if gate is not None:
+        p.gate = _vec(gate, gate.numel(), "gate", gate.get_device())
+        p.gate_numel, p.gate_dev = gate.numel(), gate.get_device()
+    if gate_logits is not None:
+        p.view = _view(gate_logits, gate_logits.get_device() if torch.is_tensor(gate_logits) else None, "gate_logits")
+        p.gate_logits = C.pointer(p.view)
+    p.keep = (keep, gate, gate_logits)
     return p
 
 
 def _norm_params(p, shape, dev):
-    """Fills in the pointers, checked against the shape of the call's tensors."""
-    for name, v in p.keep:
-        setattr(p, name, _vec(v, shape.c, name, dev))
-    p.gate = _vec(p.keep_gate, shape.n * shape.c, "gate", dev)
-    if p.keep_logits is not None:
-        p.keep_view = _view(p.keep_logits, dev, "gate_logits")
-        p.gate_logits = C.pointer(p.keep_view)
+    """The parameters, checked against the shape of the call's tensors."""
+    if p.c is not None and (p.c != shape.c or p.dev != dev):
+        raise ValueError(f"block_norm: vectors of {p.c} on cuda:{p.dev}, the tensors have {shape.c} channels on cuda:{dev}")
+    if p.gate and (p.gate_numel != shape.n * shape.c or p.gate_dev != dev):
+        raise ValueError(f"block_norm: gate of {p.gate_numel} on cuda:{p.gate_dev}, want [{shape.n}, {shape.c}] on cuda:{dev}")
+    logits = p.keep[2]
+    if torch.is_tensor(logits) and logits.get_device() != dev:
+        raise ValueError(f"block_norm: gate_logits on {logits.device}, the current device is cuda:{dev}")
     return C.byref(p)
 
 
@@ -478,7 +496,7 @@ def lamp_block_norm_fwd(p: BlockNorm, y, x, out, h=None, h_fp8=None):
     dev = torch.cuda.current_device()
     vx = _view(x, dev, "x")
     _check(lib().lamp_block_norm_fwd(_norm_params(p, vx, dev), _byref(_view(y, dev, "y")), C.byref(vx), _byref(_view(out, dev, "out")),
-                                     _byref(_view(h, dev, "h")), None if h_fp8 is None else _operand(h_fp8, dev, "h_fp8"), _stream()),
+                                     _byref(_view(h, dev, "h")), None if h_fp8 is None else _operand(h_fp8, dev, "h_fp8"), _raw_stream(dev)),
            "lamp_block_norm_fwd")
 
 
@@ -500,7 +518,7 @@ def lamp_block_norm_bwd(p: BlockNorm, y, t, dout, dh, dx, dy, ws=None, dgate_log
     w, nbytes = _ws(ws)
     _check(lib().lamp_block_norm_bwd(_norm_params(p, vt, dev), _byref(_view(y, dev, "y")), C.byref(vt), _byref(_view(dout, dev, "dout")),
                                      _byref(_view(dh, dev, "dh")), _byref(_view(dx, dev, "dx")), _byref(_view(dy, dev, "dy")),
-                                     _byref(_view(dgate_logits, dev, "dgate_logits")), C.byref(g), w, nbytes, _stream()),
+                                     _byref(_view(dgate_logits, dev, "dgate_logits")), C.byref(g), w, nbytes, _raw_stream(dev)),
            "lamp_block_norm_bwd")
 
 
@@ -539,7 +557,7 @@ def lamp_distill_topk_fwd(z, teacher: TeacherTopk, row_weight=None, loss_rows=No
     t, rows = _teacher(teacher, vz, dev)
     w, nbytes = _scratch(ws, dev)
     _check(lib().lamp_distill_topk_fwd(C.byref(vz), t, _vec(row_weight, rows, "row_weight", dev), _vec(loss_rows, rows, "loss_rows", dev),
-                                       _vec(lse, rows, "lse", dev), _vec(loss, 1, "loss", dev), w, nbytes, _stream()), "lamp_distill_topk_fwd")
+                                       _vec(lse, rows, "lse", dev), _vec(loss, 1, "loss", dev), w, nbytes, _raw_stream(dev)), "lamp_distill_topk_fwd")
 
 
 def lamp_distill_topk_bwd(z, teacher: TeacherTopk, row_grad, lse, dz):
@@ -547,7 +565,7 @@ def lamp_distill_topk_bwd(z, teacher: TeacherTopk, row_grad, lse, dz):
     vz = _view(z, dev, "z")
     t, rows = _teacher(teacher, vz, dev)
     _check(lib().lamp_distill_topk_bwd(C.byref(vz), t, _vec(row_grad, rows, "row_grad", dev), _vec(lse, rows, "lse", dev),
-                                       _byref(_view(dz, dev, "dz")), _stream()), "lamp_distill_topk_bwd")
+                                       _byref(_view(dz, dev, "dz")), _raw_stream(dev)), "lamp_distill_topk_bwd")
 
 
 def lamp_distill_topk_fwd_bwd(z, teacher: TeacherTopk, row_weight, loss_rows, loss, dz, ws=None):
@@ -556,7 +574,7 @@ def lamp_distill_topk_fwd_bwd(z, teacher: TeacherTopk, row_weight, loss_rows, lo
     t, rows = _teacher(teacher, vz, dev)
     w, nbytes = _scratch(ws, dev)
     _check(lib().lamp_distill_topk_fwd_bwd(C.byref(vz), t, _vec(row_weight, rows, "row_weight", dev), _vec(loss_rows, rows, "loss_rows", dev),
-                                           _vec(loss, 1, "loss", dev), _byref(_view(dz, dev, "dz")), w, nbytes, _stream()),
+                                           _vec(loss, 1, "loss", dev), _byref(_view(dz, dev, "dz")), w, nbytes, _raw_stream(dev)),
            "lamp_distill_topk_fwd_bwd")
 
 

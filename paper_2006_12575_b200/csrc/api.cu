@@ -80,10 +80,12 @@ void *tensor_map_encoder()
 
 int sm_count()
 {
+    static int known[64];                       // a constant of the device; races write the same value
     int dev = 0, sms = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
-        sms <= 0)
-        sms = 148;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 148;
+    if (dev >= 0 && dev < 64 && (sms = __atomic_load_n(&known[dev], __ATOMIC_RELAXED)) > 0) return sms;
+    if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms <= 0) return 148;
+    if (dev >= 0 && dev < 64) __atomic_store_n(&known[dev], sms, __ATOMIC_RELAXED);
     return sms;
 }
 
