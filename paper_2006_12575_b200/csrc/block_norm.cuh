@@ -6,6 +6,7 @@
 // sums exchanged through shared memory.
 #pragma once
 #include "common.cuh"
+#include "umma_ptx.cuh"
 
 namespace lamp {
 namespace bn {
@@ -50,12 +51,52 @@ template <bool F32> __device__ __forceinline__ void store8(void *base, int64_t o
     }
 }
 
+// the same as four packed pairs
+template <bool F32> __device__ __forceinline__ void to_pairs(const Raw<F32> &r, ptx::f32x2 (&f)[4])
+{
+    if constexpr (F32) {
+        f[0] = ptx::pack2(r.v[0].x, r.v[0].y); f[1] = ptx::pack2(r.v[0].z, r.v[0].w);
+        f[2] = ptx::pack2(r.v[1].x, r.v[1].y); f[3] = ptx::pack2(r.v[1].z, r.v[1].w);
+    } else {
+        const uint32_t w[4] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = ptx::pack2(w[i] << 16, w[i] & 0xFFFF0000u);
+    }
+}
+template <bool F32> __device__ __forceinline__ void store_pairs(void *base, int64_t off, const ptx::f32x2 (&f)[4])
+{
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) ptx::unpack2(f[i], v[2 * i], v[2 * i + 1]);
+    store8<F32>(base, off, v);
+}
+__device__ __forceinline__ float both(ptx::f32x2 v)
+{
+    float a, b;
+    ptx::unpack2(v, a, b);
+    return a + b;
+}
+// sigmoid: 2^x and the reciprocal are each within two units of the last place
+__device__ __forceinline__ float sigmoid(float x)
+{
+    float e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x * -1.4426950408889634f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+    return r;
+}
+
 // Per-channel parameters sit in shared memory as [array][half][unit] float4, so that neighbouring threads read
 // neighbouring 16-byte words.
 __device__ __forceinline__ void load_par(const float4 *par, int array, int units, int unit, float (&f)[8])
 {
     const float4 a = par[(array * 2) * units + unit], b = par[(array * 2 + 1) * units + unit];
     f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+}
+__device__ __forceinline__ void load_par(const float4 *par, int array, int units, int unit, ptx::f32x2 (&f)[4])
+{
+    const ulonglong2 a = *reinterpret_cast<const ulonglong2 *>(par + (array * 2) * units + unit);
+    const ulonglong2 b = *reinterpret_cast<const ulonglong2 *>(par + (array * 2 + 1) * units + unit);
+    f[0] = a.x; f[1] = a.y; f[2] = b.x; f[3] = b.y;
 }
 __device__ __forceinline__ void store_par(float *par, int array, int units, int ch, float v)
 {

@@ -27,16 +27,20 @@ struct BwdParams {
     float *part;                     // [samples * parts][4][c] or NULL
 };
 
-template <bool SF, bool BF, int TPR, int U, int MAXT>
-__global__ void __launch_bounds__(MAXT)
+// The running sums of a row group sit in shared memory, [sum][half][slot] float4 with slot = group * units + unit: 64 or
+// more accumulators per thread would leave 8 warps per SM (measured on 81,840 x 320, fp32 stream, gate per element: 265 us;
+// in shared memory, with packed fp32 arithmetic: MEASURED).
+template <bool SF, bool BF, int TPR, int U, int MAXT, int MINB, bool LOGITS>
+__global__ void __launch_bounds__(MAXT, MINB)
 block_norm_bwd_kernel(const BwdParams P)
 {
+    using ptx::f32x2; using ptx::fma2; using ptx::add2; using ptx::mul2; using ptx::twice; using ptx::pack2; using ptx::unpack2;
     extern __shared__ __align__(16) float par[];
     __shared__ float red[2][32];
     const int threads = TPR ? TPR : blockDim.x;
     const int groups = TPR ? blockDim.x / TPR : 1, group = TPR ? threadIdx.x / TPR : 0, tt = TPR ? threadIdx.x % TPR : threadIdx.x;
     const int units = P.c / 8;
-    const bool post = P.y != nullptr, pre = P.dh != nullptr;
+    const bool post = P.y != nullptr, pre = P.dh != nullptr, want = P.part != nullptr;
     const int64_t sample = blockIdx.x / P.parts, part = blockIdx.x - sample * P.parts;
     const int64_t base = sample * P.rows;
     pdl_launch_dependents();
@@ -44,25 +48,31 @@ block_norm_bwd_kernel(const BwdParams P)
     for (int ch = threadIdx.x; ch < P.c; ch += blockDim.x) {
         const float rg = (P.res ? P.res[ch] : 1.f) * (P.gate ? P.gate[sample * P.c + ch] : 1.f);
         store_par(par, 0, units, ch, rg * (P.post_w ? P.post_w[ch] : 1.f));
-        store_par(par, 1, units, ch, P.post_b ? rg * P.post_b[ch] : 0.f);
-        store_par(par, 2, units, ch, P.pre_w ? P.pre_w[ch] : 1.f);
+        store_par(par, 1, units, ch, P.pre_w ? P.pre_w[ch] : 1.f);
+        if (LOGITS) store_par(par, 2, units, ch, P.post_b ? rg * P.post_b[ch] : 0.f);
     }
-    __syncthreads();
     const float4 *par4 = reinterpret_cast<const float4 *>(par);
+    float4 *sums = reinterpret_cast<float4 *>(par) + (LOGITS ? 6 : 4) * units;
+    const int slots = groups * units;
+    if (want)
+        for (int i = threadIdx.x; i < 8 * slots; i += blockDim.x) sums[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    __syncthreads();
+    // sums k and k + 1 of a unit: a += f1 f2, b += f1
+    auto gather = [&](int k, int unit, const f32x2 (&f1)[4], const f32x2 (&f2)[4]) {
+        ulonglong2 *p = reinterpret_cast<ulonglong2 *>(sums + k * 2 * slots + group * units + unit);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            ulonglong2 a = p[h * slots], b = p[(2 + h) * slots];
+            a.x = fma2(f1[2 * h], f2[2 * h], a.x); a.y = fma2(f1[2 * h + 1], f2[2 * h + 1], a.y);
+            b.x = add2(b.x, f1[2 * h]); b.y = add2(b.y, f1[2 * h + 1]);
+            p[h * slots] = a; p[(2 + h) * slots] = b;
+        }
+    };
     const float inv_c = 1.f / (float)P.c;
     int turn = 0;
-
-    float acc[U][4][8];
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) acc[u][k][j] = 0.f;
-
     const int64_t step = (int64_t)P.parts * groups;
     for (int64_t r0 = part * groups; r0 < P.rows; r0 += step) {
-        const int64_t row = r0 + group;
+        const int64_t row = r0 + group, r = base + row;
         const bool active = row < P.rows;
         Raw<SF> rt[U], rdo[U];
         Raw<BF> ry[U], rdh[U], rl[U];
@@ -70,157 +80,135 @@ block_norm_bwd_kernel(const BwdParams P)
         for (int u = 0; u < U; ++u) {
             const int ch = (u * threads + tt) * 8;
             const bool in = active && ch < P.c;
-            const int64_t r = base + row;
             rt[u] = in && pre ? load_raw<SF>(P.t, r * P.pt + ch) : zero_raw<SF>();
-            rdh[u] = in && pre ? load_raw<BF>(P.dh, r * P.pdh + ch) : zero_raw<BF>();
             ry[u] = in && post ? load_raw<BF>(P.y, r * P.py + ch) : zero_raw<BF>();
+            rdh[u] = in && pre ? load_raw<BF>(P.dh, r * P.pdh + ch) : zero_raw<BF>();
             rdo[u] = in && P.dout ? load_raw<SF>(P.dout, r * P.pdo + ch) : zero_raw<SF>();
-            rl[u] = in && P.logits ? load_raw<BF>(P.logits, r * P.pl + ch) : zero_raw<BF>();
+            if (LOGITS) rl[u] = in ? load_raw<BF>(P.logits, r * P.pl + ch) : zero_raw<BF>();
         }
-        float th[U][8], yh[U][8], dt[U][8];
-        float st = 0.f, sy = 0.f;
+        f32x2 th[U][4], yh[U][4], dt[U][4];
+        float mt = 0.f, my = 0.f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) { to_pairs<SF>(rt[u], th[u]); to_pairs<BF>(ry[u], yh[u]); }
+        if (!P.rms) {
+            f32x2 st = 0, sy = 0;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) { st = add2(st, th[u][j]); sy = add2(sy, yh[u][j]); }
+            mt = both(st); my = both(sy);
+            row_sum2<TPR>(mt, my, red, turn);
+            mt *= inv_c; my *= inv_c;
+        }
+        f32x2 qt2 = 0, qy2 = 0;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            to_float<SF>(rt[u], th[u]);
-            to_float<BF>(ry[u], yh[u]);
+            if ((u * threads + tt) * 8 >= P.c) continue;               // stays zero
 #pragma unroll
-            for (int j = 0; j < 8; ++j) { st += th[u][j]; sy += yh[u][j]; }
-        }
-        if (!P.rms) row_sum2<TPR>(st, sy, red, turn); else st = sy = 0.f;
-        const float mt = st * inv_c, my = sy * inv_c;
-        float qt = 0.f, qy = 0.f;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const bool in = (u * threads + tt) * 8 < P.c;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                th[u][j] = in ? th[u][j] - mt : 0.f;
-                yh[u][j] = in ? yh[u][j] - my : 0.f;
-                qt = fmaf(th[u][j], th[u][j], qt);
-                qy = fmaf(yh[u][j], yh[u][j], qy);
+            for (int j = 0; j < 4; ++j) {
+                th[u][j] = add2(th[u][j], twice(-mt));
+                yh[u][j] = add2(yh[u][j], twice(-my));
+                qt2 = fma2(th[u][j], th[u][j], qt2);
+                qy2 = fma2(yh[u][j], yh[u][j], qy2);
             }
         }
+        float qt = both(qt2), qy = both(qy2);
         row_sum2<TPR>(qt, qy, red, turn);
-        // a row past the end takes part in the sums with zeros only, whatever eps is
+        // a row past the end takes part with zeros only, whatever eps is
         const float rst = active ? 1.f / sqrtf(qt * inv_c + P.eps) : 0.f, rsy = active ? 1.f / sqrtf(qy * inv_c + P.eps) : 0.f;
         if (pre) {
-            float s1 = 0.f, s2 = 0.f;
+            f32x2 s1 = 0, s2 = 0;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int unit = u * threads + tt;
-                float w[8], d[8];
-                to_float<BF>(rdh[u], d);
-                if (unit < units) load_par(par4, 2, units, unit, w);
-                else {
+                f32x2 w[4] = {0, 0, 0, 0}, d[4];
+                to_pairs<BF>(rdh[u], d);
+                if (unit < units) load_par(par4, 1, units, unit, w);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) w[j] = 0.f;
+                for (int j = 0; j < 4; ++j) {
+                    th[u][j] = mul2(th[u][j], twice(rst));
+                    dt[u][j] = mul2(d[j], w[j]);
+                    s1 = add2(s1, dt[u][j]);
+                    s2 = fma2(dt[u][j], th[u][j], s2);
                 }
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    th[u][j] *= rst;
-                    acc[u][2][j] = fmaf(d[j], th[u][j], acc[u][2][j]);
-                    acc[u][3][j] += d[j];
-                    dt[u][j] = d[j] * w[j];
-                    s1 += dt[u][j];
-                    s2 = fmaf(dt[u][j], th[u][j], s2);
-                }
+                if (want && active && unit < units) gather(2, unit, d, th[u]);
             }
-            row_sum2<TPR>(s1, s2, red, turn);
-            const float m1 = P.rms ? 0.f : s1 * inv_c, m2 = s2 * inv_c;
+            float m1 = both(s1), m2 = both(s2);
+            row_sum2<TPR>(m1, m2, red, turn);
+            m1 = P.rms ? 0.f : m1 * inv_c; m2 *= inv_c;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                float d[8];
-                to_float<SF>(rdo[u], d);
+                f32x2 d[4];
+                to_pairs<SF>(rdo[u], d);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) dt[u][j] = fmaf(rst, dt[u][j] - m1 - th[u][j] * m2, d[j]);
+                for (int j = 0; j < 4; ++j) dt[u][j] = fma2(twice(rst), fma2(th[u][j], twice(-m2), add2(dt[u][j], twice(-m1))), d[j]);
             }
         } else {
 #pragma unroll
-            for (int u = 0; u < U; ++u) to_float<SF>(rdo[u], dt[u]);
+            for (int u = 0; u < U; ++u) to_pairs<SF>(rdo[u], dt[u]);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int unit = u * threads + tt;
-            if (active && unit < units) store8<SF>(P.dx, (base + row) * P.pdx + unit * 8, dt[u]);
+            if (active && unit < units) store_pairs<SF>(P.dx, r * P.pdx + unit * 8, dt[u]);
         }
         if (post) {
-            float s1 = 0.f, s2 = 0.f;
-            float b[U][8];
+            f32x2 s1 = 0, s2 = 0;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int unit = u * threads + tt;
                 const bool in = active && unit < units;
-                float w[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) w[j] = 0.f;
+                f32x2 w[4] = {0, 0, 0, 0};
                 if (in) load_par(par4, 0, units, unit, w);
-                float g[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) { g[j] = 1.f; yh[u][j] *= rsy; }
-                if (P.logits) {
-                    float lg[8], wb[8];
-                    to_float<BF>(rl[u], lg);
+                for (int j = 0; j < 4; ++j) yh[u][j] = mul2(yh[u][j], twice(rsy));
+                if (LOGITS) {
+                    f32x2 g[4], wb[4] = {0, 0, 0, 0};
+                    to_pairs<BF>(rl[u], g);
+                    if (in) load_par(par4, 2, units, unit, wb);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) g[j] = 1.f / (1.f + __expf(-lg[j]));
-                    if (in) {
-                        load_par(par4, 1, units, unit, wb);
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) lg[j] = dt[u][j] * fmaf(yh[u][j], w[j], wb[j]) * (g[j] * (1.f - g[j]));
-                        store8<BF>(P.dl, (base + row) * P.pdl + unit * 8, lg);
+                    for (int j = 0; j < 4; ++j) {
+                        float a, b;
+                        unpack2(g[j], a, b);
+                        g[j] = pack2(__float_as_uint(sigmoid(a)), __float_as_uint(sigmoid(b)));
+                        // dlogit = dt r N(y) g (1 - g)
+                        wb[j] = mul2(mul2(dt[u][j], fma2(yh[u][j], w[j], wb[j])), mul2(g[j], fma2(g[j], twice(-1.f), twice(1.f))));
+                        dt[u][j] = mul2(dt[u][j], g[j]);
                     }
+                    if (in) store_pairs<BF>(P.dl, r * P.pdl + unit * 8, wb);
                 }
+                if (want && in) gather(0, unit, dt[u], yh[u]);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float d = in ? dt[u][j] * g[j] : 0.f;
-                    acc[u][0][j] = fmaf(d, yh[u][j], acc[u][0][j]);
-                    acc[u][1][j] += d;
-                    b[u][j] = d * w[j];
-                    s1 += b[u][j];
-                    s2 = fmaf(b[u][j], yh[u][j], s2);
+                for (int j = 0; j < 4; ++j) {
+                    dt[u][j] = mul2(dt[u][j], w[j]);
+                    s1 = add2(s1, dt[u][j]);
+                    s2 = fma2(dt[u][j], yh[u][j], s2);
                 }
             }
-            row_sum2<TPR>(s1, s2, red, turn);
-            const float m1 = P.rms ? 0.f : s1 * inv_c, m2 = s2 * inv_c;
+            float m1 = both(s1), m2 = both(s2);
+            row_sum2<TPR>(m1, m2, red, turn);
+            m1 = P.rms ? 0.f : m1 * inv_c; m2 *= inv_c;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int unit = u * threads + tt;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) b[u][j] = rsy * (b[u][j] - m1 - yh[u][j] * m2);
-                if (active && unit < units) store8<BF>(P.dy, (base + row) * P.pdy + unit * 8, b[u]);
+                for (int j = 0; j < 4; ++j) dt[u][j] = mul2(twice(rsy), fma2(yh[u][j], twice(-m2), add2(dt[u][j], twice(-m1))));
+                if (active && unit < units) store_pairs<BF>(P.dy, r * P.pdy + unit * 8, dt[u]);
             }
         }
     }
-    if (!P.part) return;
-    float *dst = P.part + (int64_t)blockIdx.x * 4 * P.c;
-    if (TPR == 0) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int unit = u * threads + tt;
-            if (unit < units)
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) dst[k * P.c + unit * 8 + j] = acc[u][k][j];
+    if (!want) return;
+    __syncthreads();
+    // the groups' sums, added in group order
+    float4 *dst = reinterpret_cast<float4 *>(P.part + (int64_t)blockIdx.x * 4 * P.c);
+    for (int i = threadIdx.x; i < 8 * units; i += blockDim.x) {
+        const int kh = i / units, unit = i - kh * units;
+        float4 s = sums[kh * slots + unit];
+        for (int g = 1; g < groups; ++g) {
+            const float4 v = sums[kh * slots + g * units + unit];
+            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
         }
-    } else {
-        // rows of the CTA's groups, one product at a time: [group][channel] in shared memory, added in group order
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            __syncthreads();
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int unit = u * threads + tt;
-                if (unit < units)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) par[group * P.c + unit * 8 + j] = acc[u][k][j];
-            }
-            __syncthreads();
-            for (int ch = threadIdx.x; ch < P.c; ch += blockDim.x) {
-                float s = 0.f;
-                for (int g = 0; g < groups; ++g) s += par[g * P.c + ch];
-                dst[k * P.c + ch] = s;
-            }
-        }
+        dst[(kh >> 1) * (P.c / 4) + unit * 2 + (kh & 1)] = s;
     }
 }
 
@@ -297,30 +285,29 @@ int64_t parts_of(const lamp_tensor_t *t, const lamp_block_norm_t *p, int64_t *sa
     return need < room ? need : room;
 }
 
-template <bool SF, bool BF, int TPR, int U, int MAXT>
+template <bool SF, bool BF, int TPR, int U, int MAXT, int MINB>
 lamp_status_t launch(const BwdParams &P, int64_t samples, const Shape &sh, cudaStream_t st)
 {
     const int groups = TPR ? sh.threads / TPR : 1;
-    int smem = P.c * 12;
-    if (TPR && groups * P.c * 4 > smem) smem = groups * P.c * 4;
+    const int smem = P.c * (P.logits ? 12 : 8) + (P.part ? groups * P.c * 16 : 0);
+    auto kernel = P.logits ? block_norm_bwd_kernel<SF, BF, TPR, U, MAXT, MINB, true> : block_norm_bwd_kernel<SF, BF, TPR, U, MAXT, MINB, false>;
     if (smem > 32 * 1024) {                                  // static shared memory counts too: well below the 48 KB default
-        static SmemAttrOnce attr;
-        const lamp_status_t s = attr.ensure(block_norm_bwd_kernel<SF, BF, TPR, U, MAXT>, MAX_C * 12);
+        static SmemAttrOnce attr[2];
+        const lamp_status_t s = attr[P.logits ? 1 : 0].ensure(kernel, MAX_C * 28);
         if (s != LAMP_OK) return s;
     }
-    return launch_pdl(samples * P.parts <= 8 * (int64_t)sm_count(), block_norm_bwd_kernel<SF, BF, TPR, U, MAXT>, dim3((unsigned)(samples * P.parts)),
-                      dim3(sh.threads), (size_t)smem, st, P);
+    return launch_pdl(samples * P.parts <= 8 * (int64_t)sm_count(), kernel, dim3((unsigned)(samples * P.parts)), dim3(sh.threads), (size_t)smem, st, P);
 }
 
 template <bool SF, bool BF>
 lamp_status_t dispatch(const BwdParams &P, int64_t samples, const Shape &sh, cudaStream_t st)
 {
-    if (sh.tpr == 4) return launch<SF, BF, 4, 1, 256>(P, samples, sh, st);
-    if (sh.tpr == 8) return launch<SF, BF, 8, 1, 256>(P, samples, sh, st);
-    if (sh.tpr == 16) return launch<SF, BF, 16, 1, 256>(P, samples, sh, st);
-    if (sh.tpr == 32 && sh.u == 1) return launch<SF, BF, 32, 1, 256>(P, samples, sh, st);
-    if (sh.tpr == 32) return launch<SF, BF, 32, 2, 256>(P, samples, sh, st);
-    return sh.threads <= 256 ? launch<SF, BF, 0, 2, 256>(P, samples, sh, st) : launch<SF, BF, 0, 2, 512>(P, samples, sh, st);
+    if (sh.tpr == 4) return launch<SF, BF, 4, 1, 256, 2>(P, samples, sh, st);
+    if (sh.tpr == 8) return launch<SF, BF, 8, 1, 256, 2>(P, samples, sh, st);
+    if (sh.tpr == 16) return launch<SF, BF, 16, 1, 256, 2>(P, samples, sh, st);
+    if (sh.tpr == 32 && sh.u == 1) return launch<SF, BF, 32, 1, 256, 2>(P, samples, sh, st);
+    if (sh.tpr == 32) return launch<SF, BF, 32, 2, 256, 2>(P, samples, sh, st);
+    return launch<SF, BF, 0, 2, 512, 1>(P, samples, sh, st);
 }
 
 }  // namespace

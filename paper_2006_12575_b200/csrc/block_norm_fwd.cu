@@ -111,7 +111,7 @@ block_norm_fwd_kernel(const FwdParams P)
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
                         float branch = fmaf(v[u][j] * rstd, w[j], b[j]);
-                        if (P.logits) branch *= 1.f / (1.f + __expf(-lg[u][j]));
+                        if (P.logits) branch *= sigmoid(lg[u][j]);
                         t[u][j] += branch;
                         if constexpr (!SF) t[u][j] = bf2f(f2bf(t[u][j]));       // t as stored
                     }
