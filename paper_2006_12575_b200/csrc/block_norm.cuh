@@ -123,6 +123,22 @@ __device__ __forceinline__ void row_sum2(float &a, float &b, float (*red)[32], i
     }
 }
 
+template <int TPR>
+__device__ __forceinline__ float row_sum(float a, float (*red)[32], int &turn)
+{
+#pragma unroll
+    for (int o = (TPR == 0 || TPR > 32 ? 32 : TPR) / 2; o > 0; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
+    if constexpr (TPR == 0) {
+        const int w = threadIdx.x >> 5, nw = blockDim.x >> 5;
+        if ((threadIdx.x & 31) == 0) red[turn][w] = a;
+        __syncthreads();
+        a = red[turn][0];
+        for (int i = 1; i < nw; ++i) a += red[turn][i];
+        turn ^= 1;
+    }
+    return a;
+}
+
 // How a call of c channels is laid out.
 struct Shape { int tpr, u, threads, rows_per_cta; };
 inline Shape shape_of(int c)

@@ -106,8 +106,7 @@ block_norm_bwd_kernel(const BwdParams P)
             if ((u * threads + tt) * 8 >= P.c) continue;               // stays zero
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                th[u][j] = add2(th[u][j], twice(-mt));
-                yh[u][j] = add2(yh[u][j], twice(-my));
+                if (!P.rms) { th[u][j] = add2(th[u][j], twice(-mt)); yh[u][j] = add2(yh[u][j], twice(-my)); }
                 qt2 = fma2(th[u][j], th[u][j], qt2);
                 qy2 = fma2(yh[u][j], yh[u][j], qy2);
             }
@@ -115,7 +114,7 @@ block_norm_bwd_kernel(const BwdParams P)
         float qt = both(qt2), qy = both(qy2);
         row_sum2<TPR>(qt, qy, red, turn);
         // a row past the end takes part with zeros only, whatever eps is
-        const float rst = active ? 1.f / sqrtf(qt * inv_c + P.eps) : 0.f, rsy = active ? 1.f / sqrtf(qy * inv_c + P.eps) : 0.f;
+        const float rst = active ? rsqrtf(qt * inv_c + P.eps) : 0.f, rsy = active ? rsqrtf(qy * inv_c + P.eps) : 0.f;
         if (pre) {
             f32x2 s1 = 0, s2 = 0;
 #pragma unroll

@@ -26,10 +26,11 @@ struct FwdParams {
     int64_t hs_pitch;
 };
 
-template <bool SF, bool BF, int TPR, int U, int MAXT>
-__global__ void __launch_bounds__(MAXT)
+template <bool SF, bool BF, int TPR, int U, int MAXT, int MINB, bool LOGITS>
+__global__ void __launch_bounds__(MAXT, MINB)
 block_norm_fwd_kernel(const FwdParams P)
 {
+    using ptx::f32x2; using ptx::fma2; using ptx::add2; using ptx::mul2; using ptx::twice; using ptx::pack2; using ptx::unpack2;
     extern __shared__ __align__(16) float par[];
     __shared__ float red[2][32];
     const int threads = TPR ? TPR : blockDim.x;                    // per row
@@ -61,8 +62,31 @@ block_norm_fwd_kernel(const FwdParams P)
             const bool in = row < P.rows && ch < P.c;
             rx[u] = in ? load_raw<SF>(P.x, (base + row) * P.px + ch) : zero_raw<SF>();
             if (post) ry[u] = in ? load_raw<BF>(P.y, (base + row) * P.py + ch) : zero_raw<BF>();
-            if (P.logits) rl[u] = in ? load_raw<BF>(P.logits, (base + row) * P.pl + ch) : zero_raw<BF>();
+            if (LOGITS) rl[u] = in ? load_raw<BF>(P.logits, (base + row) * P.pl + ch) : zero_raw<BF>();
         }
+    };
+    // centres v (not for rms) and returns 1 / deviation; channels behind c stay zero
+    auto centre = [&](f32x2 (&v)[U][4]) {
+        float mean = 0.f;
+        if (!P.rms) {
+            f32x2 s = 0;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s = add2(s, v[u][j]);
+            mean = row_sum<TPR>(both(s), red, turn) * inv_c;
+        }
+        f32x2 q = 0;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if ((u * threads + tt) * 8 >= P.c) continue;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (!P.rms) v[u][j] = add2(v[u][j], twice(-mean));
+                q = fma2(v[u][j], v[u][j], q);
+            }
+        }
+        return rsqrtf(row_sum<TPR>(both(q), red, turn) * inv_c + P.eps);
     };
     const int64_t step = (int64_t)P.parts * groups;
     int64_t r0 = part * groups;
@@ -70,97 +94,73 @@ block_norm_fwd_kernel(const FwdParams P)
     for (; r0 < P.rows; r0 += step) {                              // the same number of turns for every thread of the CTA
         const int64_t row = r0 + group;
         const bool active = row < P.rows;
-        float t[U][8], v[U][8], lg[U][8];
+        f32x2 t[U][4], v[U][4], lg[U][4];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            to_float<SF>(rx[u], t[u]);
-            if (post) to_float<BF>(ry[u], v[u]);
-            if (P.logits) to_float<BF>(rl[u], lg[u]);
+            to_pairs<SF>(rx[u], t[u]);
+            if (post) to_pairs<BF>(ry[u], v[u]);
+            if (LOGITS) to_pairs<BF>(rl[u], lg[u]);
         }
         if (r0 + step < P.rows) fetch(row + step);                 // in flight while this row is worked on
         if (post) {
-            float s = 0.f, d2 = 0.f, dummy = 0.f;
-            float mean = 0.f;
-            if (!P.rms) {
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) s += v[u][j];
-                row_sum2<TPR>(s, dummy, red, turn);
-                mean = s * inv_c;
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const bool in = (u * threads + tt) * 8 < P.c;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    v[u][j] = in ? v[u][j] - mean : 0.f;
-                    d2 = fmaf(v[u][j], v[u][j], d2);
-                }
-            }
-            dummy = 0.f;
-            row_sum2<TPR>(d2, dummy, red, turn);
-            const float rstd = 1.f / sqrtf(d2 * inv_c + P.eps);
+            const float rstd = centre(v);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int unit = u * threads + tt;
-                if (unit < units) {
-                    float w[8], b[8];
-                    load_par(par4, 0, units, unit, w);
-                    load_par(par4, 1, units, unit, b);
+                if (unit >= units) continue;
+                f32x2 w[4], b[4];
+                uint32_t stored[4];
+                load_par(par4, 0, units, unit, w);
+                load_par(par4, 1, units, unit, b);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        float branch = fmaf(v[u][j] * rstd, w[j], b[j]);
-                        if (P.logits) branch *= sigmoid(lg[u][j]);
-                        t[u][j] += branch;
-                        if constexpr (!SF) t[u][j] = bf2f(f2bf(t[u][j]));       // t as stored
+                for (int j = 0; j < 4; ++j) {
+                    f32x2 branch = fma2(mul2(v[u][j], twice(rstd)), w[j], b[j]);
+                    if (LOGITS) {
+                        float p, q;
+                        unpack2(lg[u][j], p, q);
+                        branch = mul2(branch, pack2(__float_as_uint(sigmoid(p)), __float_as_uint(sigmoid(q))));
                     }
-                    if (active) store8<SF>(P.out, (base + row) * P.po + unit * 8, t[u]);
+                    t[u][j] = add2(t[u][j], branch);
+                    if constexpr (!SF) {                           // t as stored
+                        float p, q;
+                        unpack2(t[u][j], p, q);
+                        const __nv_bfloat162 h = __floats2bfloat162_rn(p, q);
+                        const uint32_t bits = *reinterpret_cast<const uint32_t *>(&h);
+                        stored[j] = bits;
+                        t[u][j] = pack2(bits << 16, bits & 0xFFFF0000u);
+                    }
                 }
+                if (!active) continue;
+                if constexpr (SF) store_pairs<SF>(P.out, (base + row) * P.po + unit * 8, t[u]);
+                else *reinterpret_cast<uint4 *>((bf16 *)P.out + (base + row) * P.po + unit * 8) = make_uint4(stored[0], stored[1], stored[2], stored[3]);
             }
         }
         if (pre) {
-            float s = 0.f, d2 = 0.f, dummy = 0.f;
-            float mean = 0.f;
-            if (!P.rms) {
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) s += t[u][j];
-                row_sum2<TPR>(s, dummy, red, turn);
-                mean = s * inv_c;
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const bool in = (u * threads + tt) * 8 < P.c;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    t[u][j] = in ? t[u][j] - mean : 0.f;
-                    d2 = fmaf(t[u][j], t[u][j], d2);
-                }
-            }
-            dummy = 0.f;
-            row_sum2<TPR>(d2, dummy, red, turn);
-            const float rstd = 1.f / sqrtf(d2 * inv_c + P.eps);
+            const float rstd = centre(t);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int unit = u * threads + tt;
                 const bool in = unit < units;
                 if (in) {
-                    float w[8], b[8];
+                    f32x2 w[4], b[4];
                     load_par(par4, 2, units, unit, w);
                     load_par(par4, 3, units, unit, b);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) t[u][j] = fmaf(t[u][j] * rstd, w[j], b[j]);
-                    if (P.h && active) store8<BF>(P.h, (base + row) * P.ph + unit * 8, t[u]);
+                    for (int j = 0; j < 4; ++j) t[u][j] = fma2(mul2(t[u][j], twice(rstd)), w[j], b[j]);
+                    if (P.h && active) store_pairs<BF>(P.h, (base + row) * P.ph + unit * 8, t[u]);
                 }
                 if (P.hq) {                                        // 16 threads hold one block of 128 channels
-                    float m = in ? amax8(t[u]) : 0.f;
+                    float f[8];
 #pragma unroll
-                    for (int o = (TPR == 0 || TPR > 16 ? 16 : TPR) / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-                    m = fmaxf(m, FP8_AMAX_MIN);
+                    for (int j = 0; j < 4; ++j) unpack2(t[u][j], f[2 * j], f[2 * j + 1]);
+                    if (!in) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) f[j] = 0.f;
+                    }
+                    float m;
+                    const uint2 codes = encode_block<(TPR == 0 || TPR > 16 ? 16 : TPR)>(f, m);
                     if (in && active) {
-                        *reinterpret_cast<uint2 *>(P.hq + (base + row) * P.hq_pitch + unit * 8) = encode8(t[u], __fdiv_rn(448.f, m));
+                        *reinterpret_cast<uint2 *>(P.hq + (base + row) * P.hq_pitch + unit * 8) = codes;
                         if ((unit & 15) == 0) P.hs[(unit >> 4) * P.hs_pitch + base + row] = __fmul_rn(m, 1.0f / 448.0f);
                     }
                 }
@@ -169,28 +169,32 @@ block_norm_fwd_kernel(const FwdParams P)
     }
 }
 
-template <bool SF, bool BF, int TPR, int U, int MAXT>
+// CTAs per SM that the kernel is compiled for: the grid is that many per SM, so that all are resident at once (four per SM
+// where three fit cost a second, mostly empty wave: 120 us against MEASURED on 131,072 x 512)
+constexpr int FWD_CTAS = 3;
+
+template <bool SF, bool BF, int TPR, int U, int MAXT, int MINB>
 lamp_status_t launch(const FwdParams &P, int64_t samples, const Shape &sh, cudaStream_t st)
 {
     const int smem = P.c * 16;
+    auto kernel = P.logits ? block_norm_fwd_kernel<SF, BF, TPR, U, MAXT, MINB, true> : block_norm_fwd_kernel<SF, BF, TPR, U, MAXT, MINB, false>;
     if (smem > 32 * 1024) {                                  // static shared memory counts too: well below the 48 KB default
-        static SmemAttrOnce attr;
-        const lamp_status_t s = attr.ensure(block_norm_fwd_kernel<SF, BF, TPR, U, MAXT>, MAX_C * 16);
+        static SmemAttrOnce attr[2];
+        const lamp_status_t s = attr[P.logits ? 1 : 0].ensure(kernel, MAX_C * 16);
         if (s != LAMP_OK) return s;
     }
-    return launch_pdl(samples * P.parts <= 8 * (int64_t)sm_count(), block_norm_fwd_kernel<SF, BF, TPR, U, MAXT>, dim3((unsigned)(samples * P.parts)),
-                      dim3(sh.threads), (size_t)smem, st, P);
+    return launch_pdl(samples * P.parts <= 8 * (int64_t)sm_count(), kernel, dim3((unsigned)(samples * P.parts)), dim3(sh.threads), (size_t)smem, st, P);
 }
 
 template <bool SF, bool BF>
 lamp_status_t dispatch(const FwdParams &P, int64_t samples, const Shape &sh, cudaStream_t st)
 {
-    if (sh.tpr == 4) return launch<SF, BF, 4, 1, 256>(P, samples, sh, st);
-    if (sh.tpr == 8) return launch<SF, BF, 8, 1, 256>(P, samples, sh, st);
-    if (sh.tpr == 16) return launch<SF, BF, 16, 1, 256>(P, samples, sh, st);
-    if (sh.tpr == 32 && sh.u == 1) return launch<SF, BF, 32, 1, 256>(P, samples, sh, st);
-    if (sh.tpr == 32) return launch<SF, BF, 32, 2, 256>(P, samples, sh, st);
-    return launch<SF, BF, 0, 2, 512>(P, samples, sh, st);
+    if (sh.tpr == 4) return launch<SF, BF, 4, 1, 256, FWD_CTAS>(P, samples, sh, st);
+    if (sh.tpr == 8) return launch<SF, BF, 8, 1, 256, FWD_CTAS>(P, samples, sh, st);
+    if (sh.tpr == 16) return launch<SF, BF, 16, 1, 256, FWD_CTAS>(P, samples, sh, st);
+    if (sh.tpr == 32 && sh.u == 1) return launch<SF, BF, 32, 1, 256, FWD_CTAS>(P, samples, sh, st);
+    if (sh.tpr == 32) return launch<SF, BF, 32, 2, 256, FWD_CTAS>(P, samples, sh, st);
+    return sh.threads <= 256 ? launch<SF, BF, 0, 2, 256, FWD_CTAS>(P, samples, sh, st) : launch<SF, BF, 0, 2, 512, 1>(P, samples, sh, st);
 }
 
 }  // namespace
@@ -258,7 +262,7 @@ extern "C" lamp_status_t lamp_block_norm_fwd(const lamp_block_norm_t *p, const l
     P.rows = rows / samples;
     const Shape sh = shape_of(P.c);
     const int64_t need = (P.rows + sh.rows_per_cta - 1) / sh.rows_per_cta;
-    int64_t room = (int64_t)sm_count() * (1024 / sh.threads) / samples;
+    int64_t room = (int64_t)sm_count() * (sh.threads <= 256 ? FWD_CTAS * 256 / sh.threads : 1) / samples;
     if (room < 1) room = 1;
     P.parts = (int32_t)(need < room ? need : room);
     if (samples * P.parts > 2147483647ll) return LAMP_ERR_UNSUPPORTED;

@@ -52,12 +52,10 @@ quant_rows_kernel(const void *__restrict__ x, int64_t pitch, int c, int kb, int6
     }
 #pragma unroll
     for (int u = 0; u < QR_UNROLL; ++u) {
-        float m = amax8(f[u]);
-#pragma unroll
-        for (int o = 8; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-        m = fmaxf(m, FP8_AMAX_MIN);
+        float m;
+        const uint2 codes = encode_block<16>(f[u], m);
         if (in[u]) {
-            *reinterpret_cast<uint2 *>(q + row[u] * q_pitch + blk[u] * 128 + l16 * 8) = encode8(f[u], __fdiv_rn(448.f, m));
+            *reinterpret_cast<uint2 *>(q + row[u] * q_pitch + blk[u] * 128 + l16 * 8) = codes;
             if (l16 == 0) scale[blk[u] * scale_pitch + row[u]] = __fmul_rn(m, 1.0f / 448.0f);
         }
     }
@@ -143,8 +141,8 @@ quant_tile_kernel(const void *__restrict__ x, int64_t pitch, int c, int64_t rows
         uint32_t w0[8], w1[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            w0[i] = encode4(f0[4 * i], f0[4 * i + 1], f0[4 * i + 2], f0[4 * i + 3], i0);
-            w1[i] = encode4(f1[4 * i], f1[4 * i + 1], f1[4 * i + 2], f1[4 * i + 3], i1);
+            w0[i] = encode4<true>(f0[4 * i], f0[4 * i + 1], f0[4 * i + 2], f0[4 * i + 3], i0);
+            w1[i] = encode4<true>(f1[4 * i], f1[4 * i + 1], f1[4 * i + 2], f1[4 * i + 3], i1);
         }
         if (rows - v0 >= 32) {                                                // q_pitch and v0 are multiples of 16
             *reinterpret_cast<uint4 *>(o0) = make_uint4(w0[0], w0[1], w0[2], w0[3]);
@@ -161,7 +159,7 @@ quant_tile_kernel(const void *__restrict__ x, int64_t pitch, int c, int64_t rows
         __syncthreads();                                                      // the tile has been read by everybody
 #pragma unroll
         for (int i = 0; i < 32; ++i)
-            *reinterpret_cast<uint16_t *>(smem + (part * 32 + i) * 144 + cp * 2) = encode2(f0[i], f1[i], i0, i1);
+            *reinterpret_cast<uint16_t *>(smem + (part * 32 + i) * 144 + cp * 2) = encode2<true>(f0[i], f1[i], i0, i1);
         __syncthreads();
         for (int i = t; i < 128 * 16; i += QT) {                              // 8-byte units: c is a multiple of 8
             const int r = i >> 4, u = i & 15;
