@@ -134,7 +134,7 @@ def test_repeats_bit_for_bit_on_streams_and_in_graphs():
 
 
 # --- quantiser: bit for bit ---------------------------------------------------------------------------------------------
-@pytest.mark.parametrize("rows,c", [(1, 8), (3, 128), (129, 136), (300, 264), (17, 1000), (128, 128), (1000, 24), (257, 512)])
+@pytest.mark.parametrize("rows,c", [(1, 8), (3, 128), (129, 136), (300, 264), (17, 1000), (128, 128), (1000, 24), (257, 512), (5, 12808), (700, 640)])
 @pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("transpose,tile", [(False, False), (False, True), (True, False), (True, True)])
 def test_quantise_matches_oracle(rows, c, dt, transpose, tile):
