@@ -27,6 +27,7 @@ using namespace ptx;
 
 constexpr int KB = 128;                       // codes per scale block = bytes per shared-memory row
 constexpr int MAX_STAGES = 10, MAX_ACC = 4;
+constexpr int RING = 4;                       // blocks of scales in flight (ScaleRing)
 
 struct GemmParams {
     int32_t rows_l, rows_c;                   // rows of the lane operand and of the column operand
@@ -47,13 +48,13 @@ struct GemmParams {
 
 template <int BN> struct GemmLayout {
     static constexpr int A_BYTES = 128 * KB, C_BYTES = BN * KB, STAGE_BYTES = A_BYTES + C_BYTES;
-    static constexpr int STAGES = BN == 256 ? 4 : BN == 128 ? 6 : BN == 64 ? 8 : 9;
-    static constexpr int NACC = BN == 256 ? 2 : 4;
+    static constexpr int STAGES = BN == 128 ? 6 : BN == 64 ? 8 : 9;
+    static constexpr int NACC = 4;
     static constexpr int NEPI = BN >= 64 ? 8 : 4;                 // promotion warps
     static constexpr int CW = BN >= 64 ? BN / 2 : BN;             // columns per promotion warp
     static constexpr int THREADS = 64 + 32 * NEPI;
     static constexpr int TMEM_COLS = NACC * BN;                   // 64 .. 512, a power of two
-    static constexpr int SCALE_BYTES = NEPI * 2 * CW * 4;
+    static constexpr int SCALE_BYTES = NEPI * RING * (32 + CW) * 4;
     static constexpr int BAR_BYTES = (2 * MAX_STAGES + 2 * MAX_ACC) * 8 + 16;
     static constexpr int TOTAL = 1024 + STAGES * STAGE_BYTES + SCALE_BYTES + BAR_BYTES;
     static_assert(BN * 128 * 4 <= STAGES * STAGE_BYTES, "the split-k parts reuse the stages");
@@ -198,6 +199,71 @@ __device__ __forceinline__ void reduce_parts(const GemmParams &P, uint32_t part_
     }
 }
 
+// The scales a promotion warp needs - one per lane row, and one per column (COLVEC) or one for all its columns - come through
+// a ring in shared memory that asynchronous copies fill RING - 1 blocks ahead, across tiles.  (Loaded one block ahead into
+// registers they were the bottleneck: an L2 round trip under load, about 1300 cycles, per block of 512 tensor cycles.)
+template <int CW, bool COLVEC> struct ScaleRing {
+    static constexpr int SLOT = 32 + (COLVEC ? CW : 4);            // floats of a slot
+    float *buf;
+    const float *slp, *scp;
+    int lane, cols;                                                // cols: columns of this warp that exist
+    bool row_in;
+    int64_t tile, tile_step;
+    int kb, kb0, kb1;
+    uint32_t put;
+
+    // where the scales of `tile` start (lrows: lane rows of a tile; row0, col0: this warp's rows and columns within one)
+    __device__ __forceinline__ void at_tile(const GemmParams &P, int lrows, int bn, int row0, int col0)
+    {
+        if (tile >= P.tiles) return;
+        const int64_t row = (tile / P.nc) * lrows + row0 + lane;
+        const int64_t col = (tile % P.nc) * bn + col0;
+        row_in = row < P.rows_l;
+        cols = (int)(P.rows_c - col);
+        slp = P.sl + (P.tile_l ? row / 128 : row);
+        scp = P.sc + (P.tile_c ? col / 128 : col);
+    }
+    __device__ __forceinline__ static void copy4(float *dst, const float *src, bool in)
+    {
+        if (in) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+        else *dst = 0.f;
+    }
+    __device__ __forceinline__ void issue(const GemmParams &P, int lrows, int bn, int row0, int col0)
+    {
+        if (tile < P.tiles) {
+            float *s = buf + (put % RING) * SLOT;
+            copy4(s + lane, slp + (int64_t)kb * P.pl, row_in);
+            if constexpr (COLVEC) {
+#pragma unroll
+                for (int i = 0; i < (CW + 31) / 32; ++i) {
+                    const int j = i * 32 + lane;
+                    if (j < CW) copy4(s + 32 + j, scp + (int64_t)kb * P.pc + j, j < cols);
+                }
+            } else if (lane == 0) {
+                copy4(s + 32, scp + (int64_t)kb * P.pc, cols > 0);
+            }
+            if (++kb == kb1) { kb = kb0; tile += tile_step; at_tile(P, lrows, bn, row0, col0); }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        ++put;
+    }
+    __device__ __forceinline__ void start(const GemmParams &P, float *b, int ln, int64_t t0, int64_t ts, int k0, int k1, int lrows, int bn, int row0, int col0)
+    {
+        buf = b; lane = ln; tile = t0; tile_step = ts; kb = kb0 = k0; kb1 = k1; put = 0;
+        at_tile(P, lrows, bn, row0, col0);
+        for (int i = 0; i < RING - 1; ++i) issue(P, lrows, bn, row0, col0);
+    }
+    // the scales of the n-th block (n counts over all tiles); also keeps the ring filled
+    __device__ __forceinline__ const float *get(const GemmParams &P, uint32_t n, int lrows, int bn, int row0, int col0)
+    {
+        __syncwarp();                                              // every lane is done with the slot that is filled now
+        issue(P, lrows, bn, row0, col0);
+        asm volatile("cp.async.wait_group %0;" ::"n"(RING - 1) : "memory");
+        __syncwarp();
+        return buf + (n % RING) * SLOT;
+    }
+};
+
 template <int BN, bool COLVEC>
 __global__ void __launch_bounds__(GemmLayout<BN>::THREADS, 1)
 fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constant__ CUtensorMap map_c, const GemmParams P)
@@ -286,46 +352,20 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constant
         // ------------------------------------------------------------------ promotion
         const int q = warp & 3, half = (warp - 2) >> 2;                    // lane quarter and column part of this warp
         const int lane_row = q * 32 + lane;
-        float *sbuf = scale_buf + (warp - 2) * 2 * CW;
+        ScaleRing<CW, COLVEC> scales;
+        scales.start(P, scale_buf + (warp - 2) * RING * (32 + CW), lane, tile0, tile_step, kb0, kb1, 128, BN, q * 32, half * CW);
+        uint32_t block = 0;
         uint32_t acc = 0, acc_phase = 0;
         bool ok = true;
         for (int64_t tile = tile0; tile < P.tiles; tile += tile_step) {
             const int64_t row = (tile / P.nc) * 128 + lane_row;
             const int col0 = (int)(tile % P.nc) * BN, cbase = col0 + half * CW;
-            const bool row_in = row < P.rows_l;
-            const float *slp = P.sl + (P.tile_l ? row / 128 : row);
-            const float *scp = P.sc + (P.tile_c ? cbase / 128 : cbase);
-            const bool c_in = cbase < P.rows_c;
-            constexpr int NS = COLVEC ? (CW + 31) / 32 : 1;
-            float sl_next = 0.f, sc_next[NS];
-            auto load_scales = [&](int kb) {
-                sl_next = row_in ? __ldg(slp + (int64_t)kb * P.pl) : 0.f;
-                if constexpr (COLVEC) {
-#pragma unroll
-                    for (int i = 0; i < NS; ++i) {
-                        const int j = i * 32 + lane;
-                        sc_next[i] = (j < CW && cbase + j < P.rows_c) ? __ldg(scp + (int64_t)kb * P.pc + j) : 0.f;
-                    }
-                } else {
-                    sc_next[0] = c_in ? __ldg(scp + (int64_t)kb * P.pc) : 0.f;
-                }
-            };
             f32x2 sum[CW / 2];
 #pragma unroll
             for (int i = 0; i < CW / 2; ++i) sum[i] = 0ull;
-            load_scales(kb0);
             for (int kb = kb0; kb < kb1; ++kb) {
-                float s = sl_next;
-                float *sb = sbuf + (kb & 1) * CW;
-                if constexpr (COLVEC) {
-#pragma unroll
-                    for (int i = 0; i < NS; ++i) if (i * 32 + lane < CW) sb[i * 32 + lane] = sc_next[i];
-                    __syncwarp();                               // the buffer of block kb - 2 has been read by every lane
-                } else {
-                    s *= sc_next[0];
-                }
-                if (kb + 1 < kb1) load_scales(kb + 1);
-                const f32x2 s2 = pack2(__float_as_uint(s), __float_as_uint(s));
+                const float *sv = scales.get(P, block++, 128, BN, q * 32, half * CW), *sb = sv + 32;
+                const f32x2 s2 = twice(COLVEC ? sv[lane] : sv[lane] * sb[0]);
                 ok = ok && __all_sync(0xffffffffu, mbar_wait(tfull0 + 8 * acc, acc_phase, abort_flag));
                 if (!ok) break;
                 tc_fence_after();
@@ -404,6 +444,227 @@ bool encode_operand(const lamp_fp8_operand_t *o, int box_rows, CUtensorMap *map)
     const cuuint32_t es[2] = {1, 1};
     return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, o->q, gdim, gstride, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// ----------------------------------------------------------------------------------------------------------------------
+// CTA pairs: tiles of 256 x BN, each CTA of the pair 128 lane rows (its tensor memory) and half of the columns' operand
+// ----------------------------------------------------------------------------------------------------------------------
+// What bounds the product of large operands is the path from L2 to shared memory: a 128 x 256 tile of one CTA takes 48 KB per
+// block of k, and 148 SMs took 11 TB/s at most (16384 x 4096 x 4096: 284 us with the promotion left out).  A pair shares the column
+// operand: 32 KB per CTA for the same work.  The leader (rank 0) issues the MMAs of both CTAs; full barriers live in the
+// leader (both CTAs' copies complete there), empty and accumulator-full barriers in each CTA (the commits arrive in both),
+// accumulator-empty barriers in the leader (the promotion warps of both CTAs arrive).
+// Warps 4 .. 11 promote: 128 sums per thread and 64 loaded values need 216 registers, which the other four warps give up (384 x 168 at launch = 128 x 72 + 256 x 216).
+template <int BN> struct PairLayout {
+    static constexpr int A_BYTES = 128 * KB, C_BYTES = BN / 2 * KB, STAGE_BYTES = A_BYTES + C_BYTES;
+    static constexpr int STAGES = BN == 256 ? 6 : 8;
+    static constexpr int NACC = BN == 256 ? 2 : 4;
+    static constexpr int CW = BN / 2;                             // columns per promotion warp
+    static constexpr int THREADS = 384, TMEM_COLS = 512;
+    static constexpr int SCALE_BYTES = 8 * RING * (32 + CW) * 4;
+    static constexpr int BAR_BYTES = (2 * MAX_STAGES + 2 * MAX_ACC) * 8 + 16;
+    static constexpr int TOTAL = 1024 + STAGES * STAGE_BYTES + SCALE_BYTES + BAR_BYTES;
+    static_assert(TOTAL <= 227 * 1024 && STAGES <= MAX_STAGES && NACC <= MAX_ACC && NACC * BN <= TMEM_COLS, "");
+};
+
+__device__ __forceinline__ uint32_t map_to_rank(uint32_t addr, uint32_t rank)
+{
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap *map, uint32_t leader_bar, int c0, int c1)
+{
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(leader_bar), "r"(c0), "r"(c1) : "memory");
+}
+__device__ __forceinline__ void umma_fp8_pair(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n}"
+                 ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+// arrives on the barrier of this offset in both CTAs once the MMAs issued so far have completed
+__device__ __forceinline__ void umma_commit_pair(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(bar), "h"((uint16_t)3) : "memory");
+}
+// Arrival on a barrier of either CTA.  No release at cluster scope: what it hands over is tensor memory that has been read,
+// not memory that was written, and that release is a fence that waits for everything the thread has in flight - it took
+// 1200 cycles per block of k, three quarters of the kernel's time.
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr)
+{
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+
+template <int BN, bool COLVEC>
+__global__ void __launch_bounds__(PairLayout<BN>::THREADS, 1)
+fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constant__ CUtensorMap map_c, const GemmParams P)
+{
+    using L = PairLayout<BN>;
+    constexpr int STAGES = L::STAGES, NACC = L::NACC, CW = L::CW;
+    constexpr uint32_t IDESC = (1u << 4) | ((uint32_t)(BN >> 3) << 17) | ((256u >> 4) << 24);
+
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    float *scale_buf = (float *)(smem + STAGES * L::STAGE_BYTES);
+    uint64_t *bars = (uint64_t *)(smem + STAGES * L::STAGE_BYTES + L::SCALE_BYTES);
+    uint32_t *tmem_slot = (uint32_t *)(bars + 2 * MAX_STAGES + 2 * MAX_ACC);
+    volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    const uint32_t full0 = smem_u32(bars), empty0 = smem_u32(bars + MAX_STAGES);
+    const uint32_t tfull0 = smem_u32(bars + 2 * MAX_STAGES), tempty0 = smem_u32(bars + 2 * MAX_STAGES + MAX_ACC);
+
+    pdl_launch_dependents();
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
+        for (int a = 0; a < NACC; ++a) { mbar_init(tfull0 + 8 * a, 1); mbar_init(tempty0 + 8 * a, 16); }
+        *abort_flag = 0;
+        mbar_init_fence();
+    }
+    if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(L::TMEM_COLS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    cluster_sync_all();          // the peer's barriers exist
+    pdl_wait();                  // everything above touched shared and tensor memory only
+    const uint32_t tmem_base = *tmem_slot;
+    const int64_t tile0 = blockIdx.x >> 1, tile_step = gridDim.x >> 1;
+    bool ok = true;
+
+    if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        if (warp == 0 && lane == 0) {
+            // -------------------------------------------------------------- TMA producer, one per CTA
+            int stage = 0;
+            uint32_t phase = 0;
+            for (int64_t tile = tile0; tile < P.tiles && ok; tile += tile_step) {
+                const int l0 = (int)(tile / P.nc) * 256 + (int)rank * 128, c0 = (int)(tile % P.nc) * BN + (int)rank * (BN / 2);
+                for (int kb = 0; kb < P.kblocks; ++kb) {
+                    if (!mbar_wait(empty0 + 8 * stage, phase ^ 1, abort_flag)) { ok = false; break; }
+                    const uint32_t fb = map_to_rank(full0 + 8 * stage, 0);
+                    if (rank == 0) mbar_expect_tx(full0 + 8 * stage, 2 * L::STAGE_BYTES);
+                    const uint32_t sa = smem_u32(smem + stage * L::STAGE_BYTES);
+                    tma_load_2d_pair(sa, &map_l, fb, kb * KB, l0);
+                    tma_load_2d_pair(sa + L::A_BYTES, &map_c, fb, kb * KB, c0);
+                    if (++stage == STAGES) { stage = 0; phase ^= 1; }
+                }
+            }
+        } else if (warp == 1 && lane == 0 && rank == 0) {
+            // -------------------------------------------------------------- MMA issuer, in the leader
+            int stage = 0;
+            uint32_t phase = 0, acc = 0, acc_phase = 0;
+            for (int64_t tile = tile0; tile < P.tiles && ok; tile += tile_step) {
+                for (int kb = 0; kb < P.kblocks; ++kb) {
+                    if (!mbar_wait(tempty0 + 8 * acc, acc_phase ^ 1, abort_flag)) { ok = false; break; }
+                    if (!mbar_wait(full0 + 8 * stage, phase, abort_flag)) { ok = false; break; }
+                    tc_fence_after();
+                    const uint32_t sa = smem_u32(smem + stage * L::STAGE_BYTES);
+                    const uint64_t da = make_desc(sa, 0, 8 * KB, 2), dc = make_desc(sa + L::A_BYTES, 0, 8 * KB, 2);
+#pragma unroll
+                    for (int k = 0; k < KB / 32; ++k)
+                        umma_fp8_pair(tmem_base + acc * BN, da + 2 * k, dc + 2 * k, IDESC, k ? 1u : 0u);
+                    umma_commit_pair(empty0 + 8 * stage);
+                    umma_commit_pair(tfull0 + 8 * acc);
+                    if (++stage == STAGES) { stage = 0; phase ^= 1; }
+                    if (++acc == NACC) { acc = 0; acc_phase ^= 1; }
+                }
+            }
+        }
+        __syncwarp();
+    } else {
+        // ------------------------------------------------------------------ promotion
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        const int q = warp & 3, half = (warp - 4) >> 2;
+        const int lane_row = q * 32 + lane;
+        const int row0 = (int)rank * 128 + q * 32;
+        ScaleRing<CW, COLVEC> scales;
+        scales.start(P, scale_buf + (warp - 4) * RING * (32 + CW), lane, tile0, tile_step, 0, P.kblocks, 256, BN, row0, half * CW);
+        uint32_t block = 0;
+        uint32_t acc = 0, acc_phase = 0;
+        const uint32_t tempty_leader = map_to_rank(tempty0, 0);
+        for (int64_t tile = tile0; tile < P.tiles && ok; tile += tile_step) {
+            const int64_t row = (tile / P.nc) * 256 + rank * 128 + lane_row;
+            const int cbase = (int)(tile % P.nc) * BN + half * CW;
+            f32x2 sum[CW / 2];
+#pragma unroll
+            for (int i = 0; i < CW / 2; ++i) sum[i] = 0ull;
+            for (int kb = 0; kb < P.kblocks; ++kb) {
+                const float *sv = scales.get(P, block++, 256, BN, row0, half * CW), *sb = sv + 32;
+                const f32x2 s2 = twice(COLVEC ? sv[lane] : sv[lane] * sb[0]);
+                ok = __all_sync(0xffffffffu, mbar_wait(tfull0 + 8 * acc, acc_phase, abort_flag));
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t trow = tmem_base + ((uint32_t)(q * 32) << 16) + acc * BN + half * CW;
+                uint32_t r[2][32];
+                tmem_ld32(trow, r[0]);
+#pragma unroll
+                for (int c = 0; c < CW / 32; ++c) {
+                    tmem_ld_wait();
+                    if (c + 1 < CW / 32) {
+                        tmem_ld32(trow + (c + 1) * 32, r[(c + 1) & 1]);
+                    } else {                                       // everything is in registers: the accumulator is free
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_cluster(tempty_leader + 8 * acc);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        f32x2 v = pack2(r[c & 1][2 * j], r[c & 1][2 * j + 1]);
+                        if constexpr (COLVEC) v = mul2(v, *reinterpret_cast<const f32x2 *>(sb + c * 32 + 2 * j));
+                        sum[c * 16 + j] = fma2(v, s2, sum[c * 16 + j]);
+                    }
+                }
+                if (++acc == NACC) { acc = 0; acc_phase ^= 1; }
+            }
+            if (!ok) break;
+#pragma unroll
+            for (int c = 0; c < CW / 16; ++c) {
+                float v[16];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) unpack2(sum[c * 8 + j], v[2 * j], v[2 * j + 1]);
+                finish<16>(P, row, cbase + c * 16, v);
+            }
+        }
+    }
+    if (!ok) {
+        if (P.status) atomicExch(P.status, (int)LAMP_ERR_TIMEOUT);
+        settle();                                                  // copies in flight
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();          // no CTA leaves, or frees tensor memory, while the other still uses what is its own
+    tc_fence_after();
+    if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(L::TMEM_COLS) : "memory");
+}
+
+template <int BN, bool COLVEC>
+lamp_status_t launch_pair(const lamp_fp8_operand_t *l, const lamp_fp8_operand_t *c, const GemmParams &P, cudaStream_t st)
+{
+    using L = PairLayout<BN>;
+    CUtensorMap ml, mc;
+    if (!encode_operand(l, 128, &ml) || !encode_operand(c, BN / 2, &mc)) return LAMP_ERR_CUDA;
+    static SmemAttrOnce attr;
+    { const lamp_status_t as = attr.ensure(fp8_gemm_pair_kernel<BN, COLVEC>, (int)L::TOTAL); if (as != LAMP_OK) return as; }
+    const int pairs = sm_count() / 2;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(2 * (unsigned)(P.tiles < pairs ? P.tiles : pairs));
+    cfg.blockDim = dim3(L::THREADS);
+    cfg.dynamicSmemBytes = L::TOTAL;
+    cfg.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = 2; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = P.tiles <= 4 * (int64_t)pairs ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, fp8_gemm_pair_kernel<BN, COLVEC>, ml, mc, P) == cudaSuccess ? LAMP_OK : LAMP_ERR_CUDA;
 }
 
 template <int BN, bool COLVEC>
@@ -486,18 +747,24 @@ extern "C" lamp_status_t lamp_gemm_fp8(const lamp_fp8_operand_t *a, const lamp_f
     P.status = status_word_ptr();
     const int sms = sm_count();
     P.nl = (P.rows_l + 127) / 128;
-    int bn = P.rows_c <= 16 ? 16 : P.rows_c <= 32 ? 32 : P.rows_c <= 64 ? 64 : 128;
-    if (P.rows_c > 128 && (int64_t)P.nl * ((P.rows_c + 255) / 256) >= sms) bn = 256;
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    P.splits = 1;
+    // pairs where their tiles fill the GPU
+    for (int bn = 256; bn >= 128; bn /= 2) {
+        const int64_t nl = (P.rows_l + 255) / 256, nc = (P.rows_c + bn - 1) / bn;
+        if (swap || P.rows_c < bn || nl * nc * 2 < sms) continue;
+        P.nl = (int32_t)nl; P.nc = (int32_t)nc; P.tiles = nl * nc;
+        if (bn == 256) return c->tile_scale ? launch_pair<256, false>(l, c, P, st) : launch_pair<256, true>(l, c, P, st);
+        return c->tile_scale ? launch_pair<128, false>(l, c, P, st) : launch_pair<128, true>(l, c, P, st);
+    }
+    const int bn = P.rows_c <= 16 ? 16 : P.rows_c <= 32 ? 32 : P.rows_c <= 64 ? 64 : 128;
     P.nc = (P.rows_c + bn - 1) / bn;
     P.tiles = (int64_t)P.nl * P.nc;
-    P.splits = 1;
     while (P.splits < 8 && P.tiles * P.splits * 2 <= sms && P.kblocks >= 4 * P.splits) P.splits *= 2;
-    cudaStream_t st = (cudaStream_t)cuda_stream;
     switch (bn) {
     case 16: return launch_cv<16>(l, c, P, st);
     case 32: return launch_cv<32>(l, c, P, st);
     case 64: return launch_cv<64>(l, c, P, st);
-    case 128: return launch_cv<128>(l, c, P, st);
-    default: return launch_cv<256>(l, c, P, st);
+    default: return launch_cv<128>(l, c, P, st);
     }
 }
