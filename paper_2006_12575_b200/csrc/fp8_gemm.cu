@@ -27,7 +27,7 @@ using namespace ptx;
 
 constexpr int KB = 128;                       // codes per scale block = bytes per shared-memory row
 constexpr int MAX_STAGES = 10, MAX_ACC = 4;
-constexpr int RING = 4;                       // blocks of scales in flight (ScaleRing)
+constexpr int RING = 8;                       // blocks of scales in flight (Scales)
 
 struct GemmParams {
     int32_t rows_l, rows_c;                   // rows of the lane operand and of the column operand
@@ -52,10 +52,10 @@ template <int BN> struct GemmLayout {
     static constexpr int NACC = 4;
     static constexpr int NEPI = BN >= 64 ? 8 : 4;                 // promotion warps
     static constexpr int CW = BN >= 64 ? BN / 2 : BN;             // columns per promotion warp
-    static constexpr int THREADS = 64 + 32 * NEPI;
+    static constexpr int THREADS = 96 + 32 * NEPI;                // + TMA, MMA and scale warps
     static constexpr int TMEM_COLS = NACC * BN;                   // 64 .. 512, a power of two
-    static constexpr int SCALE_BYTES = NEPI * RING * (32 + CW) * 4;
-    static constexpr int BAR_BYTES = (2 * MAX_STAGES + 2 * MAX_ACC) * 8 + 16;
+    static constexpr int SCALE_BYTES = RING * (128 + (BN)) * 4;
+    static constexpr int BAR_BYTES = (2 * MAX_STAGES + 2 * MAX_ACC + 2 * RING) * 8 + 16;
     static constexpr int TOTAL = 1024 + STAGES * STAGE_BYTES + SCALE_BYTES + BAR_BYTES;
     static_assert(BN * 128 * 4 <= STAGES * STAGE_BYTES, "the split-k parts reuse the stages");
     static_assert(TOTAL <= 227 * 1024 && STAGES <= MAX_STAGES && NACC <= MAX_ACC, "");
@@ -199,70 +199,67 @@ __device__ __forceinline__ void reduce_parts(const GemmParams &P, uint32_t part_
     }
 }
 
-// The scales a promotion warp needs - one per lane row, and one per column (COLVEC) or one for all its columns - come through
-// a ring in shared memory that asynchronous copies fill RING - 1 blocks ahead, across tiles.  (Loaded one block ahead into
-// registers they were the bottleneck: an L2 round trip under load, about 1300 cycles, per block of 512 tensor cycles.)
-template <int CW, bool COLVEC> struct ScaleRing {
-    static constexpr int SLOT = 32 + (COLVEC ? CW : 4);            // floats of a slot
-    float *buf;
-    const float *slp, *scp;
-    int lane, cols;                                                // cols: columns of this warp that exist
-    bool row_in;
-    int64_t tile, tile_step;
-    int kb, kb0, kb1;
-    uint32_t put;
-
-    // where the scales of `tile` start (lrows: lane rows of a tile; row0, col0: this warp's rows and columns within one)
-    __device__ __forceinline__ void at_tile(const GemmParams &P, int lrows, int bn, int row0, int col0)
-    {
-        if (tile >= P.tiles) return;
-        const int64_t row = (tile / P.nc) * lrows + row0 + lane;
-        const int64_t col = (tile % P.nc) * bn + col0;
-        row_in = row < P.rows_l;
-        cols = (int)(P.rows_c - col);
-        slp = P.sl + (P.tile_l ? row / 128 : row);
-        scp = P.sc + (P.tile_c ? col / 128 : col);
-    }
+// The scales of a block - one per lane row, and one per column (COLVEC) or one per 128 columns - come through a ring of RING
+// slots in shared memory that one warp fills with asynchronous copies, ahead and across tiles; the promotion warps wait
+// for a slot as they wait for an accumulator.  (Loaded by the promotion warps themselves a block ahead they cost an L2
+// round trip under load, about 1300 cycles, per block of 512 tensor cycles; copied by them 480 cycles of their issue.)
+template <int BN, bool COLVEC> struct Scales {
+    static constexpr int SLOT = 128 + (COLVEC ? BN : 4);           // floats
     __device__ __forceinline__ static void copy4(float *dst, const float *src, bool in)
     {
-        if (in) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
-        else *dst = 0.f;
+        // not there: zeros, without reading
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(in ? 4 : 0) : "memory");
     }
-    __device__ __forceinline__ void issue(const GemmParams &P, int lrows, int bn, int row0, int col0)
+    // every lane of one warp; row0 = first lane row of the tile in this CTA, col0 = its first column
+    __device__ __forceinline__ static void fill(const GemmParams &P, float *s, int kb, int64_t row0, int64_t col0, int lane)
     {
-        if (tile < P.tiles) {
-            float *s = buf + (put % RING) * SLOT;
-            copy4(s + lane, slp + (int64_t)kb * P.pl, row_in);
-            if constexpr (COLVEC) {
+        const float *sl = P.sl + (int64_t)kb * P.pl, *sc = P.sc + (int64_t)kb * P.pc;
 #pragma unroll
-                for (int i = 0; i < (CW + 31) / 32; ++i) {
-                    const int j = i * 32 + lane;
-                    if (j < CW) copy4(s + 32 + j, scp + (int64_t)kb * P.pc + j, j < cols);
-                }
-            } else if (lane == 0) {
-                copy4(s + 32, scp + (int64_t)kb * P.pc, cols > 0);
-            }
-            if (++kb == kb1) { kb = kb0; tile += tile_step; at_tile(P, lrows, bn, row0, col0); }
+        for (int i = 0; i < 4; ++i) {
+            const int64_t row = row0 + i * 32 + lane;
+            const bool in = row < P.rows_l;
+            copy4(s + i * 32 + lane, in ? sl + (P.tile_l ? row / 128 : row) : P.sl, in);
         }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-        ++put;
+        if constexpr (COLVEC) {
+#pragma unroll
+            for (int i = 0; i < (BN + 31) / 32; ++i) {
+                const int j = i * 32 + lane;
+                const bool in = col0 + j < P.rows_c;
+                if (j < BN) copy4(s + 128 + j, in ? sc + col0 + j : P.sc, in);
+            }
+        } else if (lane < (BN + 127) / 128) {
+            const int64_t col = col0 + lane * 128;
+            const bool in = col < P.rows_c;
+            copy4(s + 128 + lane, in ? sc + col / 128 : P.sc, in);
+        }
     }
-    __device__ __forceinline__ void start(const GemmParams &P, float *b, int ln, int64_t t0, int64_t ts, int k0, int k1, int lrows, int bn, int row0, int col0)
+    // arrives on `bar` (count 32) once this lane's copies have landed
+    __device__ __forceinline__ static void arrive(uint32_t bar)
     {
-        buf = b; lane = ln; tile = t0; tile_step = ts; kb = kb0 = k0; kb1 = k1; put = 0;
-        at_tile(P, lrows, bn, row0, col0);
-        for (int i = 0; i < RING - 1; ++i) issue(P, lrows, bn, row0, col0);
-    }
-    // the scales of the n-th block (n counts over all tiles); also keeps the ring filled
-    __device__ __forceinline__ const float *get(const GemmParams &P, uint32_t n, int lrows, int bn, int row0, int col0)
-    {
-        __syncwarp();                                              // every lane is done with the slot that is filled now
-        issue(P, lrows, bn, row0, col0);
-        asm volatile("cp.async.wait_group %0;" ::"n"(RING - 1) : "memory");
-        __syncwarp();
-        return buf + (n % RING) * SLOT;
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
     }
 };
+
+// CW columns of an accumulator row (this thread's lane), times the block's scales, added to `sum`.  `done` is called once
+// everything is in registers.
+template <int CW, bool COLVEC, typename Done>
+__device__ __forceinline__ void promote(float (&sum)[CW], uint32_t taddr, float s, const float *sc, Done done)
+{
+    uint32_t r[2][16];
+    tmem_ld_x16(taddr, r[0]);
+#pragma unroll
+    for (int c = 0; c < CW / 16; ++c) {
+        tmem_ld_wait();
+        if (c + 1 < CW / 16) tmem_ld_x16(taddr + (c + 1) * 16, r[(c + 1) & 1]);
+        else done();
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            float v = __uint_as_float(r[c & 1][j]);
+            if constexpr (COLVEC) v *= sc[c * 16 + j];
+            sum[c * 16 + j] = fmaf(v, s, sum[c * 16 + j]);
+        }
+    }
+}
 
 template <int BN, bool COLVEC>
 __global__ void __launch_bounds__(GemmLayout<BN>::THREADS, 1)
@@ -276,17 +273,19 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constant
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     float *scale_buf = (float *)(smem + STAGES * L::STAGE_BYTES);
     uint64_t *bars = (uint64_t *)(smem + STAGES * L::STAGE_BYTES + L::SCALE_BYTES);
-    uint32_t *tmem_slot = (uint32_t *)(bars + 2 * MAX_STAGES + 2 * MAX_ACC);
+    uint32_t *tmem_slot = (uint32_t *)(bars + 2 * MAX_STAGES + 2 * MAX_ACC + 2 * RING);
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t full0 = smem_u32(bars), empty0 = smem_u32(bars + MAX_STAGES);
     const uint32_t tfull0 = smem_u32(bars + 2 * MAX_STAGES), tempty0 = smem_u32(bars + 2 * MAX_STAGES + MAX_ACC);
+    const uint32_t sfull0 = smem_u32(bars + 2 * MAX_STAGES + 2 * MAX_ACC), sempty0 = sfull0 + 8 * RING;
 
     pdl_launch_dependents();
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
         for (int a = 0; a < NACC; ++a) { mbar_init(tfull0 + 8 * a, 1); mbar_init(tempty0 + 8 * a, L::NEPI); }
+        for (int a = 0; a < RING; ++a) { mbar_init(sfull0 + 8 * a, 32); mbar_init(sempty0 + 8 * a, L::NEPI); }
         *abort_flag = 0;
         mbar_init_fence();
     }
@@ -348,44 +347,47 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constant
             }
         }
         __syncwarp();
+    } else if (warp == 2) {
+        // ------------------------------------------------------------------ scales
+        uint32_t n = 0;
+        bool ok = true;
+        for (int64_t tile = tile0; tile < P.tiles && ok; tile += tile_step) {
+            const int64_t row0 = (tile / P.nc) * 128, col0 = (tile % P.nc) * BN;
+            for (int kb = kb0; kb < kb1; ++kb, ++n) {
+                const uint32_t slot = n % RING;
+                ok = __all_sync(0xffffffffu, mbar_wait(sempty0 + 8 * slot, ((n / RING) & 1) ^ 1, abort_flag));
+                if (!ok) break;
+                Scales<BN, COLVEC>::fill(P, scale_buf + slot * Scales<BN, COLVEC>::SLOT, kb, row0, col0, lane);
+                Scales<BN, COLVEC>::arrive(sfull0 + 8 * slot);
+            }
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
     } else {
         // ------------------------------------------------------------------ promotion
-        const int q = warp & 3, half = (warp - 2) >> 2;                    // lane quarter and column part of this warp
+        const int q = warp & 3, half = (warp - 3) >> 2;                    // lane quarter and column part of this warp
         const int lane_row = q * 32 + lane;
-        ScaleRing<CW, COLVEC> scales;
-        scales.start(P, scale_buf + (warp - 2) * RING * (32 + CW), lane, tile0, tile_step, kb0, kb1, 128, BN, q * 32, half * CW);
-        uint32_t block = 0;
-        uint32_t acc = 0, acc_phase = 0;
+        uint32_t acc = 0, acc_phase = 0, n = 0;
         bool ok = true;
         for (int64_t tile = tile0; tile < P.tiles; tile += tile_step) {
             const int64_t row = (tile / P.nc) * 128 + lane_row;
-            const int col0 = (int)(tile % P.nc) * BN, cbase = col0 + half * CW;
-            f32x2 sum[CW / 2];
+            const int cbase = (int)(tile % P.nc) * BN + half * CW;
+            float sum[CW];
 #pragma unroll
-            for (int i = 0; i < CW / 2; ++i) sum[i] = 0ull;
-            for (int kb = kb0; kb < kb1; ++kb) {
-                const float *sv = scales.get(P, block++, 128, BN, q * 32, half * CW), *sb = sv + 32;
-                const f32x2 s2 = twice(COLVEC ? sv[lane] : sv[lane] * sb[0]);
+            for (int i = 0; i < CW; ++i) sum[i] = 0.f;
+            for (int kb = kb0; kb < kb1; ++kb, ++n) {
+                const uint32_t slot = n % RING;
+                const float *sv = scale_buf + slot * Scales<BN, COLVEC>::SLOT, *sc = sv + 128 + (COLVEC ? half * CW : half * CW / 128);
+                ok = ok && __all_sync(0xffffffffu, mbar_wait(sfull0 + 8 * slot, (n / RING) & 1, abort_flag));
                 ok = ok && __all_sync(0xffffffffu, mbar_wait(tfull0 + 8 * acc, acc_phase, abort_flag));
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t trow = tmem_base + ((uint32_t)(q * 32) << 16) + acc * BN + half * CW;
-                uint32_t r[2][16];
-                tmem_ld_x16(trow, r[0]);
-#pragma unroll
-                for (int c = 0; c < CW / 16; ++c) {
-                    tmem_ld_wait();
-                    if (c + 1 < CW / 16) tmem_ld_x16(trow + (c + 1) * 16, r[(c + 1) & 1]);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        f32x2 v = pack2(r[c & 1][2 * j], r[c & 1][2 * j + 1]);
-                        if constexpr (COLVEC) v = mul2(v, *reinterpret_cast<const f32x2 *>(sb + c * 16 + 2 * j));
-                        sum[c * 8 + j] = fma2(v, s2, sum[c * 8 + j]);
-                    }
-                }
-                tc_fence_before();
+                promote<CW, COLVEC>(sum, tmem_base + ((uint32_t)(q * 32) << 16) + acc * BN + half * CW, COLVEC ? sv[lane_row] : sv[lane_row] * sc[0], sc, [&]() {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(tempty0 + 8 * acc);
+                });
                 __syncwarp();
-                if (lane == 0) mbar_arrive(tempty0 + 8 * acc);
+                if (lane == 0) mbar_arrive(sempty0 + 8 * slot);
                 if (++acc == NACC) { acc = 0; acc_phase ^= 1; }
             }
             if (S == 1) {
@@ -394,19 +396,14 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constant
                 for (int c = 0; c < CW / 16; ++c) {
                     float v[16];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) unpack2(sum[c * 8 + j], v[2 * j], v[2 * j + 1]);
+                    for (int j = 0; j < 16; ++j) v[j] = sum[c * 16 + j];
                     finish<16>(P, row, cbase + c * 16, v);
                 }
             } else {
                 // every stage of this CTA has been read: its memory takes the parts, [column][lane row]
                 float *part = (float *)smem;
 #pragma unroll
-                for (int j = 0; j < CW / 2; ++j) {
-                    float a, b;
-                    unpack2(sum[j], a, b);
-                    part[(half * CW + 2 * j) * 128 + lane_row] = a;
-                    part[(half * CW + 2 * j + 1) * 128 + lane_row] = b;
-                }
+                for (int j = 0; j < CW; ++j) part[(half * CW + j) * 128 + lane_row] = sum[j];
             }
         }
         if (!ok) {
@@ -417,8 +414,8 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constant
     __syncwarp();
     if (S > 1) {
         cluster_sync_all();
-        if (warp >= 2) {
-            const int q = warp & 3, half = (warp - 2) >> 2, lane_row = q * 32 + lane;
+        if (warp >= 3) {
+            const int q = warp & 3, half = (warp - 3) >> 2, lane_row = q * 32 + lane;
             const int64_t row = (tile0 / P.nc) * 128 + lane_row;
             const int col0 = (int)(tile0 % P.nc) * BN;
             const uint32_t base = smem_u32(smem);
@@ -461,8 +458,8 @@ template <int BN> struct PairLayout {
     static constexpr int NACC = BN == 256 ? 2 : 4;
     static constexpr int CW = BN / 2;                             // columns per promotion warp
     static constexpr int THREADS = 384, TMEM_COLS = 512;
-    static constexpr int SCALE_BYTES = 8 * RING * (32 + CW) * 4;
-    static constexpr int BAR_BYTES = (2 * MAX_STAGES + 2 * MAX_ACC) * 8 + 16;
+    static constexpr int SCALE_BYTES = RING * (128 + BN) * 4;
+    static constexpr int BAR_BYTES = (2 * MAX_STAGES + 2 * MAX_ACC + 2 * RING) * 8 + 16;
     static constexpr int TOTAL = 1024 + STAGES * STAGE_BYTES + SCALE_BYTES + BAR_BYTES;
     static_assert(TOTAL <= 227 * 1024 && STAGES <= MAX_STAGES && NACC <= MAX_ACC && NACC * BN <= TMEM_COLS, "");
 };
@@ -509,18 +506,20 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     float *scale_buf = (float *)(smem + STAGES * L::STAGE_BYTES);
     uint64_t *bars = (uint64_t *)(smem + STAGES * L::STAGE_BYTES + L::SCALE_BYTES);
-    uint32_t *tmem_slot = (uint32_t *)(bars + 2 * MAX_STAGES + 2 * MAX_ACC);
+    uint32_t *tmem_slot = (uint32_t *)(bars + 2 * MAX_STAGES + 2 * MAX_ACC + 2 * RING);
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     const uint32_t full0 = smem_u32(bars), empty0 = smem_u32(bars + MAX_STAGES);
     const uint32_t tfull0 = smem_u32(bars + 2 * MAX_STAGES), tempty0 = smem_u32(bars + 2 * MAX_STAGES + MAX_ACC);
+    const uint32_t sfull0 = smem_u32(bars + 2 * MAX_STAGES + 2 * MAX_ACC), sempty0 = sfull0 + 8 * RING;
 
     pdl_launch_dependents();
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
         for (int a = 0; a < NACC; ++a) { mbar_init(tfull0 + 8 * a, 1); mbar_init(tempty0 + 8 * a, 16); }
+        for (int a = 0; a < RING; ++a) { mbar_init(sfull0 + 8 * a, 32); mbar_init(sempty0 + 8 * a, 8); }
         *abort_flag = 0;
         mbar_init_fence();
     }
@@ -576,50 +575,49 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
                 }
             }
         }
+        else if (warp == 3) {
+            // -------------------------------------------------------------- scales
+            uint32_t n = 0;
+            for (int64_t tile = tile0; tile < P.tiles && ok; tile += tile_step) {
+                const int64_t row0 = (tile / P.nc) * 256 + rank * 128, col0 = (tile % P.nc) * BN;
+                for (int kb = 0; kb < P.kblocks; ++kb, ++n) {
+                    const uint32_t slot = n % RING;
+                    ok = __all_sync(0xffffffffu, mbar_wait(sempty0 + 8 * slot, ((n / RING) & 1) ^ 1, abort_flag));
+                    if (!ok) break;
+                    Scales<BN, COLVEC>::fill(P, scale_buf + slot * Scales<BN, COLVEC>::SLOT, kb, row0, col0, lane);
+                    Scales<BN, COLVEC>::arrive(sfull0 + 8 * slot);
+                }
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");
+        }
         __syncwarp();
     } else {
         // ------------------------------------------------------------------ promotion
         asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         const int q = warp & 3, half = (warp - 4) >> 2;
         const int lane_row = q * 32 + lane;
-        const int row0 = (int)rank * 128 + q * 32;
-        ScaleRing<CW, COLVEC> scales;
-        scales.start(P, scale_buf + (warp - 4) * RING * (32 + CW), lane, tile0, tile_step, 0, P.kblocks, 256, BN, row0, half * CW);
-        uint32_t block = 0;
-        uint32_t acc = 0, acc_phase = 0;
+        uint32_t acc = 0, acc_phase = 0, n = 0;
         const uint32_t tempty_leader = map_to_rank(tempty0, 0);
         for (int64_t tile = tile0; tile < P.tiles && ok; tile += tile_step) {
             const int64_t row = (tile / P.nc) * 256 + rank * 128 + lane_row;
             const int cbase = (int)(tile % P.nc) * BN + half * CW;
-            f32x2 sum[CW / 2];
+            float sum[CW];
 #pragma unroll
-            for (int i = 0; i < CW / 2; ++i) sum[i] = 0ull;
-            for (int kb = 0; kb < P.kblocks; ++kb) {
-                const float *sv = scales.get(P, block++, 256, BN, row0, half * CW), *sb = sv + 32;
-                const f32x2 s2 = twice(COLVEC ? sv[lane] : sv[lane] * sb[0]);
-                ok = __all_sync(0xffffffffu, mbar_wait(tfull0 + 8 * acc, acc_phase, abort_flag));
+            for (int i = 0; i < CW; ++i) sum[i] = 0.f;
+            for (int kb = 0; kb < P.kblocks; ++kb, ++n) {
+                const uint32_t slot = n % RING;
+                const float *sv = scale_buf + slot * Scales<BN, COLVEC>::SLOT, *sc = sv + 128 + (COLVEC ? half * CW : half * CW / 128);
+                ok = __all_sync(0xffffffffu, mbar_wait(sfull0 + 8 * slot, (n / RING) & 1, abort_flag));
+                ok = ok && __all_sync(0xffffffffu, mbar_wait(tfull0 + 8 * acc, acc_phase, abort_flag));
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t trow = tmem_base + ((uint32_t)(q * 32) << 16) + acc * BN + half * CW;
-                uint32_t r[2][32];
-                tmem_ld32(trow, r[0]);
-#pragma unroll
-                for (int c = 0; c < CW / 32; ++c) {
-                    tmem_ld_wait();
-                    if (c + 1 < CW / 32) {
-                        tmem_ld32(trow + (c + 1) * 32, r[(c + 1) & 1]);
-                    } else {                                       // everything is in registers: the accumulator is free
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive_cluster(tempty_leader + 8 * acc);
-                    }
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        f32x2 v = pack2(r[c & 1][2 * j], r[c & 1][2 * j + 1]);
-                        if constexpr (COLVEC) v = mul2(v, *reinterpret_cast<const f32x2 *>(sb + c * 32 + 2 * j));
-                        sum[c * 16 + j] = fma2(v, s2, sum[c * 16 + j]);
-                    }
-                }
+                promote<CW, COLVEC>(sum, tmem_base + ((uint32_t)(q * 32) << 16) + acc * BN + half * CW, COLVEC ? sv[lane_row] : sv[lane_row] * sc[0], sc, [&]() {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(tempty_leader + 8 * acc);
+                });
+                __syncwarp();
+                if (lane == 0) mbar_arrive(sempty0 + 8 * slot);
                 if (++acc == NACC) { acc = 0; acc_phase ^= 1; }
             }
             if (!ok) break;
@@ -627,7 +625,7 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
             for (int c = 0; c < CW / 16; ++c) {
                 float v[16];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) unpack2(sum[c * 8 + j], v[2 * j], v[2 * j + 1]);
+                for (int j = 0; j < 16; ++j) v[j] = sum[c * 16 + j];
                 finish<16>(P, row, cbase + c * 16, v);
             }
         }
