@@ -52,7 +52,9 @@ template <int BN> struct GemmLayout {
     static constexpr int NACC = 4;
     static constexpr int NEPI = BN >= 64 ? 8 : 4;                 // promotion warps
     static constexpr int CW = BN >= 64 ? BN / 2 : BN;             // columns per promotion warp
-    static constexpr int THREADS = 96 + 32 * NEPI;                // + TMA, MMA and scale warps
+    static constexpr int ISSUERS = BN >= 64 ? 2 : 1;              // MMA-issuing threads; narrower tiles wait for memory
+    static constexpr int THREADS = (2 + ISSUERS + NEPI) * 32;     // TMA, MMA, scales, promotion
+    static constexpr int EPI0 = 2 + ISSUERS;                      // first promotion warp
     static constexpr int TMEM_COLS = NACC * BN;                   // 64 .. 512, a power of two
     static constexpr int SCALE_BYTES = RING * (128 + (BN)) * 4;
     static constexpr int BAR_BYTES = (2 * MAX_STAGES + 2 * MAX_ACC + 2 * RING) * 8 + 16;
@@ -180,21 +182,23 @@ __device__ __forceinline__ void finish(const GemmParams &P, int64_t row, int col
     }
 }
 
-// Sum over the cluster's parts of CW / S columns of this thread's lane row, and their store.
+// Sum over the S parts of a tile (in CTAs first, first + stride, ... of the cluster) of the `mine`-th CW / S columns of this
+// thread's lane row, and their store.
 template <int CW, int S>
-__device__ __forceinline__ void reduce_parts(const GemmParams &P, uint32_t part_base, int lane_row, int64_t row, int col_local, int col0, uint32_t rank)
+__device__ __forceinline__ void reduce_parts(const GemmParams &P, uint32_t part_base, int lane_row, int64_t row, int col_local, int col0, uint32_t mine,
+                                             uint32_t first, uint32_t stride)
 {
     constexpr int CWS = CW / S, CH = CWS < 16 ? CWS : 16;
 #pragma unroll 1
     for (int j0 = 0; j0 < CWS; j0 += CH) {
-        const int cl = col_local + (int)rank * CWS + j0;
+        const int cl = col_local + (int)mine * CWS + j0;
         float v[CH];
 #pragma unroll
         for (int j = 0; j < CH; ++j) v[j] = 0.f;
 #pragma unroll
         for (int s = 0; s < S; ++s)
 #pragma unroll
-            for (int j = 0; j < CH; ++j) v[j] += ld_peer_f32(part_base + ((cl + j) * 128 + lane_row) * 4, s);
+            for (int j = 0; j < CH; ++j) v[j] += ld_peer_f32(part_base + ((cl + j) * 128 + lane_row) * 4, first + s * stride);
         finish<CH>(P, row, col0 + cl, v);
     }
 }
@@ -253,10 +257,16 @@ __device__ __forceinline__ void promote(float (&sum)[CW], uint32_t taddr, float 
         if (c + 1 < CW / 16) tmem_ld_x16(taddr + (c + 1) * 16, r[(c + 1) & 1]);
         else done();
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            float v = __uint_as_float(r[c & 1][j]);
-            if constexpr (COLVEC) v *= sc[c * 16 + j];
-            sum[c * 16 + j] = fmaf(v, s, sum[c * 16 + j]);
+        for (int j = 0; j < 16; j += 4) {
+            float v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(r[c & 1][j + i]);
+            if constexpr (COLVEC) {
+                const float4 w = *reinterpret_cast<const float4 *>(sc + c * 16 + j);
+                v[0] *= w.x; v[1] *= w.y; v[2] *= w.z; v[3] *= w.w;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[c * 16 + j + i] = fmaf(v[i], s, sum[c * 16 + j + i]);
         }
     }
 }
@@ -323,31 +333,30 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constant
             }
         }
         __syncwarp();
-    } else if (warp == 1) {
-        // ------------------------------------------------------------------ MMA issuer
+    } else if (warp <= L::ISSUERS) {
+        // ------------------------------------------------------------------ MMA issuers, for every ISSUERS-th block
         if (lane == 0) {
-            int stage = 0;
-            uint32_t phase = 0, acc = 0, acc_phase = 0;
-            bool ok = true;
-            for (int64_t tile = tile0; tile < P.tiles && ok; tile += tile_step) {
-                for (int kb = kb0; kb < kb1; ++kb) {
-                    if (!mbar_wait(tempty0 + 8 * acc, acc_phase ^ 1, abort_flag)) { ok = false; break; }
-                    if (!mbar_wait(full0 + 8 * stage, phase, abort_flag)) { ok = false; break; }
-                    tc_fence_after();
-                    const uint32_t sa = smem_u32(smem + stage * L::STAGE_BYTES);
-                    const uint64_t da = make_desc(sa, 0, 8 * KB, 2), dc = make_desc(sa + L::A_BYTES, 0, 8 * KB, 2);
+            constexpr int NI = L::ISSUERS;
+            const int64_t mine = tile0 < P.tiles ? (P.tiles - tile0 + tile_step - 1) / tile_step * (kb1 - kb0) : 0;
+            int stage = (warp - 1) % STAGES;
+            uint32_t phase = 0, acc = warp - 1, acc_phase = 0;
+            for (int64_t n = warp - 1; n < mine; n += NI) {
+                if (!mbar_wait(tempty0 + 8 * acc, acc_phase ^ 1, abort_flag)) break;
+                if (!mbar_wait(full0 + 8 * stage, phase, abort_flag)) break;
+                tc_fence_after();
+                const uint32_t sa = smem_u32(smem + stage * L::STAGE_BYTES);
+                const uint64_t da = make_desc(sa, 0, 8 * KB, 2), dc = make_desc(sa + L::A_BYTES, 0, 8 * KB, 2);
 #pragma unroll
-                    for (int k = 0; k < KB / 32; ++k)        // 32 codes = 32 bytes = 2 descriptor address units
-                        umma_fp8(tmem_base + acc * BN, da + 2 * k, dc + 2 * k, IDESC, k ? 1u : 0u);
-                    umma_commit(empty0 + 8 * stage);         // frees the stage once these MMAs have read it
-                    umma_commit(tfull0 + 8 * acc);           // the block's sums are complete
-                    if (++stage == STAGES) { stage = 0; phase ^= 1; }
-                    if (++acc == NACC) { acc = 0; acc_phase ^= 1; }
-                }
+                for (int k = 0; k < KB / 32; ++k)            // 32 codes = 32 bytes = 2 descriptor address units
+                    umma_fp8(tmem_base + acc * BN, da + 2 * k, dc + 2 * k, IDESC, k ? 1u : 0u);
+                umma_commit(empty0 + 8 * stage);             // frees the stage once these MMAs have read it
+                umma_commit(tfull0 + 8 * acc);               // the block's sums are complete
+                if ((stage += NI) >= STAGES) { stage -= STAGES; phase ^= 1; }
+                if ((acc += NI) >= NACC) { acc -= NACC; acc_phase ^= 1; }
             }
         }
         __syncwarp();
-    } else if (warp == 2) {
+    } else if (warp == L::ISSUERS + 1) {
         // ------------------------------------------------------------------ scales
         uint32_t n = 0;
         bool ok = true;
@@ -364,7 +373,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constant
         asm volatile("cp.async.wait_all;" ::: "memory");
     } else {
         // ------------------------------------------------------------------ promotion
-        const int q = warp & 3, half = (warp - 3) >> 2;                    // lane quarter and column part of this warp
+        const int q = warp & 3, half = (warp - L::EPI0) >> 2;              // lane quarter and column part of this warp
         const int lane_row = q * 32 + lane;
         uint32_t acc = 0, acc_phase = 0, n = 0;
         bool ok = true;
@@ -414,14 +423,14 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constant
     __syncwarp();
     if (S > 1) {
         cluster_sync_all();
-        if (warp >= 3) {
-            const int q = warp & 3, half = (warp - 3) >> 2, lane_row = q * 32 + lane;
+        if (warp >= L::EPI0) {
+            const int q = warp & 3, half = (warp - L::EPI0) >> 2, lane_row = q * 32 + lane;
             const int64_t row = (tile0 / P.nc) * 128 + lane_row;
             const int col0 = (int)(tile0 % P.nc) * BN;
             const uint32_t base = smem_u32(smem);
-            if (S == 2) reduce_parts<CW, 2>(P, base, lane_row, row, half * CW, col0, rank);
-            else if (S == 4) reduce_parts<CW, 4>(P, base, lane_row, row, half * CW, col0, rank);
-            else reduce_parts<CW, 8>(P, base, lane_row, row, half * CW, col0, rank);
+            if (S == 2) reduce_parts<CW, 2>(P, base, lane_row, row, half * CW, col0, rank, 0, 1);
+            else if (S == 4) reduce_parts<CW, 4>(P, base, lane_row, row, half * CW, col0, rank, 0, 1);
+            else reduce_parts<CW, 8>(P, base, lane_row, row, half * CW, col0, rank, 0, 1);
         }
         cluster_sync_all();      // no CTA leaves while a peer still reads its parts
     }
@@ -480,11 +489,11 @@ __device__ __forceinline__ void umma_fp8_pair(uint32_t d_tmem, uint64_t adesc, u
     asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n}"
                  ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
 }
-// arrives on the barrier of this offset in both CTAs once the MMAs issued so far have completed
-__device__ __forceinline__ void umma_commit_pair(uint32_t bar)
+// arrives on the barrier of this offset in the CTAs of the mask once the MMAs issued so far have completed
+__device__ __forceinline__ void umma_commit_pair(uint32_t bar, uint32_t ctas)
 {
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                 ::"r"(bar), "h"((uint16_t)3) : "memory");
+                 ::"r"(bar), "h"((uint16_t)ctas) : "memory");
 }
 // Arrival on a barrier of either CTA.  No release at cluster scope: what it hands over is tensor memory that has been read,
 // not memory that was written, and that release is a fence that waits for everything the thread has in flight - it took
@@ -510,7 +519,9 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t rank = cluster_rank();
+    // a cluster is S pairs that share the blocks of k of one tile; the even CTA of a pair leads it
+    const uint32_t cta = cluster_rank(), rank = cta & 1, leader = cta & ~1u;
+    const int S = P.splits;
     const uint32_t full0 = smem_u32(bars), empty0 = smem_u32(bars + MAX_STAGES);
     const uint32_t tfull0 = smem_u32(bars + 2 * MAX_STAGES), tempty0 = smem_u32(bars + 2 * MAX_STAGES + MAX_ACC);
     const uint32_t sfull0 = smem_u32(bars + 2 * MAX_STAGES + 2 * MAX_ACC), sempty0 = sfull0 + 8 * RING;
@@ -533,7 +544,8 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
     cluster_sync_all();          // the peer's barriers exist
     pdl_wait();                  // everything above touched shared and tensor memory only
     const uint32_t tmem_base = *tmem_slot;
-    const int64_t tile0 = blockIdx.x >> 1, tile_step = gridDim.x >> 1;
+    const int64_t tile0 = S > 1 ? blockIdx.x / (2 * S) : blockIdx.x >> 1, tile_step = S > 1 ? P.tiles : gridDim.x >> 1;
+    const int split = (int)(cta >> 1), kb0 = (int)((int64_t)P.kblocks * split / S), kb1 = (int)((int64_t)P.kblocks * (split + 1) / S);
     bool ok = true;
 
     if (warp < 4) {
@@ -544,9 +556,9 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
             uint32_t phase = 0;
             for (int64_t tile = tile0; tile < P.tiles && ok; tile += tile_step) {
                 const int l0 = (int)(tile / P.nc) * 256 + (int)rank * 128, c0 = (int)(tile % P.nc) * BN + (int)rank * (BN / 2);
-                for (int kb = 0; kb < P.kblocks; ++kb) {
+                for (int kb = kb0; kb < kb1; ++kb) {
                     if (!mbar_wait(empty0 + 8 * stage, phase ^ 1, abort_flag)) { ok = false; break; }
-                    const uint32_t fb = map_to_rank(full0 + 8 * stage, 0);
+                    const uint32_t fb = map_to_rank(full0 + 8 * stage, leader);
                     if (rank == 0) mbar_expect_tx(full0 + 8 * stage, 2 * L::STAGE_BYTES);
                     const uint32_t sa = smem_u32(smem + stage * L::STAGE_BYTES);
                     tma_load_2d_pair(sa, &map_l, fb, kb * KB, l0);
@@ -554,25 +566,26 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
                     if (++stage == STAGES) { stage = 0; phase ^= 1; }
                 }
             }
-        } else if (warp == 1 && lane == 0 && rank == 0) {
-            // -------------------------------------------------------------- MMA issuer, in the leader
-            int stage = 0;
-            uint32_t phase = 0, acc = 0, acc_phase = 0;
-            for (int64_t tile = tile0; tile < P.tiles && ok; tile += tile_step) {
-                for (int kb = 0; kb < P.kblocks; ++kb) {
-                    if (!mbar_wait(tempty0 + 8 * acc, acc_phase ^ 1, abort_flag)) { ok = false; break; }
-                    if (!mbar_wait(full0 + 8 * stage, phase, abort_flag)) { ok = false; break; }
-                    tc_fence_after();
-                    const uint32_t sa = smem_u32(smem + stage * L::STAGE_BYTES);
-                    const uint64_t da = make_desc(sa, 0, 8 * KB, 2), dc = make_desc(sa + L::A_BYTES, 0, 8 * KB, 2);
+        } else if ((warp == 1 || warp == 2) && lane == 0 && rank == 0) {
+            // -------------------------------------------------------------- MMA issuers, in the leader
+            // Two, for alternate blocks: one thread takes about 120 cycles per MMA to issue and 300 for the two waits of a
+            // block, 780 together where the tensor cores need 512.
+            const int64_t mine = tile0 < P.tiles ? (P.tiles - tile0 + tile_step - 1) / tile_step * (kb1 - kb0) : 0;
+            int stage = warp - 1;
+            uint32_t phase = 0, acc = warp - 1, acc_phase = 0;
+            for (int64_t n = warp - 1; n < mine; n += 2) {
+                if (!mbar_wait(tempty0 + 8 * acc, acc_phase ^ 1, abort_flag)) { ok = false; break; }
+                if (!mbar_wait(full0 + 8 * stage, phase, abort_flag)) { ok = false; break; }
+                tc_fence_after();
+                const uint32_t sa = smem_u32(smem + stage * L::STAGE_BYTES);
+                const uint64_t da = make_desc(sa, 0, 8 * KB, 2), dc = make_desc(sa + L::A_BYTES, 0, 8 * KB, 2);
 #pragma unroll
-                    for (int k = 0; k < KB / 32; ++k)
-                        umma_fp8_pair(tmem_base + acc * BN, da + 2 * k, dc + 2 * k, IDESC, k ? 1u : 0u);
-                    umma_commit_pair(empty0 + 8 * stage);
-                    umma_commit_pair(tfull0 + 8 * acc);
-                    if (++stage == STAGES) { stage = 0; phase ^= 1; }
-                    if (++acc == NACC) { acc = 0; acc_phase ^= 1; }
-                }
+                for (int k = 0; k < KB / 32; ++k)
+                    umma_fp8_pair(tmem_base + acc * BN, da + 2 * k, dc + 2 * k, IDESC, k ? 1u : 0u);
+                umma_commit_pair(empty0 + 8 * stage, 3u << leader);
+                umma_commit_pair(tfull0 + 8 * acc, 3u << leader);
+                if ((stage += 2) >= STAGES) { stage -= STAGES; phase ^= 1; }
+                if ((acc += 2) >= NACC) { acc -= NACC; acc_phase ^= 1; }
             }
         }
         else if (warp == 3) {
@@ -580,7 +593,7 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
             uint32_t n = 0;
             for (int64_t tile = tile0; tile < P.tiles && ok; tile += tile_step) {
                 const int64_t row0 = (tile / P.nc) * 256 + rank * 128, col0 = (tile % P.nc) * BN;
-                for (int kb = 0; kb < P.kblocks; ++kb, ++n) {
+                for (int kb = kb0; kb < kb1; ++kb, ++n) {
                     const uint32_t slot = n % RING;
                     ok = __all_sync(0xffffffffu, mbar_wait(sempty0 + 8 * slot, ((n / RING) & 1) ^ 1, abort_flag));
                     if (!ok) break;
@@ -597,14 +610,14 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
         const int q = warp & 3, half = (warp - 4) >> 2;
         const int lane_row = q * 32 + lane;
         uint32_t acc = 0, acc_phase = 0, n = 0;
-        const uint32_t tempty_leader = map_to_rank(tempty0, 0);
+        const uint32_t tempty_leader = map_to_rank(tempty0, leader);
         for (int64_t tile = tile0; tile < P.tiles && ok; tile += tile_step) {
             const int64_t row = (tile / P.nc) * 256 + rank * 128 + lane_row;
             const int cbase = (int)(tile % P.nc) * BN + half * CW;
             float sum[CW];
 #pragma unroll
             for (int i = 0; i < CW; ++i) sum[i] = 0.f;
-            for (int kb = 0; kb < P.kblocks; ++kb, ++n) {
+            for (int kb = kb0; kb < kb1; ++kb, ++n) {
                 const uint32_t slot = n % RING;
                 const float *sv = scale_buf + slot * Scales<BN, COLVEC>::SLOT, *sc = sv + 128 + (COLVEC ? half * CW : half * CW / 128);
                 ok = __all_sync(0xffffffffu, mbar_wait(sfull0 + 8 * slot, (n / RING) & 1, abort_flag));
@@ -620,6 +633,13 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
                 if (lane == 0) mbar_arrive(sempty0 + 8 * slot);
                 if (++acc == NACC) { acc = 0; acc_phase ^= 1; }
             }
+            if (S > 1) {
+                // every stage has been read: its memory takes the parts, [column][lane row]
+                float *part = (float *)smem;
+#pragma unroll
+                for (int j = 0; j < CW; ++j) part[(half * CW + j) * 128 + lane_row] = sum[j];
+                break;
+            }
             if (!ok) break;
 #pragma unroll
             for (int c = 0; c < CW / 16; ++c) {
@@ -633,6 +653,17 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
     if (!ok) {
         if (P.status) atomicExch(P.status, (int)LAMP_ERR_TIMEOUT);
         settle();                                                  // copies in flight
+    }
+    if (S > 1) {
+        cluster_sync_all();
+        if (warp >= 4) {
+            const int q = warp & 3, half = (warp - 4) >> 2, lane_row = q * 32 + lane;
+            const int64_t row = (tile0 / P.nc) * 256 + rank * 128 + lane_row;
+            const int col0 = (int)(tile0 % P.nc) * BN;
+            const uint32_t base = smem_u32(smem);
+            if (S == 2) reduce_parts<CW, 2>(P, base, lane_row, row, half * CW, col0, split, rank, 2);
+            else reduce_parts<CW, 4>(P, base, lane_row, row, half * CW, col0, split, rank, 2);
+        }
     }
     tc_fence_before();
     __syncthreads();
@@ -649,19 +680,19 @@ lamp_status_t launch_pair(const lamp_fp8_operand_t *l, const lamp_fp8_operand_t 
     if (!encode_operand(l, 128, &ml) || !encode_operand(c, BN / 2, &mc)) return LAMP_ERR_CUDA;
     static SmemAttrOnce attr;
     { const lamp_status_t as = attr.ensure(fp8_gemm_pair_kernel<BN, COLVEC>, (int)L::TOTAL); if (as != LAMP_OK) return as; }
-    const int pairs = sm_count() / 2;
+    const int64_t pairs = sm_count() / 2;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(2 * (unsigned)(P.tiles < pairs ? P.tiles : pairs));
+    cfg.gridDim = dim3(2 * (unsigned)(P.splits > 1 ? P.tiles * P.splits : P.tiles < pairs ? P.tiles : pairs));
     cfg.blockDim = dim3(L::THREADS);
     cfg.dynamicSmemBytes = L::TOTAL;
     cfg.stream = st;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = 2; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+    at[0].val.clusterDim.x = 2 * P.splits; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
     at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
-    cfg.numAttrs = P.tiles <= 4 * (int64_t)pairs ? 2 : 1;
+    cfg.numAttrs = P.tiles <= 4 * pairs ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, fp8_gemm_pair_kernel<BN, COLVEC>, ml, mc, P) == cudaSuccess ? LAMP_OK : LAMP_ERR_CUDA;
 }
 
@@ -701,6 +732,11 @@ lamp_status_t launch_cv(const lamp_fp8_operand_t *l, const lamp_fp8_operand_t *c
 {
     return c->tile_scale ? launch<BN, false>(l, c, P, st) : launch<BN, true>(l, c, P, st);
 }
+
+// Clusters of `ctas` CTAs, one CTA per SM, that run at once: the SMs of a cluster belong to one GPC, so not every SM finds a
+// place.  (148 SMs: 74 clusters of 2, 33 of 4, 15 of 8; one cluster more than that is a second wave - 141 us against 71 for a
+// weight gradient of 512 x 2048 outputs.)
+int64_t cluster_room(int sms, int ctas) { return ctas <= 2 ? sms / ctas : ctas == 4 ? sms * 2 / 9 : sms / 10; }
 
 }  // namespace
 
@@ -750,7 +786,11 @@ extern "C" lamp_status_t lamp_gemm_fp8(const lamp_fp8_operand_t *a, const lamp_f
     // pairs where their tiles fill the GPU
     for (int bn = 256; bn >= 128; bn /= 2) {
         const int64_t nl = (P.rows_l + 255) / 256, nc = (P.rows_c + bn - 1) / bn;
-        if (swap || P.rows_c < bn || nl * nc * 2 < sms) continue;
+        if (swap || P.rows_c < bn) continue;
+        int splits = 1;
+        if (nl * nc <= cluster_room(sms, 4) && P.kblocks >= 16) splits = 2;
+        if (nl * nc * splits * 2 < sms * 3 / 4) continue;
+        P.splits = splits;
         P.nl = (int32_t)nl; P.nc = (int32_t)nc; P.tiles = nl * nc;
         if (bn == 256) return c->tile_scale ? launch_pair<256, false>(l, c, P, st) : launch_pair<256, true>(l, c, P, st);
         return c->tile_scale ? launch_pair<128, false>(l, c, P, st) : launch_pair<128, true>(l, c, P, st);
@@ -758,7 +798,7 @@ extern "C" lamp_status_t lamp_gemm_fp8(const lamp_fp8_operand_t *a, const lamp_f
     const int bn = P.rows_c <= 16 ? 16 : P.rows_c <= 32 ? 32 : P.rows_c <= 64 ? 64 : 128;
     P.nc = (P.rows_c + bn - 1) / bn;
     P.tiles = (int64_t)P.nl * P.nc;
-    while (P.splits < 8 && P.tiles * P.splits * 2 <= sms && P.kblocks >= 4 * P.splits) P.splits *= 2;
+    while (P.splits < 8 && P.tiles <= cluster_room(sms, 2 * P.splits) && P.kblocks >= 4 * P.splits) P.splits *= 2;
     switch (bn) {
     case 16: return launch_cv<16>(l, c, P, st);
     case 32: return launch_cv<32>(l, c, P, st);

@@ -66,7 +66,7 @@ def test_product_matches_oracle(m, n, k, out):
         check(y.view(m, n), a, b, bias, out)
 
 
-@pytest.mark.parametrize("m,n,tile", [(2500, 2100, True), (2500, 2100, False), (4000, 300, True), (9600, 520, False)])
+@pytest.mark.parametrize("m,n,tile", [(2500, 2100, True), (2500, 2100, False), (4000, 300, True), (9600, 520, False), (5000, 130, True)])
 def test_product_over_many_tiles(m, n, tile):
     # more tiles than SMs: the persistent walk, both scale kinds, an edge in both directions
     r = np.random.default_rng(5)
@@ -76,6 +76,19 @@ def test_product_over_many_tiles(m, n, tile):
     B.lamp_gemm_fp8(oa, ob, y)
     assert B.lamp_get_async_status() == 0
     check(y.view(m, n), a, b, None, torch.float32)
+
+
+@pytest.mark.parametrize("m,n,k,ta,tb", [(500, 2000, 9000, False, False), (300, 1200, 5000, True, True), (1100, 1000, 2100, False, True), (260, 600, 7001, False, False),
+                                         (1024, 1024, 2048, True, False)])
+def test_long_reductions_are_shared_between_the_ctas_of_a_cluster(m, n, k, ta, tb):
+    r = np.random.default_rng(6)
+    oa, a = operand(r, m, k, ta)
+    ob, b = operand(r, n, k, tb)
+    for out in (torch.float32, torch.bfloat16):
+        y = torch.empty((1, 1, 1, m, n), dtype=out, device="cuda")
+        B.lamp_gemm_fp8(oa, ob, y)
+        assert B.lamp_get_async_status() == 0
+        check(y.view(m, n), a, b, None, out)
 
 
 @pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
