@@ -258,15 +258,14 @@ __device__ __forceinline__ void promote(float (&sum)[CW], uint32_t taddr, float 
         else done();
 #pragma unroll
         for (int j = 0; j < 16; j += 4) {
-            float v[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(r[c & 1][j + i]);
-            if constexpr (COLVEC) {
-                const float4 w = *reinterpret_cast<const float4 *>(sc + c * 16 + j);
-                v[0] *= w.x; v[1] *= w.y; v[2] *= w.z; v[3] *= w.w;
+            float w[4] = {s, s, s, s};
+            if constexpr (COLVEC) {                                // products of scales two at a time (61 us on the 512 x 2048 weight gradient, 64 one by one)
+                const ulonglong2 cs = *reinterpret_cast<const ulonglong2 *>(sc + c * 16 + j);
+                unpack2(mul2(cs.x, twice(s)), w[0], w[1]);
+                unpack2(mul2(cs.y, twice(s)), w[2], w[3]);
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sum[c * 16 + j + i] = fmaf(v[i], s, sum[c * 16 + j + i]);
+            for (int i = 0; i < 4; ++i) sum[c * 16 + j + i] = fmaf(__uint_as_float(r[c & 1][j + i]), w[i], sum[c * 16 + j + i]);
         }
     }
 }
