@@ -211,8 +211,8 @@ block_norm_bwd_kernel(const BwdParams P)
     }
 }
 
-// 32 channels per CTA (one per lane); the 8 warps share the partial rows of a sample, or, with 8 samples or more, take
-// whole samples.
+// 32 channels per CTA (one per lane); its warps share the partial rows of a sample, or, with as many samples as warps or more,
+// take whole samples.
 struct FinishParams {
     const float *part;
     int32_t parts, c;
@@ -221,23 +221,25 @@ struct FinishParams {
     float *dpost_w, *dpost_b, *dpre_w, *dpre_b, *dgate, *dres;
 };
 
-__global__ void __launch_bounds__(256)
+constexpr int FIN_WARPS = 32;
+__global__ void __launch_bounds__(FIN_WARPS * 32)
 block_norm_finish_kernel(const FinishParams P)
 {
-    __shared__ double sm[8][4][32];
+    __shared__ double sm[FIN_WARPS][4][32];
     pdl_launch_dependents();
     pdl_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int ch = blockIdx.x * 32 + lane;
     const bool in = ch < P.c;
     const double w = in && P.post_w ? P.post_w[ch] : 1.0, b = in && P.post_b ? P.post_b[ch] : 0.0, r = in && P.res ? P.res[ch] : 1.0;
-    const bool whole = P.samples >= 8;                              // a warp takes whole samples
+    const bool whole = P.samples >= FIN_WARPS;                      // a warp takes whole samples
     double tot[5] = {0, 0, 0, 0, 0};                                // dw_post, db_post, dw_pre, db_pre, dr
-    for (int64_t s = whole ? warp : 0; s < P.samples; s += whole ? 8 : 1) {
+    for (int64_t s = whole ? warp : 0; s < P.samples; s += whole ? FIN_WARPS : 1) {
         double v[4] = {0, 0, 0, 0};
         if (in) {
+            const int step = whole ? 1 : FIN_WARPS;
 #pragma unroll 4
-            for (int p = whole ? 0 : warp; p < P.parts; p += whole ? 1 : 8) {
+            for (int p = whole ? 0 : warp; p < P.parts; p += step) {
                 const float *src = P.part + (s * P.parts + p) * 4 * P.c + ch;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) v[k] += (double)src[(int64_t)k * P.c];
@@ -249,28 +251,35 @@ block_norm_finish_kernel(const FinishParams P)
 #pragma unroll
             for (int k = 0; k < 4; ++k) sm[warp][k][lane] = v[k];
             __syncthreads();
-            if (warp == 0) {
-                for (int i = 1; i < 8; ++i)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) v[k] += sm[i][k][lane];
-            } else {
-                v[0] = v[1] = v[2] = v[3] = 0;
+            if (warp < 4) {                                         // one warp per sum
+                double a = 0;
+                for (int i = 0; i < FIN_WARPS; ++i) a += sm[i][warp][lane];
+                sm[0][warp][lane] = a;
             }
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = warp == 0 ? sm[0][k][lane] : 0.0;
         }
         if (P.dgate && in && (whole || warp == 0)) P.dgate[s * P.c + ch] = (float)(r * (w * v[0] + b * v[1]));
         tot[0] += r * g * v[0]; tot[1] += r * g * v[1]; tot[2] += v[2]; tot[3] += v[3]; tot[4] += g * (w * v[0] + b * v[1]);
     }
     float *outs[5] = {P.dpost_w, P.dpost_b, P.dpre_w, P.dpre_b, P.dres};
+    __syncthreads();
 #pragma unroll
-    for (int k = 0; k < 5; ++k) {
-        __syncthreads();
-        sm[warp][0][lane] = tot[k];
-        __syncthreads();
-        if (warp == 0 && in && outs[k]) {
-            double v = 0;
-            for (int i = 0; i < 8; ++i) v += sm[i][0][lane];
-            outs[k][ch] = (float)v;
-        }
+    for (int k = 0; k < 4; ++k) sm[warp][k][lane] = tot[k];
+    __syncthreads();
+    if (warp < 4 && in && outs[warp]) {
+        double v = 0;
+        for (int i = 0; i < FIN_WARPS; ++i) v += sm[i][warp][lane];
+        outs[warp][ch] = (float)v;
+    }
+    __syncthreads();
+    sm[warp][0][lane] = tot[4];
+    __syncthreads();
+    if (warp == 0 && in && P.dres) {
+        double v = 0;
+        for (int i = 0; i < FIN_WARPS; ++i) v += sm[i][0][lane];
+        P.dres[ch] = (float)v;
     }
 }
 
@@ -375,5 +384,5 @@ extern "C" lamp_status_t lamp_block_norm_bwd(const lamp_block_norm_t *p, const l
     else s = bf == LAMP_F32 ? dispatch<true, true>(P, samples, sh, st) : dispatch<true, false>(P, samples, sh, st);
     if (s != LAMP_OK || !want) return s;
     FinishParams F = {(const float *)ws, (int32_t)parts, P.c, samples, P.post_w, P.post_b, P.gate, P.res, g->post_w, g->post_b, g->pre_w, g->pre_b, g->gate, g->res_scale};
-    return launch_pdl(true, block_norm_finish_kernel, dim3((unsigned)((P.c + 31) / 32)), dim3(256), 0, st, F);
+    return launch_pdl(true, block_norm_finish_kernel, dim3((unsigned)((P.c + 31) / 32)), dim3(FIN_WARPS * 32), 0, st, F);
 }
