@@ -596,14 +596,17 @@ distill_row_kernel(const DistillParams P)
 // ----------------------------------------------------------------------------------------------------------------------
 // one CTA, or a cluster of CTAs, per row
 // ----------------------------------------------------------------------------------------------------------------------
-// Warp-specialised, two or more CTAs per SM, so that the phases of one row (maximum, sum: bound by the exponential unit;
-// gradient: by stores) overlap with other phases of another.  The helper warp prepares the next row's teacher entries and
-// has the next row (or this CTA's slice of it) copied into shared memory, chunk by chunk as the consumers' last pass
-// over the current row gives the chunks up: bulk asynchronous copies of the whole 16-byte units, the ragged first and last
-// unit by hand, filled up with -inf.  A row is read from HBM exactly once.
+// Warp-specialised, two or more CTAs per SM, so that the phases of one row (sum: bound by the exponential unit; gradient: by
+// stores) overlap with other phases of another.  The helper warp prepares the next row's teacher entries and has the next row
+// (or this CTA's slice of it) copied into shared memory, a half at a time as the consumers' last pass over the current row
+// gives the halves up (short slices whole: a wait costs about 100 cycles, four chunks 205 us where two take 191): bulk asynchronous copies of the whole 16-byte units, the ragged first and last unit by hand, filled
+// up with -inf.  The consumers' first pass takes the halves as they land, so it runs while the rest is on its way.
+// A row is read from HBM exactly once.
+// The first pass keeps maximum and sum per thread, moved on once per four units.
 // Measured (4096 x 50001 bf16, loss and gradient, us): loads by the threads that use them 348; one CTA per SM with two row
 // buffers 327; the same with the row held in registers and packed fp32 arithmetic 240 (loss alone 112, gradient alone 131:
-// the phases of a row simply add up when all warps of an SM share it); this form: MEASURED.
+// the phases of a row simply add up when all warps of an SM share it); two CTAs per SM with passes for maximum, sum and
+// gradient over a row that has landed 189 (loss alone 148, gradient alone 151); this form 191 (111, 147).
 struct RowSlot {                                    // what the helper prepares for a row
     float S, w;
 };
@@ -635,7 +638,7 @@ __device__ __forceinline__ uint32_t peer_addr(uint32_t addr, uint32_t rank)
 }
 
 __host__ __device__ constexpr int lists_of(int k) { return k <= SHORT_K ? 5 : 3; }
-constexpr int CR_MAX_THREADS = 1024, CR_CHUNKS = 16;
+constexpr int CR_MAX_THREADS = 1024, CR_CHUNKS = 2, CR_WHOLE = 2048;      // slices below CR_WHOLE units are one chunk
 
 template <bool F32, int MODE>
 __global__ void __launch_bounds__(CR_MAX_THREADS, 1)
@@ -644,7 +647,7 @@ distill_cta_kernel(const DistillParams P, const int S_CTAS)
     constexpr int E = Elem<F32>::E;
     extern __shared__ __align__(16) uint4 buf[];                       // [P.stash] units, then the lists [2][LISTS][k4]
     __shared__ __align__(16) float4 msg[2][8];                         // per row parity: (maximum, sum, D, P) of every CTA of the cluster
-    __shared__ __align__(8) uint64_t bars[6 + CR_CHUNKS];              // full, consumers, exchange[2], lists[2], chunk empty[]
+    __shared__ __align__(8) uint64_t bars[7 + 2 * CR_CHUNKS];          // consumers, exchange[2], lists ready[2], lists free[2], chunk full[], empty[]
     __shared__ float red[2][2][32];
     __shared__ RowSlot slot[2];
     __shared__ int abort_s;
@@ -654,18 +657,22 @@ distill_cta_kernel(const DistillParams P, const int S_CTAS)
     const bool brief = P.k <= SHORT_K;
     int *ids0 = (int *)(buf + P.stash);
     const int nthr = blockDim.x - 32, nwarp = nthr >> 5;               // consumers; the last warp is the helper
-    const int nch = (P.stash + nthr - 1) / nthr;                       // chunks: units [i nthr, (i + 1) nthr) of the slice
+    const int sweeps = (P.stash + nthr - 1) / nthr, chunk = (P.stash < CR_WHOLE ? sweeps : (sweeps + CR_CHUNKS - 1) / CR_CHUNKS) * nthr;   // units of a chunk
+    const int nch = (P.stash + chunk - 1) / chunk;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const float c2 = LOG2E / P.temp, inv_t = 1.f / P.temp;
     const uint32_t rank = S_CTAS > 1 ? blockIdx.x % S_CTAS : 0;
     const int64_t first = blockIdx.x / S_CTAS, step = gridDim.x / S_CTAS;
-    const uint32_t full = ptx::smem_u32(bars), cons = full + 8, exch0 = full + 16, lists0 = full + 32, chunk0 = full + 48;
+    const uint32_t cons = ptx::smem_u32(bars), exch0 = cons + 8, ready0 = cons + 24, lists0 = cons + 40, full0 = cons + 56, empty0 = full0 + 8 * CR_CHUNKS;
     pdl_launch_dependents();
     if (tid == 0) {
-        ptx::mbar_init(full, 2);
         ptx::mbar_init(cons, nwarp);
-        for (int b = 0; b < 2; ++b) { ptx::mbar_init(exch0 + 8 * b, 1); ptx::mbar_init(lists0 + 8 * b, nwarp); }
-        for (int i = 0; i < nch; ++i) ptx::mbar_init(chunk0 + 8 * i, nwarp);
+        for (int b = 0; b < 2; ++b) {
+            ptx::mbar_init(exch0 + 8 * b, 1);
+            ptx::mbar_init(ready0 + 8 * b, 1);
+            ptx::mbar_init(lists0 + 8 * b, nwarp);
+        }
+        for (int i = 0; i < CR_CHUNKS; ++i) { ptx::mbar_init(full0 + 8 * i, 1); ptx::mbar_init(empty0 + 8 * i, nwarp); }
         abort_s = 0;
         ptx::mbar_init_fence();
     }
@@ -684,18 +691,22 @@ distill_cta_kernel(const DistillParams P, const int S_CTAS)
     if (warp == nwarp) {
         // ------------------------------------------------------------------ helper
         int i = 0;
+        uint32_t loads = 0;                                            // rows copied so far: the phase of the chunk barriers
         float w_next = first < P.rows ? (P.w ? P.w[first] : P.w_all) : 0.f;
         float tl = P.tlse && first < P.rows ? P.tlse[first] : 0.f;
         Entries<SHORT_K / 32> ahead;
         if (brief && first < P.rows) ahead.load(P, first, lane);
         for (int64_t row = first; row < P.rows; row += step, ++i) {
             const int b = i & 1;
-            const uint32_t ph = (uint32_t)i & 1, lph = (uint32_t)(i >> 1) & 1;
             const float w = w_next;
             if (row + step < P.rows && P.w) w_next = P.w[row + step];
             int *ids = ids0 + b * nl * k4;
-            float *logp = (float *)(ids + k4), *pr = logp + 2 * k4, *pm = pr + k4;
-            ok = __all_sync(0xffffffffu, ptx::mbar_wait(lists0 + 8 * b, lph ^ 1, abort_flag));
+            float *logp = (float *)(ids + k4), *zt = logp + k4, *pr = zt + k4, *pm = pr + k4;
+            int off, nu, u0, u1;
+            geometry(row, off, nu, u0, u1);
+            const int64_t at = row * P.pz;
+            const int e0 = u0 * E - off, e1 = u1 * E - off;            // elements of the slice
+            ok = __all_sync(0xffffffffu, ptx::mbar_wait(lists0 + 8 * b, ((uint32_t)(i >> 1) & 1) ^ 1, abort_flag));
             if (!ok) break;
             float S = 0.f;
             if (w != 0.f) {
@@ -711,43 +722,47 @@ distill_cta_kernel(const DistillParams P, const int S_CTAS)
                 } else {
                     S = teacher_row(P, row, lane, ids, logp);
                 }
+                // the listed logits of the slice, before anything of the row is written (dz may be z)
+                if (S != 0.f)
+                    for (int j = lane; j < P.k; j += 32) {
+                        const int id = ids[j];
+                        zt[j] = id >= 0 && id >= e0 && id < e1 ? elem<F32>(P.z, at + id) : 0.f;
+                    }
             }
             if (brief && row + step < P.rows) ahead.load(P, row + step, lane);
             if (P.tlse && row + step < P.rows) tl = P.tlse[row + step];
             if (lane == 0) { slot[b].S = S; slot[b].w = w; }
-            int off, nu, u0, u1;
-            geometry(row, off, nu, u0, u1);
-            const int64_t at = row * P.pz;
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(ready0 + 8 * b);
+            if (S == 0.f) continue;                                    // nothing of this row is read
             // whole units of the slice: not the first if it starts in front of the row, not the last if it ends behind it
             const int f0 = u0 == 0 && off ? 1 : u0, f1 = u1 == nu && (P.c + off) % E ? nu - 1 : u1;
-            const bool load = S != 0.f;
             for (int ch = 0; ch < nch; ++ch) {
-                ok = __all_sync(0xffffffffu, ptx::mbar_wait(chunk0 + 8 * ch, ph ^ 1, abort_flag));
+                ok = __all_sync(0xffffffffu, ptx::mbar_wait(empty0 + 8 * ch, (loads & 1) ^ 1, abort_flag));
                 if (!ok) break;
-                // the first chunk given back: the consumers are past the previous row's phase of `full`, so this one may be
-                // announced (an arrival while the copies of the previous phase are in flight would be one too many for it)
-                if (ch == 0 && lane == 0) {
-                    if (load && f1 > f0) ptx::mbar_expect_tx(full, (uint32_t)(f1 - f0) * 16); else ptx::mbar_arrive(full);
-                }
-                if (!load) continue;
-                const int c0 = u0 + ch * nthr, c1 = c0 + nthr, g0 = c0 > f0 ? c0 : f0, g1 = c1 < f1 ? c1 : f1;
-                if (lane == 0 && g1 > g0) {
-                    ptx::fence_proxy_async();                          // the chunk's last readers, then the copy
-                    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                                 ::"r"(ptx::smem_u32(buf + (g0 - u0))), "l"((const char *)P.z + ((at + (int64_t)g0 * E - off) << Elem<F32>::SHIFT)),
-                                   "r"((uint32_t)(g1 - g0) * 16), "r"(full) : "memory");
-                }
+                const int c0 = u0 + ch * chunk, c1 = c0 + chunk, g0 = c0 > f0 ? c0 : f0, g1 = c1 < f1 ? c1 : f1;
                 if (lane == 1 && f0 > u0 && u1 > u0 && ch == 0) buf[0] = load_unit<F32>(P.z, at, off, u0, P.c);
                 if (lane == 2 && f1 < u1 && f1 >= f0 && f1 >= c0 && f1 < c1) buf[f1 - u0] = load_unit<F32>(P.z, at, off, f1, P.c);
+                __syncwarp();
+                if (lane == 0) {
+                    if (g1 > g0) {
+                        ptx::fence_proxy_async();                      // the chunk's last readers, then the copy
+                        ptx::mbar_expect_tx(full0 + 8 * ch, (uint32_t)(g1 - g0) * 16);
+                        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                                     ::"r"(ptx::smem_u32(buf + (g0 - u0))), "l"((const char *)P.z + ((at + (int64_t)g0 * E - off) << Elem<F32>::SHIFT)),
+                                       "r"((uint32_t)(g1 - g0) * 16), "r"(full0 + 8 * ch) : "memory");
+                    } else {
+                        ptx::mbar_arrive(full0 + 8 * ch);
+                    }
+                }
             }
             if (!ok) break;
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(full);
+            ++loads;
         }
     } else {
         // ------------------------------------------------------------------ consumers
-        int i = 0, ex = 0;                                             // rows, rows with an exchange
-        uint32_t cphase = 0;
+        int i = 0;
+        uint32_t cphase = 0, loads = 0;
         for (int64_t row = first; row < P.rows; row += step, ++i) {
             const int b = i & 1;
             const int64_t dat = row * P.pdz;
@@ -757,51 +772,46 @@ distill_cta_kernel(const DistillParams P, const int S_CTAS)
             const bool same = (MODE & BWD) && off == misalign<F32>(P.dz, dat);
             const int e0 = u0 * E - off, e1 = u1 * E - off;            // elements of the slice
             const int *ids = ids0 + b * nl * k4;
-            const float *logp = (const float *)(ids + k4), *pr = logp + 2 * k4, *pm = pr + k4;
-            float *zt = (float *)(logp + k4);
-            ok = __all_sync(0xffffffffu, ptx::mbar_wait(full, (uint32_t)i & 1, abort_flag));
+            const float *logp = (const float *)(ids + k4), *zt = logp + k4, *pr = zt + k4, *pm = pr + k4;
+            ok = __all_sync(0xffffffffu, ptx::mbar_wait(ready0 + 8 * b, (uint32_t)(i >> 1) & 1, abort_flag));
             if (!ok) break;
             const float S = slot[b].S, w = slot[b].w;
             float loss = 0.f, lse = 0.f;
-            int ch = 0;                                                // chunks given back so far
-            auto give_back = [&]() {
+            auto landed = [&](int ch) { return __all_sync(0xffffffffu, ptx::mbar_wait(full0 + 8 * ch, loads & 1, abort_flag)); };
+            auto give_back = [&](int ch) {
                 __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(chunk0 + 8 * ch);
-                ++ch;
+                if (lane == 0) ptx::mbar_arrive(empty0 + 8 * ch);
             };
             if (S != 0.f) {
-                // before this warp gives back any chunk: a chunk is copied over only when every warp has given it back
-                for (int j = tid; j < P.k; j += nthr) {
-                    const int id = ids[j];
-                    if (id >= 0 && id >= e0 && id < e1) zt[j] = elem<F32>(buf, id - e0);
-                }
                 float m, s = 1.f, scale = 1.f;                         // maximum of z, sum of e^((z - m) / T)
                 if constexpr (MODE & FWD) {
-                    m = -FLT_MAX;                                      // of -inf alone: the sum is 0
-#pragma unroll 4
-                    for (int u = tid; u < n; u += nthr) m = fmaxf(m, unit_max<F32>(buf[u]));
-                    m = warp_max_fast(m);
                     s = 0.f;
-                    const float mc = m * c2;
-                    // with no gradient to come this is the last pass, which gives the chunks back
-                    if constexpr (MODE & BWD) {
-                        if (fabsf(mc) < 1e38f) {
-#pragma unroll 2
-                            for (int u = tid; u < n; u += nthr) s += unit_sum<F32, false>(buf[u], c2, m, mc);
-                        } else {
-                            for (int u = tid; u < n; u += nthr) s += unit_sum<F32, true>(buf[u], c2, m, mc);
+                    m = -FLT_MAX;                                      // with -inf alone the sum stays 0
+                    for (int ch = 0; ch < nch; ++ch) {
+                        if (!(ok = landed(ch))) break;
+                        const int end = (ch + 1) * chunk < n ? (ch + 1) * chunk : n;
+                        for (int u = ch * chunk + tid; u < end; u += 4 * nthr) {       // four units at a time
+                            uint4 raw[4];
+                            float top = -FLT_MAX;
+#pragma unroll
+                            for (int q = 0; q < 4; ++q)
+                                if (u + q * nthr < end) { raw[q] = buf[u + q * nthr]; top = fmaxf(top, unit_max<F32>(raw[q])); }
+                            if (top > m) { s *= ex2((m - top) * c2); m = top; }
+                            const float mc = m * c2;
+                            if (fabsf(mc) < 1e38f) {
+#pragma unroll
+                                for (int q = 0; q < 4; ++q) if (u + q * nthr < end) s += unit_sum<F32, false>(raw[q], c2, m, mc);
+                            } else {
+#pragma unroll 1
+                                for (int q = 0; q < 4; ++q) if (u + q * nthr < end) s += unit_sum<F32, true>(buf[u + q * nthr], c2, m, mc);
+                            }
                         }
-                    } else {
-                        const uint32_t low = F32 ? 0xFF800000u : 0xFF80FF80u;
-                        const bool fits = fabsf(mc) < 1e38f;
-#pragma unroll 2
-                        for (int u = tid; ch < nch; u += nthr) {
-                            const uint4 raw = u < n ? buf[u] : make_uint4(low, low, low, low);
-                            give_back();
-                            s += fits ? unit_sum<F32, false>(raw, c2, m, mc) : unit_sum<F32, true>(raw, c2, m, mc);
-                        }
+                        if (!(MODE & BWD)) give_back(ch);              // the last pass
                     }
-                    s = warp_sum(s);
+                    if (!ok) break;
+                    const float mt = m;
+                    m = warp_max_fast(m);
+                    s = warp_sum(s * ex2((mt - m) * c2));
                     if (lane == 0) { red[i & 1][0][warp] = m; red[i & 1][1][warp] = s; }
                     if (!(ok = consumer_sync(cons, cphase, lane, abort_flag))) break;
                     const float mw = lane < nwarp ? red[i & 1][0][lane] : -FLT_MAX;
@@ -818,16 +828,15 @@ distill_cta_kernel(const DistillParams P, const int S_CTAS)
                         D = warp_sum(D); PS = warp_sum(PS);
                     }
                     if (S_CTAS > 1) {
-                        const int x = ex & 1;
+                        const int x = loads & 1;
                         if (warp == 0) {
                             if (lane == 0) ptx::mbar_expect_tx(exch0 + 8 * x, 16 * S_CTAS);
                             __syncwarp();
                             if (lane < S_CTAS)
                                 st_async_v4(peer_addr(ptx::smem_u32(&msg[x][rank]), lane), peer_addr(exch0 + 8 * x, lane), m, s, D, PS);
                         }
-                        ok = __all_sync(0xffffffffu, ptx::mbar_wait(exch0 + 8 * x, (uint32_t)(ex >> 1) & 1, abort_flag));
+                        ok = __all_sync(0xffffffffu, ptx::mbar_wait(exch0 + 8 * x, (loads >> 1) & 1, abort_flag));
                         if (!ok) break;
-                        ++ex;
                         m = -FLT_MAX; s = 0.f;
                         for (int r = 0; r < S_CTAS; ++r) join(m, s, msg[x][r].x, msg[x][r].y, c2);
                         D = 0.f; PS = 0.f;
@@ -849,16 +858,19 @@ distill_cta_kernel(const DistillParams P, const int S_CTAS)
                 if constexpr (MODE & BWD) {
                     const float gT = w * P.temp, gq = gT * S * scale, mc = m * c2;
                     const int kind = !(MODE & FWD) ? 2 : fabsf(mc) < 1e38f ? 0 : 1;
+                    for (int ch = 0; ch < nch; ++ch) {
+                        if (!(MODE & FWD) && !(ok = landed(ch))) break;
+                        const int end = (ch + 1) * chunk < n ? (ch + 1) * chunk : n;
 #pragma unroll 2
-                    for (int u = tid; ch < nch; u += nthr) {
-                        const uint4 raw = u < n ? buf[u] : make_uint4(0, 0, 0, 0);
-                        give_back();
-                        if (u >= n) continue;
-                        uint4 o;
-                        if constexpr (MODE & FWD) o = kind == 0 ? unit_grad<F32, 0>(raw, c2, m, mc, gq) : unit_grad<F32, 1>(raw, c2, m, mc, gq);
-                        else o = unit_grad<F32, 2>(raw, inv_t, m, mc, gq);
-                        put_unit<F32>(P.dz, dat, off, same, u0 + u, P.c, o);
+                        for (int u = ch * chunk + tid; u < end; u += nthr) {
+                            uint4 o = buf[u];
+                            if constexpr (MODE & FWD) o = kind == 0 ? unit_grad<F32, 0>(o, c2, m, mc, gq) : unit_grad<F32, 1>(o, c2, m, mc, gq);
+                            else o = unit_grad<F32, 2>(o, inv_t, m, mc, gq);
+                            put_unit<F32>(P.dz, dat, off, same, u0 + u, P.c, o);
+                        }
+                        give_back(ch);
                     }
+                    if (!ok) break;
                     if (!(ok = consumer_sync(cons, cphase, lane, abort_flag))) break;    // the listed classes go over what the dense pass wrote
                     for (int j = tid; j < P.k; j += nthr) {
                         const int id = ids[j];
@@ -869,14 +881,12 @@ distill_cta_kernel(const DistillParams P, const int S_CTAS)
                         put<F32>(P.dz, dat + id, gT * (S * (scale * power<MODE>(zt[j], c2, inv_t, m)) - p));
                     }
                 }
-            } else {
-                while (ch < nch) give_back();
-                if constexpr (MODE & BWD) {
-                    float v[E];
+                ++loads;
+            } else if constexpr (MODE & BWD) {
+                float v[E];
 #pragma unroll
-                    for (int j = 0; j < E; ++j) v[j] = 0.f;
-                    for (int u = u0 + tid; u < u1; u += nthr) store_unit<F32>(P.dz, dat, off, same, u, P.c, v);
-                }
+                for (int j = 0; j < E; ++j) v[j] = 0.f;
+                for (int u = u0 + tid; u < u1; u += nthr) store_unit<F32>(P.dz, dat, off, same, u, P.c, v);
             }
             if ((MODE & FWD) && rank == 0 && tid == 0) {
                 if (P.loss_rows) P.loss_rows[row] = loss;
