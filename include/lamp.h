@@ -253,7 +253,7 @@ typedef struct {
     const float *res_scale;
 } lamp_block_norm_t;
 
-/* y == NULL: t = x (the norm in front of the first block; out must be NULL).  h and h_fp8 may each be NULL; out may be x
+/* y == NULL: t = x (the norm in front of the first block; out, gate, gate_logits and res_scale must be NULL).  h and h_fp8 may each be NULL; out may be x
  * (the same view), and is required when y is given.  h_fp8 (tile_scale = 0, rows = n*d*h*w, k = c) receives h in 8 bits,
  * quantised from fp32 as lamp_fp8_quantize does, ready to be an operand of lamp_gemm_fp8. */
 lamp_status_t lamp_block_norm_fwd(const lamp_block_norm_t *p, const lamp_tensor_t *y, const lamp_tensor_t *x, lamp_tensor_t *out,
@@ -268,8 +268,8 @@ typedef struct {
  * gradient of h, or NULL for none (one of the two is required).
  *     dt = dout + dN_pre(dh),  dx = dt,  dy = dN_post(dt * r * g),  dgate_logits = dt * r * N_post(y) * g (1 - g).
  * dx may be dout (the same view).  y, dy and dgate_logits are NULL together when there is no post-norm (dgate_logits also
- * when there are no logits).  Sums over voxels run in a fixed order.  The workspace needs
- * lamp_block_norm_bwd_workspace_bytes, which is 0 when no member of grads is asked for (grads itself may be NULL). */
+ * when there are no logits).  Sums over voxels run in a fixed order.  The workspace (16-byte aligned) needs
+ * lamp_block_norm_bwd_workspace_bytes; none is needed when no member of grads is asked for (grads itself may be NULL). */
 size_t        lamp_block_norm_bwd_workspace_bytes(const lamp_tensor_t *t, const lamp_block_norm_t *p);
 lamp_status_t lamp_block_norm_bwd(const lamp_block_norm_t *p, const lamp_tensor_t *y, const lamp_tensor_t *t,
                                   const lamp_tensor_t *dout, const lamp_tensor_t *dh, lamp_tensor_t *dx, lamp_tensor_t *dy,
@@ -299,7 +299,7 @@ typedef struct {
     float          temperature;           /* > 0 */
 } lamp_teacher_topk_t;
 
-/* Scratch for `loss`; not needed where loss is NULL.  Depends on the shape of z only. */
+/* Scratch for `loss` (16-byte aligned); not needed where loss is NULL. */
 size_t        lamp_distill_topk_workspace_bytes(const lamp_tensor_t *z);
 /* loss_rows: fp32 [rows]; lse: fp32 [rows], log sum_i exp(z_i / T), needed by the backward call; loss: fp32 scalar
  * sum_r row_weight[r] * loss_rows[r].  Each of the three may be NULL. */

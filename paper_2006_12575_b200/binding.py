@@ -461,22 +461,24 @@ def lamp_gemm_fp8(a: Fp8Operand, b: Fp8Operand, y, bias=None):
 def block_norm(rms=False, eps=1e-5, post_w=None, post_b=None, pre_w=None, pre_b=None, gate=None, gate_logits=None,
                res_scale=None) -> BlockNorm:
     """Parameters of lamp_block_norm_fwd / _bwd: fp32 vectors [c] (gate: [n, c]), gate_logits a tensor like y."""
-    keep = (post_w, post_b, pre_w, pre_b, res_scale)
-    first = next((v for v in keep if v is not None), None)
-    p = BlockNorm()
-    p.rms, p.eps = 1 if rms else 0, eps
-    p.c = p.dev = None                                              # of the vectors, for the calls to check
-    if first is not None:
-        p.c, p.dev = first.numel(), first.get_device()
-        ptr = [_vec(v, p.c, name, p.dev) for v, name in zip(keep, ("post_w", "post_b", "pre_w", "pre_b", "res_scale"))]
-        p.post_w, p.post_b, p.pre_w, p.pre_b, p.res_scale = ptr
+    c = dev = None                                                  # of the vectors, for the calls to check
+    ptr = []
+    for v in (post_w, post_b, pre_w, pre_b, res_scale):
+        if v is None:
+            ptr.append(None)
+            continue
+        if c is None:
+            c, dev = v.numel(), v.get_device()
+        ptr.append(_vec(v, c, "block_norm", dev))
+    g = view = gate_shape = None
     if gate is not None:
-        p.gate = _vec(gate, gate.numel(), "gate", gate.get_device())
-        p.gate_numel, p.gate_dev = gate.numel(), gate.get_device()
+        gate_shape = (gate.numel(), gate.get_device())
+        g = _vec(gate, gate_shape[0], "gate", gate_shape[1])
     if gate_logits is not None:
-        p.view = _view(gate_logits, gate_logits.get_device() if torch.is_tensor(gate_logits) else None, "gate_logits")
-        p.gate_logits = C.pointer(p.view)
-    p.keep = (keep, gate, gate_logits)
+        view = _view(gate_logits, gate_logits.get_device() if torch.is_tensor(gate_logits) else None, "gate_logits")
+    p = BlockNorm(1 if rms else 0, eps, ptr[0], ptr[1], ptr[2], ptr[3], g, None if view is None else C.pointer(view), ptr[4])
+    p.c, p.dev, p.gate_shape, p.logits = c, dev, gate_shape, gate_logits
+    p.keep = (post_w, post_b, pre_w, pre_b, res_scale, gate, view)
     return p
 
 
@@ -484,11 +486,10 @@ def _norm_params(p, shape, dev):
     """The parameters, checked against the shape of the call's tensors."""
     if p.c is not None and (p.c != shape.c or p.dev != dev):
         raise ValueError(f"block_norm: vectors of {p.c} on cuda:{p.dev}, the tensors have {shape.c} channels on cuda:{dev}")
-    if p.gate and (p.gate_numel != shape.n * shape.c or p.gate_dev != dev):
-        raise ValueError(f"block_norm: gate of {p.gate_numel} on cuda:{p.gate_dev}, want [{shape.n}, {shape.c}] on cuda:{dev}")
-    logits = p.keep[2]
-    if torch.is_tensor(logits) and logits.get_device() != dev:
-        raise ValueError(f"block_norm: gate_logits on {logits.device}, the current device is cuda:{dev}")
+    if p.gate_shape is not None and p.gate_shape != (shape.n * shape.c, dev):
+        raise ValueError(f"block_norm: gate of {p.gate_shape[0]} on cuda:{p.gate_shape[1]}, want [{shape.n}, {shape.c}] on cuda:{dev}")
+    if p.logits is not None and torch.is_tensor(p.logits) and p.logits.get_device() != dev:
+        raise ValueError(f"block_norm: gate_logits on {p.logits.device}, the current device is cuda:{dev}")
     return C.byref(p)
 
 

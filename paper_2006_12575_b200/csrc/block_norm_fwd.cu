@@ -169,15 +169,17 @@ block_norm_fwd_kernel(const FwdParams P)
     }
 }
 
-// CTAs per SM that the kernel is compiled for: the grid is that many per SM, so that all are resident at once (four per SM
-// where three fit cost a second, mostly empty wave: 120 us against MEASURED on 131,072 x 512)
-constexpr int FWD_CTAS = 3;
+// CTAs of 256 threads per SM that a kernel is compiled for: the grid is that many per SM, so that all are resident at once (four
+// per SM where three fit cost a second, mostly empty wave: 120 us against 114 on 131,072 x 512).  Three mean 80 registers;
+// with two units per thread and fp32 or gate rows in flight as well they would spill.
+__host__ __device__ constexpr int fwd_ctas(bool wide_rows, int u) { return wide_rows && u == 2 ? 2 : 3; }
 
-template <bool SF, bool BF, int TPR, int U, int MAXT, int MINB>
+template <bool SF, bool BF, int TPR, int U, int MAXT>
 lamp_status_t launch(const FwdParams &P, int64_t samples, const Shape &sh, cudaStream_t st)
 {
     const int smem = P.c * 16;
-    auto kernel = P.logits ? block_norm_fwd_kernel<SF, BF, TPR, U, MAXT, MINB, true> : block_norm_fwd_kernel<SF, BF, TPR, U, MAXT, MINB, false>;
+    auto kernel = P.logits ? block_norm_fwd_kernel<SF, BF, TPR, U, MAXT, MAXT == 256 ? fwd_ctas(true, U) : 1, true>
+                           : block_norm_fwd_kernel<SF, BF, TPR, U, MAXT, MAXT == 256 ? fwd_ctas(SF, U) : 1, false>;
     if (smem > 32 * 1024) {                                  // static shared memory counts too: well below the 48 KB default
         static SmemAttrOnce attr[2];
         const lamp_status_t s = attr[P.logits ? 1 : 0].ensure(kernel, MAX_C * 16);
@@ -189,12 +191,12 @@ lamp_status_t launch(const FwdParams &P, int64_t samples, const Shape &sh, cudaS
 template <bool SF, bool BF>
 lamp_status_t dispatch(const FwdParams &P, int64_t samples, const Shape &sh, cudaStream_t st)
 {
-    if (sh.tpr == 4) return launch<SF, BF, 4, 1, 256, FWD_CTAS>(P, samples, sh, st);
-    if (sh.tpr == 8) return launch<SF, BF, 8, 1, 256, FWD_CTAS>(P, samples, sh, st);
-    if (sh.tpr == 16) return launch<SF, BF, 16, 1, 256, FWD_CTAS>(P, samples, sh, st);
-    if (sh.tpr == 32 && sh.u == 1) return launch<SF, BF, 32, 1, 256, FWD_CTAS>(P, samples, sh, st);
-    if (sh.tpr == 32) return launch<SF, BF, 32, 2, 256, FWD_CTAS>(P, samples, sh, st);
-    return sh.threads <= 256 ? launch<SF, BF, 0, 2, 256, FWD_CTAS>(P, samples, sh, st) : launch<SF, BF, 0, 2, 512, 1>(P, samples, sh, st);
+    if (sh.tpr == 4) return launch<SF, BF, 4, 1, 256>(P, samples, sh, st);
+    if (sh.tpr == 8) return launch<SF, BF, 8, 1, 256>(P, samples, sh, st);
+    if (sh.tpr == 16) return launch<SF, BF, 16, 1, 256>(P, samples, sh, st);
+    if (sh.tpr == 32 && sh.u == 1) return launch<SF, BF, 32, 1, 256>(P, samples, sh, st);
+    if (sh.tpr == 32) return launch<SF, BF, 32, 2, 256>(P, samples, sh, st);
+    return sh.threads <= 256 ? launch<SF, BF, 0, 2, 256>(P, samples, sh, st) : launch<SF, BF, 0, 2, 512>(P, samples, sh, st);
 }
 
 }  // namespace
@@ -262,7 +264,8 @@ extern "C" lamp_status_t lamp_block_norm_fwd(const lamp_block_norm_t *p, const l
     P.rows = rows / samples;
     const Shape sh = shape_of(P.c);
     const int64_t need = (P.rows + sh.rows_per_cta - 1) / sh.rows_per_cta;
-    int64_t room = (int64_t)sm_count() * (sh.threads <= 256 ? FWD_CTAS * 256 / sh.threads : 1) / samples;
+    const int ctas = fwd_ctas(p->gate_logits || x->dtype == LAMP_F32, sh.u);
+    int64_t room = (int64_t)sm_count() * (sh.threads <= 256 ? ctas * 256 / sh.threads : 1) / samples;
     if (room < 1) room = 1;
     P.parts = (int32_t)(need < room ? need : room);
     if (samples * P.parts > 2147483647ll) return LAMP_ERR_UNSUPPORTED;
