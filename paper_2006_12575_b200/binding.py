@@ -403,16 +403,18 @@ def _vec(t, n, what, dev, dtype=torch.float32):
     return t.data_ptr()
 
 
+_VIEW_TYPES = {torch.bfloat16: LAMP_BF16, torch.float32: LAMP_F32}
+
+
 def _view(x, dev, what):
     """Descriptor of a tensor argument (torch tensor on the current device, or a Tensor); None stays None."""
     if x is None or isinstance(x, Tensor):
         return x
-    if x.get_device() != dev:
-        raise ValueError(f"{what}: on {x.device}, the current device is cuda:{dev}")
-    if x.dim() != 5 or not x.is_contiguous() or x.dtype not in (torch.bfloat16, torch.float32):
-        raise ValueError(f"{what}: want a contiguous bf16 or fp32 tensor [n, d, h, w, c], got {tuple(x.shape)} {x.dtype}")
-    n, d, h, w, c = x.shape
-    return Tensor(x.data_ptr(), LAMP_BF16 if x.dtype is torch.bfloat16 else LAMP_F32, n, d, h, w, c, c, 0)
+    s, dt = x.shape, _VIEW_TYPES.get(x.dtype)
+    if dt is None or len(s) != 5 or x.get_device() != dev or not x.is_contiguous():
+        raise ValueError(f"{what}: want a contiguous bf16 or fp32 tensor [n, d, h, w, c] on cuda:{dev}, got {tuple(s)} {x.dtype} on {x.device}")
+    n, d, h, w, c = s
+    return Tensor(x.data_ptr(), dt, n, d, h, w, c, c, 0)
 
 
 def _byref(s):
