@@ -28,6 +28,7 @@ using namespace ptx;
 constexpr int KB = 128;                       // codes per scale block = bytes per shared-memory row
 constexpr int MAX_STAGES = 10, MAX_ACC = 4;
 constexpr int RING = 8;                       // blocks of scales in flight (Scales)
+constexpr int STAGE_FLOATS = 32 * 17;         // a promotion warp's staging area for rows that are not 16-byte aligned
 
 struct GemmParams {
     int32_t rows_l, rows_c;                   // rows of the lane operand and of the column operand
@@ -56,9 +57,9 @@ template <int BN> struct GemmLayout {
     static constexpr int THREADS = (2 + ISSUERS + NEPI) * 32;     // TMA, MMA, scales, promotion
     static constexpr int EPI0 = 2 + ISSUERS;                      // first promotion warp
     static constexpr int TMEM_COLS = NACC * BN;                   // 64 .. 512, a power of two
-    static constexpr int SCALE_BYTES = RING * (128 + (BN)) * 4;
+    static constexpr int SCALE_BYTES = RING * (128 + BN) * 4, OUT_BYTES = NEPI * STAGE_FLOATS * 4;
     static constexpr int BAR_BYTES = (2 * MAX_STAGES + 2 * MAX_ACC + 2 * RING) * 8 + 16;
-    static constexpr int TOTAL = 1024 + STAGES * STAGE_BYTES + SCALE_BYTES + BAR_BYTES;
+    static constexpr int TOTAL = 1024 + STAGES * STAGE_BYTES + SCALE_BYTES + OUT_BYTES + BAR_BYTES;
     static_assert(BN * 128 * 4 <= STAGES * STAGE_BYTES, "the split-k parts reuse the stages");
     static_assert(TOTAL <= 227 * 1024 && STAGES <= MAX_STAGES && NACC <= MAX_ACC, "");
 };
@@ -160,11 +161,15 @@ __device__ __forceinline__ void store_row(const GemmParams &P, int64_t row, int 
     }
 }
 
-// the finished sums of NV columns of lane row `row`: bias, rounding, store
-template <int NV>
-__device__ __forceinline__ void finish(const GemmParams &P, int64_t row, int col, float (&v)[NV])
+// The finished sums of NV columns of a lane row: bias, rounding, store.  Every lane of the warp takes part; row = the lane's own.
+// ODD (rows that are not 16-byte aligned, or a width that is no multiple of 16): through `stage`, 32 x 17 floats of the warp, so that
+// neighbouring lanes write neighbouring columns: stored by the lanes that hold them, every 4-byte store is a sector of its
+// own (1407 x 2805 fp32: 29 us against 12; 16384 x 4095 bf16, k = 512: 609 against 151).  A kernel of its own: the code
+// alone cost the aligned products 5 %.
+template <bool ODD, int NV>
+__device__ __forceinline__ void finish(const GemmParams &P, int64_t row, int col, float (&v)[NV], float *stage)
 {
-    if (row >= P.rows_l) return;
+    if ((!ODD || P.swap) && row >= P.rows_l) return;
     if (P.swap) {                              // lanes = channels of y, columns = its voxels
         const float b = P.bias ? __ldg(P.bias + row) : 0.f;
 #pragma unroll
@@ -173,20 +178,40 @@ __device__ __forceinline__ void finish(const GemmParams &P, int64_t row, int col
             const int64_t at = (int64_t)(col + j) * P.y_pitch + row;
             if (P.y_f32) ((float *)P.y)[at] = v[j] + b; else ((bf16 *)P.y)[at] = f2bf(v[j] + b);
         }
-    } else {
-        if (P.bias) {
-#pragma unroll
-            for (int j = 0; j < NV; ++j) if (col + j < P.rows_c) v[j] += __ldg(P.bias + col + j);
-        }
-        store_row<NV>(P, row, col, v);
+        return;
     }
+    if (P.bias) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) if (col + j < P.rows_c) v[j] += __ldg(P.bias + col + j);
+    }
+    if (!ODD || NV < 16) {
+        if (row < P.rows_l) store_row<NV>(P, row, col, v);
+        return;
+    }
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) stage[lane * 17 + j] = v[j];
+    __syncwarp();
+    const int64_t row0 = row - lane;
+    const int j = lane & 15;
+    if (col + j < P.rows_c) {
+#pragma unroll 4
+        for (int i = 0; i < 32; i += 2) {
+            const int r = i + (lane >> 4);
+            if (row0 + r >= P.rows_l) break;
+            const int64_t at = (row0 + r) * P.y_pitch + col + j;
+            const float x = stage[r * 17 + j];
+            if (P.y_f32) ((float *)P.y)[at] = x; else ((bf16 *)P.y)[at] = f2bf(x);
+        }
+    }
+    __syncwarp();
 }
 
 // Sum over the S parts of a tile (in CTAs first, first + stride, ... of the cluster) of the `mine`-th CW / S columns of this
 // thread's lane row, and their store.
-template <int CW, int S>
+template <bool ODD, int CW, int S>
 __device__ __forceinline__ void reduce_parts(const GemmParams &P, uint32_t part_base, int lane_row, int64_t row, int col_local, int col0, uint32_t mine,
-                                             uint32_t first, uint32_t stride)
+                                             uint32_t first, uint32_t stride, float *stage)
 {
     constexpr int CWS = CW / S, CH = CWS < 16 ? CWS : 16;
 #pragma unroll 1
@@ -199,7 +224,7 @@ __device__ __forceinline__ void reduce_parts(const GemmParams &P, uint32_t part_
         for (int s = 0; s < S; ++s)
 #pragma unroll
             for (int j = 0; j < CH; ++j) v[j] += ld_peer_f32(part_base + ((cl + j) * 128 + lane_row) * 4, first + s * stride);
-        finish<CH>(P, row, col0 + cl, v);
+        finish<ODD, CH>(P, row, col0 + cl, v, stage);
     }
 }
 
@@ -270,7 +295,7 @@ __device__ __forceinline__ void promote(float (&sum)[CW], uint32_t taddr, float 
     }
 }
 
-template <int BN, bool COLVEC>
+template <int BN, bool COLVEC, bool ODD>
 __global__ void __launch_bounds__(GemmLayout<BN>::THREADS, 1)
 fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constant__ CUtensorMap map_c, const GemmParams P)
 {
@@ -281,7 +306,8 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constant
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     float *scale_buf = (float *)(smem + STAGES * L::STAGE_BYTES);
-    uint64_t *bars = (uint64_t *)(smem + STAGES * L::STAGE_BYTES + L::SCALE_BYTES);
+    float *out_stage = (float *)(smem + STAGES * L::STAGE_BYTES + L::SCALE_BYTES);
+    uint64_t *bars = (uint64_t *)(smem + STAGES * L::STAGE_BYTES + L::SCALE_BYTES + L::OUT_BYTES);
     uint32_t *tmem_slot = (uint32_t *)(bars + 2 * MAX_STAGES + 2 * MAX_ACC + 2 * RING);
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
 
@@ -373,6 +399,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constant
     } else {
         // ------------------------------------------------------------------ promotion
         const int q = warp & 3, half = (warp - L::EPI0) >> 2;              // lane quarter and column part of this warp
+        float *stage = out_stage + (warp - L::EPI0) * STAGE_FLOATS;
         const int lane_row = q * 32 + lane;
         uint32_t acc = 0, acc_phase = 0, n = 0;
         bool ok = true;
@@ -405,7 +432,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constant
                     float v[16];
 #pragma unroll
                     for (int j = 0; j < 16; ++j) v[j] = sum[c * 16 + j];
-                    finish<16>(P, row, cbase + c * 16, v);
+                    finish<ODD, 16>(P, row, cbase + c * 16, v, stage);
                 }
             } else {
                 // every stage of this CTA has been read: its memory takes the parts, [column][lane row]
@@ -424,12 +451,13 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constant
         cluster_sync_all();
         if (warp >= L::EPI0) {
             const int q = warp & 3, half = (warp - L::EPI0) >> 2, lane_row = q * 32 + lane;
+            float *stage = out_stage + (warp - L::EPI0) * STAGE_FLOATS;
             const int64_t row = (tile0 / P.nc) * 128 + lane_row;
             const int col0 = (int)(tile0 % P.nc) * BN;
             const uint32_t base = smem_u32(smem);
-            if (S == 2) reduce_parts<CW, 2>(P, base, lane_row, row, half * CW, col0, rank, 0, 1);
-            else if (S == 4) reduce_parts<CW, 4>(P, base, lane_row, row, half * CW, col0, rank, 0, 1);
-            else reduce_parts<CW, 8>(P, base, lane_row, row, half * CW, col0, rank, 0, 1);
+            if (S == 2) reduce_parts<ODD, CW, 2>(P, base, lane_row, row, half * CW, col0, rank, 0, 1, stage);
+            else if (S == 4) reduce_parts<ODD, CW, 4>(P, base, lane_row, row, half * CW, col0, rank, 0, 1, stage);
+            else reduce_parts<ODD, CW, 8>(P, base, lane_row, row, half * CW, col0, rank, 0, 1, stage);
         }
         cluster_sync_all();      // no CTA leaves while a peer still reads its parts
     }
@@ -466,9 +494,9 @@ template <int BN> struct PairLayout {
     static constexpr int NACC = BN == 256 ? 2 : 4;
     static constexpr int CW = BN / 2;                             // columns per promotion warp
     static constexpr int THREADS = 384, TMEM_COLS = 512;
-    static constexpr int SCALE_BYTES = RING * (128 + BN) * 4;
+    static constexpr int SCALE_BYTES = RING * (128 + BN) * 4, OUT_BYTES = 8 * STAGE_FLOATS * 4;
     static constexpr int BAR_BYTES = (2 * MAX_STAGES + 2 * MAX_ACC + 2 * RING) * 8 + 16;
-    static constexpr int TOTAL = 1024 + STAGES * STAGE_BYTES + SCALE_BYTES + BAR_BYTES;
+    static constexpr int TOTAL = 1024 + STAGES * STAGE_BYTES + SCALE_BYTES + OUT_BYTES + BAR_BYTES;
     static_assert(TOTAL <= 227 * 1024 && STAGES <= MAX_STAGES && NACC <= MAX_ACC && NACC * BN <= TMEM_COLS, "");
 };
 
@@ -502,7 +530,7 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr)
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 
-template <int BN, bool COLVEC>
+template <int BN, bool COLVEC, bool ODD>
 __global__ void __launch_bounds__(PairLayout<BN>::THREADS, 1)
 fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constant__ CUtensorMap map_c, const GemmParams P)
 {
@@ -513,7 +541,8 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     float *scale_buf = (float *)(smem + STAGES * L::STAGE_BYTES);
-    uint64_t *bars = (uint64_t *)(smem + STAGES * L::STAGE_BYTES + L::SCALE_BYTES);
+    float *out_stage = (float *)(smem + STAGES * L::STAGE_BYTES + L::SCALE_BYTES);
+    uint64_t *bars = (uint64_t *)(smem + STAGES * L::STAGE_BYTES + L::SCALE_BYTES + L::OUT_BYTES);
     uint32_t *tmem_slot = (uint32_t *)(bars + 2 * MAX_STAGES + 2 * MAX_ACC + 2 * RING);
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
 
@@ -608,6 +637,7 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
         asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         const int q = warp & 3, half = (warp - 4) >> 2;
         const int lane_row = q * 32 + lane;
+        float *stage = out_stage + (warp - 4) * STAGE_FLOATS;
         uint32_t acc = 0, acc_phase = 0, n = 0;
         const uint32_t tempty_leader = map_to_rank(tempty0, leader);
         for (int64_t tile = tile0; tile < P.tiles && ok; tile += tile_step) {
@@ -645,7 +675,7 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
                 float v[16];
 #pragma unroll
                 for (int j = 0; j < 16; ++j) v[j] = sum[c * 16 + j];
-                finish<16>(P, row, cbase + c * 16, v);
+                finish<ODD, 16>(P, row, cbase + c * 16, v, stage);
             }
         }
     }
@@ -657,11 +687,12 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
         cluster_sync_all();
         if (warp >= 4) {
             const int q = warp & 3, half = (warp - 4) >> 2, lane_row = q * 32 + lane;
+            float *stage = out_stage + (warp - 4) * STAGE_FLOATS;
             const int64_t row = (tile0 / P.nc) * 256 + rank * 128 + lane_row;
             const int col0 = (int)(tile0 % P.nc) * BN;
             const uint32_t base = smem_u32(smem);
-            if (S == 2) reduce_parts<CW, 2>(P, base, lane_row, row, half * CW, col0, split, rank, 2);
-            else reduce_parts<CW, 4>(P, base, lane_row, row, half * CW, col0, split, rank, 2);
+            if (S == 2) reduce_parts<ODD, CW, 2>(P, base, lane_row, row, half * CW, col0, split, rank, 2, stage);
+            else reduce_parts<ODD, CW, 4>(P, base, lane_row, row, half * CW, col0, split, rank, 2, stage);
         }
     }
     tc_fence_before();
@@ -671,14 +702,14 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
     if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(L::TMEM_COLS) : "memory");
 }
 
-template <int BN, bool COLVEC>
-lamp_status_t launch_pair(const lamp_fp8_operand_t *l, const lamp_fp8_operand_t *c, const GemmParams &P, cudaStream_t st)
+template <int BN, bool COLVEC, bool ODD>
+lamp_status_t launch_pair_k(const lamp_fp8_operand_t *l, const lamp_fp8_operand_t *c, const GemmParams &P, cudaStream_t st)
 {
     using L = PairLayout<BN>;
     CUtensorMap ml, mc;
     if (!encode_operand(l, 128, &ml) || !encode_operand(c, BN / 2, &mc)) return LAMP_ERR_CUDA;
     static SmemAttrOnce attr;
-    { const lamp_status_t as = attr.ensure(fp8_gemm_pair_kernel<BN, COLVEC>, (int)L::TOTAL); if (as != LAMP_OK) return as; }
+    { const lamp_status_t as = attr.ensure(fp8_gemm_pair_kernel<BN, COLVEC, ODD>, (int)L::TOTAL); if (as != LAMP_OK) return as; }
     const int64_t pairs = sm_count() / 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2 * (unsigned)(P.splits > 1 ? P.tiles * P.splits : P.tiles < pairs ? P.tiles : pairs));
@@ -692,17 +723,17 @@ lamp_status_t launch_pair(const lamp_fp8_operand_t *l, const lamp_fp8_operand_t 
     at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = P.tiles <= 4 * pairs ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, fp8_gemm_pair_kernel<BN, COLVEC>, ml, mc, P) == cudaSuccess ? LAMP_OK : LAMP_ERR_CUDA;
+    return cudaLaunchKernelEx(&cfg, fp8_gemm_pair_kernel<BN, COLVEC, ODD>, ml, mc, P) == cudaSuccess ? LAMP_OK : LAMP_ERR_CUDA;
 }
 
-template <int BN, bool COLVEC>
+template <int BN, bool COLVEC, bool ODD>
 lamp_status_t launch(const lamp_fp8_operand_t *l, const lamp_fp8_operand_t *c, const GemmParams &P, cudaStream_t st)
 {
     using L = GemmLayout<BN>;
     CUtensorMap ml, mc;
     if (!encode_operand(l, 128, &ml) || !encode_operand(c, BN, &mc)) return LAMP_ERR_CUDA;
     static SmemAttrOnce attr;
-    { const lamp_status_t as = attr.ensure(fp8_gemm_kernel<BN, COLVEC>, (int)L::TOTAL); if (as != LAMP_OK) return as; }
+    { const lamp_status_t as = attr.ensure(fp8_gemm_kernel<BN, COLVEC, ODD>, (int)L::TOTAL); if (as != LAMP_OK) return as; }
     const int sms = sm_count();
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(P.splits > 1 ? (unsigned)(P.tiles * P.splits) : (unsigned)(P.tiles < sms ? P.tiles : sms));
@@ -723,13 +754,21 @@ lamp_status_t launch(const lamp_fp8_operand_t *l, const lamp_fp8_operand_t *c, c
     }
     cfg.attrs = at;
     cfg.numAttrs = na;
-    return cudaLaunchKernelEx(&cfg, fp8_gemm_kernel<BN, COLVEC>, ml, mc, P) == cudaSuccess ? LAMP_OK : LAMP_ERR_CUDA;
+    return cudaLaunchKernelEx(&cfg, fp8_gemm_kernel<BN, COLVEC, ODD>, ml, mc, P) == cudaSuccess ? LAMP_OK : LAMP_ERR_CUDA;
 }
 
+bool odd_rows(const GemmParams &P) { return !P.swap && (P.vec == 0 || P.rows_c % 16 != 0); }
 template <int BN>
 lamp_status_t launch_cv(const lamp_fp8_operand_t *l, const lamp_fp8_operand_t *c, const GemmParams &P, cudaStream_t st)
 {
-    return c->tile_scale ? launch<BN, false>(l, c, P, st) : launch<BN, true>(l, c, P, st);
+    if (odd_rows(P)) return c->tile_scale ? launch<BN, false, true>(l, c, P, st) : launch<BN, true, true>(l, c, P, st);
+    return c->tile_scale ? launch<BN, false, false>(l, c, P, st) : launch<BN, true, false>(l, c, P, st);
+}
+template <int BN>
+lamp_status_t launch_pair(const lamp_fp8_operand_t *l, const lamp_fp8_operand_t *c, const GemmParams &P, cudaStream_t st)
+{
+    if (odd_rows(P)) return c->tile_scale ? launch_pair_k<BN, false, true>(l, c, P, st) : launch_pair_k<BN, true, true>(l, c, P, st);
+    return c->tile_scale ? launch_pair_k<BN, false, false>(l, c, P, st) : launch_pair_k<BN, true, false>(l, c, P, st);
 }
 
 // Clusters of `ctas` CTAs, one CTA per SM, that run at once: the SMs of a cluster belong to one GPC, so not every SM finds a
@@ -791,8 +830,7 @@ extern "C" lamp_status_t lamp_gemm_fp8(const lamp_fp8_operand_t *a, const lamp_f
         if (nl * nc * splits * 2 < sms * 3 / 4) continue;
         P.splits = splits;
         P.nl = (int32_t)nl; P.nc = (int32_t)nc; P.tiles = nl * nc;
-        if (bn == 256) return c->tile_scale ? launch_pair<256, false>(l, c, P, st) : launch_pair<256, true>(l, c, P, st);
-        return c->tile_scale ? launch_pair<128, false>(l, c, P, st) : launch_pair<128, true>(l, c, P, st);
+        return bn == 256 ? launch_pair<256>(l, c, P, st) : launch_pair<128>(l, c, P, st);
     }
     const int bn = P.rows_c <= 16 ? 16 : P.rows_c <= 32 ? 32 : P.rows_c <= 64 ? 64 : 128;
     P.nc = (P.rows_c + bn - 1) / bn;
