@@ -1,7 +1,10 @@
 // Distillation loss from a teacher's top logits, and its gradient:
 //   loss_r = T^2 sum_j p_j (log p_j - log q_{idx_j}),   dloss_r/dz_i = T (q_i S - sum_{j: idx_j = i} p_j),   S = sum_j p_j.
 // Bound by memory: a row of c logits is read once and its gradient written once.  The exponentials are taken relative to
-// the row's maximum, with the difference formed first, so q is as exact as fp32 allows whatever the size of the logits.
+// the row's maximum, with the difference formed first in every form, so q is as exact as fp32 allows whatever the size of the
+// logits (2^(z c - m c) with one rounded product m c is not: it carries half a unit of m c, a factor of 2^18 at logits of
+// -1e9, and infinity where one thread's first classes are all masked with -1e10).  Only the gradient alone starts from the
+// stored log-sum, whose rounding it carries.
 // The gradient of a listed class is the difference of two numbers that training makes nearly equal, so it is formed in
 // fp32 and rounded once: the dense pass writes q_i S everywhere, then the owner of each listed class overwrites it.
 // A class listed twice subtracts both probabilities (each of its entries writes the same value).
@@ -393,45 +396,40 @@ template <bool F32> __device__ __forceinline__ ptx::f32x2 unit_pair(const uint4 
     const uint32_t w = i == 0 ? r.x : i == 1 ? r.y : i == 2 ? r.z : r.w;
     return ptx::pack2(w << 16, w & 0xFFFF0000u);
 }
-// e^((z - m) / T) of a packed pair: 2^(z c - m c) in one packed FMA, or, where the products could overflow, the difference first
-template <bool SAFE> __device__ __forceinline__ ptx::f32x2 pair_exp(ptx::f32x2 z, float c, float m, float mc)
+// e^((z - m) / T) of a packed pair, c = log2(e) / T
+__device__ __forceinline__ ptx::f32x2 pair_exp(ptx::f32x2 z, float c, float m)
 {
     float a, b;
-    if (SAFE) {
-        ptx::unpack2(z, a, b);
-        a = (a - m) * c; b = (b - m) * c;
-    } else {
-        ptx::unpack2(ptx::fma2(z, ptx::twice(c), ptx::twice(-mc)), a, b);
-    }
+    ptx::unpack2(ptx::mul2(ptx::add2(z, ptx::twice(-m)), ptx::twice(c)), a, b);
     return ptx::pack2(__float_as_uint(ex2(a)), __float_as_uint(ex2(b)));
 }
 
-template <bool F32, bool SAFE>
-__device__ __forceinline__ float unit_sum(const uint4 &raw, float c, float m, float mc)
+template <bool F32>
+__device__ __forceinline__ float unit_sum(const uint4 &raw, float c, float m)
 {
     ptx::f32x2 s = 0;
 #pragma unroll
-    for (int j = 0; j < Elem<F32>::E / 2; ++j) s = ptx::add2(s, pair_exp<SAFE>(unit_pair<F32>(raw, j), c, m, mc));
+    for (int j = 0; j < Elem<F32>::E / 2; ++j) s = ptx::add2(s, pair_exp(unit_pair<F32>(raw, j), c, m));
     float a, b;
     ptx::unpack2(s, a, b);
     return a + b;
 }
 
-// gradient of a unit before the listed classes are taken off.  KIND 0: from maximum and sum; 1: the same where z c could
-// overflow; 2: from a given log-sum m: e^(z / T - m), the difference before the change of base (c = 1 / T)
-template <bool F32, int KIND>
-__device__ __forceinline__ uint4 unit_grad(const uint4 &raw, float c, float m, float mc, float gq)
+// gradient of a unit before the listed classes are taken off.  FWD in MODE: from the maximum m (c = log2(e) / T); else from a
+// given log-sum m: e^(z / T - m), the difference before the change of base (c = 1 / T)
+template <bool F32, int MODE>
+__device__ __forceinline__ uint4 unit_grad(const uint4 &raw, float c, float m, float gq)
 {
     uint32_t o[4];
 #pragma unroll
     for (int j = 0; j < Elem<F32>::E / 2; ++j) {
         ptx::f32x2 e = unit_pair<F32>(raw, j);
         float x, y;
-        if (KIND == 2) {
+        if constexpr (MODE & FWD) {
+            e = pair_exp(e, c, m);
+        } else {
             ptx::unpack2(ptx::mul2(ptx::fma2(e, ptx::twice(c), ptx::twice(-m)), ptx::twice(LOG2E)), x, y);
             e = ptx::pack2(__float_as_uint(ex2(x)), __float_as_uint(ex2(y)));
-        } else {
-            e = pair_exp<KIND == 1>(e, c, m, mc);
         }
         ptx::unpack2(ptx::mul2(e, ptx::twice(gq)), x, y);
         if constexpr (F32) {
@@ -531,15 +529,9 @@ distill_row_kernel(const DistillParams P)
 #pragma unroll
                 for (int i = 0; i < NU; ++i) m = fmaxf(m, unit_max<F32>(raw[i]));
                 m = warp_max_fast(m);
-                const float mc = m * c2;
                 float s = 0.f;
-                if (fabsf(mc) < 1e38f) {
 #pragma unroll
-                    for (int i = 0; i < NU; ++i) s += unit_sum<F32, false>(raw[i], c2, m, mc);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < NU; ++i) s += unit_sum<F32, true>(raw[i], c2, m, mc);
-                }
+                for (int i = 0; i < NU; ++i) s += unit_sum<F32>(raw[i], c2, m);
                 s = warp_sum(s);
                 if (s == 0.f) s = NAN;                                      // no logit above -inf: there is no softmax
                 const float ls = logf(s);
@@ -552,16 +544,12 @@ distill_row_kernel(const DistillParams P)
                 m = lse_in;
             }
             if constexpr (MODE & BWD) {
-                const float gT = w * P.temp, gq = gT * S * scale, mc = m * c2;
-                const bool fits = fabsf(mc) < 1e38f;
+                const float gT = w * P.temp, gq = gT * S * scale;
 #pragma unroll
                 for (int i = 0; i < NU; ++i) {
                     const int u = lane + 32 * i;
                     if (u >= nu) break;
-                    uint4 o;
-                    if constexpr (MODE & FWD) o = fits ? unit_grad<F32, 0>(raw[i], c2, m, mc, gq) : unit_grad<F32, 1>(raw[i], c2, m, mc, gq);
-                    else o = unit_grad<F32, 2>(raw[i], inv_t, m, mc, gq);
-                    put_unit<F32>(P.dz, dat, off, same, u, P.c, o);
+                    put_unit<F32>(P.dz, dat, off, same, u, P.c, unit_grad<F32, MODE>(raw[i], (MODE & FWD) ? c2 : inv_t, m, gq));
                 }
                 float pm[KE];
                 e.merge(P.k, k4, lane, p, pm, sh_ids[warp], sh_p[warp]);
@@ -797,14 +785,8 @@ distill_cta_kernel(const DistillParams P, const int S_CTAS)
                             for (int q = 0; q < 4; ++q)
                                 if (u + q * nthr < end) { raw[q] = buf[u + q * nthr]; top = fmaxf(top, unit_max<F32>(raw[q])); }
                             if (top > m) { s *= ex2((m - top) * c2); m = top; }
-                            const float mc = m * c2;
-                            if (fabsf(mc) < 1e38f) {
 #pragma unroll
-                                for (int q = 0; q < 4; ++q) if (u + q * nthr < end) s += unit_sum<F32, false>(raw[q], c2, m, mc);
-                            } else {
-#pragma unroll 1
-                                for (int q = 0; q < 4; ++q) if (u + q * nthr < end) s += unit_sum<F32, true>(buf[u + q * nthr], c2, m, mc);
-                            }
+                            for (int q = 0; q < 4; ++q) if (u + q * nthr < end) s += unit_sum<F32>(raw[q], c2, m);
                         }
                         if (!(MODE & BWD)) give_back(ch);              // the last pass
                     }
@@ -856,17 +838,13 @@ distill_cta_kernel(const DistillParams P, const int S_CTAS)
                     m = P.lse_in[row];
                 }
                 if constexpr (MODE & BWD) {
-                    const float gT = w * P.temp, gq = gT * S * scale, mc = m * c2;
-                    const int kind = !(MODE & FWD) ? 2 : fabsf(mc) < 1e38f ? 0 : 1;
+                    const float gT = w * P.temp, gq = gT * S * scale;
                     for (int ch = 0; ch < nch; ++ch) {
                         if (!(MODE & FWD) && !(ok = landed(ch))) break;
                         const int end = (ch + 1) * chunk < n ? (ch + 1) * chunk : n;
 #pragma unroll 2
                         for (int u = ch * chunk + tid; u < end; u += nthr) {
-                            uint4 o = buf[u];
-                            if constexpr (MODE & FWD) o = kind == 0 ? unit_grad<F32, 0>(o, c2, m, mc, gq) : unit_grad<F32, 1>(o, c2, m, mc, gq);
-                            else o = unit_grad<F32, 2>(o, inv_t, m, mc, gq);
-                            put_unit<F32>(P.dz, dat, off, same, u0 + u, P.c, o);
+                            put_unit<F32>(P.dz, dat, off, same, u0 + u, P.c, unit_grad<F32, MODE>(buf[u], (MODE & FWD) ? c2 : inv_t, m, gq));
                         }
                         give_back(ch);
                     }
