@@ -304,6 +304,7 @@ distill_warp_kernel(const DistillParams P)
             float m = -FLT_MAX, s = 0.f;
 #pragma unroll
             for (int i = 0; i < NU; ++i) if (lane + 32 * i < nu) raw[i] = load_unit<F32>(P.z, at, off, lane + 32 * i, P.c);
+            __syncwarp();                                           // the listed logits lie in other lanes' units: read before any is written
             float scale;                                            // 1 / sum, relative to the maximum
             if constexpr (MODE & FWD) {
 #pragma unroll
@@ -545,6 +546,7 @@ distill_row_kernel(const DistillParams P)
             }
             if constexpr (MODE & BWD) {
                 const float gT = w * P.temp, gq = gT * S * scale;
+                __syncwarp();                                               // every lane has the listed logits of its entries
 #pragma unroll
                 for (int i = 0; i < NU; ++i) {
                     const int u = lane + 32 * i;
