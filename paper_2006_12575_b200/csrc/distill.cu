@@ -151,39 +151,41 @@ __device__ __forceinline__ float warp_max_fast(float v)
     return __int_as_float(i ^ ((i >> 31) & 0x7fffffff));
 }
 // One warp reads the teacher's entries of a row: ids (-1: absent) and log p to shared memory; returns S (0: no entry left).
+// As for the student, the difference to the largest entry is formed before anything is divided by T.
 __device__ __forceinline__ float teacher_row(const DistillParams &P, int64_t row, int lane, int *ids, float *logp)
 {
-    const float inv_t = 1.f / P.temp;
-    float m = -INFINITY;
-    bool nan = false;
+    const float inv_t = 1.f / P.temp, tlse = P.tlse ? P.tlse[row] : 0.f;
+    float m = -FLT_MAX, S = 0.f;
+    bool some = false;
     for (int j = lane; j < P.k; j += 32) {
         int id = P.idx[row * P.k + j];
         if (id < 0 || id >= P.c) id = -1;
-        const float v = id >= 0 ? P.t[row * P.k + j] * inv_t : -INFINITY;
+        const float v = id >= 0 ? P.t[row * P.k + j] : -INFINITY;
         ids[j] = id;
         logp[j] = v;
-        nan |= v != v;
+        some |= v != -INFINITY;                                     // NaN counts
         m = fmaxf(m, v);
     }
-    nan = __any_sync(0xffffffffu, nan);
-    float lse;
+    if (!__any_sync(0xffffffffu, some)) return 0.f;
     if (P.tlse) {
-        lse = P.tlse[row];
-    } else {
-        const float mm = warp_max(m);
-        if (mm == -INFINITY && !nan) return 0.f;
-        float s = 0.f;
-        for (int j = lane; j < P.k; j += 32) s += expf(logp[j] - mm);
-        lse = mm + logf(warp_sum(s));
+        for (int j = lane; j < P.k; j += 32) {
+            logp[j] = fmaf(logp[j], inv_t, -tlse);
+            S += ids[j] >= 0 ? expf(logp[j]) : 0.f;
+        }
+        S = warp_sum(S);
+        __syncwarp();
+        return S;
     }
-    float S = 0.f;
+    m = warp_max_fast(m);
     for (int j = lane; j < P.k; j += 32) {
-        logp[j] -= lse;
+        logp[j] = (logp[j] - m) * inv_t;
         S += expf(logp[j]);
     }
     S = warp_sum(S);
+    const float ls = logf(S);
+    for (int j = lane; j < P.k; j += 32) logp[j] -= ls;
     __syncwarp();
-    return P.tlse || S != S ? S : 1.f;
+    return S == S ? 1.f : NAN;
 }
 
 // A row's teacher entries in the registers of a warp (k <= 32 KE), lane + 32 i, so that they can be loaded a row ahead.
@@ -997,9 +999,9 @@ distill_thread_kernel(const DistillParams P, const ThreadPlan G)
         // the teacher: S and, for every entry of a listed class, log p and p.  Short lists keep them in registers.
         int id4[SHORT ? 4 : 1];
         float lp4[SHORT ? 4 : 1], p4[SHORT ? 4 : 1];
-        float S = 0.f, lt = tl;                                        // log p = t / T - lt
+        float S = 0.f, mt = 0.f, lt = tl;                              // log p = (t - mt) / T - lt
         if constexpr (SHORT) {
-            float mt = -INFINITY;
+            mt = -INFINITY;
             bool nan = false;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -1025,20 +1027,24 @@ distill_thread_kernel(const DistillParams P, const ThreadPlan G)
                 for (int j = 0; j < 4; ++j) { lp4[j] = fmaf(lp4[j], inv_t, -lt); p4[j] = id4[j] >= 0 ? expf(lp4[j]) : 0.f; S += p4[j]; }
             }
         } else if (w != 0.f) {
-            float mt = -INFINITY;
-            bool nan = false;
-            for (int j = 0; j < k; ++j) {
-                if ((uint32_t)id_s[j] >= (uint32_t)c) continue;
-                nan |= t_s[j] != t_s[j];
-                mt = fmaxf(mt, t_s[j]);
+            if (P.tlse) {
+                for (int j = 0; j < k; ++j) if ((uint32_t)id_s[j] < (uint32_t)c) S += expf(fmaf(t_s[j], inv_t, -lt));
+            } else {
+                float top = -INFINITY;
+                bool nan = false;
+                for (int j = 0; j < k; ++j) {
+                    if ((uint32_t)id_s[j] >= (uint32_t)c) continue;
+                    nan |= t_s[j] != t_s[j];
+                    top = fmaxf(top, t_s[j]);
+                }
+                if (top != -INFINITY || nan) {
+                    float s = 0.f;
+                    for (int j = 0; j < k; ++j) if ((uint32_t)id_s[j] < (uint32_t)c) s += ex2((t_s[j] - top) * c2);
+                    mt = top;
+                    lt = logf(s);
+                    S = s == s ? 1.f : NAN;
+                }
             }
-            if (!P.tlse && (mt != -INFINITY || nan)) {
-                float s = 0.f;
-                for (int j = 0; j < k; ++j) if ((uint32_t)id_s[j] < (uint32_t)c) s += ex2((t_s[j] - mt) * c2);
-                lt = mt * inv_t + logf(s);
-                S = s == s ? 1.f : NAN;
-            }
-            if (P.tlse) for (int j = 0; j < k; ++j) if ((uint32_t)id_s[j] < (uint32_t)c) S += expf(fmaf(t_s[j], inv_t, -lt));
         }
         auto entries = [&](auto f) {                                   // f(class, log p, p)
             if constexpr (SHORT) {
@@ -1047,7 +1053,7 @@ distill_thread_kernel(const DistillParams P, const ThreadPlan G)
             } else {
                 for (int j = 0; j < k; ++j) {
                     const int id = id_s[j];
-                    if ((uint32_t)id < (uint32_t)c) { const float lp = fmaf(t_s[j], inv_t, -lt); f(id, lp, expf(lp)); }
+                    if ((uint32_t)id < (uint32_t)c) { const float lp = fmaf(t_s[j] - mt, inv_t, -lt); f(id, lp, expf(lp)); }
                 }
             }
         };

@@ -160,3 +160,27 @@ def test_rows_of_one_large_value_are_uniform(c, k, dt, temp):
     if dt is torch.bfloat16:
         tol = tol + 2.0 ** -8 * (np.abs(g) + tol)
     near(dz.view(rows, c).double().cpu().numpy(), g, tol, "gradient")
+
+
+@pytest.mark.parametrize("temp", [1.0, 1.5, 5.0])
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("c,k", FORMS + [(9, 8), (40, 32), (600, 32), (600, 128), (700, 512), (5000, 1000)])
+def test_teacher_far_from_zero(c, k, tail, temp):
+    """The teacher's logits moved by a common offset, masked with large negative values, or all of one value (then p = 1 / k)."""
+    r = np.random.default_rng(4)
+    t = (np.round(16 * 2 * r.standard_normal((12, k))) / 16).astype(np.float32)
+    low = np.finfo(np.float32).min
+    for i, v in enumerate([1e3, -1e3, 1e5, -1e5, 3e7]):
+        t[i] += np.float32(v)
+    t[5, : k // 2] = -1e9
+    t[6, k // 2 + 1:] = -1e30
+    t[7, ::2] = low
+    tlse = None
+    if tail:                                                             # the log-sum of the first eight and a tail
+        tt = t.astype(np.float64) / temp
+        tlse = (tt.max(1) + np.log(np.exp(tt - tt.max(1, keepdims=True)).sum(1)) + 0.3).astype(np.float32)
+        t, tlse = t[:8], tlse[:8]
+    else:
+        t[8], t[9], t[10], t[11] = -1e9, -1e30, low, -low
+    z = torch.from_numpy((2 * r.standard_normal((len(t), c))).astype(np.float32)).cuda()
+    check(z, listed(len(t), c, k), t, temp, tlse)
