@@ -76,13 +76,30 @@ __device__ __forceinline__ float both(ptx::f32x2 v)
     ptx::unpack2(v, a, b);
     return a + b;
 }
-// sigmoid: 2^x and the reciprocal are each within two units of the last place
-__device__ __forceinline__ float sigmoid(float x)
+// e^x for the gates.  From fp32 logits with expf; from bf16 ones without its correction for the rounding of x log2(e): that error
+// is 2^-24 |x| of e^x, so a gate of size e^-|x| is off by less than 2^-24 of one, and a bf16 gradient is rounded far more coarsely
+// (expf for both: 138 us against 133 on 81,840 x 320 backward, 66 against 60 on 131,072 x 256 forward, gate per element).
+template <bool FINE> __device__ __forceinline__ float gate_exp(float x)
 {
-    float e, r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x * -1.4426950408889634f));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+    if (FINE) return expf(x);
+    float e;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x * 1.4426950408889634f));
+    return e;
+}
+__device__ __forceinline__ float reciprocal(float x)               // within a unit of the last place
+{
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
+}
+template <bool FINE> __device__ __forceinline__ float sigmoid(float x) { return reciprocal(1.f + gate_exp<FINE>(-x)); }
+// g = sigmoid(x) and its slope g (1 - g), both to a few units of their own last place: from e^-|x|, so that nothing cancels (1 - g
+// from a rounded g has no digit left at x = 17)
+template <bool FINE> __device__ __forceinline__ void sigmoid_slope(float x, float &g, float &slope)
+{
+    const float e = gate_exp<FINE>(-fabsf(x)), r = reciprocal(1.f + e), er = e * r;
+    g = x >= 0.f ? r : er;
+    slope = er * r;
 }
 
 // Per-channel parameters sit in shared memory as [array][half][unit] float4, so that neighbouring threads read

@@ -167,11 +167,13 @@ block_norm_bwd_kernel(const BwdParams P)
                     if (in) load_par(par4, 2, units, unit, wb);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        float a, b;
+                        float a, b, ga, gb, sa, sb;
                         unpack2(g[j], a, b);
-                        g[j] = pack2(__float_as_uint(sigmoid(a)), __float_as_uint(sigmoid(b)));
+                        sigmoid_slope<BF>(a, ga, sa);
+                        sigmoid_slope<BF>(b, gb, sb);
+                        g[j] = pack2(__float_as_uint(ga), __float_as_uint(gb));
                         // dlogit = dt r N(y) g (1 - g)
-                        wb[j] = mul2(mul2(dt[u][j], fma2(yh[u][j], w[j], wb[j])), mul2(g[j], fma2(g[j], twice(-1.f), twice(1.f))));
+                        wb[j] = mul2(mul2(dt[u][j], fma2(yh[u][j], w[j], wb[j])), pack2(__float_as_uint(sa), __float_as_uint(sb)));
                         dt[u][j] = mul2(dt[u][j], g[j]);
                     }
                     if (in) store_pairs<BF>(P.dl, r * P.pdl + unit * 8, wb);

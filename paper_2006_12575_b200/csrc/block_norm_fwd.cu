@@ -118,7 +118,7 @@ block_norm_fwd_kernel(const FwdParams P)
                     if (LOGITS) {
                         float p, q;
                         unpack2(lg[u][j], p, q);
-                        branch = mul2(branch, pack2(__float_as_uint(sigmoid(p)), __float_as_uint(sigmoid(q))));
+                        branch = mul2(branch, pack2(__float_as_uint(sigmoid<BF>(p)), __float_as_uint(sigmoid<BF>(q))));
                     }
                     t[u][j] = add2(t[u][j], branch);
                     if constexpr (!SF) {                           // t as stored
