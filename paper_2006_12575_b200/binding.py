@@ -474,8 +474,8 @@ def block_norm(rms=False, eps=1e-5, post_w=None, post_b=None, pre_w=None, pre_b=
         ptr.append(_vec(v, c, "block_norm", dev))
     g = view = gate_shape = None
     if gate is not None:
-        gate_shape = (gate.numel(), gate.get_device())
-        g = _vec(gate, gate_shape[0], "gate", gate_shape[1])
+        gate_shape = (tuple(gate.shape), gate.get_device())
+        g = _vec(gate, gate.numel(), "gate", gate_shape[1])
     if gate_logits is not None:
         view = _view(gate_logits, gate_logits.get_device() if torch.is_tensor(gate_logits) else None, "gate_logits")
     p = BlockNorm(1 if rms else 0, eps, ptr[0], ptr[1], ptr[2], ptr[3], g, None if view is None else C.pointer(view), ptr[4])
@@ -488,11 +488,16 @@ def _norm_params(p, shape, dev):
     """The parameters, checked against the shape of the call's tensors."""
     if p.c is not None and (p.c != shape.c or p.dev != dev):
         raise ValueError(f"block_norm: vectors of {p.c} on cuda:{p.dev}, the tensors have {shape.c} channels on cuda:{dev}")
-    if p.gate_shape is not None and p.gate_shape != (shape.n * shape.c, dev):
-        raise ValueError(f"block_norm: gate of {p.gate_shape[0]} on cuda:{p.gate_shape[1]}, want [{shape.n}, {shape.c}] on cuda:{dev}")
+    if p.gate_shape is not None and (p.gate_shape[1] != dev or not _per_sample(p.gate_shape[0], shape)):
+        raise ValueError(f"block_norm: gate {p.gate_shape[0]} on cuda:{p.gate_shape[1]}, want [{shape.n}, {shape.c}] on cuda:{dev}")
     if p.logits is not None and torch.is_tensor(p.logits) and p.logits.get_device() != dev:
         raise ValueError(f"block_norm: gate_logits on {p.logits.device}, the current device is cuda:{dev}")
     return C.byref(p)
+
+
+def _per_sample(s, shape):
+    """Whether s is [n, c], with axes of one element left out or added between the two."""
+    return len(s) > 0 and s[-1] == shape.c and [i for i in s[:-1] if i != 1] == ([shape.n] if shape.n != 1 else [])
 
 
 def lamp_block_norm_fwd(p: BlockNorm, y, x, out, h=None, h_fp8=None):
@@ -514,6 +519,8 @@ def lamp_block_norm_bwd(p: BlockNorm, y, t, dout, dh, dx, dy, ws=None, dgate_log
     dev = torch.cuda.current_device()
     vt = _view(t, dev, "t")
     c = vt.c
+    if dgate is not None and not _per_sample(dgate.shape, vt):
+        raise ValueError(f"dgate: want [{vt.n}, {c}], got {tuple(dgate.shape)}")
     g = BlockNormGrads(_vec(dpost_w, c, "dpost_w", dev), _vec(dpost_b, c, "dpost_b", dev), _vec(dpre_w, c, "dpre_w", dev),
                        _vec(dpre_b, c, "dpre_b", dev), _vec(dgate, vt.n * c, "dgate", dev), _vec(dres_scale, c, "dres_scale", dev))
     if ws is not None and ws.get_device() != dev:
@@ -528,8 +535,9 @@ def lamp_block_norm_bwd(p: BlockNorm, y, t, dout, dh, dx, dy, ws=None, dgate_log
 def teacher_topk(idx, logits, temperature=1.0, lse=None) -> TeacherTopk:
     """The teacher's k listed classes per row: idx int32 [rows, k], logits fp32 [rows, k], lse fp32 [rows] or None."""
     t = TeacherTopk()
-    if idx.dim() != 2:
-        raise ValueError("teacher_topk: idx is a matrix [rows, k]")
+    if idx.dim() != 2 or logits.shape != idx.shape or (lse is not None and lse.numel() != idx.shape[0]):
+        raise ValueError(f"teacher_topk: idx and logits are matrices [rows, k], lse a vector [rows]; got {tuple(idx.shape)}, {tuple(logits.shape)}"
+                         + ("" if lse is None else f", {tuple(lse.shape)}"))
     t.k, t.temperature = idx.shape[1], temperature
     t.keep = (idx, logits, lse)
     return t
