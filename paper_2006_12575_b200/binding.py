@@ -169,7 +169,9 @@ def tensor(t: torch.Tensor, c=None, c_offset=0) -> Tensor:
     assert t.dim() == 5 and t.is_contiguous()
     dt = {torch.bfloat16: LAMP_BF16, torch.float32: LAMP_F32}[t.dtype]
     n, d, h, w, pitch = t.shape
-    return Tensor(t.data_ptr(), dt, n, d, h, w, pitch - c_offset if c is None else c, pitch, c_offset)
+    o = Tensor(t.data_ptr(), dt, n, d, h, w, pitch - c_offset if c is None else c, pitch, c_offset)
+    o.keep, o.dev = t, t.get_device()                               # the memory lives as long as its descriptor
+    return o
 
 
 def _td(x):
@@ -408,7 +410,11 @@ _VIEW_TYPES = {torch.bfloat16: LAMP_BF16, torch.float32: LAMP_F32}
 
 def _view(x, dev, what):
     """Descriptor of a tensor argument (torch tensor on the current device, or a Tensor); None stays None."""
-    if x is None or isinstance(x, Tensor):
+    if x is None:
+        return x
+    if isinstance(x, Tensor):
+        if getattr(x, "dev", dev) != dev:
+            raise ValueError(f"{what}: descriptor of a tensor on device {x.dev}, the current device is cuda:{dev}")
         return x
     s, dt = x.shape, _VIEW_TYPES.get(x.dtype)
     if dt is None or len(s) != 5 or x.get_device() != dev or not x.is_contiguous():
@@ -477,7 +483,7 @@ def block_norm(rms=False, eps=1e-5, post_w=None, post_b=None, pre_w=None, pre_b=
         gate_shape = (tuple(gate.shape), gate.get_device())
         g = _vec(gate, gate.numel(), "gate", gate_shape[1])
     if gate_logits is not None:
-        view = _view(gate_logits, gate_logits.get_device() if torch.is_tensor(gate_logits) else None, "gate_logits")
+        view = _view(gate_logits, gate_logits.get_device() if torch.is_tensor(gate_logits) else getattr(gate_logits, "dev", None), "gate_logits")
     p = BlockNorm(1 if rms else 0, eps, ptr[0], ptr[1], ptr[2], ptr[3], g, None if view is None else C.pointer(view), ptr[4])
     p.c, p.dev, p.gate_shape, p.logits = c, dev, gate_shape, gate_logits
     p.keep = (post_w, post_b, pre_w, pre_b, res_scale, gate, view)
@@ -490,8 +496,8 @@ def _norm_params(p, shape, dev):
         raise ValueError(f"block_norm: vectors of {p.c} on cuda:{p.dev}, the tensors have {shape.c} channels on cuda:{dev}")
     if p.gate_shape is not None and (p.gate_shape[1] != dev or not _per_sample(p.gate_shape[0], shape)):
         raise ValueError(f"block_norm: gate {p.gate_shape[0]} on cuda:{p.gate_shape[1]}, want [{shape.n}, {shape.c}] on cuda:{dev}")
-    if p.logits is not None and torch.is_tensor(p.logits) and p.logits.get_device() != dev:
-        raise ValueError(f"block_norm: gate_logits on {p.logits.device}, the current device is cuda:{dev}")
+    if p.logits is not None and (p.logits.get_device() if torch.is_tensor(p.logits) else getattr(p.logits, "dev", dev)) != dev:
+        raise ValueError(f"block_norm: gate_logits on another device than the current one, cuda:{dev}")
     return C.byref(p)
 
 

@@ -1,5 +1,8 @@
-"""What the binding refuses before any call: matrices of the right size in the wrong order (no GPU needed: the checks
-look at shapes and device numbers, -1 standing for host memory)."""
+"""What the binding refuses before any call: matrices of the right size in the wrong order, descriptors of memory on another device (no GPU
+needed: the checks look at shapes and device numbers, -1 standing for host memory)."""
+import gc
+import weakref
+
 import pytest
 import torch
 
@@ -28,3 +31,19 @@ def test_gate_is_per_sample_then_channel():
             B._norm_params(B.block_norm(gate=torch.zeros(shape)), like(2, 24), -1)
     with pytest.raises(ValueError):
         B._norm_params(B.block_norm(gate=torch.zeros(2, 24)), like(2, 24), 0)            # host memory, device 0
+
+
+def test_descriptors_keep_their_memory_and_their_device():
+    t = torch.zeros(1, 1, 1, 3, 24)
+    d = B.tensor(t, 8, 8)
+    alive = weakref.ref(t)
+    del t
+    gc.collect()
+    assert alive() is not None
+    assert B._view(d, -1, "x") is d
+    with pytest.raises(ValueError):
+        B._view(d, 0, "x")
+    with pytest.raises(ValueError):
+        B._norm_params(B.block_norm(gate_logits=d), like(1, 8), 0)
+    bare = like(1, 8)                                                     # built field by field: nothing to check
+    assert B._view(bare, 0, "x") is bare
