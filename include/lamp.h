@@ -296,7 +296,7 @@ typedef struct {
     const float   *logits;                /* [rows][k] */
     const float   *lse;                   /* [rows] or NULL */
     int32_t        k;                     /* 1 .. 1024 */
-    float          temperature;           /* > 0 */
+    float          temperature;           /* > 0; 2^-60 .. 2^60 */
 } lamp_teacher_topk_t;
 
 /* Scratch for `loss` (16-byte aligned); not needed where loss is NULL. */

@@ -1308,8 +1308,9 @@ lamp_status_t run(DistillParams &P, bool f32, float *loss, void *ws, cudaStream_
 
 lamp_status_t check_teacher(const lamp_teacher_topk_t *t)
 {
-    if (!t || t->k < 1 || !(t->temperature > 0.f) || t->temperature > 3.0e38f) return LAMP_ERR_INVALID_ARG;
+    if (!t || t->k < 1 || !(t->temperature > 0.f) || t->temperature > 3.402823466e+38f) return LAMP_ERR_INVALID_ARG;
     if (t->k > MAX_K) return LAMP_ERR_UNSUPPORTED;
+    if (t->temperature < 0x1p-60f || t->temperature > 0x1p60f) return LAMP_ERR_UNSUPPORTED;     // T^2 and log2(e) / T stay well inside fp32
     if (((uintptr_t)t->idx | (uintptr_t)t->logits | (uintptr_t)t->lse) & 3) return LAMP_ERR_INVALID_ARG;
     return LAMP_OK;
 }

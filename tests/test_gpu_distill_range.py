@@ -184,3 +184,12 @@ def test_teacher_far_from_zero(c, k, tail, temp):
         t[8], t[9], t[10], t[11] = -1e9, -1e30, low, -low
     z = torch.from_numpy((2 * r.standard_normal((len(t), c))).astype(np.float32)).cuda()
     check(z, listed(len(t), c, k), t, temp, tlse)
+
+
+@pytest.mark.parametrize("temp", [2.0 ** -60, 2.0 ** -20, 2.0 ** 20, 2.0 ** 60])
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("c,k", FORMS)
+def test_smallest_and_largest_temperatures(c, k, dt, temp):
+    r = np.random.default_rng(5)
+    z = torch.from_numpy((2 * temp * r.standard_normal((3, c))).astype(np.float32)).cuda().to(dt)
+    check(z, listed(3, c, k), (2 * temp * r.standard_normal((3, k))).astype(np.float32), temp)
