@@ -279,7 +279,7 @@ template <bool F32, int MODE>
 __global__ void __launch_bounds__(WR_WARPS * 32)
 distill_warp_kernel(const DistillParams P)
 {
-    constexpr int E = Elem<F32>::E, NU = WR_MAX_C / (32 * E) + (F32 ? 1 : 1);
+    constexpr int E = Elem<F32>::E, NU = WR_MAX_C / (32 * E) + 1;
     extern __shared__ int smem_i[];
     __shared__ double wl[WR_WARPS];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -1262,10 +1262,9 @@ lamp_status_t run(DistillParams &P, bool f32, float *loss, void *ws, cudaStream_
     P.part = loss ? (double *)ws : nullptr;
     P.status = status_word_ptr();
     if (P.c <= TR_MAX_C && P.k <= TR_MAX_K) {
-        const int turn = tr_rows(P.c <= TR_REG_C), room = 27;
+        const int turn = tr_rows(P.c <= TR_REG_C), room = MAX_PARTS / sms * sms;     // as many turns at a time as there are partial losses
         const int64_t need = (P.rows + turn - 1) / turn;
-        parts = (int)(need < (int64_t)room * sms ? need : (int64_t)room * sms);
-        if (parts > MAX_PARTS) parts = MAX_PARTS;
+        parts = (int)(need < room ? need : room);
         const bool vec = P.pz == P.c && ((uintptr_t)P.z & 15) == 0 && (!(MODE & BWD) || (P.pdz == P.c && ((uintptr_t)P.dz & 15) == 0));
         s = f32 ? launch_thread_c<true, MODE>(P, parts, vec, st) : launch_thread_c<false, MODE>(P, parts, vec, st);
     } else if (P.k <= SHORT_K && P.c <= (f32 ? 4 : 8) * (32 * RW_MAX_UNITS - 1)) {

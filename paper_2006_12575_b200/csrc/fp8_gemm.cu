@@ -493,7 +493,8 @@ bool encode_operand(const lamp_fp8_operand_t *o, int box_rows, CUtensorMap *map)
 // operand: 32 KB per CTA for the same work.  The leader (rank 0) issues the MMAs of both CTAs; full barriers live in the
 // leader (both CTAs' copies complete there), empty and accumulator-full barriers in each CTA (the commits arrive in both),
 // accumulator-empty barriers in the leader (the promotion warps of both CTAs arrive).
-// Warps 4 .. 11 promote: 128 sums per thread and 64 loaded values need 216 registers, which the other four warps give up (384 x 168 at launch = 128 x 72 + 256 x 216).
+// Warps 4 .. 11 promote: 128 sums per thread, 32 loaded values and their addresses need 216 registers, which the other four warps
+// give up (384 x 168 at launch = 128 x 72 + 256 x 216).
 template <int BN> struct PairLayout {
     static constexpr int A_BYTES = 128 * KB, C_BYTES = BN / 2 * KB, STAGE_BYTES = A_BYTES + C_BYTES;
     static constexpr int STAGES = BN == 256 ? 6 : 8;
@@ -503,6 +504,7 @@ template <int BN> struct PairLayout {
     static constexpr int SCALE_BYTES = RING * (128 + BN) * 4, OUT_BYTES = 8 * STAGE_FLOATS * 4;
     static constexpr int BAR_BYTES = (2 * MAX_STAGES + 2 * MAX_ACC + 2 * RING) * 8 + 16;
     static constexpr int TOTAL = 1024 + STAGES * STAGE_BYTES + SCALE_BYTES + OUT_BYTES + BAR_BYTES;
+    static_assert(BN * 128 * 4 <= STAGES * STAGE_BYTES, "the split-k parts reuse the stages");
     static_assert(TOTAL <= 227 * 1024 && STAGES <= MAX_STAGES && NACC <= MAX_ACC && NACC * BN <= TMEM_COLS, "");
 };
 
@@ -553,7 +555,7 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    // a cluster is S pairs that share the blocks of k of one tile; the even CTA of a pair leads it
+    // a cluster is S (1 or 2) pairs that share the blocks of k of one tile; the even CTA of a pair leads it
     const uint32_t cta = cluster_rank(), rank = cta & 1, leader = cta & ~1u;
     const int S = P.splits;
     const uint32_t full0 = smem_u32(bars), empty0 = smem_u32(bars + MAX_STAGES);
@@ -616,6 +618,8 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
 #pragma unroll
                 for (int k = 0; k < KB / 32; ++k)
                     umma_fp8_pair(tmem_base + acc * BN, da + 2 * k, dc + 2 * k, IDESC, k ? 1u : 0u);
+                // nobody waits for the last arrivals of the empty barriers in the other CTA; the accumulator's commit behind them,
+                // which its promotion warps do wait for, completes after them, so they land before that CTA leaves
                 umma_commit_pair(empty0 + 8 * stage, 3u << leader);
                 umma_commit_pair(tfull0 + 8 * acc, 3u << leader);
                 if ((stage += 2) >= STAGES) { stage -= STAGES; phase ^= 1; }
@@ -697,8 +701,7 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
             const int64_t row = (tile0 / P.nc) * 256 + rank * 128 + lane_row;
             const int col0 = (int)(tile0 % P.nc) * BN;
             const uint32_t base = smem_u32(smem);
-            if (S == 2) reduce_parts<ODD, CW, 2>(P, base, lane_row, row, half * CW, col0, split, rank, 2, stage);
-            else reduce_parts<ODD, CW, 4>(P, base, lane_row, row, half * CW, col0, split, rank, 2, stage);
+            reduce_parts<ODD, CW, 2>(P, base, lane_row, row, half * CW, col0, split, rank, 2, stage);
         }
     }
     tc_fence_before();
