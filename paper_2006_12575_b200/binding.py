@@ -503,7 +503,8 @@ def _norm_params(p, shape, dev):
 
 def _per_sample(s, shape):
     """Whether s is [n, c], with axes of one element left out or added between the two."""
-    return len(s) > 0 and s[-1] == shape.c and [i for i in s[:-1] if i != 1] == ([shape.n] if shape.n != 1 else [])
+    n, c = shape.n, shape.c
+    return s == (n, c) or (len(s) > 0 and s[-1] == c and [i for i in s[:-1] if i != 1] == ([n] if n != 1 else []))
 
 
 def lamp_block_norm_fwd(p: BlockNorm, y, x, out, h=None, h_fp8=None):
