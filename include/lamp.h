@@ -199,7 +199,7 @@ lamp_status_t lamp_instnorm_relu_bwd(const lamp_tensor_t *dz_a, const lamp_tenso
  *                                                   or  scale[(j / 128) * scale_pitch + r / 128]     (tile_scale = 1)
  * The scales are block-major, so that the 128 scales a tile of rows needs are one contiguous line.
  * q 16-byte aligned, q_pitch (bytes) a multiple of 16 and >= k; bytes behind k are neither read nor written.
- * scale 4-byte aligned, scale_pitch >= rows (tile_scale = 0) or >= ceil(rows / 128).  rows, k < 2^31.
+ * scale 4-byte aligned, scale_pitch >= rows (tile_scale = 0) or >= ceil(rows / 128).  rows, k < 2^31 - 256; a product needs k >= 1.
  * ---------------------------------------------------------------------- */
 typedef struct {
     void   *q;
@@ -221,7 +221,8 @@ lamp_status_t lamp_fp8_quantize(const lamp_tensor_t *x, int32_t transpose, const
 
 /* y[m][n] = bias[n] + sum_k a(m, k) * b(n, k), m = 0 .. a->rows - 1 (the voxels of y, n*d*h*w of them), n = 0 .. b->rows - 1
  * (the channels of y).  The products of one block of 128 are summed on the tensor cores, the blocks in fp32 with
- * their scales: y = bias + sum_blocks (sum_block qa qb) * sa * sb.  sa * sb must be finite in fp32.
+ * their scales: y = bias + sum_blocks (sum_block qa qb) * sa * sb.  sa * sb is formed
+ * in fp32: it must be finite, and below 2^-126 it loses digits (sums of less than about 2^-100).
  * y: bf16 or fp32, any c, c_pitch and c_offset.  bias: fp32 [n] or NULL.  The sum runs in a fixed order (results repeat
  * bit for bit).  No workspace: where few tiles would leave SMs idle, the CTAs of a cluster share the k axis of a tile and
  * add their parts through distributed shared memory. */
@@ -237,7 +238,8 @@ lamp_status_t lamp_gemm_fp8(const lamp_fp8_operand_t *a, const lamp_fp8_operand_
  *     rms = 1:  v / sqrt(mean(v^2) + eps) * w[c] + b[c].
  * h is the input of the NEXT block, so one pass serves the end of one block and the start of the next; h is the norm of
  * t as stored (rounded to the type of out), which is what the backward pass reads.
- * Arithmetic in fp32, mean and variance in two passes over the row.
+ * Arithmetic in fp32, mean and variance in two passes over the row: the sum of c squares has to stay inside fp32 (rows of up to about
+ * 10^17; beyond, the deviation is infinite and N(v) = b).
  * w, b, res_scale: fp32 [c] or NULL (1, 0, 1).  g = gate[n][c] (fp32), or sigmoid(gate_logits) per element, or 1 (both NULL).
  * Types: x, out and the gradients of them share one type, y, h, gate_logits and their gradients another; (bf16, bf16),
  * (fp32, bf16) or (fp32, fp32).  All tensors have the same n, d, h, w, c; c, c_pitch and c_offset are multiples of 8 and
@@ -286,7 +288,7 @@ lamp_status_t lamp_block_norm_bwd(const lamp_block_norm_t *p, const lamp_tensor_
  *     q_i = exp(z_i / T) / sum_i exp(z_i / T) over all c classes;
  *     loss_row = T^2 sum_j p_j (log p_j - log q_{idx_j}),      dloss_row / dz_i = T (q_i sum_j p_j - sum_{j: idx_j = i} p_j).
  * Entries with idx outside [0, c) are absent; p_j = 0 contributes 0; the same class listed twice counts twice.  A row
- * with no entry left (none listed, or all logits -inf) has loss, log-sum and gradient 0.  A class with z = -inf has q = 0; a
+ * with no entry left (none listed, all logits -inf, or every p_j 0) has loss, log-sum and gradient 0.  A class with z = -inf has q = 0; a
  * row of nothing but -inf has no softmax and gives NaN.
  * row_weight: fp32 [rows], or NULL for 1 / rows each.  Rows of weight 0 are not read: their loss, log-sum and gradient are 0.
  * Sums are held in fp32 (log-sums, losses of a row) and fp64 (over rows), in a fixed order.
@@ -306,7 +308,9 @@ size_t        lamp_distill_topk_workspace_bytes(const lamp_tensor_t *z);
 lamp_status_t lamp_distill_topk_fwd(const lamp_tensor_t *z, const lamp_teacher_topk_t *teacher, const float *row_weight,
                                     float *loss_rows, float *lse, float *loss, void *ws, size_t ws_bytes, void *cuda_stream);
 /* dz = row_grad[row] * dloss_row / dz in the type of z (row_grad: fp32 [rows] or NULL for 1 / rows; rows of gradient 0 are not
- * read).  dz may be z (the same view). */
+ * read).  dz may be z (the same view).  q comes from the stored log-sum, e^(z / T - lse), and carries its rounding, up to
+ * 2^-24 (|lse| + |z| / T) of q: for logits far from 0 as a whole row (masks among ordinary logits do no harm) take the fused call, which
+ * works from the row's maximum. */
 lamp_status_t lamp_distill_topk_bwd(const lamp_tensor_t *z, const lamp_teacher_topk_t *teacher, const float *row_grad,
                                     const float *lse, lamp_tensor_t *dz, void *cuda_stream);
 /* Loss and gradient of sum_r row_weight[r] * loss_rows[r] in one pass over the logits.  dz may be z. */

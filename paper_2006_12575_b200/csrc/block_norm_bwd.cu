@@ -3,7 +3,7 @@
 //     a  = dh w_pre,        dt = dout + rstd_t (a - mean(a) - th mean(a th)),          dx = dt
 //     b  = dt r g w_post,   dy = rstd_y (b - mean(b) - yh mean(b yh)),                 dlogit = dt r (yh w_post + b_post) g (1 - g)
 // Means and deviations are computed again from the rows, which are read anyway.  Bound by memory: t, y, dout, dh read once, dx
-// and dy written once (134 us on 81,840 x 320, fp32 stream, gate per element, at a floor of 88).
+// and dy written once (133 us with the finish kernel on 81,840 x 320, fp32 stream, gate per element, at a floor of 88).
 // Parameter gradients are sums over voxels of four products per channel, P = dt g' yh, Q = dt g' (g' = the gate where it has
 // a value per element, else 1), dh th and dh: each thread adds them up for its own channels over the rows it works on, a CTA
 // joins its threads in a fixed order and leaves one row of 4 c partial sums in the workspace; block_norm_finish_kernel adds
@@ -28,8 +28,8 @@ struct BwdParams {
 };
 
 // The running sums of a row group sit in shared memory, [sum][half][slot] float4 with slot = group * units + unit: 64 or
-// more accumulators per thread would leave 8 warps per SM (measured on 81,840 x 320, fp32 stream, gate per element: 265 us;
-// in shared memory, with packed fp32 arithmetic, 126).
+// more accumulators per thread would leave 8 warps per SM (measured on 81,840 x 320, fp32 stream, gate per element, this
+// kernel alone: 265 us; in shared memory, with packed fp32 arithmetic, 129).
 template <bool SF, bool BF, int TPR, int U, int MAXT, int MINB, bool LOGITS>
 __global__ void __launch_bounds__(MAXT, MINB)
 block_norm_bwd_kernel(const BwdParams P)

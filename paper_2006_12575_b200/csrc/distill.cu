@@ -598,7 +598,7 @@ distill_row_kernel(const DistillParams P)
 // Measured (4096 x 50001 bf16, loss and gradient, us): loads by the threads that use them 348; one CTA per SM with two row
 // buffers 327; the same with the row held in registers and packed fp32 arithmetic 240 (loss alone 112, gradient alone 131:
 // the phases of a row simply add up when all warps of an SM share it); two CTAs per SM with passes for maximum, sum and
-// gradient over a row that has landed 189 (loss alone 148, gradient alone 151); this form 191 (111, 147).
+// gradient over a row that has landed 189 (loss alone 148, gradient alone 151); this form 192 (117, 151).
 struct RowSlot {                                    // what the helper prepares for a row
     float S, w;
 };
