@@ -192,6 +192,39 @@ lamp_status_t lamp_instnorm_relu_bwd(const lamp_tensor_t *dz_a, const lamp_tenso
                                      double *sums, lamp_tensor_t *dy, void *cuda_stream);
 
 /* ------------------------------------------------------------------------
+ * Group norm with an activation, channels last.  No passage of the paper (its blocks use InstanceNorm, above): the norm of networks
+ * whose samples are few, in the place of lamp_instnorm_relu_fwd / _bwd.  A group is c / groups consecutive channels of one sample; with
+ * m = d*h*w*c/groups values in it, mean and var = sum (x - mean)^2 / m over them,
+ *     t = (x - mean) * rstd * w[c] + b[c],   rstd = 1 / sqrt(var + eps),   z = act(t),
+ *     act: t;   t > 0 ? t : slope * t;   t / (1 + e^-t);   t * (1 + erf(t / sqrt(2))) / 2.
+ * Tensors: x and dx of one type, z and dz of another: (bf16, bf16), (fp32, fp32) or (fp32, bf16); all of the same n, d, h, w, c, any channel
+ * slices; c, c_pitch and c_offset are multiples of 8.  Arithmetic in fp32; the sums of a thread run about a value of its own data, those
+ * of a group in fp64, in a fixed order.  A group with a value that is not finite becomes NaN.
+ * ---------------------------------------------------------------------- */
+enum { LAMP_ACT_NONE = 0, LAMP_ACT_LEAKY_RELU = 1, LAMP_ACT_SILU = 2, LAMP_ACT_GELU = 3 };
+typedef struct {
+    int32_t groups;                       /* divides c; c: instance norm, 1: all channels of a sample together */
+    int32_t act;
+    float   slope;                        /* of the leaky ReLU, 0 = ReLU; finite */
+    float   eps;                          /* >= 0 */
+    const float *w, *b;                   /* fp32 [c] or NULL (1, 0) */
+} lamp_group_norm_t;
+
+/* Scratch of either pass (16-byte aligned). */
+size_t        lamp_group_norm_workspace_bytes(const lamp_group_norm_t *p, const lamp_tensor_t *x);
+/* stats: NULL, or fp64 [n][c][2], the sums and sums of squares per channel as lamp_conv3d_fwd adds them up: x is then read once.
+ * mean_rstd: fp32 [n][groups][2], (mean, rstd), needed again by the backward call; t is computed from the rounded values, as there.
+ * z may be x (the same view, the same type). */
+lamp_status_t lamp_group_norm_act_fwd(const lamp_group_norm_t *p, const lamp_tensor_t *x, const double *stats, lamp_tensor_t *z,
+                                      float *mean_rstd, void *ws, size_t ws_bytes, void *cuda_stream);
+/* With xhat = (x - mean) * rstd and dt = dz * act'(t) (act'(0) = slope for the leaky ReLU):
+ *     dw = sum dt * xhat,  db = sum dt  over samples and voxels (fp32 [c], each may be NULL),
+ *     dx = rstd * (w dt - mean_g(w dt) - xhat * mean_g(w dt xhat)), the means over the group (mean and rstd taken as functions of x).
+ * dx may be dz or x (the same view, the same type). */
+lamp_status_t lamp_group_norm_act_bwd(const lamp_group_norm_t *p, const lamp_tensor_t *dz, const lamp_tensor_t *x, const float *mean_rstd,
+                                      lamp_tensor_t *dx, float *dw, float *db, void *ws, size_t ws_bytes, void *cuda_stream);
+
+/* ------------------------------------------------------------------------
  * Channel-mixing (pointwise) layers in 8 bits.  No passage of the paper: they stand beside the dense bf16 convolutions
  * for the 1x1x1 layers of a network (bottleneck, head, the linear layers of a token block over the voxels).
  * An operand of the matrix product is a matrix [rows][k], k being the axis the product sums over:
@@ -227,6 +260,47 @@ lamp_status_t lamp_fp8_quantize(const lamp_tensor_t *x, int32_t transpose, const
  * bit for bit).  No workspace: where few tiles would leave SMs idle, the CTAs of a cluster share the k axis of a tile and
  * add their parts through distributed shared memory. */
 lamp_status_t lamp_gemm_fp8(const lamp_fp8_operand_t *a, const lamp_fp8_operand_t *b, const float *bias, lamp_tensor_t *y,
+                            void *cuda_stream);
+
+/* ------------------------------------------------------------------------
+ * Channel-mixing layers in 4 bits, microscaled: the operands of lamp_gemm_fp8 at half the bytes, on tensor cores that apply the scales.
+ * An operand is a matrix [rows][k], k being the axis the product sums over:
+ *   element (r, j) = code(r, j) * scale(r, j / block) * g
+ *   code: e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6; bit 3 = sign), two in a byte: q[r * q_pitch + j / 2], even j in the low half;
+ *   block = 32: scale e8m0, 2^(byte - 127), byte 255 = NaN; tensor_scale must be NULL (g = 1);
+ *   block = 16: scale e4m3 (sign 0; 0x7F = NaN); g = *tensor_scale (fp32 on the device), or 1 (NULL).
+ *   The scale of (r, i) is the byte ((r / 128) * ceil(kb / 4) + i / 4) * 512 + (r % 32) * 16 + (r % 128) / 32 * 4 + i % 4 with kb = ceil(k / block):
+ *   tiles of 128 rows x 4 blocks in the order in which tensor memory takes them; lamp_fp4_scale_bytes in all.
+ * q and scale 16-byte aligned, q_pitch (bytes) a multiple of 16 and >= ceil(k / 2).  Bytes behind ceil(k / 2) are neither read nor
+ * written; with an odd k the high half of a row's last byte has to be 0, and the scales of blocks that the last tile of a row has beyond kb
+ * must not be NaN (the quantiser writes 0 in both, and 0 for rows behind the last).  rows, k < 2^31 - 256; a product needs k >= 1.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+    void        *q;
+    int64_t      q_pitch;
+    uint8_t     *scale;
+    const float *tensor_scale;
+    int64_t      rows, k;
+    int32_t      block;                   /* 16 or 32 */
+} lamp_fp4_operand_t;
+
+/* Bytes of the scales of an operand (0 for invalid arguments). */
+size_t        lamp_fp4_scale_bytes(int64_t rows, int64_t k, int32_t block);
+/* Quantises x (bf16 or fp32, any channel slice) into `out`.  transpose = 0: rows = voxels of x, k = channels; 1: rows = channels, k = voxels
+ * (the operands of a weight gradient).  With amax = the largest |x| of a block:
+ *   block = 32: scale = the smallest power of two with amax <= 6 * scale, not below 2^-127;
+ *   block = 16: scale = e4m3(amax / (6 g)), rounded to nearest even, kept within 2^-9 .. 448; the product scale * g is formed in fp32 and has to
+ *               be a normal number (with g = amax of the tensor / 2688, or that rounded up to a power of two, every block fits);
+ *   code = x / (scale * g), in fp32, to the nearest code, ties to the even one, at most 6.
+ * A block with an element that is not finite gets the NaN scale.  c, c_pitch and c_offset are multiples of 8. */
+lamp_status_t lamp_fp4_quantize(const lamp_tensor_t *x, int32_t transpose, const lamp_fp4_operand_t *out, void *cuda_stream);
+/* The values an operand stands for: code * (scale * g), products in fp32, rounded to the type of y (bf16 holds them exactly where g is a
+ * power of two and they are normal).  transpose and shapes as in lamp_fp4_quantize. */
+lamp_status_t lamp_fp4_dequantize(const lamp_fp4_operand_t *in, int32_t transpose, lamp_tensor_t *y, void *cuda_stream);
+/* y[m][n] = bias[n] + ga gb sum_k a(m, k) b(n, k), a and b without their g; m = 0 .. a->rows - 1 (the voxels of y), n = 0 .. b->rows - 1 (its
+ * channels).  Both operands have the same block.  Products of codes and scales are exact, their sum is held in fp32 and runs in a fixed order.  y: bf16 or
+ * fp32, any c, c_pitch and c_offset.  bias: fp32 [n] or NULL.  No workspace. */
+lamp_status_t lamp_gemm_fp4(const lamp_fp4_operand_t *a, const lamp_fp4_operand_t *b, const float *bias, lamp_tensor_t *y,
                             void *cuda_stream);
 
 /* ------------------------------------------------------------------------
@@ -490,6 +564,34 @@ lamp_status_t lamp_overlap_add(const float *patch_probs, int32_t k, int32_t d, i
  * that the network calls read), one for the biases (param_bf16 = NULL, master = the bias vector). */
 lamp_status_t lamp_rmsprop_step(int64_t n, const float *grad, float *master, float *v, void *param_bf16,
                                 float lr, float alpha, float eps, void *cuda_stream);
+
+/* The same update with every gradient first multiplied by *grad_scale (fp32 on the device): the factor that lamp_grad_norm leaves, so that
+ * clipping by the global norm costs no pass over the gradients of its own. */
+lamp_status_t lamp_rmsprop_step_scaled(int64_t n, const float *grad, const float *grad_scale, float *master, float *v,
+                                       void *param_bf16, float lr, float alpha, float eps, void *cuda_stream);
+
+/* ------------------------------------------------------------------------
+ * Global norm of the gradients of many tensors, and clipping by it (no passage of the paper; for the update above).
+ *     norm = sqrt(sum over all tensors of g^2),   factor = 1 where norm <= max_norm, else max_norm / norm,   out = g * factor.
+ * So factor is 0 for an infinite norm and NaN for a norm that is NaN; g * factor follows IEEE rules (an infinite g then gives NaN).
+ * Squares are added in fp32 over 8 neighbours (in fp64 where that would leave its range) and in fp64 beyond, in a fixed order.
+ * max_norm >= 0 (infinite: the norm alone).  No tensors, or empty ones: norm 0, factor 1.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+    const void *g;                        /* n elements, contiguous; aligned to an element */
+    void       *out;                      /* g itself, or n elements that overlap no tensor of the list; not read by lamp_grad_norm */
+    int64_t     n;                        /* 0 .. 2^40 */
+    int32_t     dtype;                    /* of both */
+} lamp_grad_t;
+
+/* Scratch of the two calls below (16-byte aligned).  grads: a host array of count entries (0 .. 2^20). */
+size_t        lamp_grad_norm_workspace_bytes(const lamp_grad_t *grads, int32_t count);
+/* norm, factor: fp32 scalars on the device; factor may be NULL (norm alone). */
+lamp_status_t lamp_grad_norm(const lamp_grad_t *grads, int32_t count, float max_norm, float *norm, float *factor,
+                             void *ws, size_t ws_bytes, void *cuda_stream);
+/* lamp_grad_norm and out = g * factor, rounded to the tensor's type.  Where factor is 1 a tensor with out = g is not written. */
+lamp_status_t lamp_grad_clip(const lamp_grad_t *grads, int32_t count, float max_norm, float *norm, float *factor,
+                             void *ws, size_t ws_bytes, void *cuda_stream);
 
 /* Synchronises `cuda_stream`, then returns and clears the device-side status word
  * (LAMP_OK, or LAMP_ERR_TIMEOUT if a bounded wait inside a kernel ran out). */

@@ -60,6 +60,19 @@ class TeacherTopk(C.Structure):
     _fields_ = [("idx", C.c_void_p), ("logits", C.c_void_p), ("lse", C.c_void_p), ("k", C.c_int32), ("temperature", C.c_float)]
 
 
+class Fp4Operand(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("q_pitch", C.c_int64), ("scale", C.c_void_p), ("tensor_scale", C.c_void_p), ("rows", C.c_int64),
+                ("k", C.c_int64), ("block", C.c_int32)]
+
+
+class GroupNorm(C.Structure):
+    _fields_ = [("groups", C.c_int32), ("act", C.c_int32), ("slope", C.c_float), ("eps", C.c_float), ("w", C.c_void_p), ("b", C.c_void_p)]
+
+
+class Grad(C.Structure):
+    _fields_ = [("g", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32)]
+
+
 _lib = None
 
 
@@ -74,6 +87,7 @@ def lib():
         TP, DP, SP = C.POINTER(Tensor), C.POINTER(ConvDesc), C.POINTER(UNetSpec)
         I3 = C.POINTER(C.c_int32)
         FP, NP, GP, KP = C.POINTER(Fp8Operand), C.POINTER(BlockNorm), C.POINTER(BlockNormGrads), C.POINTER(TeacherTopk)
+        QP, UP, RP = C.POINTER(Fp4Operand), C.POINTER(GroupNorm), C.POINTER(Grad)
         sig = {
             "lamp_conv3d_workspace_bytes": (sz, [DP, TP, C.c_int]),
             "lamp_conv3d_workspace_min_bytes": (sz, [DP, TP, C.c_int]),
@@ -91,6 +105,13 @@ def lib():
             "lamp_se_apply_bwd": (C.c_int, [TP, vp, vp, TP, vp]),
             "lamp_fp8_quantize": (C.c_int, [TP, i32, FP, vp]),
             "lamp_gemm_fp8": (C.c_int, [FP, FP, vp, TP, vp]),
+            "lamp_fp4_scale_bytes": (sz, [C.c_int64, C.c_int64, i32]),
+            "lamp_fp4_quantize": (C.c_int, [TP, i32, QP, vp]),
+            "lamp_fp4_dequantize": (C.c_int, [QP, i32, TP, vp]),
+            "lamp_gemm_fp4": (C.c_int, [QP, QP, vp, TP, vp]),
+            "lamp_group_norm_workspace_bytes": (sz, [UP, TP]),
+            "lamp_group_norm_act_fwd": (C.c_int, [UP, TP, vp, TP, vp, vp, sz, vp]),
+            "lamp_group_norm_act_bwd": (C.c_int, [UP, TP, TP, vp, TP, vp, vp, vp, sz, vp]),
             "lamp_block_norm_fwd": (C.c_int, [NP, TP, TP, TP, TP, FP, vp]),
             "lamp_block_norm_bwd_workspace_bytes": (sz, [TP, NP]),
             "lamp_block_norm_bwd": (C.c_int, [NP, TP, TP, TP, TP, TP, TP, TP, GP, vp, sz, vp]),
@@ -119,6 +140,10 @@ def lib():
             "lamp_sliding_window_infer": (C.c_int, [vp, vp, vp, TP, I3, f32, i32, i32, vp, vp, vp, sz, vp]),
             "lamp_overlap_add": (C.c_int, [vp, i32, i32, i32, i32, I3, f32, i32, vp, vp, vp]),
             "lamp_rmsprop_step": (C.c_int, [C.c_int64, vp, vp, vp, vp, f32, f32, f32, vp]),
+            "lamp_rmsprop_step_scaled": (C.c_int, [C.c_int64, vp, vp, vp, vp, vp, f32, f32, f32, vp]),
+            "lamp_grad_norm_workspace_bytes": (sz, [RP, i32]),
+            "lamp_grad_norm": (C.c_int, [RP, i32, f32, vp, vp, vp, sz, vp]),
+            "lamp_grad_clip": (C.c_int, [RP, i32, f32, vp, vp, vp, sz, vp]),
             "lamp_get_async_status": (C.c_int, [vp]),
             "lamp_selftest_wait_timeout": (C.c_int, [vp]),
             "lamp_status_string": (C.c_char_p, [C.c_int]),
@@ -136,7 +161,8 @@ EXPORTS = ["lamp_conv3d_workspace_bytes", "lamp_conv3d_workspace_min_bytes", "la
            "lamp_conv3d_wgrad",
            "lamp_instnorm_relu_fwd", "lamp_instnorm_relu_bwd",
            "lamp_se_squeeze", "lamp_se_excite", "lamp_se_apply_fwd", "lamp_se_bwd_reduce", "lamp_se_excite_bwd", "lamp_se_apply_bwd",
-           "lamp_fp8_quantize", "lamp_gemm_fp8", "lamp_block_norm_fwd", "lamp_block_norm_bwd_workspace_bytes", "lamp_block_norm_bwd",
+           "lamp_fp8_quantize", "lamp_gemm_fp8", "lamp_fp4_scale_bytes", "lamp_fp4_quantize", "lamp_fp4_dequantize", "lamp_gemm_fp4",
+           "lamp_group_norm_workspace_bytes", "lamp_group_norm_act_fwd", "lamp_group_norm_act_bwd", "lamp_block_norm_fwd", "lamp_block_norm_bwd_workspace_bytes", "lamp_block_norm_bwd",
            "lamp_distill_topk_workspace_bytes", "lamp_distill_topk_fwd", "lamp_distill_topk_bwd", "lamp_distill_topk_fwd_bwd",
            "lamp_unet_create", "lamp_unet_se_layout", "lamp_unet_destroy",
            "lamp_unet_num_layers", "lamp_unet_weight_count", "lamp_unet_bias_count", "lamp_unet_param_layout",
@@ -144,7 +170,7 @@ EXPORTS = ["lamp_conv3d_workspace_bytes", "lamp_conv3d_workspace_min_bytes", "la
            "lamp_unet_train_step_buckets", "lamp_sliding_window_num_patches", "lamp_sliding_window_partial",
            "lamp_sliding_window_finish",
            "lamp_sliding_window_workspace_bytes", "lamp_sliding_window_infer", "lamp_overlap_add",
-           "lamp_rmsprop_step", "lamp_get_async_status", "lamp_selftest_wait_timeout", "lamp_status_string", "lamp_version"]
+           "lamp_rmsprop_step", "lamp_rmsprop_step_scaled", "lamp_grad_norm_workspace_bytes", "lamp_grad_norm", "lamp_grad_clip", "lamp_get_async_status", "lamp_selftest_wait_timeout", "lamp_status_string", "lamp_version"]
 
 
 def _check(st, what):
@@ -599,6 +625,156 @@ def lamp_distill_topk_fwd_bwd(z, teacher: TeacherTopk, row_weight, loss_rows, lo
 def lamp_rmsprop_step(grad, master, v, param_bf16=None, lr=1e-3, alpha=0.99, eps=1e-8):
     _check(lib().lamp_rmsprop_step(grad.numel(), _ptr(grad), _ptr(master), _ptr(v), _ptr(param_bf16), lr, alpha, eps,
                                    _stream()), "lamp_rmsprop_step")
+
+
+# --- group norm with an activation ---------------------------------------------------------------------------------
+ACTIVATIONS = {"none": 0, "leaky_relu": 1, "silu": 2, "gelu": 3}
+
+
+def group_norm(groups, w=None, b=None, act="none", slope=0.0, eps=1e-5) -> GroupNorm:
+    """Parameters of lamp_group_norm_act_fwd / _bwd: w, b fp32 [c]; act a name of ACTIVATIONS ("leaky_relu" with slope 0 is ReLU)."""
+    c, dev, ptr = None, None, []
+    for v in (w, b):
+        if v is not None and c is None:
+            c, dev = v.numel(), v.get_device()
+        ptr.append(None if v is None else _vec(v, c, "group_norm", dev))
+    if act not in ACTIVATIONS:
+        raise ValueError(f"group_norm: act is one of {', '.join(ACTIVATIONS)}, got {act!r}")
+    p = GroupNorm(groups, ACTIVATIONS[act], slope, eps, ptr[0], ptr[1])
+    p.c, p.dev, p.keep = c, dev, (w, b)
+    return p
+
+
+def _group_params(p, shape, dev):
+    if getattr(p, "c", None) is not None and (p.c != shape.c or p.dev != dev):
+        raise ValueError(f"group_norm: vectors of {p.c} on cuda:{p.dev}, the tensors have {shape.c} channels on cuda:{dev}")
+    return C.byref(p)
+
+
+def lamp_group_norm_workspace_bytes(p: GroupNorm, x):
+    return lib().lamp_group_norm_workspace_bytes(C.byref(p), C.byref(_td(x)))
+
+
+def lamp_group_norm_act_fwd(p: GroupNorm, x, z, mean_rstd, ws=None, stats=None):
+    dev = torch.cuda.current_device()
+    vx = _view(x, dev, "x")
+    w, nbytes = _scratch(ws, dev)
+    _check(lib().lamp_group_norm_act_fwd(_group_params(p, vx, dev), C.byref(vx), _vec(stats, 2 * vx.n * vx.c, "stats", dev, torch.float64),
+                                         _byref(_view(z, dev, "z")), _vec(mean_rstd, 2 * vx.n * p.groups, "mean_rstd", dev), w, nbytes,
+                                         _raw_stream(dev)), "lamp_group_norm_act_fwd")
+
+
+def lamp_group_norm_act_bwd(p: GroupNorm, dz, x, mean_rstd, dx, dw=None, db=None, ws=None):
+    dev = torch.cuda.current_device()
+    vx = _view(x, dev, "x")
+    w, nbytes = _scratch(ws, dev)
+    _check(lib().lamp_group_norm_act_bwd(_group_params(p, vx, dev), _byref(_view(dz, dev, "dz")), C.byref(vx),
+                                         _vec(mean_rstd, 2 * vx.n * p.groups, "mean_rstd", dev), _byref(_view(dx, dev, "dx")),
+                                         _vec(dw, vx.c, "dw", dev), _vec(db, vx.c, "db", dev), w, nbytes, _raw_stream(dev)), "lamp_group_norm_act_bwd")
+
+
+# --- 4-bit layers --------------------------------------------------------------------------------------------------
+def lamp_fp4_scale_bytes(rows, k, block=32):
+    return lib().lamp_fp4_scale_bytes(rows, k, block)
+
+
+def fp4_operand(q, scale, rows=None, k=None, block=32, tensor_scale=None) -> Fp4Operand:
+    """Operand [rows][k] of lamp_gemm_fp4: q uint8 [rows, pitch], two codes a byte; scale uint8, lamp_fp4_scale_bytes(rows, k, block) of them in
+    their tiles; tensor_scale fp32 scalar on the device or None."""
+    dev = q.get_device()
+    if q.dtype is not torch.uint8 or scale.dtype is not torch.uint8 or dev < 0 or scale.get_device() != dev or q.dim() != 2 or not scale.is_contiguous():
+        raise ValueError("fp4_operand: q is a CUDA uint8 matrix, scale a contiguous uint8 tensor on the same device")
+    (qr, qc), (qp, q1) = q.shape, q.stride()
+    if rows is None:
+        rows = qr
+    if k is None:
+        k = 2 * qc
+    if block not in (16, 32):
+        raise ValueError(f"fp4_operand: blocks of 16 or 32, got {block}")
+    need = (rows + 127) // 128 * (((k + block - 1) // block + 3) // 4) * 512
+    if rows < 0 or k < 0 or rows > qr or (k + 1) // 2 > qc or (q1 != 1 and qc > 1) or scale.numel() < need:
+        raise ValueError(f"fp4_operand: [{rows}, {k}] in blocks of {block} does not fit q {tuple(q.shape)} and {scale.numel()} scales")
+    # the stride of an axis of one element says nothing: the pitch only has to cover the row
+    if qr <= 1:
+        qp = (max(qp, qc) + 15) // 16 * 16
+    o = Fp4Operand(q.data_ptr(), qp, scale.data_ptr(), _vec(tensor_scale, 1, "tensor_scale", dev), rows, k, block)
+    o.keep, o.dev = (q, scale, tensor_scale), dev
+    return o
+
+
+def lamp_fp4_quantize(x, out: Fp4Operand, transpose=False):
+    dev = torch.cuda.current_device()
+    _check(lib().lamp_fp4_quantize(_byref(_view(x, dev, "x")), 1 if transpose else 0, _operand(out, dev, "out"), _raw_stream(dev)), "lamp_fp4_quantize")
+
+
+def lamp_fp4_dequantize(op: Fp4Operand, y, transpose=False):
+    dev = torch.cuda.current_device()
+    _check(lib().lamp_fp4_dequantize(_operand(op, dev, "op"), 1 if transpose else 0, _byref(_view(y, dev, "y")), _raw_stream(dev)), "lamp_fp4_dequantize")
+
+
+def lamp_gemm_fp4(a: Fp4Operand, b: Fp4Operand, y, bias=None):
+    dev = torch.cuda.current_device()
+    _check(lib().lamp_gemm_fp4(_operand(a, dev, "a"), _operand(b, dev, "b"), _vec(bias, b.rows, "bias", dev), _byref(_view(y, dev, "y")),
+                               _raw_stream(dev)), "lamp_gemm_fp4")
+
+
+# --- gradient clipping ---------------------------------------------------------------------------------------------
+class GradList:
+    """The tensors of lamp_grad_norm / lamp_grad_clip, described once and used for many steps; holds them."""
+
+    def __init__(self, tensors, outs):
+        self.keep = (tensors, outs)
+        self.count, self.dev = len(tensors), tensors[0].get_device() if tensors else None
+        self.array = (Grad * max(1, self.count))()
+        for i, (g, o) in enumerate(zip(tensors, outs)):
+            dt = _VIEW_TYPES.get(g.dtype)
+            if dt is None or not g.is_contiguous() or g.get_device() != self.dev or self.dev < 0:
+                raise ValueError(f"grad_list: tensor {i}: want a contiguous bf16 or fp32 tensor on one CUDA device, got {tuple(g.shape)} {g.dtype} on {g.device}")
+            if o is not g and (o.dtype is not g.dtype or o.numel() != g.numel() or not o.is_contiguous() or o.get_device() != self.dev):
+                raise ValueError(f"grad_list: output {i}: want a contiguous {g.dtype} tensor of {g.numel()} elements on {g.device}, got {tuple(o.shape)} {o.dtype} on {o.device}")
+            self.array[i] = Grad(g.data_ptr(), o.data_ptr(), g.numel(), dt)
+
+
+def grad_list(tensors, outs=None) -> GradList:
+    """tensors: gradients (bf16 or fp32, contiguous); outs: where lamp_grad_clip writes, None for in place."""
+    tensors = list(tensors)
+    outs = tensors if outs is None else list(outs)
+    if len(outs) != len(tensors):
+        raise ValueError(f"grad_list: {len(tensors)} tensors and {len(outs)} outputs")
+    return GradList(tensors, outs)
+
+
+def _grads(g, dev):
+    if g.dev is not None and g.dev != dev:
+        raise ValueError(f"grads: on cuda:{g.dev}, the current device is cuda:{dev}")
+    return g.array
+
+
+def lamp_grad_norm_workspace_bytes(grads: GradList):
+    return lib().lamp_grad_norm_workspace_bytes(grads.array, grads.count)
+
+
+def lamp_grad_norm(grads: GradList, max_norm, norm, factor=None, ws=None):
+    dev = torch.cuda.current_device()
+    w, nbytes = _scratch(ws, dev)
+    _check(lib().lamp_grad_norm(_grads(grads, dev), grads.count, max_norm, _vec(norm, 1, "norm", dev), _vec(factor, 1, "factor", dev), w, nbytes,
+                                _raw_stream(dev)), "lamp_grad_norm")
+
+
+def lamp_grad_clip(grads: GradList, max_norm, norm, factor, ws=None):
+    dev = torch.cuda.current_device()
+    w, nbytes = _scratch(ws, dev)
+    _check(lib().lamp_grad_clip(_grads(grads, dev), grads.count, max_norm, _vec(norm, 1, "norm", dev), _vec(factor, 1, "factor", dev), w, nbytes,
+                                _raw_stream(dev)), "lamp_grad_clip")
+
+
+def lamp_rmsprop_step_scaled(grad, grad_scale, master, v, param_bf16=None, lr=1e-3, alpha=0.99, eps=1e-8):
+    """lamp_rmsprop_step with the gradients times grad_scale (fp32 scalar on the device, as lamp_grad_norm leaves it in factor)."""
+    dev = torch.cuda.current_device()
+    n = grad.numel()
+    _check(lib().lamp_rmsprop_step_scaled(n, _vec(grad, n, "grad", dev), _vec(grad_scale, 1, "grad_scale", dev), _vec(master, n, "master", dev),
+                                          _vec(v, n, "v", dev), _vec(param_bf16, n, "param_bf16", dev, torch.bfloat16), lr, alpha, eps,
+                                          _raw_stream(dev)), "lamp_rmsprop_step_scaled")
 
 
 def lamp_get_async_status():

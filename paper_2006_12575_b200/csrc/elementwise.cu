@@ -507,14 +507,18 @@ head_bwd_kernel(const bf16 *__restrict__ z, int64_t zp, int C, const bf16 *__res
 // ------------------------------------------------------------------ parameter update
 // v = alpha v + (1 - alpha) g^2; w -= lr g / (sqrt(v) + eps); bf16 copy.  Four elements per thread when the
 // pointers allow 16-byte accesses (22 bytes of traffic per element: HBM-bound).
+// SCALED: g times *scale (the clipping factor).
+template <bool SCALED>
 __global__ void __launch_bounds__(256)
-rmsprop_kernel(int64_t n, const float *__restrict__ g, float *__restrict__ w, float *__restrict__ v,
+rmsprop_kernel(int64_t n, const float *__restrict__ g, const float *__restrict__ scale, float *__restrict__ w, float *__restrict__ v,
                bf16 *__restrict__ wb, float lr, float alpha, float eps, int vec)
 {
     pdl_launch_dependents();
     pdl_wait();
+    const float gs = SCALED ? __ldg(scale) : 1.f;
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     auto upd = [&](float gi, float &wi, float &vi) {
+        if (SCALED) gi *= gs;
         vi = fmaf(alpha, vi, (1.0f - alpha) * gi * gi);
         wi -= lr * gi / (sqrtf(vi) + eps);
     };
@@ -901,13 +905,14 @@ lamp_status_t k_head_bwd(const TView &z, const bf16 *w, int K, const float *prob
     return db ? reduce_partials(partB, K, (int)(blocks * z.n), db, st) : LAMP_OK;
 }
 
-lamp_status_t k_rmsprop(int64_t n, const float *g, float *w, float *v, bf16 *wb, float lr, float alpha, float eps,
+lamp_status_t k_rmsprop(int64_t n, const float *g, const float *scale, float *w, float *v, bf16 *wb, float lr, float alpha, float eps,
                         cudaStream_t st)
 {
     if (n == 0) return LAMP_OK;
     const bool vec = n % 4 == 0 && (((uintptr_t)g | (uintptr_t)w | (uintptr_t)v) & 15) == 0 && ((uintptr_t)wb & 7) == 0;
     const int64_t threads = vec ? n / 4 : n;
-    (void)launch_pdl(n <= SHORT_ELEMS, rmsprop_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), (size_t)(0), st, n, g, w, v, wb, lr, alpha, eps, vec ? 1 : 0);
+    (void)launch_pdl(n <= SHORT_ELEMS, scale ? rmsprop_kernel<true> : rmsprop_kernel<false>, dim3((unsigned)((threads + 255) / 256)), dim3(256), (size_t)(0), st,
+                     n, g, scale, w, v, wb, lr, alpha, eps, vec ? 1 : 0);
     return launch_status();
 }
 

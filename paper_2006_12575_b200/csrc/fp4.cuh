@@ -1,0 +1,106 @@
+// 4-bit codes (e2m1) and their block scales: e8m0 per 32, or e4m3 per 16 times a tensor's scale.
+#pragma once
+#include <stdint.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+#include "block_norm.cuh"
+
+namespace lamp {
+namespace fp4 {
+
+// Place of the scale of (row, block i) among an operand's scales: tiles of 128 rows x 4 blocks, `tiles` of them along k
+__host__ __device__ __forceinline__ int64_t scale_at(int64_t row, int64_t i, int64_t tiles)
+{
+    return ((row >> 7) * tiles + (i >> 2)) * 512 + (row & 31) * 16 + ((row >> 5) & 3) * 4 + (i & 3);
+}
+__host__ __device__ __forceinline__ int64_t blocks_of(int64_t k, int block) { return (k + block - 1) / block; }
+__host__ __device__ __forceinline__ int64_t tiles_of(int64_t k, int block) { return (blocks_of(k, block) + 3) / 4; }
+
+// bits of the largest |v|: infinities above every finite value, NaN above both
+__device__ __forceinline__ uint32_t amax_bits(const float (&f)[8])
+{
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(f[i]) & 0x7FFFFFFFu);
+    return m;
+}
+
+// What a block's values are divided by: either exactly by a multiplication (block of 32: a power of two) or by `wide`
+struct Scale { uint32_t byte; float by; };
+
+// The scale of a block from the bits of its amax.  BLOCK = 32: by = 1 / scale.  BLOCK = 16: by = scale * g.  by = 0 for a NaN scale.
+template <int BLOCK> __device__ __forceinline__ Scale block_scale(uint32_t amax, float g, float six_g)
+{
+    Scale s;
+    const bool nan = amax >= 0x7F800000u;
+    if constexpr (BLOCK == 32) {
+        // amax = 1.m 2^(E - 127) <= 6 2^e = 1.5 2^(e + 2)  <=>  e >= E - 129, one more where 1.m > 1.5
+        const int e = (int)(amax >> 23) - 2 + ((amax & 0x7FFFFFu) > 0x400000u ? 1 : 0);
+        s.byte = nan ? 255u : (uint32_t)max(e, 0);
+        s.by = nan ? 0.f : __uint_as_float((254u - s.byte) << 23);
+    } else {
+        const float v = fminf(fmaxf(__fdiv_rn(__uint_as_float(amax), six_g), 0.001953125f), 448.f);
+        uint16_t two;
+        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(0.f), "f"(v));
+        s.byte = nan ? 0x7Fu : (two & 0xFFu);
+        uint32_t half2;
+        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(half2) : "h"(two));
+        s.by = nan ? 0.f : __fmul_rn(__half2float(__ushort_as_half((unsigned short)(half2 & 0xFFFFu))), g);
+    }
+    return s;
+}
+
+// x over the block's scale in fp32, correctly rounded
+template <int BLOCK> __device__ __forceinline__ float scaled(float x, float by)
+{
+    return BLOCK == 32 ? x * by : __fdiv_rn(x, by);
+}
+
+// Eight codes, the first in the low half of the low byte.  The conversion rounds to nearest even and saturates.
+__device__ __forceinline__ uint32_t encode8(const float (&v)[8])
+{
+    uint32_t r;
+    asm("{\n.reg .b8 b0, b1, b2, b3;\n"
+        "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n"
+        "cvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n"
+        "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n"
+        "cvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n"
+        "mov.b32 %0, {b0, b1, b2, b3};\n}"
+        : "=r"(r) : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+    return r;
+}
+template <int BLOCK> __device__ __forceinline__ uint32_t encode8(const float (&f)[8], const Scale &s)
+{
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = scaled<BLOCK>(f[i], s.by);
+    return s.by == 0.f ? 0u : encode8(v);
+}
+
+__device__ __forceinline__ void decode8(uint32_t codes, float (&v)[8])
+{
+    uint32_t h[4];
+    asm("{\n.reg .b8 b0, b1, b2, b3;\nmov.b32 {b0, b1, b2, b3}, %4;\n"
+        "cvt.rn.f16x2.e2m1x2 %0, b0;\ncvt.rn.f16x2.e2m1x2 %1, b1;\ncvt.rn.f16x2.e2m1x2 %2, b2;\ncvt.rn.f16x2.e2m1x2 %3, b3;\n}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(codes));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h[i]));
+        v[2 * i] = f.x; v[2 * i + 1] = f.y;
+    }
+}
+// scale * g of a scale byte
+template <int BLOCK> __device__ __forceinline__ float decode_scale(uint32_t byte, float g)
+{
+    if constexpr (BLOCK == 32) return __uint_as_float(byte == 255u ? 0x7FC00000u : byte == 0u ? 0x00400000u : byte << 23);
+    uint32_t half2;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(half2) : "h"((uint16_t)byte));
+    return __fmul_rn(__half2float(__ushort_as_half((unsigned short)(half2 & 0xFFFFu))), g);
+}
+
+}  // namespace fp4
+
+// fp4_quant.cu.  Argument check of a 4-bit operand.
+lamp_status_t check_fp4_operand(const lamp_fp4_operand_t *o);
+
+}  // namespace lamp

@@ -22,22 +22,20 @@
 // Every mbarrier wait is bounded; on expiry the CTA records LAMP_ERR_TIMEOUT and winds down.
 #include <cuda.h>
 #include <cudaTypedefs.h>
-#include "common.cuh"
-#include "umma_ptx.cuh"
+#include "gemm_out.cuh"
 
 namespace lamp {
 
 namespace {
 
 using namespace ptx;
+using namespace gemm;
 
 constexpr int KB = 128;                       // codes per scale block = bytes per shared-memory row
 constexpr int MAX_STAGES = 10, MAX_ACC = 4;
 constexpr int RING = 8;                       // blocks of scales in flight (Scales)
-constexpr int STAGE_FLOATS = 32 * 17;         // a promotion warp's staging area for rows that are not 16-byte aligned
 
-struct GemmParams {
-    int32_t rows_l, rows_c;                   // rows of the lane operand and of the column operand
+struct GemmParams : OutParams {
     int32_t kblocks;
     int32_t nl, nc;                           // tiles per axis
     int64_t tiles;
@@ -45,11 +43,6 @@ struct GemmParams {
     const float *sl, *sc;
     int64_t pl, pc;                           // scale pitches
     int32_t tile_l, tile_c;                   // scale per 128 rows
-    const float *bias;
-    void *y;
-    int64_t y_pitch;
-    int32_t y_f32, swap;
-    int32_t vec;                              // alignment of every row's tile start: 2 = 32 bytes, 1 = 16 bytes, 0 = neither
     int *status;
 };
 
@@ -78,162 +71,6 @@ __device__ __forceinline__ void umma_fp8(uint32_t d_tmem, uint64_t adesc, uint64
     asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}"
                  ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
 }
-__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int c0, int c1)
-{
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-                 ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1) : "memory");
-}
-// 32 lanes x 16 columns into 16 registers
-__device__ __forceinline__ void tmem_ld_x16(uint32_t taddr, uint32_t (&r)[16])
-{
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-                 "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-                 : "r"(taddr) : "memory");
-}
-
-__device__ __forceinline__ uint32_t cluster_rank()
-{
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ void cluster_sync_all()
-{
-    asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
-}
-__device__ __forceinline__ float ld_peer_f32(uint32_t addr, uint32_t rank)
-{
-    uint32_t a;
-    float v;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
-    return v;
-}
-
-// NV consecutive outputs of one row (columns col .. col + NV - 1, of which `left` exist)
-template <int NV>
-__device__ __forceinline__ void store_row(const GemmParams &P, int64_t row, int col, const float (&v)[NV])
-{
-    const int left = P.rows_c - col;
-    if (left <= 0) return;
-    if (P.y_f32) {
-        float *o = (float *)P.y + row * P.y_pitch + col;
-        if (NV % 4 == 0 && left >= NV && P.vec >= 1) {
-            if (NV % 8 == 0 && P.vec == 2) {
-#pragma unroll
-                for (int j = 0; j + 8 <= NV; j += 8) {
-                    uint32_t u[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) u[i] = __float_as_uint(v[j + i]);
-                    st_global_32B(o + j, u);
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j + 4 <= NV; j += 4) *reinterpret_cast<float4 *>(o + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < NV; ++j) if (j < left) o[j] = v[j];
-        }
-    } else {
-        bf16 *o = (bf16 *)P.y + row * P.y_pitch + col;
-        if (NV % 8 == 0 && left >= NV && P.vec >= 1) {
-            uint32_t u[(NV + 1) / 2];
-#pragma unroll
-            for (int j = 0; j + 2 <= NV; j += 2) {
-                __nv_bfloat162 h = __floats2bfloat162_rn(v[j], v[j + 1]);
-                u[j / 2] = *reinterpret_cast<uint32_t *>(&h);
-            }
-            if (NV % 16 == 0 && P.vec == 2) {
-#pragma unroll
-                for (int j = 0; j + 16 <= NV; j += 16) {
-                    uint32_t w[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) w[i] = u[(j / 2 + i) % ((NV + 1) / 2)];
-                    st_global_32B(o + j, w);
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j + 8 <= NV; j += 8)
-                    *reinterpret_cast<uint4 *>(o + j) = make_uint4(u[j / 2], u[(j / 2 + 1) % ((NV + 1) / 2)], u[(j / 2 + 2) % ((NV + 1) / 2)],
-                                                                   u[(j / 2 + 3) % ((NV + 1) / 2)]);
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < NV; ++j) if (j < left) o[j] = f2bf(v[j]);
-        }
-    }
-}
-
-// The finished sums of NV columns of a lane row: bias, rounding, store.  Every lane of the warp takes part; row = the lane's own.
-// ODD (rows that are not 16-byte aligned, or a width that is no multiple of 16): through `stage`, 32 x 17 floats of the warp, so that
-// neighbouring lanes write neighbouring columns: stored by the lanes that hold them, every 4-byte store is a sector of its
-// own (1407 x 2805 fp32: 29 us against 12; 16384 x 4095 bf16, k = 512: 609 against 151).  A kernel of its own: the code
-// alone cost the aligned products 5 %.
-template <bool ODD, int NV>
-__device__ __forceinline__ void finish(const GemmParams &P, int64_t row, int col, float (&v)[NV], float *stage)
-{
-    if ((!ODD || P.swap) && row >= P.rows_l) return;
-    if (P.swap) {                              // lanes = channels of y, columns = its voxels
-        const float b = P.bias ? __ldg(P.bias + row) : 0.f;
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            if (col + j >= P.rows_c) break;
-            const int64_t at = (int64_t)(col + j) * P.y_pitch + row;
-            if (P.y_f32) ((float *)P.y)[at] = v[j] + b; else ((bf16 *)P.y)[at] = f2bf(v[j] + b);
-        }
-        return;
-    }
-    if (P.bias) {
-#pragma unroll
-        for (int j = 0; j < NV; ++j) if (col + j < P.rows_c) v[j] += __ldg(P.bias + col + j);
-    }
-    if (!ODD || NV < 16) {
-        if (row < P.rows_l) store_row<NV>(P, row, col, v);
-        return;
-    }
-    const int lane = threadIdx.x & 31;
-#pragma unroll
-    for (int j = 0; j < NV; ++j) stage[lane * 17 + j] = v[j];
-    __syncwarp();
-    const int64_t row0 = row - lane;
-    const int j = lane & 15;
-    if (col + j < P.rows_c) {
-#pragma unroll 4
-        for (int i = 0; i < 32; i += 2) {
-            const int r = i + (lane >> 4);
-            if (row0 + r >= P.rows_l) break;
-            const int64_t at = (row0 + r) * P.y_pitch + col + j;
-            const float x = stage[r * 17 + j];
-            if (P.y_f32) ((float *)P.y)[at] = x; else ((bf16 *)P.y)[at] = f2bf(x);
-        }
-    }
-    __syncwarp();
-}
-
-// Sum over the S parts of a tile (in CTAs first, first + stride, ... of the cluster) of the `mine`-th CW / S columns of this
-// thread's lane row, and their store.
-template <bool ODD, int CW, int S>
-__device__ __forceinline__ void reduce_parts(const GemmParams &P, uint32_t part_base, int lane_row, int64_t row, int col_local, int col0, uint32_t mine,
-                                             uint32_t first, uint32_t stride, float *stage)
-{
-    constexpr int CWS = CW / S, CH = CWS < 16 ? CWS : 16;
-#pragma unroll 1
-    for (int j0 = 0; j0 < CWS; j0 += CH) {
-        const int cl = col_local + (int)mine * CWS + j0;
-        float v[CH];
-#pragma unroll
-        for (int j = 0; j < CH; ++j) v[j] = 0.f;
-#pragma unroll
-        for (int s = 0; s < S; ++s)
-#pragma unroll
-            for (int j = 0; j < CH; ++j) v[j] += ld_peer_f32(part_base + ((cl + j) * 128 + lane_row) * 4, first + s * stride);
-        finish<ODD, CH>(P, row, col0 + cl, v, stage);
-    }
-}
-
 // The scales of a block - one per lane row, and one per column (COLVEC) or one per 128 columns - come through a ring of RING
 // slots in shared memory that one warp fills with asynchronous copies, ahead and across tiles; the promotion warps wait
 // for a slot as they wait for an accumulator.  (Loaded by the promotion warps themselves a block ahead they cost an L2
@@ -508,36 +345,11 @@ template <int BN> struct PairLayout {
     static_assert(TOTAL <= 227 * 1024 && STAGES <= MAX_STAGES && NACC <= MAX_ACC && NACC * BN <= TMEM_COLS, "");
 };
 
-__device__ __forceinline__ uint32_t map_to_rank(uint32_t addr, uint32_t rank)
-{
-    uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
-    return r;
-}
-__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap *map, uint32_t leader_bar, int c0, int c1)
-{
-    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-                 ::"r"(dst), "l"(map), "r"(leader_bar), "r"(c0), "r"(c1) : "memory");
-}
 __device__ __forceinline__ void umma_fp8_pair(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
 {
     asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n}"
                  ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
 }
-// arrives on the barrier of this offset in the CTAs of the mask once the MMAs issued so far have completed
-__device__ __forceinline__ void umma_commit_pair(uint32_t bar, uint32_t ctas)
-{
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                 ::"r"(bar), "h"((uint16_t)ctas) : "memory");
-}
-// Arrival on a barrier of either CTA.  No release at cluster scope: what it hands over is tensor memory that has been read,
-// not memory that was written, and that release is a fence that waits for everything the thread has in flight - it took
-// 1200 cycles per block of k, three quarters of the kernel's time.
-__device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr)
-{
-    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
-}
-
 template <int BN, bool COLVEC, bool ODD>
 __global__ void __launch_bounds__(PairLayout<BN>::THREADS, 1)
 fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constant__ CUtensorMap map_c, const GemmParams P)
@@ -766,7 +578,6 @@ lamp_status_t launch(const lamp_fp8_operand_t *l, const lamp_fp8_operand_t *c, c
     return cudaLaunchKernelEx(&cfg, fp8_gemm_kernel<BN, COLVEC, ODD>, ml, mc, P) == cudaSuccess ? LAMP_OK : LAMP_ERR_CUDA;
 }
 
-bool odd_rows(const GemmParams &P) { return !P.swap && (P.vec == 0 || P.rows_c % 16 != 0); }
 template <int BN>
 lamp_status_t launch_cv(const lamp_fp8_operand_t *l, const lamp_fp8_operand_t *c, const GemmParams &P, cudaStream_t st)
 {
@@ -779,11 +590,6 @@ lamp_status_t launch_pair(const lamp_fp8_operand_t *l, const lamp_fp8_operand_t 
     if (odd_rows(P)) return c->tile_scale ? launch_pair_k<BN, false, true>(l, c, P, st) : launch_pair_k<BN, true, true>(l, c, P, st);
     return c->tile_scale ? launch_pair_k<BN, false, false>(l, c, P, st) : launch_pair_k<BN, true, false>(l, c, P, st);
 }
-
-// Clusters of `ctas` CTAs, one CTA per SM, that run at once: the SMs of a cluster belong to one GPC, so not every SM finds a
-// place.  (148 SMs: 74 clusters of 2, 33 of 4, 15 of 8; one cluster more than that is a second wave - 141 us against 71 for a
-// weight gradient of 512 x 2048 outputs.)
-int64_t cluster_room(int sms, int ctas) { return ctas <= 2 ? sms / ctas : ctas == 4 ? sms * 2 / 9 : sms / 10; }
 
 }  // namespace
 
@@ -821,10 +627,7 @@ extern "C" lamp_status_t lamp_gemm_fp8(const lamp_fp8_operand_t *a, const lamp_f
     P.kblocks = (int32_t)((a->k + KB - 1) / KB);
     P.sl = l->scale; P.sc = c->scale; P.pl = l->scale_pitch; P.pc = c->scale_pitch;
     P.tile_l = l->tile_scale; P.tile_c = c->tile_scale;
-    P.bias = bias; P.y = v.p; P.y_pitch = v.pitch; P.y_f32 = v.f32; P.swap = swap;
-    const size_t es = v.f32 ? 4 : 2;
-    const uintptr_t mis = (uintptr_t)v.p | (uintptr_t)(v.pitch * es);
-    P.vec = (mis & 31) == 0 ? 2 : (mis & 15) == 0 ? 1 : 0;
+    set_output(P, v, bias, swap);
     P.status = status_word_ptr();
     const int sms = sm_count();
     P.nl = (P.rows_l + 127) / 128;

@@ -1,0 +1,312 @@
+// Global norm of the gradients of many tensors, and clipping by it.
+//
+// Bound by memory: the norm reads every gradient once, the scaling reads and writes it.  The tensors' table travels in the
+// kernel's parameters (a captured graph keeps it), so no copy to the device precedes a call.  The elements are cut into pieces of
+// PIECE, laid from a 16-byte boundary of their tensor; a CTA takes a contiguous run of pieces, the scaling the runs in the opposite
+// order, so that it starts with what the norm left in L2.
+// Sums: 8 squares in fp32 where that stays well inside its range, otherwise the 8 again in fp64; fp64 beyond, per thread, then over the
+// CTA in a fixed order, one partial sum per CTA.  Every CTA of the scaling adds all of them in the same order: no counter, no atomic, nothing
+// that has to be zero beforehand.
+#include "block_norm.cuh"
+
+namespace lamp {
+
+namespace {
+
+using namespace bn;
+
+constexpr int CT = 256, PIECE = 8192;
+
+struct Entry {
+    const void *g;
+    void *out;
+    int64_t n;
+    int32_t first;                            // pieces of the tensors in front of it
+    int32_t f32;
+};
+template <int N> struct Table {
+    int32_t count, pieces;
+    Entry e[N];
+};
+constexpr int SMALL = 120, LARGE = 1000;      // parameters of 4 KB and of just under 32 KB
+static_assert(sizeof(Table<LARGE>) + 64 <= 32764, "kernel parameters");
+
+// elements in front of the first 16-byte boundary
+__host__ __device__ __forceinline__ int64_t head_of(const void *p, int64_t n, bool f32)
+{
+    const int64_t h = (int64_t)((16 - ((uintptr_t)p & 15)) & 15) / (f32 ? 4 : 2);
+    return h < n ? h : n;
+}
+__host__ __forceinline__ int64_t pieces_of(const lamp_grad_t &t)
+{
+    if (t.n == 0) return 0;
+    const int64_t body = t.n - head_of(t.g, t.n, t.dtype == LAMP_F32);
+    return body == 0 ? 1 : (body + PIECE - 1) / PIECE;
+}
+
+// The run of pieces of this CTA, tensor by tensor: f(entry, first element of the body of the piece, its end, whether the head comes with it).
+template <int N, typename F>
+__device__ __forceinline__ void for_pieces(const Table<N> &T, int64_t block, F f)
+{
+    const int p0 = (int)((int64_t)T.pieces * block / gridDim.x), p1 = (int)((int64_t)T.pieces * (block + 1) / gridDim.x);
+    if (p0 >= p1) return;
+    int lo = 0, hi = T.count - 1;             // the last entry that starts at p0 or before it (entries without pieces lie in front of their successor)
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (T.e[mid].first <= p0) lo = mid; else hi = mid - 1;
+    }
+    for (int i = lo, p = p0; p < p1; ++i) {
+        const Entry &e = T.e[i];
+        const int end = i + 1 < T.count ? T.e[i + 1].first : T.pieces;
+        const int64_t h = head_of(e.g, e.n, e.f32);
+        for (; p < p1 && p < end; ++p) {
+            const int64_t b0 = h + (int64_t)(p - e.first) * PIECE;
+            f(e, b0, b0 + PIECE < e.n ? b0 + PIECE : e.n, p == e.first ? h : 0);
+        }
+    }
+}
+
+__device__ __forceinline__ float element(const void *p, int64_t i, int f32) { return f32 ? ((const float *)p)[i] : bf2f(((const bf16 *)p)[i]); }
+
+template <bool F32> __device__ __forceinline__ void add_squares(const Raw<F32> &r, double &acc)
+{
+    ptx::f32x2 v[4];
+    to_pairs<F32>(r, v);
+    const float s = both(ptx::fma2(v[3], v[3], ptx::fma2(v[2], v[2], ptx::fma2(v[1], v[1], ptx::mul2(v[0], v[0])))));
+    if (s >= 8.6736174e-19f && s <= 1.3292279957849159e36f) {        // 2^-60 .. 2^120: what underflowed is nothing beside s
+        acc += (double)s;
+    } else {
+        float f[8];
+        to_float<F32>(r, f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc = fma((double)f[j], (double)f[j], acc);
+    }
+}
+
+template <bool F32> __device__ __forceinline__ void piece_squares(const void *g, int64_t b0, int64_t b1, double &acc)
+{
+    constexpr int U = 4;                      // PIECE = CT * 8 * U
+    Raw<F32> r[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int64_t at = b0 + (u * CT + threadIdx.x) * 8;
+        if (at + 8 <= b1) r[u] = load_raw<F32>(g, at);
+        else {
+            r[u] = zero_raw<F32>();
+            for (int64_t i = at; i < b1; ++i) { const double v = element(g, i, F32); acc = fma(v, v, acc); }
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) if (b0 + (u * CT + threadIdx.x) * 8 + 8 <= b1) add_squares<F32>(r[u], acc);
+}
+static_assert(PIECE == CT * 8 * 4, "");
+
+// Sum over the CTA, in every thread; fixed order.
+__device__ __forceinline__ double block_sum(double v, double *red)
+{
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
+    __syncthreads();
+    double t = red[0];
+    for (int i = 1; i < CT / 32; ++i) t += red[i];
+    return t;
+}
+
+template <int N>
+__global__ void __launch_bounds__(CT)
+grad_norm_parts_kernel(const __grid_constant__ Table<N> T, double *__restrict__ part)
+{
+    __shared__ double red[CT / 32];
+    pdl_launch_dependents();
+    pdl_wait();
+    double acc = 0.0;
+    for_pieces(T, blockIdx.x, [&](const Entry &e, int64_t b0, int64_t b1, int64_t h) {
+        if (threadIdx.x < h) { const double v = element(e.g, threadIdx.x, e.f32); acc = fma(v, v, acc); }
+        if (e.f32) piece_squares<true>(e.g, b0, b1, acc);
+        else piece_squares<false>(e.g, b0, b1, acc);
+    });
+    acc = block_sum(acc, red);
+    if (threadIdx.x == 0) part[blockIdx.x] = acc;
+}
+
+// norm and factor of all partial sums, the same in every CTA
+__device__ __forceinline__ float clip_factor(const double *part, int parts, float max_norm, float &norm, double *red)
+{
+    double s = 0.0;
+    for (int i = threadIdx.x; i < parts; i += CT) s += part[i];
+    norm = (float)sqrt(block_sum(s, red));
+    return norm <= max_norm ? 1.f : max_norm / norm;
+}
+
+__global__ void __launch_bounds__(CT)
+grad_norm_finish_kernel(const double *part, int parts, float max_norm, float *norm, float *factor)
+{
+    __shared__ double red[CT / 32];
+    pdl_launch_dependents();
+    pdl_wait();
+    float v;
+    const float f = clip_factor(part, parts, max_norm, v, red);
+    if (threadIdx.x == 0) {
+        *norm = v;
+        if (factor) *factor = f;
+    }
+}
+
+template <bool F32> __device__ __forceinline__ void piece_scale(const Entry &e, int64_t b0, int64_t b1, float f)
+{
+    constexpr int U = 4;
+    if (((uintptr_t)e.out ^ (uintptr_t)e.g) & 15) {                   // the two cannot both be on 16-byte boundaries: an element per lane
+        for (int64_t i = b0 + threadIdx.x; i < b1; i += CT) {
+            if (F32) ((float *)e.out)[i] = ((const float *)e.g)[i] * f;
+            else ((bf16 *)e.out)[i] = f2bf(bf2f(((const bf16 *)e.g)[i]) * f);
+        }
+        return;
+    }
+    Raw<F32> r[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int64_t at = b0 + (u * CT + threadIdx.x) * 8;
+        if (at + 8 <= b1) r[u] = load_raw<F32>(e.g, at);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int64_t at = b0 + (u * CT + threadIdx.x) * 8;
+        if (at + 8 <= b1) {
+            float v[8];
+            to_float<F32>(r[u], v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] *= f;
+            store8<F32>(e.out, at, v);
+        } else {
+            for (int64_t i = at; i < b1; ++i) {
+                if (F32) ((float *)e.out)[i] = ((const float *)e.g)[i] * f;
+                else ((bf16 *)e.out)[i] = f2bf(bf2f(((const bf16 *)e.g)[i]) * f);
+            }
+        }
+    }
+}
+
+template <int N>
+__global__ void __launch_bounds__(CT)
+grad_scale_kernel(const __grid_constant__ Table<N> T, const double *part, int parts, float max_norm, float *norm, float *factor)
+{
+    __shared__ double red[CT / 32];
+    pdl_launch_dependents();
+    pdl_wait();
+    float v;
+    const float f = clip_factor(part, parts, max_norm, v, red);
+    if (blockIdx.x == 0 && threadIdx.x == 0) {                        // every launch of a call writes the same values
+        *norm = v;
+        *factor = f;
+    }
+    for_pieces(T, gridDim.x - 1 - blockIdx.x, [&](const Entry &e, int64_t b0, int64_t b1, int64_t h) {
+        if (f == 1.f && e.out == e.g) return;
+        if (threadIdx.x < h) {
+            if (e.f32) ((float *)e.out)[threadIdx.x] = ((const float *)e.g)[threadIdx.x] * f;
+            else ((bf16 *)e.out)[threadIdx.x] = f2bf(bf2f(((const bf16 *)e.g)[threadIdx.x]) * f);
+        }
+        if (e.f32) piece_scale<true>(e, b0, b1, f);
+        else piece_scale<false>(e, b0, b1, f);
+    });
+}
+
+// ----------------------------------------------------------------------------------------------------------- host
+constexpr int SHORT = 4096;                   // pieces up to which the next launch is scheduled early
+int max_ctas() { return sm_count() * 8; }
+
+lamp_status_t check_grads(const lamp_grad_t *grads, int32_t count, bool outs)
+{
+    if (count < 0 || (count > 0 && !grads)) return LAMP_ERR_INVALID_ARG;
+    if (count > (1 << 20)) return LAMP_ERR_UNSUPPORTED;
+    int64_t total = 0;
+    for (int32_t i = 0; i < count; ++i) {
+        const lamp_grad_t &t = grads[i];
+        if (t.dtype != LAMP_BF16 && t.dtype != LAMP_F32) return LAMP_ERR_UNSUPPORTED;
+        if (t.n < 0) return LAMP_ERR_INVALID_ARG;
+        if (t.n > (1ll << 40)) return LAMP_ERR_UNSUPPORTED;
+        if ((total += t.n) > (1ll << 42)) return LAMP_ERR_UNSUPPORTED;  // 2^29 pieces
+        if (t.n == 0) continue;
+        const uintptr_t mask = t.dtype == LAMP_F32 ? 3 : 1;
+        if (!t.g || ((uintptr_t)t.g & mask) || (outs && (!t.out || ((uintptr_t)t.out & mask)))) return LAMP_ERR_INVALID_ARG;
+    }
+    return LAMP_OK;
+}
+
+// Fills a table from entry i on; returns the entry behind it.
+template <int N>
+int32_t fill(Table<N> &T, const lamp_grad_t *grads, int32_t count, int32_t i)
+{
+    T.count = T.pieces = 0;
+    for (; i < count && T.count < N; ++i) {
+        const int64_t p = pieces_of(grads[i]);
+        if (p == 0) continue;
+        T.e[T.count++] = Entry{grads[i].g, grads[i].out, grads[i].n, T.pieces, grads[i].dtype == LAMP_F32};
+        T.pieces += (int32_t)p;
+    }
+    return i;
+}
+
+template <int N> int ctas(const Table<N> &T) { return T.pieces < max_ctas() ? T.pieces : max_ctas(); }
+
+template <int N>
+lamp_status_t run(const lamp_grad_t *grads, int32_t count, float max_norm, float *norm, float *factor, bool scale, double *part, cudaStream_t st)
+{
+    lamp_status_t s;
+    Table<N> T;
+    int parts = 0, tables = 0;
+    for (int32_t i = 0; i < count;) {
+        i = fill(T, grads, count, i);
+        const int g = ctas(T);
+        if (g == 0) break;                                            // nothing but empty tensors left
+        if ((s = launch_pdl(T.pieces <= SHORT, grad_norm_parts_kernel<N>, dim3((unsigned)g), dim3(CT), 0, st, T, part + parts)) != LAMP_OK) return s;
+        parts += g;
+        ++tables;
+    }
+    if (!scale || parts == 0) return launch_pdl(true, grad_norm_finish_kernel, dim3(1), dim3(CT), 0, st, (const double *)part, parts, max_norm, norm, factor);
+    int32_t i = 0;
+    for (int t = 0; t < tables; ++t) {
+        i = fill(T, grads, count, i);
+        if ((s = launch_pdl(T.pieces <= SHORT, grad_scale_kernel<N>, dim3((unsigned)ctas(T)), dim3(CT), 0, st, T, (const double *)part, parts, max_norm, norm,
+                            factor)) != LAMP_OK) return s;
+    }
+    return LAMP_OK;
+}
+
+size_t workspace(int32_t count)
+{
+    const size_t tables = count <= SMALL ? 1 : (size_t)(count + LARGE - 1) / LARGE;
+    return tables * max_ctas() * sizeof(double);
+}
+
+lamp_status_t clip(const lamp_grad_t *grads, int32_t count, float max_norm, float *norm, float *factor, bool scale, void *ws, size_t ws_bytes, void *stream)
+{
+    lamp_status_t s;
+    if ((s = check_grads(grads, count, scale)) != LAMP_OK) return s;
+    if (!norm || ((uintptr_t)norm & 3) || (scale && !factor) || ((uintptr_t)factor & 3) || !(max_norm >= 0.f)) return LAMP_ERR_INVALID_ARG;
+    if (!ws || ((uintptr_t)ws & 15) || ws_bytes < lamp_grad_norm_workspace_bytes(grads, count)) return LAMP_ERR_WORKSPACE;
+    cudaStream_t st = (cudaStream_t)stream;
+    return count <= SMALL ? run<SMALL>(grads, count, max_norm, norm, factor, scale, (double *)ws, st)
+                          : run<LARGE>(grads, count, max_norm, norm, factor, scale, (double *)ws, st);
+}
+
+}  // namespace
+
+}  // namespace lamp
+
+using namespace lamp;
+
+extern "C" size_t lamp_grad_norm_workspace_bytes(const lamp_grad_t *grads, int32_t count)
+{
+    return check_grads(grads, count, false) == LAMP_OK ? workspace(count) : 0;
+}
+extern "C" lamp_status_t lamp_grad_norm(const lamp_grad_t *grads, int32_t count, float max_norm, float *norm, float *factor, void *ws, size_t ws_bytes,
+                                        void *cuda_stream)
+{
+    return clip(grads, count, max_norm, norm, factor, false, ws, ws_bytes, cuda_stream);
+}
+extern "C" lamp_status_t lamp_grad_clip(const lamp_grad_t *grads, int32_t count, float max_norm, float *norm, float *factor, void *ws, size_t ws_bytes,
+                                        void *cuda_stream)
+{
+    return clip(grads, count, max_norm, norm, factor, true, ws, ws_bytes, cuda_stream);
+}
