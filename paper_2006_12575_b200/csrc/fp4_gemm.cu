@@ -64,6 +64,14 @@ __device__ __forceinline__ void umma_fp4(uint32_t d_tmem, uint64_t adesc, uint64
     if constexpr (GROUP == 2 && BLOCK == 32) LAMP_FP4_MMA("2", "mxf4", "2X");
     if constexpr (GROUP == 2 && BLOCK == 16) LAMP_FP4_MMA("2", "mxf4nvf4", "4X");
 }
+// True in one lane of the warp.  The issuing loops run in the whole warp and only the tcgen05 instructions under this predicate: their
+// descriptors then stay in uniform registers.
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t p;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xFFFFFFFF;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(p));
+    return p != 0;
+}
 // 512 bytes of scales from shared memory to 4 columns
 template <int GROUP> __device__ __forceinline__ void scales_to_tmem(uint32_t taddr, uint64_t sdesc)
 {
@@ -180,25 +188,28 @@ fp4_gemm_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constant
         __syncwarp();
     } else if (warp == 1) {
         // ------------------------------------------------------------------ MMA issuer
-        if (lane == 0) {
-            int stage = 0;
-            uint32_t phase = 0, acc = 0, acc_phase = 0;
-            for (int64_t tile = tile0; tile < P.tiles && ok; tile += tile_step) {
-                if (!mbar_wait(tempty0 + 8 * acc, acc_phase ^ 1, abort_flag)) { ok = false; break; }
+        int stage = 0;
+        uint32_t phase = 0, acc = 0, acc_phase = 0;
+        for (int64_t tile = tile0; tile < P.tiles && ok; tile += tile_step) {
+            ok = __all_sync(0xffffffffu, mbar_wait(tempty0 + 8 * acc, acc_phase ^ 1, abort_flag));
+            if (!ok) break;
+            tc_fence_after();
+            for (int kb = kb0; kb < kb1; ++kb) {
+                ok = __all_sync(0xffffffffu, mbar_wait(full0 + 8 * stage, phase, abort_flag));
+                if (!ok) break;
                 tc_fence_after();
-                for (int kb = kb0; kb < kb1; ++kb) {
-                    if (!mbar_wait(full0 + 8 * stage, phase, abort_flag)) { ok = false; break; }
-                    tc_fence_after();
-                    const uint32_t sa = smem_u32(smem + stage * L::STAGE_BYTES), sc = sa + L::A_BYTES, ss = sc + L::C_BYTES;
+                const uint32_t sa = smem_u32(smem + stage * L::STAGE_BYTES), sc = sa + L::A_BYTES, ss = sc + L::C_BYTES;
+                if (elect_one()) {
                     stage_mmas<1, BLOCK, 128, BN>(tmem_base + acc * BN, tmem_base + L::SF0 + stage * L::SFC, sa, sc, ss, ss + L::S_BYTES, kb == kb0);
-                    umma_commit(empty0 + 8 * stage);         // frees the stage, and its scales, once these MMAs have read them
-                    if (++stage == STAGES) { stage = 0; phase ^= 1; }
+                    umma_commit(empty0 + 8 * stage);     // frees the stage, and its scales, once these MMAs have read them
                 }
-                umma_commit(tfull0 + 8 * acc);
-                if (++acc == NACC) { acc = 0; acc_phase ^= 1; }
+                __syncwarp();
+                if (++stage == STAGES) { stage = 0; phase ^= 1; }
             }
+            if (elect_one()) umma_commit(tfull0 + 8 * acc);
+            __syncwarp();
+            if (++acc == NACC) { acc = 0; acc_phase ^= 1; }
         }
-        __syncwarp();
     } else {
         // ------------------------------------------------------------------ epilogue
         const int q = warp & 3, half = (warp - 2) >> 2;                    // lane quarter and column part of this warp
@@ -275,15 +286,15 @@ template <int BN, int BLOCK> struct PairLayout {
     static constexpr int CT = BN / 128;
     static constexpr int A_BYTES = 128 * KB, C_BYTES = BN / 2 * KB, S_BYTES = Kind<BLOCK>::BYTES;
     static constexpr int STAGE_BYTES = A_BYTES + C_BYTES + (1 + CT) * S_BYTES;
-    static constexpr int STAGES = BN == 256 ? 5 : 7;
+    static constexpr int STAGES = BN == 256 ? 5 : 6;
     static constexpr int NACC = BN == 256 ? 1 : 2;
     static constexpr int CW = BN / 2;                             // columns per epilogue warp
     static constexpr int THREADS = 384, TMEM_COLS = 512;
     static constexpr int SF0 = NACC * BN, SFC = (1 + CT) * Kind<BLOCK>::COLS;
-    static constexpr int OUT_BYTES = 8 * STAGE_FLOATS * 4;
+    static constexpr int OUT_BYTES = 8 * 4096;                    // per epilogue warp 32 rows x 128 bytes
     static constexpr int BAR_BYTES = (2 * MAX_STAGES + 2 * NACC) * 8 + 16;
     static constexpr int TOTAL = 1024 + STAGES * STAGE_BYTES + OUT_BYTES + BAR_BYTES;
-    static_assert(STAGE_BYTES % 1024 == 0, "128-byte swizzle");
+    static_assert(STAGE_BYTES % 1024 == 0 && STAGE_FLOATS * 4 <= 4096, "128-byte swizzle");
     static_assert(SF0 + STAGES * SFC <= TMEM_COLS, "");
     static_assert(TOTAL <= 227 * 1024 && STAGES <= MAX_STAGES, "");
 };
@@ -294,10 +305,32 @@ __device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap
                  ::"r"(dst), "l"(map), "r"(leader_bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
 }
 
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t src, int c0, int c1)
+{
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(map), "r"(src), "r"(c0), "r"(c1) : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+// 32 rows x 128 bytes of y from a warp's registers (lane = row, NW words) through its 4 KB of shared memory, by a bulk store that clips
+// what lies beyond y.  Whole 128-byte lines leave, and nothing waits for them (stored by the lanes that hold them, 32 bytes of 32 rows at a
+// time, 16384 x 4096 x 512 took 70 us).
+__device__ __forceinline__ void store_box(const CUtensorMap *map, uint32_t buf, const uint32_t (&w)[32], int col, int row, int lane)
+{
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");       // the store before has read the buffer
+    __syncwarp();
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(buf + lane * 128 + ((c ^ (lane & 7)) * 16)), "r"(w[4 * c]), "r"(w[4 * c + 1]), "r"(w[4 * c + 2]),
+                     "r"(w[4 * c + 3]) : "memory");
+    fence_proxy_async();
+    __syncwarp();
+    if (lane == 0) tma_store_2d(map, buf, col, row);
+}
+
+// ODD: rows of y that are not 16-byte aligned.
 template <int BN, int BLOCK, bool ODD>
 __global__ void __launch_bounds__(PairLayout<BN, BLOCK>::THREADS, 1)
 fp4_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constant__ CUtensorMap map_c, const __grid_constant__ CUtensorMap map_sl,
-                     const __grid_constant__ CUtensorMap map_sc, const GemmParams P)
+                     const __grid_constant__ CUtensorMap map_sc, const __grid_constant__ CUtensorMap map_y, const GemmParams P)
 {
     using L = PairLayout<BN, BLOCK>;
     constexpr int STAGES = L::STAGES, NACC = L::NACC, CW = L::CW;
@@ -353,24 +386,30 @@ fp4_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
                     if (++stage == STAGES) { stage = 0; phase ^= 1; }
                 }
             }
-        } else if (warp == 1 && lane == 0 && rank == 0) {
+        } else if (warp == 1 && rank == 0) {
             // -------------------------------------------------------------- MMA issuer, in the leader
             int stage = 0;
             uint32_t phase = 0, acc = 0, acc_phase = 0;
             for (int64_t tile = tile0; tile < P.tiles && ok; tile += tile_step) {
-                if (!mbar_wait(tempty0 + 8 * acc, acc_phase ^ 1, abort_flag)) { ok = false; break; }
+                ok = __all_sync(0xffffffffu, mbar_wait(tempty0 + 8 * acc, acc_phase ^ 1, abort_flag));
+                if (!ok) break;
                 tc_fence_after();
                 for (int kb = 0; kb < P.kblocks; ++kb) {
-                    if (!mbar_wait(full0 + 8 * stage, phase, abort_flag)) { ok = false; break; }
+                    ok = __all_sync(0xffffffffu, mbar_wait(full0 + 8 * stage, phase, abort_flag));
+                    if (!ok) break;
                     tc_fence_after();
                     const uint32_t sa = smem_u32(smem + stage * L::STAGE_BYTES), sc = sa + L::A_BYTES, ss = sc + L::C_BYTES;
-                    stage_mmas<2, BLOCK, 256, BN>(tmem_base + acc * BN, tmem_base + L::SF0 + stage * L::SFC, sa, sc, ss, ss + L::S_BYTES, kb == 0);
-                    // nobody waits for the last arrivals of the empty barriers in the other CTA; the accumulator's commit behind them,
-                    // which its epilogue warps do wait for, completes after them, so they land before that CTA leaves
-                    umma_commit_pair(empty0 + 8 * stage, 3u);
+                    if (elect_one()) {
+                        stage_mmas<2, BLOCK, 256, BN>(tmem_base + acc * BN, tmem_base + L::SF0 + stage * L::SFC, sa, sc, ss, ss + L::S_BYTES, kb == 0);
+                        // nobody waits for the last arrivals of the empty barriers in the other CTA; the accumulator's commit behind them,
+                        // which its epilogue warps do wait for, completes after them, so they land before that CTA leaves
+                        umma_commit_pair(empty0 + 8 * stage, 3u);
+                    }
+                    __syncwarp();
                     if (++stage == STAGES) { stage = 0; phase ^= 1; }
                 }
-                umma_commit_pair(tfull0 + 8 * acc, 3u);
+                if (elect_one()) umma_commit_pair(tfull0 + 8 * acc, 3u);
+                __syncwarp();
                 if (++acc == NACC) { acc = 0; acc_phase ^= 1; }
             }
         }
@@ -379,7 +418,7 @@ fp4_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
         // ------------------------------------------------------------------ epilogue
         const int q = warp & 3, half = (warp - 4) >> 2;
         const int lane_row = q * 32 + lane;
-        float *stage = out_stage + (warp - 4) * STAGE_FLOATS;
+        float *stage = out_stage + (warp - 4) * 1024;
         uint32_t acc = 0, acc_phase = 0;
         const uint32_t tempty_leader = map_to_rank(tempty0, 0);
         const float alpha = (P.ga ? __ldg(P.ga) : 1.f) * (P.gb ? __ldg(P.gb) : 1.f);
@@ -397,15 +436,52 @@ fp4_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(tempty_leader + 8 * acc);
+            if constexpr (ODD) {
 #pragma unroll
-            for (int c = 0; c < CW / 16; ++c) {
-                float v[16];
+                for (int c = 0; c < CW / 16; ++c) {
+                    float v[16];
 #pragma unroll
-                for (int j = 0; j < 16; ++j) v[j] = __uint_as_float(r[c][j]) * alpha;
-                finish<ODD, 16>(P, row, cbase + c * 16, v, stage);
+                    for (int j = 0; j < 16; ++j) v[j] = __uint_as_float(r[c][j]) * alpha;
+                    finish<true, 16>(P, row, cbase + c * 16, v, stage);
+                }
+            } else {
+                const int row0 = (int)(row - lane);
+                const uint32_t buf = smem_u32(stage);
+                if (row0 < P.rows_l) {
+#pragma unroll
+                    for (int c = 0; c < CW / 16; ++c)
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) {
+                            const int col = cbase + c * 16 + j;
+                            r[c][j] = __float_as_uint(__uint_as_float(r[c][j]) * alpha + (P.bias && col < P.rows_c ? __ldg(P.bias + col) : 0.f));
+                        }
+                    if (P.y_f32) {
+#pragma unroll
+                        for (int b = 0; b < CW / 32; ++b) {
+                            if (cbase + b * 32 >= P.rows_c) break;
+                            uint32_t w[32];
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) w[j] = r[2 * b + j / 16][j % 16];
+                            store_box(&map_y, buf, w, cbase + b * 32, row0, lane);
+                        }
+                    } else {
+#pragma unroll
+                        for (int b = 0; b < CW / 64; ++b) {
+                            if (cbase + b * 64 >= P.rows_c) break;
+                            uint32_t w[32];
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) {
+                                const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(r[4 * b + j / 8][2 * j % 16]), __uint_as_float(r[4 * b + j / 8][2 * j % 16 + 1]));
+                                w[j] = *reinterpret_cast<const uint32_t *>(&h);
+                            }
+                            store_box(&map_y, buf, w, cbase + b * 64, row0, lane);
+                        }
+                    }
+                }
             }
             if (++acc == NACC) { acc = 0; acc_phase ^= 1; }
         }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");       // stores still read shared memory
     }
     if (!ok) {
         if (P.status) atomicExch(P.status, (int)LAMP_ERR_TIMEOUT);
@@ -447,12 +523,23 @@ bool encode_scales(const lamp_fp4_operand_t *o, int box_tiles, CUtensorMap *map)
                CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <typename Kernel>
-lamp_status_t launch_tiles(Kernel kernel, SmemAttrOnce &attr, int smem, int threads, unsigned grid, int cluster, bool early, const lamp_fp4_operand_t *l,
-                           const lamp_fp4_operand_t *c, int box_c, int tiles_c, const GemmParams &P, cudaStream_t st)
+// y as [rows][columns], boxes of 32 rows x 128 bytes
+bool encode_output(const GemmParams &P, CUtensorMap *map)
 {
-    CUtensorMap ml, mc, msl, msc;
-    if (!encode_codes(l, 128, &ml) || !encode_codes(c, box_c, &mc) || !encode_scales(l, 1, &msl) || !encode_scales(c, tiles_c, &msc)) return LAMP_ERR_CUDA;
+    PFN_cuTensorMapEncodeTiled_v12000 enc = (PFN_cuTensorMapEncodeTiled_v12000)tensor_map_encoder();
+    if (!enc) return false;
+    const int es = P.y_f32 ? 4 : 2;
+    const cuuint64_t gdim[2] = {(cuuint64_t)P.rows_c, (cuuint64_t)P.rows_l};
+    const cuuint64_t gstride[1] = {(cuuint64_t)P.y_pitch * es};
+    const cuuint32_t box[2] = {(cuuint32_t)(128 / es), 32};
+    const cuuint32_t one[2] = {1, 1};
+    return enc(map, P.y_f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, P.y, gdim, gstride, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename... KArgs, typename... Args>
+lamp_status_t launch_tiles(void (*kernel)(KArgs...), SmemAttrOnce &attr, int smem, int threads, unsigned grid, int cluster, bool early, cudaStream_t st, const Args &...args)
+{
     { const lamp_status_t as = attr.ensure(kernel, smem); if (as != LAMP_OK) return as; }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(grid);
@@ -473,7 +560,7 @@ lamp_status_t launch_tiles(Kernel kernel, SmemAttrOnce &attr, int smem, int thre
     }
     cfg.attrs = at;
     cfg.numAttrs = na;
-    return cudaLaunchKernelEx(&cfg, kernel, ml, mc, msl, msc, P) == cudaSuccess ? LAMP_OK : LAMP_ERR_CUDA;
+    return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess ? LAMP_OK : LAMP_ERR_CUDA;
 }
 
 template <int BN, int BLOCK, bool ODD>
@@ -481,18 +568,23 @@ lamp_status_t launch_pair(const lamp_fp4_operand_t *l, const lamp_fp4_operand_t 
 {
     using L = PairLayout<BN, BLOCK>;
     static SmemAttrOnce attr;
+    CUtensorMap ml, mc, msl, msc, my = {};
+    if (!encode_codes(l, 128, &ml) || !encode_codes(c, BN / 2, &mc) || !encode_scales(l, 1, &msl) || !encode_scales(c, L::CT, &msc)) return LAMP_ERR_CUDA;
+    if (!ODD && !encode_output(P, &my)) return LAMP_ERR_CUDA;
     const int64_t pairs = sm_count() / 2;
-    return launch_tiles(fp4_gemm_pair_kernel<BN, BLOCK, ODD>, attr, L::TOTAL, L::THREADS, 2 * (unsigned)(P.tiles < pairs ? P.tiles : pairs), 2, P.tiles <= 4 * pairs,
-                        l, c, BN / 2, L::CT, P, st);
+    return launch_tiles(fp4_gemm_pair_kernel<BN, BLOCK, ODD>, attr, L::TOTAL, L::THREADS, 2 * (unsigned)(P.tiles < pairs ? P.tiles : pairs), 2, P.tiles <= 4 * pairs, st,
+                        ml, mc, msl, msc, my, P);
 }
 template <int BN, int BLOCK, bool ODD>
 lamp_status_t launch_one(const lamp_fp4_operand_t *l, const lamp_fp4_operand_t *c, const GemmParams &P, cudaStream_t st)
 {
     using L = GemmLayout<BN, BLOCK>;
     static SmemAttrOnce attr;
+    CUtensorMap ml, mc, msl, msc;
+    if (!encode_codes(l, 128, &ml) || !encode_codes(c, BN, &mc) || !encode_scales(l, 1, &msl) || !encode_scales(c, 1, &msc)) return LAMP_ERR_CUDA;
     const int sms = sm_count();
-    return launch_tiles(fp4_gemm_kernel<BN, BLOCK, ODD>, attr, L::TOTAL, L::THREADS, (unsigned)(P.splits > 1 ? P.tiles * P.splits : P.tiles < sms ? P.tiles : sms),
-                        P.splits, P.tiles <= 4 * (int64_t)sms, l, c, BN, 1, P, st);
+    return launch_tiles(fp4_gemm_kernel<BN, BLOCK, ODD>, attr, L::TOTAL, L::THREADS, (unsigned)(P.splits > 1 ? P.tiles * P.splits : P.tiles < sms ? P.tiles : sms), P.splits,
+                        P.tiles <= 4 * (int64_t)sms, st, ml, mc, msl, msc, P);
 }
 
 template <int BLOCK>
@@ -506,8 +598,9 @@ lamp_status_t product(const lamp_fp4_operand_t *l, const lamp_fp4_operand_t *c, 
         const int64_t nl = (P.rows_l + 255) / 256, nc = (P.rows_c + bn - 1) / bn;
         if (P.swap || P.rows_c < bn || nl * nc * 2 < sms * 3 / 4) continue;
         P.nl = (int32_t)nl; P.nc = (int32_t)nc; P.tiles = nl * nc;
-        if (bn == 256) return odd ? launch_pair<256, BLOCK, true>(l, c, P, st) : launch_pair<256, BLOCK, false>(l, c, P, st);
-        return odd ? launch_pair<128, BLOCK, true>(l, c, P, st) : launch_pair<128, BLOCK, false>(l, c, P, st);
+        const bool unaligned = P.vec == 0;
+        if (bn == 256) return unaligned ? launch_pair<256, BLOCK, true>(l, c, P, st) : launch_pair<256, BLOCK, false>(l, c, P, st);
+        return unaligned ? launch_pair<128, BLOCK, true>(l, c, P, st) : launch_pair<128, BLOCK, false>(l, c, P, st);
     }
     const int bn = P.rows_c <= 16 ? 16 : P.rows_c <= 32 ? 32 : P.rows_c <= 64 ? 64 : 128;
     P.nl = (P.rows_l + 127) / 128;
