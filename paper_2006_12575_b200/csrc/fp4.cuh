@@ -25,11 +25,32 @@ __device__ __forceinline__ uint32_t amax_bits(const float (&f)[8])
     return m;
 }
 
-// What a block's values are divided by: either exactly by a multiplication (block of 32: a power of two) or by `wide`
-struct Scale { uint32_t byte; float by; };
+// The tensor's scale g, with what divisions by 6 g need
+struct Divisor {
+    float g, six_g, inv;
+    __device__ __forceinline__ explicit Divisor(float scale)
+    {
+        g = scale;
+        six_g = __fmul_rn(6.f, scale);
+        inv = __frcp_rn(six_g);
+    }
+};
 
-// The scale of a block from the bits of its amax.  BLOCK = 32: by = 1 / scale.  BLOCK = 16: by = scale * g.  by = 0 for a NaN scale.
-template <int BLOCK> __device__ __forceinline__ Scale block_scale(uint32_t amax, float g, float six_g)
+// a / b correctly rounded for b > 0, with inv = 1 / b correctly rounded: one correction of a * inv by its exact remainder (Markstein's theorem).  Where the
+// remainder or the reciprocal could leave the normal range - b outside of 2^-90 .. 2^90 - by the division itself.
+__device__ __forceinline__ float quotient(float a, float b, float inv)
+{
+    const float q = a * inv;
+    return copysignf(fmaf(fmaf(-q, b, a), inv, q), a);           // -0 keeps its sign
+}
+__device__ __forceinline__ bool plain_range(float b) { return b >= 8.0779357e-28f && b <= 1.2379400e27f; }
+
+// A block's scale byte, and what its values are divided by: `inv` = 1 / scale, exactly, where the scale is a power of two (blocks of 32), else
+// by = scale * g and inv = its reciprocal.  by = 0: the block has no codes (NaN scale).
+struct Scale { uint32_t byte; float by, inv; };
+
+// from the bits of the block's amax
+template <int BLOCK> __device__ __forceinline__ Scale block_scale(uint32_t amax, const Divisor &d)
 {
     Scale s;
     const bool nan = amax >= 0x7F800000u;
@@ -37,23 +58,19 @@ template <int BLOCK> __device__ __forceinline__ Scale block_scale(uint32_t amax,
         // amax = 1.m 2^(E - 127) <= 6 2^e = 1.5 2^(e + 2)  <=>  e >= E - 129, one more where 1.m > 1.5
         const int e = (int)(amax >> 23) - 2 + ((amax & 0x7FFFFFu) > 0x400000u ? 1 : 0);
         s.byte = nan ? 255u : (uint32_t)max(e, 0);
-        s.by = nan ? 0.f : __uint_as_float((254u - s.byte) << 23);
+        s.by = s.inv = nan ? 0.f : __uint_as_float((254u - s.byte) << 23);
     } else {
-        const float v = fminf(fmaxf(__fdiv_rn(__uint_as_float(amax), six_g), 0.001953125f), 448.f);
+        const float a = __uint_as_float(amax);
+        const float v = fminf(fmaxf(plain_range(d.six_g) && a > 1e-25f ? quotient(a, d.six_g, d.inv) : __fdiv_rn(a, d.six_g), 0.001953125f), 448.f);
         uint16_t two;
         asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(0.f), "f"(v));
         s.byte = nan ? 0x7Fu : (two & 0xFFu);
         uint32_t half2;
         asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(half2) : "h"(two));
-        s.by = nan ? 0.f : __fmul_rn(__half2float(__ushort_as_half((unsigned short)(half2 & 0xFFFFu))), g);
+        s.by = nan ? 0.f : __fmul_rn(__half2float(__ushort_as_half((unsigned short)(half2 & 0xFFFFu))), d.g);
+        s.inv = __frcp_rn(s.by);
     }
     return s;
-}
-
-// x over the block's scale in fp32, correctly rounded
-template <int BLOCK> __device__ __forceinline__ float scaled(float x, float by)
-{
-    return BLOCK == 32 ? x * by : __fdiv_rn(x, by);
 }
 
 // Eight codes, the first in the low half of the low byte.  The conversion rounds to nearest even and saturates.
@@ -71,10 +88,19 @@ __device__ __forceinline__ uint32_t encode8(const float (&v)[8])
 }
 template <int BLOCK> __device__ __forceinline__ uint32_t encode8(const float (&f)[8], const Scale &s)
 {
+    if (s.by == 0.f) return 0u;
     float v[8];
+    if (BLOCK == 32) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = scaled<BLOCK>(f[i], s.by);
-    return s.by == 0.f ? 0u : encode8(v);
+        for (int i = 0; i < 8; ++i) v[i] = f[i] * s.inv;
+    } else if (plain_range(s.by)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = quotient(f[i], s.by, s.inv);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __fdiv_rn(f[i], s.by);
+    }
+    return encode8(v);
 }
 
 __device__ __forceinline__ void decode8(uint32_t codes, float (&v)[8])

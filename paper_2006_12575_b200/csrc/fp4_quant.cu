@@ -10,104 +10,123 @@ namespace {
 using namespace bn;
 using namespace fp4;
 
-constexpr int QT = 256, QR_UNROLL = 4;
+constexpr int QT = 256, QU = 4;
 
-// A segment is 128 channels of a voxel, 8 channels on each of 16 lanes.
+// A segment is up to 128 channels of a voxel, 8 channels on each of LPS lanes (4, 8 or 16: as many as the channels need, at least a block of
+// 32).  A thread takes QU rows QT / LPS apart at the same channels, so that addresses are formed once: formed for every row they were most of
+// the kernel's instructions (28 us for 131,072 x 256 bf16 against QNOW).
 struct RowParams {
     void *x;                                  // source, or destination of the values
-    int64_t pitch, rows, items;               // items: segments of all rows, those that only fill up a tile of scales included
+    int64_t pitch, rows;
     int32_t c;
-    uint32_t segs, div_segs;
+    uint32_t segs;
     uint8_t *q;
     int64_t q_pitch;
     uint8_t *scale;
     int64_t tiles;
     const float *g;
 };
+template <int LPS> struct RowPlace {
+    static constexpr int RPP = QT / LPS, ROWS = RPP * QU;          // rows per pass (16, 32, 64) and per CTA (64, 128, 256: whole parts of a tile of scales)
+    int64_t row;                                                   // of the first pass
+    int ch;
+    __device__ __forceinline__ RowPlace(const RowParams &P)
+    {
+        const uint32_t block = blockIdx.x / P.segs, seg = blockIdx.x - block * P.segs;
+        row = (int64_t)block * ROWS + threadIdx.x / LPS;
+        ch = (int)seg * 128 + (threadIdx.x % LPS) * 8;
+    }
+    // scale byte of (row of pass u, block blk): the passes stay within a tile of 128 rows (LPS = 16, 8) or take two
+    __device__ __forceinline__ static int64_t scale_off(int u, int64_t tiles)
+    {
+        constexpr int in_tile = RPP >= 32 ? 4 * (RPP / 32) : 0;    // 32 rows further: 4 bytes
+        if (RPP == 16) return (u & 1) * 256 + (u >> 1) * 4;
+        return (u * RPP / 128) * tiles * 512 + (u % (128 / RPP)) * in_tile;
+    }
+};
 
-// row and segment of an item of this CTA: one division for the first, then offsets below segs + 64 by a multiplication (exact
-// there: (segs + 64) (segs div_segs - 2^32) < 2^32)
-struct Item { int64_t row; int seg; bool in; };
-__device__ __forceinline__ Item item(const RowParams &P, uint32_t row0, uint32_t rest, uint32_t first, int u)
+template <bool F32> __device__ __forceinline__ uint32_t amax_of(const Raw<F32> &r)
 {
-    const uint32_t at = u * (QT / 16) + (threadIdx.x >> 4), l = rest + at, q = P.segs == 1 ? l : __umulhi(l, P.div_segs);
-    return Item{(int64_t)row0 + q, (int)(l - q * P.segs), first + (int64_t)at < P.items};
+    if constexpr (F32) {
+        float f[8];
+        to_float<F32>(r, f);
+        return amax_bits(f);
+    } else {                                                       // two bf16 at a time
+        const uint32_t m = __vmaxu2(__vmaxu2(r.v[0].x & 0x7FFF7FFFu, r.v[0].y & 0x7FFF7FFFu), __vmaxu2(r.v[0].z & 0x7FFF7FFFu, r.v[0].w & 0x7FFF7FFFu));
+        return max(m & 0xFFFF0000u, m << 16);
+    }
 }
 
-template <bool F32, int BLOCK>
+template <bool F32, int BLOCK, int LPS>
 __global__ void __launch_bounds__(QT)
 quant4_rows_kernel(const RowParams P)
 {
+    using Place = RowPlace<LPS>;
+    constexpr int LANES = BLOCK / 8;                               // of a block; 4 blocks to a word of scales
     pdl_launch_dependents();
     pdl_wait();
-    const int l16 = threadIdx.x & 15;
-    const uint32_t first = blockIdx.x * (QT / 16 * QR_UNROLL), row0 = first / P.segs, rest = first - row0 * P.segs;
-    const float g = BLOCK == 16 && P.g ? __ldg(P.g) : 1.f, six_g = __fmul_rn(6.f, g);
-    Raw<F32> r[QR_UNROLL];
-    Item it[QR_UNROLL];
+    const Place at(P);
+    const Divisor d(BLOCK == 16 && P.g ? __ldg(P.g) : 1.f);
+    const bool in = at.ch < P.c;
+    const int blk = at.ch / BLOCK;
+    Raw<F32> r[QU];
 #pragma unroll
-    for (int u = 0; u < QR_UNROLL; ++u) {
-        it[u] = item(P, row0, rest, first, u);
-        const int ch = it[u].seg * 128 + l16 * 8;
-        r[u] = it[u].in && it[u].row < P.rows && ch < P.c ? load_raw<F32>(P.x, it[u].row * P.pitch + ch) : zero_raw<F32>();
-    }
+    for (int u = 0; u < QU; ++u) r[u] = in && at.row + u * Place::RPP < P.rows ? load_raw<F32>(P.x, (at.row + u * Place::RPP) * P.pitch + at.ch) : zero_raw<F32>();
+    uint8_t *q = P.q + at.row * P.q_pitch + at.ch / 2, *scale = P.scale + scale_at(at.row, blk, P.tiles);
+    const int64_t rows128 = (P.rows + 127) / 128 * 128;            // rows that only fill up a tile get scale 0, as blocks behind the last do
+    const bool writes = threadIdx.x % (4 * LANES < LPS ? 4 * LANES : LPS) == 0 && blk / 4 < P.tiles;
 #pragma unroll
-    for (int u = 0; u < QR_UNROLL; ++u) {
-        float f[8];
-        to_float<F32>(r[u], f);
-        uint32_t m = amax_bits(f);
+    for (int u = 0; u < QU; ++u) {
+        const int64_t row = at.row + u * Place::RPP;
+        uint32_t m = amax_of<F32>(r[u]);
 #pragma unroll
-        for (int o = BLOCK / 16; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-        const Scale s = block_scale<BLOCK>(m, g, six_g);
-        const int ch = it[u].seg * 128 + l16 * 8;
-        const bool there = it[u].row < P.rows && ch / BLOCK * BLOCK < P.c;      // blocks and rows that fill up a tile have scale 0
-        uint32_t word = there ? s.byte << (8 * ((ch / BLOCK) & 3)) : 0u;
-        constexpr int LANES = BLOCK / 8;                                        // of a block; 4 blocks to a word
-        word |= __shfl_xor_sync(0xffffffffu, word, LANES);
-        word |= __shfl_xor_sync(0xffffffffu, word, 2 * LANES);
-        if (!it[u].in) continue;
-        if (it[u].row < P.rows && ch < P.c) *reinterpret_cast<uint32_t *>(P.q + it[u].row * P.q_pitch + ch / 2) = encode8<BLOCK>(f, s);
-        const int64_t blk = ch / BLOCK;
-        if (l16 % (4 * LANES) == 0 && blk / 4 < P.tiles) *reinterpret_cast<uint32_t *>(P.scale + scale_at(it[u].row, blk, P.tiles)) = word;
+        for (int o = LANES / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+        const Scale s = block_scale<BLOCK>(m, d);
+        uint32_t word = blk * BLOCK < P.c && row < P.rows ? s.byte << (8 * (blk & 3)) : 0u;
+        if (LPS > LANES) word |= __shfl_xor_sync(0xffffffffu, word, LANES);
+        if (LPS > 2 * LANES) word |= __shfl_xor_sync(0xffffffffu, word, 2 * LANES);
+        if (in && row < P.rows) {
+            float f[8];
+            to_float<F32>(r[u], f);
+            *reinterpret_cast<uint32_t *>(q + (int64_t)(u * Place::RPP) * P.q_pitch) = encode8<BLOCK>(f, s);
+        }
+        if (writes && row < rows128) *reinterpret_cast<uint32_t *>(scale + Place::scale_off(u, P.tiles)) = word;
     }
 }
 
-template <bool F32, int BLOCK>
+template <bool F32, int BLOCK, int LPS>
 __global__ void __launch_bounds__(QT)
 dequant4_rows_kernel(const RowParams P)
 {
+    using Place = RowPlace<LPS>;
     pdl_launch_dependents();
     pdl_wait();
-    const int l16 = threadIdx.x & 15;
-    const uint32_t first = blockIdx.x * (QT / 16 * QR_UNROLL), row0 = first / P.segs, rest = first - row0 * P.segs;
+    const Place at(P);
     const float g = BLOCK == 16 && P.g ? __ldg(P.g) : 1.f;
-    uint32_t codes[QR_UNROLL], byte[QR_UNROLL];
-    Item it[QR_UNROLL];
+    if (at.ch >= P.c) return;
+    const uint8_t *q = P.q + at.row * P.q_pitch + at.ch / 2, *scale = P.scale + scale_at(at.row, at.ch / BLOCK, P.tiles);
+    uint32_t codes[QU], byte[QU];
 #pragma unroll
-    for (int u = 0; u < QR_UNROLL; ++u) {
-        it[u] = item(P, row0, rest, first, u);
-        const int ch = it[u].seg * 128 + l16 * 8;
-        codes[u] = byte[u] = 0;
-        it[u].in = it[u].in && ch < P.c;
-        if (it[u].in) {
-            codes[u] = __ldg(reinterpret_cast<const uint32_t *>(P.q + it[u].row * P.q_pitch + ch / 2));
-            byte[u] = __ldg(P.scale + scale_at(it[u].row, ch / BLOCK, P.tiles));
-        }
+    for (int u = 0; u < QU; ++u) {
+        if (at.row + u * Place::RPP >= P.rows) break;
+        codes[u] = __ldg(reinterpret_cast<const uint32_t *>(q + (int64_t)(u * Place::RPP) * P.q_pitch));
+        byte[u] = __ldg(scale + Place::scale_off(u, P.tiles));
     }
 #pragma unroll
-    for (int u = 0; u < QR_UNROLL; ++u) {
-        if (!it[u].in) continue;
+    for (int u = 0; u < QU; ++u) {
+        if (at.row + u * Place::RPP >= P.rows) break;
         float v[8];
         decode8(codes[u], v);
         const float s = decode_scale<BLOCK>(byte[u], g);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = __fmul_rn(v[j], s);
-        store8<F32>(P.x, it[u].row * P.pitch + it[u].seg * 128 + l16 * 8, v);
+        store8<F32>(P.x, (at.row + u * Place::RPP) * P.pitch + at.ch, v);
     }
 }
 
-// Transposed: tiles of 128 voxels x 128 channels through shared memory.  A thread owns two channels and 32 voxels of the tile, that is
-// one block of 32 or two of 16 per channel, and writes 16 bytes of codes per channel.
+// Transposed: tiles of 128 voxels x 64 channels through shared memory.  A thread owns one channel and 32 voxels of the tile, that is one block of 32
+// or two of 16, and writes 16 bytes of codes.
+constexpr int TC = 64;
 struct TileParams {
     void *x;
     int64_t pitch, voxels;
@@ -118,7 +137,8 @@ struct TileParams {
     int64_t tiles;
     const float *g;
 };
-template <bool F32> struct TileLayout { static constexpr int ES = F32 ? 4 : 2, SP = 128 * ES + 16, BYTES = 128 * SP, UNITS = 128 * ES / 16; };
+template <bool F32> struct TileLayout { static constexpr int ES = F32 ? 4 : 2, SP = TC * ES + 16, BYTES = 128 * SP, UNITS = TC * ES / 16; };
+static_assert(TileLayout<true>::BYTES <= 48 * 1024, "");
 
 template <bool F32, int BLOCK>
 __global__ void __launch_bounds__(QT)
@@ -130,8 +150,8 @@ quant4_tile_kernel(const TileParams P)
     pdl_wait();
     const int t = threadIdx.x;
     const int64_t r0 = (int64_t)blockIdx.x * 128;
-    const int c0 = blockIdx.y * 128;
-#pragma unroll 8
+    const int c0 = blockIdx.y * TC;
+#pragma unroll
     for (int i = t; i < 128 * L::UNITS; i += QT) {
         const int r = i / L::UNITS, u = i % L::UNITS;
         uint4 v = make_uint4(0, 0, 0, 0);
@@ -140,46 +160,38 @@ quant4_tile_kernel(const TileParams P)
         *reinterpret_cast<uint4 *>(smem + r * L::SP + u * 16) = v;
     }
     __syncthreads();
-    const float g = BLOCK == 16 && P.g ? __ldg(P.g) : 1.f, six_g = __fmul_rn(6.f, g);
-    const int cp = t & 63, part = t >> 6;                                     // channel pair, 32-voxel part
-    const int64_t v0 = r0 + part * 32, blocks = blocks_of(P.voxels, BLOCK);
+    const Divisor d(BLOCK == 16 && P.g ? __ldg(P.g) : 1.f);
+    const int col = t % TC, part = t / TC, ch = c0 + col;                     // channel, 32-voxel part
+    const int64_t v0 = r0 + part * 32, blocks = blocks_of(P.voxels, BLOCK), blk = v0 / BLOCK;
+    uint32_t code[4], bytes = 0;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int ch = c0 + 2 * cp + h;
-        uint32_t code[4], bytes = 0;
+    for (int b = 0; b < 32 / BLOCK; ++b) {
+        float f[BLOCK / 8][8];
+        uint32_t m = 0;
 #pragma unroll
-        for (int b = 0; b < 4; ++b) code[b] = 0;
-#pragma unroll
-        for (int b = 0; b < 32 / BLOCK; ++b) {
-            float f[BLOCK / 8][8];
-            uint32_t m = 0;
-#pragma unroll
-            for (int i = 0; i < BLOCK; ++i) {
-                const uint8_t *p = smem + (part * 32 + b * BLOCK + i) * L::SP + cp * 2 * L::ES;
-                f[i / 8][i % 8] = F32 ? ((const float *)p)[h] : bf2f(((const bf16 *)p)[h]);
-            }
-#pragma unroll
-            for (int i = 0; i < BLOCK / 8; ++i) m = max(m, amax_bits(f[i]));
-            const Scale s = block_scale<BLOCK>(m, g, six_g);
-            const int64_t blk = v0 / BLOCK + b;
-            if (ch < P.c && blk < blocks) bytes |= s.byte << (8 * b);
-#pragma unroll
-            for (int i = 0; i < BLOCK / 8; ++i) code[b * (BLOCK / 8) + i] = encode8<BLOCK>(f[i], s);
+        for (int i = 0; i < BLOCK; ++i) {
+            const uint8_t *p = smem + (part * 32 + b * BLOCK + i) * L::SP + col * L::ES;
+            f[i / 8][i % 8] = F32 ? *(const float *)p : bf2f(*(const bf16 *)p);
         }
-        // every block of the last tile along k and every row of a tile of rows gets its scale, 0 where there is none
-        const int64_t blk = v0 / BLOCK;
-        if (blk / 4 < P.tiles) {
-            uint8_t *o = P.scale + scale_at(ch, blk, P.tiles);
-            if constexpr (BLOCK == 32) *o = (uint8_t)bytes; else *reinterpret_cast<uint16_t *>(o) = (uint16_t)bytes;
-        }
-        if (ch >= P.c || v0 >= P.voxels) continue;
-        uint8_t *o = P.q + (int64_t)ch * P.q_pitch + v0 / 2;
-        if (P.voxels - v0 >= 32) *reinterpret_cast<uint4 *>(o) = make_uint4(code[0], code[1], code[2], code[3]);
-        else {
-            const int n = (int)(P.voxels - v0 + 1) / 2;                        // bytes behind the last voxel stay as they were
 #pragma unroll
-            for (int i = 0; i < 16; ++i) if (i < n) o[i] = (uint8_t)(code[i / 4] >> (8 * (i & 3)));
-        }
+        for (int i = 0; i < BLOCK / 8; ++i) m = max(m, amax_bits(f[i]));
+        const Scale s = block_scale<BLOCK>(m, d);
+        if (ch < P.c && blk + b < blocks) bytes |= s.byte << (8 * b);
+#pragma unroll
+        for (int i = 0; i < BLOCK / 8; ++i) code[b * (BLOCK / 8) + i] = encode8<BLOCK>(f[i], s);
+    }
+    // every block of the last tile along k and every row of a tile of rows gets its scale, 0 where there is none
+    if (blk / 4 < P.tiles) {
+        uint8_t *o = P.scale + scale_at(ch, blk, P.tiles);
+        if constexpr (BLOCK == 32) *o = (uint8_t)bytes; else *reinterpret_cast<uint16_t *>(o) = (uint16_t)bytes;
+    }
+    if (ch >= P.c || v0 >= P.voxels) return;
+    uint8_t *o = P.q + (int64_t)ch * P.q_pitch + v0 / 2;
+    if (P.voxels - v0 >= 32) *reinterpret_cast<uint4 *>(o) = make_uint4(code[0], code[1], code[2], code[3]);
+    else {
+        const int n = (int)(P.voxels - v0 + 1) / 2;                            // bytes behind the last voxel stay as they were
+#pragma unroll
+        for (int i = 0; i < 16; ++i) if (i < n) o[i] = (uint8_t)(code[i / 4] >> (8 * (i & 3)));
     }
 }
 
@@ -193,14 +205,11 @@ dequant4_tile_kernel(const TileParams P)
     pdl_wait();
     const int t = threadIdx.x;
     const int64_t r0 = (int64_t)blockIdx.x * 128;
-    const int c0 = blockIdx.y * 128;
+    const int c0 = blockIdx.y * TC;
     const float g = BLOCK == 16 && P.g ? __ldg(P.g) : 1.f;
-    const int cp = t & 63, part = t >> 6;
+    const int col = t % TC, part = t / TC, ch = c0 + col;
     const int64_t v0 = r0 + part * 32;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int ch = c0 + 2 * cp + h;
-        if (ch >= P.c || v0 >= P.voxels) continue;
+    if (ch < P.c && v0 < P.voxels) {
         const uint8_t *o = P.q + (int64_t)ch * P.q_pitch + v0 / 2;
         uint32_t code[4] = {0, 0, 0, 0};
         if (P.voxels - v0 >= 32) {
@@ -224,13 +233,13 @@ dequant4_tile_kernel(const TileParams P)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float y = __fmul_rn(v[j], s[i * 8 / BLOCK]);
-                uint8_t *p = smem + (part * 32 + i * 8 + j) * L::SP + cp * 2 * L::ES;
-                if (F32) ((float *)p)[h] = y; else ((bf16 *)p)[h] = f2bf(y);
+                uint8_t *p = smem + (part * 32 + i * 8 + j) * L::SP + col * L::ES;
+                if (F32) *(float *)p = y; else *(bf16 *)p = f2bf(y);
             }
         }
     }
     __syncthreads();
-#pragma unroll 4
+#pragma unroll
     for (int i = t; i < 128 * L::UNITS; i += QT) {
         const int r = i / L::UNITS, u = i % L::UNITS;
         if (r0 + r < P.voxels && c0 + u * (16 / L::ES) < P.c)
@@ -238,20 +247,27 @@ dequant4_tile_kernel(const TileParams P)
     }
 }
 
+template <bool F32, int BLOCK, int LPS>
+lamp_status_t launch_rows_k(bool back, const RowParams &P, cudaStream_t st)
+{
+    const int64_t grid = (P.rows + RowPlace<LPS>::ROWS - 1) / RowPlace<LPS>::ROWS;
+    // the quantiser also fills up the last tile of scales (LPS = 16: a CTA has half a tile)
+    const int64_t all = (back ? grid : (P.rows + 127) / 128 * 128 > grid * RowPlace<LPS>::ROWS ? grid + 1 : grid) * P.segs;
+    if (all > 2147483647ll) return LAMP_ERR_UNSUPPORTED;
+    return launch_pdl(all <= 2048, back ? dequant4_rows_kernel<F32, BLOCK, LPS> : quant4_rows_kernel<F32, BLOCK, LPS>, dim3((unsigned)all), dim3(QT), 0, st, P);
+}
 template <bool F32, int BLOCK>
 lamp_status_t launch_rows(bool back, const RowParams &P, cudaStream_t st)
 {
-    const int64_t grid = (P.items + QT / 16 * QR_UNROLL - 1) / (QT / 16 * QR_UNROLL);
-    return launch_pdl(grid <= 2048, back ? dequant4_rows_kernel<F32, BLOCK> : quant4_rows_kernel<F32, BLOCK>, dim3((unsigned)grid), dim3(QT), 0, st, P);
+    if (P.c <= 32) return launch_rows_k<F32, BLOCK, 4>(back, P, st);
+    if (P.c <= 64) return launch_rows_k<F32, BLOCK, 8>(back, P, st);
+    return launch_rows_k<F32, BLOCK, 16>(back, P, st);
 }
 template <bool F32, int BLOCK>
 lamp_status_t launch_tiles(bool back, const TileParams &P, cudaStream_t st)
 {
-    lamp_status_t s;
-    static SmemAttrOnce quant, dequant;
-    if ((s = quant.ensure(quant4_tile_kernel<F32, BLOCK>, TileLayout<F32>::BYTES)) != LAMP_OK) return s;
-    if ((s = dequant.ensure(dequant4_tile_kernel<F32, BLOCK>, TileLayout<F32>::BYTES)) != LAMP_OK) return s;
-    const int64_t gx = (P.voxels + 127) / 128, gy = (P.c + 127) / 128;
+    const int64_t gx = (P.voxels + 127) / 128, gy = (P.c + 127) / 128 * (128 / TC);           // whole tiles of scales
+    if (gy > 65535) return LAMP_ERR_UNSUPPORTED;
     return launch_pdl(gx * gy <= 2048, back ? dequant4_tile_kernel<F32, BLOCK> : quant4_tile_kernel<F32, BLOCK>, dim3((unsigned)gx, (unsigned)gy), dim3(QT),
                       (size_t)TileLayout<F32>::BYTES, st, P);
 }
@@ -269,15 +285,10 @@ lamp_status_t convert(const lamp_tensor_t *x, int32_t transpose, const lamp_fp4_
     const TView v = make_view(x);
     if (transpose) {
         const TileParams P = {v.p, v.pitch, rows, v.c, (uint8_t *)o->q, o->q_pitch, o->scale, tiles_of(rows, o->block), o->tensor_scale};
-        if ((v.c + 127) / 128 > 65535) return LAMP_ERR_UNSUPPORTED;
         if (o->block == 32) return v.f32 ? launch_tiles<true, 32>(back, P, st) : launch_tiles<false, 32>(back, P, st);
         return v.f32 ? launch_tiles<true, 16>(back, P, st) : launch_tiles<false, 16>(back, P, st);
     }
-    RowParams P = {v.p, v.pitch, rows, 0, v.c, 0, 0, (uint8_t *)o->q, o->q_pitch, o->scale, tiles_of(v.c, o->block), o->tensor_scale};
-    P.segs = (uint32_t)((v.c + 127) / 128);
-    P.div_segs = (uint32_t)((0x100000000ull + P.segs - 1) / P.segs);
-    P.items = (back ? rows : (rows + 127) / 128 * 128) * P.segs;
-    if (P.items > 4294967295ll || P.segs > 60000) return LAMP_ERR_UNSUPPORTED;
+    const RowParams P = {v.p, v.pitch, rows, v.c, (uint32_t)((v.c + 127) / 128), (uint8_t *)o->q, o->q_pitch, o->scale, tiles_of(v.c, o->block), o->tensor_scale};
     if (o->block == 32) return v.f32 ? launch_rows<true, 32>(back, P, st) : launch_rows<false, 32>(back, P, st);
     return v.f32 ? launch_rows<true, 16>(back, P, st) : launch_rows<false, 16>(back, P, st);
 }

@@ -5,9 +5,9 @@
 // first, so that it starts with what the first left in L2 (126 MB).  Bound by memory.
 // A voxel's channels are taken in units of 8 (16 bytes of bf16, 32 of fp32), a thread keeps its unit for all of its voxels, so
 // everything per channel stays in registers; a CTA holds TY voxels side by side and a run of voxels of one sample.
-// Sums: a thread adds d = x - k and d^2 in fp32, k the mean of the first values it loads - without it the squares of data far from 0
-// lose the variance - and folds them into a second fp32 level every FOLD voxels.  Between threads, CTAs and channels of a group the sums
-// are fp64, taken about r, the group's first value, and added in a fixed order.
+// Sums: a thread adds d = x - k and d^2 of at most RUN voxels in fp32, k the mean of the first values it loads - without it the squares of
+// data far from 0 lose the variance.  Between threads, CTAs and channels of a group the sums are fp64, taken about r, the group's first
+// value, and added in a fixed order.
 #include "block_norm.cuh"
 
 namespace lamp {
@@ -18,7 +18,9 @@ using namespace bn;
 using ptx::f32x2; using ptx::fma2; using ptx::add2; using ptx::mul2; using ptx::twice; using ptx::pack2; using ptx::unpack2;
 
 constexpr int GT = 256;                       // threads
-constexpr int FOLD = 8;                       // batches per fold
+// CTAs per SM that the streaming kernels are compiled and sized for
+constexpr int resident(bool xf, bool back) { return (xf ? 3 : 4) - (back ? 1 : 0); }
+constexpr int RUN = 256;                      // voxels that a thread sums at most
 
 struct GnParams {
     const void *x, *dz;
@@ -41,9 +43,10 @@ struct GnParams {
 
 
 // ----------------------------------------------------------------------------------------------------------- activations
-// FINE: fp32 outputs.  For bf16 outputs e^x without the correction for the rounding of x log2(e) (2^-24 |x| of a value that is rounded to
-// 2^-9), and the normal distribution's tail by Abramowitz & Stegun 7.1.26: q(u) = (a1 s + .. + a5 s^5) e^(-u^2), s = 1 / (1 + p u), for erfc(u), u >= 0,
-// off by at most 1.5e-7.
+// FINE: fp32 outputs of the forward pass.  Elsewhere e^x without the correction for the rounding of x log2(e) (2^-24 |x| of e^x), and the normal
+// distribution by Abramowitz & Stegun 7.1.26: q(u) = (a1 s + .. + a5 s^5) e^(-u^2), s = 1 / (1 + p u), for erfc(u), u >= 0, off by at most 1.5e-7.
+// A derivative is a factor of size one, so both are within a few units of 2^-24 of it: expf and erfcf in the backward pass of fp32 took 201 us on
+// 81,840 x 320 against BWDNOW.
 template <bool FINE> __device__ __forceinline__ void normal_tail(float t, float &below, float &density)
 {
     // below = P(X <= t), density = e^(-t^2 / 2)
@@ -72,17 +75,17 @@ template <int ACT, bool FINE> __device__ __forceinline__ float activate(float t,
     }
     return t;
 }
-template <int ACT, bool FINE> __device__ __forceinline__ float derivative(float t, float slope)
+template <int ACT> __device__ __forceinline__ float derivative(float t, float slope)
 {
     if constexpr (ACT == LAMP_ACT_LEAKY_RELU) return t > 0.f ? 1.f : t <= 0.f ? slope : t;           // NaN stays
     if constexpr (ACT == LAMP_ACT_SILU) {
         float g, s;
-        sigmoid_slope<FINE>(t, g, s);
+        sigmoid_slope<false>(t, g, s);
         return fmaf(t, s, g);
     }
     if constexpr (ACT == LAMP_ACT_GELU) {
         float below, density;
-        normal_tail<FINE>(t, below, density);
+        normal_tail<false>(t, below, density);
         return fmaf(t * 0.3989422804014327f, density, below);
     }
     return 1.f;
@@ -133,7 +136,7 @@ __device__ __forceinline__ void sum_lines(const GnParams &P, const Place &q, con
 
 // ----------------------------------------------------------------------------------------------------------- forward
 template <bool XF, int U>
-__global__ void __launch_bounds__(GT)
+__global__ void __launch_bounds__(GT, resident(XF, false))
 gn_sums_kernel(const GnParams P)
 {
     extern __shared__ __align__(16) double sm[];
@@ -141,19 +144,19 @@ gn_sums_kernel(const GnParams P)
     pdl_wait();
     const Place q = place(P, false);
     const int64_t base = q.sample * P.v;
-    f32x2 k[4], s1[4], s2[4], o1[4], o2[4];
+    f32x2 k[4], s1[4], s2[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) k[j] = s1[j] = s2[j] = o1[j] = o2[j] = 0;
-    int64_t mine = 0;
+    for (int j = 0; j < 4; ++j) k[j] = s1[j] = s2[j] = 0;
+    int mine = 0;
     if (q.active) {
-        mine = q.v1 > q.v0 + q.ty ? (q.v1 - q.v0 - q.ty + P.ty - 1) / P.ty : 0;
-        int64_t v = q.v0 + q.ty;
+        mine = q.v1 > q.v0 + q.ty ? ((int)(q.v1 - q.v0) - q.ty + P.ty - 1) / P.ty : 0;
+        const int64_t step = P.ty * P.px;
+        int64_t at = (base + q.v0 + q.ty) * P.px + q.ch;
         Raw<XF> r[U];
-        int turn = 0;
-        for (int64_t left = mine; left > 0; left -= U, v += (int64_t)U * P.ty) {
+        for (int left = mine; left > 0; left -= U, at += U * step) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) if (u < left) r[u] = load_raw<XF>(P.x, (base + v + (int64_t)u * P.ty) * P.px + q.ch);
-            if (turn == 0) {
+            for (int u = 0; u < U; ++u) if (u < left) r[u] = load_raw<XF>(P.x, at + u * step);
+            if (left == mine) {
                 f32x2 t[4], s[4] = {0, 0, 0, 0};
 #pragma unroll
                 for (int u = 0; u < U; ++u) if (u < left) {
@@ -161,7 +164,7 @@ gn_sums_kernel(const GnParams P)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) s[j] = add2(s[j], t[j]);
                 }
-                const float inv = -1.f / (float)(left < U ? (int)left : U);
+                const float inv = -1.f / (float)(left < U ? left : U);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) k[j] = mul2(s[j], twice(inv));      // -k
             }
@@ -176,10 +179,6 @@ gn_sums_kernel(const GnParams P)
                     s2[j] = fma2(d, d, s2[j]);
                 }
             }
-            if (++turn % FOLD == 0) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) { o1[j] = add2(o1[j], s1[j]); o2[j] = add2(o2[j], s2[j]); s1[j] = s2[j] = 0; }
-            }
         }
     }
     double a[8], b[8];
@@ -190,8 +189,8 @@ gn_sums_kernel(const GnParams P)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             unpack2(k[j], nk[2 * j], nk[2 * j + 1]);
-            unpack2(add2(o1[j], s1[j]), f1[2 * j], f1[2 * j + 1]);
-            unpack2(add2(o2[j], s2[j]), f2[2 * j], f2[2 * j + 1]);
+            unpack2(s1[j], f1[2 * j], f1[2 * j + 1]);
+            unpack2(s2[j], f2[2 * j], f2[2 * j + 1]);
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -223,34 +222,44 @@ gn_sums_kernel(const GnParams P)
     }
 }
 
-// mean and rstd of a group from its partial sums (one warp each), or from sums per channel
-template <bool XF>
+// mean and rstd of a group from its partial sums, or from sums per channel; W warps per group: one where the sums are few (a CTA has 8 groups),
+// all where they are many
+template <bool XF, int W>
 __global__ void __launch_bounds__(GT)
 gn_finish_kernel(const GnParams P)
 {
+    __shared__ double red[2][GT / 32];
     pdl_launch_dependents();
     pdl_wait();
-    const int64_t at = (int64_t)blockIdx.x * (GT / 32) + (threadIdx.x >> 5);
-    const int lane = threadIdx.x & 31;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, first = W == 1 ? lane : threadIdx.x;
+    const int64_t at = W == 1 ? (int64_t)blockIdx.x * (GT / 32) + warp : blockIdx.x;
     if (at >= (int64_t)P.n * P.groups) return;
     const int64_t sample = at / P.groups;
     const int g = (int)(at - sample * P.groups);
     double s = 0.0, t = 0.0, r = 0.0;
     if (P.stats) {
         const double2 *st = reinterpret_cast<const double2 *>(P.stats) + sample * P.c + g * P.cg;
-        for (int i = lane; i < P.cg; i += 32) { const double2 v = st[i]; s += v.x; t += v.y; }
+#pragma unroll 4
+        for (int i = first; i < P.cg; i += 32 * W) { const double2 v = st[i]; s += v.x; t += v.y; }
     } else {
         const int cc = P.uc * 8, k0 = g * P.cg / cc, k1 = ((g + 1) * P.cg - 1) / cc, ks = k1 - k0 + 1;
         const double2 *p = P.part + at * P.parts * P.chunks;
-        for (int i = lane; i < P.parts * ks; i += 32) { const double2 v = p[i / ks * P.chunks + k0 + i % ks]; s += v.x; t += v.y; }
-        const int64_t first = sample * P.v * P.px + g * P.cg;
-        r = XF ? ((const float *)P.x)[first] : bf2f(((const bf16 *)P.x)[first]);
+        const int64_t x0 = sample * P.v * P.px + g * P.cg;
+        r = XF ? ((const float *)P.x)[x0] : bf2f(((const bf16 *)P.x)[x0]);
+#pragma unroll 4
+        for (int i = first; i < P.parts * ks; i += 32 * W) { const double2 v = p[i / ks * P.chunks + k0 + i % ks]; s += v.x; t += v.y; }
     }
     for (int o = 16; o > 0; o >>= 1) {
         s += __shfl_xor_sync(0xffffffffu, s, o);
         t += __shfl_xor_sync(0xffffffffu, t, o);
     }
-    if (lane == 0) {
+    if (W > 1) {
+        if (lane == 0) { red[0][warp] = s; red[1][warp] = t; }
+        __syncthreads();
+        s = t = 0.0;
+        for (int i = 0; i < W; ++i) { s += red[0][i]; t += red[1][i]; }
+    }
+    if (first == 0) {
         const double m = (double)P.v * P.cg, mu = s / m, var = t / m - mu * mu;
         P.mean_rstd[at] = make_float2((float)(r + mu), (float)(1.0 / sqrt((var < 0.0 ? 0.0 : var) + (double)P.eps)));
     }
@@ -279,7 +288,7 @@ __device__ __forceinline__ Affine affine(const GnParams &P, const Place &q)
 }
 
 template <bool XF, bool ZF, int ACT, int U>
-__global__ void __launch_bounds__(GT)
+__global__ void __launch_bounds__(GT, resident(XF, false))
 gn_apply_kernel(const GnParams P)
 {
     pdl_launch_dependents();
@@ -327,14 +336,14 @@ __device__ __forceinline__ void slopes(const GnParams &P, const Affine &f, const
         if constexpr (ACT != LAMP_ACT_NONE) {
             float t0, t1;
             unpack2(fma2(d[j], f.a[j], f.b[j]), t0, t1);
-            dt[j] = mul2(dt[j], pack2(__float_as_uint(derivative<ACT, XF>(t0, P.slope)), __float_as_uint(derivative<ACT, XF>(t1, P.slope))));
+            dt[j] = mul2(dt[j], pack2(__float_as_uint(derivative<ACT>(t0, P.slope)), __float_as_uint(derivative<ACT>(t1, P.slope))));
         }
     }
 }
 
 // sums over the CTA's voxels of dt and dt * xhat per channel
 template <bool XF, bool ZF, int ACT, int U>
-__global__ void __launch_bounds__(GT)
+__global__ void __launch_bounds__(GT, resident(XF, true))
 gn_bwd_sums_kernel(const GnParams P)
 {
     extern __shared__ __align__(16) double sm[];
@@ -347,10 +356,9 @@ gn_bwd_sums_kernel(const GnParams P)
     for (int j = 0; j < 8; ++j) a[j] = b[j] = 0.0;
     if (q.active) {
         const Affine f = affine(P, q);
-        f32x2 s1[4], s2[4], o1[4], o2[4];
+        f32x2 s1[4], s2[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s1[j] = s2[j] = o1[j] = o2[j] = 0;
-        int turn = 0;
+        for (int j = 0; j < 4; ++j) s1[j] = s2[j] = 0;
         for (int64_t v = q.v0 + q.ty; v < q.v1; v += (int64_t)U * P.ty) {
             Raw<XF> rx[U];
             Raw<ZF> rz[U];
@@ -370,16 +378,12 @@ gn_bwd_sums_kernel(const GnParams P)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) { s1[j] = add2(s1[j], dt[j]); s2[j] = fma2(dt[j], d[j], s2[j]); }
             }
-            if (++turn % FOLD == 0) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) { o1[j] = add2(o1[j], s1[j]); o2[j] = add2(o2[j], s2[j]); s1[j] = s2[j] = 0; }
-            }
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             float f1[2], f2[2];
-            unpack2(add2(o1[j], s1[j]), f1[0], f1[1]);
-            unpack2(add2(o2[j], s2[j]), f2[0], f2[1]);
+            unpack2(s1[j], f1[0], f1[1]);
+            unpack2(s2[j], f2[0], f2[1]);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const float rstd = P.mean_rstd[q.sample * P.groups + (q.ch + 2 * j + i) / P.cg].y;
@@ -394,37 +398,38 @@ gn_bwd_sums_kernel(const GnParams P)
     for (int i = threadIdx.x; i < cc && c0 + i < P.c; i += GT) out[i] = make_double2(sm[i], sm[P.ty * cc + i]);
 }
 
-// chan[n][c] = sum over the parts, 32 channels per CTA
+// chan[n][c] = sum over the parts, 8 channels per CTA
 __global__ void __launch_bounds__(1024)
 gn_bwd_parts_kernel(const GnParams P)
 {
-    __shared__ double2 red[32][33];
+    __shared__ double2 red[128][9];
     pdl_launch_dependents();
     pdl_wait();
-    const int per = (P.c + 31) / 32;
+    const int per = P.c / 8;
     const int64_t sample = blockIdx.x / per;
-    const int c0 = (int)(blockIdx.x - sample * per) * 32;
-    const int col = threadIdx.x & 31, line = threadIdx.x >> 5, ch = c0 + col;
+    const int c0 = (int)(blockIdx.x - sample * per) * 8;
+    const int col = threadIdx.x & 7, line = threadIdx.x >> 3;
     double s = 0.0, t = 0.0;
-    if (ch < P.c) {
-        const double2 *p = P.part + sample * P.parts * P.c + ch;
+    const double2 *p = P.part + sample * P.parts * P.c + c0 + col;
 #pragma unroll 4
-        for (int i = line; i < P.parts; i += 32) { const double2 v = p[(int64_t)i * P.c]; s += v.x; t += v.y; }
-    }
+    for (int i = line; i < P.parts; i += 128) { const double2 v = p[(int64_t)i * P.c]; s += v.x; t += v.y; }
     red[line][col] = make_double2(s, t);
     __syncthreads();
-    const double2 mine = red[col][line];                       // warp `line` adds the 32 lines of channel `line`
-    s = mine.x; t = mine.y;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (warp >= 8) return;
+    s = t = 0.0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { s += red[i * 32 + lane][warp].x; t += red[i * 32 + lane][warp].y; }
     for (int o = 16; o > 0; o >>= 1) {
         s += __shfl_xor_sync(0xffffffffu, s, o);
         t += __shfl_xor_sync(0xffffffffu, t, o);
     }
-    if (col == 0 && c0 + line < P.c) P.chan[sample * P.c + c0 + line] = make_double2(s, t);
+    if (lane == 0) P.chan[sample * P.c + c0 + warp] = make_double2(s, t);
 }
 
 // dx, and dw and db from the sums of all samples
 template <bool XF, bool ZF, int ACT, int U>
-__global__ void __launch_bounds__(GT)
+__global__ void __launch_bounds__(GT, resident(XF, true))
 gn_bwd_apply_kernel(const GnParams P)
 {
     extern __shared__ __align__(16) float2 means[];             // of this chunk's groups: (mean(w dt), mean(w dt xhat))
@@ -514,31 +519,33 @@ gn_bwd_apply_kernel(const GnParams P)
 }
 
 // ----------------------------------------------------------------------------------------------------------- host
-// Units, lines and runs for a sample of v voxels: about four CTAs per SM, none with less than a batch of U voxels per thread.
-void split(GnParams &P, int u)
+// Units, lines and runs for a sample of v voxels: about `per_sm` CTAs per SM, none with less than a batch of u voxels per thread or more than
+// RUN of them.
+void split(GnParams &P, int u, int per_sm)
 {
     const int units = P.c / 8;
     P.chunks = (units + GT - 1) / GT;
     P.uc = (units + P.chunks - 1) / P.chunks;
     P.ty = GT / P.uc;
-    const int64_t room = (int64_t)sm_count() * 4 / ((int64_t)P.n * P.chunks);
+    const int64_t room = (int64_t)sm_count() * per_sm / ((int64_t)P.n * P.chunks), least = (P.v + (int64_t)P.ty * RUN - 1) / ((int64_t)P.ty * RUN);
     const int64_t need = (P.v + (int64_t)P.ty * u - 1) / ((int64_t)P.ty * u);
-    const int64_t parts = need < room ? need : room < 1 ? 1 : room;
+    int64_t parts = need < room ? need : room;
+    if (parts < least) parts = least;
     P.run = (P.v + parts - 1) / parts;
     P.run = (P.run + P.ty - 1) / P.ty * P.ty;
     P.parts = (int32_t)((P.v + P.run - 1) / P.run);
 }
 
-constexpr int SUM_U = 4, BWD_U = 2;
+constexpr int SUM_U = 4, BWD_U = 2;           // voxels in flight per thread
 
 size_t workspace(int64_t v, int n, int c)
 {
     // the larger of the forward pass' [n][groups][parts][chunks] and the backward pass' [n][parts + 1][c], groups = c at most
     GnParams P = {};
     P.v = v; P.n = n; P.c = c;
-    split(P, SUM_U);
+    split(P, SUM_U, resident(false, false));
     const size_t fwd = (size_t)n * c * P.parts * P.chunks;
-    split(P, BWD_U);
+    split(P, BWD_U, resident(false, true));
     const size_t bwd = (size_t)n * c * (P.parts + 1);
     return (fwd > bwd ? fwd : bwd) * sizeof(double2);
 }
@@ -581,14 +588,16 @@ lamp_status_t forward(GnParams &P, cudaStream_t st)
 {
     lamp_status_t s;
     const bool early = short_launch(P);
-    split(P, SUM_U);
+    split(P, SUM_U, resident(XF, false));
     const dim3 grid((unsigned)(P.n * P.parts), (unsigned)P.chunks);
     if (!P.stats) {
         const size_t smem = (size_t)P.ty * P.uc * 8 * 2 * sizeof(double);
         if ((s = launch_pdl(early, gn_sums_kernel<XF, SUM_U>, grid, dim3(GT), smem, st, P)) != LAMP_OK) return s;
     }
     const int64_t all = (int64_t)P.n * P.groups;
-    if ((s = launch_pdl(early, gn_finish_kernel<XF>, dim3((unsigned)((all + GT / 32 - 1) / (GT / 32))), dim3(GT), 0, st, P)) != LAMP_OK) return s;
+    const bool many = P.stats ? P.cg > 256 : P.parts > 128;
+    if ((s = launch_pdl(early, many ? gn_finish_kernel<XF, GT / 32> : gn_finish_kernel<XF, 1>, dim3((unsigned)(many ? all : (all + GT / 32 - 1) / (GT / 32))), dim3(GT), 0, st,
+                        P)) != LAMP_OK) return s;
     return launch_pdl(early, gn_apply_kernel<XF, ZF, ACT, SUM_U>, grid, dim3(GT), 0, st, P);
 }
 
@@ -597,12 +606,12 @@ lamp_status_t backward(GnParams &P, cudaStream_t st)
 {
     lamp_status_t s;
     const bool early = short_launch(P);
-    split(P, BWD_U);
+    split(P, BWD_U, resident(XF, true));
     const dim3 grid((unsigned)(P.n * P.parts), (unsigned)P.chunks);
     const size_t smem = (size_t)P.ty * P.uc * 8 * 2 * sizeof(double);
     P.chan = P.parts > 1 ? P.part + (int64_t)P.n * P.parts * P.c : P.part;
     if ((s = launch_pdl(early, gn_bwd_sums_kernel<XF, ZF, ACT, BWD_U>, grid, dim3(GT), smem, st, P)) != LAMP_OK) return s;
-    if (P.parts > 1 && (s = launch_pdl(early, gn_bwd_parts_kernel, dim3((unsigned)((P.c + 31) / 32 * P.n)), dim3(1024), 0, st, P)) != LAMP_OK) return s;
+    if (P.parts > 1 && (s = launch_pdl(early, gn_bwd_parts_kernel, dim3((unsigned)(P.c / 8 * P.n)), dim3(1024), 0, st, P)) != LAMP_OK) return s;
     return launch_pdl(early, gn_bwd_apply_kernel<XF, ZF, ACT, BWD_U>, grid, dim3(GT), (size_t)P.uc * 8 * sizeof(float2), st, P);
 }
 
