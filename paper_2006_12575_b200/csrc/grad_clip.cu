@@ -2,8 +2,8 @@
 //
 // Bound by memory: the norm reads every gradient once, the scaling reads and writes it.  The tensors' table travels in the
 // kernel's parameters (a captured graph keeps it), so no copy to the device precedes a call.  The elements are cut into pieces of
-// PIECE, laid from a 16-byte boundary of their tensor; a CTA takes a contiguous run of pieces, the scaling the runs in the opposite
-// order, so that it starts with what the norm left in L2.
+// 32 KB, laid from a 16-byte boundary of their tensor; a CTA takes a contiguous run of pieces, the scaling the same run backwards, so that
+// it starts with what the norm left in L2.
 // Sums: 8 squares in fp32 where that stays well inside its range, otherwise the 8 again in fp64; fp64 beyond, per thread, then over the
 // CTA in a fixed order, one partial sum per CTA.  Every CTA of the scaling adds all of them in the same order: no counter, no atomic, nothing
 // that has to be zero beforehand.
@@ -15,7 +15,9 @@ namespace {
 
 using namespace bn;
 
-constexpr int CT = 256, PIECE = 8192;
+constexpr int CT = 256, UNITS = 8;              // threads, 16-byte units of a piece per thread: neighbouring lanes take neighbouring units
+__host__ __device__ constexpr int piece_of(bool f32) { return CT * UNITS * (f32 ? 4 : 8); }                    // elements
+constexpr int CTAS = 4;                       // per SM: all of them resident, so that the sum over the parts is formed once per place
 
 struct Entry {
     const void *g;
@@ -40,66 +42,108 @@ __host__ __device__ __forceinline__ int64_t head_of(const void *p, int64_t n, bo
 __host__ __forceinline__ int64_t pieces_of(const lamp_grad_t &t)
 {
     if (t.n == 0) return 0;
-    const int64_t body = t.n - head_of(t.g, t.n, t.dtype == LAMP_F32);
-    return body == 0 ? 1 : (body + PIECE - 1) / PIECE;
+    const bool f32 = t.dtype == LAMP_F32;
+    const int64_t body = t.n - head_of(t.g, t.n, f32), piece = piece_of(f32);
+    return body == 0 ? 1 : (body + piece - 1) / piece;
 }
 
-// The run of pieces of this CTA, tensor by tensor: f(entry, first element of the body of the piece, its end, whether the head comes with it).
-template <int N, typename F>
-__device__ __forceinline__ void for_pieces(const Table<N> &T, int64_t block, F f)
+// The run of pieces of this CTA, tensor by tensor, forwards or BACK: f(entry, first element of the body of the piece, its end, elements of the head).
+template <bool BACK, int N, typename F>
+__device__ __forceinline__ void for_pieces(const Table<N> &T, F f)
 {
-    const int p0 = (int)((int64_t)T.pieces * block / gridDim.x), p1 = (int)((int64_t)T.pieces * (block + 1) / gridDim.x);
+    const int p0 = (int)((int64_t)T.pieces * blockIdx.x / gridDim.x), p1 = (int)((int64_t)T.pieces * (blockIdx.x + 1) / gridDim.x);
     if (p0 >= p1) return;
-    int lo = 0, hi = T.count - 1;             // the last entry that starts at p0 or before it (entries without pieces lie in front of their successor)
+    const int start = BACK ? p1 - 1 : p0;
+    int lo = 0, hi = T.count - 1;             // the entry of piece `start`: the last that begins at it or before it
     while (lo < hi) {
         const int mid = (lo + hi + 1) / 2;
-        if (T.e[mid].first <= p0) lo = mid; else hi = mid - 1;
+        if (T.e[mid].first <= start) lo = mid; else hi = mid - 1;
     }
-    for (int i = lo, p = p0; p < p1; ++i) {
+    for (int i = lo, p = start; BACK ? p >= p0 : p < p1; i += BACK ? -1 : 1) {
         const Entry &e = T.e[i];
         const int end = i + 1 < T.count ? T.e[i + 1].first : T.pieces;
         const int64_t h = head_of(e.g, e.n, e.f32);
-        for (; p < p1 && p < end; ++p) {
-            const int64_t b0 = h + (int64_t)(p - e.first) * PIECE;
-            f(e, b0, b0 + PIECE < e.n ? b0 + PIECE : e.n, p == e.first ? h : 0);
+        for (; BACK ? p >= p0 && p >= e.first : p < p1 && p < end; p += BACK ? -1 : 1) {
+            const int64_t b0 = h + (int64_t)(p - e.first) * piece_of(e.f32), b1 = b0 + piece_of(e.f32);
+            f(e, b0, b1 < e.n ? b1 : e.n, p == e.first ? h : 0);
         }
     }
 }
 
 __device__ __forceinline__ float element(const void *p, int64_t i, int f32) { return f32 ? ((const float *)p)[i] : bf2f(((const bf16 *)p)[i]); }
 
-template <bool F32> __device__ __forceinline__ void add_squares(const Raw<F32> &r, double &acc)
+// 16 bytes as pairs of fp32, and their squares added to `s`
+template <bool F32> __device__ __forceinline__ void unit_pairs(const uint4 &u, ptx::f32x2 (&v)[F32 ? 2 : 4])
 {
-    ptx::f32x2 v[4];
-    to_pairs<F32>(r, v);
-    const float s = both(ptx::fma2(v[3], v[3], ptx::fma2(v[2], v[2], ptx::fma2(v[1], v[1], ptx::mul2(v[0], v[0])))));
+    if constexpr (F32) {
+        v[0] = ptx::pack2(u.x, u.y); v[1] = ptx::pack2(u.z, u.w);
+    } else {
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = ptx::pack2(w[i] << 16, w[i] & 0xFFFF0000u);
+    }
+}
+// N units = 8 values
+template <bool F32, int N> __device__ __forceinline__ void add_squares(const uint4 (&r)[N], double &acc)
+{
+    constexpr int PAIRS = F32 ? 2 : 4;
+    static_assert(N * PAIRS == 4, "");
+    ptx::f32x2 v[N][PAIRS], sum = 0;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        unit_pairs<F32>(r[n], v[n]);
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) sum = ptx::fma2(v[n][i], v[n][i], sum);
+    }
+    const float s = both(sum);
     if (s >= 8.6736174e-19f && s <= 1.3292279957849159e36f) {        // 2^-60 .. 2^120: what underflowed is nothing beside s
         acc += (double)s;
     } else {
-        float f[8];
-        to_float<F32>(r, f);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc = fma((double)f[j], (double)f[j], acc);
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i) {
+                float a, b;
+                ptx::unpack2(v[n][i], a, b);
+                acc = fma((double)a, (double)a, acc);
+                acc = fma((double)b, (double)b, acc);
+            }
+    }
+}
+
+// The units of a piece: all of them loaded, the ones that the tensor's end cuts left zero.  f(first element) for the elements of a cut unit.
+template <bool F32, typename Tail>
+__device__ __forceinline__ void load_piece(const void *g, int64_t b0, int64_t b1, uint4 (&r)[UNITS], Tail tail)
+{
+    constexpr int E = F32 ? 4 : 8;
+    const uint4 *p = (const uint4 *)((const char *)g + b0 * (F32 ? 4 : 2)) + threadIdx.x;
+    if (b1 - b0 == piece_of(F32)) {
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) r[u] = p[u * CT];
+        return;
+    }
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) {
+        const int64_t at = b0 + (int64_t)(u * CT + threadIdx.x) * E;
+        r[u] = make_uint4(0, 0, 0, 0);
+        if (at + E <= b1) r[u] = p[u * CT];
+        else for (int64_t i = at; i < b1; ++i) tail(i);
     }
 }
 
 template <bool F32> __device__ __forceinline__ void piece_squares(const void *g, int64_t b0, int64_t b1, double &acc)
 {
-    constexpr int U = 4;                      // PIECE = CT * 8 * U
-    Raw<F32> r[U];
+    constexpr int N = F32 ? 2 : 1;
+    uint4 r[UNITS];
+    load_piece<F32>(g, b0, b1, r, [&](int64_t i) { const double v = element(g, i, F32); acc = fma(v, v, acc); });
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int64_t at = b0 + (u * CT + threadIdx.x) * 8;
-        if (at + 8 <= b1) r[u] = load_raw<F32>(g, at);
-        else {
-            r[u] = zero_raw<F32>();
-            for (int64_t i = at; i < b1; ++i) { const double v = element(g, i, F32); acc = fma(v, v, acc); }
-        }
+    for (int u = 0; u < UNITS; u += N) {
+        uint4 e[N];
+#pragma unroll
+        for (int n = 0; n < N; ++n) e[n] = r[u + n];
+        add_squares<F32, N>(e, acc);
     }
-#pragma unroll
-    for (int u = 0; u < U; ++u) if (b0 + (u * CT + threadIdx.x) * 8 + 8 <= b1) add_squares<F32>(r[u], acc);
 }
-static_assert(PIECE == CT * 8 * 4, "");
 
 // Sum over the CTA, in every thread; fixed order.
 __device__ __forceinline__ double block_sum(double v, double *red)
@@ -114,14 +158,14 @@ __device__ __forceinline__ double block_sum(double v, double *red)
 }
 
 template <int N>
-__global__ void __launch_bounds__(CT)
+__global__ void __launch_bounds__(CT, CTAS)
 grad_norm_parts_kernel(const __grid_constant__ Table<N> T, double *__restrict__ part)
 {
     __shared__ double red[CT / 32];
     pdl_launch_dependents();
     pdl_wait();
     double acc = 0.0;
-    for_pieces(T, blockIdx.x, [&](const Entry &e, int64_t b0, int64_t b1, int64_t h) {
+    for_pieces<false>(T, [&](const Entry &e, int64_t b0, int64_t b1, int64_t h) {
         if (threadIdx.x < h) { const double v = element(e.g, threadIdx.x, e.f32); acc = fma(v, v, acc); }
         if (e.f32) piece_squares<true>(e.g, b0, b1, acc);
         else piece_squares<false>(e.g, b0, b1, acc);
@@ -153,42 +197,38 @@ grad_norm_finish_kernel(const double *part, int parts, float max_norm, float *no
     }
 }
 
+template <bool F32> __device__ __forceinline__ void scale_element(const Entry &e, int64_t i, float f)
+{
+    if (F32) ((float *)e.out)[i] = ((const float *)e.g)[i] * f;
+    else ((bf16 *)e.out)[i] = f2bf(bf2f(((const bf16 *)e.g)[i]) * f);
+}
+
 template <bool F32> __device__ __forceinline__ void piece_scale(const Entry &e, int64_t b0, int64_t b1, float f)
 {
-    constexpr int U = 4;
     if (((uintptr_t)e.out ^ (uintptr_t)e.g) & 15) {                   // the two cannot both be on 16-byte boundaries: an element per lane
-        for (int64_t i = b0 + threadIdx.x; i < b1; i += CT) {
-            if (F32) ((float *)e.out)[i] = ((const float *)e.g)[i] * f;
-            else ((bf16 *)e.out)[i] = f2bf(bf2f(((const bf16 *)e.g)[i]) * f);
-        }
+        for (int64_t i = b0 + threadIdx.x; i < b1; i += CT) scale_element<F32>(e, i, f);
         return;
     }
-    Raw<F32> r[U];
+    constexpr int E = F32 ? 4 : 8, PAIRS = F32 ? 2 : 4;
+    uint4 r[UNITS];
+    load_piece<F32>(e.g, b0, b1, r, [&](int64_t i) { scale_element<F32>(e, i, f); });
+    uint4 *o = (uint4 *)((char *)e.out + b0 * (F32 ? 4 : 2)) + threadIdx.x;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int64_t at = b0 + (u * CT + threadIdx.x) * 8;
-        if (at + 8 <= b1) r[u] = load_raw<F32>(e.g, at);
-    }
+    for (int u = 0; u < UNITS; ++u) {
+        ptx::f32x2 v[PAIRS];
+        float x[8];
+        unit_pairs<F32>(r[u], v);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int64_t at = b0 + (u * CT + threadIdx.x) * 8;
-        if (at + 8 <= b1) {
-            float v[8];
-            to_float<F32>(r[u], v);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] *= f;
-            store8<F32>(e.out, at, v);
-        } else {
-            for (int64_t i = at; i < b1; ++i) {
-                if (F32) ((float *)e.out)[i] = ((const float *)e.g)[i] * f;
-                else ((bf16 *)e.out)[i] = f2bf(bf2f(((const bf16 *)e.g)[i]) * f);
-            }
-        }
+        for (int i = 0; i < PAIRS; ++i) ptx::unpack2(ptx::mul2(v[i], ptx::twice(f)), x[2 * i], x[2 * i + 1]);
+        uint4 w;
+        if constexpr (F32) w = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+        else w = pack8(x);
+        if (b1 - b0 == piece_of(F32) || b0 + (int64_t)(u * CT + threadIdx.x + 1) * E <= b1) __stcs(o + u * CT, w);
     }
 }
 
 template <int N>
-__global__ void __launch_bounds__(CT)
+__global__ void __launch_bounds__(CT, CTAS)
 grad_scale_kernel(const __grid_constant__ Table<N> T, const double *part, int parts, float max_norm, float *norm, float *factor)
 {
     __shared__ double red[CT / 32];
@@ -200,11 +240,11 @@ grad_scale_kernel(const __grid_constant__ Table<N> T, const double *part, int pa
         *norm = v;
         *factor = f;
     }
-    for_pieces(T, gridDim.x - 1 - blockIdx.x, [&](const Entry &e, int64_t b0, int64_t b1, int64_t h) {
+    for_pieces<true>(T, [&](const Entry &e, int64_t b0, int64_t b1, int64_t h) {
         if (f == 1.f && e.out == e.g) return;
         if (threadIdx.x < h) {
-            if (e.f32) ((float *)e.out)[threadIdx.x] = ((const float *)e.g)[threadIdx.x] * f;
-            else ((bf16 *)e.out)[threadIdx.x] = f2bf(bf2f(((const bf16 *)e.g)[threadIdx.x]) * f);
+            if (e.f32) scale_element<true>(e, threadIdx.x, f);
+            else scale_element<false>(e, threadIdx.x, f);
         }
         if (e.f32) piece_scale<true>(e, b0, b1, f);
         else piece_scale<false>(e, b0, b1, f);
@@ -213,7 +253,7 @@ grad_scale_kernel(const __grid_constant__ Table<N> T, const double *part, int pa
 
 // ----------------------------------------------------------------------------------------------------------- host
 constexpr int SHORT = 4096;                   // pieces up to which the next launch is scheduled early
-int max_ctas() { return sm_count() * 8; }
+int max_ctas() { return sm_count() * CTAS; }
 
 lamp_status_t check_grads(const lamp_grad_t *grads, int32_t count, bool outs)
 {

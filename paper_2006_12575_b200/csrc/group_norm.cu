@@ -97,11 +97,10 @@ struct Place {
     int part, ch, unit, ty;                   // this thread's first channel, its unit in the chunk, its voxel line
     bool active;
 };
-// `back`: samples and parts in the opposite order
-__device__ __forceinline__ Place place(const GnParams &P, bool back)
+__device__ __forceinline__ Place place(const GnParams &P)
 {
     Place q;
-    const int64_t at = back ? (int64_t)P.n * P.parts - 1 - blockIdx.x : blockIdx.x;
+    const int64_t at = blockIdx.x;
     q.sample = at / P.parts;
     q.part = (int)(at - q.sample * P.parts);
     q.ty = threadIdx.x / P.uc;
@@ -112,6 +111,13 @@ __device__ __forceinline__ Place place(const GnParams &P, bool back)
     q.v0 = q.part * P.run;
     q.v1 = min(P.v, q.v0 + P.run);
     return q;
+}
+
+// first voxel of this thread's last batch of U (below v0 where it has none)
+template <int U> __device__ __forceinline__ int64_t last_batch(const GnParams &P, const Place &q)
+{
+    const int64_t first = q.v0 + q.ty;
+    return first < q.v1 ? first + (q.v1 - first - 1) / (U * P.ty) * (U * P.ty) : q.v0 - 1;
 }
 
 // Sum over the CTA's voxel lines of 8 pairs of fp64 per thread; on return tot[2 * channel + {0, 1}] (channels of the chunk) is in shared memory.
@@ -142,7 +148,7 @@ gn_sums_kernel(const GnParams P)
     extern __shared__ __align__(16) double sm[];
     pdl_launch_dependents();
     pdl_wait();
-    const Place q = place(P, false);
+    const Place q = place(P);
     const int64_t base = q.sample * P.v;
     f32x2 k[4], s1[4], s2[4];
 #pragma unroll
@@ -293,11 +299,11 @@ gn_apply_kernel(const GnParams P)
 {
     pdl_launch_dependents();
     pdl_wait();
-    const Place q = place(P, true);
+    const Place q = place(P);
     if (!q.active) return;
     const int64_t base = q.sample * P.v;
     const Affine f = affine(P, q);
-    for (int64_t v = q.v0 + q.ty; v < q.v1; v += (int64_t)U * P.ty) {
+    for (int64_t v = last_batch<U>(P, q); v >= q.v0; v -= (int64_t)U * P.ty) {
         Raw<XF> r[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -318,7 +324,7 @@ gn_apply_kernel(const GnParams P)
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) z[j] = activate<ACT, ZF>(z[j], P.slope);
-            store8<ZF>(P.out, (base + at) * P.po + q.ch, z);
+            store8_last<ZF>(P.out, (base + at) * P.po + q.ch, z);
         }
     }
 }
@@ -349,7 +355,7 @@ gn_bwd_sums_kernel(const GnParams P)
     extern __shared__ __align__(16) double sm[];
     pdl_launch_dependents();
     pdl_wait();
-    const Place q = place(P, false);
+    const Place q = place(P);
     const int64_t base = q.sample * P.v;
     double a[8], b[8];
 #pragma unroll
@@ -435,7 +441,7 @@ gn_bwd_apply_kernel(const GnParams P)
     extern __shared__ __align__(16) float2 means[];             // of this chunk's groups: (mean(w dt), mean(w dt xhat))
     pdl_launch_dependents();
     pdl_wait();
-    const Place q = place(P, true);
+    const Place q = place(P);
     const int64_t base = q.sample * P.v;
     const int cc = P.uc * 8, c0 = blockIdx.y * cc, c1 = min(P.c, c0 + cc), g0 = c0 / P.cg, g1 = (c1 - 1) / P.cg;
     {
@@ -494,7 +500,7 @@ gn_bwd_apply_kernel(const GnParams P)
         e[j] = pack2(__float_as_uint(ev[0]), __float_as_uint(ev[1]));
         h[j] = pack2(__float_as_uint(hv[0]), __float_as_uint(hv[1]));
     }
-    for (int64_t v = q.v0 + q.ty; v < q.v1; v += (int64_t)U * P.ty) {
+    for (int64_t v = last_batch<U>(P, q); v >= q.v0; v -= (int64_t)U * P.ty) {
         Raw<XF> rx[U];
         Raw<ZF> rz[U];
 #pragma unroll
@@ -513,7 +519,10 @@ gn_bwd_apply_kernel(const GnParams P)
             slopes<XF, ZF, ACT>(P, f, rx[u], rz[u], d, dt);
 #pragma unroll
             for (int j = 0; j < 4; ++j) d[j] = fma2(dt[j], f.a[j], fma2(d[j], e[j], h[j]));
-            store_pairs<XF>(P.out, (base + at) * P.po + q.ch, d);
+            float o[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) unpack2(d[j], o[2 * j], o[2 * j + 1]);
+            store8_last<XF>(P.out, (base + at) * P.po + q.ch, o);
         }
     }
 }
