@@ -2,8 +2,8 @@
 //
 // Bound by memory: the norm reads every gradient once, the scaling reads and writes it.  The tensors' table travels in the
 // kernel's parameters (a captured graph keeps it), so no copy to the device precedes a call.  The elements are cut into pieces of
-// 32 KB, laid from a 16-byte boundary of their tensor; a CTA takes a contiguous run of pieces, the scaling the same run backwards, so that
-// it starts with what the norm left in L2.
+// 32 KB, laid from a 128-byte boundary of their tensor; the CTAs take them in turn, the scaling backwards, so that it
+// starts with what the norm left in L2.
 // Sums: 8 squares in fp32 where that stays well inside its range, otherwise the 8 again in fp64; fp64 beyond, per thread, then over the
 // CTA in a fixed order, one partial sum per CTA.  Every CTA of the scaling adds all of them in the same order: no counter, no atomic, nothing
 // that has to be zero beforehand.
@@ -33,10 +33,10 @@ template <int N> struct Table {
 constexpr int SMALL = 120, LARGE = 1000;      // parameters of 4 KB and of just under 32 KB
 static_assert(sizeof(Table<LARGE>) + 64 <= 32764, "kernel parameters");
 
-// elements in front of the first 16-byte boundary
+// elements in front of the first 128-byte boundary: a warp's 512 bytes are then whole lines
 __host__ __device__ __forceinline__ int64_t head_of(const void *p, int64_t n, bool f32)
 {
-    const int64_t h = (int64_t)((16 - ((uintptr_t)p & 15)) & 15) / (f32 ? 4 : 2);
+    const int64_t h = (int64_t)((128 - ((uintptr_t)p & 127)) & 127) / (f32 ? 4 : 2);
     return h < n ? h : n;
 }
 __host__ __forceinline__ int64_t pieces_of(const lamp_grad_t &t)
@@ -47,26 +47,24 @@ __host__ __forceinline__ int64_t pieces_of(const lamp_grad_t &t)
     return body == 0 ? 1 : (body + piece - 1) / piece;
 }
 
-// The run of pieces of this CTA, tensor by tensor, forwards or BACK: f(entry, first element of the body of the piece, its end, elements of the head).
+// The pieces blockIdx.x, blockIdx.x + gridDim.x, .. of the tensors, forwards or BACK: f(entry, first element of the body of the piece, its end,
+// elements of the head).
 template <bool BACK, int N, typename F>
 __device__ __forceinline__ void for_pieces(const Table<N> &T, F f)
 {
-    const int p0 = (int)((int64_t)T.pieces * blockIdx.x / gridDim.x), p1 = (int)((int64_t)T.pieces * (blockIdx.x + 1) / gridDim.x);
-    if (p0 >= p1) return;
-    const int start = BACK ? p1 - 1 : p0;
-    int lo = 0, hi = T.count - 1;             // the entry of piece `start`: the last that begins at it or before it
+    const int step = gridDim.x, turns = (T.pieces - (int)blockIdx.x + step - 1) / step;             // at least one: no more CTAs than pieces
+    int p = blockIdx.x + (BACK ? turns - 1 : 0) * step;
+    int lo = 0, hi = T.count - 1;             // the entry of piece p: the last that begins at it or before it
     while (lo < hi) {
         const int mid = (lo + hi + 1) / 2;
-        if (T.e[mid].first <= start) lo = mid; else hi = mid - 1;
+        if (T.e[mid].first <= p) lo = mid; else hi = mid - 1;
     }
-    for (int i = lo, p = start; BACK ? p >= p0 : p < p1; i += BACK ? -1 : 1) {
-        const Entry &e = T.e[i];
-        const int end = i + 1 < T.count ? T.e[i + 1].first : T.pieces;
-        const int64_t h = head_of(e.g, e.n, e.f32);
-        for (; BACK ? p >= p0 && p >= e.first : p < p1 && p < end; p += BACK ? -1 : 1) {
-            const int64_t b0 = h + (int64_t)(p - e.first) * piece_of(e.f32), b1 = b0 + piece_of(e.f32);
-            f(e, b0, b1 < e.n ? b1 : e.n, p == e.first ? h : 0);
-        }
+    for (int t = 0; t < turns; ++t, p += BACK ? -step : step) {
+        if (BACK) while (T.e[lo].first > p) --lo;
+        else while (lo + 1 < T.count && T.e[lo + 1].first <= p) ++lo;
+        const Entry &e = T.e[lo];
+        const int64_t h = head_of(e.g, e.n, e.f32), b0 = h + (int64_t)(p - e.first) * piece_of(e.f32), b1 = b0 + piece_of(e.f32);
+        f(e, b0, b1 < e.n ? b1 : e.n, p == e.first ? h : 0);
     }
 }
 
