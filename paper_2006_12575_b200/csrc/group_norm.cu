@@ -43,52 +43,71 @@ struct GnParams {
 
 
 // ----------------------------------------------------------------------------------------------------------- activations
-// FINE: fp32 outputs of the forward pass.  Elsewhere e^x without the correction for the rounding of x log2(e) (2^-24 |x| of e^x), and the normal
-// distribution by Abramowitz & Stegun 7.1.26: q(u) = (a1 s + .. + a5 s^5) e^(-u^2), s = 1 / (1 + p u), for erfc(u), u >= 0, off by at most 1.5e-7.
-// A derivative is a factor of size one, so both are within a few units of 2^-24 of it: expf and erfcf in the backward pass of fp32 took 201 us on
-// 81,840 x 320 against BWDNOW.
-template <bool FINE> __device__ __forceinline__ void normal_tail(float t, float &below, float &density)
+// Two values at a time: the packed fp32 instructions halve what is issued, which with a SiLU or GELU bounds these kernels as much as memory does.
+// FINE: fp32 outputs of the forward pass, with expf and erfcf.  Elsewhere e^x without the correction for the rounding of x log2(e) (2^-24 |x| of e^x),
+// and the normal distribution by Abramowitz & Stegun 7.1.26: q(u) = (a1 s + .. + a5 s^5) e^(-u^2), s = 1 / (1 + p u), for erfc(u), u >= 0, off by at
+// most 1.5e-7.  A derivative is a factor of size one, so both are within a few units of 2^-24 of it.
+__device__ __forceinline__ float ex2(float x)
 {
-    // below = P(X <= t), density = e^(-t^2 / 2)
-    if constexpr (FINE) {
-        below = 0.5f * erfcf(t * -0.70710678118654752f);
-        density = expf(-0.5f * t * t);
-    } else {
-        density = gate_exp<false>(-0.5f * t * t);
-        const float s = reciprocal(fmaf(fabsf(t), 0.3275911f * 0.70710678118654752f, 1.f));
-        float q = fmaf(s, 1.061405429f, -1.453152027f);
-        q = fmaf(s, q, 1.421413741f);
-        q = fmaf(s, q, -0.284496736f);
-        q = fmaf(s, q, 0.254829592f);
-        q = 0.5f * s * q * density;
-        below = t > 0.f ? 1.f - q : q;
-    }
+    float e;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x));
+    return e;
 }
-template <int ACT, bool FINE> __device__ __forceinline__ float activate(float t, float slope)
+__device__ __forceinline__ f32x2 pair(float a, float b) { return pack2(__float_as_uint(a), __float_as_uint(b)); }
+__device__ __forceinline__ f32x2 ex2_2(f32x2 v) { float a, b; unpack2(v, a, b); return pair(ex2(a), ex2(b)); }
+__device__ __forceinline__ f32x2 rcp_2(f32x2 v) { float a, b; unpack2(v, a, b); return pair(reciprocal(a), reciprocal(b)); }
+__device__ __forceinline__ f32x2 sigmoid_2(f32x2 t) { return rcp_2(add2(ex2_2(mul2(t, twice(-1.4426950408889634f))), twice(1.f))); }
+
+// below = P(X <= t) of the normal distribution, density = e^(-t^2 / 2)
+__device__ __forceinline__ void normal_2(f32x2 t, f32x2 &below, f32x2 &density)
 {
-    if constexpr (ACT == LAMP_ACT_LEAKY_RELU) return t > 0.f ? t : slope * t;
-    if constexpr (ACT == LAMP_ACT_SILU) return t * sigmoid<FINE>(t);
-    if constexpr (ACT == LAMP_ACT_GELU) {
-        float below, density;
-        normal_tail<FINE>(t, below, density);
-        return t * below;
-    }
-    return t;
+    density = ex2_2(mul2(t, mul2(t, twice(-0.72134752044448170f))));
+    float a, b;
+    unpack2(t, a, b);
+    const f32x2 s = rcp_2(fma2(pair(fabsf(a), fabsf(b)), twice(0.3275911f * 0.70710678118654752f), twice(1.f)));
+    f32x2 q = fma2(s, twice(0.5f * 1.061405429f), twice(0.5f * -1.453152027f));
+    q = fma2(s, q, twice(0.5f * 1.421413741f));
+    q = fma2(s, q, twice(0.5f * -0.284496736f));
+    q = fma2(s, q, twice(0.5f * 0.254829592f));
+    q = mul2(mul2(q, s), density);
+    float q0, q1, u0, u1;
+    unpack2(q, q0, q1);
+    unpack2(fma2(q, twice(-1.f), twice(1.f)), u0, u1);
+    below = pair(a > 0.f ? u0 : q0, b > 0.f ? u1 : q1);
 }
-template <int ACT> __device__ __forceinline__ float derivative(float t, float slope)
+template <int ACT, bool FINE> __device__ __forceinline__ f32x2 activate(f32x2 t, float slope)
 {
-    if constexpr (ACT == LAMP_ACT_LEAKY_RELU) return t > 0.f ? 1.f : t <= 0.f ? slope : t;           // NaN stays
+    if constexpr (ACT == LAMP_ACT_NONE) return t;
+    float a, b;
+    unpack2(t, a, b);
+    if constexpr (ACT == LAMP_ACT_LEAKY_RELU) return pair(a > 0.f ? a : slope * a, b > 0.f ? b : slope * b);
     if constexpr (ACT == LAMP_ACT_SILU) {
-        float g, s;
-        sigmoid_slope<false>(t, g, s);
-        return fmaf(t, s, g);
+        if (FINE) return pair(a * sigmoid<true>(a), b * sigmoid<true>(b));
+        return mul2(t, sigmoid_2(t));
     }
-    if constexpr (ACT == LAMP_ACT_GELU) {
-        float below, density;
-        normal_tail<false>(t, below, density);
-        return fmaf(t * 0.3989422804014327f, density, below);
+    if (FINE) return pair(a * (0.5f * erfcf(a * -0.70710678118654752f)), b * (0.5f * erfcf(b * -0.70710678118654752f)));
+    f32x2 below, density;
+    normal_2(t, below, density);
+    return mul2(t, below);
+}
+// v * act'(t)
+template <int ACT> __device__ __forceinline__ f32x2 times_derivative(f32x2 v, f32x2 t, float slope)
+{
+    if constexpr (ACT == LAMP_ACT_NONE) return v;
+    if constexpr (ACT == LAMP_ACT_LEAKY_RELU) {
+        float a, b, x, y;
+        unpack2(t, a, b);
+        unpack2(v, x, y);
+        return pair(a > 0.f ? x : a <= 0.f ? slope * x : a, b > 0.f ? y : b <= 0.f ? slope * y : b);       // NaN stays
     }
-    return 1.f;
+    if constexpr (ACT == LAMP_ACT_SILU) {
+        // s (1 + t (1 - s)) = s + y - y s with y = t s
+        const f32x2 s = sigmoid_2(t), y = mul2(t, s);
+        return mul2(v, add2(fma2(mul2(y, twice(-1.f)), s, y), s));
+    }
+    f32x2 below, density;
+    normal_2(t, below, density);
+    return mul2(v, fma2(mul2(t, twice(0.3989422804014327f)), density, below));
 }
 
 // ----------------------------------------------------------------------------------------------------------- places
@@ -318,12 +337,7 @@ gn_apply_kernel(const GnParams P)
             to_pairs<XF>(r[u], t);
             float z[8];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                t[j] = fma2(add2(t[j], f.nm[j]), f.a[j], f.b[j]);
-                unpack2(t[j], z[2 * j], z[2 * j + 1]);
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) z[j] = activate<ACT, ZF>(z[j], P.slope);
+            for (int j = 0; j < 4; ++j) unpack2(activate<ACT, ZF>(fma2(add2(t[j], f.nm[j]), f.a[j], f.b[j]), P.slope), z[2 * j], z[2 * j + 1]);
             store8_last<ZF>(P.out, (base + at) * P.po + q.ch, z);
         }
     }
@@ -339,11 +353,7 @@ __device__ __forceinline__ void slopes(const GnParams &P, const Affine &f, const
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         d[j] = add2(d[j], f.nm[j]);
-        if constexpr (ACT != LAMP_ACT_NONE) {
-            float t0, t1;
-            unpack2(fma2(d[j], f.a[j], f.b[j]), t0, t1);
-            dt[j] = mul2(dt[j], pack2(__float_as_uint(derivative<ACT>(t0, P.slope)), __float_as_uint(derivative<ACT>(t1, P.slope))));
-        }
+        dt[j] = times_derivative<ACT>(dt[j], fma2(d[j], f.a[j], f.b[j]), P.slope);
     }
 }
 
