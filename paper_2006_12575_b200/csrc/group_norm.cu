@@ -8,107 +8,17 @@
 // Sums: a thread adds d = x - k and d^2 of at most RUN voxels in fp32, k the mean of the first values it loads - without it the squares of
 // data far from 0 lose the variance.  Between threads, CTAs and channels of a group the sums are fp64, taken about r, the group's first
 // value, and added in a fixed order.
-#include "block_norm.cuh"
+#include "group_norm.cuh"
 
 namespace lamp {
 
 namespace {
 
-using namespace bn;
-using ptx::f32x2; using ptx::fma2; using ptx::add2; using ptx::mul2; using ptx::twice; using ptx::pack2; using ptx::unpack2;
+using namespace gn;
 
-constexpr int GT = 256;                       // threads
 // CTAs per SM that the streaming kernels are compiled and sized for
 constexpr int resident(bool xf, bool back) { return (xf ? 3 : 4) - (back ? 1 : 0); }
 constexpr int RUN = 256;                      // voxels that a thread sums at most
-
-struct GnParams {
-    const void *x, *dz;
-    void *out;                                // z, or dx
-    int64_t px, pdz, po;
-    int64_t v;                                // voxels of one sample
-    int32_t n, c, groups, cg;                 // cg = channels per group
-    int32_t parts;                            // CTAs per sample (and chunk of channels)
-    int64_t run;                              // voxels per CTA
-    int32_t chunks, uc, ty;                   // chunks of channels, units of a chunk, voxels side by side
-    int32_t act;
-    float slope, eps;
-    const float *w, *b;
-    const double *stats;
-    double2 *part;                            // forward [n][groups][parts][chunks], backward [n][parts][c]
-    double2 *chan;                            // backward [n][c]
-    float2 *mean_rstd;
-    float *dw, *db;
-};
-
-
-// ----------------------------------------------------------------------------------------------------------- activations
-// Two values at a time: the packed fp32 instructions halve what is issued, which with a SiLU or GELU bounds these kernels as much as memory does.
-// FINE: fp32 outputs of the forward pass, with expf and erfcf.  Elsewhere e^x without the correction for the rounding of x log2(e) (2^-24 |x| of e^x),
-// and the normal distribution by Abramowitz & Stegun 7.1.26: q(u) = (a1 s + .. + a5 s^5) e^(-u^2), s = 1 / (1 + p u), for erfc(u), u >= 0, off by at
-// most 1.5e-7.  A derivative is a factor of size one, so both are within a few units of 2^-24 of it.
-__device__ __forceinline__ float ex2(float x)
-{
-    float e;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x));
-    return e;
-}
-__device__ __forceinline__ f32x2 pair(float a, float b) { return pack2(__float_as_uint(a), __float_as_uint(b)); }
-__device__ __forceinline__ f32x2 ex2_2(f32x2 v) { float a, b; unpack2(v, a, b); return pair(ex2(a), ex2(b)); }
-__device__ __forceinline__ f32x2 rcp_2(f32x2 v) { float a, b; unpack2(v, a, b); return pair(reciprocal(a), reciprocal(b)); }
-__device__ __forceinline__ f32x2 sigmoid_2(f32x2 t) { return rcp_2(add2(ex2_2(mul2(t, twice(-1.4426950408889634f))), twice(1.f))); }
-
-// below = P(X <= t) of the normal distribution, density = e^(-t^2 / 2)
-__device__ __forceinline__ void normal_2(f32x2 t, f32x2 &below, f32x2 &density)
-{
-    density = ex2_2(mul2(t, mul2(t, twice(-0.72134752044448170f))));
-    float a, b;
-    unpack2(t, a, b);
-    const f32x2 s = rcp_2(fma2(pair(fabsf(a), fabsf(b)), twice(0.3275911f * 0.70710678118654752f), twice(1.f)));
-    f32x2 q = fma2(s, twice(0.5f * 1.061405429f), twice(0.5f * -1.453152027f));
-    q = fma2(s, q, twice(0.5f * 1.421413741f));
-    q = fma2(s, q, twice(0.5f * -0.284496736f));
-    q = fma2(s, q, twice(0.5f * 0.254829592f));
-    q = mul2(mul2(q, s), density);
-    float q0, q1, u0, u1;
-    unpack2(q, q0, q1);
-    unpack2(fma2(q, twice(-1.f), twice(1.f)), u0, u1);
-    below = pair(a > 0.f ? u0 : q0, b > 0.f ? u1 : q1);
-}
-template <int ACT, bool FINE> __device__ __forceinline__ f32x2 activate(f32x2 t, float slope)
-{
-    if constexpr (ACT == LAMP_ACT_NONE) return t;
-    float a, b;
-    unpack2(t, a, b);
-    if constexpr (ACT == LAMP_ACT_LEAKY_RELU) return pair(a > 0.f ? a : slope * a, b > 0.f ? b : slope * b);
-    if constexpr (ACT == LAMP_ACT_SILU) {
-        if (FINE) return pair(a * sigmoid<true>(a), b * sigmoid<true>(b));
-        return mul2(t, sigmoid_2(t));
-    }
-    if (FINE) return pair(a * (0.5f * erfcf(a * -0.70710678118654752f)), b * (0.5f * erfcf(b * -0.70710678118654752f)));
-    f32x2 below, density;
-    normal_2(t, below, density);
-    return mul2(t, below);
-}
-// v * act'(t)
-template <int ACT> __device__ __forceinline__ f32x2 times_derivative(f32x2 v, f32x2 t, float slope)
-{
-    if constexpr (ACT == LAMP_ACT_NONE) return v;
-    if constexpr (ACT == LAMP_ACT_LEAKY_RELU) {
-        float a, b, x, y;
-        unpack2(t, a, b);
-        unpack2(v, x, y);
-        return pair(a > 0.f ? x : a <= 0.f ? slope * x : a, b > 0.f ? y : b <= 0.f ? slope * y : b);       // NaN stays
-    }
-    if constexpr (ACT == LAMP_ACT_SILU) {
-        // s (1 + t (1 - s)) = s + y - y s with y = t s
-        const f32x2 s = sigmoid_2(t), y = mul2(t, s);
-        return mul2(v, add2(fma2(mul2(y, twice(-1.f)), s, y), s));
-    }
-    f32x2 below, density;
-    normal_2(t, below, density);
-    return mul2(v, fma2(mul2(t, twice(0.3989422804014327f)), density, below));
-}
 
 // ----------------------------------------------------------------------------------------------------------- places
 struct Place {
@@ -137,26 +47,6 @@ template <int U> __device__ __forceinline__ int64_t last_batch(const GnParams &P
 {
     const int64_t first = q.v0 + q.ty;
     return first < q.v1 ? first + (q.v1 - first - 1) / (U * P.ty) * (U * P.ty) : q.v0 - 1;
-}
-
-// Sum over the CTA's voxel lines of 8 pairs of fp64 per thread; on return tot[2 * channel + {0, 1}] (channels of the chunk) is in shared memory.
-__device__ __forceinline__ void sum_lines(const GnParams &P, const Place &q, const double (&a)[8], const double (&b)[8], double *sm)
-{
-    // [line][channel of the chunk], first all a, then all b; the totals replace line 0
-    const int cc = P.uc * 8;
-    double *sa = sm, *sb = sm + P.ty * cc;
-    if (q.ty < P.ty) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) { sa[q.ty * cc + q.unit * 8 + j] = a[j]; sb[q.ty * cc + q.unit * 8 + j] = b[j]; }
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < 2 * cc; i += GT) {
-        double *s = i < cc ? sa + i : sb + (i - cc);
-        double t = s[0];
-        for (int l = 1; l < P.ty; ++l) t += s[l * cc];
-        s[0] = t;
-    }
-    __syncthreads();
 }
 
 // ----------------------------------------------------------------------------------------------------------- forward
@@ -219,32 +109,17 @@ gn_sums_kernel(const GnParams P)
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const int64_t first = base * P.px + (q.ch + j) / P.cg * P.cg;
-            const double r = XF ? ((const float *)P.x)[first] : bf2f(((const bf16 *)P.x)[first]);
-            const double e = -(double)nk[j] - r, m = (double)mine;
-            a[j] = (double)f1[j] + m * e;
-            b[j] = (double)f2[j] + e * (2.0 * f1[j] + m * e);
+            const double r = value_at<XF>(P.x, base * P.px + (q.ch + j) / P.cg * P.cg);
+            about(nk[j], f1[j], f2[j], (int)mine, r, a[j], b[j]);
         }
     }
-    sum_lines(P, q, a, b, sm);
-    // channels of a group
+    const Totals tot = sum_lines(P.ty, P.uc, q.ty, q.unit, a, b, sm);
     const int cc = P.uc * 8, c0 = blockIdx.y * cc, c1 = min(P.c, c0 + cc);
-    const int g0 = c0 / P.cg, g1 = (c1 - 1) / P.cg;
-    int lanes = 1;
-    while (lanes < 32 && lanes * 2 <= P.cg) lanes *= 2;
-    const int l = threadIdx.x % lanes, per = GT / lanes;
-    for (int g = g0; g <= g1; g += per) {                        // the same number of turns for every thread
-        const int mg = g + threadIdx.x / lanes;
-        double s = 0.0, t = 0.0;
-        if (mg <= g1) {
-            for (int ch = max(c0, mg * P.cg) + l; ch < min(c1, (mg + 1) * P.cg); ch += lanes) { s += sm[ch - c0]; t += sm[P.ty * cc + ch - c0]; }
-        }
-        for (int o = lanes / 2; o > 0; o >>= 1) {
-            s += __shfl_xor_sync(0xffffffffu, s, o);
-            t += __shfl_xor_sync(0xffffffffu, t, o);
-        }
-        if (mg <= g1 && l == 0) P.part[((q.sample * P.groups + mg) * P.parts + q.part) * P.chunks + blockIdx.y] = make_double2(s, t);
-    }
+    sum_groups(c0 / P.cg, (c1 - 1) / P.cg, P.cg,
+               [&](int g, int l, int lanes, double &s, double &t) {
+                   for (int ch = max(c0, g * P.cg) + l; ch < min(c1, (g + 1) * P.cg); ch += lanes) { s += tot.a[ch - c0]; t += tot.b[ch - c0]; }
+               },
+               [&](int g, double s, double t) { P.part[((q.sample * P.groups + g) * P.parts + q.part) * P.chunks + blockIdx.y] = make_double2(s, t); });
 }
 
 // mean and rstd of a group from its partial sums, or from sums per channel; W warps per group: one where the sums are few (a CTA has 8 groups),
@@ -270,7 +145,7 @@ gn_finish_kernel(const GnParams P)
         const int cc = P.uc * 8, k0 = g * P.cg / cc, k1 = ((g + 1) * P.cg - 1) / cc, ks = k1 - k0 + 1;
         const double2 *p = P.part + at * P.parts * P.chunks;
         const int64_t x0 = sample * P.v * P.px + g * P.cg;
-        r = XF ? ((const float *)P.x)[x0] : bf2f(((const bf16 *)P.x)[x0]);
+        r = value_at<XF>(P.x, x0);
 #pragma unroll 4
         for (int i = first; i < P.parts * ks; i += 32 * W) { const double2 v = p[i / ks * P.chunks + k0 + i % ks]; s += v.x; t += v.y; }
     }
@@ -284,32 +159,13 @@ gn_finish_kernel(const GnParams P)
         s = t = 0.0;
         for (int i = 0; i < W; ++i) { s += red[0][i]; t += red[1][i]; }
     }
-    if (first == 0) {
-        const double m = (double)P.v * P.cg, mu = s / m, var = t / m - mu * mu;
-        P.mean_rstd[at] = make_float2((float)(r + mu), (float)(1.0 / sqrt((var < 0.0 ? 0.0 : var) + (double)P.eps)));
-    }
+    if (first == 0) P.mean_rstd[at] = mean_rstd_of(s, t, r, (double)P.v * P.cg, P.eps);
 }
 
-// -mean, rstd * w and b of this thread's channels
-struct Affine { f32x2 nm[4], a[4], b[4]; };
-__device__ __forceinline__ Affine affine(const GnParams &P, const Place &q)
+// (mean, rstd) of a group of the sample
+__device__ __forceinline__ auto stats_of(const GnParams &P, const Place &q)
 {
-    float nm[8], a[8], b[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const float2 mr = P.mean_rstd[q.sample * P.groups + (q.ch + j) / P.cg];
-        nm[j] = -mr.x;
-        a[j] = mr.y * (P.w ? P.w[q.ch + j] : 1.f);
-        b[j] = P.b ? P.b[q.ch + j] : 0.f;
-    }
-    Affine f;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        f.nm[j] = pack2(__float_as_uint(nm[2 * j]), __float_as_uint(nm[2 * j + 1]));
-        f.a[j] = pack2(__float_as_uint(a[2 * j]), __float_as_uint(a[2 * j + 1]));
-        f.b[j] = pack2(__float_as_uint(b[2 * j]), __float_as_uint(b[2 * j + 1]));
-    }
-    return f;
+    return [mr = P.mean_rstd + q.sample * P.groups](int g) { return mr[g]; };
 }
 
 template <bool XF, bool ZF, int ACT, int U>
@@ -321,7 +177,7 @@ gn_apply_kernel(const GnParams P)
     const Place q = place(P);
     if (!q.active) return;
     const int64_t base = q.sample * P.v;
-    const Affine f = affine(P, q);
+    const Affine f = affine(P, q.ch, stats_of(P, q));
     for (int64_t v = last_batch<U>(P, q); v >= q.v0; v -= (int64_t)U * P.ty) {
         Raw<XF> r[U];
 #pragma unroll
@@ -333,30 +189,14 @@ gn_apply_kernel(const GnParams P)
         for (int u = 0; u < U; ++u) {
             const int64_t at = v + (int64_t)u * P.ty;
             if (at >= q.v1) continue;
-            f32x2 t[4];
-            to_pairs<XF>(r[u], t);
             float z[8];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) unpack2(activate<ACT, ZF>(fma2(add2(t[j], f.nm[j]), f.a[j], f.b[j]), P.slope), z[2 * j], z[2 * j + 1]);
+            apply<XF, ZF, ACT>(P, f, r[u], z);
             store8_last<ZF>(P.out, (base + at) * P.po + q.ch, z);
         }
     }
 }
 
 // ----------------------------------------------------------------------------------------------------------- backward
-// dt and (x - mean) of 8 channels
-template <bool XF, bool ZF, int ACT>
-__device__ __forceinline__ void slopes(const GnParams &P, const Affine &f, const Raw<XF> &rx, const Raw<ZF> &rz, f32x2 (&d)[4], f32x2 (&dt)[4])
-{
-    to_pairs<XF>(rx, d);
-    to_pairs<ZF>(rz, dt);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        d[j] = add2(d[j], f.nm[j]);
-        dt[j] = times_derivative<ACT>(dt[j], fma2(d[j], f.a[j], f.b[j]), P.slope);
-    }
-}
-
 // sums over the CTA's voxels of dt and dt * xhat per channel
 template <bool XF, bool ZF, int ACT, int U>
 __global__ void __launch_bounds__(GT, resident(XF, true))
@@ -371,7 +211,7 @@ gn_bwd_sums_kernel(const GnParams P)
 #pragma unroll
     for (int j = 0; j < 8; ++j) a[j] = b[j] = 0.0;
     if (q.active) {
-        const Affine f = affine(P, q);
+        const Affine f = affine(P, q.ch, stats_of(P, q));
         f32x2 s1[4], s2[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) s1[j] = s2[j] = 0;
@@ -408,10 +248,10 @@ gn_bwd_sums_kernel(const GnParams P)
             }
         }
     }
-    sum_lines(P, q, a, b, sm);
+    const Totals tot = sum_lines(P.ty, P.uc, q.ty, q.unit, a, b, sm);
     const int cc = P.uc * 8, c0 = blockIdx.y * cc;
     double2 *out = P.part + (q.sample * P.parts + q.part) * P.c + c0;
-    for (int i = threadIdx.x; i < cc && c0 + i < P.c; i += GT) out[i] = make_double2(sm[i], sm[P.ty * cc + i]);
+    for (int i = threadIdx.x; i < cc && c0 + i < P.c; i += GT) out[i] = make_double2(tot.a[i], tot.b[i]);
 }
 
 // chan[n][c] = sum over the parts, 8 channels per CTA
@@ -454,30 +294,17 @@ gn_bwd_apply_kernel(const GnParams P)
     const Place q = place(P);
     const int64_t base = q.sample * P.v;
     const int cc = P.uc * 8, c0 = blockIdx.y * cc, c1 = min(P.c, c0 + cc), g0 = c0 / P.cg, g1 = (c1 - 1) / P.cg;
-    {
-        int lanes = 1;
-        while (lanes < 32 && lanes * 2 <= P.cg) lanes *= 2;
-        const int l = threadIdx.x % lanes, per = GT / lanes;
-        const double inv = 1.0 / ((double)P.v * P.cg);
-        for (int g = g0; g <= g1; g += per) {
-            const int mg = g + threadIdx.x / lanes;
-            double s = 0.0, t = 0.0;
-            if (mg <= g1) {
-                for (int i = l; i < P.cg; i += lanes) {
-                    const int ch = mg * P.cg + i;
-                    const double2 v = P.chan[q.sample * P.c + ch];
-                    const double w = P.w ? P.w[ch] : 1.f;
-                    s += w * v.x;
-                    t += w * v.y;
-                }
-            }
-            for (int o = lanes / 2; o > 0; o >>= 1) {
-                s += __shfl_xor_sync(0xffffffffu, s, o);
-                t += __shfl_xor_sync(0xffffffffu, t, o);
-            }
-            if (mg <= g1 && l == 0) means[mg - g0] = make_float2((float)(s * inv), (float)(t * inv));
-        }
-    }
+    const double inv = 1.0 / ((double)P.v * P.cg);
+    sum_groups(g0, g1, P.cg,
+               [&](int g, int l, int lanes, double &s, double &t) {
+                   for (int ch = g * P.cg + l; ch < (g + 1) * P.cg; ch += lanes) {
+                       const double2 v = P.chan[q.sample * P.c + ch];
+                       const double w = P.w ? P.w[ch] : 1.f;
+                       s += w * v.x;
+                       t += w * v.y;
+                   }
+               },
+               [&](int g, double s, double t) { means[g - g0] = make_float2((float)(s * inv), (float)(t * inv)); });
     __syncthreads();
     if (blockIdx.y == 0 && (P.dw || P.db)) {                    // a warp per channel, the lanes over the samples
         const int lane = threadIdx.x & 31;
@@ -493,23 +320,8 @@ gn_bwd_apply_kernel(const GnParams P)
         }
     }
     if (!q.active) return;
-    const Affine f = affine(P, q);
-    // dx = dt a + (x - mean) e + h,  e = -rstd^2 mean(w dt xhat), h = -rstd mean(w dt)
-    f32x2 e[4], h[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        float ev[2], hv[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int g = (q.ch + 2 * j + i) / P.cg;
-            const float rstd = P.mean_rstd[q.sample * P.groups + g].y;
-            const float2 m = means[g - g0];
-            ev[i] = -rstd * (rstd * m.y);
-            hv[i] = -rstd * m.x;
-        }
-        e[j] = pack2(__float_as_uint(ev[0]), __float_as_uint(ev[1]));
-        h[j] = pack2(__float_as_uint(hv[0]), __float_as_uint(hv[1]));
-    }
+    const Affine f = affine(P, q.ch, stats_of(P, q));
+    const Back k = back_terms(P, q.ch, stats_of(P, q), [&](int g) { return means[g - g0]; });
     for (int64_t v = last_batch<U>(P, q); v >= q.v0; v -= (int64_t)U * P.ty) {
         Raw<XF> rx[U];
         Raw<ZF> rz[U];
@@ -525,13 +337,8 @@ gn_bwd_apply_kernel(const GnParams P)
         for (int u = 0; u < U; ++u) {
             const int64_t at = v + (int64_t)u * P.ty;
             if (at >= q.v1) continue;
-            f32x2 d[4], dt[4];
-            slopes<XF, ZF, ACT>(P, f, rx[u], rz[u], d, dt);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) d[j] = fma2(dt[j], f.a[j], fma2(d[j], e[j], h[j]));
             float o[8];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) unpack2(d[j], o[2 * j], o[2 * j + 1]);
+            back_apply<XF, ZF, ACT>(P, f, k, rx[u], rz[u], o);
             store8_last<XF>(P.out, (base + at) * P.po + q.ch, o);
         }
     }
@@ -647,6 +454,7 @@ lamp_status_t by_act(GnParams &P, bool back, cudaStream_t st)
 
 lamp_status_t by_type(GnParams &P, bool xf, bool zf, bool back, cudaStream_t st)
 {
+    if (!P.stats && gn_small_fits(P, xf, back)) return gn_small(P, xf, zf, back, st);
     if (!xf) return by_act<false, false>(P, back, st);
     return zf ? by_act<true, true>(P, back, st) : by_act<true, false>(P, back, st);
 }

@@ -1,0 +1,242 @@
+// What the two forms of the group norm share (group_norm.cu: tensors that stream through, group_norm_small.cu: samples that a cluster holds).
+// A voxel's channels are taken in units of 8 (16 bytes of bf16, 32 of fp32); a thread keeps its unit for all of its voxels, so everything per
+// channel stays in registers.
+#pragma once
+#include "block_norm.cuh"
+
+namespace lamp {
+namespace gn {
+
+using namespace bn;
+using ptx::f32x2; using ptx::fma2; using ptx::add2; using ptx::mul2; using ptx::twice; using ptx::pack2; using ptx::unpack2;
+
+constexpr int GT = 256;                       // threads
+
+struct GnParams {
+    const void *x, *dz;
+    void *out;                                // z, or dx
+    int64_t px, pdz, po;
+    int64_t v;                                // voxels of one sample
+    int32_t n, c, groups, cg;                 // cg = channels per group
+    int32_t parts;                            // CTAs per sample (and chunk of channels)
+    int64_t run;                              // voxels per CTA
+    int32_t chunks, uc, ty;                   // chunks of channels, units of a chunk, voxels side by side
+    int32_t act;
+    float slope, eps;
+    const float *w, *b;
+    const double *stats;
+    double2 *part;                            // forward [n][groups][parts][chunks], backward [n][parts][c]
+    double2 *chan;                            // backward [n][c]
+    float2 *mean_rstd;
+    float *dw, *db;
+};
+
+
+// ----------------------------------------------------------------------------------------------------------- activations
+// Two values at a time: the packed fp32 instructions halve what is issued, which with a SiLU or GELU bounds these kernels as much as memory does.
+// FINE: fp32 outputs of the forward pass, with expf and erfcf.  Elsewhere e^x without the correction for the rounding of x log2(e) (2^-24 |x| of e^x),
+// and the normal distribution by Abramowitz & Stegun 7.1.26: q(u) = (a1 s + .. + a5 s^5) e^(-u^2), s = 1 / (1 + p u), for erfc(u), u >= 0, off by at
+// most 1.5e-7.  A derivative is a factor of size one, so both are within a few units of 2^-24 of it.
+__device__ __forceinline__ float ex2(float x)
+{
+    float e;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x));
+    return e;
+}
+__device__ __forceinline__ f32x2 pair(float a, float b) { return pack2(__float_as_uint(a), __float_as_uint(b)); }
+__device__ __forceinline__ f32x2 ex2_2(f32x2 v) { float a, b; unpack2(v, a, b); return pair(ex2(a), ex2(b)); }
+__device__ __forceinline__ f32x2 rcp_2(f32x2 v) { float a, b; unpack2(v, a, b); return pair(reciprocal(a), reciprocal(b)); }
+__device__ __forceinline__ f32x2 sigmoid_2(f32x2 t) { return rcp_2(add2(ex2_2(mul2(t, twice(-1.4426950408889634f))), twice(1.f))); }
+
+// below = P(X <= t) of the normal distribution, density = e^(-t^2 / 2)
+__device__ __forceinline__ void normal_2(f32x2 t, f32x2 &below, f32x2 &density)
+{
+    density = ex2_2(mul2(t, mul2(t, twice(-0.72134752044448170f))));
+    float a, b;
+    unpack2(t, a, b);
+    const f32x2 s = rcp_2(fma2(pair(fabsf(a), fabsf(b)), twice(0.3275911f * 0.70710678118654752f), twice(1.f)));
+    f32x2 q = fma2(s, twice(0.5f * 1.061405429f), twice(0.5f * -1.453152027f));
+    q = fma2(s, q, twice(0.5f * 1.421413741f));
+    q = fma2(s, q, twice(0.5f * -0.284496736f));
+    q = fma2(s, q, twice(0.5f * 0.254829592f));
+    q = mul2(mul2(q, s), density);
+    float q0, q1, u0, u1;
+    unpack2(q, q0, q1);
+    unpack2(fma2(q, twice(-1.f), twice(1.f)), u0, u1);
+    below = pair(a > 0.f ? u0 : q0, b > 0.f ? u1 : q1);
+}
+template <int ACT, bool FINE> __device__ __forceinline__ f32x2 activate(f32x2 t, float slope)
+{
+    if constexpr (ACT == LAMP_ACT_NONE) return t;
+    float a, b;
+    unpack2(t, a, b);
+    if constexpr (ACT == LAMP_ACT_LEAKY_RELU) return pair(a > 0.f ? a : slope * a, b > 0.f ? b : slope * b);
+    if constexpr (ACT == LAMP_ACT_SILU) {
+        if (FINE) return pair(a * sigmoid<true>(a), b * sigmoid<true>(b));
+        return mul2(t, sigmoid_2(t));
+    }
+    if (FINE) return pair(a * (0.5f * erfcf(a * -0.70710678118654752f)), b * (0.5f * erfcf(b * -0.70710678118654752f)));
+    f32x2 below, density;
+    normal_2(t, below, density);
+    return mul2(t, below);
+}
+// v * act'(t)
+template <int ACT> __device__ __forceinline__ f32x2 times_derivative(f32x2 v, f32x2 t, float slope)
+{
+    if constexpr (ACT == LAMP_ACT_NONE) return v;
+    if constexpr (ACT == LAMP_ACT_LEAKY_RELU) {
+        float a, b, x, y;
+        unpack2(t, a, b);
+        unpack2(v, x, y);
+        return pair(a > 0.f ? x : a <= 0.f ? slope * x : a, b > 0.f ? y : b <= 0.f ? slope * y : b);       // NaN stays
+    }
+    if constexpr (ACT == LAMP_ACT_SILU) {
+        // s (1 + t (1 - s)) = s + y - y s with y = t s
+        const f32x2 s = sigmoid_2(t), y = mul2(t, s);
+        return mul2(v, add2(fma2(mul2(y, twice(-1.f)), s, y), s));
+    }
+    f32x2 below, density;
+    normal_2(t, below, density);
+    return mul2(v, fma2(mul2(t, twice(0.3989422804014327f)), density, below));
+}
+
+// -mean, rstd * w and b of this thread's channels
+struct Affine { f32x2 nm[4], a[4], b[4]; };
+// mr(g): (mean, rstd) of group g
+template <typename F> __device__ __forceinline__ Affine affine(const GnParams &P, int ch, F mr)
+{
+    float nm[8], a[8], b[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float2 s = mr((ch + j) / P.cg);
+        nm[j] = -s.x;
+        a[j] = s.y * (P.w ? P.w[ch + j] : 1.f);
+        b[j] = P.b ? P.b[ch + j] : 0.f;
+    }
+    Affine f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        f.nm[j] = pack2(__float_as_uint(nm[2 * j]), __float_as_uint(nm[2 * j + 1]));
+        f.a[j] = pack2(__float_as_uint(a[2 * j]), __float_as_uint(a[2 * j + 1]));
+        f.b[j] = pack2(__float_as_uint(b[2 * j]), __float_as_uint(b[2 * j + 1]));
+    }
+    return f;
+}
+
+// dt and (x - mean) of 8 channels
+template <bool XF, bool ZF, int ACT>
+__device__ __forceinline__ void slopes(const GnParams &P, const Affine &f, const Raw<XF> &rx, const Raw<ZF> &rz, f32x2 (&d)[4], f32x2 (&dt)[4])
+{
+    to_pairs<XF>(rx, d);
+    to_pairs<ZF>(rz, dt);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        d[j] = add2(d[j], f.nm[j]);
+        dt[j] = times_derivative<ACT>(dt[j], fma2(d[j], f.a[j], f.b[j]), P.slope);
+    }
+}
+
+// z of 8 channels
+template <bool XF, bool ZF, int ACT>
+__device__ __forceinline__ void apply(const GnParams &P, const Affine &f, const Raw<XF> &r, float (&z)[8])
+{
+    f32x2 t[4];
+    to_pairs<XF>(r, t);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) unpack2(activate<ACT, ZF>(fma2(add2(t[j], f.nm[j]), f.a[j], f.b[j]), P.slope), z[2 * j], z[2 * j + 1]);
+}
+
+// dx = dt a + (x - mean) e + h,  e = -rstd^2 mean(w dt xhat), h = -rstd mean(w dt);  m: the two means
+struct Back { f32x2 e[4], h[4]; };
+template <typename F, typename G> __device__ __forceinline__ Back back_terms(const GnParams &P, int ch, F mr, G means)
+{
+    Back k;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        float ev[2], hv[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int g = (ch + 2 * j + i) / P.cg;
+            const float rstd = mr(g).y;
+            const float2 m = means(g);
+            ev[i] = -rstd * (rstd * m.y);
+            hv[i] = -rstd * m.x;
+        }
+        k.e[j] = pair(ev[0], ev[1]);
+        k.h[j] = pair(hv[0], hv[1]);
+    }
+    return k;
+}
+template <bool XF, bool ZF, int ACT>
+__device__ __forceinline__ void back_apply(const GnParams &P, const Affine &f, const Back &k, const Raw<XF> &rx, const Raw<ZF> &rz, float (&o)[8])
+{
+    f32x2 d[4], dt[4];
+    slopes<XF, ZF, ACT>(P, f, rx, rz, d, dt);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) unpack2(fma2(dt[j], f.a[j], fma2(d[j], k.e[j], k.h[j])), o[2 * j], o[2 * j + 1]);
+}
+
+template <bool XF> __device__ __forceinline__ float value_at(const void *p, int64_t i) { return XF ? ((const float *)p)[i] : bf2f(((const bf16 *)p)[i]); }
+
+// A thread's sums of d and d^2 about k (nk = -k) as fp64 sums about r
+__device__ __forceinline__ void about(float nk, float s1, float s2, int n, double r, double &a, double &b)
+{
+    const double e = -(double)nk - r, m = (double)n;
+    a = (double)s1 + m * e;
+    b = (double)s2 + e * (2.0 * s1 + m * e);
+}
+__device__ __forceinline__ float2 mean_rstd_of(double s, double t, double r, double count, float eps)
+{
+    const double mu = s / count, var = t / count - mu * mu;
+    return make_float2((float)(r + mu), (float)(1.0 / sqrt((var < 0.0 ? 0.0 : var) + (double)eps)));
+}
+
+// Sum over `ty` lines of uc units of 8 pairs of fp64 per thread: sa[channel], sb[channel] of the chunk on return.  sm: 2 * ty * uc * 8 values.
+struct Totals { const double *a, *b; };
+__device__ __forceinline__ Totals sum_lines(int ty, int uc, int my_line, int my_unit, const double (&a)[8], const double (&b)[8], double *sm)
+{
+    const int cc = uc * 8;
+    double *sa = sm, *sb = sm + ty * cc;
+    if (my_line < ty) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) { sa[my_line * cc + my_unit * 8 + j] = a[j]; sb[my_line * cc + my_unit * 8 + j] = b[j]; }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * cc; i += GT) {
+        double *s = i < cc ? sa + i : sb + (i - cc);
+        double t = s[0];
+#pragma unroll 8
+        for (int l = 1; l < ty; ++l) t += s[l * cc];
+        s[0] = t;
+    }
+    __syncthreads();
+    return Totals{sa, sb};
+}
+
+// For the groups g0 .. g1 in turn, several at a time: load(group, i) -> pair of values for i < count(group), their sum to done(group, s, t) in one
+// lane.  Every thread takes part.
+template <typename L, typename D> __device__ __forceinline__ void sum_groups(int g0, int g1, int cg, L load, D done)
+{
+    int lanes = 1;
+    while (lanes < 32 && lanes * 2 <= cg) lanes *= 2;
+    const int l = threadIdx.x % lanes, per = GT / lanes;
+    for (int g = g0; g <= g1; g += per) {                        // the same number of turns for every thread
+        const int mg = g + threadIdx.x / lanes;
+        double s = 0.0, t = 0.0;
+        if (mg <= g1) load(mg, l, lanes, s, t);
+        for (int o = lanes / 2; o > 0; o >>= 1) {
+            s += __shfl_xor_sync(0xffffffffu, s, o);
+            t += __shfl_xor_sync(0xffffffffu, t, o);
+        }
+        if (mg <= g1 && l == 0) done(mg, s, t);
+    }
+}
+
+}  // namespace gn
+
+// group_norm_small.cu.  Whether a cluster can hold what a group needs, and the pass in that form (forward, or backward with dz set; scratch:
+// [n][c] pairs of fp64 where dw or db is asked for).
+bool          gn_small_fits(const gn::GnParams &P, bool xf, bool back);
+lamp_status_t gn_small(const gn::GnParams &P, bool xf, bool zf, bool back, cudaStream_t st);
+
+}  // namespace lamp

@@ -1,8 +1,7 @@
 """Group norm with an activation on the GPU against the fp64 oracle, forward and backward.
 
 Tolerances, u = 2^-24, a = |w| rstd, t the argument of the activation.
-  Sums of a thread run about a value of its own data in two fp32 levels of at most 32 and 256 additions here, so a mean is off by at most
-  300 u of the spread (2 sd counted for |x - k|) and by its own rounding u |mean|; a variance by 600 u relative, rstd by half of that and its
+  Sums of a thread run about a value of its own data over at most 256 values in fp32, so a mean is off by at most 300 u of the spread (2 sd counted for |x - k|) and by its own rounding u |mean|; a variance by 600 u relative, rstd by half of that and its
   rounding:  e_t = u (a (2 |mean| + 600 sd + 304 |x - mean|) + 4 (|t| + |b|)).
   The slope of every activation is below 1.13; its own value is off by 8 u |z| (fp32: expf, erfcf, one product) or, for bf16 outputs, by
   8 u |z| + 4 u t^2 |z| (e^x without the correction of x log2 e) + 2^-22 |t| (the rational form of the normal distribution).  Then half a step of the type
@@ -24,7 +23,9 @@ TYPES = {"bf16": (torch.bfloat16, torch.bfloat16), "f32": (torch.float32, torch.
 # n, (d, h, w), c, groups
 SHAPES = [(1, (1, 1, 1), 8, 8), (2, (1, 1, 1), 16, 2), (1, (1, 1, 2), 24, 8), (3, (2, 3, 5), 24, 3), (2, (4, 4, 4), 512, 32), (1, (7, 9, 11), 40, 40),
           (2, (8, 8, 8), 320, 32), (1, (20, 21, 22), 32, 4), (4, (5, 5, 5), 64, 1), (1, (6, 5, 4), 2056, 8), (2, (3, 3, 3), 4096, 4096), (1, (33, 32, 31), 136, 17),
-          (1, (2, 2, 2), 2064, 3), (70, (1, 2, 3), 8, 2)]
+          (1, (2, 2, 2), 2064, 3), (70, (1, 2, 3), 8, 2),
+          # too many voxels for a cluster
+          (1, (26, 26, 26), 24, 3), (2, (20, 30, 31), 48, 2), (1, (21, 21, 21), 320, 32)]
 
 
 def dev(a, dt=torch.float32):
@@ -152,6 +153,21 @@ def test_backward_matches_oracle(shape, types):
         B.lamp_group_norm_act_bwd(p, vg, vx, mr, vd, dw, db, scratch(p, vx))
         check_backward(dv, dw, db, host(gv), host(xv), host(mr), w if i != 1 else np.ones(c), b if i != 2 else np.zeros(c), shape, name, slope, 1e-5, xt)
         assert untouched(db_, 16, c)
+
+
+def test_more_channels_than_a_cta_holds():
+    shape = (1, (26, 25, 26), 2064, 2064)
+    n, dhw, c, groups = shape
+    r, x, w, b = case(shape, 9)
+    tx, tg = dev(x, torch.bfloat16), dev(r.standard_normal(x.shape), torch.bfloat16)
+    z, dx, mr = torch.empty_like(tx), torch.empty_like(tx), torch.empty(n, groups, 2, device="cuda")
+    dw, db = torch.empty(c, device="cuda"), torch.empty(c, device="cuda")
+    p = B.group_norm(groups, dev(w), dev(b), "leaky_relu", 0.1)
+    ws = scratch(p, tx)
+    B.lamp_group_norm_act_fwd(p, tx, z, mr, ws)
+    check_forward(z, mr, host(tx), w, b, shape, "leaky_relu", 0.1, 1e-5, torch.bfloat16)
+    B.lamp_group_norm_act_bwd(p, tg, tx, mr, dx, dw, db, ws)
+    check_backward(dx, dw, db, host(tg), host(tx), host(mr), w, b, shape, "leaky_relu", 0.1, 1e-5, torch.bfloat16)
 
 
 @pytest.mark.parametrize("loc,spread", [(300.0, 0.01), (-1e4, 1.0), (0.0, 1e-3), (1e15, 1e13)])
