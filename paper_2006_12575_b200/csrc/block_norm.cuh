@@ -51,18 +51,6 @@ template <bool F32> __device__ __forceinline__ void store8(void *base, int64_t o
     }
 }
 
-// the same for data that nothing reads soon: it leaves L2 before what still has to be read there
-template <bool F32> __device__ __forceinline__ void store8_last(void *base, int64_t off, const float (&f)[8])
-{
-    if constexpr (F32) {
-        float4 *p = reinterpret_cast<float4 *>((float *)base + off);
-        __stcs(p, make_float4(f[0], f[1], f[2], f[3]));
-        __stcs(p + 1, make_float4(f[4], f[5], f[6], f[7]));
-    } else {
-        __stcs(reinterpret_cast<uint4 *>((bf16 *)base + off), pack8(f));
-    }
-}
-
 // the same as four packed pairs
 template <bool F32> __device__ __forceinline__ void to_pairs(const Raw<F32> &r, ptx::f32x2 (&f)[4])
 {

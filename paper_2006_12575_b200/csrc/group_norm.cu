@@ -4,7 +4,11 @@
 // sums, a pass that applies.  Forward both passes read x, backward both read x and dz; the second runs against the direction of the
 // first, so that it starts with what the first left in L2 (126 MB).  Bound by memory.
 // A voxel's channels are taken in units of 8 (16 bytes of bf16, 32 of fp32), a thread keeps its unit for all of its voxels, so
-// everything per channel stays in registers; a CTA holds TY voxels side by side and a run of voxels of one sample.
+// everything per channel stays in registers; a CTA holds TY voxels of one sample side by side and takes every parts-th TY of them.
+// Each thread copies its values asynchronously into a ring of its own in shared memory, D units ahead of the one it works on (nobody else reads
+// them, so no barrier): as many bytes in flight as with registers, all the time, and the first are on their way while the constants are
+// formed.  With U units loaded into registers, worked on, and the next ones loaded, 128^3 x 32 bf16 backward took 129 us (now 118), 81,840 x 320
+// fp32 101 (89); 128^3 x 64 bf16 forward takes 152 either way.
 // Sums: a thread adds d = x - k and d^2 of at most RUN voxels in fp32, k the mean of the first values it loads - without it the squares of
 // data far from 0 lose the variance.  Between threads, CTAs and channels of a group the sums are fp64, taken about r, the group's first
 // value, and added in a fixed order.
@@ -19,12 +23,15 @@ using namespace gn;
 // CTAs per SM that the streaming kernels are compiled and sized for
 constexpr int resident(bool xf, bool back) { return (xf ? 3 : 4) - (back ? 1 : 0); }
 constexpr int RUN = 256;                      // voxels that a thread sums at most
+// units ahead: 32 KB of rings per CTA forward, 48 KB (36 KB for fp32 with bf16) backward; deeper ones leave the L1 cache too little for fp32 (six
+// units: 105 us on 81,840 x 320 fp32 backward, three: 89)
+__host__ __device__ constexpr int depth(bool xf, bool back) { return back ? (xf ? 3 : 6) : (xf ? 4 : 8); }
 
 // ----------------------------------------------------------------------------------------------------------- places
 struct Place {
-    int64_t sample, v0, v1;                   // voxels of this CTA
+    int64_t sample, v0;                       // this thread's first voxel
     int part, ch, unit, ty;                   // this thread's first channel, its unit in the chunk, its voxel line
-    bool active;
+    int count;                                // of this thread's voxels, P.apart apart
 };
 __device__ __forceinline__ Place place(const GnParams &P)
 {
@@ -36,66 +43,107 @@ __device__ __forceinline__ Place place(const GnParams &P)
     q.unit = threadIdx.x - q.ty * P.uc;
     const int u = blockIdx.y * P.uc + q.unit;
     q.ch = u * 8;
-    q.active = q.ty < P.ty && q.ch < P.c;
-    q.v0 = q.part * P.run;
-    q.v1 = min(P.v, q.v0 + P.run);
+    q.v0 = (int64_t)q.part * P.ty + q.ty;
+    q.count = q.ty < P.ty && q.ch < P.c && q.v0 < P.v ? (int)((P.v - q.v0 + P.apart - 1) / P.apart) : 0;
     return q;
 }
 
-// first voxel of this thread's last batch of U (below v0 where it has none)
-template <int U> __device__ __forceinline__ int64_t last_batch(const GnParams &P, const Place &q)
+// This thread's D units in shared memory
+template <bool F32, int D> struct Ring {
+    static constexpr int PLANE = GT * 16, SLOT = PLANE * (F32 ? 2 : 1), BYTES = D * SLOT;
+    uint32_t at;
+    __device__ __forceinline__ explicit Ring(void *smem) { at = ptx::smem_u32(smem) + threadIdx.x * 16; }
+    __device__ __forceinline__ void load(int slot, const void *base, int64_t off) const
+    {
+        const char *p = (const char *)base + off * (F32 ? 4 : 2);
+        if (F32) {                                                // the two halves of a sector come one after the other: through L1
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(at + slot * SLOT), "l"(p) : "memory");
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(at + slot * SLOT + PLANE), "l"(p + 16) : "memory");
+        } else asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at + slot * SLOT), "l"(p) : "memory");
+    }
+    __device__ __forceinline__ Raw<F32> get(int slot) const
+    {
+        Raw<F32> r;
+#pragma unroll
+        for (int i = 0; i < (F32 ? 2 : 1); ++i)
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.v[i].x), "=r"(r.v[i].y), "=r"(r.v[i].z), "=r"(r.v[i].w) : "r"(at + slot * SLOT + i * PLANE) : "memory");
+        return r;
+    }
+};
+// One group per unit, empty ones behind the last: the group D - N units ahead has landed when at most N are outstanding.
+__device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void landed() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// start(i, slot) sends for unit i, take(slot) reads it out of its slot, work(i, unit) does the rest; all of the `count` units in turn.
+template <int D, typename S> __device__ __forceinline__ void begin(int count, S start)
 {
-    const int64_t first = q.v0 + q.ty;
-    return first < q.v1 ? first + (q.v1 - first - 1) / (U * P.ty) * (U * P.ty) : q.v0 - 1;
+#pragma unroll
+    for (int i = 0; i < D; ++i) {
+        if (i < count) start(i, i);
+        commit();
+    }
+}
+template <int D, typename S, typename T, typename W> __device__ __forceinline__ void stream(int count, S start, T take, W work)
+{
+    int slot = 0;
+#pragma unroll 1
+    for (int i = 0; i < count; ++i) {
+        landed<D - 1>();
+        const auto unit = take(slot);
+        if (i + D < count) start(i + D, slot);                   // the slot has been read
+        commit();
+        work(i, unit);
+        slot = slot + 1 == D ? 0 : slot + 1;
+    }
 }
 
 // ----------------------------------------------------------------------------------------------------------- forward
-template <bool XF, int U>
+template <bool XF>
 __global__ void __launch_bounds__(GT, resident(XF, false))
 gn_sums_kernel(const GnParams P)
 {
-    extern __shared__ __align__(16) double sm[];
+    extern __shared__ __align__(16) double sm[];                // the rings, then the sums over the lines
+    constexpr int D = depth(XF, false);
     pdl_launch_dependents();
     pdl_wait();
     const Place q = place(P);
-    const int64_t base = q.sample * P.v;
+    const int64_t base = q.sample * P.v, step = P.apart * P.px, x0 = (base + q.v0) * P.px + q.ch;
+    const int mine = q.count;
+    const Ring<XF, D> ring(sm);
+    const auto start = [&](int i, int slot) { ring.load(slot, P.x, x0 + i * step); };
     f32x2 k[4], s1[4], s2[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) k[j] = s1[j] = s2[j] = 0;
-    int mine = 0;
-    if (q.active) {
-        mine = q.v1 > q.v0 + q.ty ? ((int)(q.v1 - q.v0) - q.ty + P.ty - 1) / P.ty : 0;
-        const int64_t step = P.ty * P.px;
-        int64_t at = (base + q.v0 + q.ty) * P.px + q.ch;
-        Raw<XF> r[U];
-        for (int left = mine; left > 0; left -= U, at += U * step) {
+    begin<D>(mine, start);
+    if (mine > 0) {
+        constexpr int FIRST = D < 4 ? D : 4;
+        const int first = mine < FIRST ? mine : FIRST;
+        landed<D - FIRST>();
 #pragma unroll
-            for (int u = 0; u < U; ++u) if (u < left) r[u] = load_raw<XF>(P.x, at + u * step);
-            if (left == mine) {
-                f32x2 t[4], s[4] = {0, 0, 0, 0};
+        for (int u = 0; u < FIRST; ++u) {
+            if (u >= first) break;
+            f32x2 t[4];
+            to_pairs<XF>(ring.get(u), t);
 #pragma unroll
-                for (int u = 0; u < U; ++u) if (u < left) {
-                    to_pairs<XF>(r[u], t);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) s[j] = add2(s[j], t[j]);
-                }
-                const float inv = -1.f / (float)(left < U ? left : U);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) k[j] = mul2(s[j], twice(inv));      // -k
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) if (u < left) {
-                f32x2 t[4];
-                to_pairs<XF>(r[u], t);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const f32x2 d = add2(t[j], k[j]);
-                    s1[j] = add2(s1[j], d);
-                    s2[j] = fma2(d, d, s2[j]);
-                }
-            }
+            for (int j = 0; j < 4; ++j) k[j] = add2(k[j], t[j]);
         }
+        const float inv = -1.f / (float)first;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) k[j] = mul2(k[j], twice(inv));              // -k
     }
+    stream<D>(mine, start, [&](int slot) { return ring.get(slot); },
+              [&](int, const Raw<XF> &r) {
+                  f32x2 t[4];
+                  to_pairs<XF>(r, t);
+#pragma unroll
+                  for (int j = 0; j < 4; ++j) {
+                      const f32x2 d = add2(t[j], k[j]);
+                      s1[j] = add2(s1[j], d);
+                      s2[j] = fma2(d, d, s2[j]);
+                  }
+              });
+    landed<0>();
+    __syncthreads();                                            // the rings make room
     double a[8], b[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) a[j] = b[j] = 0.0;
@@ -110,7 +158,7 @@ gn_sums_kernel(const GnParams P)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const double r = value_at<XF>(P.x, base * P.px + (q.ch + j) / P.cg * P.cg);
-            about(nk[j], f1[j], f2[j], (int)mine, r, a[j], b[j]);
+            about(nk[j], f1[j], f2[j], mine, r, a[j], b[j]);
         }
     }
     const Totals tot = sum_lines(P.ty, P.uc, q.ty, q.unit, a, b, sm);
@@ -168,73 +216,65 @@ __device__ __forceinline__ auto stats_of(const GnParams &P, const Place &q)
     return [mr = P.mean_rstd + q.sample * P.groups](int g) { return mr[g]; };
 }
 
-template <bool XF, bool ZF, int ACT, int U>
+template <bool XF, bool ZF, int ACT>
 __global__ void __launch_bounds__(GT, resident(XF, false))
 gn_apply_kernel(const GnParams P)
 {
+    extern __shared__ __align__(16) double sm[];
+    constexpr int D = depth(XF, false);
     pdl_launch_dependents();
     pdl_wait();
     const Place q = place(P);
-    if (!q.active) return;
-    const int64_t base = q.sample * P.v;
+    const int mine = q.count;
+    if (mine == 0) return;
+    const int64_t line = q.sample * P.v + q.v0 + (mine - 1) * P.apart;             // backwards from the last voxel
+    const int64_t step = P.apart * P.px, x0 = line * P.px + q.ch, out_step = P.apart * P.po, o0 = line * P.po + q.ch;
+    const Ring<XF, D> ring(sm);
+    const auto start = [&](int i, int slot) { ring.load(slot, P.x, x0 - i * step); };
+    begin<D>(mine, start);
     const Affine f = affine(P, q.ch, stats_of(P, q));
-    for (int64_t v = last_batch<U>(P, q); v >= q.v0; v -= (int64_t)U * P.ty) {
-        Raw<XF> r[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t at = v + (int64_t)u * P.ty;
-            if (at < q.v1) r[u] = load_raw<XF>(P.x, (base + at) * P.px + q.ch);
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t at = v + (int64_t)u * P.ty;
-            if (at >= q.v1) continue;
-            float z[8];
-            apply<XF, ZF, ACT>(P, f, r[u], z);
-            store8_last<ZF>(P.out, (base + at) * P.po + q.ch, z);
-        }
-    }
+    stream<D>(mine, start, [&](int slot) { return ring.get(slot); },
+              [&](int i, const Raw<XF> &r) {
+                  float z[8];
+                  apply<XF, ZF, ACT>(P, f, r, z);
+                  store8<ZF>(P.out, o0 - i * out_step, z);
+              });
 }
 
 // ----------------------------------------------------------------------------------------------------------- backward
 // sums over the CTA's voxels of dt and dt * xhat per channel
-template <bool XF, bool ZF, int ACT, int U>
+template <bool XF, bool ZF> struct Both { Raw<XF> x; Raw<ZF> z; };
+
+template <bool XF, bool ZF, int ACT>
 __global__ void __launch_bounds__(GT, resident(XF, true))
 gn_bwd_sums_kernel(const GnParams P)
 {
-    extern __shared__ __align__(16) double sm[];
+    extern __shared__ __align__(16) double sm[];                // the rings, then the sums over the lines
+    constexpr int D = depth(XF, true);
     pdl_launch_dependents();
     pdl_wait();
     const Place q = place(P);
-    const int64_t base = q.sample * P.v;
+    const int mine = q.count;
+    const int64_t line = q.sample * P.v + q.v0, xs = P.apart * P.px, x0 = line * P.px + q.ch, zs = P.apart * P.pdz, z0 = line * P.pdz + q.ch;
+    const Ring<XF, D> rx(sm);
+    const Ring<ZF, D> rz((char *)sm + Ring<XF, D>::BYTES);
+    const auto start = [&](int i, int slot) { rx.load(slot, P.x, x0 + i * xs); rz.load(slot, P.dz, z0 + i * zs); };
+    begin<D>(mine, start);
     double a[8], b[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) a[j] = b[j] = 0.0;
-    if (q.active) {
+    if (mine > 0) {
         const Affine f = affine(P, q.ch, stats_of(P, q));
         f32x2 s1[4], s2[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) s1[j] = s2[j] = 0;
-        for (int64_t v = q.v0 + q.ty; v < q.v1; v += (int64_t)U * P.ty) {
-            Raw<XF> rx[U];
-            Raw<ZF> rz[U];
+        stream<D>(mine, start, [&](int slot) { return Both<XF, ZF>{rx.get(slot), rz.get(slot)}; },
+                  [&](int, const Both<XF, ZF> &r) {
+                      f32x2 d[4], dt[4];
+                      slopes<XF, ZF, ACT>(P, f, r.x, r.z, d, dt);
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int64_t at = v + (int64_t)u * P.ty;
-                if (at < q.v1) {
-                    rx[u] = load_raw<XF>(P.x, (base + at) * P.px + q.ch);
-                    rz[u] = load_raw<ZF>(P.dz, (base + at) * P.pdz + q.ch);
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (v + (int64_t)u * P.ty >= q.v1) continue;
-                f32x2 d[4], dt[4];
-                slopes<XF, ZF, ACT>(P, f, rx[u], rz[u], d, dt);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) { s1[j] = add2(s1[j], dt[j]); s2[j] = fma2(dt[j], d[j], s2[j]); }
-            }
-        }
+                      for (int j = 0; j < 4; ++j) { s1[j] = add2(s1[j], dt[j]); s2[j] = fma2(dt[j], d[j], s2[j]); }
+                  });
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             float f1[2], f2[2];
@@ -248,6 +288,8 @@ gn_bwd_sums_kernel(const GnParams P)
             }
         }
     }
+    landed<0>();
+    __syncthreads();                                            // the rings make room
     const Totals tot = sum_lines(P.ty, P.uc, q.ty, q.unit, a, b, sm);
     const int cc = P.uc * 8, c0 = blockIdx.y * cc;
     double2 *out = P.part + (q.sample * P.parts + q.part) * P.c + c0;
@@ -284,15 +326,23 @@ gn_bwd_parts_kernel(const GnParams P)
 }
 
 // dx, and dw and db from the sums of all samples
-template <bool XF, bool ZF, int ACT, int U>
+template <bool XF, bool ZF, int ACT>
 __global__ void __launch_bounds__(GT, resident(XF, true))
 gn_bwd_apply_kernel(const GnParams P)
 {
-    extern __shared__ __align__(16) float2 means[];             // of this chunk's groups: (mean(w dt), mean(w dt xhat))
+    extern __shared__ __align__(16) double sm[];                // the rings, then of this chunk's groups (mean(w dt), mean(w dt xhat))
+    constexpr int D = depth(XF, true);
     pdl_launch_dependents();
     pdl_wait();
     const Place q = place(P);
-    const int64_t base = q.sample * P.v;
+    const int mine = q.count;
+    const int64_t line = q.sample * P.v + q.v0 + (mine - 1) * P.apart;             // backwards from the last voxel
+    const int64_t xs = P.apart * P.px, x0 = line * P.px + q.ch, zs = P.apart * P.pdz, z0 = line * P.pdz + q.ch, os = P.apart * P.po, o0 = line * P.po + q.ch;
+    const Ring<XF, D> rx(sm);
+    const Ring<ZF, D> rz((char *)sm + Ring<XF, D>::BYTES);
+    float2 *means = (float2 *)((char *)sm + Ring<XF, D>::BYTES + Ring<ZF, D>::BYTES);
+    const auto start = [&](int i, int slot) { rx.load(slot, P.x, x0 - i * xs); rz.load(slot, P.dz, z0 - i * zs); };
+    begin<D>(mine, start);
     const int cc = P.uc * 8, c0 = blockIdx.y * cc, c1 = min(P.c, c0 + cc), g0 = c0 / P.cg, g1 = (c1 - 1) / P.cg;
     const double inv = 1.0 / ((double)P.v * P.cg);
     sum_groups(g0, g1, P.cg,
@@ -319,59 +369,42 @@ gn_bwd_apply_kernel(const GnParams P)
             if (lane == 0 && P.dw) P.dw[ch] = (float)t;
         }
     }
-    if (!q.active) return;
+    if (mine == 0) return;
     const Affine f = affine(P, q.ch, stats_of(P, q));
     const Back k = back_terms(P, q.ch, stats_of(P, q), [&](int g) { return means[g - g0]; });
-    for (int64_t v = last_batch<U>(P, q); v >= q.v0; v -= (int64_t)U * P.ty) {
-        Raw<XF> rx[U];
-        Raw<ZF> rz[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t at = v + (int64_t)u * P.ty;
-            if (at < q.v1) {
-                rx[u] = load_raw<XF>(P.x, (base + at) * P.px + q.ch);
-                rz[u] = load_raw<ZF>(P.dz, (base + at) * P.pdz + q.ch);
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t at = v + (int64_t)u * P.ty;
-            if (at >= q.v1) continue;
-            float o[8];
-            back_apply<XF, ZF, ACT>(P, f, k, rx[u], rz[u], o);
-            store8_last<XF>(P.out, (base + at) * P.po + q.ch, o);
-        }
-    }
+    stream<D>(mine, start, [&](int slot) { return Both<XF, ZF>{rx.get(slot), rz.get(slot)}; },
+              [&](int i, const Both<XF, ZF> &r) {
+                  float o[8];
+                  back_apply<XF, ZF, ACT>(P, f, k, r.x, r.z, o);
+                  store8<XF>(P.out, o0 - i * os, o);
+              });
 }
 
 // ----------------------------------------------------------------------------------------------------------- host
-// Units, lines and runs for a sample of v voxels: about `per_sm` CTAs per SM, none with less than a batch of u voxels per thread or more than
-// RUN of them.
-void split(GnParams &P, int u, int per_sm)
+// Units, lines and parts for a sample of v voxels: about `per_sm` CTAs per SM, none with fewer than 4 voxels per thread where that leaves it without
+// work, none with more than RUN.
+void split(GnParams &P, int per_sm)
 {
     const int units = P.c / 8;
     P.chunks = (units + GT - 1) / GT;
     P.uc = (units + P.chunks - 1) / P.chunks;
     P.ty = GT / P.uc;
     const int64_t room = (int64_t)sm_count() * per_sm / ((int64_t)P.n * P.chunks), least = (P.v + (int64_t)P.ty * RUN - 1) / ((int64_t)P.ty * RUN);
-    const int64_t need = (P.v + (int64_t)P.ty * u - 1) / ((int64_t)P.ty * u);
+    const int64_t need = (P.v + (int64_t)P.ty * 4 - 1) / ((int64_t)P.ty * 4);
     int64_t parts = need < room ? need : room;
     if (parts < least) parts = least;
-    P.run = (P.v + parts - 1) / parts;
-    P.run = (P.run + P.ty - 1) / P.ty * P.ty;
-    P.parts = (int32_t)((P.v + P.run - 1) / P.run);
+    P.parts = (int32_t)parts;
+    P.apart = (int64_t)P.ty * parts;
 }
-
-constexpr int SUM_U = 4, BWD_U = 2;           // voxels in flight per thread
 
 size_t workspace(int64_t v, int n, int c)
 {
     // the larger of the forward pass' [n][groups][parts][chunks] and the backward pass' [n][parts + 1][c], groups = c at most
     GnParams P = {};
     P.v = v; P.n = n; P.c = c;
-    split(P, SUM_U, resident(false, false));
+    split(P, resident(false, false));
     const size_t fwd = (size_t)n * c * P.parts * P.chunks;
-    split(P, BWD_U, resident(false, true));
+    split(P, resident(false, true));
     const size_t bwd = (size_t)n * c * (P.parts + 1);
     return (fwd > bwd ? fwd : bwd) * sizeof(double2);
 }
@@ -409,22 +442,23 @@ GnParams params(const lamp_group_norm_t *p, const lamp_tensor_t *x, const float 
 
 bool short_launch(const GnParams &P) { return (int64_t)P.n * P.v * P.c <= 32 * 1024 * 1024; }
 
+size_t larger(size_t a, size_t b) { return a > b ? a : b; }
+size_t lines_bytes(const GnParams &P) { return (size_t)P.ty * P.uc * 8 * 2 * sizeof(double); }
+
 template <bool XF, bool ZF, int ACT>
 lamp_status_t forward(GnParams &P, cudaStream_t st)
 {
     lamp_status_t s;
     const bool early = short_launch(P);
-    split(P, SUM_U, resident(XF, false));
+    const size_t rings = Ring<XF, depth(XF, false)>::BYTES;
+    split(P, resident(XF, false));
     const dim3 grid((unsigned)(P.n * P.parts), (unsigned)P.chunks);
-    if (!P.stats) {
-        const size_t smem = (size_t)P.ty * P.uc * 8 * 2 * sizeof(double);
-        if ((s = launch_pdl(early, gn_sums_kernel<XF, SUM_U>, grid, dim3(GT), smem, st, P)) != LAMP_OK) return s;
-    }
+    if (!P.stats && (s = launch_pdl(early, gn_sums_kernel<XF>, grid, dim3(GT), larger(rings, lines_bytes(P)), st, P)) != LAMP_OK) return s;
     const int64_t all = (int64_t)P.n * P.groups;
     const bool many = P.stats ? P.cg > 256 : P.parts > 128;
     if ((s = launch_pdl(early, many ? gn_finish_kernel<XF, GT / 32> : gn_finish_kernel<XF, 1>, dim3((unsigned)(many ? all : (all + GT / 32 - 1) / (GT / 32))), dim3(GT), 0, st,
                         P)) != LAMP_OK) return s;
-    return launch_pdl(early, gn_apply_kernel<XF, ZF, ACT, SUM_U>, grid, dim3(GT), 0, st, P);
+    return launch_pdl(early, gn_apply_kernel<XF, ZF, ACT>, grid, dim3(GT), rings, st, P);
 }
 
 template <bool XF, bool ZF, int ACT>
@@ -432,13 +466,17 @@ lamp_status_t backward(GnParams &P, cudaStream_t st)
 {
     lamp_status_t s;
     const bool early = short_launch(P);
-    split(P, BWD_U, resident(XF, true));
+    constexpr int D = depth(XF, true);
+    const size_t rings = Ring<XF, D>::BYTES + Ring<ZF, D>::BYTES;
+    split(P, resident(XF, true));
     const dim3 grid((unsigned)(P.n * P.parts), (unsigned)P.chunks);
-    const size_t smem = (size_t)P.ty * P.uc * 8 * 2 * sizeof(double);
     P.chan = P.parts > 1 ? P.part + (int64_t)P.n * P.parts * P.c : P.part;
-    if ((s = launch_pdl(early, gn_bwd_sums_kernel<XF, ZF, ACT, BWD_U>, grid, dim3(GT), smem, st, P)) != LAMP_OK) return s;
+    static SmemAttrOnce sums, applies;
+    if ((s = sums.ensure(gn_bwd_sums_kernel<XF, ZF, ACT>, (int)rings)) != LAMP_OK) return s;
+    if ((s = applies.ensure(gn_bwd_apply_kernel<XF, ZF, ACT>, (int)(rings + (size_t)GT * 8 * sizeof(float2)))) != LAMP_OK) return s;
+    if ((s = launch_pdl(early, gn_bwd_sums_kernel<XF, ZF, ACT>, grid, dim3(GT), larger(rings, lines_bytes(P)), st, P)) != LAMP_OK) return s;
     if (P.parts > 1 && (s = launch_pdl(early, gn_bwd_parts_kernel, dim3((unsigned)(P.c / 8 * P.n)), dim3(1024), 0, st, P)) != LAMP_OK) return s;
-    return launch_pdl(early, gn_bwd_apply_kernel<XF, ZF, ACT, BWD_U>, grid, dim3(GT), (size_t)P.uc * 8 * sizeof(float2), st, P);
+    return launch_pdl(early, gn_bwd_apply_kernel<XF, ZF, ACT>, grid, dim3(GT), rings + (size_t)P.uc * 8 * sizeof(float2), st, P);
 }
 
 template <bool XF, bool ZF>

@@ -2,7 +2,8 @@
 // A cluster of up to 8 CTAs takes the channels c0 .. c0 + cc of a sample (whole groups, whole units), each CTA a run of its voxels, at most U per
 // thread.  The values are loaded all at once and stay in registers while the sums go through shared memory, over the cluster's
 // distributed shared memory (added in rank order in every CTA), and back.
-// Bound by latency: the deepest level of a U-Net (2 x 512 voxels x 512 channels) took 11 us as three kernels of the streaming form, SMALLNOW here.
+// Bound by latency: the deepest level of a U-Net (2 x 512 voxels x 512 channels) took 11 us as three kernels of the streaming form and 25 us a call;
+// 8.5 and 12 here.
 #include "group_norm.cuh"
 #include <numeric>
 
