@@ -41,7 +41,12 @@ struct Divisor {
 __device__ __forceinline__ float quotient(float a, float b, float inv)
 {
     const float q = a * inv;
-    return copysignf(fmaf(fmaf(-q, b, a), inv, q), a);           // -0 keeps its sign
+    return fmaf(-fmaf(q, b, -a), inv, q);                        // the remainder's negative: so -0 keeps its sign
+}
+__device__ __forceinline__ ptx::f32x2 quotient2(ptx::f32x2 a, ptx::f32x2 b, ptx::f32x2 inv, ptx::f32x2 minus_inv)
+{
+    const ptx::f32x2 q = ptx::mul2(a, inv);
+    return ptx::fma2(ptx::fma2(q, b, ptx::mul2(a, ptx::twice(-1.f))), minus_inv, q);
 }
 __device__ __forceinline__ bool plain_range(float b) { return b >= 8.0779357e-28f && b <= 1.2379400e27f; }
 
@@ -88,19 +93,21 @@ __device__ __forceinline__ uint32_t encode8(const float (&v)[8])
 }
 template <int BLOCK> __device__ __forceinline__ uint32_t encode8(const float (&f)[8], const Scale &s)
 {
-    if (s.by == 0.f) return 0u;
     float v[8];
     if (BLOCK == 32) {
+        const ptx::f32x2 inv = ptx::twice(s.inv);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = f[i] * s.inv;
+        for (int i = 0; i < 8; i += 2) ptx::unpack2(ptx::mul2(ptx::pack2(__float_as_uint(f[i]), __float_as_uint(f[i + 1])), inv), v[i], v[i + 1]);
     } else if (plain_range(s.by)) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = quotient(f[i], s.by, s.inv);
+        for (int i = 0; i < 8; i += 2)
+            ptx::unpack2(quotient2(ptx::pack2(__float_as_uint(f[i]), __float_as_uint(f[i + 1])), ptx::twice(s.by), ptx::twice(s.inv), ptx::twice(-s.inv)), v[i], v[i + 1]);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = __fdiv_rn(f[i], s.by);
     }
-    return encode8(v);
+    const uint32_t r = encode8(v);
+    return s.by == 0.f ? 0u : r;
 }
 
 __device__ __forceinline__ void decode8(uint32_t codes, float (&v)[8])

@@ -14,7 +14,8 @@ constexpr int QT = 256, QU = 4;
 
 // A segment is up to 128 channels of a voxel, 8 channels on each of LPS lanes (4, 8 or 16: as many as the channels need, at least a block of
 // 32).  A thread takes QU rows QT / LPS apart at the same channels, so that addresses are formed once: formed for every row they were most of
-// the kernel's instructions (28 us for 131,072 x 256 bf16 against QNOW).
+// the kernel's instructions (28 us for 131,072 x 256 bf16 against QNOW;
+// what is left is bound by the instructions of the conversion as much as by memory).
 struct RowParams {
     void *x;                                  // source, or destination of the values
     int64_t pitch, rows;
@@ -45,52 +46,87 @@ template <int LPS> struct RowPlace {
     }
 };
 
-template <bool F32> __device__ __forceinline__ uint32_t amax_of(const Raw<F32> &r)
+// Bits of the amax of each of the thread's units over the LANES lanes of its block.  bf16: two values, then two units, at a time.
+template <bool F32, int LANES> __device__ __forceinline__ void block_amax(const Raw<F32> (&r)[QU], uint32_t (&m)[QU])
 {
     if constexpr (F32) {
-        float f[8];
-        to_float<F32>(r, f);
-        return amax_bits(f);
-    } else {                                                       // two bf16 at a time
-        const uint32_t m = __vmaxu2(__vmaxu2(r.v[0].x & 0x7FFF7FFFu, r.v[0].y & 0x7FFF7FFFu), __vmaxu2(r.v[0].z & 0x7FFF7FFFu, r.v[0].w & 0x7FFF7FFFu));
-        return max(m & 0xFFFF0000u, m << 16);
+#pragma unroll
+        for (int u = 0; u < QU; ++u) {
+            float f[8];
+            to_float<F32>(r[u], f);
+            m[u] = amax_bits(f);
+#pragma unroll
+            for (int o = LANES / 2; o > 0; o >>= 1) m[u] = max(m[u], __shfl_xor_sync(0xffffffffu, m[u], o));
+        }
+    } else {
+        uint32_t both[QU / 2];
+#pragma unroll
+        for (int u = 0; u < QU; ++u) {
+            const uint4 &v = r[u].v[0];
+            m[u] = __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
+        }
+#pragma unroll
+        for (int u = 0; u < QU / 2; ++u) {                         // the halves of two units into one word
+            both[u] = __vmaxu2(__byte_perm(m[2 * u], m[2 * u + 1], 0x5410), __byte_perm(m[2 * u], m[2 * u + 1], 0x7632));
+#pragma unroll
+            for (int o = LANES / 2; o > 0; o >>= 1) both[u] = __vmaxu2(both[u], __shfl_xor_sync(0xffffffffu, both[u], o));
+            m[2 * u] = both[u] << 16;
+            m[2 * u + 1] = both[u] & 0xFFFF0000u;
+        }
     }
 }
+static_assert(QU == 4, "");
 
 template <bool F32, int BLOCK, int LPS>
 __global__ void __launch_bounds__(QT)
 quant4_rows_kernel(const RowParams P)
 {
     using Place = RowPlace<LPS>;
-    constexpr int LANES = BLOCK / 8;                               // of a block; 4 blocks to a word of scales
+    constexpr int LANES = BLOCK / 8;                               // of a block
     pdl_launch_dependents();
     pdl_wait();
     const Place at(P);
     const Divisor d(BLOCK == 16 && P.g ? __ldg(P.g) : 1.f);
-    const bool in = at.ch < P.c;
     const int blk = at.ch / BLOCK;
+    // rows of this thread (0 where its channels do not exist), and those that have a place among the scales: the last tile is filled up
+    const int64_t left = P.rows - at.row, left128 = (P.rows + 127) / 128 * 128 - at.row;
+    auto count = [](int64_t n) { return n <= 0 ? 0 : n > (QU - 1) * Place::RPP ? QU : (int)((n + Place::RPP - 1) / Place::RPP); };
+    const int rows = at.ch < P.c ? count(left) : 0, places = blk / 4 < P.tiles ? count(left128) : 0;
+    const int64_t step = Place::RPP * P.pitch, q_step = Place::RPP * P.q_pitch, x0 = at.row * P.pitch + at.ch;
     Raw<F32> r[QU];
 #pragma unroll
-    for (int u = 0; u < QU; ++u) r[u] = in && at.row + u * Place::RPP < P.rows ? load_raw<F32>(P.x, (at.row + u * Place::RPP) * P.pitch + at.ch) : zero_raw<F32>();
-    uint8_t *q = P.q + at.row * P.q_pitch + at.ch / 2, *scale = P.scale + scale_at(at.row, blk, P.tiles);
-    const int64_t rows128 = (P.rows + 127) / 128 * 128;            // rows that only fill up a tile get scale 0, as blocks behind the last do
-    const bool writes = threadIdx.x % (4 * LANES < LPS ? 4 * LANES : LPS) == 0 && blk / 4 < P.tiles;
+    for (int u = 0; u < QU; ++u) r[u] = u < rows ? load_raw<F32>(P.x, x0 + u * step) : zero_raw<F32>();
+    uint8_t *q = P.q + at.row * P.q_pitch + at.ch / 2, *scale = P.scale + scale_at(at.row, blk & ~3, P.tiles);
+    uint32_t m[QU], bytes = 0;                                     // scale bytes of this thread's block, one per unit
+    block_amax<F32, LANES>(r, m);
 #pragma unroll
     for (int u = 0; u < QU; ++u) {
-        const int64_t row = at.row + u * Place::RPP;
-        uint32_t m = amax_of<F32>(r[u]);
+        const Scale s = block_scale<BLOCK>(m[u], d);
+        bytes |= s.byte << (8 * u);
+        float f[8];
+        to_float<F32>(r[u], f);
+        if (u < rows) *reinterpret_cast<uint32_t *>(q + u * q_step) = encode8<BLOCK>(f, s);
+    }
+    // scale 0 for rows that only fill up a tile, as for blocks behind the last
+    const int have = blk * BLOCK < P.c ? count(left) : 0;
+    bytes &= have >= 4 ? 0xFFFFFFFFu : (1u << (8 * have)) - 1u;
+    if constexpr (LPS >= 4 * LANES) {
+        // Four blocks have four units' bytes each; a word of scales is one unit's byte of the four.  A transposition of 4 x 4 bytes over the
+        // lanes of the blocks: block j then holds the word of unit j.
+        const int j = (threadIdx.x / LANES) & 3;
+        uint32_t o = __shfl_xor_sync(0xffffffffu, bytes, LANES);
+        bytes = __byte_perm(bytes, o, j & 1 ? 0x3715 : 0x6240);
+        o = __shfl_xor_sync(0xffffffffu, bytes, 2 * LANES);
+        bytes = __byte_perm(bytes, o, j & 2 ? 0x3276 : 0x5410);
+        if (threadIdx.x % LANES == 0 && j < places) *reinterpret_cast<uint32_t *>(scale + Place::scale_off(j, P.tiles)) = bytes;
+    } else {
+        // fewer than four blocks in all: LPS / LANES of them, the rest of the word is 0
 #pragma unroll
-        for (int o = LANES / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-        const Scale s = block_scale<BLOCK>(m, d);
-        uint32_t word = blk * BLOCK < P.c && row < P.rows ? s.byte << (8 * (blk & 3)) : 0u;
-        if (LPS > LANES) word |= __shfl_xor_sync(0xffffffffu, word, LANES);
-        if (LPS > 2 * LANES) word |= __shfl_xor_sync(0xffffffffu, word, 2 * LANES);
-        if (in && row < P.rows) {
-            float f[8];
-            to_float<F32>(r[u], f);
-            *reinterpret_cast<uint32_t *>(q + (int64_t)(u * Place::RPP) * P.q_pitch) = encode8<BLOCK>(f, s);
+        for (int u = 0; u < QU; ++u) {
+            uint32_t word = ((bytes >> (8 * u)) & 0xFFu) << (8 * blk);
+            if (LPS > LANES) word |= __shfl_xor_sync(0xffffffffu, word, LANES);
+            if (threadIdx.x % LPS == 0 && u < places) *reinterpret_cast<uint32_t *>(scale + Place::scale_off(u, P.tiles)) = word;
         }
-        if (writes && row < rows128) *reinterpret_cast<uint32_t *>(scale + Place::scale_off(u, P.tiles)) = word;
     }
 }
 
@@ -124,9 +160,8 @@ dequant4_rows_kernel(const RowParams P)
     }
 }
 
-// Transposed: tiles of 128 voxels x 64 channels through shared memory.  A thread owns one channel and 32 voxels of the tile, that is one block of 32
-// or two of 16, and writes 16 bytes of codes.
-constexpr int TC = 64;
+// Transposed: tiles of 128 voxels x 64 channels (256 x 32 where there are no more channels) through shared memory.  A thread owns one channel and
+// 32 voxels of the tile, that is one block of 32 or two of 16, and writes 16 bytes of codes.
 struct TileParams {
     void *x;
     int64_t pitch, voxels;
@@ -137,22 +172,24 @@ struct TileParams {
     int64_t tiles;
     const float *g;
 };
-template <bool F32> struct TileLayout { static constexpr int ES = F32 ? 4 : 2, SP = TC * ES + 16, BYTES = 128 * SP, UNITS = TC * ES / 16; };
-static_assert(TileLayout<true>::BYTES <= 48 * 1024, "");
+template <bool F32, int TC> struct TileLayout {
+    static constexpr int VOX = QT / TC * 32, ES = F32 ? 4 : 2, SP = TC * ES + 16, BYTES = VOX * SP, UNITS = TC * ES / 16;
+    static_assert(BYTES <= 48 * 1024, "");
+};
 
-template <bool F32, int BLOCK>
+template <bool F32, int BLOCK, int TC>
 __global__ void __launch_bounds__(QT)
 quant4_tile_kernel(const TileParams P)
 {
-    using L = TileLayout<F32>;
+    using L = TileLayout<F32, TC>;
     extern __shared__ __align__(16) uint8_t smem[];
     pdl_launch_dependents();
     pdl_wait();
     const int t = threadIdx.x;
-    const int64_t r0 = (int64_t)blockIdx.x * 128;
+    const int64_t r0 = (int64_t)blockIdx.x * L::VOX;
     const int c0 = blockIdx.y * TC;
 #pragma unroll
-    for (int i = t; i < 128 * L::UNITS; i += QT) {
+    for (int i = t; i < L::VOX * L::UNITS; i += QT) {
         const int r = i / L::UNITS, u = i % L::UNITS;
         uint4 v = make_uint4(0, 0, 0, 0);
         if (r0 + r < P.voxels && c0 + u * (16 / L::ES) < P.c)
@@ -180,10 +217,15 @@ quant4_tile_kernel(const TileParams P)
 #pragma unroll
         for (int i = 0; i < BLOCK / 8; ++i) code[b * (BLOCK / 8) + i] = encode8<BLOCK>(f[i], s);
     }
-    // every block of the last tile along k and every row of a tile of rows gets its scale, 0 where there is none
+    // every block of the last tile along k and every row of a tile of rows gets its scale, 0 where there is none; the CTAs of the last channels
+    // write those of the rows behind their own
     if (blk / 4 < P.tiles) {
-        uint8_t *o = P.scale + scale_at(ch, blk, P.tiles);
-        if constexpr (BLOCK == 32) *o = (uint8_t)bytes; else *reinterpret_cast<uint16_t *>(o) = (uint16_t)bytes;
+        const int last = c0 + TC >= P.c ? (P.c + 127) / 128 * 128 : c0 + TC;
+        for (int row = ch; row < last; row += TC) {
+            uint8_t *o = P.scale + scale_at(row, blk, P.tiles);
+            const uint32_t v = row == ch ? bytes : 0u;
+            if constexpr (BLOCK == 32) *o = (uint8_t)v; else *reinterpret_cast<uint16_t *>(o) = (uint16_t)v;
+        }
     }
     if (ch >= P.c || v0 >= P.voxels) return;
     uint8_t *o = P.q + (int64_t)ch * P.q_pitch + v0 / 2;
@@ -195,16 +237,16 @@ quant4_tile_kernel(const TileParams P)
     }
 }
 
-template <bool F32, int BLOCK>
+template <bool F32, int BLOCK, int TC>
 __global__ void __launch_bounds__(QT)
 dequant4_tile_kernel(const TileParams P)
 {
-    using L = TileLayout<F32>;
+    using L = TileLayout<F32, TC>;
     extern __shared__ __align__(16) uint8_t smem[];
     pdl_launch_dependents();
     pdl_wait();
     const int t = threadIdx.x;
-    const int64_t r0 = (int64_t)blockIdx.x * 128;
+    const int64_t r0 = (int64_t)blockIdx.x * L::VOX;
     const int c0 = blockIdx.y * TC;
     const float g = BLOCK == 16 && P.g ? __ldg(P.g) : 1.f;
     const int col = t % TC, part = t / TC, ch = c0 + col;
@@ -240,7 +282,7 @@ dequant4_tile_kernel(const TileParams P)
     }
     __syncthreads();
 #pragma unroll
-    for (int i = t; i < 128 * L::UNITS; i += QT) {
+    for (int i = t; i < L::VOX * L::UNITS; i += QT) {
         const int r = i / L::UNITS, u = i % L::UNITS;
         if (r0 + r < P.voxels && c0 + u * (16 / L::ES) < P.c)
             *reinterpret_cast<uint4 *>((uint8_t *)P.x + ((r0 + r) * P.pitch + c0) * L::ES + u * 16) = *reinterpret_cast<const uint4 *>(smem + r * L::SP + u * 16);
@@ -263,13 +305,19 @@ lamp_status_t launch_rows(bool back, const RowParams &P, cudaStream_t st)
     if (P.c <= 64) return launch_rows_k<F32, BLOCK, 8>(back, P, st);
     return launch_rows_k<F32, BLOCK, 16>(back, P, st);
 }
+template <bool F32, int BLOCK, int TC>
+lamp_status_t launch_tiles_k(bool back, const TileParams &P, cudaStream_t st)
+{
+    using L = TileLayout<F32, TC>;
+    const int64_t gx = (P.voxels + L::VOX - 1) / L::VOX, gy = (P.c + TC - 1) / TC;
+    if (gy > 65535) return LAMP_ERR_UNSUPPORTED;
+    return launch_pdl(gx * gy <= 2048, back ? dequant4_tile_kernel<F32, BLOCK, TC> : quant4_tile_kernel<F32, BLOCK, TC>, dim3((unsigned)gx, (unsigned)gy), dim3(QT),
+                      (size_t)L::BYTES, st, P);
+}
 template <bool F32, int BLOCK>
 lamp_status_t launch_tiles(bool back, const TileParams &P, cudaStream_t st)
 {
-    const int64_t gx = (P.voxels + 127) / 128, gy = (P.c + 127) / 128 * (128 / TC);           // whole tiles of scales
-    if (gy > 65535) return LAMP_ERR_UNSUPPORTED;
-    return launch_pdl(gx * gy <= 2048, back ? dequant4_tile_kernel<F32, BLOCK> : quant4_tile_kernel<F32, BLOCK>, dim3((unsigned)gx, (unsigned)gy), dim3(QT),
-                      (size_t)TileLayout<F32>::BYTES, st, P);
+    return P.c <= 32 ? launch_tiles_k<F32, BLOCK, 32>(back, P, st) : launch_tiles_k<F32, BLOCK, 64>(back, P, st);
 }
 
 lamp_status_t convert(const lamp_tensor_t *x, int32_t transpose, const lamp_fp4_operand_t *o, bool back, cudaStream_t st)

@@ -129,7 +129,7 @@ def values(r, rows, c, dt):
     return x if dt is torch.float32 else torch.from_numpy(x).to(torch.bfloat16).float().numpy()
 
 
-@pytest.mark.parametrize("rows,c", [(1, 8), (3, 128), (130, 136), (257, 264), (1000, 40), (33, 1024), (700, 520)])
+@pytest.mark.parametrize("rows,c", [(1, 8), (3, 128), (130, 136), (257, 264), (1000, 40), (300, 32), (33, 1024), (700, 520)])
 @pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("block", [32, 16])
 @pytest.mark.parametrize("transpose", [False, True])
