@@ -51,6 +51,22 @@ template <bool F32> __device__ __forceinline__ void store8(void *base, int64_t o
     }
 }
 
+// the same in one store of 32 bytes where the address allows it: two of 16 bytes each write half of every sector that the warp touches
+template <bool F32> __device__ __forceinline__ void store8_whole(void *base, int64_t off, const float (&f)[8])
+{
+    if constexpr (F32) {
+        float *p = (float *)base + off;
+        if (((uintptr_t)p & 31) == 0) {
+            uint32_t u[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) u[i] = __float_as_uint(f[i]);
+            ptx::st_global_32B(p, u);
+            return;
+        }
+    }
+    store8<F32>(base, off, f);
+}
+
 // the same as four packed pairs
 template <bool F32> __device__ __forceinline__ void to_pairs(const Raw<F32> &r, ptx::f32x2 (&f)[4])
 {

@@ -156,7 +156,7 @@ dequant4_rows_kernel(const RowParams P)
         const float s = decode_scale<BLOCK>(byte[u], g);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = __fmul_rn(v[j], s);
-        store8<F32>(P.x, (at.row + u * Place::RPP) * P.pitch + at.ch, v);
+        store8_whole<F32>(P.x, (at.row + u * Place::RPP) * P.pitch + at.ch, v);
     }
 }
 

@@ -237,7 +237,7 @@ gn_apply_kernel(const GnParams P)
               [&](int i, const Raw<XF> &r) {
                   float z[8];
                   apply<XF, ZF, ACT>(P, f, r, z);
-                  store8<ZF>(P.out, o0 - i * out_step, z);
+                  store8_whole<ZF>(P.out, o0 - i * out_step, z);
               });
 }
 
@@ -376,7 +376,7 @@ gn_bwd_apply_kernel(const GnParams P)
               [&](int i, const Both<XF, ZF> &r) {
                   float o[8];
                   back_apply<XF, ZF, ACT>(P, f, k, r.x, r.z, o);
-                  store8<XF>(P.out, o0 - i * os, o);
+                  store8_whole<XF>(P.out, o0 - i * os, o);
               });
 }
 

@@ -145,7 +145,7 @@ gn_small_kernel(const SmallParams P)
     for (int u = 0; u < U; ++u) {
         if (u >= q.have) break;
         apply<XF, ZF, ACT>(P, f, r[u], zs);
-        store8<ZF>(P.out, to + u * out_line, zs);
+        store8_whole<ZF>(P.out, to + u * out_line, zs);
     }
 }
 
@@ -239,7 +239,7 @@ gn_small_bwd_kernel(const SmallParams P)
             if (u >= q.have) break;
             float o[8];
             back_apply<XF, ZF, ACT>(P, f, k, rx[u], rz[u], o);
-            store8<XF>(P.out, to + u * ol, o);
+            store8_whole<XF>(P.out, to + u * ol, o);
         }
     }
     if (P.cl > 1) cluster_wait();                                // no CTA leaves while a peer still reads its sums
