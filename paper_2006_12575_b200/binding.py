@@ -182,6 +182,10 @@ def _check(st, what):
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
 
+# the current device without torch.cuda's check that CUDA is up: whoever passes a CUDA tensor has brought it up
+_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 def _stream():
     return _raw_stream(torch.cuda.current_device())
 
@@ -656,7 +660,7 @@ def lamp_group_norm_workspace_bytes(p: GroupNorm, x):
 
 
 def lamp_group_norm_act_fwd(p: GroupNorm, x, z, mean_rstd, ws=None, stats=None):
-    dev = torch.cuda.current_device()
+    dev = _device()
     vx = _view(x, dev, "x")
     w, nbytes = _scratch(ws, dev)
     _check(lib().lamp_group_norm_act_fwd(_group_params(p, vx, dev), C.byref(vx), _vec(stats, 2 * vx.n * vx.c, "stats", dev, torch.float64),
@@ -665,7 +669,7 @@ def lamp_group_norm_act_fwd(p: GroupNorm, x, z, mean_rstd, ws=None, stats=None):
 
 
 def lamp_group_norm_act_bwd(p: GroupNorm, dz, x, mean_rstd, dx, dw=None, db=None, ws=None):
-    dev = torch.cuda.current_device()
+    dev = _device()
     vx = _view(x, dev, "x")
     w, nbytes = _scratch(ws, dev)
     _check(lib().lamp_group_norm_act_bwd(_group_params(p, vx, dev), _byref(_view(dz, dev, "dz")), C.byref(vx),
@@ -674,6 +678,9 @@ def lamp_group_norm_act_bwd(p: GroupNorm, dz, x, mean_rstd, dx, dw=None, db=None
 
 
 # --- 4-bit layers --------------------------------------------------------------------------------------------------
+_U8 = torch.uint8
+
+
 def lamp_fp4_scale_bytes(rows, k, block=32):
     return lib().lamp_fp4_scale_bytes(rows, k, block)
 
@@ -682,38 +689,37 @@ def fp4_operand(q, scale, rows=None, k=None, block=32, tensor_scale=None) -> Fp4
     """Operand [rows][k] of lamp_gemm_fp4: q uint8 [rows, pitch], two codes a byte; scale uint8, lamp_fp4_scale_bytes(rows, k, block) of them in
     their tiles; tensor_scale fp32 scalar on the device or None."""
     dev = q.get_device()
-    if q.dtype is not torch.uint8 or scale.dtype is not torch.uint8 or dev < 0 or scale.get_device() != dev or q.dim() != 2 or not scale.is_contiguous():
+    if q.dtype is not _U8 or scale.dtype is not _U8 or dev < 0 or scale.get_device() != dev or q.dim() != 2 or not scale.is_contiguous():
         raise ValueError("fp4_operand: q is a CUDA uint8 matrix, scale a contiguous uint8 tensor on the same device")
     (qr, qc), (qp, q1) = q.shape, q.stride()
     if rows is None:
         rows = qr
     if k is None:
         k = 2 * qc
-    if block not in (16, 32):
+    if block != 32 and block != 16:
         raise ValueError(f"fp4_operand: blocks of 16 or 32, got {block}")
-    need = (rows + 127) // 128 * (((k + block - 1) // block + 3) // 4) * 512
-    if rows < 0 or k < 0 or rows > qr or (k + 1) // 2 > qc or (q1 != 1 and qc > 1) or scale.numel() < need:
+    if rows < 0 or k < 0 or rows > qr or k > 2 * qc or (q1 != 1 and qc > 1) or scale.numel() < (rows + 127) // 128 * ((k + 4 * block - 1) // (4 * block)) * 512:
         raise ValueError(f"fp4_operand: [{rows}, {k}] in blocks of {block} does not fit q {tuple(q.shape)} and {scale.numel()} scales")
     # the stride of an axis of one element says nothing: the pitch only has to cover the row
     if qr <= 1:
         qp = (max(qp, qc) + 15) // 16 * 16
-    o = Fp4Operand(q.data_ptr(), qp, scale.data_ptr(), _vec(tensor_scale, 1, "tensor_scale", dev), rows, k, block)
+    o = Fp4Operand(q.data_ptr(), qp, scale.data_ptr(), None if tensor_scale is None else _vec(tensor_scale, 1, "tensor_scale", dev), rows, k, block)
     o.keep, o.dev = (q, scale, tensor_scale), dev
     return o
 
 
 def lamp_fp4_quantize(x, out: Fp4Operand, transpose=False):
-    dev = torch.cuda.current_device()
+    dev = _device()
     _check(lib().lamp_fp4_quantize(_byref(_view(x, dev, "x")), 1 if transpose else 0, _operand(out, dev, "out"), _raw_stream(dev)), "lamp_fp4_quantize")
 
 
 def lamp_fp4_dequantize(op: Fp4Operand, y, transpose=False):
-    dev = torch.cuda.current_device()
+    dev = _device()
     _check(lib().lamp_fp4_dequantize(_operand(op, dev, "op"), 1 if transpose else 0, _byref(_view(y, dev, "y")), _raw_stream(dev)), "lamp_fp4_dequantize")
 
 
 def lamp_gemm_fp4(a: Fp4Operand, b: Fp4Operand, y, bias=None):
-    dev = torch.cuda.current_device()
+    dev = _device()
     _check(lib().lamp_gemm_fp4(_operand(a, dev, "a"), _operand(b, dev, "b"), _vec(bias, b.rows, "bias", dev), _byref(_view(y, dev, "y")),
                                _raw_stream(dev)), "lamp_gemm_fp4")
 
@@ -755,14 +761,14 @@ def lamp_grad_norm_workspace_bytes(grads: GradList):
 
 
 def lamp_grad_norm(grads: GradList, max_norm, norm, factor=None, ws=None):
-    dev = torch.cuda.current_device()
+    dev = _device()
     w, nbytes = _scratch(ws, dev)
     _check(lib().lamp_grad_norm(_grads(grads, dev), grads.count, max_norm, _vec(norm, 1, "norm", dev), _vec(factor, 1, "factor", dev), w, nbytes,
                                 _raw_stream(dev)), "lamp_grad_norm")
 
 
 def lamp_grad_clip(grads: GradList, max_norm, norm, factor, ws=None):
-    dev = torch.cuda.current_device()
+    dev = _device()
     w, nbytes = _scratch(ws, dev)
     _check(lib().lamp_grad_clip(_grads(grads, dev), grads.count, max_norm, _vec(norm, 1, "norm", dev), _vec(factor, 1, "factor", dev), w, nbytes,
                                 _raw_stream(dev)), "lamp_grad_clip")
@@ -770,7 +776,7 @@ def lamp_grad_clip(grads: GradList, max_norm, norm, factor, ws=None):
 
 def lamp_rmsprop_step_scaled(grad, grad_scale, master, v, param_bf16=None, lr=1e-3, alpha=0.99, eps=1e-8):
     """lamp_rmsprop_step with the gradients times grad_scale (fp32 scalar on the device, as lamp_grad_norm leaves it in factor)."""
-    dev = torch.cuda.current_device()
+    dev = _device()
     n = grad.numel()
     _check(lib().lamp_rmsprop_step_scaled(n, _vec(grad, n, "grad", dev), _vec(grad_scale, 1, "grad_scale", dev), _vec(master, n, "master", dev),
                                           _vec(v, n, "v", dev), _vec(param_bf16, n, "param_bf16", dev, torch.bfloat16), lr, alpha, eps,

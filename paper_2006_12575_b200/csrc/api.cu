@@ -45,10 +45,12 @@ CUresult CUDAAPI encode_tiled_cached(CUtensorMap *out, CUtensorMapDataType dt, c
     k.l2 = (uint32_t)l2; k.oob = (uint32_t)oob;
     for (cuuint32_t i = 0; i < rank; ++i) { k.gdim[i] = gdim[i]; k.box[i] = box[i]; k.es[i] = es[i]; }
     for (cuuint32_t i = 0; i + 1 < rank; ++i) k.gstride[i] = gstride[i];
-    uint64_t h = 1469598103934665603ull;
-    const unsigned char *b = (const unsigned char *)&k;
-    for (size_t i = 0; i < sizeof(k); ++i) h = (h ^ b[i]) * 1099511628211ull;
-    MapEntry &e = g_map_cache[h % MAP_CACHE_SLOTS];
+    // eight bytes at a time (one by one they cost 0.2 us, four times in a call of the 4-bit product); the product's upper bits pick the slot
+    static_assert(sizeof(k) % 8 == 0, "");
+    uint64_t h = 1469598103934665603ull, word[sizeof(k) / 8];
+    memcpy(word, &k, sizeof(k));
+    for (uint64_t w : word) { h = (h ^ w) * 1099511628211ull; h ^= h >> 29; }
+    MapEntry &e = g_map_cache[(h >> 20) % MAP_CACHE_SLOTS];
     {
         std::lock_guard<std::mutex> lock(g_map_mutex);
         if (e.valid && memcmp(&e.key, &k, sizeof(k)) == 0) { *out = e.map; return CUDA_SUCCESS; }

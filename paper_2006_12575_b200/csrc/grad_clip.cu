@@ -16,22 +16,31 @@ namespace {
 using namespace bn;
 
 constexpr int CT = 256, UNITS = 8;              // threads, 16-byte units of a piece per thread: neighbouring lanes take neighbouring units
-__host__ __device__ constexpr int piece_of(bool f32) { return CT * UNITS * (f32 ? 4 : 8); }                    // elements
+// Elements of a piece that T threads take: a CTA's 32 KB, or a warp's 4 KB where all of the gradients are few
+template <int T> __host__ __device__ constexpr int piece_of(bool f32) { return T * UNITS * (f32 ? 4 : 8); }
 constexpr int CTAS = 4;                       // per SM: all of them resident, so that the sum over the parts is formed once per place
 
 struct Entry {
     const void *g;
     void *out;
     int64_t n;
-    int32_t first;                            // pieces of the tensors in front of it
-    int32_t f32;
+    int64_t f32;
 };
+// Every line of the parameters that a kernel touches is a miss at first, 0.5 us each in turn: the search runs over an array of its own, and where
+// the pieces are few a piece has its tensor written beside it.
 template <int N> struct Table {
     int32_t count, pieces;
+    int32_t first[N];                         // pieces of the tensors in front of it
     Entry e[N];
 };
-constexpr int SMALL = 120, LARGE = 1000;      // parameters of 4 KB and of just under 32 KB
-static_assert(sizeof(Table<LARGE>) + 64 <= 32764, "kernel parameters");
+constexpr int SMALL = 110, LARGE = 900;       // parameters of 4 KB and of just under 32 KB
+constexpr int CLUSTER = 8, FEW = 2 * CLUSTER * (CT / 32);          // pieces of a warp each: two per warp of a cluster
+struct FewTable {
+    int32_t pieces;
+    uint8_t owner[FEW], index[FEW];           // of each piece: its tensor, its number there
+    Entry e[SMALL];
+};
+static_assert(sizeof(Table<LARGE>) + 64 <= 32764 && sizeof(Table<SMALL>) <= 4040 && sizeof(FewTable) <= 4040 && FEW <= 255, "kernel parameters");
 
 // elements in front of the first 128-byte boundary: a warp's 512 bytes are then whole lines
 __host__ __device__ __forceinline__ int64_t head_of(const void *p, int64_t n, bool f32)
@@ -39,32 +48,37 @@ __host__ __device__ __forceinline__ int64_t head_of(const void *p, int64_t n, bo
     const int64_t h = (int64_t)((128 - ((uintptr_t)p & 127)) & 127) / (f32 ? 4 : 2);
     return h < n ? h : n;
 }
-__host__ __forceinline__ int64_t pieces_of(const lamp_grad_t &t)
+template <int T> __host__ __forceinline__ int64_t pieces_of(const lamp_grad_t &t)
 {
     if (t.n == 0) return 0;
     const bool f32 = t.dtype == LAMP_F32;
-    const int64_t body = t.n - head_of(t.g, t.n, f32), piece = piece_of(f32);
+    const int64_t body = t.n - head_of(t.g, t.n, f32), piece = piece_of<T>(f32);
     return body == 0 ? 1 : (body + piece - 1) / piece;
 }
 
-// The pieces blockIdx.x, blockIdx.x + gridDim.x, .. of the tensors, forwards or BACK: f(entry, first element of the body of the piece, its end,
-// elements of the head).
-template <bool BACK, int N, typename F>
-__device__ __forceinline__ void for_pieces(const Table<N> &T, F f)
+// Piece `index` of W threads of a tensor: f(entry, first element of its body, its end, elements of the head)
+template <int W, typename F> __device__ __forceinline__ void piece(const Entry &e, int index, F f)
 {
-    const int step = gridDim.x, turns = (T.pieces - (int)blockIdx.x + step - 1) / step;             // at least one: no more CTAs than pieces
-    int p = blockIdx.x + (BACK ? turns - 1 : 0) * step;
+    const int64_t h = head_of(e.g, e.n, e.f32), b0 = h + (int64_t)index * piece_of<W>(e.f32), b1 = b0 + piece_of<W>(e.f32);
+    f(e, b0, b1 < e.n ? b1 : e.n, index == 0 ? h : 0);
+}
+
+// The pieces `me`, me + step, .. of the tensors, forwards or BACK
+template <int W, bool BACK, int N, typename F>
+__device__ __forceinline__ void for_pieces(const Table<N> &T, int me, int step, F f)
+{
+    if (me >= T.pieces) return;
+    const int turns = (T.pieces - me + step - 1) / step;
+    int p = me + (BACK ? turns - 1 : 0) * step;
     int lo = 0, hi = T.count - 1;             // the entry of piece p: the last that begins at it or before it
     while (lo < hi) {
         const int mid = (lo + hi + 1) / 2;
-        if (T.e[mid].first <= p) lo = mid; else hi = mid - 1;
+        if (T.first[mid] <= p) lo = mid; else hi = mid - 1;
     }
     for (int t = 0; t < turns; ++t, p += BACK ? -step : step) {
-        if (BACK) while (T.e[lo].first > p) --lo;
-        else while (lo + 1 < T.count && T.e[lo + 1].first <= p) ++lo;
-        const Entry &e = T.e[lo];
-        const int64_t h = head_of(e.g, e.n, e.f32), b0 = h + (int64_t)(p - e.first) * piece_of(e.f32), b1 = b0 + piece_of(e.f32);
-        f(e, b0, b1 < e.n ? b1 : e.n, p == e.first ? h : 0);
+        if (BACK) while (T.first[lo] > p) --lo;
+        else while (lo + 1 < T.count && T.first[lo + 1] <= p) ++lo;
+        piece<W>(T.e[lo], p - T.first[lo], f);
     }
 }
 
@@ -81,6 +95,13 @@ template <bool F32> __device__ __forceinline__ void unit_pairs(const uint4 &u, p
         for (int i = 0; i < 4; ++i) v[i] = ptx::pack2(w[i] << 16, w[i] & 0xFFFF0000u);
     }
 }
+template <int N> __device__ __forceinline__ bool nonzero(const uint4 (&r)[N])
+{
+    uint32_t any = 0;
+#pragma unroll
+    for (int n = 0; n < N; ++n) any |= r[n].x | r[n].y | r[n].z | r[n].w;
+    return any != 0;
+}
 // N units = 8 values
 template <bool F32, int N> __device__ __forceinline__ void add_squares(const uint4 (&r)[N], double &acc)
 {
@@ -96,7 +117,7 @@ template <bool F32, int N> __device__ __forceinline__ void add_squares(const uin
     const float s = both(sum);
     if (s >= 8.6736174e-19f && s <= 1.3292279957849159e36f) {        // 2^-60 .. 2^120: what underflowed is nothing beside s
         acc += (double)s;
-    } else {
+    } else if (nonzero<N>(r)) {
 #pragma unroll
         for (int n = 0; n < N; ++n)
 #pragma unroll
@@ -110,30 +131,30 @@ template <bool F32, int N> __device__ __forceinline__ void add_squares(const uin
 }
 
 // The units of a piece: all of them loaded, the ones that the tensor's end cuts left zero.  f(first element) for the elements of a cut unit.
-template <bool F32, typename Tail>
+template <int W, bool F32, typename Tail>
 __device__ __forceinline__ void load_piece(const void *g, int64_t b0, int64_t b1, uint4 (&r)[UNITS], Tail tail)
 {
     constexpr int E = F32 ? 4 : 8;
-    const uint4 *p = (const uint4 *)((const char *)g + b0 * (F32 ? 4 : 2)) + threadIdx.x;
-    if (b1 - b0 == piece_of(F32)) {
+    const uint4 *p = (const uint4 *)((const char *)g + b0 * (F32 ? 4 : 2)) + threadIdx.x % W;
+    if (b1 - b0 == piece_of<W>(F32)) {
 #pragma unroll
-        for (int u = 0; u < UNITS; ++u) r[u] = p[u * CT];
+        for (int u = 0; u < UNITS; ++u) r[u] = p[u * W];
         return;
     }
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
-        const int64_t at = b0 + (int64_t)(u * CT + threadIdx.x) * E;
+        const int64_t at = b0 + (int64_t)(u * W + threadIdx.x % W) * E;
         r[u] = make_uint4(0, 0, 0, 0);
-        if (at + E <= b1) r[u] = p[u * CT];
+        if (at + E <= b1) r[u] = p[u * W];
         else for (int64_t i = at; i < b1; ++i) tail(i);
     }
 }
 
-template <bool F32> __device__ __forceinline__ void piece_squares(const void *g, int64_t b0, int64_t b1, double &acc)
+template <int W, bool F32> __device__ __forceinline__ void piece_squares(const void *g, int64_t b0, int64_t b1, double &acc)
 {
     constexpr int N = F32 ? 2 : 1;
     uint4 r[UNITS];
-    load_piece<F32>(g, b0, b1, r, [&](int64_t i) { const double v = element(g, i, F32); acc = fma(v, v, acc); });
+    load_piece<W, F32>(g, b0, b1, r, [&](int64_t i) { const double v = element(g, i, F32); acc = fma(v, v, acc); });
 #pragma unroll
     for (int u = 0; u < UNITS; u += N) {
         uint4 e[N];
@@ -143,6 +164,13 @@ template <bool F32> __device__ __forceinline__ void piece_squares(const void *g,
     }
 }
 
+// the head of a tensor and a piece of it
+template <int W> __device__ __forceinline__ void add_piece(const Entry &e, int64_t b0, int64_t b1, int64_t h, double &acc)
+{
+    for (int64_t i = threadIdx.x % W; i < h; i += W) { const double v = element(e.g, i, e.f32); acc = fma(v, v, acc); }
+    if (e.f32) piece_squares<W, true>(e.g, b0, b1, acc);
+    else piece_squares<W, false>(e.g, b0, b1, acc);
+}
 // Sum over the CTA, in every thread; fixed order.
 __device__ __forceinline__ double block_sum(double v, double *red)
 {
@@ -163,11 +191,7 @@ grad_norm_parts_kernel(const __grid_constant__ Table<N> T, double *__restrict__ 
     pdl_launch_dependents();
     pdl_wait();
     double acc = 0.0;
-    for_pieces<false>(T, [&](const Entry &e, int64_t b0, int64_t b1, int64_t h) {
-        if (threadIdx.x < h) { const double v = element(e.g, threadIdx.x, e.f32); acc = fma(v, v, acc); }
-        if (e.f32) piece_squares<true>(e.g, b0, b1, acc);
-        else piece_squares<false>(e.g, b0, b1, acc);
-    });
+    for_pieces<CT, false>(T, blockIdx.x, gridDim.x, [&](const Entry &e, int64_t b0, int64_t b1, int64_t h) { add_piece<CT>(e, b0, b1, h, acc); });
     acc = block_sum(acc, red);
     if (threadIdx.x == 0) part[blockIdx.x] = acc;
 }
@@ -201,16 +225,16 @@ template <bool F32> __device__ __forceinline__ void scale_element(const Entry &e
     else ((bf16 *)e.out)[i] = f2bf(bf2f(((const bf16 *)e.g)[i]) * f);
 }
 
-template <bool F32> __device__ __forceinline__ void piece_scale(const Entry &e, int64_t b0, int64_t b1, float f)
+template <int W, bool F32> __device__ __forceinline__ void piece_scale(const Entry &e, int64_t b0, int64_t b1, float f)
 {
     if (((uintptr_t)e.out ^ (uintptr_t)e.g) & 15) {                   // the two cannot both be on 16-byte boundaries: an element per lane
-        for (int64_t i = b0 + threadIdx.x; i < b1; i += CT) scale_element<F32>(e, i, f);
+        for (int64_t i = b0 + threadIdx.x % W; i < b1; i += W) scale_element<F32>(e, i, f);
         return;
     }
     constexpr int E = F32 ? 4 : 8, PAIRS = F32 ? 2 : 4;
     uint4 r[UNITS];
-    load_piece<F32>(e.g, b0, b1, r, [&](int64_t i) { scale_element<F32>(e, i, f); });
-    uint4 *o = (uint4 *)((char *)e.out + b0 * (F32 ? 4 : 2)) + threadIdx.x;
+    load_piece<W, F32>(e.g, b0, b1, r, [&](int64_t i) { scale_element<F32>(e, i, f); });
+    uint4 *o = (uint4 *)((char *)e.out + b0 * (F32 ? 4 : 2)) + threadIdx.x % W;
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
         ptx::f32x2 v[PAIRS];
@@ -221,8 +245,19 @@ template <bool F32> __device__ __forceinline__ void piece_scale(const Entry &e, 
         uint4 w;
         if constexpr (F32) w = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
         else w = pack8(x);
-        if (b1 - b0 == piece_of(F32) || b0 + (int64_t)(u * CT + threadIdx.x + 1) * E <= b1) __stcs(o + u * CT, w);
+        if (b1 - b0 == piece_of<W>(F32) || b0 + (int64_t)(u * W + threadIdx.x % W + 1) * E <= b1) __stcs(o + u * W, w);
     }
+}
+
+template <int W> __device__ __forceinline__ void scale_piece(const Entry &e, int64_t b0, int64_t b1, int64_t h, float f)
+{
+    if (f == 1.f && e.out == e.g) return;
+    for (int64_t i = threadIdx.x % W; i < h; i += W) {
+        if (e.f32) scale_element<true>(e, i, f);
+        else scale_element<false>(e, i, f);
+    }
+    if (e.f32) piece_scale<W, true>(e, b0, b1, f);
+    else piece_scale<W, false>(e, b0, b1, f);
 }
 
 template <int N>
@@ -238,15 +273,44 @@ grad_scale_kernel(const __grid_constant__ Table<N> T, const double *part, int pa
         *norm = v;
         *factor = f;
     }
-    for_pieces<true>(T, [&](const Entry &e, int64_t b0, int64_t b1, int64_t h) {
-        if (f == 1.f && e.out == e.g) return;
-        if (threadIdx.x < h) {
-            if (e.f32) scale_element<true>(e, threadIdx.x, f);
-            else scale_element<false>(e, threadIdx.x, f);
-        }
-        if (e.f32) piece_scale<true>(e, b0, b1, f);
-        else piece_scale<false>(e, b0, b1, f);
-    });
+    for_pieces<CT, true>(T, blockIdx.x, gridDim.x, [&](const Entry &e, int64_t b0, int64_t b1, int64_t h) { scale_piece<CT>(e, b0, b1, h, f); });
+}
+
+// All of it in one launch where the gradients are few: a cluster, a piece per warp, the CTAs' sums over distributed shared memory in rank order.
+// (62 vectors of 512: two launches took 6.9 us and 9.4 a call, this 6.7 and 6.8.)
+__global__ void __launch_bounds__(CT)
+grad_clip_small_kernel(const __grid_constant__ FewTable T, float max_norm, float *norm, float *factor, int scale)
+{
+    __shared__ double red[CT / 32], mine;
+    pdl_launch_dependents();
+    pdl_wait();
+    uint32_t rank;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    const int me = rank * (CT / 32) + (threadIdx.x >> 5), all = CLUSTER * (CT / 32);
+    double acc = 0.0;
+    for (int p = me; p < T.pieces; p += all)
+        piece<32>(T.e[T.owner[p]], T.index[p], [&](const Entry &e, int64_t b0, int64_t b1, int64_t h) { add_piece<32>(e, b0, b1, h, acc); });
+    acc = block_sum(acc, red);
+    if (threadIdx.x == 0) mine = acc;
+    asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
+    double sum = 0.0;
+    for (uint32_t i = 0; i < CLUSTER; ++i) {
+        uint32_t a;
+        double v;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(ptx::smem_u32(&mine)), "r"(i));
+        asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(a) : "memory");
+        sum += v;
+    }
+    asm volatile("barrier.cluster.arrive.release;" ::: "memory");    // this CTA has read its peers' sums; waited for at the end
+    const float v = (float)sqrt(sum), f = v <= max_norm ? 1.f : max_norm / v;
+    if (rank == 0 && threadIdx.x == 0) {
+        *norm = v;
+        if (factor) *factor = f;
+    }
+    if (scale)
+        for (int p = me; p < T.pieces; p += all)
+            piece<32>(T.e[T.owner[p]], T.index[p], [&](const Entry &e, int64_t b0, int64_t b1, int64_t h) { scale_piece<32>(e, b0, b1, h, f); });
+    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
 }
 
 // ----------------------------------------------------------------------------------------------------------- host
@@ -277,9 +341,10 @@ int32_t fill(Table<N> &T, const lamp_grad_t *grads, int32_t count, int32_t i)
 {
     T.count = T.pieces = 0;
     for (; i < count && T.count < N; ++i) {
-        const int64_t p = pieces_of(grads[i]);
+        const int64_t p = pieces_of<CT>(grads[i]);
         if (p == 0) continue;
-        T.e[T.count++] = Entry{grads[i].g, grads[i].out, grads[i].n, T.pieces, grads[i].dtype == LAMP_F32};
+        T.first[T.count] = T.pieces;
+        T.e[T.count++] = Entry{grads[i].g, grads[i].out, grads[i].n, grads[i].dtype == LAMP_F32};
         T.pieces += (int32_t)p;
     }
     return i;
@@ -311,6 +376,36 @@ lamp_status_t run(const lamp_grad_t *grads, int32_t count, float max_norm, float
     return LAMP_OK;
 }
 
+// Whether all of the gradients are FEW pieces of a warp (512 KB) at most, and the table of them.
+bool fill_few(FewTable &T, const lamp_grad_t *grads, int32_t count)
+{
+    if (count > SMALL) return false;
+    T.pieces = 0;
+    for (int32_t i = 0; i < count; ++i) {
+        const int64_t p = pieces_of<32>(grads[i]);
+        if (T.pieces + p > FEW) return false;
+        for (int64_t k = 0; k < p; ++k) { T.owner[T.pieces] = (uint8_t)i; T.index[T.pieces++] = (uint8_t)k; }
+        T.e[i] = Entry{grads[i].g, grads[i].out, grads[i].n, grads[i].dtype == LAMP_F32};
+    }
+    return T.pieces > 0;
+}
+lamp_status_t run_few(const FewTable &T, float max_norm, float *norm, float *factor, bool scale, cudaStream_t st)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(CLUSTER);
+    cfg.blockDim = dim3(CT);
+    cfg.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = CLUSTER;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, grad_clip_small_kernel, T, max_norm, norm, factor, scale ? 1 : 0) == cudaSuccess ? LAMP_OK : LAMP_ERR_CUDA;
+}
+
 size_t workspace(int32_t count)
 {
     const size_t tables = count <= SMALL ? 1 : (size_t)(count + LARGE - 1) / LARGE;
@@ -324,6 +419,8 @@ lamp_status_t clip(const lamp_grad_t *grads, int32_t count, float max_norm, floa
     if (!norm || ((uintptr_t)norm & 3) || (scale && !factor) || ((uintptr_t)factor & 3) || !(max_norm >= 0.f)) return LAMP_ERR_INVALID_ARG;
     if (!ws || ((uintptr_t)ws & 15) || ws_bytes < lamp_grad_norm_workspace_bytes(grads, count)) return LAMP_ERR_WORKSPACE;
     cudaStream_t st = (cudaStream_t)stream;
+    FewTable T;
+    if (fill_few(T, grads, count)) return run_few(T, max_norm, norm, factor, scale, st);
     return count <= SMALL ? run<SMALL>(grads, count, max_norm, norm, factor, scale, (double *)ws, st)
                           : run<LARGE>(grads, count, max_norm, norm, factor, scale, (double *)ws, st);
 }
