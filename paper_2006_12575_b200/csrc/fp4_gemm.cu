@@ -115,7 +115,8 @@ template <int BN, int BLOCK> struct GemmLayout {
     static constexpr int THREADS = (2 + NEPI) * 32;
     static constexpr int SF0 = NACC * BN, SFC = 2 * Kind<BLOCK>::COLS;
     static constexpr int TMEM_COLS = 512;
-    static constexpr int OUT_BYTES = NEPI * STAGE_FLOATS * 4;
+    static constexpr int STAGE_WORDS = BN == 128 ? BOX_WORDS : STAGE_FLOATS;
+    static constexpr int OUT_BYTES = NEPI * STAGE_WORDS * 4;
     static constexpr int BAR_BYTES = (2 * MAX_STAGES + 2 * NACC) * 8 + 16;
     static constexpr int TOTAL = 1024 + STAGES * STAGE_BYTES + OUT_BYTES + BAR_BYTES;
     static_assert(BN * 128 * 4 <= STAGES * STAGE_BYTES, "the split-k parts reuse the stages");
@@ -213,7 +214,7 @@ fp4_gemm_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constant
     } else {
         // ------------------------------------------------------------------ epilogue
         const int q = warp & 3, half = (warp - 2) >> 2;                    // lane quarter and column part of this warp
-        float *stage = out_stage + (warp - 2) * STAGE_FLOATS;
+        float *stage = out_stage + (warp - 2) * L::STAGE_WORDS;
         const int lane_row = q * 32 + lane;
         const float alpha = (P.ga ? __ldg(P.ga) : 1.f) * (P.gb ? __ldg(P.gb) : 1.f);
         uint32_t acc = 0, acc_phase = 0;
@@ -224,6 +225,33 @@ fp4_gemm_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constant
             const int64_t row = (tile / P.nc) * 128 + lane_row;
             const int cbase = (int)(tile % P.nc) * BN + half * CW;
             const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + acc * BN + half * CW;
+            if constexpr (ODD && BN == 128) {
+                if (S == 1) {                                              // rows that start anywhere: 128 bytes of each at a time
+                    uint32_t all[4][16], w[32];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) tmem_ld_x16(taddr + c * 16, all[c]);
+                    tmem_ld_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(tempty0 + 8 * acc);
+                    if (++acc == NACC) { acc = 0; acc_phase ^= 1; }
+                    const int64_t row0 = row - lane;
+                    if (row0 >= P.rows_l) continue;
+                    scale_bias<4>(P, all, alpha, cbase);
+                    if (P.y_f32) {
+#pragma unroll
+                        for (int b = 0; b < 2; ++b) {
+                            if (cbase + b * 32 >= P.rows_c) break;
+                            box_words<true, 4>(all, b, w);
+                            store_box_odd(P, w, row0, cbase + b * 32, (uint32_t *)stage, lane);
+                        }
+                    } else if (cbase < P.rows_c) {
+                        box_words<false, 4>(all, 0, w);
+                        store_box_odd(P, w, row0, cbase, (uint32_t *)stage, lane);
+                    }
+                    continue;
+                }
+            }
             uint32_t r[2][16];
             tmem_ld_x16(taddr, r[0]);
 #pragma unroll
@@ -258,7 +286,7 @@ fp4_gemm_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constant
         cluster_sync_all();
         if (warp >= 2) {
             const int q = warp & 3, half = (warp - 2) >> 2, lane_row = q * 32 + lane;
-            float *stage = out_stage + (warp - 2) * STAGE_FLOATS;
+            float *stage = out_stage + (warp - 2) * L::STAGE_WORDS;
             const int64_t row = (tile0 / P.nc) * 128 + lane_row;
             const int col0 = (int)(tile0 % P.nc) * BN;
             const uint32_t base = smem_u32(smem);
@@ -291,10 +319,10 @@ template <int BN, int BLOCK> struct PairLayout {
     static constexpr int CW = BN / 2;                             // columns per epilogue warp
     static constexpr int THREADS = 384, TMEM_COLS = 512;
     static constexpr int SF0 = NACC * BN, SFC = (1 + CT) * Kind<BLOCK>::COLS;
-    static constexpr int OUT_BYTES = 8 * 4096;                    // per epilogue warp 32 rows x 128 bytes
+    static constexpr int OUT_BYTES = 8 * BOX_WORDS * 4;           // per epilogue warp 32 rows x 128 bytes, or those with a pitch of 33 words
     static constexpr int BAR_BYTES = (2 * MAX_STAGES + 2 * NACC) * 8 + 16;
     static constexpr int TOTAL = 1024 + STAGES * STAGE_BYTES + OUT_BYTES + BAR_BYTES;
-    static_assert(STAGE_BYTES % 1024 == 0 && STAGE_FLOATS * 4 <= 4096, "128-byte swizzle");
+    static_assert(STAGE_BYTES % 1024 == 0 && OUT_BYTES >= 8 * 4096, "128-byte swizzle");
     static_assert(SF0 + STAGES * SFC <= TMEM_COLS, "");
     static_assert(TOTAL <= 227 * 1024 && STAGES <= MAX_STAGES, "");
 };
@@ -418,7 +446,8 @@ fp4_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
         // ------------------------------------------------------------------ epilogue
         const int q = warp & 3, half = (warp - 4) >> 2;
         const int lane_row = q * 32 + lane;
-        float *stage = out_stage + (warp - 4) * 1024;
+        uint32_t *odd_stage = (uint32_t *)out_stage + (warp - 4) * BOX_WORDS;
+        const uint32_t box_stage = smem_u32(out_stage) + (warp - 4) * 4096;        // 1024-byte boundaries, as the swizzle wants
         uint32_t acc = 0, acc_phase = 0;
         const uint32_t tempty_leader = map_to_rank(tempty0, 0);
         const float alpha = (P.ga ? __ldg(P.ga) : 1.f) * (P.gb ? __ldg(P.gb) : 1.f);
@@ -436,46 +465,27 @@ fp4_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(tempty_leader + 8 * acc);
-            if constexpr (ODD) {
+            const int row0 = (int)(row - lane);
+            if (row0 < P.rows_l) {
+                scale_bias<CW / 16>(P, r, alpha, cbase);
+                auto store = [&](const uint32_t (&w)[32], int col) {
+                    if constexpr (ODD) store_box_odd(P, w, row0, col, odd_stage, lane);
+                    else store_box(&map_y, box_stage, w, col, row0, lane);
+                };
+                uint32_t w[32];
+                if (P.y_f32) {
 #pragma unroll
-                for (int c = 0; c < CW / 16; ++c) {
-                    float v[16];
+                    for (int b = 0; b < CW / 32; ++b) {
+                        if (cbase + b * 32 >= P.rows_c) break;
+                        box_words<true, CW / 16>(r, b, w);
+                        store(w, cbase + b * 32);
+                    }
+                } else {
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) v[j] = __uint_as_float(r[c][j]) * alpha;
-                    finish<true, 16>(P, row, cbase + c * 16, v, stage);
-                }
-            } else {
-                const int row0 = (int)(row - lane);
-                const uint32_t buf = smem_u32(stage);
-                if (row0 < P.rows_l) {
-#pragma unroll
-                    for (int c = 0; c < CW / 16; ++c)
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) {
-                            const int col = cbase + c * 16 + j;
-                            r[c][j] = __float_as_uint(__uint_as_float(r[c][j]) * alpha + (P.bias && col < P.rows_c ? __ldg(P.bias + col) : 0.f));
-                        }
-                    if (P.y_f32) {
-#pragma unroll
-                        for (int b = 0; b < CW / 32; ++b) {
-                            if (cbase + b * 32 >= P.rows_c) break;
-                            uint32_t w[32];
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) w[j] = r[2 * b + j / 16][j % 16];
-                            store_box(&map_y, buf, w, cbase + b * 32, row0, lane);
-                        }
-                    } else {
-#pragma unroll
-                        for (int b = 0; b < CW / 64; ++b) {
-                            if (cbase + b * 64 >= P.rows_c) break;
-                            uint32_t w[32];
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) {
-                                const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(r[4 * b + j / 8][2 * j % 16]), __uint_as_float(r[4 * b + j / 8][2 * j % 16 + 1]));
-                                w[j] = *reinterpret_cast<const uint32_t *>(&h);
-                            }
-                            store_box(&map_y, buf, w, cbase + b * 64, row0, lane);
-                        }
+                    for (int b = 0; b < CW / 64; ++b) {
+                        if (cbase + b * 64 >= P.rows_c) break;
+                        box_words<false, CW / 16>(r, b, w);
+                        store(w, cbase + b * 64);
                     }
                 }
             }

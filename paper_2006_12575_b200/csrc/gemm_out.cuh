@@ -163,6 +163,94 @@ __device__ __forceinline__ void finish(const OutParams &P, int64_t row, int col,
     __syncwarp();
 }
 
+// 32 rows x 128 bytes of y (lane = row, `w` its words: 32 columns of fp32 or 64 of bf16) to rows that start anywhere, through `stage`, BOX_WORDS words of
+// the warp: a row at a time, a word per lane, so that 128 bytes in a row leave together (16 columns of two rows at a time, as finish() does it,
+// wrote most sectors in two pieces: 16384 x 4095 bf16, k = 512 took 122 us, this 81; 28 with aligned rows - the sectors that two stores share cost).  bf16 rows that start between two words are shifted by one
+// element.  Every lane takes part.
+constexpr int BOX_WORDS = 32 * 33;
+__device__ __forceinline__ void store_box_odd(const OutParams &P, const uint32_t (&w)[32], int64_t row0, int col, uint32_t *stage, int lane)
+{
+#pragma unroll
+    for (int j = 0; j < 32; ++j) stage[lane * 33 + j] = w[j];
+    __syncwarp();
+    const int rows = P.rows_l - row0 < 32 ? (int)(P.rows_l - row0) : 32, left = P.rows_c - col;      // rows and columns that exist
+    if (P.y_f32) {
+        float *o = (float *)P.y + row0 * P.y_pitch + col + lane;
+        if (left >= 32 && rows == 32) {
+            float v[32];                                           // all of them first: the compiler does not move a load past a store
+#pragma unroll
+            for (int r = 0; r < 32; ++r) v[r] = __uint_as_float(stage[r * 33 + lane]);
+#pragma unroll
+            for (int r = 0; r < 32; ++r, o += P.y_pitch) *o = v[r];
+        } else if (lane < left) {
+            for (int r = 0; r < rows; ++r, o += P.y_pitch) *o = __uint_as_float(stage[r * 33 + lane]);
+        }
+    } else {
+        // every second row starts alike
+        for (int p = 0; p < 2; ++p) {
+            bf16 *o = (bf16 *)P.y + (row0 + p) * P.y_pitch + col;
+            const uint32_t *s = stage + p * 33 + lane;
+            const bool between = (uintptr_t)o & 2;
+            const int64_t step = 2 * P.y_pitch;
+            if (left >= 64 && rows == 32) {
+                uint32_t v[16];                                    // all of them first: the compiler does not move a load past a store
+#pragma unroll
+                for (int r = 0; r < 16; ++r) v[r] = s[r * 66];
+                if (!between) {
+                    o += 2 * lane;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r, o += step) *reinterpret_cast<uint32_t *>(o) = v[r];
+                } else {
+                    // lane l has elements 2 l + 1 and 2 l + 2; the first and the last one go by themselves
+                    bf16 *e = o + (lane == 0 ? 0 : 63);
+                    const bool edge = lane == 0 || lane == 31;
+                    const int next = lane < 31 ? 1 : 0;
+                    o += 2 * lane + 1;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r, o += step, e += step) {
+                        if (lane < 31) *reinterpret_cast<uint32_t *>(o) = __byte_perm(v[r], s[r * 66 + next], 0x5432);
+                        if (edge) *reinterpret_cast<uint16_t *>(e) = (uint16_t)(lane == 0 ? v[r] : v[r] >> 16);
+                    }
+                }
+            } else {
+                const int e = 2 * lane + (between ? 1 : 0);        // first element of this lane's word
+                for (int r = p; r < rows; r += 2, o += step, s += 66) {
+                    const uint32_t a = s[0], b = between && lane < 31 ? s[1] : 0u, v = between ? __byte_perm(a, b, 0x5432) : a;
+                    if (e + 1 < left && e + 1 < 64) *reinterpret_cast<uint32_t *>(o + e) = v;
+                    else if (e < left) *reinterpret_cast<uint16_t *>(o + e) = (uint16_t)v;
+                    if (between && lane == 0) *reinterpret_cast<uint16_t *>(o) = (uint16_t)a;
+                }
+            }
+        }
+    }
+    __syncwarp();
+}
+// alpha * (16 * N accumulator columns) + bias, and the words of 128 bytes of a row from them
+template <int N> __device__ __forceinline__ void scale_bias(const OutParams &P, uint32_t (&r)[N][16], float alpha, int col0)
+{
+#pragma unroll
+    for (int c = 0; c < N; ++c)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) r[c][j] = __float_as_uint(__uint_as_float(r[c][j]) * alpha);
+    if (!P.bias) return;
+    const int last = P.rows_c - 1;
+#pragma unroll
+    for (int c = 0; c < N; ++c)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) r[c][j] = __float_as_uint(__uint_as_float(r[c][j]) + __ldg(P.bias + min(col0 + c * 16 + j, last)));      // columns behind the last are not stored
+}
+template <bool F32, int N> __device__ __forceinline__ void box_words(const uint32_t (&r)[N][16], int b, uint32_t (&w)[32])
+{
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+        if constexpr (F32) w[j] = r[2 * b + j / 16][j % 16];
+        else {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(r[4 * b + j / 8][2 * j % 16]), __uint_as_float(r[4 * b + j / 8][2 * j % 16 + 1]));
+            w[j] = *reinterpret_cast<const uint32_t *>(&h);
+        }
+    }
+}
+
 // Sum over the S parts of a tile (in CTAs first, first + stride, ... of the cluster) of the `mine`-th CW / S columns of this
 // thread's lane row, and their store.
 template <bool ODD, int CW, int S>
