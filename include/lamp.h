@@ -268,7 +268,7 @@ lamp_status_t lamp_gemm_fp8(const lamp_fp8_operand_t *a, const lamp_fp8_operand_
  *   element (r, j) = code(r, j) * scale(r, j / block) * g
  *   code: e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6; bit 3 = sign), two in a byte: q[r * q_pitch + j / 2], even j in the low half;
  *   block = 32: scale e8m0, 2^(byte - 127), byte 255 = NaN; tensor_scale must be NULL (g = 1);
- *   block = 16: scale e4m3 (sign 0; 0x7F = NaN); g = *tensor_scale (fp32 on the device), or 1 (NULL).
+ *   block = 16: scale e4m3 (sign 0; 0x7F = NaN); g = *tensor_scale (fp32 on the device, > 0), or 1 (NULL).
  *   The scale of (r, i) is the byte ((r / 128) * ceil(kb / 4) + i / 4) * 512 + (r % 32) * 16 + (r % 128) / 32 * 4 + i % 4 with kb = ceil(k / block):
  *   tiles of 128 rows x 4 blocks in the order in which tensor memory takes them; lamp_fp4_scale_bytes in all.
  * q and scale 16-byte aligned, q_pitch (bytes) a multiple of 16 and >= ceil(k / 2).  Bytes behind ceil(k / 2) are neither read nor
@@ -579,7 +579,7 @@ lamp_status_t lamp_rmsprop_step_scaled(int64_t n, const float *grad, const float
  * ---------------------------------------------------------------------- */
 typedef struct {
     const void *g;                        /* n elements, contiguous; aligned to an element */
-    void       *out;                      /* g itself, or n elements that overlap no tensor of the list; not read by lamp_grad_norm */
+    void       *out;                      /* g itself, or n elements; overlaps nothing else of the list.  lamp_grad_norm does not use it */
     int64_t     n;                        /* 0 .. 2^40 */
     int32_t     dtype;                    /* of both */
 } lamp_grad_t;

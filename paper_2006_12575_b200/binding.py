@@ -739,6 +739,22 @@ class GradList:
             if o is not g and (o.dtype is not g.dtype or o.numel() != g.numel() or not o.is_contiguous() or o.get_device() != self.dev):
                 raise ValueError(f"grad_list: output {i}: want a contiguous {g.dtype} tensor of {g.numel()} elements on {g.device}, got {tuple(o.shape)} {o.dtype} on {o.device}")
             self.array[i] = Grad(g.data_ptr(), o.data_ptr(), g.numel(), dt)
+        # what is written must not be part of anything else: sorted by address, each range against the furthest one in front of it
+        ranges = []
+        for i, (g, o) in enumerate(zip(tensors, outs)):
+            if g.numel():
+                size = g.numel() * g.element_size()
+                a, b = g.data_ptr(), o.data_ptr()
+                ranges.append((a, a + size, a == b, i))
+                if a != b:
+                    ranges.append((b, b + size, True, i))
+        end, written_end = 0, 0                                       # of all ranges so far, of the written ones
+        for a, b, written, i in sorted(ranges):
+            if a < written_end or (written and a < end):
+                raise ValueError(f"grad_list: tensor {i} or its output overlaps another one that is written")
+            end = max(end, b)
+            if written:
+                written_end = max(written_end, b)
 
 
 def grad_list(tensors, outs=None) -> GradList:

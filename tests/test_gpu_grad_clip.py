@@ -163,3 +163,22 @@ def test_scaled_update_is_the_update_of_scaled_gradients(n):
     assert torch.equal(dev[1], plain[1]) and torch.equal(dev[2], plain[2]) and torch.equal(p16, q16)
     rw, rv = optim.rmsprop_step(w, g.astype(np.float64) * float(s), v, 1e-2, 0.9, 1e-6)[:2]
     assert np.abs(host(dev[1]) - rw).max() < 1e-5 and np.abs(host(dev[2]) - rv).max() < 1e-5
+
+
+def test_list_refuses_overlaps_and_foreign_tensors():
+    a, b = torch.zeros(100, device="cuda"), torch.zeros(100, device="cuda")
+    for tensors, outs in (([a, a], None), ([a, a[50:]], None), ([a[:60], a[50:]], None), ([a, b], [b, torch.zeros_like(b)]), ([a[:50], b[:50]], [a[25:75], b[50:]]),
+                          ([a, b], [torch.zeros_like(a), a])):
+        with pytest.raises(ValueError):
+            B.grad_list(tensors, outs)
+    assert B.grad_list([a[:50], a[50:]]).count == 2                      # neighbours
+    assert B.grad_list([a, a], [torch.zeros_like(a), torch.zeros_like(a)]).count == 2
+    for bad, outs in (([a.half()], None), ([a.cpu()], None), ([torch.zeros(10, 10, device="cuda")[:, ::2]], None), ([a], [b[:50]]), ([a], [b.bfloat16()])):
+        with pytest.raises(ValueError):
+            B.grad_list(bad, outs)
+    lst = B.grad_list([a])
+    n, f = scalars()
+    with pytest.raises(B.LampError):
+        B.lamp_grad_norm(lst, 1.0, n, f, None)
+    with pytest.raises(ValueError):
+        B.lamp_grad_norm(lst, 1.0, n.double(), f, scratch(lst))
