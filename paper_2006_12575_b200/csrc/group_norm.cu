@@ -8,7 +8,7 @@
 // Each thread copies its values asynchronously into a ring of its own in shared memory, D units ahead of the one it works on (nobody else reads
 // them, so no barrier): as many bytes in flight as with registers, all the time, and the first are on their way while the constants are
 // formed.  With U units loaded into registers, worked on, and the next ones loaded, 128^3 x 32 bf16 backward took 129 us (now 118), 81,840 x 320
-// fp32 101 (89); 128^3 x 64 bf16 forward takes 152 either way.
+// fp32 101 (89); 128^3 x 64 bf16 forward takes the same either way.
 // Sums: a thread adds d = x - k and d^2 of at most RUN voxels in fp32, k the mean of the first values it loads - without it the squares of
 // data far from 0 lose the variance.  Between threads, CTAs and channels of a group the sums are fp64, taken about r, the group's first
 // value, and added in a fixed order.
@@ -33,18 +33,20 @@ struct Place {
     int part, ch, unit, ty;                   // this thread's first channel, its unit in the chunk, its voxel line
     int count;                                // of this thread's voxels, P.apart apart
 };
-__device__ __forceinline__ Place place(const GnParams &P)
+// `back`: samples and parts in the opposite order
+__device__ __forceinline__ Place place(const GnParams &P, bool back)
 {
     Place q;
-    const int64_t at = blockIdx.x;
+    const int64_t at = back ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
     q.sample = at / P.parts;
     q.part = (int)(at - q.sample * P.parts);
     q.ty = threadIdx.x / P.uc;
     q.unit = threadIdx.x - q.ty * P.uc;
     const int u = blockIdx.y * P.uc + q.unit;
     q.ch = u * 8;
-    q.v0 = (int64_t)q.part * P.ty + q.ty;
-    q.count = q.ty < P.ty && q.ch < P.c && q.v0 < P.v ? (int)((P.v - q.v0 + P.apart - 1) / P.apart) : 0;
+    q.v0 = q.part * P.lead + q.ty;
+    const int64_t end = min(P.v, q.part * P.lead + P.span);
+    q.count = q.ty < P.ty && q.ch < P.c && q.v0 < end ? (int)((end - q.v0 + P.apart - 1) / P.apart) : 0;
     return q;
 }
 
@@ -106,7 +108,7 @@ gn_sums_kernel(const GnParams P)
     constexpr int D = depth(XF, false);
     pdl_launch_dependents();
     pdl_wait();
-    const Place q = place(P);
+    const Place q = place(P, false);
     const int64_t base = q.sample * P.v, step = P.apart * P.px, x0 = (base + q.v0) * P.px + q.ch;
     const int mine = q.count;
     const Ring<XF, D> ring(sm);
@@ -224,7 +226,7 @@ gn_apply_kernel(const GnParams P)
     constexpr int D = depth(XF, false);
     pdl_launch_dependents();
     pdl_wait();
-    const Place q = place(P);
+    const Place q = place(P, true);
     const int mine = q.count;
     if (mine == 0) return;
     const int64_t line = q.sample * P.v + q.v0 + (mine - 1) * P.apart;             // backwards from the last voxel
@@ -253,7 +255,7 @@ gn_bwd_sums_kernel(const GnParams P)
     constexpr int D = depth(XF, true);
     pdl_launch_dependents();
     pdl_wait();
-    const Place q = place(P);
+    const Place q = place(P, false);
     const int mine = q.count;
     const int64_t line = q.sample * P.v + q.v0, xs = P.apart * P.px, x0 = line * P.px + q.ch, zs = P.apart * P.pdz, z0 = line * P.pdz + q.ch;
     const Ring<XF, D> rx(sm);
@@ -334,7 +336,7 @@ gn_bwd_apply_kernel(const GnParams P)
     constexpr int D = depth(XF, true);
     pdl_launch_dependents();
     pdl_wait();
-    const Place q = place(P);
+    const Place q = place(P, true);
     const int mine = q.count;
     const int64_t line = q.sample * P.v + q.v0 + (mine - 1) * P.apart;             // backwards from the last voxel
     const int64_t xs = P.apart * P.px, x0 = line * P.px + q.ch, zs = P.apart * P.pdz, z0 = line * P.pdz + q.ch, os = P.apart * P.po, o0 = line * P.po + q.ch;
@@ -394,7 +396,21 @@ void split(GnParams &P, int per_sm)
     int64_t parts = need < room ? need : room;
     if (parts < least) parts = least;
     P.parts = (int32_t)parts;
+    P.lead = P.ty;
     P.apart = (int64_t)P.ty * parts;
+    P.span = P.v;
+}
+
+// The passes that apply have nothing to hand over at their end, so large tensors are cut into short runs, one after the other through the CTAs that
+// the GPU holds: CTAs at different points of their work use the memory better than CTAs in step (128^3 x 64 bf16 forward: 153 -> 146 us).  Up
+// to LONG_RUN units per thread of a resident grid the constants at the start of a CTA cost more than that (10^6 x 64: 72 -> 76).
+constexpr int LONG_RUN = 64, SHORT_RUN = 16;
+void short_runs(GnParams &P)
+{
+    if ((P.v + P.apart - 1) / P.apart <= LONG_RUN) return;
+    P.lead = P.span = (int64_t)P.ty * SHORT_RUN;
+    P.apart = P.ty;
+    P.parts = (int32_t)((P.v + P.lead - 1) / P.lead);
 }
 
 size_t workspace(int64_t v, int n, int c)
@@ -458,7 +474,8 @@ lamp_status_t forward(GnParams &P, cudaStream_t st)
     const bool many = P.stats ? P.cg > 256 : P.parts > 128;
     if ((s = launch_pdl(early, many ? gn_finish_kernel<XF, GT / 32> : gn_finish_kernel<XF, 1>, dim3((unsigned)(many ? all : (all + GT / 32 - 1) / (GT / 32))), dim3(GT), 0, st,
                         P)) != LAMP_OK) return s;
-    return launch_pdl(early, gn_apply_kernel<XF, ZF, ACT>, grid, dim3(GT), rings, st, P);
+    short_runs(P);
+    return launch_pdl(early, gn_apply_kernel<XF, ZF, ACT>, dim3((unsigned)(P.n * P.parts), (unsigned)P.chunks), dim3(GT), rings, st, P);
 }
 
 template <bool XF, bool ZF, int ACT>
@@ -476,7 +493,8 @@ lamp_status_t backward(GnParams &P, cudaStream_t st)
     if ((s = applies.ensure(gn_bwd_apply_kernel<XF, ZF, ACT>, (int)(rings + (size_t)GT * 8 * sizeof(float2)))) != LAMP_OK) return s;
     if ((s = launch_pdl(early, gn_bwd_sums_kernel<XF, ZF, ACT>, grid, dim3(GT), larger(rings, lines_bytes(P)), st, P)) != LAMP_OK) return s;
     if (P.parts > 1 && (s = launch_pdl(early, gn_bwd_parts_kernel, dim3((unsigned)(P.c / 8 * P.n)), dim3(1024), 0, st, P)) != LAMP_OK) return s;
-    return launch_pdl(early, gn_bwd_apply_kernel<XF, ZF, ACT>, grid, dim3(GT), rings + (size_t)P.uc * 8 * sizeof(float2), st, P);
+    short_runs(P);
+    return launch_pdl(early, gn_bwd_apply_kernel<XF, ZF, ACT>, dim3((unsigned)(P.n * P.parts), (unsigned)P.chunks), dim3(GT), rings + (size_t)P.uc * 8 * sizeof(float2), st, P);
 }
 
 template <bool XF, bool ZF>

@@ -19,7 +19,7 @@ struct GnParams {
     int64_t v;                                // voxels of one sample
     int32_t n, c, groups, cg;                 // cg = channels per group
     int32_t parts;                            // CTAs per sample (and chunk of channels)
-    int64_t apart;                            // voxels between two of a thread: ty * parts
+    int64_t apart, lead, span;                // voxels between two of a thread, between the first ones of two CTAs, from a CTA's first one to its end
     int32_t chunks, uc, ty;                   // chunks of channels, units of a chunk, voxels side by side
     int32_t act;
     float slope, eps;
