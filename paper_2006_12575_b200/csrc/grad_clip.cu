@@ -18,7 +18,7 @@ using namespace bn;
 constexpr int CT = 256, UNITS = 8;              // threads, 16-byte units of a piece per thread: neighbouring lanes take neighbouring units
 // Elements of a piece that T threads take: a CTA's 32 KB, or a warp's 4 KB where all of the gradients are few
 template <int T> __host__ __device__ constexpr int piece_of(bool f32) { return T * UNITS * (f32 ? 4 : 8); }
-constexpr int CTAS = 4;                       // per SM: all of them resident, so that the sum over the parts is formed once per place
+constexpr int CTAS = 4;                       // per SM, all of them resident
 
 struct Entry {
     const void *g;
@@ -273,7 +273,7 @@ grad_scale_kernel(const __grid_constant__ Table<N> T, const double *part, int pa
         *norm = v;
         *factor = f;
     }
-    for_pieces<CT, true>(T, blockIdx.x, gridDim.x, [&](const Entry &e, int64_t b0, int64_t b1, int64_t h) { scale_piece<CT>(e, b0, b1, h, f); });
+    for_pieces<CT, true>(T, gridDim.x - 1 - blockIdx.x, gridDim.x, [&](const Entry &e, int64_t b0, int64_t b1, int64_t h) { scale_piece<CT>(e, b0, b1, h, f); });
 }
 
 // All of it in one launch where the gradients are few: a cluster, a piece per warp, the CTAs' sums over distributed shared memory in rank order.
@@ -352,6 +352,10 @@ int32_t fill(Table<N> &T, const lamp_grad_t *grads, int32_t count, int32_t i)
 
 template <int N> int ctas(const Table<N> &T) { return T.pieces < max_ctas() ? T.pieces : max_ctas(); }
 
+// Many pieces: four to a CTA, one CTA after the other.  CTAs at different points of their work use the memory better than resident ones in step, which
+// pays for the sum over the parts at the start of each (211 M mixed gradients: 324 us resident, 303 so, 310 with two or eight).
+template <int N> int scale_ctas(const Table<N> &T) { return T.pieces <= 8 * max_ctas() ? ctas(T) : (T.pieces + 3) / 4; }
+
 template <int N>
 lamp_status_t run(const lamp_grad_t *grads, int32_t count, float max_norm, float *norm, float *factor, bool scale, double *part, cudaStream_t st)
 {
@@ -370,7 +374,7 @@ lamp_status_t run(const lamp_grad_t *grads, int32_t count, float max_norm, float
     int32_t i = 0;
     for (int t = 0; t < tables; ++t) {
         i = fill(T, grads, count, i);
-        if ((s = launch_pdl(T.pieces <= SHORT, grad_scale_kernel<N>, dim3((unsigned)ctas(T)), dim3(CT), 0, st, T, (const double *)part, parts, max_norm, norm,
+        if ((s = launch_pdl(T.pieces <= SHORT, grad_scale_kernel<N>, dim3((unsigned)scale_ctas(T)), dim3(CT), 0, st, T, (const double *)part, parts, max_norm, norm,
                             factor)) != LAMP_OK) return s;
     }
     return LAMP_OK;
