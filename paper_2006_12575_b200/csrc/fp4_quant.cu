@@ -14,7 +14,7 @@ constexpr int QT = 256, QU = 4;
 
 // A segment is up to 128 channels of a voxel, 8 channels on each of LPS lanes (4, 8 or 16: as many as the channels need, at least a block of
 // 32).  A thread takes QU rows QT / LPS apart at the same channels, so that addresses are formed once: formed for every row they were most of
-// the kernel's instructions (28 us for 131,072 x 256 bf16 against QNOW;
+// the kernel's instructions (28 us for 131,072 x 256 bf16 against 18;
 // what is left is bound by the instructions of the conversion as much as by memory).
 struct RowParams {
     void *x;                                  // source, or destination of the values
