@@ -635,16 +635,25 @@ def lamp_rmsprop_step(grad, master, v, param_bf16=None, lr=1e-3, alpha=0.99, eps
 ACTIVATIONS = {"none": 0, "leaky_relu": 1, "silu": 2, "gelu": 3}
 
 
+def _space(ws, dev):
+    """Address and bytes of a scratch tensor (None: none)."""
+    if ws is None:
+        return None, 0
+    if ws.get_device() != dev or not ws.is_contiguous():
+        raise ValueError(f"ws: want a contiguous tensor on cuda:{dev}, got {tuple(ws.shape)} on {ws.device}")
+    return ws.data_ptr(), ws.nbytes
+
+
 def group_norm(groups, w=None, b=None, act="none", slope=0.0, eps=1e-5) -> GroupNorm:
     """Parameters of lamp_group_norm_act_fwd / _bwd: w, b fp32 [c]; act a name of ACTIVATIONS ("leaky_relu" with slope 0 is ReLU)."""
-    c, dev, ptr = None, None, []
-    for v in (w, b):
-        if v is not None and c is None:
-            c, dev = v.numel(), v.get_device()
-        ptr.append(None if v is None else _vec(v, c, "group_norm", dev))
-    if act not in ACTIVATIONS:
+    c = dev = None
+    v = b if w is None else w
+    if v is not None:
+        c, dev = v.numel(), v.get_device()
+    a = ACTIVATIONS.get(act)
+    if a is None:
         raise ValueError(f"group_norm: act is one of {', '.join(ACTIVATIONS)}, got {act!r}")
-    p = GroupNorm(groups, ACTIVATIONS[act], slope, eps, ptr[0], ptr[1])
+    p = GroupNorm(groups, a, slope, eps, _vec(w, c, "group_norm", dev), _vec(b, c, "group_norm", dev))
     p.c, p.dev, p.keep = c, dev, (w, b)
     return p
 
@@ -662,7 +671,7 @@ def lamp_group_norm_workspace_bytes(p: GroupNorm, x):
 def lamp_group_norm_act_fwd(p: GroupNorm, x, z, mean_rstd, ws=None, stats=None):
     dev = _device()
     vx = _view(x, dev, "x")
-    w, nbytes = _scratch(ws, dev)
+    w, nbytes = _space(ws, dev)
     _check(lib().lamp_group_norm_act_fwd(_group_params(p, vx, dev), C.byref(vx), _vec(stats, 2 * vx.n * vx.c, "stats", dev, torch.float64),
                                          _byref(_view(z, dev, "z")), _vec(mean_rstd, 2 * vx.n * p.groups, "mean_rstd", dev), w, nbytes,
                                          _raw_stream(dev)), "lamp_group_norm_act_fwd")
@@ -671,7 +680,7 @@ def lamp_group_norm_act_fwd(p: GroupNorm, x, z, mean_rstd, ws=None, stats=None):
 def lamp_group_norm_act_bwd(p: GroupNorm, dz, x, mean_rstd, dx, dw=None, db=None, ws=None):
     dev = _device()
     vx = _view(x, dev, "x")
-    w, nbytes = _scratch(ws, dev)
+    w, nbytes = _space(ws, dev)
     _check(lib().lamp_group_norm_act_bwd(_group_params(p, vx, dev), _byref(_view(dz, dev, "dz")), C.byref(vx),
                                          _vec(mean_rstd, 2 * vx.n * p.groups, "mean_rstd", dev), _byref(_view(dx, dev, "dx")),
                                          _vec(dw, vx.c, "dw", dev), _vec(db, vx.c, "db", dev), w, nbytes, _raw_stream(dev)), "lamp_group_norm_act_bwd")
@@ -778,14 +787,14 @@ def lamp_grad_norm_workspace_bytes(grads: GradList):
 
 def lamp_grad_norm(grads: GradList, max_norm, norm, factor=None, ws=None):
     dev = _device()
-    w, nbytes = _scratch(ws, dev)
+    w, nbytes = _space(ws, dev)
     _check(lib().lamp_grad_norm(_grads(grads, dev), grads.count, max_norm, _vec(norm, 1, "norm", dev), _vec(factor, 1, "factor", dev), w, nbytes,
                                 _raw_stream(dev)), "lamp_grad_norm")
 
 
 def lamp_grad_clip(grads: GradList, max_norm, norm, factor, ws=None):
     dev = _device()
-    w, nbytes = _scratch(ws, dev)
+    w, nbytes = _space(ws, dev)
     _check(lib().lamp_grad_clip(_grads(grads, dev), grads.count, max_norm, _vec(norm, 1, "norm", dev), _vec(factor, 1, "factor", dev), w, nbytes,
                                 _raw_stream(dev)), "lamp_grad_clip")
 

@@ -209,7 +209,7 @@ gn_finish_kernel(const GnParams P)
         s = t = 0.0;
         for (int i = 0; i < W; ++i) { s += red[0][i]; t += red[1][i]; }
     }
-    if (first == 0) P.mean_rstd[at] = mean_rstd_of(s, t, r, (double)P.v * P.cg, P.eps);
+    if (first == 0) P.mean_rstd[at] = mean_rstd_of(s, t, r, P.inv_count, P.eps);
 }
 
 // (mean, rstd) of a group of the sample
@@ -346,7 +346,7 @@ gn_bwd_apply_kernel(const GnParams P)
     const auto start = [&](int i, int slot) { rx.load(slot, P.x, x0 - i * xs); rz.load(slot, P.dz, z0 - i * zs); };
     begin<D>(mine, start);
     const int cc = P.uc * 8, c0 = blockIdx.y * cc, c1 = min(P.c, c0 + cc), g0 = c0 / P.cg, g1 = (c1 - 1) / P.cg;
-    const double inv = 1.0 / ((double)P.v * P.cg);
+    const double inv = P.inv_count;
     sum_groups(g0, g1, P.cg,
                [&](int g, int l, int lanes, double &s, double &t) {
                    for (int ch = g * P.cg + l; ch < (g + 1) * P.cg; ch += lanes) {
@@ -450,6 +450,7 @@ GnParams params(const lamp_group_norm_t *p, const lamp_tensor_t *x, const float 
     const TView v = make_view(x);
     P.x = v.p; P.px = v.pitch;
     P.n = x->n; P.v = (int64_t)x->d * x->h * x->w; P.c = x->c; P.groups = p->groups; P.cg = x->c / p->groups;
+    if (P.v > 0) P.inv_count = 1.0 / ((double)P.v * P.cg);
     P.act = p->act; P.slope = p->slope; P.eps = p->eps; P.w = p->w; P.b = p->b;
     P.mean_rstd = (float2 *)mean_rstd;
     P.part = (double2 *)ws;
@@ -510,7 +511,10 @@ lamp_status_t by_act(GnParams &P, bool back, cudaStream_t st)
 
 lamp_status_t by_type(GnParams &P, bool xf, bool zf, bool back, cudaStream_t st)
 {
-    if (!P.stats && gn_small_fits(P, xf, back)) return gn_small(P, xf, zf, back, st);
+    if (!P.stats) {
+        const lamp_status_t s = gn_small(P, xf, zf, back, st);
+        if (s != LAMP_ERR_UNSUPPORTED) return s;
+    }
     if (!xf) return by_act<false, false>(P, back, st);
     return zf ? by_act<true, true>(P, back, st) : by_act<true, false>(P, back, st);
 }

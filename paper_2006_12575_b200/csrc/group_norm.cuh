@@ -17,6 +17,7 @@ struct GnParams {
     void *out;                                // z, or dx
     int64_t px, pdz, po;
     int64_t v;                                // voxels of one sample
+    double inv_count;                         // 1 / values of a group
     int32_t n, c, groups, cg;                 // cg = channels per group
     int32_t parts;                            // CTAs per sample (and chunk of channels)
     int64_t apart, lead, span;                // voxels between two of a thread, between the first ones of two CTAs, from a CTA's first one to its end
@@ -185,10 +186,19 @@ __device__ __forceinline__ void about(float nk, float s1, float s2, int n, doubl
     a = (double)s1 + m * e;
     b = (double)s2 + e * (2.0 * s1 + m * e);
 }
-__device__ __forceinline__ float2 mean_rstd_of(double s, double t, double r, double count, float eps)
+// 1 / sqrt(v): a step of Newton's method in fp64 from the fp32 value (2^-22 off before, 2^-43 after), the division and the root themselves - a microsecond
+// together - only where fp32 has no such value
+__device__ __forceinline__ double inverse_root(double v)
 {
-    const double mu = s / count, var = t / count - mu * mu;
-    return make_float2((float)(r + mu), (float)(1.0 / sqrt((var < 0.0 ? 0.0 : var) + (double)eps)));
+    if (!(v >= 1e-30 && v <= 1e30)) return 1.0 / sqrt(v);
+    const double r = (double)rsqrtf((float)v);
+    return r * (1.5 - 0.5 * v * r * r);
+}
+// from the sums about r of `1 / inv` values
+__device__ __forceinline__ float2 mean_rstd_of(double s, double t, double r, double inv, float eps)
+{
+    const double mu = s * inv, var = t * inv - mu * mu;
+    return make_float2((float)(r + mu), (float)inverse_root((var < 0.0 ? 0.0 : var) + (double)eps));
 }
 
 // Sum over `ty` lines of uc units of 8 pairs of fp64 per thread: sa[channel], sb[channel] of the chunk on return.  sm: 2 * ty * uc * 8 values.
@@ -234,9 +244,8 @@ template <typename L, typename D> __device__ __forceinline__ void sum_groups(int
 
 }  // namespace gn
 
-// group_norm_small.cu.  Whether a cluster can hold what a group needs, and the pass in that form (forward, or backward with dz set; scratch:
-// [n][c] pairs of fp64 where dw or db is asked for).
-bool          gn_small_fits(const gn::GnParams &P, bool xf, bool back);
+// group_norm_small.cu.  The pass in the form in which a cluster holds what a group needs (forward, or backward with dz set; P.part takes [n][c] pairs of
+// fp64 where dw or db is asked for); LAMP_ERR_UNSUPPORTED, and nothing launched, where it cannot hold it.
 lamp_status_t gn_small(const gn::GnParams &P, bool xf, bool zf, bool back, cudaStream_t st);
 
 }  // namespace lamp

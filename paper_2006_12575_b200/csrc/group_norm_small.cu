@@ -5,6 +5,7 @@
 // Bound by latency: the deepest level of a U-Net (2 x 512 voxels x 512 channels) took 11 us as three kernels of the streaming form and 25 us a call;
 // 8.5 and 12 here.
 #include "group_norm.cuh"
+#include <algorithm>
 #include <numeric>
 
 namespace lamp {
@@ -13,7 +14,7 @@ namespace {
 
 using namespace gn;
 
-constexpr int MAX_CC = 512, MAX_GROUPS = 256, MAX_CL = 8;
+constexpr int MAX_CC = 512, MAX_GROUPS = GT, MAX_CL = 8;
 
 struct SmallParams : GnParams {
     int32_t cc, cl;                           // channels of a cluster, CTAs of a cluster
@@ -76,6 +77,8 @@ gn_small_kernel(const SmallParams P)
     for (int u = 0; u < U; ++u) r[u] = u < q.have ? load_raw<XF>(P.x, at + u * line) : zero_raw<XF>();
 #pragma unroll
     for (int j = 0; j < 8; ++j) ref[j] = q.have ? value_at<XF>(P.x, q.sample * P.v * P.px + (q.ch + j) / P.cg * P.cg) : 0.f;
+    const int mine = g0 + threadIdx.x;                           // the group whose sums this thread finishes: no more groups than threads
+    const float own_first = mine <= g1 ? value_at<XF>(P.x, q.sample * P.v * P.px + (int64_t)mine * P.cg) : 0.f;
     double a[8], b[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) a[j] = b[j] = 0.0;
@@ -123,16 +126,18 @@ gn_small_kernel(const SmallParams P)
                [&](int g, double s, double t) { gs[g - g0] = s; gt[g - g0] = t; });
     if (P.cl > 1) { cluster_arrive(); cluster_wait(); }
     else __syncthreads();
-    for (int g = g0 + threadIdx.x; g <= g1; g += GT) {
-        double s = gs[g - g0], t = gt[g - g0];
+    if (mine <= g1) {
+        double s = 0.0, t = 0.0;
         if (P.cl > 1) {
-            s = t = 0.0;
-            for (int i = 0; i < P.cl; ++i) { s += peer_f64(&gs[g - g0], i); t += peer_f64(&gt[g - g0], i); }
-        }
-        const double first = value_at<XF>(P.x, q.sample * P.v * P.px + (int64_t)g * P.cg);
-        const float2 v = mean_rstd_of(s, t, first, (double)P.v * P.cg, P.eps);
-        mr[g - g0] = v;
-        if (q.rank == 0) P.mean_rstd[q.sample * P.groups + g] = v;
+            double ps[MAX_CL], pt[MAX_CL];                       // all of them on their way at once
+#pragma unroll
+            for (int i = 0; i < MAX_CL; ++i) { ps[i] = i < P.cl ? peer_f64(&gs[mine - g0], i) : 0.0; pt[i] = i < P.cl ? peer_f64(&gt[mine - g0], i) : 0.0; }
+#pragma unroll
+            for (int i = 0; i < MAX_CL; ++i) { s += ps[i]; t += pt[i]; }
+        } else { s = gs[mine - g0]; t = gt[mine - g0]; }
+        const float2 v = mean_rstd_of(s, t, own_first, P.inv_count, P.eps);
+        mr[mine - g0] = v;
+        if (q.rank == 0) P.mean_rstd[q.sample * P.groups + mine] = v;
     }
     __syncthreads();
     if (P.cl > 1) cluster_arrive();                              // this CTA has read its peers' sums, and x for the last time but from registers
@@ -201,8 +206,11 @@ gn_small_bwd_kernel(const SmallParams P)
         cluster_wait();
         double *all = sm + 2 * P.ty * cc;
         for (int i = threadIdx.x; i < cc; i += GT) {
-            double s = 0.0, t = 0.0;
-            for (int k = 0; k < P.cl; ++k) { s += peer_f64(tot.a + i, k); t += peer_f64(tot.b + i, k); }
+            double ps[MAX_CL], pt[MAX_CL], s = 0.0, t = 0.0;     // all of them on their way at once
+#pragma unroll
+            for (int k = 0; k < MAX_CL; ++k) { ps[k] = k < P.cl ? peer_f64(tot.a + i, k) : 0.0; pt[k] = k < P.cl ? peer_f64(tot.b + i, k) : 0.0; }
+#pragma unroll
+            for (int k = 0; k < MAX_CL; ++k) { s += ps[k]; t += pt[k]; }
             all[i] = s;
             all[cc + i] = t;
         }
@@ -220,7 +228,7 @@ gn_small_bwd_kernel(const SmallParams P)
             }
         }
     }
-    const double inv = 1.0 / ((double)P.v * P.cg);
+    const double inv = P.inv_count;
     sum_groups(g0, g1, P.cg,
                [&](int g, int l, int lanes, double &s, double &t) {
                    for (int ch = g * P.cg + l; ch < (g + 1) * P.cg; ch += lanes) {
@@ -270,15 +278,20 @@ constexpr int most(bool xf, bool back) { return (xf ? 8 : 16) / (back ? 2 : 1); 
 struct Plan { int cc, cl, u; };
 bool plan(const GnParams &P, bool xf, bool back, Plan &out)
 {
-    const int base = std::lcm(8, P.cg), widest = P.c < MAX_CC ? P.c : MAX_CC, es = xf ? 4 : 2;
-    auto fits = [&](int cc, int cl, int u) { return (P.v + cl - 1) / cl <= (int64_t)(GT / (cc / 8)) * u && cc / P.cg <= MAX_GROUPS; };
-    int m = 0;
-    while (base * (m + 1) <= widest && fits(base * (m + 1), MAX_CL, most(xf, back))) ++m;
+    const int base = std::lcm(8, P.cg), es = xf ? 4 : 2;
+    auto fits = [&](int cc, int cl, int u) { return (P.v + cl - 1) / cl <= (int64_t)(GT / (cc / 8)) * u; };
+    // the widest piece: its units leave room for the lines that MAX_CL CTAs need
+    const int64_t lines = ((P.v + MAX_CL - 1) / MAX_CL + most(xf, back) - 1) / most(xf, back);
+    if (lines > GT) return false;
+    const int widest = std::min({P.c, MAX_CC, (int)(GT / lines) * 8, MAX_GROUPS * P.cg});
+    int m = widest / base;
     if (m == 0) return false;
     if (base * m * es < 32 && base * m < P.c) return false;      // pieces of rows shorter than a sector of memory: twice the traffic
     const int sms = sm_count();
     auto chunks = [&](int k) { return (int64_t)P.n * ((P.c + base * k - 1) / (base * k)); };
-    while (m > 1 && chunks(m) * MAX_CL < sms && base * (m - 1) * es >= 64) --m;            // narrower pieces until the GPU is full
+    // narrower pieces, of 64 bytes at least, until clusters of MAX_CL fill the GPU
+    const int want = P.n < sms ? (sms + MAX_CL * P.n - 1) / (MAX_CL * P.n) : 1;
+    if (want > 1 && chunks(m) < (int64_t)want * P.n) m = std::min(m, std::max({1, (64 / es + base - 1) / base, (P.c - 1) / ((want - 1) * base)}));
     out.cc = base * m;
     out.cl = 1;
     while (out.cl < MAX_CL && (!fits(out.cc, out.cl, few(back)) || chunks(m) * out.cl * 2 <= sms)) {
@@ -334,12 +347,6 @@ lamp_status_t by_act(SmallParams &P, bool back, int u, int64_t clusters, cudaStr
 }
 
 }  // namespace
-
-bool gn_small_fits(const gn::GnParams &P, bool xf, bool back)
-{
-    Plan p;
-    return plan(P, xf, back, p);
-}
 
 lamp_status_t gn_small(const gn::GnParams &G, bool xf, bool zf, bool back, cudaStream_t st)
 {
