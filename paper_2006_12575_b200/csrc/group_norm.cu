@@ -13,6 +13,7 @@
 // data far from 0 lose the variance.  Between threads, CTAs and channels of a group the sums are fp64, taken about r, the group's first
 // value, and added in a fixed order.
 #include "group_norm.cuh"
+#include <algorithm>
 
 namespace lamp {
 
@@ -117,6 +118,9 @@ gn_sums_kernel(const GnParams P)
 #pragma unroll
     for (int j = 0; j < 4; ++j) k[j] = s1[j] = s2[j] = 0;
     begin<D>(mine, start);
+    float ref[8];                                               // its groups' first values
+#pragma unroll
+    for (int j = 0; j < 8; ++j) ref[j] = mine > 0 ? value_at<XF>(P.x, base * P.px + group_of(P, q.ch + j) * P.cg) : 0.f;
     if (mine > 0) {
         constexpr int FIRST = D < 4 ? D : 4;
         const int first = mine < FIRST ? mine : FIRST;
@@ -158,23 +162,46 @@ gn_sums_kernel(const GnParams P)
             unpack2(s2[j], f2[2 * j], f2[2 * j + 1]);
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const double r = value_at<XF>(P.x, base * P.px + (q.ch + j) / P.cg * P.cg);
-            about(nk[j], f1[j], f2[j], mine, r, a[j], b[j]);
-        }
+        for (int j = 0; j < 8; ++j) about(nk[j], f1[j], f2[j], mine, ref[j], a[j], b[j]);
     }
     const Totals tot = sum_lines(P.ty, P.uc, q.ty, q.unit, a, b, sm);
     const int cc = P.uc * 8, c0 = blockIdx.y * cc, c1 = min(P.c, c0 + cc);
     sum_groups(c0 / P.cg, (c1 - 1) / P.cg, P.cg,
                [&](int g, int l, int lanes, double &s, double &t) {
-                   for (int ch = max(c0, g * P.cg) + l; ch < min(c1, (g + 1) * P.cg); ch += lanes) { s += tot.a[ch - c0]; t += tot.b[ch - c0]; }
+                   for (int ch = max(c0, g * P.cg) + l; ch < min(c1, (g + 1) * P.cg); ch += lanes) { s += tot.a(ch - c0); t += tot.b(ch - c0); }
                },
-               [&](int g, double s, double t) { P.part[((q.sample * P.groups + g) * P.parts + q.part) * P.chunks + blockIdx.y] = make_double2(s, t); });
+               [&](int g, double s, double t) {
+                   P.part[((q.sample * P.groups + g) * P.parts + q.part) * P.chunks + blockIdx.y] = make_double2(s, t);
+                   if (q.part == 0 && g * P.cg >= c0) P.ref[q.sample * P.groups + g] = value_at<XF>(P.x, base * P.px + g * P.cg);
+               });
 }
 
-// mean and rstd of a group from its partial sums, or from sums per channel; W warps per group: one where the sums are few (a CTA has 8 groups),
-// all where they are many
-template <bool XF, int W>
+// Adds a group's sums about its first value: the partial sums first, first + step, .., or given sums per channel about 0
+__device__ __forceinline__ void add_sums(const GnParams &P, int64_t sample, int g, int first, int step, double &s, double &t)
+{
+    if (P.stats) {
+        const double2 *p = reinterpret_cast<const double2 *>(P.stats) + sample * P.c + g * P.cg;
+#pragma unroll 4
+        for (int i = first; i < P.cg; i += step) { const double2 v = p[i]; s += v.x; t += v.y; }
+        return;
+    }
+    const double2 *p = P.part + (sample * P.groups + g) * P.parts * P.chunks;
+    if (P.chunks == 1) {
+#pragma unroll 4
+        for (int i = first; i < P.parts; i += step) { const double2 v = p[i]; s += v.x; t += v.y; }
+        return;
+    }
+    const int cc = P.uc * 8, k0 = g * P.cg / cc, ks = ((g + 1) * P.cg - 1) / cc - k0 + 1;
+#pragma unroll 4
+    for (int i = first; i < P.parts * ks; i += step) { const double2 v = p[i / ks * P.chunks + k0 + i % ks]; s += v.x; t += v.y; }
+}
+__device__ __forceinline__ float2 finish(const GnParams &P, int64_t at, double s, double t)
+{
+    return mean_rstd_of(s, t, P.stats ? 0.0 : P.ref[at], P.inv_count, P.eps);
+}
+
+// mean and rstd of a group; W warps per group: one where the sums are few (a CTA has 8 groups), all where they are many
+template <int W>
 __global__ void __launch_bounds__(GT)
 gn_finish_kernel(const GnParams P)
 {
@@ -185,20 +212,8 @@ gn_finish_kernel(const GnParams P)
     const int64_t at = W == 1 ? (int64_t)blockIdx.x * (GT / 32) + warp : blockIdx.x;
     if (at >= (int64_t)P.n * P.groups) return;
     const int64_t sample = at / P.groups;
-    const int g = (int)(at - sample * P.groups);
-    double s = 0.0, t = 0.0, r = 0.0;
-    if (P.stats) {
-        const double2 *st = reinterpret_cast<const double2 *>(P.stats) + sample * P.c + g * P.cg;
-#pragma unroll 4
-        for (int i = first; i < P.cg; i += 32 * W) { const double2 v = st[i]; s += v.x; t += v.y; }
-    } else {
-        const int cc = P.uc * 8, k0 = g * P.cg / cc, k1 = ((g + 1) * P.cg - 1) / cc, ks = k1 - k0 + 1;
-        const double2 *p = P.part + at * P.parts * P.chunks;
-        const int64_t x0 = sample * P.v * P.px + g * P.cg;
-        r = value_at<XF>(P.x, x0);
-#pragma unroll 4
-        for (int i = first; i < P.parts * ks; i += 32 * W) { const double2 v = p[i / ks * P.chunks + k0 + i % ks]; s += v.x; t += v.y; }
-    }
+    double s = 0.0, t = 0.0;
+    add_sums(P, sample, (int)(at - sample * P.groups), first, 32 * W, s, t);
     for (int o = 16; o > 0; o >>= 1) {
         s += __shfl_xor_sync(0xffffffffu, s, o);
         t += __shfl_xor_sync(0xffffffffu, t, o);
@@ -209,7 +224,7 @@ gn_finish_kernel(const GnParams P)
         s = t = 0.0;
         for (int i = 0; i < W; ++i) { s += red[0][i]; t += red[1][i]; }
     }
-    if (first == 0) P.mean_rstd[at] = mean_rstd_of(s, t, r, P.inv_count, P.eps);
+    if (first == 0) P.mean_rstd[at] = finish(P, at, s, t);
 }
 
 // (mean, rstd) of a group of the sample
@@ -228,13 +243,27 @@ gn_apply_kernel(const GnParams P)
     pdl_wait();
     const Place q = place(P, true);
     const int mine = q.count;
-    if (mine == 0) return;
+    if (mine == 0 && !P.fused) return;
     const int64_t line = q.sample * P.v + q.v0 + (mine - 1) * P.apart;             // backwards from the last voxel
     const int64_t step = P.apart * P.px, x0 = line * P.px + q.ch, out_step = P.apart * P.po, o0 = line * P.po + q.ch;
     const Ring<XF, D> ring(sm);
     const auto start = [&](int i, int slot) { ring.load(slot, P.x, x0 - i * step); };
     begin<D>(mine, start);
-    const Affine f = affine(P, q.ch, stats_of(P, q));
+    Affine f;
+    if (P.fused) {                                              // every CTA finishes the sums of its groups
+        float2 *mr = (float2 *)((char *)sm + Ring<XF, D>::BYTES);
+        const int cc = P.uc * 8, c0 = blockIdx.y * cc, g0 = c0 / P.cg, g1 = (min(P.c, c0 + cc) - 1) / P.cg;
+        sum_groups(g0, g1, P.stats ? P.cg : P.parts, [&](int g, int l, int lanes, double &s, double &t) { add_sums(P, q.sample, g, l, lanes, s, t); },
+                   [&](int g, double s, double t) {
+                       const int64_t at = q.sample * P.groups + g;
+                       const float2 v = finish(P, at, s, t);
+                       mr[g - g0] = v;
+                       if (q.part == 0 && g * P.cg >= c0) P.mean_rstd[at] = v;
+                   });
+        __syncthreads();
+        if (mine == 0) return;
+        f = affine(P, q.ch, [&](int g) { return mr[g - g0]; });
+    } else f = affine(P, q.ch, stats_of(P, q));
     stream<D>(mine, start, [&](int slot) { return ring.get(slot); },
               [&](int i, const Raw<XF> &r) {
                   float z[8];
@@ -284,7 +313,7 @@ gn_bwd_sums_kernel(const GnParams P)
             unpack2(s2[j], f2[0], f2[1]);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const float rstd = P.mean_rstd[q.sample * P.groups + (q.ch + 2 * j + i) / P.cg].y;
+                const float rstd = P.mean_rstd[q.sample * P.groups + group_of(P, q.ch + 2 * j + i)].y;
                 a[2 * j + i] = f1[i];
                 b[2 * j + i] = (double)f2[i] * rstd;
             }
@@ -295,7 +324,7 @@ gn_bwd_sums_kernel(const GnParams P)
     const Totals tot = sum_lines(P.ty, P.uc, q.ty, q.unit, a, b, sm);
     const int cc = P.uc * 8, c0 = blockIdx.y * cc;
     double2 *out = P.part + (q.sample * P.parts + q.part) * P.c + c0;
-    for (int i = threadIdx.x; i < cc && c0 + i < P.c; i += GT) out[i] = make_double2(tot.a[i], tot.b[i]);
+    for (int i = threadIdx.x; i < cc && c0 + i < P.c; i += GT) out[i] = make_double2(tot.a(i), tot.b(i));
 }
 
 // chan[n][c] = sum over the parts, 8 channels per CTA
@@ -413,13 +442,24 @@ void short_runs(GnParams &P)
     P.parts = (int32_t)((P.v + P.lead - 1) / P.lead);
 }
 
+// Whether the CTAs of the forward pass that apply also finish the sums, each those of its own groups: the launch of the kernel that does it otherwise costs
+// 3 us, what a CTA reads for it less while that is little and one run per CTA (2 x 32,768 x 64 bf16: 18.2 -> 15.1 us, some of it from the sums' bank conflicts).
+constexpr int FUSE_GROUPS = GT, FUSE_SUMS = 4096;
+bool fuse(const GnParams &P)
+{
+    if ((P.v + P.apart - 1) / P.apart > LONG_RUN) return false;
+    const int cc = P.uc * 8, groups = std::min(P.groups, (cc - 1) / P.cg + 2);        // of a chunk, at most
+    const int64_t sums = P.stats ? P.cg : (int64_t)P.parts * std::min(P.chunks, (P.cg - 1) / cc + 2);
+    return groups <= FUSE_GROUPS && groups * sums <= FUSE_SUMS;
+}
+
 size_t workspace(int64_t v, int n, int c)
 {
     // the larger of the forward pass' [n][groups][parts][chunks] and the backward pass' [n][parts + 1][c], groups = c at most
     GnParams P = {};
     P.v = v; P.n = n; P.c = c;
     split(P, resident(false, false));
-    const size_t fwd = (size_t)n * c * P.parts * P.chunks;
+    const size_t fwd = (size_t)n * c * P.parts * P.chunks + ((size_t)n * c + 1) / 2;        // and the groups' first values
     split(P, resident(false, true));
     const size_t bwd = (size_t)n * c * (P.parts + 1);
     return (fwd > bwd ? fwd : bwd) * sizeof(double2);
@@ -450,6 +490,7 @@ GnParams params(const lamp_group_norm_t *p, const lamp_tensor_t *x, const float 
     const TView v = make_view(x);
     P.x = v.p; P.px = v.pitch;
     P.n = x->n; P.v = (int64_t)x->d * x->h * x->w; P.c = x->c; P.groups = p->groups; P.cg = x->c / p->groups;
+    P.inv_cg = ((1ull << 32) + P.cg - 1) / P.cg;
     if (P.v > 0) P.inv_count = 1.0 / ((double)P.v * P.cg);
     P.act = p->act; P.slope = p->slope; P.eps = p->eps; P.w = p->w; P.b = p->b;
     P.mean_rstd = (float2 *)mean_rstd;
@@ -460,7 +501,6 @@ GnParams params(const lamp_group_norm_t *p, const lamp_tensor_t *x, const float 
 bool short_launch(const GnParams &P) { return (int64_t)P.n * P.v * P.c <= 32 * 1024 * 1024; }
 
 size_t larger(size_t a, size_t b) { return a > b ? a : b; }
-size_t lines_bytes(const GnParams &P) { return (size_t)P.ty * P.uc * 8 * 2 * sizeof(double); }
 
 template <bool XF, bool ZF, int ACT>
 lamp_status_t forward(GnParams &P, cudaStream_t st)
@@ -470,13 +510,17 @@ lamp_status_t forward(GnParams &P, cudaStream_t st)
     const size_t rings = Ring<XF, depth(XF, false)>::BYTES;
     split(P, resident(XF, false));
     const dim3 grid((unsigned)(P.n * P.parts), (unsigned)P.chunks);
-    if (!P.stats && (s = launch_pdl(early, gn_sums_kernel<XF>, grid, dim3(GT), larger(rings, lines_bytes(P)), st, P)) != LAMP_OK) return s;
-    const int64_t all = (int64_t)P.n * P.groups;
-    const bool many = P.stats ? P.cg > 256 : P.parts > 128;
-    if ((s = launch_pdl(early, many ? gn_finish_kernel<XF, GT / 32> : gn_finish_kernel<XF, 1>, dim3((unsigned)(many ? all : (all + GT / 32 - 1) / (GT / 32))), dim3(GT), 0, st,
-                        P)) != LAMP_OK) return s;
-    short_runs(P);
-    return launch_pdl(early, gn_apply_kernel<XF, ZF, ACT>, dim3((unsigned)(P.n * P.parts), (unsigned)P.chunks), dim3(GT), rings, st, P);
+    P.ref = (double *)(P.part + (int64_t)P.n * P.groups * P.parts * P.chunks);
+    if (!P.stats && (s = launch_pdl(early, gn_sums_kernel<XF>, grid, dim3(GT), larger(rings, lines_bytes(P.ty, P.uc)), st, P)) != LAMP_OK) return s;
+    P.fused = fuse(P);
+    if (!P.fused) {
+        const int64_t all = (int64_t)P.n * P.groups;
+        const bool many = P.stats ? P.cg > 256 : P.parts > 128;
+        if ((s = launch_pdl(early, many ? gn_finish_kernel<GT / 32> : gn_finish_kernel<1>, dim3((unsigned)(many ? all : (all + GT / 32 - 1) / (GT / 32))), dim3(GT), 0, st, P)) !=
+            LAMP_OK) return s;
+        short_runs(P);
+    }
+    return launch_pdl(early, gn_apply_kernel<XF, ZF, ACT>, dim3((unsigned)(P.n * P.parts), (unsigned)P.chunks), dim3(GT), rings + FUSE_GROUPS * sizeof(float2), st, P);
 }
 
 template <bool XF, bool ZF, int ACT>
@@ -490,9 +534,9 @@ lamp_status_t backward(GnParams &P, cudaStream_t st)
     const dim3 grid((unsigned)(P.n * P.parts), (unsigned)P.chunks);
     P.chan = P.parts > 1 ? P.part + (int64_t)P.n * P.parts * P.c : P.part;
     static SmemAttrOnce sums, applies;
-    if ((s = sums.ensure(gn_bwd_sums_kernel<XF, ZF, ACT>, (int)rings)) != LAMP_OK) return s;
+    if ((s = sums.ensure(gn_bwd_sums_kernel<XF, ZF, ACT>, (int)larger(rings, lines_bytes(GT, 1)))) != LAMP_OK) return s;
     if ((s = applies.ensure(gn_bwd_apply_kernel<XF, ZF, ACT>, (int)(rings + (size_t)GT * 8 * sizeof(float2)))) != LAMP_OK) return s;
-    if ((s = launch_pdl(early, gn_bwd_sums_kernel<XF, ZF, ACT>, grid, dim3(GT), larger(rings, lines_bytes(P)), st, P)) != LAMP_OK) return s;
+    if ((s = launch_pdl(early, gn_bwd_sums_kernel<XF, ZF, ACT>, grid, dim3(GT), larger(rings, lines_bytes(P.ty, P.uc)), st, P)) != LAMP_OK) return s;
     if (P.parts > 1 && (s = launch_pdl(early, gn_bwd_parts_kernel, dim3((unsigned)(P.c / 8 * P.n)), dim3(1024), 0, st, P)) != LAMP_OK) return s;
     short_runs(P);
     return launch_pdl(early, gn_bwd_apply_kernel<XF, ZF, ACT>, dim3((unsigned)(P.n * P.parts), (unsigned)P.chunks), dim3(GT), rings + (size_t)P.uc * 8 * sizeof(float2), st, P);

@@ -19,6 +19,7 @@ struct GnParams {
     int64_t v;                                // voxels of one sample
     double inv_count;                         // 1 / values of a group
     int32_t n, c, groups, cg;                 // cg = channels per group
+    uint64_t inv_cg;                          // 2^32 / cg, rounded up
     int32_t parts;                            // CTAs per sample (and chunk of channels)
     int64_t apart, lead, span;                // voxels between two of a thread, between the first ones of two CTAs, from a CTA's first one to its end
     int32_t chunks, uc, ty;                   // chunks of channels, units of a chunk, voxels side by side
@@ -28,10 +29,14 @@ struct GnParams {
     const double *stats;
     double2 *part;                            // forward [n][groups][parts][chunks], backward [n][parts][c]
     double2 *chan;                            // backward [n][c]
+    double *ref;                              // forward [n][groups], the first values
     float2 *mean_rstd;
     float *dw, *db;
+    bool fused;                               // the apply pass finishes the sums itself
 };
 
+// ch / cg: inv_cg cg is less than cg above 2^32 and ch < 2^16, so what it adds stays below 1 / cg
+__device__ __forceinline__ int group_of(const GnParams &P, int ch) { return (int)(((uint64_t)(uint32_t)ch * P.inv_cg) >> 32); }
 
 // ----------------------------------------------------------------------------------------------------------- activations
 // Two values at a time: the packed fp32 instructions halve what is issued, which with a SiLU or GELU bounds these kernels as much as memory does.
@@ -109,7 +114,7 @@ template <typename F> __device__ __forceinline__ Affine affine(const GnParams &P
     float nm[8], a[8], b[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const float2 s = mr((ch + j) / P.cg);
+        const float2 s = mr(group_of(P, ch + j));
         nm[j] = -s.x;
         a[j] = s.y * (P.w ? P.w[ch + j] : 1.f);
         b[j] = P.b ? P.b[ch + j] : 0.f;
@@ -157,7 +162,7 @@ template <typename F, typename G> __device__ __forceinline__ Back back_terms(con
         float ev[2], hv[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const int g = (ch + 2 * j + i) / P.cg;
+            const int g = group_of(P, ch + 2 * j + i);
             const float rstd = mr(g).y;
             const float2 m = means(g);
             ev[i] = -rstd * (rstd * m.y);
@@ -201,42 +206,60 @@ __device__ __forceinline__ float2 mean_rstd_of(double s, double t, double r, dou
     return make_float2((float)(r + mu), (float)inverse_root((var < 0.0 ? 0.0 : var) + (double)eps));
 }
 
-// Sum over `ty` lines of uc units of 8 pairs of fp64 per thread: sa[channel], sb[channel] of the chunk on return.  sm: 2 * ty * uc * 8 values.
-struct Totals { const double *a, *b; };
+// Channel i of a line in shared memory: an empty place behind every two units, so that lanes with neighbouring units write to different banks.
+__host__ __device__ constexpr int padded(int i) { return i + (i >> 4); }
+// fp64 values of a line, and bytes of `ty` of them twice
+__host__ __device__ constexpr int line_of(int uc) { return uc * 8 + (uc + 1) / 2; }
+__host__ __device__ constexpr size_t lines_bytes(int ty, int uc) { return (size_t)ty * line_of(uc) * 2 * sizeof(double); }
+
+// Sum over `ty` lines of uc units of 8 pairs of fp64 per thread, over the chunk's channels.
+struct Totals {
+    const double *sa, *sb;
+    __device__ __forceinline__ double a(int i) const { return sa[padded(i)]; }
+    __device__ __forceinline__ double b(int i) const { return sb[padded(i)]; }
+};
 __device__ __forceinline__ Totals sum_lines(int ty, int uc, int my_line, int my_unit, const double (&a)[8], const double (&b)[8], double *sm)
 {
-    const int cc = uc * 8;
-    double *sa = sm, *sb = sm + ty * cc;
+    const int cc = uc * 8, row = line_of(uc);
+    double *sa = sm, *sb = sm + ty * row;
     if (my_line < ty) {
+        const int at = my_line * row + padded(my_unit * 8);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) { sa[my_line * cc + my_unit * 8 + j] = a[j]; sb[my_line * cc + my_unit * 8 + j] = b[j]; }
+        for (int j = 0; j < 8; ++j) { sa[at + j] = a[j]; sb[at + j] = b[j]; }
     }
     __syncthreads();
     for (int i = threadIdx.x; i < 2 * cc; i += GT) {
-        double *s = i < cc ? sa + i : sb + (i - cc);
+        double *s = i < cc ? sa + padded(i) : sb + padded(i - cc);
         double t = s[0];
 #pragma unroll 8
-        for (int l = 1; l < ty; ++l) t += s[l * cc];
+        for (int l = 1; l < ty; ++l) t += s[l * row];
         s[0] = t;
     }
     __syncthreads();
     return Totals{sa, sb};
 }
 
-// For the groups g0 .. g1 in turn, several at a time: load(group, i) -> pair of values for i < count(group), their sum to done(group, s, t) in one
-// lane.  Every thread takes part.
-template <typename L, typename D> __device__ __forceinline__ void sum_groups(int g0, int g1, int cg, L load, D done)
+// For the groups g0 .. g1 in turn, several at a time: load(group, lane, lanes) -> sums of its values `lane`, lane + lanes, .. of `count`, their sum to
+// done(group, s, t) in one lane.  Few groups of many values take several warps each.  Every thread takes part.
+template <typename L, typename D> __device__ __forceinline__ void sum_groups(int g0, int g1, int count, L load, D done)
 {
+    __shared__ double2 red[GT / 32];
     int lanes = 1;
-    while (lanes < 32 && lanes * 2 <= cg) lanes *= 2;
-    const int l = threadIdx.x % lanes, per = GT / lanes;
-    for (int g = g0; g <= g1; g += per) {                        // the same number of turns for every thread
+    while (lanes * 2 <= count && (lanes < 32 || (lanes * 2 <= GT && lanes * 2 * (g1 - g0 + 1) <= GT))) lanes *= 2;
+    const int l = threadIdx.x % lanes, per = GT / lanes, wide = lanes < 32 ? lanes : 32;
+    for (int g = g0; g <= g1; g += per) {                        // the same number of turns for every thread; one where lanes > 32
         const int mg = g + threadIdx.x / lanes;
         double s = 0.0, t = 0.0;
         if (mg <= g1) load(mg, l, lanes, s, t);
-        for (int o = lanes / 2; o > 0; o >>= 1) {
+        for (int o = wide / 2; o > 0; o >>= 1) {
             s += __shfl_xor_sync(0xffffffffu, s, o);
             t += __shfl_xor_sync(0xffffffffu, t, o);
+        }
+        if (lanes > 32) {
+            if (l % 32 == 0) red[threadIdx.x / 32] = make_double2(s, t);
+            __syncthreads();
+            if (l == 0)
+                for (int w = 1; w < lanes / 32; ++w) { s += red[threadIdx.x / 32 + w].x; t += red[threadIdx.x / 32 + w].y; }
         }
         if (mg <= g1 && l == 0) done(mg, s, t);
     }

@@ -2,8 +2,8 @@
 // A cluster of up to 8 CTAs takes the channels c0 .. c0 + cc of a sample (whole groups, whole units), each CTA a run of its voxels, at most U per
 // thread.  The values are loaded all at once and stay in registers while the sums go through shared memory, over the cluster's
 // distributed shared memory (added in rank order in every CTA), and back.
-// Bound by latency: the deepest level of a U-Net (2 x 512 voxels x 512 channels) took 11 us as three kernels of the streaming form and 25 us a call;
-// 8.5 and 12 here.
+// Bound by latency: the deepest level of a U-Net (2 x 512 voxels x 512 channels) took 11 us as three kernels of the streaming form;
+// 6.2 here, of which bank conflicts of the fp64 sums and integer divisions had been 1.9 more.
 #include "group_norm.cuh"
 #include <algorithm>
 #include <numeric>
@@ -76,7 +76,7 @@ gn_small_kernel(const SmallParams P)
 #pragma unroll
     for (int u = 0; u < U; ++u) r[u] = u < q.have ? load_raw<XF>(P.x, at + u * line) : zero_raw<XF>();
 #pragma unroll
-    for (int j = 0; j < 8; ++j) ref[j] = q.have ? value_at<XF>(P.x, q.sample * P.v * P.px + (q.ch + j) / P.cg * P.cg) : 0.f;
+    for (int j = 0; j < 8; ++j) ref[j] = q.have ? value_at<XF>(P.x, q.sample * P.v * P.px + group_of(P, q.ch + j) * P.cg) : 0.f;
     const int mine = g0 + threadIdx.x;                           // the group whose sums this thread finishes: no more groups than threads
     const float own_first = mine <= g1 ? value_at<XF>(P.x, q.sample * P.v * P.px + (int64_t)mine * P.cg) : 0.f;
     double a[8], b[8];
@@ -121,7 +121,7 @@ gn_small_kernel(const SmallParams P)
     const Totals tot = sum_lines(P.ty, P.uc, q.line, q.unit, a, b, sm);
     sum_groups(g0, g1, P.cg,
                [&](int g, int l, int lanes, double &s, double &t) {
-                   for (int ch = g * P.cg - q.c0 + l; ch < (g + 1) * P.cg - q.c0; ch += lanes) { s += tot.a[ch]; t += tot.b[ch]; }
+                   for (int ch = g * P.cg - q.c0 + l; ch < (g + 1) * P.cg - q.c0; ch += lanes) { s += tot.a(ch); t += tot.b(ch); }
                },
                [&](int g, double s, double t) { gs[g - g0] = s; gt[g - g0] = t; });
     if (P.cl > 1) { cluster_arrive(); cluster_wait(); }
@@ -196,7 +196,7 @@ gn_small_bwd_kernel(const SmallParams P)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 a[2 * j + i] = f1[i];
-                b[2 * j + i] = (double)f2[i] * mr[(q.ch + 2 * j + i) / P.cg].y;
+                b[2 * j + i] = (double)f2[i] * mr[group_of(P, q.ch + 2 * j + i)].y;
             }
         }
     }
@@ -204,27 +204,27 @@ gn_small_bwd_kernel(const SmallParams P)
     if (P.cl > 1) {
         cluster_arrive();
         cluster_wait();
-        double *all = sm + 2 * P.ty * cc;
+        double *all = sm + 2 * P.ty * line_of(P.uc);
         for (int i = threadIdx.x; i < cc; i += GT) {
             double ps[MAX_CL], pt[MAX_CL], s = 0.0, t = 0.0;     // all of them on their way at once
 #pragma unroll
-            for (int k = 0; k < MAX_CL; ++k) { ps[k] = k < P.cl ? peer_f64(tot.a + i, k) : 0.0; pt[k] = k < P.cl ? peer_f64(tot.b + i, k) : 0.0; }
+            for (int k = 0; k < MAX_CL; ++k) { ps[k] = k < P.cl ? peer_f64(tot.sa + padded(i), k) : 0.0; pt[k] = k < P.cl ? peer_f64(tot.sb + padded(i), k) : 0.0; }
 #pragma unroll
             for (int k = 0; k < MAX_CL; ++k) { s += ps[k]; t += pt[k]; }
-            all[i] = s;
-            all[cc + i] = t;
+            all[padded(i)] = s;
+            all[line_of(P.uc) + padded(i)] = t;
         }
         __syncthreads();
-        tot = Totals{all, all + cc};
+        tot = Totals{all, all + line_of(P.uc)};
         cluster_arrive();                                        // this CTA has read its peers' sums; waited for at the end
     }
     if (q.rank == 0) {
         for (int i = threadIdx.x; i < c1 - q.c0; i += GT) {
             const int ch = q.c0 + i;
-            if (P.chan) P.chan[q.sample * P.c + ch] = make_double2(tot.a[i], tot.b[i]);
+            if (P.chan) P.chan[q.sample * P.c + ch] = make_double2(tot.a(i), tot.b(i));
             else {                                               // one sample: its sums are the parameters' gradients
-                if (P.db) P.db[ch] = (float)tot.a[i];
-                if (P.dw) P.dw[ch] = (float)tot.b[i];
+                if (P.db) P.db[ch] = (float)tot.a(i);
+                if (P.dw) P.dw[ch] = (float)tot.b(i);
             }
         }
     }
@@ -233,8 +233,8 @@ gn_small_bwd_kernel(const SmallParams P)
                [&](int g, int l, int lanes, double &s, double &t) {
                    for (int ch = g * P.cg + l; ch < (g + 1) * P.cg; ch += lanes) {
                        const double w = P.w ? P.w[ch] : 1.f;
-                       s += w * tot.a[ch - q.c0];
-                       t += w * tot.b[ch - q.c0];
+                       s += w * tot.a(ch - q.c0);
+                       t += w * tot.b(ch - q.c0);
                    }
                },
                [&](int g, double s, double t) { means[g - g0] = make_float2((float)(s * inv), (float)(t * inv)); });
@@ -324,11 +324,11 @@ lamp_status_t launch(Kernel kernel, const SmallParams &P, int64_t clusters, size
 template <bool XF, bool ZF, int ACT>
 lamp_status_t run(SmallParams &P, bool back, int u, int64_t clusters, cudaStream_t st)
 {
-    const size_t lines = (size_t)P.ty * P.uc * 8 * 2 * sizeof(double);
+    const size_t lines = lines_bytes(P.ty, P.uc);
     if (!back)
         return u == few(false) ? launch(gn_small_kernel<XF, ZF, ACT, few(false)>, P, clusters, lines, st)
                                : launch(gn_small_kernel<XF, ZF, ACT, most(XF, false)>, P, clusters, lines, st);
-    const size_t smem = lines + (P.cl > 1 ? (size_t)P.uc * 8 * 2 * sizeof(double) : 0);
+    const size_t smem = lines + (P.cl > 1 ? lines_bytes(1, P.uc) : 0);
     const lamp_status_t s = u == few(true) ? launch(gn_small_bwd_kernel<XF, ZF, ACT, few(true)>, P, clusters, smem, st)
                                            : launch(gn_small_bwd_kernel<XF, ZF, ACT, most(XF, true)>, P, clusters, smem, st);
     if (s != LAMP_OK || !P.chan) return s;
