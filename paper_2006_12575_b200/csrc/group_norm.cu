@@ -387,17 +387,23 @@ gn_bwd_apply_kernel(const GnParams P)
                },
                [&](int g, double s, double t) { means[g - g0] = make_float2((float)(s * inv), (float)(t * inv)); });
     __syncthreads();
-    if (blockIdx.y == 0 && (P.dw || P.db)) {                    // a warp per channel, the lanes over the samples
-        const int lane = threadIdx.x & 31;
-        for (int64_t ch = (int64_t)blockIdx.x * (GT / 32) + (threadIdx.x >> 5); ch < P.c; ch += (int64_t)gridDim.x * (GT / 32)) {
+    if (blockIdx.y == 0 && (P.dw || P.db)) {                    // a few lanes per channel, four samples each where that is enough
+        int lanes = 1;
+        while (lanes < 32 && lanes * 4 < P.n) lanes *= 2;
+        const int l = threadIdx.x % lanes, per = GT / lanes;
+        for (int64_t c0 = (int64_t)blockIdx.x * per; c0 < P.c; c0 += (int64_t)gridDim.x * per) {      // the same turns for every thread
+            const int64_t ch = c0 + threadIdx.x / lanes;
             double s = 0.0, t = 0.0;
-            for (int i = lane; i < P.n; i += 32) { const double2 v = P.chan[(int64_t)i * P.c + ch]; s += v.x; t += v.y; }
-            for (int o = 16; o > 0; o >>= 1) {
+            if (ch < P.c) {
+#pragma unroll 4
+                for (int i = l; i < P.n; i += lanes) { const double2 v = P.chan[(int64_t)i * P.c + ch]; s += v.x; t += v.y; }
+            }
+            for (int o = lanes / 2; o > 0; o >>= 1) {
                 s += __shfl_xor_sync(0xffffffffu, s, o);
                 t += __shfl_xor_sync(0xffffffffu, t, o);
             }
-            if (lane == 0 && P.db) P.db[ch] = (float)s;
-            if (lane == 0 && P.dw) P.dw[ch] = (float)t;
+            if (ch < P.c && l == 0 && P.db) P.db[ch] = (float)s;
+            if (ch < P.c && l == 0 && P.dw) P.dw[ch] = (float)t;
         }
     }
     if (mine == 0) return;
