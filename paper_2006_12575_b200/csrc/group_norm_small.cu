@@ -38,6 +38,18 @@ __device__ __forceinline__ double peer_f64(const double *p, uint32_t rank)
     return v;
 }
 
+// s = sum of *a over the cluster's CTAs, t of *b, in rank order
+__device__ __forceinline__ void over_cluster(int cl, const double *a, const double *b, double &s, double &t)
+{
+    if (cl == 1) { s = *a; t = *b; return; }
+    double ps[MAX_CL], pt[MAX_CL];                               // all of them on their way at once
+#pragma unroll
+    for (int i = 0; i < MAX_CL; ++i) { ps[i] = i < cl ? peer_f64(a, i) : 0.0; pt[i] = i < cl ? peer_f64(b, i) : 0.0; }
+    s = t = 0.0;
+#pragma unroll
+    for (int i = 0; i < MAX_CL; ++i) { s += ps[i]; t += pt[i]; }
+}
+
 struct Spot {
     int64_t sample, v0;                       // first voxel of this thread
     int c0, ch, unit, line, have;             // have: of this thread's voxels, `ty` apart
@@ -127,14 +139,8 @@ gn_small_kernel(const SmallParams P)
     if (P.cl > 1) { cluster_arrive(); cluster_wait(); }
     else __syncthreads();
     if (mine <= g1) {
-        double s = 0.0, t = 0.0;
-        if (P.cl > 1) {
-            double ps[MAX_CL], pt[MAX_CL];                       // all of them on their way at once
-#pragma unroll
-            for (int i = 0; i < MAX_CL; ++i) { ps[i] = i < P.cl ? peer_f64(&gs[mine - g0], i) : 0.0; pt[i] = i < P.cl ? peer_f64(&gt[mine - g0], i) : 0.0; }
-#pragma unroll
-            for (int i = 0; i < MAX_CL; ++i) { s += ps[i]; t += pt[i]; }
-        } else { s = gs[mine - g0]; t = gt[mine - g0]; }
+        double s, t;
+        over_cluster(P.cl, &gs[mine - g0], &gt[mine - g0], s, t);
         const float2 v = mean_rstd_of(s, t, own_first, P.inv_count, P.eps);
         mr[mine - g0] = v;
         if (q.rank == 0) P.mean_rstd[q.sample * P.groups + mine] = v;
@@ -158,13 +164,14 @@ template <bool XF, bool ZF, int ACT, int U>
 __global__ void __launch_bounds__(GT)
 gn_small_bwd_kernel(const SmallParams P)
 {
-    extern __shared__ __align__(16) double sm[];                // sums over the lines, then [2][cc] over the cluster
+    extern __shared__ __align__(16) double sm[];
+    __shared__ double gs[MAX_GROUPS], gt[MAX_GROUPS];
     __shared__ float2 means[MAX_GROUPS];
     pdl_launch_dependents();
     pdl_wait();
     const Spot q = spot(P);
     const int64_t xl = P.ty * P.px, zl = P.ty * P.pdz, at = (q.sample * P.v + q.v0) * P.px + q.ch, dz_at = (q.sample * P.v + q.v0) * P.pdz + q.ch;
-    const int g0 = q.c0 / P.cg, c1 = min(P.c, q.c0 + P.cc), g1 = (c1 - 1) / P.cg, cc = P.uc * 8;
+    const int g0 = q.c0 / P.cg, c1 = min(P.c, q.c0 + P.cc), g1 = (c1 - 1) / P.cg;
     const float2 *mr = P.mean_rstd + q.sample * P.groups;
     Raw<XF> rx[U];
     Raw<ZF> rz[U];
@@ -200,35 +207,9 @@ gn_small_bwd_kernel(const SmallParams P)
             }
         }
     }
-    Totals tot = sum_lines(P.ty, P.uc, q.line, q.unit, a, b, sm);
-    if (P.cl > 1) {
-        cluster_arrive();
-        cluster_wait();
-        double *all = sm + 2 * P.ty * line_of(P.uc);
-        for (int i = threadIdx.x; i < cc; i += GT) {
-            double ps[MAX_CL], pt[MAX_CL], s = 0.0, t = 0.0;     // all of them on their way at once
-#pragma unroll
-            for (int k = 0; k < MAX_CL; ++k) { ps[k] = k < P.cl ? peer_f64(tot.sa + padded(i), k) : 0.0; pt[k] = k < P.cl ? peer_f64(tot.sb + padded(i), k) : 0.0; }
-#pragma unroll
-            for (int k = 0; k < MAX_CL; ++k) { s += ps[k]; t += pt[k]; }
-            all[padded(i)] = s;
-            all[line_of(P.uc) + padded(i)] = t;
-        }
-        __syncthreads();
-        tot = Totals{all, all + line_of(P.uc)};
-        cluster_arrive();                                        // this CTA has read its peers' sums; waited for at the end
-    }
-    if (q.rank == 0) {
-        for (int i = threadIdx.x; i < c1 - q.c0; i += GT) {
-            const int ch = q.c0 + i;
-            if (P.chan) P.chan[q.sample * P.c + ch] = make_double2(tot.a(i), tot.b(i));
-            else {                                               // one sample: its sums are the parameters' gradients
-                if (P.db) P.db[ch] = (float)tot.a(i);
-                if (P.dw) P.dw[ch] = (float)tot.b(i);
-            }
-        }
-    }
-    const double inv = P.inv_count;
+    // The cluster exchanges the groups' sums, which every CTA needs; of the channels' sums each CTA adds a slice.  (All of them in every CTA: 32 x 64 x 512
+    // channels took 21.7 us.)
+    const Totals tot = sum_lines(P.ty, P.uc, q.line, q.unit, a, b, sm);
     sum_groups(g0, g1, P.cg,
                [&](int g, int l, int lanes, double &s, double &t) {
                    for (int ch = g * P.cg + l; ch < (g + 1) * P.cg; ch += lanes) {
@@ -237,8 +218,30 @@ gn_small_bwd_kernel(const SmallParams P)
                        t += w * tot.b(ch - q.c0);
                    }
                },
-               [&](int g, double s, double t) { means[g - g0] = make_float2((float)(s * inv), (float)(t * inv)); });
+               [&](int g, double s, double t) { gs[g - g0] = s; gt[g - g0] = t; });
+    if (P.cl > 1) { cluster_arrive(); cluster_wait(); }
+    else __syncthreads();
+    const int mine = g0 + threadIdx.x;                           // the group whose sums this thread finishes: no more groups than threads
+    if (mine <= g1) {
+        double s, t;
+        over_cluster(P.cl, &gs[mine - g0], &gt[mine - g0], s, t);
+        means[mine - g0] = make_float2((float)(s * P.inv_count), (float)(t * P.inv_count));
+    }
+    if (P.chan || P.dw || P.db) {
+        const int slice = (c1 - q.c0 + P.cl - 1) / P.cl, end = min(c1 - q.c0, (int)(q.rank + 1) * slice);
+        for (int i = q.rank * slice + (GT - 1 - threadIdx.x); i < end; i += GT) {        // the warps that have no group first
+            const int ch = q.c0 + i;
+            double s, t;
+            over_cluster(P.cl, tot.sa + padded(i), tot.sb + padded(i), s, t);
+            if (P.chan) P.chan[q.sample * P.c + ch] = make_double2(s, t);
+            else {                                               // one sample: its sums are the parameters' gradients
+                if (P.db) P.db[ch] = (float)s;
+                if (P.dw) P.dw[ch] = (float)t;
+            }
+        }
+    }
     __syncthreads();
+    if (P.cl > 1) cluster_arrive();                              // this CTA has read its peers' sums; waited for at the end
     if (q.have) {
         const Back k = back_terms(P, q.ch, [&](int g) { return mr[g]; }, [&](int g) { return means[g - g0]; });
         const int64_t ol = P.ty * P.po, to = (q.sample * P.v + q.v0) * P.po + q.ch;
@@ -328,9 +331,8 @@ lamp_status_t run(SmallParams &P, bool back, int u, int64_t clusters, cudaStream
     if (!back)
         return u == few(false) ? launch(gn_small_kernel<XF, ZF, ACT, few(false)>, P, clusters, lines, st)
                                : launch(gn_small_kernel<XF, ZF, ACT, most(XF, false)>, P, clusters, lines, st);
-    const size_t smem = lines + (P.cl > 1 ? lines_bytes(1, P.uc) : 0);
-    const lamp_status_t s = u == few(true) ? launch(gn_small_bwd_kernel<XF, ZF, ACT, few(true)>, P, clusters, smem, st)
-                                           : launch(gn_small_bwd_kernel<XF, ZF, ACT, most(XF, true)>, P, clusters, smem, st);
+    const lamp_status_t s = u == few(true) ? launch(gn_small_bwd_kernel<XF, ZF, ACT, few(true)>, P, clusters, lines, st)
+                                           : launch(gn_small_bwd_kernel<XF, ZF, ACT, most(XF, true)>, P, clusters, lines, st);
     if (s != LAMP_OK || !P.chan) return s;
     return launch_pdl(true, gn_small_params_kernel, dim3((unsigned)((P.c + GT / 32 - 1) / (GT / 32))), dim3(GT), 0, st, (const double2 *)P.chan, (int)P.n, (int)P.c, P.dw, P.db);
 }
