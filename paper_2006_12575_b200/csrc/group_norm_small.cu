@@ -305,6 +305,9 @@ bool plan(const GnParams &P, bool xf, bool back, Plan &out)
     // With as many values as the registers hold an SM has one CTA, and one wave of them waits for memory, works and stores in step: behind one and a half
     // waves the streaming form is ahead (16 x 512 x 512 forward 25.6 here, 20.6 there; 64 x 1,500 x 128 42.6 and 22.5; 8 x 1,024 x 512, 1.3 waves, 18.1 and 21.4).
     if (out.u != few(back) && chunks(m) * out.cl * 2 > 3ll * sms) return false;
+    // With few values the same holds behind four CTAs per SM (512 x 64 x 512 forward 59.2 here, 30.0 there, backward 141 and 47), but forward without a cluster
+    // (1,000 x 64 x 64: 16.4 and 19.8).
+    if ((back || out.cl > 1) && chunks(m) * out.cl > 4ll * sms) return false;
     return chunks(m) * out.cl <= 2147483647ll;
 }
 
