@@ -36,8 +36,8 @@ struct Divisor {
     }
 };
 
-// a / b correctly rounded for b > 0, with inv = 1 / b correctly rounded: one correction of a * inv by its exact remainder (Markstein's theorem).  Where the
-// remainder or the reciprocal could leave the normal range - b outside of 2^-90 .. 2^90 - by the division itself.
+// a / b correctly rounded for b > 0, with inv = 1 / b correctly rounded: one correction of a * inv by its exact remainder (Markstein's theorem).  Only
+// where nothing leaves fp32's range - b within 2^-90 .. 2^90, a * inv finite (from an infinite one the correction makes NaN) - elsewhere the division itself.
 __device__ __forceinline__ float quotient(float a, float b, float inv)
 {
     const float q = a * inv;
@@ -51,7 +51,7 @@ __device__ __forceinline__ ptx::f32x2 quotient2(ptx::f32x2 a, ptx::f32x2 b, ptx:
 __device__ __forceinline__ bool plain_range(float b) { return b >= 8.0779357e-28f && b <= 1.2379400e27f; }
 
 // A block's scale byte, and what its values are divided by: `inv` = 1 / scale, exactly, where the scale is a power of two (blocks of 32), else
-// by = scale * g and inv = its reciprocal.  by = 0: the block has no codes (NaN scale).
+// by = scale * g and inv = its reciprocal, 0 where the division itself has to be taken.  by = 0: the block has no codes (NaN scale).
 struct Scale { uint32_t byte; float by, inv; };
 
 // from the bits of the block's amax
@@ -66,7 +66,8 @@ template <int BLOCK> __device__ __forceinline__ Scale block_scale(uint32_t amax,
         s.by = s.inv = nan ? 0.f : __uint_as_float((254u - s.byte) << 23);
     } else {
         const float a = __uint_as_float(amax);
-        const float v = fminf(fmaxf(plain_range(d.six_g) && a > 1e-25f ? quotient(a, d.six_g, d.inv) : __fdiv_rn(a, d.six_g), 0.001953125f), 448.f);
+        // at 2^20 and above the scale is the largest, whatever the last digits are
+        const float v = fminf(fmaxf(plain_range(d.six_g) && a > 1e-25f && a * d.inv < 1048576.f ? quotient(a, d.six_g, d.inv) : __fdiv_rn(a, d.six_g), 0.001953125f), 448.f);
         uint16_t two;
         asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(0.f), "f"(v));
         s.byte = nan ? 0x7Fu : (two & 0xFFu);
@@ -74,6 +75,8 @@ template <int BLOCK> __device__ __forceinline__ Scale block_scale(uint32_t amax,
         asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(half2) : "h"(two));
         s.by = nan ? 0.f : __fmul_rn(__half2float(__ushort_as_half((unsigned short)(half2 & 0xFFFFu))), d.g);
         s.inv = __frcp_rn(s.by);
+        // values far above the largest scale: no |x| * inv is larger than amax * inv, so one look decides for the block
+        if (!plain_range(s.by) || !(a * s.inv <= 3.4028235e38f)) s.inv = 0.f;
     }
     return s;
 }
@@ -98,7 +101,7 @@ template <int BLOCK> __device__ __forceinline__ uint32_t encode8(const float (&f
         const ptx::f32x2 inv = ptx::twice(s.inv);
 #pragma unroll
         for (int i = 0; i < 8; i += 2) ptx::unpack2(ptx::mul2(ptx::pack2(__float_as_uint(f[i]), __float_as_uint(f[i + 1])), inv), v[i], v[i + 1]);
-    } else if (plain_range(s.by)) {
+    } else if (s.inv != 0.f) {
 #pragma unroll
         for (int i = 0; i < 8; i += 2)
             ptx::unpack2(quotient2(ptx::pack2(__float_as_uint(f[i]), __float_as_uint(f[i + 1])), ptx::twice(s.by), ptx::twice(s.inv), ptx::twice(-s.inv)), v[i], v[i + 1]);
