@@ -198,8 +198,9 @@ lamp_status_t lamp_instnorm_relu_bwd(const lamp_tensor_t *dz_a, const lamp_tenso
  *     t = (x - mean) * rstd * w[c] + b[c],   rstd = 1 / sqrt(var + eps),   z = act(t),
  *     act: t;   t > 0 ? t : slope * t;   t / (1 + e^-t);   t * (1 + erf(t / sqrt(2))) / 2.
  * Tensors: x and dx of one type, z and dz of another: (bf16, bf16), (fp32, fp32) or (fp32, bf16); all of the same n, d, h, w, c, any channel
- * slices; c, c_pitch and c_offset are multiples of 8.  Arithmetic in fp32; the sums of a thread run about a value of its own data, those
- * of a group in fp64, in a fixed order.  A group with a value that is not finite becomes NaN.
+ * slices; c, c_pitch and c_offset are multiples of 8.  Arithmetic in fp32; the sums of a thread run about a value of its own data (in fp64
+ * where the squares are no fp32 numbers), those of a group in fp64, in a fixed order.  mean, rstd, x - mean and rstd * w have to be fp32 numbers:
+ * deviations of 1e-37 to 1e37 keep their digits.  A group with a value that is not finite becomes NaN.
  * ---------------------------------------------------------------------- */
 enum { LAMP_ACT_NONE = 0, LAMP_ACT_LEAKY_RELU = 1, LAMP_ACT_SILU = 2, LAMP_ACT_GELU = 3 };
 typedef struct {

@@ -10,7 +10,7 @@
 // formed.  With U units loaded into registers, worked on, and the next ones loaded, 128^3 x 32 bf16 backward took 129 us (now 114), 81,840 x 320
 // fp32 101 (87); 128^3 x 64 bf16 forward takes the same either way.
 // Sums: a thread adds d = x - k and d^2 of at most RUN voxels in fp32, k the mean of the first values it loads - without it the squares of
-// data far from 0 lose the variance.  Between threads, CTAs and channels of a group the sums are fp64, taken about r, the group's first
+// data far from 0 lose the variance; where the squares leave fp32's range the thread adds its values again in fp64.  Between threads, CTAs and channels of a group the sums are fp64, taken about r, the group's first
 // value, and added in a fixed order.
 #include "group_norm.cuh"
 #include <algorithm>
@@ -151,6 +151,7 @@ gn_sums_kernel(const GnParams P)
     landed<0>();
     __syncthreads();                                            // the rings make room
     double a[8], b[8];
+    uint32_t again = 0;                                         // channels whose squares left fp32
 #pragma unroll
     for (int j = 0; j < 8; ++j) a[j] = b[j] = 0.0;
     if (mine > 0) {
@@ -162,9 +163,14 @@ gn_sums_kernel(const GnParams P)
             unpack2(s2[j], f2[2 * j], f2[2 * j + 1]);
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) about(nk[j], f1[j], f2[j], mine, ref[j], a[j], b[j]);
+        for (int j = 0; j < 8; ++j) {
+            about(nk[j], f1[j], f2[j], mine, ref[j], a[j], b[j]);
+            again |= squares_hold(f2[j], P.eps) ? 0u : 1u << j;
+        }
     }
-    const Totals tot = sum_lines(P.ty, P.uc, q.ty, q.unit, a, b, sm);
+    const Totals tot = sum_lines(P.ty, P.uc, q.ty, q.unit, a, b, sm, [&](double *sa, double *sb) {
+        if (again) sums_again<XF>(P.x, P.cg, again, x0, step, mine, base * P.px, q.ch, sa, sb);
+    });
     const int cc = P.uc * 8, c0 = blockIdx.y * cc, c1 = min(P.c, c0 + cc);
     sum_groups(c0 / P.cg, (c1 - 1) / P.cg, P.cg,
                [&](int g, int l, int lanes, double &s, double &t) {
@@ -321,7 +327,7 @@ gn_bwd_sums_kernel(const GnParams P)
     }
     landed<0>();
     __syncthreads();                                            // the rings make room
-    const Totals tot = sum_lines(P.ty, P.uc, q.ty, q.unit, a, b, sm);
+    const Totals tot = sum_lines(P.ty, P.uc, q.ty, q.unit, a, b, sm, [](double *, double *) {});
     const int cc = P.uc * 8, c0 = blockIdx.y * cc;
     double2 *out = P.part + (q.sample * P.parts + q.part) * P.c + c0;
     for (int i = threadIdx.x; i < cc && c0 + i < P.c; i += GT) out[i] = make_double2(tot.a(i), tot.b(i));

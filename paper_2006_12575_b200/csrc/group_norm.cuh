@@ -191,6 +191,27 @@ __device__ __forceinline__ void about(float nk, float s1, float s2, int n, doubl
     a = (double)s1 + m * e;
     b = (double)s2 + e * (2.0 * s1 + m * e);
 }
+// Whether the fp32 sum of a thread's squares may stand: finite, so that no square or shift left fp32's range; and, where eps does not hide it, well above the
+// 256 halves of fp32's smallest step that squares may have lost.
+__device__ __forceinline__ bool squares_hold(float s2, float eps) { return s2 <= 3.4028235e38f && (s2 >= 7.8886091e-31f || eps >= 7.8886091e-31f); }      // 2^-100
+// The same sums about the group's first value, in fp64 from the values themselves, for the channels of `mask` where they may not: `count` voxels, `step`
+// elements apart, the first at `at`; first: the sample's first voxel.  To where the thread's sums lie in shared memory, so that nothing is held in registers
+// for it.
+template <bool XF> __device__ __noinline__ void sums_again(const void *x, int cg, uint32_t mask, int64_t at, int64_t step, int count, int64_t first, int ch, double *sa, double *sb)
+{
+    for (; mask; mask &= mask - 1) {
+        const int j = __ffs(mask) - 1;
+        const double r = value_at<XF>(x, first + (ch + j) / cg * cg);
+        double s = 0.0, t = 0.0;
+#pragma unroll 1
+        for (int i = 0; i < count; ++i) {
+            const double d = (double)value_at<XF>(x, at + i * step + j) - r;
+            s += d;
+            t = fma(d, d, t);
+        }
+        sa[j] = s; sb[j] = t;
+    }
+}
 // 1 / sqrt(v): a step of Newton's method in fp64 from the fp32 value (2^-22 off before, 2^-43 after), the division and the root themselves - a microsecond
 // together - only where fp32 has no such value
 __device__ __forceinline__ double inverse_root(double v)
@@ -212,13 +233,13 @@ __host__ __device__ constexpr int padded(int i) { return i + (i >> 4); }
 __host__ __device__ constexpr int line_of(int uc) { return uc * 8 + (uc + 1) / 2; }
 __host__ __device__ constexpr size_t lines_bytes(int ty, int uc) { return (size_t)ty * line_of(uc) * 2 * sizeof(double); }
 
-// Sum over `ty` lines of uc units of 8 pairs of fp64 per thread, over the chunk's channels.
+// Sum over `ty` lines of uc units of 8 pairs of fp64 per thread, over the chunk's channels.  mend(sa, sb): a thread's last word on its own.
 struct Totals {
     const double *sa, *sb;
     __device__ __forceinline__ double a(int i) const { return sa[padded(i)]; }
     __device__ __forceinline__ double b(int i) const { return sb[padded(i)]; }
 };
-__device__ __forceinline__ Totals sum_lines(int ty, int uc, int my_line, int my_unit, const double (&a)[8], const double (&b)[8], double *sm)
+template <typename M> __device__ __forceinline__ Totals sum_lines(int ty, int uc, int my_line, int my_unit, const double (&a)[8], const double (&b)[8], double *sm, M mend)
 {
     const int cc = uc * 8, row = line_of(uc);
     double *sa = sm, *sb = sm + ty * row;
@@ -226,6 +247,7 @@ __device__ __forceinline__ Totals sum_lines(int ty, int uc, int my_line, int my_
         const int at = my_line * row + padded(my_unit * 8);
 #pragma unroll
         for (int j = 0; j < 8; ++j) { sa[at + j] = a[j]; sb[at + j] = b[j]; }
+        mend(sa + at, sb + at);
     }
     __syncthreads();
     for (int i = threadIdx.x; i < 2 * cc; i += GT) {

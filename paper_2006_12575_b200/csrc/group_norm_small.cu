@@ -92,6 +92,7 @@ gn_small_kernel(const SmallParams P)
     const int mine = g0 + threadIdx.x;                           // the group whose sums this thread finishes: no more groups than threads
     const float own_first = mine <= g1 ? value_at<XF>(P.x, q.sample * P.v * P.px + (int64_t)mine * P.cg) : 0.f;
     double a[8], b[8];
+    uint32_t again = 0;                                         // channels whose squares left fp32
 #pragma unroll
     for (int j = 0; j < 8; ++j) a[j] = b[j] = 0.0;
     if (q.have) {
@@ -128,9 +129,14 @@ gn_small_kernel(const SmallParams P)
             unpack2(s2[j], f2[2 * j], f2[2 * j + 1]);
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) about(nk[j], f1[j], f2[j], q.have, ref[j], a[j], b[j]);
+        for (int j = 0; j < 8; ++j) {
+            about(nk[j], f1[j], f2[j], q.have, ref[j], a[j], b[j]);
+            again |= squares_hold(f2[j], P.eps) ? 0u : 1u << j;
+        }
     }
-    const Totals tot = sum_lines(P.ty, P.uc, q.line, q.unit, a, b, sm);
+    const Totals tot = sum_lines(P.ty, P.uc, q.line, q.unit, a, b, sm, [&](double *sa, double *sb) {
+        if (again) sums_again<XF>(P.x, P.cg, again, at, line, q.have, q.sample * P.v * P.px, q.ch, sa, sb);
+    });
     sum_groups(g0, g1, P.cg,
                [&](int g, int l, int lanes, double &s, double &t) {
                    for (int ch = g * P.cg - q.c0 + l; ch < (g + 1) * P.cg - q.c0; ch += lanes) { s += tot.a(ch); t += tot.b(ch); }
@@ -209,7 +215,7 @@ gn_small_bwd_kernel(const SmallParams P)
     }
     // The cluster exchanges the groups' sums, which every CTA needs; of the channels' sums each CTA adds a slice.  (All of them in every CTA: 32 x 64 x 512
     // channels took 21.7 us.)
-    const Totals tot = sum_lines(P.ty, P.uc, q.line, q.unit, a, b, sm);
+    const Totals tot = sum_lines(P.ty, P.uc, q.line, q.unit, a, b, sm, [](double *, double *) {});
     sum_groups(g0, g1, P.cg,
                [&](int g, int l, int lanes, double &s, double &t) {
                    for (int ch = g * P.cg + l; ch < (g + 1) * P.cg; ch += lanes) {
