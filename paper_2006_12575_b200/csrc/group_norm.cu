@@ -282,9 +282,25 @@ gn_apply_kernel(const GnParams P)
 // sums over the CTA's voxels of dt and dt * xhat per channel
 template <bool XF, bool ZF> struct Both { Raw<XF> x; Raw<ZF> z; };
 
+// The calls for channels whose rstd is far from 1
+template <bool XF, bool ZF, int ACT> __device__ __noinline__ void sums_far(const GnParams &P, double *sa, double *sb)
+{
+    const Place q = place(P, false);
+    const int64_t line = q.sample * P.v + q.v0;
+    far_sums<XF, ZF, ACT>(far_of(P, q.sample), Run{line * P.px + q.ch, P.apart * P.px, line * P.pdz + q.ch, P.apart * P.pdz, 0, 0, q.count},
+                          far_channels(P, q.ch, stats_of(P, q)), q.ch, sa, sb);
+}
+template <bool XF, bool ZF, int ACT> __device__ __noinline__ void apply_far(const GnParams &P, const float2 *means, int g0)
+{
+    const Place q = place(P, true);
+    const int64_t line = q.sample * P.v + q.v0;
+    far_apply<XF, ZF, ACT>(far_of(P, q.sample), Run{line * P.px + q.ch, P.apart * P.px, line * P.pdz + q.ch, P.apart * P.pdz, line * P.po + q.ch, P.apart * P.po, q.count},
+                           q.ch, means, g0);
+}
+
 template <bool XF, bool ZF, int ACT>
 __global__ void __launch_bounds__(GT, resident(XF, true))
-gn_bwd_sums_kernel(const GnParams P)
+gn_bwd_sums_kernel(const __grid_constant__ GnParams P)
 {
     extern __shared__ __align__(16) double sm[];                // the rings, then the sums over the lines
     constexpr int D = depth(XF, true);
@@ -300,7 +316,9 @@ gn_bwd_sums_kernel(const GnParams P)
     double a[8], b[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) a[j] = b[j] = 0.0;
+    bool far = false;
     if (mine > 0) {
+        far = far_channels(P, q.ch, stats_of(P, q)) != 0;
         const Affine f = affine(P, q.ch, stats_of(P, q));
         f32x2 s1[4], s2[4];
 #pragma unroll
@@ -327,7 +345,9 @@ gn_bwd_sums_kernel(const GnParams P)
     }
     landed<0>();
     __syncthreads();                                            // the rings make room
-    const Totals tot = sum_lines(P.ty, P.uc, q.ty, q.unit, a, b, sm, [](double *, double *) {});
+    const Totals tot = sum_lines(P.ty, P.uc, q.ty, q.unit, a, b, sm, [&](double *sa, double *sb) {
+        if (far) sums_far<XF, ZF, ACT>(P, sa, sb);
+    });
     const int cc = P.uc * 8, c0 = blockIdx.y * cc;
     double2 *out = P.part + (q.sample * P.parts + q.part) * P.c + c0;
     for (int i = threadIdx.x; i < cc && c0 + i < P.c; i += GT) out[i] = make_double2(tot.a(i), tot.b(i));
@@ -365,7 +385,7 @@ gn_bwd_parts_kernel(const GnParams P)
 // dx, and dw and db from the sums of all samples
 template <bool XF, bool ZF, int ACT>
 __global__ void __launch_bounds__(GT, resident(XF, true))
-gn_bwd_apply_kernel(const GnParams P)
+gn_bwd_apply_kernel(const __grid_constant__ GnParams P)
 {
     extern __shared__ __align__(16) double sm[];                // the rings, then of this chunk's groups (mean(w dt), mean(w dt xhat))
     constexpr int D = depth(XF, true);
@@ -413,6 +433,11 @@ gn_bwd_apply_kernel(const GnParams P)
         }
     }
     if (mine == 0) return;
+    if (far_channels(P, q.ch, stats_of(P, q))) {
+        landed<0>();
+        apply_far<XF, ZF, ACT>(P, means, g0);
+        return;
+    }
     const Affine f = affine(P, q.ch, stats_of(P, q));
     const Back k = back_terms(P, q.ch, stats_of(P, q), [&](int g) { return means[g - g0]; });
     stream<D>(mine, start, [&](int slot) { return Both<XF, ZF>{rx.get(slot), rz.get(slot)}; },

@@ -182,7 +182,71 @@ __device__ __forceinline__ void back_apply(const GnParams &P, const Affine &f, c
     for (int j = 0; j < 4; ++j) unpack2(fma2(dt[j], f.a[j], fma2(d[j], k.e[j], k.h[j])), o[2 * j], o[2 * j + 1]);
 }
 
+
 template <bool XF> __device__ __forceinline__ float value_at(const void *p, int64_t i) { return XF ? ((const float *)p)[i] : bf2f(((const bf16 *)p)[i]); }
+
+// The channels of a thread, one bit each, whose rstd is so far from 1 that dt (x - mean) and rstd^2 may leave fp32's range while dt and dx do not (inside,
+// they hold for gradients down to 1e-23).  Their values go through the two functions below, which divide by the deviation first, in fp64;
+// the kernels reach them by calls that find their own places, so that they cost the usual values next to no registers.
+template <typename F> __device__ __forceinline__ uint32_t far_channels(const GnParams &P, int ch, F mr)
+{
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float r = mr(group_of(P, ch + j)).y;
+        m |= r < 5.9604645e-8f || r > 16777216.f ? 1u << j : 0u;
+    }
+    return m;
+}
+// where a thread's values lie: the first of x, of dz and of dx, elements between two, how many
+struct Run { int64_t x, xs, z, zs, o, os; int count; };
+// what the functions need of the layer: mean and rstd of the sample's groups, channels of a group
+struct Far { const void *x, *dz; void *out; const float *w, *b; const float2 *mr; int cg; float slope; };
+__device__ __forceinline__ Far far_of(const GnParams &P, int64_t sample) { return Far{P.x, P.dz, P.out, P.w, P.b, P.mean_rstd + sample * P.groups, P.cg, P.slope}; }
+// dt, and x in deviations from the mean; t as the forward pass forms it
+template <bool XF, bool ZF, int ACT> __device__ __forceinline__ float far_slope(const Far &f, float2 mr, float w, float b, int64_t x, int64_t z, double &xhat)
+{
+    const float v = value_at<XF>(f.x, x), dz = value_at<ZF>(f.dz, z), t = fmaf(v - mr.x, mr.y * w, b);
+    xhat = ((double)v - mr.x) * mr.y;
+    float dt, same;
+    unpack2(times_derivative<ACT>(twice(dz), twice(t), f.slope), dt, same);
+    return dt;
+}
+// Sums of dt and dt * xhat of the channels of `mask`, to where the thread's sums lie in shared memory.
+template <bool XF, bool ZF, int ACT> __device__ __forceinline__ void far_sums(const Far &f, const Run &r, uint32_t mask, int ch, double *sa, double *sb)
+{
+    for (; mask; mask &= mask - 1) {
+        const int j = __ffs(mask) - 1;
+        const float2 mr = f.mr[(ch + j) / f.cg];
+        const float w = f.w ? f.w[ch + j] : 1.f, b = f.b ? f.b[ch + j] : 0.f;
+        double s = 0.0, t = 0.0;
+#pragma unroll 1
+        for (int i = 0; i < r.count; ++i) {
+            double xhat;
+            const double dt = far_slope<XF, ZF, ACT>(f, mr, w, b, r.x + i * r.xs + j, r.z + i * r.zs + j, xhat);
+            s += dt;
+            t = fma(dt, xhat, t);
+        }
+        sa[j] = s; sb[j] = t;
+    }
+}
+// dx of all 8 channels; means: (mean(w dt), mean(w dt xhat)) of the groups from g0 on.  An element is read before it is written: dx may be x or dz.
+template <bool XF, bool ZF, int ACT> __device__ __forceinline__ void far_apply(const Far &f, const Run &r, int ch, const float2 *means, int g0)
+{
+#pragma unroll 1
+    for (int j = 0; j < 8; ++j) {
+        const int g = (ch + j) / f.cg;
+        const float2 mr = f.mr[g], m = means[g - g0];
+        const float w = f.w ? f.w[ch + j] : 1.f, b = f.b ? f.b[ch + j] : 0.f;
+#pragma unroll 1
+        for (int i = 0; i < r.count; ++i) {
+            double xhat;
+            const double dt = far_slope<XF, ZF, ACT>(f, mr, w, b, r.x + i * r.xs + j, r.z + i * r.zs + j, xhat);
+            const float o = (float)(mr.y * (w * dt - m.x - xhat * m.y));
+            if (XF) ((float *)f.out)[r.o + i * r.os + j] = o; else ((bf16 *)f.out)[r.o + i * r.os + j] = f2bf(o);
+        }
+    }
+}
 
 // A thread's sums of d and d^2 about k (nk = -k) as fp64 sums about r
 __device__ __forceinline__ void about(float nk, float s1, float s2, int n, double r, double &a, double &b)

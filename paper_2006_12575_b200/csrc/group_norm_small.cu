@@ -15,6 +15,9 @@ namespace {
 using namespace gn;
 
 constexpr int MAX_CC = 512, MAX_GROUPS = GT, MAX_CL = 8;
+// Units per thread: a few where that is enough, else as many as 64 registers of values hold.
+constexpr int few(bool back) { return back ? 2 : 4; }
+constexpr int most(bool xf, bool back) { return (xf ? 8 : 16) / (back ? 2 : 1); }
 
 struct SmallParams : GnParams {
     int32_t cc, cl;                           // channels of a cluster, CTAs of a cluster
@@ -166,9 +169,27 @@ gn_small_kernel(const SmallParams P)
     }
 }
 
+// The calls for channels whose rstd is far from 1
+__device__ __forceinline__ Run run_of(const SmallParams &P, const Spot &q)
+{
+    const int64_t line = q.sample * P.v + q.v0;
+    return Run{line * P.px + q.ch, P.ty * P.px, line * P.pdz + q.ch, P.ty * P.pdz, line * P.po + q.ch, P.ty * P.po, q.have};
+}
+template <bool XF, bool ZF, int ACT> __device__ __noinline__ void sums_far(const SmallParams &P, double *sa, double *sb)
+{
+    const Spot q = spot(P);
+    const Far f = far_of(P, q.sample);
+    far_sums<XF, ZF, ACT>(f, run_of(P, q), far_channels(P, q.ch, [&](int g) { return f.mr[g]; }), q.ch, sa, sb);
+}
+template <bool XF, bool ZF, int ACT> __device__ __noinline__ void apply_far(const SmallParams &P, const float2 *means, int g0)
+{
+    const Spot q = spot(P);
+    far_apply<XF, ZF, ACT>(far_of(P, q.sample), run_of(P, q), q.ch, means, g0);
+}
+
 template <bool XF, bool ZF, int ACT, int U>
-__global__ void __launch_bounds__(GT)
-gn_small_bwd_kernel(const SmallParams P)
+__global__ void __launch_bounds__(GT, U == few(true) ? 2 : 1)         // 2 x 512 x 512 fp32 with 150 registers: a second wave, 12.5 us for 9
+gn_small_bwd_kernel(const __grid_constant__ SmallParams P)
 {
     extern __shared__ __align__(16) double sm[];
     __shared__ double gs[MAX_GROUPS], gt[MAX_GROUPS];
@@ -190,7 +211,9 @@ gn_small_bwd_kernel(const SmallParams P)
     double a[8], b[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) a[j] = b[j] = 0.0;
+    bool far = false;
     if (q.have) {
+        far = far_channels(P, q.ch, [&](int g) { return mr[g]; }) != 0;
         f = affine(P, q.ch, [&](int g) { return mr[g]; });
         f32x2 s1[4] = {0, 0, 0, 0}, s2[4] = {0, 0, 0, 0};
 #pragma unroll
@@ -215,7 +238,9 @@ gn_small_bwd_kernel(const SmallParams P)
     }
     // The cluster exchanges the groups' sums, which every CTA needs; of the channels' sums each CTA adds a slice.  (All of them in every CTA: 32 x 64 x 512
     // channels took 21.7 us.)
-    const Totals tot = sum_lines(P.ty, P.uc, q.line, q.unit, a, b, sm, [](double *, double *) {});
+    const Totals tot = sum_lines(P.ty, P.uc, q.line, q.unit, a, b, sm, [&](double *sa, double *sb) {
+        if (far) sums_far<XF, ZF, ACT>(P, sa, sb);
+    });
     sum_groups(g0, g1, P.cg,
                [&](int g, int l, int lanes, double &s, double &t) {
                    for (int ch = g * P.cg + l; ch < (g + 1) * P.cg; ch += lanes) {
@@ -248,7 +273,8 @@ gn_small_bwd_kernel(const SmallParams P)
     }
     __syncthreads();
     if (P.cl > 1) cluster_arrive();                              // this CTA has read its peers' sums; waited for at the end
-    if (q.have) {
+    if (far) apply_far<XF, ZF, ACT>(P, means, g0);
+    else if (q.have) {
         const Back k = back_terms(P, q.ch, [&](int g) { return mr[g]; }, [&](int g) { return means[g - g0]; });
         const int64_t ol = P.ty * P.po, to = (q.sample * P.v + q.v0) * P.po + q.ch;
 #pragma unroll
@@ -279,10 +305,6 @@ gn_small_params_kernel(const double2 *chan, int n, int c, float *dw, float *db)
     if (lane == 0 && db) db[ch] = (float)s;
     if (lane == 0 && dw) dw[ch] = (float)t;
 }
-
-// Units per thread: a few where that is enough, else as many as 64 registers of values hold.
-constexpr int few(bool back) { return back ? 2 : 4; }
-constexpr int most(bool xf, bool back) { return (xf ? 8 : 16) / (back ? 2 : 1); }
 
 struct Plan { int cc, cl, u; };
 bool plan(const GnParams &P, bool xf, bool back, Plan &out)
