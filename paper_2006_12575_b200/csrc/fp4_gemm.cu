@@ -220,7 +220,7 @@ fp4_gemm_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constant
         const int q = warp & 3, half = (warp - 2) >> 2;                    // lane quarter and column part of this warp
         float *stage = out_stage + (warp - 2) * L::STAGE_WORDS;
         const int lane_row = q * 32 + lane;
-        const float alpha = (P.ga ? __ldg(P.ga) : 1.f) * (P.gb ? __ldg(P.gb) : 1.f);
+        const Alpha alpha = alpha_of(P.ga ? __ldg(P.ga) : 1.f, P.gb ? __ldg(P.gb) : 1.f);
         uint32_t acc = 0, acc_phase = 0;
         for (int64_t tile = tile0; tile < P.tiles && ok; tile += tile_step) {
             ok = __all_sync(0xffffffffu, mbar_wait(tfull0 + 8 * acc, acc_phase, abort_flag));
@@ -269,7 +269,11 @@ fp4_gemm_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constant
                 }
                 float v[16];
 #pragma unroll
-                for (int j = 0; j < 16; ++j) v[j] = __uint_as_float(r[c & 1][j]) * alpha;
+                for (int j = 0; j < 16; j += 2) {
+                    uint32_t x = r[c & 1][j], y = r[c & 1][j + 1];
+                    mul_twice(x, y, twice(alpha.first), twice(alpha.rest));
+                    v[j] = __uint_as_float(x); v[j + 1] = __uint_as_float(y);
+                }
                 if (S == 1) finish<ODD, 16>(P, row, cbase + c * 16, v, stage);
                 else {
                     // every stage of this CTA has been read: its memory takes the parts, [column][lane row]
@@ -454,7 +458,7 @@ fp4_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
         const uint32_t box_stage = smem_u32(out_stage) + (warp - 4) * 4096;        // 1024-byte boundaries, as the swizzle wants
         uint32_t acc = 0, acc_phase = 0;
         const uint32_t tempty_leader = map_to_rank(tempty0, 0);
-        const float alpha = (P.ga ? __ldg(P.ga) : 1.f) * (P.gb ? __ldg(P.gb) : 1.f);
+        const Alpha alpha = alpha_of(P.ga ? __ldg(P.ga) : 1.f, P.gb ? __ldg(P.gb) : 1.f);
         for (int64_t tile = tile0; tile < P.tiles && ok; tile += tile_step) {
             ok = __all_sync(0xffffffffu, mbar_wait(tfull0 + 8 * acc, acc_phase, abort_flag));
             if (!ok) break;

@@ -225,13 +225,32 @@ __device__ __forceinline__ void store_box_odd(const OutParams &P, const uint32_t
     }
     __syncwarp();
 }
-// alpha * (16 * N accumulator columns) + bias, and the words of 128 bytes of a row from them
-template <int N> __device__ __forceinline__ void scale_bias(const OutParams &P, uint32_t (&r)[N][16], float alpha, int col0)
+// ga gb of two tensors' scales as factors to be applied in turn.  Their product alone (rest = 1) where it is well inside fp32's range, else
+// the one nearer to 1 first: what lies between is then never further from 1 than the result or the sum is, so nothing is lost or infinite that the result is not.
+struct Alpha { float first, rest; };
+__device__ __forceinline__ Alpha alpha_of(float ga, float gb)
 {
+    const float both = ga * gb, low = fminf(ga, gb), high = fmaxf(ga, gb);
+    if (both >= 7.8886091e-31f && both <= 1.2676506e30f) return {both, 1.f};               // 2^-100 .. 2^100
+    if (both < 1.f) return {high, low};
+    return {low, high};
+}
+// both factors, two values per instruction: as many instructions as one factor took a value at a time, and no branch
+__device__ __forceinline__ void mul_twice(uint32_t &x, uint32_t &y, f32x2 first, f32x2 rest)
+{
+    float u, v;
+    unpack2(mul2(mul2(pack2(x, y), first), rest), u, v);
+    x = __float_as_uint(u);
+    y = __float_as_uint(v);
+}
+// alpha * (16 * N accumulator columns) + bias, and the words of 128 bytes of a row from them
+template <int N> __device__ __forceinline__ void scale_bias(const OutParams &P, uint32_t (&r)[N][16], Alpha a, int col0)
+{
+    const f32x2 first = twice(a.first), rest = twice(a.rest);
 #pragma unroll
     for (int c = 0; c < N; ++c)
 #pragma unroll
-        for (int j = 0; j < 16; ++j) r[c][j] = __float_as_uint(__uint_as_float(r[c][j]) * alpha);
+        for (int j = 0; j < 16; j += 2) mul_twice(r[c][j], r[c][j + 1], first, rest);
     if (!P.bias) return;
     const int last = P.rows_c - 1;
 #pragma unroll
