@@ -40,9 +40,9 @@ __device__ __forceinline__ int group_of(const GnParams &P, int ch) { return (int
 
 // ----------------------------------------------------------------------------------------------------------- activations
 // Two values at a time: the packed fp32 instructions halve what is issued, which with a SiLU or GELU bounds these kernels as much as memory does.
-// FINE: fp32 outputs of the forward pass, with expf and erfcf.  Elsewhere e^x without the correction for the rounding of x log2(e) (2^-24 |x| of e^x),
-// and the normal distribution by Abramowitz & Stegun 7.1.26: q(u) = (a1 s + .. + a5 s^5) e^(-u^2), s = 1 / (1 + p u), for erfc(u), u >= 0, off by at
-// most 1.5e-7.  A derivative is a factor of size one, so both are within a few units of 2^-24 of it.
+// FINE: fp32 outputs; forward with expf and erfcf, backward with the two functions below that say so.  Elsewhere e^x without the correction for the rounding
+// of x log2(e) (2^-24 |x| of e^x), and the normal distribution by Abramowitz & Stegun 7.1.26: q(u) = (a1 s + .. + a5 s^5) e^(-u^2), s = 1 / (1 + p u), for
+// erfc(u), u >= 0, off by at most 1.5e-7 of one: both less than half a step of a bf16 gradient of ordinary size.
 __device__ __forceinline__ float ex2(float x)
 {
     float e;
@@ -71,6 +71,43 @@ __device__ __forceinline__ void normal_2(f32x2 t, f32x2 &below, f32x2 &density)
     unpack2(fma2(q, twice(-1.f), twice(1.f)), u0, u1);
     below = pair(a > 0.f ? u0 : q0, b > 0.f ? u1 : q1);
 }
+// The same to a few units of 2^-24 of their own size.  An exponent is formed with its rounding error (by fma, which gives a product's remainder exactly, and
+// the rest of the constant); that error, a small number, goes into 2^x as the factor 1 + ln(2) error.
+__device__ __forceinline__ f32x2 sigmoid_fine_2(f32x2 t)
+{
+    float a, b;
+    unpack2(t, a, b);
+    const f32x2 u = pair(fminf(a, 127.f), fminf(b, 127.f));      // beyond, e^-t is 0 and the error would not stay small
+    const f32x2 hi = mul2(u, twice(-1.4426950216293335f));
+    const f32x2 over = fma2(u, twice(1.9259629911266175e-08f), fma2(u, twice(1.4426950216293335f), hi));         // hi - (-u log2 e)
+    return rcp_2(fma2(ex2_2(hi), fma2(over, twice(-0.69314718f), twice(1.f)), twice(1.f)));
+}
+// e^(t^2 / 2) P(X <= -|t|) as a polynomial in s = 1 / (1 + p |t|) without its constant term: degree and p chosen, coefficients fitted for the least relative
+// error, over |t| <= 14 (2.0e-8; 2.8e-7 in fp32).
+__device__ __forceinline__ void normal_fine_2(f32x2 t, f32x2 &below, f32x2 &density)
+{
+    float a, b;
+    unpack2(t, a, b);
+    const f32x2 u = pair(fminf(fabsf(a), 20.f), fminf(fabsf(b), 20.f));          // beyond, both are 0
+    const f32x2 m = mul2(u, twice(-0.7213475108146667f)), n = mul2(u, twice(0.7213475108146667f)), hi = mul2(u, m);
+    // hi - (-u^2 log2(e) / 2): the product's remainder, and u times m's
+    const f32x2 over = fma2(fma2(u, twice(9.629814955633087e-09f), fma2(u, twice(0.7213475108146667f), m)), u, fma2(u, n, hi));
+    density = mul2(ex2_2(hi), fma2(over, twice(-0.69314718f), twice(1.f)));
+    const f32x2 s = rcp_2(fma2(u, twice(0.345f), twice(1.f)));
+    f32x2 q = fma2(s, twice(-0.028381966f), twice(0.145282f));
+    q = fma2(s, q, twice(-0.27117312f));
+    q = fma2(s, q, twice(0.187196702f));
+    q = fma2(s, q, twice(-0.0376016721f));
+    q = fma2(s, q, twice(0.11179959f));
+    q = fma2(s, q, twice(0.117238291f));
+    q = fma2(s, q, twice(0.138020888f));
+    q = fma2(s, q, twice(0.137619287f));
+    q = mul2(mul2(q, s), density);
+    float q0, q1, u0, u1;
+    unpack2(q, q0, q1);
+    unpack2(fma2(q, twice(-1.f), twice(1.f)), u0, u1);
+    below = pair(a > 0.f ? u0 : q0, b > 0.f ? u1 : q1);
+}
 template <int ACT, bool FINE> __device__ __forceinline__ f32x2 activate(f32x2 t, float slope)
 {
     if constexpr (ACT == LAMP_ACT_NONE) return t;
@@ -86,8 +123,8 @@ template <int ACT, bool FINE> __device__ __forceinline__ f32x2 activate(f32x2 t,
     normal_2(t, below, density);
     return mul2(t, below);
 }
-// v * act'(t)
-template <int ACT> __device__ __forceinline__ f32x2 times_derivative(f32x2 v, f32x2 t, float slope)
+// v * act'(t); FINE: fp32 gradients
+template <int ACT, bool FINE> __device__ __forceinline__ f32x2 times_derivative(f32x2 v, f32x2 t, float slope)
 {
     if constexpr (ACT == LAMP_ACT_NONE) return v;
     if constexpr (ACT == LAMP_ACT_LEAKY_RELU) {
@@ -98,11 +135,12 @@ template <int ACT> __device__ __forceinline__ f32x2 times_derivative(f32x2 v, f3
     }
     if constexpr (ACT == LAMP_ACT_SILU) {
         // s (1 + t (1 - s)) = s + y - y s with y = t s
-        const f32x2 s = sigmoid_2(t), y = mul2(t, s);
+        const f32x2 s = FINE ? sigmoid_fine_2(t) : sigmoid_2(t), y = mul2(t, s);
         return mul2(v, add2(fma2(mul2(y, twice(-1.f)), s, y), s));
     }
     f32x2 below, density;
-    normal_2(t, below, density);
+    if (FINE) normal_fine_2(t, below, density);
+    else normal_2(t, below, density);
     return mul2(v, fma2(mul2(t, twice(0.3989422804014327f)), density, below));
 }
 
@@ -138,7 +176,7 @@ __device__ __forceinline__ void slopes(const GnParams &P, const Affine &f, const
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         d[j] = add2(d[j], f.nm[j]);
-        dt[j] = times_derivative<ACT>(dt[j], fma2(d[j], f.a[j], f.b[j]), P.slope);
+        dt[j] = times_derivative<ACT, XF>(dt[j], fma2(d[j], f.a[j], f.b[j]), P.slope);
     }
 }
 
@@ -209,7 +247,7 @@ template <bool XF, bool ZF, int ACT> __device__ __forceinline__ float far_slope(
     const float v = value_at<XF>(f.x, x), dz = value_at<ZF>(f.dz, z), t = fmaf(v - mr.x, mr.y * w, b);
     xhat = ((double)v - mr.x) * mr.y;
     float dt, same;
-    unpack2(times_derivative<ACT>(twice(dz), twice(t), f.slope), dt, same);
+    unpack2(times_derivative<ACT, XF>(twice(dz), twice(t), f.slope), dt, same);
     return dt;
 }
 // Sums of dt and dt * xhat of the channels of `mask`, to where the thread's sums lie in shared memory.
