@@ -490,13 +490,13 @@ bool fuse(const GnParams &P)
     return groups <= FUSE_GROUPS && groups * sums <= FUSE_SUMS;
 }
 
-size_t workspace(int64_t v, int n, int c)
+size_t workspace(int64_t v, int n, int c, int groups)
 {
-    // the larger of the forward pass' [n][groups][parts][chunks] and the backward pass' [n][parts + 1][c], groups = c at most
+    // the larger of the forward pass' [n][groups][parts][chunks] and the backward pass' [n][parts + 1][c]
     GnParams P = {};
     P.v = v; P.n = n; P.c = c;
-    split(P, resident(false, false));
-    const size_t fwd = (size_t)n * c * P.parts * P.chunks + ((size_t)n * c + 1) / 2;        // and the groups' first values
+    split(P, resident(false, false));                          // bf16 has the more parts
+    const size_t fwd = (size_t)n * groups * P.parts * P.chunks + ((size_t)n * groups + 1) / 2;        // and the groups' first values
     split(P, resident(false, true));
     const size_t bwd = (size_t)n * c * (P.parts + 1);
     return (fwd > bwd ? fwd : bwd) * sizeof(double2);
@@ -602,7 +602,7 @@ lamp_status_t by_type(GnParams &P, bool xf, bool zf, bool back, cudaStream_t st)
 
 lamp_status_t check_scratch(const GnParams &P, const void *ws, size_t ws_bytes)
 {
-    return !ws || ((uintptr_t)ws & 15) || ws_bytes < workspace(P.v, P.n, P.c) ? LAMP_ERR_WORKSPACE : LAMP_OK;
+    return !ws || ((uintptr_t)ws & 15) || ws_bytes < workspace(P.v, P.n, P.c, P.groups) ? LAMP_ERR_WORKSPACE : LAMP_OK;
 }
 
 }  // namespace
@@ -614,7 +614,7 @@ using namespace lamp;
 extern "C" size_t lamp_group_norm_workspace_bytes(const lamp_group_norm_t *p, const lamp_tensor_t *x)
 {
     if (!x || check_same(x, x) != LAMP_OK || check_params(p, x) != LAMP_OK) return 0;
-    return voxels(x) == 0 ? 0 : workspace((int64_t)x->d * x->h * x->w, x->n, x->c);
+    return voxels(x) == 0 ? 0 : workspace((int64_t)x->d * x->h * x->w, x->n, x->c, p->groups);
 }
 
 extern "C" lamp_status_t lamp_group_norm_act_fwd(const lamp_group_norm_t *p, const lamp_tensor_t *x, const double *stats, lamp_tensor_t *z,
