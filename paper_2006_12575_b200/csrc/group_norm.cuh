@@ -82,27 +82,27 @@ __device__ __forceinline__ f32x2 sigmoid_fine_2(f32x2 t)
     const f32x2 over = fma2(u, twice(1.9259629911266175e-08f), fma2(u, twice(1.4426950216293335f), hi));         // hi - (-u log2 e)
     return rcp_2(fma2(ex2_2(hi), fma2(over, twice(-0.69314718f), twice(1.f)), twice(1.f)));
 }
-// e^(t^2 / 2) P(X <= -|t|) as a polynomial in s = 1 / (1 + p |t|) without its constant term: degree and p chosen, coefficients fitted for the least relative
-// error, over |t| <= 14 (2.0e-8; 2.8e-7 in fp32).
+// e^(t^2 / 2) P(X <= -|t|) as a polynomial in s = 1 / (1 + p |t|): degree and p chosen, coefficients fitted for the least relative error, over |t| <= 14
+// (3.7e-8; 3.4e-7 in fp32).  81,840 x 320 fp32 backward with GELU takes 91 us, with the two functions above 88, 10^6 x 64 205 and 196.
 __device__ __forceinline__ void normal_fine_2(f32x2 t, f32x2 &below, f32x2 &density)
 {
     float a, b;
     unpack2(t, a, b);
-    const f32x2 u = pair(fminf(fabsf(a), 20.f), fminf(fabsf(b), 20.f));          // beyond, both are 0
-    const f32x2 m = mul2(u, twice(-0.7213475108146667f)), n = mul2(u, twice(0.7213475108146667f)), hi = mul2(u, m);
+    const f32x2 u = pair(fminf(fabsf(a), 20.f), fminf(fabsf(b), 20.f)), nu = pair(fmaxf(-fabsf(a), -20.f), fmaxf(-fabsf(b), -20.f));      // beyond, both are 0
+    const f32x2 m = mul2(nu, twice(0.7213475108146667f)), hi = mul2(u, m);
     // hi - (-u^2 log2(e) / 2): the product's remainder, and u times m's
-    const f32x2 over = fma2(fma2(u, twice(9.629814955633087e-09f), fma2(u, twice(0.7213475108146667f), m)), u, fma2(u, n, hi));
+    const f32x2 over = fma2(fma2(u, twice(9.629814955633087e-09f), fma2(u, twice(0.7213475108146667f), m)), u, fma2(nu, m, hi));
     density = mul2(ex2_2(hi), fma2(over, twice(-0.69314718f), twice(1.f)));
-    const f32x2 s = rcp_2(fma2(u, twice(0.345f), twice(1.f)));
-    f32x2 q = fma2(s, twice(-0.028381966f), twice(0.145282f));
-    q = fma2(s, q, twice(-0.27117312f));
-    q = fma2(s, q, twice(0.187196702f));
-    q = fma2(s, q, twice(-0.0376016721f));
-    q = fma2(s, q, twice(0.11179959f));
-    q = fma2(s, q, twice(0.117238291f));
-    q = fma2(s, q, twice(0.138020888f));
-    q = fma2(s, q, twice(0.137619287f));
-    q = mul2(mul2(q, s), density);
+    const f32x2 s = rcp_2(fma2(u, twice(0.295f), twice(1.f)));
+    f32x2 q = fma2(s, twice(0.0394211486f), twice(-0.183406189f));
+    q = fma2(s, q, twice(0.271016657f));
+    q = fma2(s, q, twice(-0.117071159f));
+    q = fma2(s, q, twice(0.166289002f));
+    q = fma2(s, q, twice(0.0847447962f));
+    q = fma2(s, q, twice(0.121699385f));
+    q = fma2(s, q, twice(0.117289335f));
+    q = fma2(s, q, twice(1.70069379e-05f));
+    q = mul2(q, density);
     float q0, q1, u0, u1;
     unpack2(q, q0, q1);
     unpack2(fma2(q, twice(-1.f), twice(1.f)), u0, u1);

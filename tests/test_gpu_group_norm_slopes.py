@@ -2,8 +2,8 @@
 
 With mean 0, rstd 1, no w and b, t is x; with dz 1 at one voxel and 0 elsewhere, db is the derivative at that voxel's t.
 Tolerances, u = 2^-24: an exponential 7 u (the instruction's 4, its argument's and its factor's rounding), 1 + e^-t one, a reciprocal 2, so sigmoid s 10 u and y = t s
-11 u: s + y - y s is within 24 u (s + |y| + |y s|).  The normal distribution P and its density p: e^(-t^2 / 2) 8 u, the polynomial 7 u (2.8e-7 in fp32
-arithmetic and the reciprocal), their product and 1 - P one each: P + t p is within 24 u (P + |t| p).  Below 2^-126 the instructions flush to 0."""
+11 u: s + y - y s is within 24 u (s + |y| + |y s|).  The normal distribution P and its density p: e^(-t^2 / 2) 8 u, the polynomial 8 u (3.4e-7 in fp32
+arithmetic, and the reciprocal), their product and 1 - P one each: P + t p is within 24 u (P + |t| p).  Below 2^-126 the instructions flush to 0."""
 import math
 
 import numpy as np
