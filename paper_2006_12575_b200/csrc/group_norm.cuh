@@ -40,7 +40,7 @@ __device__ __forceinline__ int group_of(const GnParams &P, int ch) { return (int
 
 // ----------------------------------------------------------------------------------------------------------- activations
 // Two values at a time: the packed fp32 instructions halve what is issued, which with a SiLU or GELU bounds these kernels as much as memory does.
-// FINE: fp32 outputs; forward with expf and erfcf, backward with the two functions below that say so.  Elsewhere e^x without the correction for the rounding
+// FINE: fp32 outputs; forward with expf and erfcf, backward with the two functions below whose names say so.  Elsewhere e^x without the correction for the rounding
 // of x log2(e) (2^-24 |x| of e^x), and the normal distribution by Abramowitz & Stegun 7.1.26: q(u) = (a1 s + .. + a5 s^5) e^(-u^2), s = 1 / (1 + p u), for
 // erfc(u), u >= 0, off by at most 1.5e-7 of one: both less than half a step of a bf16 gradient of ordinary size.
 __device__ __forceinline__ float ex2(float x)
@@ -82,9 +82,10 @@ __device__ __forceinline__ f32x2 sigmoid_fine_2(f32x2 t)
     const f32x2 over = fma2(u, twice(1.9259629911266175e-08f), fma2(u, twice(1.4426950216293335f), hi));         // hi - (-u log2 e)
     return rcp_2(fma2(ex2_2(hi), fma2(over, twice(-0.69314718f), twice(1.f)), twice(1.f)));
 }
-// e^(t^2 / 2) P(X <= -|t|) as a polynomial in s = 1 / (1 + p |t|): degree and p chosen, coefficients fitted for the least relative error, over |t| <= 14
-// (3.7e-8; 3.4e-7 in fp32).  81,840 x 320 fp32 backward with GELU takes 91 us, with the two functions above 88, 10^6 x 64 205 and 196.
-__device__ __forceinline__ void normal_fine_2(f32x2 t, f32x2 &below, f32x2 &density)
+// GELU' = P(X <= t) + t p(t) = h(t) for t <= 0, 1 - h(-t) for t > 0, with h(-u) = e^(-u^2 / 2) (R(u) - u / sqrt(2 pi)), R(u) = e^(u^2 / 2) P(X <= -u).  R as a
+// polynomial in s = 1 / (1 + p u): degree and p chosen, coefficients fitted for the least relative error, over u <= 14 (3.7e-8; 3.4e-7 in fp32).
+// 81,840 x 320 fp32 backward takes 91 us so and 88 by normal_2, 10^6 x 64 202 and 196.
+__device__ __forceinline__ f32x2 gelu_slope_fine_2(f32x2 t)
 {
     float a, b;
     unpack2(t, a, b);
@@ -92,7 +93,7 @@ __device__ __forceinline__ void normal_fine_2(f32x2 t, f32x2 &below, f32x2 &dens
     const f32x2 m = mul2(nu, twice(0.7213475108146667f)), hi = mul2(u, m);
     // hi - (-u^2 log2(e) / 2): the product's remainder, and u times m's
     const f32x2 over = fma2(fma2(u, twice(9.629814955633087e-09f), fma2(u, twice(0.7213475108146667f), m)), u, fma2(nu, m, hi));
-    density = mul2(ex2_2(hi), fma2(over, twice(-0.69314718f), twice(1.f)));
+    const f32x2 density = mul2(ex2_2(hi), fma2(over, twice(-0.69314718f), twice(1.f)));
     const f32x2 s = rcp_2(fma2(u, twice(0.295f), twice(1.f)));
     f32x2 q = fma2(s, twice(0.0394211486f), twice(-0.183406189f));
     q = fma2(s, q, twice(0.271016657f));
@@ -102,11 +103,11 @@ __device__ __forceinline__ void normal_fine_2(f32x2 t, f32x2 &below, f32x2 &dens
     q = fma2(s, q, twice(0.121699385f));
     q = fma2(s, q, twice(0.117289335f));
     q = fma2(s, q, twice(1.70069379e-05f));
-    q = mul2(q, density);
-    float q0, q1, u0, u1;
-    unpack2(q, q0, q1);
-    unpack2(fma2(q, twice(-1.f), twice(1.f)), u0, u1);
-    below = pair(a > 0.f ? u0 : q0, b > 0.f ? u1 : q1);
+    const f32x2 h = mul2(fma2(u, twice(-0.3989422804014327f), q), density);
+    float h0, h1, r0, r1;
+    unpack2(h, h0, h1);
+    unpack2(fma2(h, twice(-1.f), twice(1.f)), r0, r1);
+    return pair(a > 0.f ? r0 : a <= 0.f ? h0 : a, b > 0.f ? r1 : b <= 0.f ? h1 : b);                   // NaN stays
 }
 template <int ACT, bool FINE> __device__ __forceinline__ f32x2 activate(f32x2 t, float slope)
 {
@@ -138,9 +139,9 @@ template <int ACT, bool FINE> __device__ __forceinline__ f32x2 times_derivative(
         const f32x2 s = FINE ? sigmoid_fine_2(t) : sigmoid_2(t), y = mul2(t, s);
         return mul2(v, add2(fma2(mul2(y, twice(-1.f)), s, y), s));
     }
+    if (FINE) return mul2(v, gelu_slope_fine_2(t));
     f32x2 below, density;
-    if (FINE) normal_fine_2(t, below, density);
-    else normal_2(t, below, density);
+    normal_2(t, below, density);
     return mul2(v, fma2(mul2(t, twice(0.3989422804014327f)), density, below));
 }
 

@@ -47,3 +47,17 @@ def test_slopes_keep_their_digits(name, reach, voxels, zt):
         a, m = np.abs(v.reshape(-1, 8)), mag.reshape(-1, 8)
         tol = 32 * U * (m + m.mean(1, keepdims=True) + a * (m * a).mean(1, keepdims=True)).reshape(-1) + 2.0 ** -120
         assert (np.abs(dx.view(-1).double().cpu().numpy() - want) <= tol).all()
+
+
+@pytest.mark.parametrize("name", ["silu", "gelu"])
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+def test_slopes_far_out(name, dt):
+    """0 below and 1 above, however far t is."""
+    t = torch.tensor([-3e38, -1e30, -1e10, -1e3, 1e3, 1e10, 1e30, 3e38], device="cuda")
+    x = t.to(dt).view(1, 1, 1, 1, 8)
+    mr = torch.tensor([0.0, 1.0], device="cuda").repeat(1, 8, 1).contiguous()
+    p = B.group_norm(8, None, None, name)
+    ws = torch.empty(B.lamp_group_norm_workspace_bytes(p, x), dtype=torch.uint8, device="cuda")
+    db = torch.empty(8, device="cuda")
+    B.lamp_group_norm_act_bwd(p, torch.ones_like(x), x, mr, torch.empty_like(x), None, db, ws)
+    assert (db == torch.tensor([0.0] * 4 + [1.0] * 4, device="cuda")).all(), db
