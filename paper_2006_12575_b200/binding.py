@@ -767,7 +767,10 @@ class GradList:
 
 
 def grad_list(tensors, outs=None) -> GradList:
-    """tensors: gradients (bf16 or fp32, contiguous); outs: where lamp_grad_clip writes, None for in place."""
+    """tensors: gradients (bf16 or fp32, contiguous); outs: where lamp_grad_clip writes, None for in place.
+
+    Made once for buffers that stay from step to step: the checks and the search for overlaps run on the host, about 2 us a tensor (0.13 ms for 62,
+    0.5 ms for 301), and the list holds the memory it was made of.  Gradients that are freed and made anew need a new list every step."""
     tensors = list(tensors)
     outs = tensors if outs is None else list(outs)
     if len(outs) != len(tensors):
