@@ -231,7 +231,7 @@ struct Alpha { float first, rest; };
 __device__ __forceinline__ Alpha alpha_of(float ga, float gb)
 {
     const float both = ga * gb, low = fminf(ga, gb), high = fmaxf(ga, gb);
-    if (both >= 7.8886091e-31f && both <= 1.2676506e30f) return {both, 1.f};               // 2^-100 .. 2^100
+    if (!(both < 7.8886091e-31f) && !(both > 1.2676506e30f)) return {both, 1.f};           // 2^-100 .. 2^100, and NaN
     if (both < 1.f) return {high, low};
     return {low, high};
 }

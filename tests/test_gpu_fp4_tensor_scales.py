@@ -49,3 +49,13 @@ def test_product_of_scales_outside_of_fp32(ga, gb, low, high, m, n, k):
         bad = ~(np.abs(got - ref) <= tol)
         assert not bad.any(), (bad.sum(), np.argwhere(bad)[:4], got[bad][:4], ref[bad][:4])
         assert (got[m // 2] == 0).all() and (got[:, n // 2] == 0).all()
+
+
+@pytest.mark.parametrize("ga,gb", [(float("nan"), 1.0), (1e-25, float("nan")), (float("nan"), 1e30)])
+@pytest.mark.parametrize("m,n,k", SHAPES[:4])
+def test_a_scale_that_is_nan_stays(ga, gb, m, n, k):
+    r = np.random.default_rng(m)
+    oa, ob = operand(r, m, k, 0x18, 0x30, ga)[0], operand(r, n, k, 0x18, 0x30, gb)[0]
+    y = torch.zeros(1, 1, 1, m, n, device="cuda")
+    B.lamp_gemm_fp4(oa, ob, y)
+    assert y.isnan().all()
