@@ -283,12 +283,12 @@ gn_apply_kernel(const GnParams P)
 template <bool XF, bool ZF> struct Both { Raw<XF> x; Raw<ZF> z; };
 
 // The calls for channels whose rstd is far from 1
-template <bool XF, bool ZF, int ACT> __device__ __noinline__ void sums_far(const GnParams &P, double *sa, double *sb)
+template <bool XF, bool ZF, int ACT> __device__ __noinline__ void sums_far(const GnParams &P, uint32_t far, double *sa, double *sb)
 {
     const Place q = place(P, false);
     const int64_t line = q.sample * P.v + q.v0;
     far_sums<XF, ZF, ACT>(far_of(P, q.sample), Run{line * P.px + q.ch, P.apart * P.px, line * P.pdz + q.ch, P.apart * P.pdz, 0, 0, q.count},
-                          far_channels(P, q.ch, stats_of(P, q)), q.ch, sa, sb);
+                          far, q.ch, sa, sb);
 }
 template <bool XF, bool ZF, int ACT> __device__ __noinline__ void apply_far(const GnParams &P, const float2 *means, int g0)
 {
@@ -316,9 +316,8 @@ gn_bwd_sums_kernel(const __grid_constant__ GnParams P)
     double a[8], b[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) a[j] = b[j] = 0.0;
-    bool far = false;
+    uint32_t far = 0;                                           // channels whose sums left fp32
     if (mine > 0) {
-        far = far_channels(P, q.ch, stats_of(P, q)) != 0;
         const Affine f = affine(P, q.ch, stats_of(P, q));
         f32x2 s1[4], s2[4];
 #pragma unroll
@@ -340,13 +339,14 @@ gn_bwd_sums_kernel(const __grid_constant__ GnParams P)
                 const float rstd = P.mean_rstd[q.sample * P.groups + group_of(P, q.ch + 2 * j + i)].y;
                 a[2 * j + i] = f1[i];
                 b[2 * j + i] = (double)f2[i] * rstd;
+                far |= sum_is_far(rstd, f2[i]) ? 1u << (2 * j + i) : 0u;
             }
         }
     }
     landed<0>();
     __syncthreads();                                            // the rings make room
     const Totals tot = sum_lines(P.ty, P.uc, q.ty, q.unit, a, b, sm, [&](double *sa, double *sb) {
-        if (far) sums_far<XF, ZF, ACT>(P, sa, sb);
+        if (far) sums_far<XF, ZF, ACT>(P, far, sa, sb);
     });
     const int cc = P.uc * 8, c0 = blockIdx.y * cc;
     double2 *out = P.part + (q.sample * P.parts + q.part) * P.c + c0;
@@ -433,7 +433,7 @@ gn_bwd_apply_kernel(const __grid_constant__ GnParams P)
         }
     }
     if (mine == 0) return;
-    if (far_channels(P, q.ch, stats_of(P, q))) {
+    if (terms_are_far(P, q.ch, stats_of(P, q), [&](int g) { return means[g - g0]; })) {
         landed<0>();
         apply_far<XF, ZF, ACT>(P, means, g0);
         return;

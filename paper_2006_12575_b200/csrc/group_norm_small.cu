@@ -175,11 +175,10 @@ __device__ __forceinline__ Run run_of(const SmallParams &P, const Spot &q)
     const int64_t line = q.sample * P.v + q.v0;
     return Run{line * P.px + q.ch, P.ty * P.px, line * P.pdz + q.ch, P.ty * P.pdz, line * P.po + q.ch, P.ty * P.po, q.have};
 }
-template <bool XF, bool ZF, int ACT> __device__ __noinline__ void sums_far(const SmallParams &P, double *sa, double *sb)
+template <bool XF, bool ZF, int ACT> __device__ __noinline__ void sums_far(const SmallParams &P, uint32_t far, double *sa, double *sb)
 {
     const Spot q = spot(P);
-    const Far f = far_of(P, q.sample);
-    far_sums<XF, ZF, ACT>(f, run_of(P, q), far_channels(P, q.ch, [&](int g) { return f.mr[g]; }), q.ch, sa, sb);
+    far_sums<XF, ZF, ACT>(far_of(P, q.sample), run_of(P, q), far, q.ch, sa, sb);
 }
 template <bool XF, bool ZF, int ACT> __device__ __noinline__ void apply_far(const SmallParams &P, const float2 *means, int g0)
 {
@@ -211,9 +210,8 @@ gn_small_bwd_kernel(const __grid_constant__ SmallParams P)
     double a[8], b[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) a[j] = b[j] = 0.0;
-    bool far = false;
+    uint32_t far = 0;                                           // channels whose sums left fp32
     if (q.have) {
-        far = far_channels(P, q.ch, [&](int g) { return mr[g]; }) != 0;
         f = affine(P, q.ch, [&](int g) { return mr[g]; });
         f32x2 s1[4] = {0, 0, 0, 0}, s2[4] = {0, 0, 0, 0};
 #pragma unroll
@@ -232,14 +230,16 @@ gn_small_bwd_kernel(const __grid_constant__ SmallParams P)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 a[2 * j + i] = f1[i];
-                b[2 * j + i] = (double)f2[i] * mr[group_of(P, q.ch + 2 * j + i)].y;
+                const float rstd = mr[group_of(P, q.ch + 2 * j + i)].y;
+                b[2 * j + i] = (double)f2[i] * rstd;
+                far |= sum_is_far(rstd, f2[i]) ? 1u << (2 * j + i) : 0u;
             }
         }
     }
     // The cluster exchanges the groups' sums, which every CTA needs; of the channels' sums each CTA adds a slice.  (All of them in every CTA: 32 x 64 x 512
     // channels took 21.7 us.)
     const Totals tot = sum_lines(P.ty, P.uc, q.line, q.unit, a, b, sm, [&](double *sa, double *sb) {
-        if (far) sums_far<XF, ZF, ACT>(P, sa, sb);
+        if (far) sums_far<XF, ZF, ACT>(P, far, sa, sb);
     });
     sum_groups(g0, g1, P.cg,
                [&](int g, int l, int lanes, double &s, double &t) {
@@ -273,9 +273,10 @@ gn_small_bwd_kernel(const __grid_constant__ SmallParams P)
     }
     __syncthreads();
     if (P.cl > 1) cluster_arrive();                              // this CTA has read its peers' sums; waited for at the end
-    if (far) apply_far<XF, ZF, ACT>(P, means, g0);
+    const auto means_of = [&](int g) { return means[g - g0]; };
+    if (q.have && terms_are_far(P, q.ch, [&](int g) { return mr[g]; }, means_of)) apply_far<XF, ZF, ACT>(P, means, g0);
     else if (q.have) {
-        const Back k = back_terms(P, q.ch, [&](int g) { return mr[g]; }, [&](int g) { return means[g - g0]; });
+        const Back k = back_terms(P, q.ch, [&](int g) { return mr[g]; }, means_of);
         const int64_t ol = P.ty * P.po, to = (q.sample * P.v + q.v0) * P.po + q.ch;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
