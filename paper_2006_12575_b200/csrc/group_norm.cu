@@ -433,13 +433,14 @@ gn_bwd_apply_kernel(const __grid_constant__ GnParams P)
         }
     }
     if (mine == 0) return;
-    if (terms_are_far(P, q.ch, stats_of(P, q), [&](int g) { return means[g - g0]; })) {
+    const auto means_of = [&](int g) { return means[g - g0]; };
+    const Affine f = affine(P, q.ch, stats_of(P, q));
+    const Back k = back_terms(P, q.ch, stats_of(P, q), means_of);
+    if (terms_are_far(P, q.ch, k, stats_of(P, q), means_of)) {
         landed<0>();
         apply_far<XF, ZF, ACT>(P, means, g0);
         return;
     }
-    const Affine f = affine(P, q.ch, stats_of(P, q));
-    const Back k = back_terms(P, q.ch, stats_of(P, q), [&](int g) { return means[g - g0]; });
     stream<D>(mine, start, [&](int slot) { return Both<XF, ZF>{rx.get(slot), rz.get(slot)}; },
               [&](int i, const Both<XF, ZF> &r) {
                   float o[8];

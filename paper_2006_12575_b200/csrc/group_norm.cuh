@@ -231,10 +231,20 @@ __device__ __forceinline__ bool sum_is_far(float rstd, float s2)
 {
     return rstd > 16777216.f || (rstd < 5.9604645e-8f && !(fabsf(s2) <= 3.4028235e38f));         // squares or products of small values vanish; of large ones overflow
 }
-template <typename F, typename G> __device__ __forceinline__ bool terms_are_far(const GnParams &P, int ch, F mr, G means)
+// k: the terms as they came out.  Ordinary ones take a look at the smallest and the largest.
+template <typename F, typename G> __device__ __forceinline__ bool terms_are_far(const GnParams &P, int ch, const Back &k, F mr, G means)
 {
-    bool far = false;
+    float low = 3.4028235e38f, high = 0.f;
 #pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        float a, b;
+        unpack2(k.e[j], a, b);
+        low = fminf(low, fminf(fabsf(a), fabsf(b)));
+        high = fmaxf(high, fmaxf(fabsf(a), fabsf(b)));
+    }
+    if (low >= 1.1754944e-38f && high <= 3.4028235e38f) return false;
+    bool far = false;
+#pragma unroll 1
     for (int j = 0; j < 8; ++j) {
         const int g = group_of(P, ch + j);
         const float rstd = mr(g).y, m = means(g).y, e = fabsf(rstd * (rstd * m));

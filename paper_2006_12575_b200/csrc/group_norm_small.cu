@@ -273,17 +273,20 @@ gn_small_bwd_kernel(const __grid_constant__ SmallParams P)
     }
     __syncthreads();
     if (P.cl > 1) cluster_arrive();                              // this CTA has read its peers' sums; waited for at the end
-    const auto means_of = [&](int g) { return means[g - g0]; };
-    if (q.have && terms_are_far(P, q.ch, [&](int g) { return mr[g]; }, means_of)) apply_far<XF, ZF, ACT>(P, means, g0);
-    else if (q.have) {
-        const Back k = back_terms(P, q.ch, [&](int g) { return mr[g]; }, means_of);
-        const int64_t ol = P.ty * P.po, to = (q.sample * P.v + q.v0) * P.po + q.ch;
+    if (q.have) {
+        const auto mr_of = [&](int g) { return mr[g]; };
+        const auto means_of = [&](int g) { return means[g - g0]; };
+        const Back k = back_terms(P, q.ch, mr_of, means_of);
+        if (terms_are_far(P, q.ch, k, mr_of, means_of)) apply_far<XF, ZF, ACT>(P, means, g0);
+        else {
+            const int64_t ol = P.ty * P.po, to = (q.sample * P.v + q.v0) * P.po + q.ch;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (u >= q.have) break;
-            float o[8];
-            back_apply<XF, ZF, ACT>(P, f, k, rx[u], rz[u], o);
-            store8_whole<XF>(P.out, to + u * ol, o);
+            for (int u = 0; u < U; ++u) {
+                if (u >= q.have) break;
+                float o[8];
+                back_apply<XF, ZF, ACT>(P, f, k, rx[u], rz[u], o);
+                store8_whole<XF>(P.out, to + u * ol, o);
+            }
         }
     }
     if (P.cl > 1) cluster_wait();                                // no CTA leaves while a peer still reads its sums
