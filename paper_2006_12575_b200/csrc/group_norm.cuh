@@ -71,8 +71,8 @@ __device__ __forceinline__ void normal_2(f32x2 t, f32x2 &below, f32x2 &density)
     unpack2(fma2(q, twice(-1.f), twice(1.f)), u0, u1);
     below = pair(a > 0.f ? u0 : q0, b > 0.f ? u1 : q1);
 }
-// The same to a few units of 2^-24 of their own size.  An exponent is formed with its rounding error (by fma, which gives a product's remainder exactly, and
-// the rest of the constant); that error, a small number, goes into 2^x as the factor 1 + ln(2) error.
+// The sigmoid to a few units of 2^-24 of its own size.  The exponent is formed with its rounding error (by fma, which gives a product's remainder exactly,
+// and the rest of the constant); that error, a small number, goes into 2^x as the factor 1 + ln(2) error.
 __device__ __forceinline__ f32x2 sigmoid_fine_2(f32x2 t)
 {
     float a, b;
@@ -83,17 +83,14 @@ __device__ __forceinline__ f32x2 sigmoid_fine_2(f32x2 t)
     return rcp_2(fma2(ex2_2(hi), fma2(over, twice(-0.69314718f), twice(1.f)), twice(1.f)));
 }
 // GELU' = P(X <= t) + t p(t) = h(t) for t <= 0, 1 - h(-t) for t > 0, with h(-u) = e^(-u^2 / 2) (R(u) - u / sqrt(2 pi)), R(u) = e^(u^2 / 2) P(X <= -u).  R as a
-// polynomial in s = 1 / (1 + p u): degree and p chosen, coefficients fitted for the least relative error, over u <= 14 (3.7e-8; 3.4e-7 in fp32).
-// 81,840 x 320 fp32 backward takes 91 us so and 88 by normal_2, 10^6 x 64 202 and 196.
+// polynomial in s = 1 / (1 + p u): degree and p chosen, coefficients fitted for the least relative error, over u <= 14 (3.7e-8; 3.4e-7 in fp32).  The
+// exponential is off by 2^-24 t^2 of itself, at most 2^-24 of one: carrying its exponent's rounding as above took 91 us on 81,840 x 320 fp32 backward, so
+// it takes 89, by normal_2 87.
 __device__ __forceinline__ f32x2 gelu_slope_fine_2(f32x2 t)
 {
     float a, b;
     unpack2(t, a, b);
-    const f32x2 u = pair(fminf(fabsf(a), 20.f), fminf(fabsf(b), 20.f)), nu = pair(fmaxf(-fabsf(a), -20.f), fmaxf(-fabsf(b), -20.f));      // beyond, both are 0
-    const f32x2 m = mul2(nu, twice(0.7213475108146667f)), hi = mul2(u, m);
-    // hi - (-u^2 log2(e) / 2): the product's remainder, and u times m's
-    const f32x2 over = fma2(fma2(u, twice(9.629814955633087e-09f), fma2(u, twice(0.7213475108146667f), m)), u, fma2(nu, m, hi));
-    const f32x2 density = mul2(ex2_2(hi), fma2(over, twice(-0.69314718f), twice(1.f)));
+    const f32x2 u = pair(fabsf(a), fabsf(b)), density = ex2_2(mul2(t, mul2(t, twice(-0.72134752044448170f))));
     const f32x2 s = rcp_2(fma2(u, twice(0.295f), twice(1.f)));
     f32x2 q = fma2(s, twice(0.0394211486f), twice(-0.183406189f));
     q = fma2(s, q, twice(0.271016657f));
