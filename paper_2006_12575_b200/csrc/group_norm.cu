@@ -101,9 +101,16 @@ template <int D, typename S, typename T, typename W> __device__ __forceinline__ 
 }
 
 // ----------------------------------------------------------------------------------------------------------- forward
+template <bool XF> __device__ __noinline__ void sums_exact(const GnParams &P, uint32_t again, double *sa, double *sb)
+{
+    const Place q = place(P, false);
+    const int64_t base = q.sample * P.v;
+    sums_again<XF>(P, again, (base + q.v0) * P.px + q.ch, P.apart * P.px, q.count, base * P.px, q.ch, sa, sb);
+}
+
 template <bool XF>
 __global__ void __launch_bounds__(GT, resident(XF, false))
-gn_sums_kernel(const GnParams P)
+gn_sums_kernel(const __grid_constant__ GnParams P)
 {
     extern __shared__ __align__(16) double sm[];                // the rings, then the sums over the lines
     constexpr int D = depth(XF, false);
@@ -169,7 +176,7 @@ gn_sums_kernel(const GnParams P)
         }
     }
     const Totals tot = sum_lines(P.ty, P.uc, q.ty, q.unit, a, b, sm, [&](double *sa, double *sb) {
-        if (again) sums_again<XF>(P.x, P.cg, again, x0, step, mine, base * P.px, q.ch, sa, sb);
+        if (again) sums_exact<XF>(P, again, sa, sb);
     });
     const int cc = P.uc * 8, c0 = blockIdx.y * cc, c1 = min(P.c, c0 + cc);
     sum_groups(c0 / P.cg, (c1 - 1) / P.cg, P.cg,

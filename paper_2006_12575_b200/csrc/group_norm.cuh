@@ -310,17 +310,17 @@ __device__ __forceinline__ void about(float nk, float s1, float s2, int n, doubl
 // 256 halves of fp32's smallest step that squares may have lost.
 __device__ __forceinline__ bool squares_hold(float s2, float eps) { return s2 <= 3.4028235e38f && (s2 >= 7.8886091e-31f || eps >= 7.8886091e-31f); }      // 2^-100
 // The same sums about the group's first value, in fp64 from the values themselves, for the channels of `mask` where they may not: `count` voxels, `step`
-// elements apart, the first at `at`; first: the sample's first voxel.  To where the thread's sums lie in shared memory, so that nothing is held in registers
-// for it.
-template <bool XF> __device__ __noinline__ void sums_again(const void *x, int cg, uint32_t mask, int64_t at, int64_t step, int count, int64_t first, int ch, double *sa, double *sb)
+// elements apart, the first at `at`; first: the sample's first voxel.  To where the thread's sums lie in shared memory.  The kernels reach it by calls
+// that find their own places, as those for deviations far from 1 below.
+template <bool XF> __device__ __forceinline__ void sums_again(const GnParams &P, uint32_t mask, int64_t at, int64_t step, int count, int64_t first, int ch, double *sa, double *sb)
 {
     for (; mask; mask &= mask - 1) {
         const int j = __ffs(mask) - 1;
-        const double r = value_at<XF>(x, first + (ch + j) / cg * cg);
+        const double r = value_at<XF>(P.x, first + group_of(P, ch + j) * P.cg);
         double s = 0.0, t = 0.0;
 #pragma unroll 1
         for (int i = 0; i < count; ++i) {
-            const double d = (double)value_at<XF>(x, at + i * step + j) - r;
+            const double d = (double)value_at<XF>(P.x, at + i * step + j) - r;
             s += d;
             t = fma(d, d, t);
         }

@@ -74,9 +74,15 @@ __device__ __forceinline__ Spot spot(const SmallParams &P)
     return q;
 }
 
+template <bool XF> __device__ __noinline__ void sums_exact(const SmallParams &P, uint32_t again, double *sa, double *sb)
+{
+    const Spot q = spot(P);
+    sums_again<XF>(P, again, (q.sample * P.v + q.v0) * P.px + q.ch, P.ty * P.px, q.have, q.sample * P.v * P.px, q.ch, sa, sb);
+}
+
 template <bool XF, bool ZF, int ACT, int U>
 __global__ void __launch_bounds__(GT)
-gn_small_kernel(const SmallParams P)
+gn_small_kernel(const __grid_constant__ SmallParams P)
 {
     extern __shared__ __align__(16) double sm[];
     __shared__ double gs[MAX_GROUPS], gt[MAX_GROUPS];
@@ -138,7 +144,7 @@ gn_small_kernel(const SmallParams P)
         }
     }
     const Totals tot = sum_lines(P.ty, P.uc, q.line, q.unit, a, b, sm, [&](double *sa, double *sb) {
-        if (again) sums_again<XF>(P.x, P.cg, again, at, line, q.have, q.sample * P.v * P.px, q.ch, sa, sb);
+        if (again) sums_exact<XF>(P, again, sa, sb);
     });
     sum_groups(g0, g1, P.cg,
                [&](int g, int l, int lanes, double &s, double &t) {
