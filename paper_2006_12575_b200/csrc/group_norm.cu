@@ -7,7 +7,7 @@
 // everything per channel stays in registers; a CTA holds TY voxels of one sample side by side and takes every parts-th TY of them.
 // Each thread copies its values asynchronously into a ring of its own in shared memory, D units ahead of the one it works on (nobody else reads
 // them, so no barrier): as many bytes in flight as with registers, all the time, and the first are on their way while the constants are
-// formed.  With U units loaded into registers, worked on, and the next ones loaded, 128^3 x 32 bf16 backward took 129 us (now 115), 81,840 x 320
+// formed.  With U units loaded into registers, worked on, and the next ones loaded, 128^3 x 32 bf16 backward took 129 us (now 114), 81,840 x 320
 // fp32 101 (87, with a GELU that keeps its digits 89); 128^3 x 64 bf16 forward takes the same either way.
 // Sums: a thread adds d = x - k and d^2 of at most RUN voxels in fp32, k the mean of the first values it loads - without it the squares of
 // data far from 0 lose the variance; where the squares leave fp32's range the thread adds its values again in fp64.  Between threads, CTAs and channels of a group the sums are fp64, taken about r, the group's first

@@ -223,7 +223,7 @@ template <bool XF> __device__ __forceinline__ float value_at(const void *p, int6
 
 // Deviations far from 1 (outside of 2^-24 .. 2^24): where dt (x - mean), or rstd^2 times the mean of w dt xhat, leaves fp32's range while dw and dx do not, the
 // values go through the two functions below, which divide by the deviation first, in fp64.  The kernels reach them by calls that find their own places, so
-// that they cost the usual values next to no registers.  (128^3 x 32 bf16 with a deviation of 1e25: 760 us for 115.)
+// that they cost the usual values next to no registers.  (128^3 x 32 bf16 with a deviation of 1e25: 355 us for 114.)
 __device__ __forceinline__ bool sum_is_far(float rstd, float s2)
 {
     return rstd > 16777216.f || (rstd < 5.9604645e-8f && !(fabsf(s2) <= 3.4028235e38f));         // squares or products of small values vanish; of large ones overflow
@@ -311,7 +311,7 @@ __device__ __forceinline__ void about(float nk, float s1, float s2, int n, doubl
 __device__ __forceinline__ bool squares_hold(float s2, float eps) { return s2 <= 3.4028235e38f && (s2 >= 7.8886091e-31f || eps >= 7.8886091e-31f); }      // 2^-100
 // The same sums about the group's first value, in fp64 from the values themselves, for the channels of `mask` where they may not: `count` voxels, `step`
 // elements apart, the first at `at`; first: the sample's first voxel.  To where the thread's sums lie in shared memory.  The kernels reach it by calls
-// that find their own places, as those for deviations far from 1 below.
+// that find their own places, as those for deviations far from 1 above.
 template <bool XF> __device__ __forceinline__ void sums_again(const GnParams &P, uint32_t mask, int64_t at, int64_t step, int count, int64_t first, int ch, double *sa, double *sb)
 {
     for (; mask; mask &= mask - 1) {
